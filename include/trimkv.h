@@ -341,6 +341,93 @@ TRIMKV_API trimkv_status trimkv_select_topk(const float* scores, int64_t n, int6
 TRIMKV_API trimkv_status trimkv_select_topk_static(const float* scores, int64_t n, int64_t k_keep, uint64_t* keep_bits,
                                         int32_t* status_out, void* stream);
 
+/* ---- a paged cache that is not evicted, owned by the caller -----------------------------------------
+ * A handle's sequences advance in lock step under a budget.  These calls serve the other kind of cache a program keeps
+ * beside it -- layers or requests that stay dense, the full cache that the method is compared with (Sec. 5) -- for requests
+ * of different lengths.  (No counterpart in the paper.)  They take no handle and allocate nothing: every buffer is the
+ * caller's device memory.
+ *   pages        k_pages, v_pages [n_pages, kv_heads, 64, head_dim]: entry e of a request lies in row e % 64 of page
+ *                block_table[request][e / 64]. 
+ *   key_bounds   [n_pages, kv_heads, 2, head_dim]: the channelwise smallest and largest key of each FULL page, kept by
+ *                trimkv_paged_append, read by trimkv_paged_sparse_attention.  May be NULL where neither is needed.
+ *   block_table  int32 [n_req, table_width] physical pages; entries behind a request's last page are not read.
+ *   lens         int32 [n_req] entries of each request, the call's new tokens included.
+ *   cu_new       int32 [n_req + 1], ascending from 0: request r's new tokens are rows cu_new[r] .. cu_new[r + 1] - 1 of k, v,
+ *                q and out, and stand at positions lens[r] - n .. lens[r] - 1 (n of them).  Rows behind cu_new[n_req] are
+ *                padding: neither read nor written.
+ *   status       device int32, may be NULL: latched (written only while 0) with what a kernel finds wrong: E_ARG for
+ *                lengths, offsets, slots or pages out of range (a request with bad lengths or offsets is skipped, a bad
+ *                page or slot too), E_NOMEM where the plan finds too few free pages, E_TIMEOUT where a bounded wait gave up.
+ * Lengths and tables live on the device, so a captured graph serves every step.  Two calls that may overlap on the GPU
+ * need workspaces (and outputs) of their own; contents of a workspace are ignored and may be overwritten after the call.
+ * At most TRIMKV_PAGED_MAX_REQ requests, 64 x TRIMKV_PAGED_MAX_WIDTH entries per request. */
+#define TRIMKV_PAGED_MAX_REQ 8192
+#define TRIMKV_PAGED_MAX_WIDTH 16384
+#define TRIMKV_PAGED_MAX_PAGES (1 << 24)
+
+typedef struct trimkv_paged_cache {
+    void* k_pages;       /* 16-byte aligned, as are the next two */
+    void* v_pages;
+    void* key_bounds;    /* or NULL */
+    int32_t n_pages;
+    int32_t kv_heads;
+    int32_t head_dim;    /* a multiple of 8, at most 256 */
+    int32_t kv_dtype;    /* TRIMKV_DTYPE_BF16 or TRIMKV_DTYPE_F32: pages, bounds, k, v, q and out */
+    int32_t page_size;   /* must be 64 */
+    int32_t reserved;    /* must be 0 */
+} trimkv_paged_cache;
+
+/* Block tables and slot maps from request lengths.  Request r owns the first ceil(old_lens[r] / 64) entries of its table
+ * row; after the call it owns ceil(new_lens[r] / 64).  Its first keep_lens[r] entries stay (keep_lens = NULL: the smaller of
+ * old and new), its new tokens are positions keep_lens[r] .. new_lens[r] - 1: old = 0 starts a request, new = 0 ends one,
+ * keep < old takes rejected drafts back before the next ones.  0 <= keep <= min(old, new) <= 64 x table_width.
+ * free_pages: int32 [n_pages], a stack of free pages of which the first *free_count are live.  Pages given back are pushed in
+ * (request, page) order, then the missing ones are popped in (request, page) order; memory above the top is left as it is.
+ * Table entries behind a request's last page are left as they are.
+ * Written: block_table, free_pages, free_count_out [1], lens_out [n_req] (= new_lens), cu_new [n_req + 1], and for each of
+ * the max_tokens places slot_map (page x 64 + row) and positions (may be NULL), -1 behind the last token.  free_count_out may
+ * be free_count, lens_out any of the length arrays.
+ * If a length is wrong, there are more than max_tokens new tokens (E_ARG) or too few free pages (E_NOMEM), nothing changes
+ * hands: lens_out = old_lens, cu_new = 0, slot_map = positions = -1, so the calls that follow do nothing. */
+TRIMKV_API trimkv_status trimkv_paged_plan(int32_t n_req, const int32_t* old_lens, const int32_t* keep_lens, const int32_t* new_lens,
+                                int32_t* block_table, int32_t table_width, int32_t* free_pages, int32_t n_pages,
+                                const int32_t* free_count, int32_t* free_count_out, int64_t max_tokens, int32_t* lens_out,
+                                int32_t* cu_new, int32_t* slot_map, int32_t* positions, int32_t* status, void* stream);
+
+/* Writes k and v (rows of [kv_heads, head_dim], k_stride and v_stride elements apart) of token t to slot slot_map[t]; -1
+ * skips a token.  A page whose last row (slot % 64 = 63) is written gets its key_bounds from its 64 keys; a NaN key makes
+ * its channel's bounds NaN.  The tokens that this call puts into one page are consecutive rows in slot order, as
+ * trimkv_paged_plan lays them out, and no slot is given twice. */
+TRIMKV_API trimkv_status trimkv_paged_append(const trimkv_paged_cache* cache, int64_t n_tokens, const void* k, int64_t k_stride,
+                                  const void* v, int64_t v_stride, const int32_t* slot_map, int32_t* status, void* stream);
+
+/* Scratch of the two attention calls, in bytes; 0 for a head layout they refuse. */
+TRIMKV_API size_t trimkv_paged_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+
+/* Causal attention of the new tokens (one per request: a decode step; a few: drafted tokens; many: a prompt chunk; mixed
+ * freely): the token at position p attends to entries max(0, p - window + 1) .. p of its request (window = 0: 0 .. p), query
+ * head j reads KV head j / (q_heads / kv_heads), weights softmax(scale q . k).  A token that sees no entry (p < 0) gets
+ * zeros.  q: rows of [q_heads, head_dim], q_stride elements apart; out [n_tokens, q_heads, head_dim].  max_new: the most new
+ * tokens of one request as far as the host knows; it only guides the choice of kernels (0: not known).
+ * Rows of a page behind a request's last entry may hold anything, also NaN.  A NaN or infinity in an entry of the request
+ * itself may reach every token that the same call computes for it.  workspace: at least trimkv_paged_workspace_bytes, 256-byte aligned. */
+TRIMKV_API trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t max_new,
+                                     int32_t q_heads, const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
+                                     const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,
+                                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* The same attention restricted, for every token and KV head, to top_pages of the pages up to its own: the first sink_pages,
+ * the newest recent_pages (>= 1: the token's own page is among them) and, for the places left, the pages of the largest
+ *     U(page) = max over the query heads of the group of sum_c max(q_c lo_c, q_c hi_c)        (lo, hi: key_bounds)
+ * -- no key of the page has a larger q . k --, ties to the lower page, NaN first.  U is summed in 64 bits.  A token with at
+ * most top_pages pages reads them all.  sink_pages + recent_pages <= top_pages.  selected: int32 [n_tokens, kv_heads,
+ * top_pages], the pages read (places in the block-table row), ascending, -1 behind the last. */
+TRIMKV_API trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t q_heads,
+                                            const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
+                                            const int32_t* block_table, int32_t table_width, float scale, int32_t top_pages,
+                                            int32_t sink_pages, int32_t recent_pages, int32_t* selected, void* out, void* workspace,
+                                            size_t workspace_bytes, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,8 @@ EXPORTS = [
     "trimkv_select_topk", "trimkv_select_topk_static", "trimkv_set_test_hooks",
     "trimkv_step_stream", "trimkv_check_invariants", "trimkv_import_pool", "trimkv_import_finish", "trimkv_shard_sample_cap", "trimkv_shard_sample", "trimkv_shard_bracket", "trimkv_shard_filter", "trimkv_shard_candidates",
     "trimkv_shard_resolve", "trimkv_shard_hist", "trimkv_shard_digit", "trimkv_shard_mark", "trimkv_shard_compact",
+    "trimkv_paged_plan", "trimkv_paged_append", "trimkv_paged_workspace_bytes", "trimkv_paged_attention",
+    "trimkv_paged_sparse_attention",
 ]
 
 
@@ -45,6 +47,15 @@ class Config(C.Structure):
         ("max_chunk", C.c_int32), ("reserved", C.c_int32), ("max_pool_pages", C.c_int64),
         ("retention_bias", C.c_int32), ("per_pool_budget", C.c_int32),
         ("shard_total_layers", C.c_int32), ("shard_layer0", C.c_int32),
+    ]
+
+
+class PagedCache(C.Structure):
+    """trimkv_paged_cache: the page arrays of a caller-owned cache."""
+    _fields_ = [
+        ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("key_bounds", C.c_void_p), ("n_pages", C.c_int32),
+        ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32), ("page_size", C.c_int32),
+        ("reserved", C.c_int32),
     ]
 
 
@@ -116,6 +127,14 @@ def lib() -> C.CDLL:
     L.trimkv_select_workspace_bytes.restype = C.c_size_t
     L.trimkv_select_topk.argtypes = [vp, i64, i64, vp, vp, C.c_size_t, vp, vp]
     L.trimkv_select_topk_static.argtypes = [vp, i64, i64, vp, vp, vp]
+    pc, sz = C.POINTER(PagedCache), C.c_size_t
+    L.trimkv_paged_plan.argtypes = [i32, vp, vp, vp, vp, i32, vp, i32, vp, vp, i64, vp, vp, vp, vp, vp, vp]
+    L.trimkv_paged_append.argtypes = [pc, i64, vp, i64, vp, i64, vp, vp, vp]
+    L.trimkv_paged_workspace_bytes.argtypes = [i32, i32, i32]
+    L.trimkv_paged_workspace_bytes.restype = sz
+    L.trimkv_paged_attention.argtypes = [pc, i32, i64, i32, i32, vp, i64, vp, vp, vp, i32, f32, i32, vp, vp, sz, vp, vp]
+    L.trimkv_paged_sparse_attention.argtypes = [pc, i32, i64, i32, vp, i64, vp, vp, vp, i32, f32, i32, i32, i32, vp, vp, vp,
+                                                sz, vp, vp]
     for name in ("trimkv_create_ex", "trimkv_reset", "trimkv_set_gate", "trimkv_set_shared_projection", "trimkv_gate",
                  "trimkv_append", "trimkv_score_and_evict", "trimkv_decode_attention", "trimkv_decode_step_all",
                  "trimkv_get_lengths", "trimkv_get_kept", "trimkv_get_pool", "trimkv_get_select_stats",
@@ -384,3 +403,148 @@ def select_topk_static(scores: torch.Tensor, k_keep: int, keep_bits: torch.Tenso
     _check(lib().trimkv_select_topk_static(_ptr(scores, torch.float32), n, k_keep, _ptr(keep_bits), _ptr(status),
                                            _stream()))
     return keep_bits, status
+
+
+# ---- the caller-owned paged cache (trimkv_paged_*): see include/trimkv.h for the layouts
+PAGE_SIZE = 64
+_KV_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
+def _on(device, name: str, t: torch.Tensor, dtype, *shape) -> int:
+    """Address of a contiguous tensor of this device, type and shape (None: any extent)."""
+    if t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    got = t.shape
+    if len(got) != len(shape) or any(w is not None and w != n for w, n in zip(shape, got)):
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(got)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    return t.data_ptr()
+
+
+def _rows(device, name: str, t: torch.Tensor, dtype, heads: int, d: int):
+    """(address, elements between tokens) of a [tokens, heads, d] tensor whose rows [heads, d] are contiguous."""
+    if t.device != device or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype} on {device}, got {t.dtype} on {t.device}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name}: expected shape (tokens, {heads}, {d}), got {tuple(t.shape)}")
+    step, sh, sd = t.stride()
+    if t.shape[0] and ((d > 1 and sd != 1) or (heads > 1 and sh != d)):
+        raise ValueError(f"{name}: the {heads} x {d} values of a token must be contiguous")
+    return t.data_ptr(), (step if t.shape[0] > 1 else heads * d)
+
+
+def _paged_cache(k_pages, v_pages, key_bounds):
+    if not k_pages.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if k_pages.dim() != 4 or k_pages.dtype not in _KV_DTYPES:
+        raise ValueError("k_pages: expected bf16 or fp32 [n_pages, kv_heads, 64, head_dim]")
+    dev, dt = k_pages.device, k_pages.dtype
+    n, h, page, d = k_pages.shape
+    return PagedCache(_on(dev, "k_pages", k_pages, dt, n, h, page, d), _on(dev, "v_pages", v_pages, dt, n, h, page, d),
+                      None if key_bounds is None else _on(dev, "key_bounds", key_bounds, dt, n, h, 2, d),
+                      n, h, d, _KV_DTYPES[dt], page, 0)
+
+
+class _Launch:
+    """Makes the tensors' device current for a call (the library launches on the current device)."""
+
+    def __init__(self, device):
+        self.index = device.index if device.index is not None else torch.cuda.current_device()
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def paged_plan(old_lens, keep_lens, new_lens, block_table, free_pages, free_count, free_count_out, lens_out, cu_new, slot_map,
+               positions=None, status=None):
+    """Block tables and slot maps from request lengths (trimkv_paged_plan).  int32 tensors: old_lens, keep_lens (or None),
+    new_lens, lens_out [R], block_table [R, W], free_pages [n_pages], free_count and free_count_out [1], cu_new [R + 1],
+    slot_map and positions (or None) [max_tokens], status [1].  Works in place; returns nothing."""
+    dev, i = old_lens.device, torch.int32
+    if dev.type != "cuda":
+        raise ValueError("expected a CUDA tensor")
+    r, w, m = old_lens.shape[0] if old_lens.dim() == 1 else -1, block_table.shape[-1], slot_map.numel()
+    args = (r, _on(dev, "old_lens", old_lens, i, r), None if keep_lens is None else _on(dev, "keep_lens", keep_lens, i, r),
+            _on(dev, "new_lens", new_lens, i, r), _on(dev, "block_table", block_table, i, r, w), w,
+            _on(dev, "free_pages", free_pages, i, None), free_pages.numel(), _on(dev, "free_count", free_count, i, 1),
+            _on(dev, "free_count_out", free_count_out, i, 1), m, _on(dev, "lens_out", lens_out, i, r),
+            _on(dev, "cu_new", cu_new, i, r + 1), _on(dev, "slot_map", slot_map, i, m),
+            None if positions is None else _on(dev, "positions", positions, i, m),
+            None if status is None else _on(dev, "status", status, i, 1))
+    with _Launch(dev) as stream:
+        _check(lib().trimkv_paged_plan(*args, stream))
+
+
+def paged_append(k_pages, v_pages, k, v, slot_map, key_bounds=None, status=None):
+    """Writes k and v [tokens, H, d] (rows may be strided) to the slots of slot_map [tokens] (trimkv_paged_append)."""
+    cache = _paged_cache(k_pages, v_pages, key_bounds)
+    dev, dt, t = k_pages.device, k_pages.dtype, k.shape[0]
+    kp, ks = _rows(dev, "k", k, dt, cache.kv_heads, cache.head_dim)
+    vp, vs = _rows(dev, "v", v, dt, cache.kv_heads, cache.head_dim)
+    if v.shape[0] != t:
+        raise ValueError("k and v hold different numbers of tokens")
+    sm = _on(dev, "slot_map", slot_map, torch.int32, t)
+    st = None if status is None else _on(dev, "status", status, torch.int32, 1)
+    with _Launch(dev) as stream:
+        _check(lib().trimkv_paged_append(C.byref(cache), t, kp, ks, vp, vs, sm, st, stream))
+
+
+def paged_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().trimkv_paged_workspace_bytes(q_heads, kv_heads, head_dim))
+
+
+def _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status):
+    dev, dt, i = k_pages.device, k_pages.dtype, torch.int32
+    if q.dim() != 3:
+        raise ValueError("q: expected [tokens, q_heads, head_dim]")
+    t, hq, d = q.shape[0], q.shape[1], cache.head_dim
+    qp, qs = _rows(dev, "q", q, dt, hq, d)
+    r = lens.shape[0] if lens.dim() == 1 else -1
+    w = block_table.shape[-1]
+    if out is None:
+        out = torch.empty((t, hq, d), dtype=dt, device=dev)
+    if workspace is None:
+        workspace = torch.empty(max(256, paged_workspace_bytes(hq, cache.kv_heads, d)), dtype=torch.uint8, device=dev)
+    if scale is None:
+        scale = d ** -0.5
+    batch = (qp, qs, _on(dev, "cu_new", cu_new, i, r + 1), _on(dev, "lens", lens, i, r),
+             _on(dev, "block_table", block_table, i, r, w), w, scale)
+    tail = (_on(dev, "out", out, dt, t, hq, d), _on(dev, "workspace", workspace, torch.uint8, None), workspace.numel(),
+            None if status is None else _on(dev, "status", status, i, 1))
+    return r, t, hq, batch, tail, out
+
+
+def paged_attention(k_pages, v_pages, q, cu_new, lens, block_table, max_new: int = 0, *, scale: Optional[float] = None,
+                    window: int = 0, out=None, workspace=None, status=None):
+    """Causal attention of the new tokens q [tokens, Hq, d] over a caller-owned paged cache (trimkv_paged_attention)."""
+    cache = _paged_cache(k_pages, v_pages, None)
+    r, t, hq, batch, tail, out = _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status)
+    with _Launch(k_pages.device) as stream:
+        _check(lib().trimkv_paged_attention(C.byref(cache), r, t, max_new, hq, *batch, window, *tail, stream))
+    return out
+
+
+def paged_sparse_attention(k_pages, v_pages, key_bounds, q, cu_new, lens, block_table, top_pages: int, *, sink_pages: int = 0,
+                           recent_pages: int = 1, scale: Optional[float] = None, out=None, selected=None, workspace=None,
+                           status=None):
+    """Attention over the top_pages pages that each token selects by their key bounds (trimkv_paged_sparse_attention).
+    Returns (out, selected [tokens, H, top_pages])."""
+    cache = _paged_cache(k_pages, v_pages, key_bounds)
+    r, t, hq, batch, tail, out = _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status)
+    if selected is None:
+        selected = torch.empty((t, cache.kv_heads, max(top_pages, 0)), dtype=torch.int32, device=k_pages.device)
+    sel = _on(k_pages.device, "selected", selected, torch.int32, t, cache.kv_heads, top_pages)
+    with _Launch(k_pages.device) as stream:
+        _check(lib().trimkv_paged_sparse_attention(C.byref(cache), r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel,
+                                                   *tail, stream))
+    return out, selected

@@ -1,0 +1,261 @@
+// The caller-owned paged cache: views, work split and launchers shared by the paged kernels.  Not part of the public ABI.
+//
+// Pages hold 64 entries of every KV head: k_pages, v_pages [n_pages][H][64][d].  A request's entries 0 .. len-1 lie in the
+// pages of its block-table row, in order.  The n new tokens of request r are rows cu_new[r] .. cu_new[r+1]-1 of q and out;
+// new token j stands at position len - n + j and sees the entries up to it.
+#pragma once
+
+#include <limits.h>
+
+#include <atomic>
+
+#include "trimkv_internal.cuh"
+
+namespace tkv {
+
+// Opts the kernel in to `bytes` of dynamic shared memory on the current device, once per device.  The bit is set after the
+// call has succeeded, so a thread that finds it set may launch; two threads that race both make the call.
+inline cudaError_t paged_allow_smem(const void* kernel, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (bit & done.load(std::memory_order_acquire)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
+struct PagedView {
+    const char* k;
+    const char* v;
+    const char* bounds;       // [n_pages][H][2][d]: channelwise smallest and largest key of a full page; may be null
+    int n_pages, H, d;
+};
+
+struct PagedBatch {
+    const int32_t* cu_new;    // [R + 1]
+    const int32_t* lens;      // [R]
+    const int32_t* table;     // [R][W]
+    int R, W, T;              // requests, table width, rows of q
+    int Hq, g;                // query heads, query heads per KV head
+    long long q_stride;       // elements from one token's q to the next
+    int window;               // > 0: a token sees the last `window` entries up to its own; 0: all of them
+    int top, sink, recent;    // page selection (top = 0: every page is read)
+    const int32_t* selected;  // [T][H][top] pages to read, ascending, -1 behind the last
+    int32_t* status;          // latched status, may be null
+};
+
+constexpr int PAGED_MAX_REQ = 8192;
+
+// Rows and length of request r; a request whose offsets or length are out of range counts as having no rows.
+struct PagedReq { int row0, n, len; };
+__device__ __forceinline__ PagedReq paged_request(const PagedBatch& pb, int r) {
+    PagedReq q;
+    q.row0 = pb.cu_new[r];
+    const int end = pb.cu_new[r + 1];
+    q.len = pb.lens[r];
+    q.n = end - q.row0;
+    if (q.row0 < 0 || end < q.row0 || end > pb.T || q.len < 0 || q.len > pb.W * (long long)PAGE) {
+        latch_error(pb.status, TRIMKV_E_ARG);
+        q.row0 = q.n = q.len = 0;
+    }
+    return q;
+}
+
+// ---------------------------------------------------------------- work split
+// A request has U units per KV head -- blocks of `tile_rows` of its n * g (token, query head) rows, or single tokens when
+// pages are selected -- and each unit counts C steps of one page (the most pages any of its units reads; at least 1, so
+// that a unit with nothing to read still writes its zeros).  All units of all requests, laid end to end, form one line of
+// `total` steps, and worker w of N takes the steps [total w / N, total (w + 1) / N): equal shares whatever the lengths, no
+// counters.  A worker's first and last unit may be shared with its neighbours; then it stores a partial result
+// (m, l, O) -- slot 2 w for a unit that it did not begin, slot 2 w + 1 for one that it began and did not end -- and a
+// second kernel joins the partials.
+struct PagedCost { int U, C; };
+__device__ __forceinline__ PagedCost paged_cost(const PagedBatch& pb, const PagedReq& q, int tile_rows, int min_rows, int max_rows) {
+    PagedCost c;
+    const int rows = q.n * pb.g;
+    if (q.n == 0 || rows < min_rows || rows > max_rows) { c.U = 0; c.C = 1; return c; }
+    int pages = (q.len + PAGE - 1) / PAGE;
+    if (pb.top > 0) {
+        c.U = q.n;
+        pages = min(pages, pb.top);
+    } else {
+        c.U = (rows + tile_rows - 1) / tile_rows;
+        if (pb.window > 0) {                              // entries that the tokens of one unit see, spread over pages
+            const long long span = (long long)pb.window + min(q.n, tile_rows / pb.g + 2);
+            pages = (int)min((long long)pages, span / PAGE + 2);
+        }
+    }
+    c.C = max(pages, 1);
+    return c;
+}
+
+constexpr int PAGED_GROUPS = 1024;            // groups of consecutive requests in the shared-memory table
+struct PagedTable {
+    long long* grp;                           // shared [PAGED_GROUPS + 1]: steps before a group
+    int gsz, ngrp, heads;
+    int tile_rows, min_rows, max_rows;
+    long long total;
+    int workers;                              // workers that take part: no share is under min_share steps
+};
+
+// Every thread of the block calls it.  prefix (may be null): steps before each request, [R + 1], written by block 0;
+// prefix[R + 1] = workers.
+__device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
+                                                  int max_rows, int max_workers, int min_share, long long* grp, long long* prefix) {
+    t.grp = grp;
+    t.heads = heads;
+    t.tile_rows = tile_rows; t.min_rows = min_rows; t.max_rows = max_rows;
+    t.gsz = (pb.R + PAGED_GROUPS - 1) / PAGED_GROUPS;
+    if (t.gsz < 1) t.gsz = 1;
+    t.ngrp = (pb.R + t.gsz - 1) / t.gsz;
+    for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
+        long long sum = 0;
+        for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
+            const PagedCost c = paged_cost(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
+            sum += (long long)c.U * c.C * heads;
+        }
+        grp[gi + 1] = sum;
+    }
+    if (threadIdx.x == 0) grp[0] = 0;
+    __syncthreads();
+    if (threadIdx.x < 32) {                   // inclusive scan by one warp
+        const int lane = threadIdx.x, per = (t.ngrp + 31) / 32;
+        const int g0 = min(t.ngrp, lane * per), g1 = min(t.ngrp, g0 + per);
+        long long local = 0;
+        for (int gi = g0; gi < g1; ++gi) local += grp[gi + 1];
+        long long incl = local;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        long long run = incl - local;
+        for (int gi = g0; gi < g1; ++gi) { run += grp[gi + 1]; grp[gi + 1] = run; }
+    }
+    __syncthreads();
+    t.total = grp[t.ngrp];
+    t.workers = (int)min((long long)max_workers, (t.total + min_share - 1) / min_share);
+    if (prefix && blockIdx.x == 0) {
+        for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
+            long long run = grp[gi];
+            for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
+                prefix[r] = run;
+                const PagedCost c = paged_cost(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
+                run += (long long)c.U * c.C * heads;
+            }
+        }
+        if (threadIdx.x == 0) { prefix[pb.R] = t.total; prefix[pb.R + 1] = t.workers; }
+    }
+}
+
+// First step of worker w; the worker that owns step x.
+__device__ __forceinline__ long long paged_share(long long total, int workers, int w) { return total * w / workers; }
+__device__ __forceinline__ int paged_owner(long long total, int workers, long long x) {
+    int w = (int)(((x + 1) * workers - 1) / total);
+    w = min(w, workers - 1);
+    while (w > 0 && paged_share(total, workers, w) > x) --w;
+    while (w + 1 < workers && paged_share(total, workers, w + 1) <= x) ++w;
+    return w;
+}
+
+// One stretch of a unit, as a worker meets it.
+struct PagedItem {
+    int r, h, u;            // request, KV head, unit of the request
+    PagedReq q;
+    int p0, p1;             // first page and one past the last (of the unit's pages, or places in its list of selected pages)
+    long long steps;        // steps of the line that it covers
+    int slot;               // -1: the whole unit (the result is final); else 2 w or 2 w + 1, see above
+    int tok0, tok1;         // tokens (of the request) that the unit's rows belong to, tok1 inclusive
+};
+
+__device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const PagedBatch& pb, long long x, long long end, int w) {
+    PagedItem it;
+    int lo = 0, hi = t.ngrp - 1;
+    while (lo < hi) {                                     // last group that begins at or before x
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.grp[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    long long base = t.grp[lo];
+    int r = lo * t.gsz;
+    PagedReq q;
+    PagedCost c;
+    for (;; ++r) {
+        q = paged_request(pb, r);
+        c = paged_cost(pb, q, t.tile_rows, t.min_rows, t.max_rows);
+        const long long s = (long long)c.U * c.C * t.heads;
+        if (x < base + s || r + 1 >= pb.R) break;
+        base += s;
+    }
+    const long long off = x - base;
+    const int unit = (int)(off / c.C), v0 = (int)(off - (long long)unit * c.C);
+    it.steps = min((long long)(c.C - v0), end - x);
+    const int v1 = v0 + (int)it.steps;
+    it.r = r;
+    it.q = q;
+    it.h = unit / c.U;
+    it.u = unit - it.h * c.U;
+    int first, count;                                     // the unit's pages
+    if (pb.top > 0) {
+        it.tok0 = it.tok1 = it.u;
+        const int pos = q.len - q.n + it.u;
+        first = 0;
+        count = pos < 0 ? 0 : min(pb.top, pos / PAGE + 1);
+    } else {
+        it.tok0 = it.u * t.tile_rows / pb.g;
+        it.tok1 = min(q.n - 1, ((it.u + 1) * t.tile_rows - 1) / pb.g);
+        const int plo = q.len - q.n + it.tok0, phi = q.len - q.n + it.tok1;
+        first = pb.window > 0 ? max(0, plo - pb.window + 1) / PAGE : 0;
+        count = phi < 0 ? 0 : phi / PAGE + 1 - first;
+    }
+    it.p0 = first + (int)((long long)count * v0 / c.C);
+    it.p1 = first + (int)((long long)count * v1 / c.C);
+    it.slot = (v0 == 0 && v1 == c.C) ? -1 : (v0 == 0 ? 2 * w + 1 : 2 * w);
+    return it;
+}
+
+// Physical page of a logical one, or -1 (latched) where the table's entry is out of range: its entries count as masked.
+__device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedView& pv, int r, int page) {
+    const int p = (page >= 0 && page < pb.W) ? pb.table[(size_t)r * pb.W + page] : -1;
+    if (p < 0 || p >= pv.n_pages) {
+        latch_error(pb.status, TRIMKV_E_ARG);
+        return -1;
+    }
+    return p;
+}
+
+// ---------------------------------------------------------------- workspace
+// [prefix: (PAGED_MAX_REQ + 2) int64][partials of the first kernel][of the second][the second kernel's schedule]
+constexpr int PAGED_SMS = 148;
+constexpr int PAGED_WARP_ROWS = 16, PAGED_WARPS = 4;              // warp kernel: rows per unit, warps per SM
+constexpr int PAGED_PLAIN_ROWS = 16, PAGED_PLAIN_CTAS = 4;        // plain kernel: rows per unit, CTAs per SM
+constexpr size_t PAGED_PREFIX_BYTES = ((size_t)(PAGED_MAX_REQ + 2) * 8 + 255) & ~(size_t)255;
+constexpr size_t paged_partial_bytes(int workers, int rows, int d) { return ((size_t)2 * workers * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
+
+struct PagedWork {
+    long long* prefix;
+    float* part_o;            // [slots][rows][d]
+    float* part_ml;           // [slots][rows][2]: running maximum (log2 units) and sum
+};
+
+// ---------------------------------------------------------------- launchers (host)
+cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* keep_lens, const int32_t* new_lens, int32_t* table,
+                              int W, int32_t* free_pages, int n_pages, const int32_t* free_count, int32_t* free_count_out,
+                              int max_tokens, int32_t* lens_out, int32_t* cu_new, int32_t* slot_map, int32_t* positions,
+                              int32_t* status, cudaStream_t st);
+cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_pages, char* bounds, int is_bf16, int T, const void* k,
+                                long long k_stride, const void* v, long long v_stride, const int32_t* slot_map, int32_t* status,
+                                cudaStream_t st);
+constexpr int PAGED_SELECT_SMEM = 200 * 1024;
+size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
+cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
+                                cudaStream_t st);
+// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows.
+cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
+                              int min_rows, int max_rows, cudaStream_t st);
+// dependent: launched behind launch_paged_select's kernel as its programmatic dependent.
+cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
+                                         float scale, const PagedWork& w, bool dependent, cudaStream_t st);
+
+}  // namespace tkv

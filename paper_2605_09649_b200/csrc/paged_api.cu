@@ -1,0 +1,188 @@
+// C entry points of the caller-owned paged cache: argument checks, workspace layout, choice of kernels.
+#include <math.h>
+
+#include "paged.cuh"
+
+using namespace tkv;
+
+namespace {
+
+template <typename... A>
+trimkv_status refuse(trimkv_status s, const char* fmt, A... args) {
+    set_last_error(fmt, args...);
+    return s;
+}
+bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool ok4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+trimkv_status done(cudaError_t e, const char* what) {
+    if (e == cudaSuccess) return TRIMKV_OK;
+    cudaGetLastError();
+    return refuse(TRIMKV_E_CUDA, "%s launch failed: %s", what, cudaGetErrorString(e));
+}
+
+trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
+    if (!c || !c->k_pages || !c->v_pages) return refuse(TRIMKV_E_ARG, "cache, k_pages and v_pages must not be NULL");
+    if (c->reserved != 0) return refuse(TRIMKV_E_ARG, "reserved must be 0");
+    if (c->kv_dtype != TRIMKV_DTYPE_BF16 && c->kv_dtype != TRIMKV_DTYPE_F32) return refuse(TRIMKV_E_ARG, "unknown kv_dtype %d", c->kv_dtype);
+    if (c->page_size != PAGE) return refuse(TRIMKV_E_UNSUPPORTED, "page_size must be %d", PAGE);
+    if (c->n_pages < 1 || c->n_pages > TRIMKV_PAGED_MAX_PAGES) return refuse(TRIMKV_E_ARG, "n_pages must be in [1, %d]", TRIMKV_PAGED_MAX_PAGES);
+    if (c->kv_heads < 1 || c->kv_heads > 1024) return refuse(TRIMKV_E_ARG, "kv_heads must be in [1, 1024]");
+    if (c->head_dim < 8 || c->head_dim % 8 || c->head_dim > 256) return refuse(TRIMKV_E_UNSUPPORTED, "head_dim must be a multiple of 8 up to 256");
+    if (!ok16(c->k_pages) || !ok16(c->v_pages) || !ok16(c->key_bounds)) return refuse(TRIMKV_E_ARG, "k_pages, v_pages and key_bounds must be 16-byte aligned");
+    pv->k = (const char*)c->k_pages;
+    pv->v = (const char*)c->v_pages;
+    pv->bounds = (const char*)c->key_bounds;
+    pv->n_pages = c->n_pages;
+    pv->H = c->kv_heads;
+    pv->d = c->head_dim;
+    return TRIMKV_OK;
+}
+
+struct WorkLayout {
+    size_t prefix, part, total;
+};
+// One area per kernel that may run in a call; the sizes depend on the head layout alone.
+WorkLayout layout(int g, int d) {
+    const int rows = g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS;   // page selection: a unit is a token's g rows
+    WorkLayout l;
+    l.prefix = PAGED_PREFIX_BYTES;
+    l.part = paged_partial_bytes(PAGED_SMS * PAGED_PLAIN_CTAS, rows, d);
+    l.total = l.prefix + l.part + 256;
+    return l;
+}
+PagedWork carve(void* workspace, int workers, int rows, int d) {
+    char* p = (char*)workspace;
+    PagedWork w;
+    w.prefix = (long long*)p;
+    w.part_o = (float*)(p + PAGED_PREFIX_BYTES);
+    w.part_ml = w.part_o + (size_t)2 * workers * rows * d;
+    return w;
+}
+
+trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64_t n_tokens, int32_t q_heads, const void* q, int64_t q_stride,
+                          const int32_t* cu_new, const int32_t* lens, const int32_t* block_table, int32_t table_width, float scale,
+                          const void* out, const void* workspace, size_t workspace_bytes, int32_t* status, PagedBatch* pb) {
+    if (n_req < 1 || n_req > PAGED_MAX_REQ) return refuse(TRIMKV_E_ARG, "n_req must be in [1, %d]", PAGED_MAX_REQ);
+    if (table_width < 1 || table_width > TRIMKV_PAGED_MAX_WIDTH) return refuse(TRIMKV_E_ARG, "table_width must be in [1, %d]", TRIMKV_PAGED_MAX_WIDTH);
+    if (q_heads < pv.H || q_heads % pv.H || q_heads / pv.H > 128) return refuse(TRIMKV_E_ARG, "q_heads must be kv_heads times 1 to 128");
+    if (n_tokens < 0 || n_tokens * q_heads > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x q_heads must be in [0, 2^30]");
+    if (n_tokens > 0) {
+        if (!q || !out || !ok16(q) || !ok16(out)) return refuse(TRIMKV_E_ARG, "q and out must be non-NULL and 16-byte aligned");
+        if (q_stride < (int64_t)q_heads * pv.d || q_stride > (1LL << 31) || (q_stride * (is_bf16 ? 2 : 4)) % 16)
+            return refuse(TRIMKV_E_ARG, "q_stride must cover a token's q and be a multiple of 16 bytes");
+    }
+    if (!cu_new || !lens || !block_table || !ok4(cu_new) || !ok4(lens) || !ok4(block_table) || !ok4(status))
+        return refuse(TRIMKV_E_ARG, "cu_new, lens and block_table must be non-NULL and aligned");
+    if (!(scale > 0.f) || isinf(scale)) return refuse(TRIMKV_E_ARG, "scale must be positive and finite");
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return refuse(TRIMKV_E_ARG, "workspace must be non-NULL and 256-byte aligned");
+    const int g = q_heads / pv.H;
+    const size_t need = layout(g, pv.d).total;
+    if (workspace_bytes < need) return refuse(TRIMKV_E_ARG, "workspace too small: %zu bytes, %zu needed", workspace_bytes, need);
+    *pb = PagedBatch{};
+    pb->cu_new = cu_new;
+    pb->lens = lens;
+    pb->table = block_table;
+    pb->R = n_req;
+    pb->W = table_width;
+    pb->T = (int)n_tokens;
+    pb->Hq = q_heads;
+    pb->g = g;
+    pb->q_stride = q_stride;
+    pb->status = status;
+    return TRIMKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+trimkv_status trimkv_paged_plan(int32_t n_req, const int32_t* old_lens, const int32_t* keep_lens, const int32_t* new_lens,
+                                int32_t* block_table, int32_t table_width, int32_t* free_pages, int32_t n_pages,
+                                const int32_t* free_count, int32_t* free_count_out, int64_t max_tokens, int32_t* lens_out,
+                                int32_t* cu_new, int32_t* slot_map, int32_t* positions, int32_t* status, void* stream) {
+    if (n_req < 1 || n_req > PAGED_MAX_REQ) return refuse(TRIMKV_E_ARG, "n_req must be in [1, %d]", PAGED_MAX_REQ);
+    if (table_width < 1 || table_width > TRIMKV_PAGED_MAX_WIDTH) return refuse(TRIMKV_E_ARG, "table_width must be in [1, %d]", TRIMKV_PAGED_MAX_WIDTH);
+    if (n_pages < 1 || n_pages > TRIMKV_PAGED_MAX_PAGES) return refuse(TRIMKV_E_ARG, "n_pages must be in [1, %d]", TRIMKV_PAGED_MAX_PAGES);
+    if (max_tokens < 0 || max_tokens > (1LL << 30)) return refuse(TRIMKV_E_ARG, "max_tokens must be in [0, 2^30]");
+    if (!old_lens || !new_lens || !block_table || !free_pages || !free_count || !free_count_out || !lens_out || !cu_new || (max_tokens > 0 && !slot_map))
+        return refuse(TRIMKV_E_ARG, "NULL buffer");
+    if (!ok4(old_lens) || !ok4(keep_lens) || !ok4(new_lens) || !ok4(block_table) || !ok4(free_pages) || !ok4(free_count) || !ok4(free_count_out) ||
+        !ok4(lens_out) || !ok4(cu_new) || !ok4(status) || !ok16(slot_map) || !ok16(positions))
+        return refuse(TRIMKV_E_ARG, "misaligned buffer (slot_map and positions 16 B, the others 4 B)");
+    return done(launch_paged_plan(n_req, old_lens, keep_lens, new_lens, block_table, table_width, free_pages, n_pages, free_count, free_count_out,
+                                  (int)max_tokens, lens_out, cu_new, slot_map, positions, status, (cudaStream_t)stream),
+                "plan");
+}
+
+trimkv_status trimkv_paged_append(const trimkv_paged_cache* cache, int64_t n_tokens, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, const int32_t* slot_map, int32_t* status, void* stream) {
+    PagedView pv;
+    const trimkv_status s = check_cache(cache, &pv);
+    if (s != TRIMKV_OK) return s;
+    if (n_tokens < 0 || n_tokens * pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
+    if (n_tokens == 0) return TRIMKV_OK;
+    const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16, elt = is_bf16 ? 2 : 4;
+    if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
+    const int64_t row = (int64_t)pv.H * pv.d;
+    if (k_stride < row || v_stride < row || k_stride > (1LL << 31) || v_stride > (1LL << 31) || (k_stride * elt) % 16 || (v_stride * elt) % 16)
+        return refuse(TRIMKV_E_ARG, "k_stride and v_stride must cover a token's row and be multiples of 16 bytes");
+    return done(launch_paged_append(pv, (char*)cache->k_pages, (char*)cache->v_pages, (char*)cache->key_bounds, is_bf16, (int)n_tokens, k, k_stride, v,
+                                    v_stride, slot_map, status, (cudaStream_t)stream),
+                "append");
+}
+
+size_t trimkv_paged_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+    if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads || head_dim < 8 || head_dim > 256 || head_dim % 8 || q_heads / kv_heads > 128) return 0;
+    return layout(q_heads / kv_heads, head_dim).total;
+}
+
+trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t max_new, int32_t q_heads,
+                                     const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
+                                     const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,
+                                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+    PagedView pv;
+    PagedBatch pb;
+    trimkv_status s = check_cache(cache, &pv);
+    if (s != TRIMKV_OK) return s;
+    const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16;
+    s = check_batch(pv, is_bf16, n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
+    if (s != TRIMKV_OK) return s;
+    if (window < 0 || window > (1 << 30)) return refuse(TRIMKV_E_ARG, "window must be in [0, 2^30]");
+    if (max_new < 0) return refuse(TRIMKV_E_ARG, "max_new must not be negative");
+    if (n_tokens == 0) return TRIMKV_OK;
+    pb.window = window;
+    const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, PAGED_PLAIN_ROWS, pv.d);
+    return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, false, (cudaStream_t)stream), "attention");
+}
+
+trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t q_heads, const void* q,
+                                            int64_t q_stride, const int32_t* cu_new, const int32_t* lens, const int32_t* block_table,
+                                            int32_t table_width, float scale, int32_t top_pages, int32_t sink_pages, int32_t recent_pages,
+                                            int32_t* selected, void* out, void* workspace, size_t workspace_bytes, int32_t* status,
+                                            void* stream) {
+    PagedView pv;
+    PagedBatch pb;
+    trimkv_status s = check_cache(cache, &pv);
+    if (s != TRIMKV_OK) return s;
+    const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16;
+    s = check_batch(pv, is_bf16, n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
+    if (s != TRIMKV_OK) return s;
+    if (!pv.bounds) return refuse(TRIMKV_E_ARG, "the cache has no key_bounds");
+    if (sink_pages < 0 || recent_pages < 1 || top_pages > TRIMKV_PAGED_MAX_WIDTH || sink_pages > top_pages || recent_pages > top_pages - sink_pages)
+        return refuse(TRIMKV_E_ARG, "sink_pages >= 0, recent_pages >= 1 and sink_pages + recent_pages <= top_pages <= %d are wanted", TRIMKV_PAGED_MAX_WIDTH);
+    if (n_tokens == 0) return TRIMKV_OK;
+    if (!selected || !ok4(selected)) return refuse(TRIMKV_E_ARG, "selected must be non-NULL and aligned");
+    if (paged_select_smem(table_width, pb.g, pv.d, is_bf16) > (size_t)PAGED_SELECT_SMEM)
+        return refuse(TRIMKV_E_UNSUPPORTED, "%d query heads per KV head of %d and a table of %d pages do not fit the selection's shared memory", pb.g, pv.d, table_width);
+    pb.top = top_pages;
+    pb.sink = sink_pages;
+    pb.recent = recent_pages;
+    pb.selected = selected;
+    s = done(launch_paged_select(pv, pb, is_bf16, q, selected, (cudaStream_t)stream), "page selection");
+    if (s != TRIMKV_OK) return s;
+    const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, pb.g > PAGED_PLAIN_ROWS ? pb.g : PAGED_PLAIN_ROWS, pv.d);
+    return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, true, (cudaStream_t)stream), "attention");
+}
+
+}  // extern "C"
