@@ -7,7 +7,10 @@
 
 #include <limits.h>
 
+#include <cuda.h>
+
 #include <atomic>
+#include <type_traits>
 
 #include "trimkv_internal.cuh"
 
@@ -160,6 +163,11 @@ __device__ __forceinline__ int paged_owner(long long total, int workers, long lo
     return w;
 }
 
+// Order of a request's units on the line: last, first, last but one, second, ...  Later units see more entries, so pairs of
+// neighbours cost about the same and equal shares of the line stay equal shares of the work.
+__device__ __forceinline__ int paged_fold(int v, int U) { return (v & 1) ? v / 2 : U - 1 - v / 2; }
+__device__ __forceinline__ int paged_unfold(int u, int U) { return u >= U - 1 - (U - 1) / 2 ? 2 * (U - 1 - u) : 2 * u + 1; }
+
 // One stretch of a unit, as a worker meets it.
 struct PagedItem {
     int r, h, u;            // request, KV head, unit of the request
@@ -195,7 +203,7 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     it.r = r;
     it.q = q;
     it.h = unit / c.U;
-    it.u = unit - it.h * c.U;
+    it.u = paged_fold(unit - it.h * c.U, c.U);
     int first, count;                                     // the unit's pages
     if (pb.top > 0) {
         it.tok0 = it.tok1 = it.u;
@@ -230,6 +238,7 @@ __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedV
 constexpr int PAGED_SMS = 148;
 constexpr int PAGED_WARP_ROWS = 16, PAGED_WARPS = 4;              // warp kernel: rows per unit, warps per SM
 constexpr int PAGED_PLAIN_ROWS = 16, PAGED_PLAIN_CTAS = 4;        // plain kernel: rows per unit, CTAs per SM
+constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
 constexpr size_t PAGED_PREFIX_BYTES = ((size_t)(PAGED_MAX_REQ + 2) * 8 + 255) & ~(size_t)255;
 constexpr size_t paged_partial_bytes(int workers, int rows, int d) { return ((size_t)2 * workers * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
 
@@ -257,5 +266,13 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
 // dependent: launched behind launch_paged_select's kernel as its programmatic dependent.
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
                                          float scale, const PagedWork& w, bool dependent, cudaStream_t st);
+
+cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows);
+// The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8
+// or 16 (page selection: g <= 16).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
+cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
+                                        int tile_rows, int max_rows, bool dependent, cudaStream_t st);
+cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
+                                      int min_rows, cudaStream_t st);
 
 }  // namespace tkv

@@ -39,20 +39,16 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
     return TRIMKV_OK;
 }
 
-struct WorkLayout {
-    size_t prefix, part, total;
-};
-// One area per kernel that may run in a call; the sizes depend on the head layout alone.
-WorkLayout layout(int g, int d) {
-    const int rows = g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS;   // page selection: a unit is a token's g rows
-    WorkLayout l;
-    l.prefix = PAGED_PREFIX_BYTES;
-    l.part = paged_partial_bytes(PAGED_SMS * PAGED_PLAIN_CTAS, rows, d);
-    l.total = l.prefix + l.part + 256;
-    return l;
+// Workspace: two areas {steps before each request, partial results}.  The first serves the kernel that a call always has or the
+// only one, the second the tensor-core kernel.  Sizes depend on the head layout alone.
+size_t area_bytes(int workers, int rows, int d) { return PAGED_PREFIX_BYTES + paged_partial_bytes(workers, rows, d); }
+size_t first_area(int g, int d) {
+    // page selection: a unit is a token's g rows
+    return area_bytes(PAGED_SMS * PAGED_PLAIN_CTAS, g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS, d);
 }
-PagedWork carve(void* workspace, int workers, int rows, int d) {
-    char* p = (char*)workspace;
+size_t work_bytes(int g, int d) { return first_area(g, d) + area_bytes(PAGED_SMS, PAGED_TC_ROWS, d); }
+PagedWork carve(void* area, int workers, int rows, int d) {
+    char* p = (char*)area;
     PagedWork w;
     w.prefix = (long long*)p;
     w.part_o = (float*)(p + PAGED_PREFIX_BYTES);
@@ -77,7 +73,7 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
     if (!(scale > 0.f) || isinf(scale)) return refuse(TRIMKV_E_ARG, "scale must be positive and finite");
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return refuse(TRIMKV_E_ARG, "workspace must be non-NULL and 256-byte aligned");
     const int g = q_heads / pv.H;
-    const size_t need = layout(g, pv.d).total;
+    const size_t need = work_bytes(g, pv.d);
     if (workspace_bytes < need) return refuse(TRIMKV_E_ARG, "workspace too small: %zu bytes, %zu needed", workspace_bytes, need);
     *pb = PagedBatch{};
     pb->cu_new = cu_new;
@@ -134,7 +130,7 @@ trimkv_status trimkv_paged_append(const trimkv_paged_cache* cache, int64_t n_tok
 
 size_t trimkv_paged_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
     if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads || head_dim < 8 || head_dim > 256 || head_dim % 8 || q_heads / kv_heads > 128) return 0;
-    return layout(q_heads / kv_heads, head_dim).total;
+    return work_bytes(q_heads / kv_heads, head_dim);
 }
 
 trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t max_new, int32_t q_heads,
@@ -152,8 +148,22 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     if (max_new < 0) return refuse(TRIMKV_E_ARG, "max_new must not be negative");
     if (n_tokens == 0) return TRIMKV_OK;
     pb.window = window;
+    const cudaStream_t st = (cudaStream_t)stream;
     const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, PAGED_PLAIN_ROWS, pv.d);
-    return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, false, (cudaStream_t)stream), "attention");
+    if (!is_bf16 || (pv.d != 64 && pv.d != 128)) return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, false, st), "attention");
+    // Requests of up to 16 rows (tokens x query heads of a KV head) stream through the warp kernel, larger ones go to the
+    // tensor cores.  max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
+    const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
+    cudaError_t e = cudaSuccess;
+    if (most <= PAGED_WARP_ROWS) {
+        e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : 16, INT_MAX, false, st);
+    } else {
+        const bool equal = max_new > 0 && n_tokens == (int64_t)n_req * max_new;    // every request has max_new tokens: one kernel
+        const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS, PAGED_TC_ROWS, pv.d);
+        e = launch_paged_attention_tc(pv, pb, q, out, scale, w2, equal ? 1 : PAGED_WARP_ROWS + 1, st);
+        if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 16, PAGED_WARP_ROWS, false, st);
+    }
+    return done(e, "attention");
 }
 
 trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t q_heads, const void* q,
@@ -182,7 +192,10 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     s = done(launch_paged_select(pv, pb, is_bf16, q, selected, (cudaStream_t)stream), "page selection");
     if (s != TRIMKV_OK) return s;
     const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, pb.g > PAGED_PLAIN_ROWS ? pb.g : PAGED_PLAIN_ROWS, pv.d);
-    return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, true, (cudaStream_t)stream), "attention");
+    const bool warp = is_bf16 && (pv.d == 64 || pv.d == 128) && pb.g <= PAGED_WARP_ROWS;
+    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : 16, INT_MAX, true, (cudaStream_t)stream)
+                     : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, true, (cudaStream_t)stream),
+                "attention");
 }
 
 }  // extern "C"

@@ -222,7 +222,7 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     const int h = hq / g, row = j * g + hq % g;
     const int u = pb.top > 0 ? j : row / tile_rows, unit_rows = pb.top > 0 ? g : tile_rows;
     const int rr = row - u * unit_rows;
-    const long long a = wk.prefix[lo] + ((long long)h * c.U + u) * c.C, b = a + c.C;
+    const long long a = wk.prefix[lo] + ((long long)h * c.U + paged_unfold(u, c.U)) * c.C, b = a + c.C;
     const int w0 = paged_owner(total, workers, a), w1 = paged_owner(total, workers, b - 1);
     if (w0 == w1) return;
     auto slot_row = [&](int i) {                                  // i-th part of the unit

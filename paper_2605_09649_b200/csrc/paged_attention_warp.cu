@@ -1,0 +1,358 @@
+// Attention over the caller-owned paged cache for few query rows: bf16, head size 64 or 128.
+//
+// A decode step does 2 g flops per byte of K and V, far below the machine's balance, so the kernel is a stream from HBM:
+// one CTA per SM, four independent warps, each with a ring of its own (48 KB) that TMA fills 32 entries at a time, one
+// or two 64-column boxes of K and of V, 128-byte swizzled so that ldmatrix meets no bank conflict.  A warp takes an equal
+// share of the line of page steps (paged.cuh), computes S^T = K Q^T and O^T += V^T P^T with mma.sync m16n8k16 -- the
+// (token, head) rows are the N dimension, 8 or 16 columns, so a group of 4 to 16 heads wastes little -- and keeps the
+// softmax in registers.  P is rounded to bf16 for the second product, and the sum takes the rounded values, so the weights
+// still add up to one.  Rows behind a request's last entry are zeroed in shared memory (they may hold NaN, and 0 x NaN is
+// NaN).  Every wait is bounded: on expiry the warp latches TRIMKV_E_TIMEOUT, drains its copies and returns.
+#include "async_copy.cuh"
+#include "mma_sync.cuh"
+#include "paged.cuh"
+#include "tcgen05_attn.cuh"
+
+namespace tkv {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int W_TILE = 32;                                            // entries per stage
+constexpr int W_WARPS = PAGED_WARPS;
+
+template <int D>
+struct WarpShape {
+    static constexpr int PLANE = W_TILE * 128;                        // 32 entries x 64 columns
+    static constexpr int PLANES = D / 64;
+    static constexpr int STAGE = 2 * PLANES * PLANE;                  // K planes, V planes
+    static constexpr int STAGES = 48 * 1024 / STAGE;                  // 3 or 6
+    static constexpr int RING = STAGES * STAGE;
+    static constexpr int OFF_BAR = W_WARPS * RING;
+    static constexpr int OFF_META = OFF_BAR + W_WARPS * STAGES * 8;
+    static constexpr int OFF_GRP = (OFF_META + W_WARPS * STAGES * 4 + 15) & ~15;
+    static constexpr int SMEM = OFF_GRP + (PAGED_GROUPS + 1) * 8 + 1024;      // 1024: alignment slack
+};
+
+// A place on the line and the stretch of a unit that begins there.
+struct WarpCursor {
+    long long x;
+    PagedItem it;
+    int ntile;          // 32-entry tiles to read
+    bool on;
+};
+
+template <int D, int NT, bool SELECT>
+__global__ void __launch_bounds__(W_WARPS * 32, 1)
+paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
+                       const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int max_rows) {
+    using S = WarpShape<D>;
+    constexpr int KS = D / 16;
+    extern __shared__ unsigned char w_smem_raw[];
+    unsigned char* smem = w_smem_raw + ((1024u - (smem_u32(w_smem_raw) & 1023u)) & 1023u);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
+    unsigned char* ring = smem + (size_t)warp * S::RING;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + warp * S::STAGES;
+    volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + warp * S::STAGES;      // first entry of the stage's tile; -1: skip
+    long long* grp = reinterpret_cast<long long*>(smem + S::OFF_GRP);
+    const int unit_rows = SELECT ? g : NT * 8;
+
+    if (lane == 0)
+        for (int s = 0; s < S::STAGES; ++s) mbar_init(bars + s, 1);
+    // rows that no copy ever filled are multiplied by weights of zero: they must be finite
+    for (int i = lane * 16; i < S::RING; i += 32 * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    grid_dependency_wait();
+    PagedTable tab;
+    paged_build_table(tab, pb, pv.H, NT * 8, 1, max_rows, (int)gridDim.x * W_WARPS, 4, grp, wk.prefix);
+    grid_dependents_may_launch();
+    // workers are spread over the SMs first, so that a short line uses many of them
+    const int w = warp * (int)gridDim.x + (int)blockIdx.x;
+    if (w >= tab.workers) return;
+    const long long end = paged_share(tab.total, tab.workers, w + 1);
+
+    auto at = [&](long long x) {
+        WarpCursor c;
+        c.x = x;
+        c.ntile = 0;
+        c.on = x < end;
+        if (!c.on) return c;
+        c.it = paged_item(tab, pb, x, end, w);
+        c.ntile = 2 * (c.it.p1 - c.it.p0);
+        // the page of the unit's last token: its second half may lie behind what is seen
+        if (c.ntile) {
+            const int phi = c.it.q.len - c.it.q.n + c.it.tok1, np = phi / PAGE + 1;
+            const bool last = SELECT ? c.it.p1 == min(pb.top, np) : c.it.p1 == np;
+            if (last && phi % PAGE < W_TILE) --c.ntile;
+        }
+        return c;
+    };
+    WarpCursor cons = at(paged_share(tab.total, tab.workers, w)), prod = cons;
+    int prod_tile = 0, log_page = 0, phys_page = 0;                   // lane l: page l of the current run of 32
+    unsigned issued = 0, consumed = 0;
+    bool failed = false;
+
+    auto issue_one = [&]() {
+        while (prod.on && prod_tile == prod.ntile) { prod = at(prod.x + prod.it.steps); prod_tile = 0; }
+        if (!prod.on) return;
+        if ((prod_tile & 63) == 0) {                                  // the next 32 pages
+            const int p = prod.it.p0 + (prod_tile >> 1) + lane;
+            log_page = -1;
+            if (p < prod.it.p1) log_page = SELECT ? pb.selected[((size_t)(prod.it.q.row0 + prod.it.u) * pv.H + prod.it.h) * pb.top + p] : p;
+            phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, log_page) : -1;
+        }
+        const int src = (prod_tile >> 1) & 31, half = prod_tile & 1;
+        const int lp = __shfl_sync(0xffffffffu, log_page, src), pp = __shfl_sync(0xffffffffu, phys_page, src);
+        if (lane == 0) {
+            const unsigned s = issued % S::STAGES;
+            meta[s] = pp < 0 ? -1 : lp * PAGE + half * W_TILE;
+            if (pp < 0) {
+                mbar_arrive(bars + s);
+            } else {
+                const uint32_t dst = smem_u32(ring + s * S::STAGE), bar = smem_u32(bars + s);
+                const int row = (pp * pv.H + prod.it.h) * PAGE + half * W_TILE;
+                fence_proxy_async_smem();
+                mbar_expect_tx(bars + s, S::STAGE);
+#pragma unroll
+                for (int p = 0; p < S::PLANES; ++p) {
+                    a_tma_2d(dst + p * S::PLANE, &map_k, p * 64, row, bar);
+                    a_tma_2d(dst + (S::PLANES + p) * S::PLANE, &map_v, p * 64, row, bar);
+                }
+            }
+        }
+        ++issued;
+        ++prod_tile;
+    };
+    for (int s = 0; s < S::STAGES - 1; ++s) issue_one();
+
+    uint32_t bq[NT][KS][2];
+    float o[NT][KS][4];
+    float m_run[NT][2], l_run[NT][2];
+
+    while (cons.on && !failed) {
+        const PagedItem& it = cons.it;
+        const int row_first = SELECT ? it.u * g : it.u * NT * 8;
+        const int rows = min(unit_rows, it.q.n * g - row_first);
+        // ---- Q fragments (B operand: k = channel, n = row); the span of entries that each of the thread's columns sees
+        int see_lo[NT][2], see_hi[NT][2];
+        int all_lo, all_hi;                                           // entries that every row of the unit sees
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = nt * 8 + (lane >> 2);
+            const int qr = row_first + row;
+            const __nv_bfloat16* p = q + (size_t)(it.q.row0 + (row < rows ? qr / g : 0)) * pb.q_stride + (size_t)(it.h * g + (row < rows ? qr % g : 0)) * D + 2 * (lane & 3);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                bq[nt][ks][0] = row < rows ? *reinterpret_cast<const uint32_t*>(p + ks * 16) : 0u;
+                bq[nt][ks][1] = row < rows ? *reinterpret_cast<const uint32_t*>(p + ks * 16 + 8) : 0u;
+                o[nt][ks][0] = o[nt][ks][1] = o[nt][ks][2] = o[nt][ks][3] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int col = nt * 8 + 2 * (lane & 3) + c;
+                see_lo[nt][c] = see_hi[nt][c] = 0;
+                if (col < rows) {
+                    const int pos = it.q.len - it.q.n + (row_first + col) / g;
+                    see_hi[nt][c] = max(pos + 1, 0);
+                    see_lo[nt][c] = pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
+                }
+                m_run[nt][c] = -INFINITY;
+                l_run[nt][c] = 0.f;
+            }
+        }
+        {                                                             // from the unit's first and last row
+            const int p0 = it.q.len - it.q.n + row_first / g, p1 = it.q.len - it.q.n + (row_first + rows - 1) / g;
+            all_hi = max(p0 + 1, 0);
+            all_lo = pb.window > 0 ? max(p1 + 1 - pb.window, 0) : 0;
+        }
+
+        for (int tt = 0; tt < cons.ntile; ++tt) {
+            issue_one();                                              // refill the stage that the previous tile freed
+            const unsigned s = consumed % S::STAGES;
+            if (!mbar_wait_bounded(bars + s, (consumed / S::STAGES) & 1u)) { failed = true; break; }
+            ++consumed;
+            const int e0 = meta[s];
+            if (e0 < 0) { __syncwarp(); continue; }
+            const uint32_t kbase = smem_u32(ring + s * S::STAGE), vbase = kbase + S::PLANES * S::PLANE;
+            const int held = it.q.len - e0;                           // entries of the tile, if fewer than 32
+            if (held < W_TILE) {
+                for (int i = max(held, 0) * 8 + lane; i < W_TILE * 8; i += 32)
+#pragma unroll
+                    for (int p = 0; p < S::PLANES; ++p)
+                        *reinterpret_cast<uint4*>(ring + s * S::STAGE + (S::PLANES + p) * S::PLANE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                fence_proxy_async_smem();                             // before a later copy into this stage
+                __syncwarp();
+            }
+            // ---- S^T[entry][row] = K Q^T
+            float sacc[2][NT][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) sacc[mt][nt][0] = sacc[mt][nt][1] = sacc[mt][nt][2] = sacc[mt][nt][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    const int row = mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
+                    const int c = 2 * ks + (lane >> 4);
+                    uint32_t a[4];
+                    ldsm_x4(a, kbase + (c >> 3) * S::PLANE + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_bf16(sacc[mt][nt], a, bq[nt][ks][0], bq[nt][ks][1]);
+                }
+            }
+            // ---- softmax over the entries; this thread owns rows 2 (lane & 3), + 1 of each column tile
+            const bool edge = e0 + W_TILE > all_hi || e0 < all_lo;
+            uint32_t pbf[2][NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = e0 + mt * 16 + (lane >> 2) + (i >> 1) * 8;
+                        float v = sacc[mt][nt][i] * scale_log2;
+                        if (edge && (e >= see_hi[nt][i & 1] || e < see_lo[nt][i & 1])) v = -INFINITY;
+                        sacc[mt][nt][i] = v;
+                        mx[i & 1] = fmaxf(mx[i & 1], v);
+                    }
+                float f[2], ref[2], ls[2] = {0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], off));
+                    const float mn = fmaxf(m_run[nt][c], mx[c]);
+                    ref[c] = mn == -INFINITY ? 0.f : mn;              // nothing seen yet: every weight is 0
+                    f[c] = exp2f(m_run[nt][c] - ref[c]);
+                    m_run[nt][c] = mn;
+                }
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    const float* sc = sacc[mt][nt];
+                    const __nv_bfloat162 plo = __floats2bfloat162_rn(exp2f(sc[0] - ref[0]), exp2f(sc[1] - ref[1]));
+                    const __nv_bfloat162 phi = __floats2bfloat162_rn(exp2f(sc[2] - ref[0]), exp2f(sc[3] - ref[1]));
+                    ls[0] += __low2float(plo) + __low2float(phi);     // the sum of what the tensor cores will see
+                    ls[1] += __high2float(plo) + __high2float(phi);
+                    pbf[mt][nt][0] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&plo));
+                    pbf[mt][nt][1] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&phi));
+                }
+                l_run[nt][0] = l_run[nt][0] * f[0] + ls[0];
+                l_run[nt][1] = l_run[nt][1] * f[1] + ls[1];
+#pragma unroll
+                for (int dt = 0; dt < KS; ++dt) {
+                    o[nt][dt][0] *= f[0]; o[nt][dt][1] *= f[1]; o[nt][dt][2] *= f[0]; o[nt][dt][3] *= f[1];
+                }
+            }
+            // ---- O^T[channel][row] += V^T P^T
+#pragma unroll
+            for (int dt = 0; dt < KS; ++dt) {
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    const int row = mt * 16 + (lane & 7) + (lane >> 4) * 8;
+                    const int c = 2 * dt + ((lane >> 3) & 1);
+                    uint32_t a[4];
+                    ldsm_x4_trans(a, vbase + (c >> 3) * S::PLANE + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][dt], a, pbf[mt][nt][0], pbf[mt][nt][1]);
+                }
+            }
+            __syncwarp();                                             // all lanes are done with the stage before it is refilled
+        }
+        if (failed) break;
+
+        // ---- the unit's result, or this worker's part of it
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float l = l_run[nt][c];
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+                const int col = nt * 8 + 2 * (lane & 3) + c;
+                if (col >= rows) continue;
+                const int dr = lane >> 2;
+                if (it.slot < 0) {
+                    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+                    const int qr = row_first + col;
+                    __nv_bfloat16* op = out + ((size_t)(it.q.row0 + qr / g) * pb.Hq + (size_t)(it.h * g + qr % g)) * D + dr;
+#pragma unroll
+                    for (int dt = 0; dt < KS; ++dt) {
+                        op[dt * 16] = __float2bfloat16_rn(o[nt][dt][c] * inv);
+                        op[dt * 16 + 8] = __float2bfloat16_rn(o[nt][dt][c + 2] * inv);
+                    }
+                } else {
+                    const size_t pr = (size_t)it.slot * unit_rows + col;
+                    float* op = wk.part_o + pr * D + dr;
+#pragma unroll
+                    for (int dt = 0; dt < KS; ++dt) { op[dt * 16] = o[nt][dt][c]; op[dt * 16 + 8] = o[nt][dt][c + 2]; }
+                    if (dr == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
+                }
+            }
+        const long long next = cons.x + it.steps;
+        if (prod.on && prod.x == next) cons = prod; else cons = at(next);
+    }
+    if (failed) {
+        if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
+        while (consumed < issued) {                                   // wait (bounded) for the copies still in flight
+            mbar_wait_bounded(bars + consumed % S::STAGES, (consumed / S::STAGES) & 1u);
+            ++consumed;
+        }
+    }
+}
+
+template <int D, int NT, bool SELECT>
+cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows,
+                     bool dependent, cudaStream_t st) {
+    using S = WarpShape<D>;
+    static std::atomic<unsigned long long> done{0};
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, SELECT>), S::SMEM, done);
+    if (e != cudaSuccess) return e;
+    CUtensorMap mk, mv;
+    e = paged_tensor_map(&mk, pv.k, pv, W_TILE);
+    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, W_TILE);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    const dim3 grid(PAGED_SMS), block(W_WARPS * 32);
+    const __nv_bfloat16* qq = (const __nv_bfloat16*)q;
+    __nv_bfloat16* oo = (__nv_bfloat16*)out;
+    if (dependent)
+        e = launch_dependent(paged_attn_warp_kernel<D, NT, SELECT>, grid, block, S::SMEM, st, mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
+    else {
+        paged_attn_warp_kernel<D, NT, SELECT><<<grid, block, S::SMEM, st>>>(mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
+        e = cudaGetLastError();
+    }
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, NT * 8, 1, max_rows, st);
+}
+
+}  // namespace
+
+// The pages as a matrix of n_pages x H x 64 rows of d bf16; box 64 columns x box_rows rows, 128-byte swizzle.
+cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows) {
+    EncodeTiledFnA fn = a_encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)pv.d, (cuuint64_t)pv.n_pages * pv.H * PAGE};
+    const cuuint64_t strides[1] = {(cuuint64_t)pv.d * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
+                                        int tile_rows, int max_rows, bool dependent, cudaStream_t st) {
+    auto go = [&](auto d, auto nt) {
+        constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+        return pb.top > 0 ? run_warp<D, NT, true>(pv, pb, q, out, scale, w, max_rows, dependent, st)
+                          : run_warp<D, NT, false>(pv, pb, q, out, scale, w, max_rows, dependent, st);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (pv.d == 64) return tile_rows <= 8 ? go(D64{}, One{}) : go(D64{}, Two{});
+    return tile_rows <= 8 ? go(D128{}, One{}) : go(D128{}, Two{});
+}
+
+}  // namespace tkv
