@@ -410,59 +410,53 @@ PAGE_SIZE = 64
 _KV_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
 
 
-def _on(device, name: str, t: torch.Tensor, dtype, *shape) -> int:
-    """Address of a contiguous tensor of this device, type and shape (None: any extent)."""
-    if t.device != device:
-        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    got = t.shape
-    if len(got) != len(shape) or any(w is not None and w != n for w, n in zip(shape, got)):
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(got)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor")
-    return t.data_ptr()
+def _on(index: int, name: str, t: torch.Tensor, dtype, shape) -> int:
+    """Address of a contiguous tensor of device `index`, type and shape (None: any one-dimensional shape)."""
+    if t.dtype is dtype and t.get_device() == index and (t.shape == shape if shape is not None else t.dim() == 1) and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor {'(any length)' if shape is None else tuple(shape)} on cuda:{index}, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _rows(device, name: str, t: torch.Tensor, dtype, heads: int, d: int):
+def _rows(index: int, name: str, t: torch.Tensor, dtype, heads: int, d: int):
     """(address, elements between tokens) of a [tokens, heads, d] tensor whose rows [heads, d] are contiguous."""
-    if t.device != device or t.dtype != dtype:
-        raise ValueError(f"{name}: expected {dtype} on {device}, got {t.dtype} on {t.device}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError(f"{name}: expected shape (tokens, {heads}, {d}), got {tuple(t.shape)}")
-    step, sh, sd = t.stride()
-    if t.shape[0] and ((d > 1 and sd != 1) or (heads > 1 and sh != d)):
-        raise ValueError(f"{name}: the {heads} x {d} values of a token must be contiguous")
-    return t.data_ptr(), (step if t.shape[0] > 1 else heads * d)
+    if t.dim() == 3 and t.dtype is dtype and t.get_device() == index:
+        n, h, e = t.shape
+        step, sh, sd = t.stride()
+        if h == heads and e == d and (n == 0 or ((sd == 1 or d == 1) and (sh == d or heads == 1))):
+            return t.data_ptr(), (step if n > 1 else heads * d)
+    raise ValueError(f"{name}: expected {dtype} [tokens, {heads}, {d}] on cuda:{index}, the {heads} x {d} values of a token contiguous, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
 def _paged_cache(k_pages, v_pages, key_bounds):
     if not k_pages.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    if k_pages.dim() != 4 or k_pages.dtype not in _KV_DTYPES:
+    dt = k_pages.dtype
+    if k_pages.dim() != 4 or dt not in _KV_DTYPES:
         raise ValueError("k_pages: expected bf16 or fp32 [n_pages, kv_heads, 64, head_dim]")
-    dev, dt = k_pages.device, k_pages.dtype
-    n, h, page, d = k_pages.shape
-    return PagedCache(_on(dev, "k_pages", k_pages, dt, n, h, page, d), _on(dev, "v_pages", v_pages, dt, n, h, page, d),
-                      None if key_bounds is None else _on(dev, "key_bounds", key_bounds, dt, n, h, 2, d),
-                      n, h, d, _KV_DTYPES[dt], page, 0)
+    index, shape = k_pages.get_device(), k_pages.shape
+    n, h, page, d = shape
+    return PagedCache(_on(index, "k_pages", k_pages, dt, shape), _on(index, "v_pages", v_pages, dt, shape),
+                      None if key_bounds is None else _on(index, "key_bounds", key_bounds, dt, (n, h, 2, d)),
+                      n, h, d, _KV_DTYPES[dt], page, 0), index, dt
 
 
-class _Launch:
-    """Makes the tensors' device current for a call (the library launches on the current device)."""
+# The raw handle of a device's current stream and the current device's number, without the wrapper objects where torch
+# offers them so: a decode step makes several of these short calls.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
-    def __init__(self, device):
-        self.index = device.index if device.index is not None else torch.cuda.current_device()
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+def _launch(fn, index: int, *args):
+    """Calls fn(*args, stream) with device `index` current (the library launches on the current device)."""
+    if _current_device() == index:
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != OK:
+        _check(status)
 
 
 def paged_plan(old_lens, keep_lens, new_lens, block_table, free_pages, free_count, free_count_out, lens_out, cu_new, slot_map,
@@ -470,67 +464,60 @@ def paged_plan(old_lens, keep_lens, new_lens, block_table, free_pages, free_coun
     """Block tables and slot maps from request lengths (trimkv_paged_plan).  int32 tensors: old_lens, keep_lens (or None),
     new_lens, lens_out [R], block_table [R, W], free_pages [n_pages], free_count and free_count_out [1], cu_new [R + 1],
     slot_map and positions (or None) [max_tokens], status [1].  Works in place; returns nothing."""
-    dev, i = old_lens.device, torch.int32
-    if dev.type != "cuda":
+    if not old_lens.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    r, w, m = old_lens.shape[0] if old_lens.dim() == 1 else -1, block_table.shape[-1], slot_map.numel()
-    args = (r, _on(dev, "old_lens", old_lens, i, r), None if keep_lens is None else _on(dev, "keep_lens", keep_lens, i, r),
-            _on(dev, "new_lens", new_lens, i, r), _on(dev, "block_table", block_table, i, r, w), w,
-            _on(dev, "free_pages", free_pages, i, None), free_pages.numel(), _on(dev, "free_count", free_count, i, 1),
-            _on(dev, "free_count_out", free_count_out, i, 1), m, _on(dev, "lens_out", lens_out, i, r),
-            _on(dev, "cu_new", cu_new, i, r + 1), _on(dev, "slot_map", slot_map, i, m),
-            None if positions is None else _on(dev, "positions", positions, i, m),
-            None if status is None else _on(dev, "status", status, i, 1))
-    with _Launch(dev) as stream:
-        _check(lib().trimkv_paged_plan(*args, stream))
+    n, i, one = old_lens.get_device(), torch.int32, (1,)
+    r, w, m = old_lens.numel(), block_table.shape[-1], slot_map.numel()
+    per = (r,)
+    _launch(lib().trimkv_paged_plan, n, r, _on(n, "old_lens", old_lens, i, per),
+            None if keep_lens is None else _on(n, "keep_lens", keep_lens, i, per), _on(n, "new_lens", new_lens, i, per),
+            _on(n, "block_table", block_table, i, (r, w)), w, _on(n, "free_pages", free_pages, i, None), free_pages.numel(),
+            _on(n, "free_count", free_count, i, one), _on(n, "free_count_out", free_count_out, i, one), m,
+            _on(n, "lens_out", lens_out, i, per), _on(n, "cu_new", cu_new, i, (r + 1,)), _on(n, "slot_map", slot_map, i, (m,)),
+            None if positions is None else _on(n, "positions", positions, i, (m,)),
+            None if status is None else _on(n, "status", status, i, one))
 
 
 def paged_append(k_pages, v_pages, k, v, slot_map, key_bounds=None, status=None):
     """Writes k and v [tokens, H, d] (rows may be strided) to the slots of slot_map [tokens] (trimkv_paged_append)."""
-    cache = _paged_cache(k_pages, v_pages, key_bounds)
-    dev, dt, t = k_pages.device, k_pages.dtype, k.shape[0]
-    kp, ks = _rows(dev, "k", k, dt, cache.kv_heads, cache.head_dim)
-    vp, vs = _rows(dev, "v", v, dt, cache.kv_heads, cache.head_dim)
+    cache, n, dt = _paged_cache(k_pages, v_pages, key_bounds)
+    t = k.shape[0]
+    kp, ks = _rows(n, "k", k, dt, cache.kv_heads, cache.head_dim)
+    vp, vs = _rows(n, "v", v, dt, cache.kv_heads, cache.head_dim)
     if v.shape[0] != t:
         raise ValueError("k and v hold different numbers of tokens")
-    sm = _on(dev, "slot_map", slot_map, torch.int32, t)
-    st = None if status is None else _on(dev, "status", status, torch.int32, 1)
-    with _Launch(dev) as stream:
-        _check(lib().trimkv_paged_append(C.byref(cache), t, kp, ks, vp, vs, sm, st, stream))
+    _launch(lib().trimkv_paged_append, n, C.byref(cache), t, kp, ks, vp, vs, _on(n, "slot_map", slot_map, torch.int32, (t,)),
+            None if status is None else _on(n, "status", status, torch.int32, (1,)))
 
 
 def paged_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().trimkv_paged_workspace_bytes(q_heads, kv_heads, head_dim))
 
 
-def _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status):
-    dev, dt, i = k_pages.device, k_pages.dtype, torch.int32
+def _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status):
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, q_heads, head_dim]")
+    i = torch.int32
     t, hq, d = q.shape[0], q.shape[1], cache.head_dim
-    qp, qs = _rows(dev, "q", q, dt, hq, d)
-    r = lens.shape[0] if lens.dim() == 1 else -1
-    w = block_table.shape[-1]
+    qp, qs = _rows(n, "q", q, dt, hq, d)
+    r, w = lens.numel(), block_table.shape[-1]
     if out is None:
-        out = torch.empty((t, hq, d), dtype=dt, device=dev)
+        out = torch.empty((t, hq, d), dtype=dt, device=q.device)
     if workspace is None:
-        workspace = torch.empty(max(256, paged_workspace_bytes(hq, cache.kv_heads, d)), dtype=torch.uint8, device=dev)
-    if scale is None:
-        scale = d ** -0.5
-    batch = (qp, qs, _on(dev, "cu_new", cu_new, i, r + 1), _on(dev, "lens", lens, i, r),
-             _on(dev, "block_table", block_table, i, r, w), w, scale)
-    tail = (_on(dev, "out", out, dt, t, hq, d), _on(dev, "workspace", workspace, torch.uint8, None), workspace.numel(),
-            None if status is None else _on(dev, "status", status, i, 1))
+        workspace = torch.empty(max(256, paged_workspace_bytes(hq, cache.kv_heads, d)), dtype=torch.uint8, device=q.device)
+    batch = (qp, qs, _on(n, "cu_new", cu_new, i, (r + 1,)), _on(n, "lens", lens, i, (r,)), _on(n, "block_table", block_table, i, (r, w)), w,
+             d ** -0.5 if scale is None else scale)
+    tail = (_on(n, "out", out, dt, (t, hq, d)), _on(n, "workspace", workspace, torch.uint8, None), workspace.numel(),
+            None if status is None else _on(n, "status", status, i, (1,)))
     return r, t, hq, batch, tail, out
 
 
 def paged_attention(k_pages, v_pages, q, cu_new, lens, block_table, max_new: int = 0, *, scale: Optional[float] = None,
                     window: int = 0, out=None, workspace=None, status=None):
     """Causal attention of the new tokens q [tokens, Hq, d] over a caller-owned paged cache (trimkv_paged_attention)."""
-    cache = _paged_cache(k_pages, v_pages, None)
-    r, t, hq, batch, tail, out = _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status)
-    with _Launch(k_pages.device) as stream:
-        _check(lib().trimkv_paged_attention(C.byref(cache), r, t, max_new, hq, *batch, window, *tail, stream))
+    cache, n, dt = _paged_cache(k_pages, v_pages, None)
+    r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
+    _launch(lib().trimkv_paged_attention, n, C.byref(cache), r, t, max_new, hq, *batch, window, *tail)
     return out
 
 
@@ -539,12 +526,10 @@ def paged_sparse_attention(k_pages, v_pages, key_bounds, q, cu_new, lens, block_
                            status=None):
     """Attention over the top_pages pages that each token selects by their key bounds (trimkv_paged_sparse_attention).
     Returns (out, selected [tokens, H, top_pages])."""
-    cache = _paged_cache(k_pages, v_pages, key_bounds)
-    r, t, hq, batch, tail, out = _paged_batch(cache, k_pages, q, cu_new, lens, block_table, scale, out, workspace, status)
+    cache, n, dt = _paged_cache(k_pages, v_pages, key_bounds)
+    r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
     if selected is None:
-        selected = torch.empty((t, cache.kv_heads, max(top_pages, 0)), dtype=torch.int32, device=k_pages.device)
-    sel = _on(k_pages.device, "selected", selected, torch.int32, t, cache.kv_heads, top_pages)
-    with _Launch(k_pages.device) as stream:
-        _check(lib().trimkv_paged_sparse_attention(C.byref(cache), r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel,
-                                                   *tail, stream))
+        selected = torch.empty((t, cache.kv_heads, max(top_pages, 0)), dtype=torch.int32, device=q.device)
+    sel = _on(n, "selected", selected, torch.int32, (t, cache.kv_heads, top_pages))
+    _launch(lib().trimkv_paged_sparse_attention, n, C.byref(cache), r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel, *tail)
     return out, selected

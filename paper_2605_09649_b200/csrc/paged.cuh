@@ -223,6 +223,20 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     return it;
 }
 
+// Last request r with cu_new[r] <= t, by the whole warp: 32 offsets per step.
+__device__ __forceinline__ int paged_find_request(const PagedBatch& pb, int t) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = pb.R;
+    while (n > 1) {
+        const int step = (n + 31) / 32, i = lane * step;
+        const int v = i < n ? pb.cu_new[lo + i] : INT_MAX;
+        const int k = max(__popc(__ballot_sync(0xffffffffu, i < n && v <= t)), 1) - 1;
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
 // Physical page of a logical one, or -1 (latched) where the table's entry is out of range: its entries count as masked.
 __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedView& pv, int r, int page) {
     const int p = (page >= 0 && page < pb.W) ? pb.table[(size_t)r * pb.W + page] : -1;
@@ -236,11 +250,12 @@ __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedV
 // ---------------------------------------------------------------- workspace
 // [prefix: (PAGED_MAX_REQ + 2) int64][partials of the first kernel][of the second][the second kernel's schedule]
 constexpr int PAGED_SMS = 148;
-constexpr int PAGED_WARP_ROWS = 16, PAGED_WARPS = 4;              // warp kernel: rows per unit, warps per SM
-constexpr int PAGED_PLAIN_ROWS = 16, PAGED_PLAIN_CTAS = 4;        // plain kernel: rows per unit, CTAs per SM
+constexpr int PAGED_WARP_ROWS = 64, PAGED_WARPS = 4;              // warp kernel: rows per unit at most, workers per SM (2 above 16 rows)
+constexpr int PAGED_PLAIN_ROWS = 16, PAGED_PLAIN_CTAS = 4;        // plain kernel: rows per unit, CTAs per SM at most
 constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
 constexpr size_t PAGED_PREFIX_BYTES = ((size_t)(PAGED_MAX_REQ + 2) * 8 + 255) & ~(size_t)255;
-constexpr size_t paged_partial_bytes(int workers, int rows, int d) { return ((size_t)2 * workers * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
+// partial results of `rows` rows (workers x rows per unit), two slots each
+constexpr size_t paged_partial_bytes(int rows, int d) { return ((size_t)2 * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
 
 struct PagedWork {
     long long* prefix;
@@ -260,16 +275,17 @@ constexpr int PAGED_SELECT_SMEM = 200 * 1024;
 size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st);
-// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows.
+// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows; many_rows: units of
+// many rows and few parts (the tensor-core kernel's).
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
-                              int min_rows, int max_rows, cudaStream_t st);
+                              int min_rows, int max_rows, bool many_rows, cudaStream_t st);
 // dependent: launched behind launch_paged_select's kernel as its programmatic dependent.
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
                                          float scale, const PagedWork& w, bool dependent, cudaStream_t st);
 
 cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows);
-// The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8
-// or 16 (page selection: g <= 16).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
+// The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8,
+// 16, 32 or 64 (page selection: g <= 64).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                         int tile_rows, int max_rows, bool dependent, cudaStream_t st);
 cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,

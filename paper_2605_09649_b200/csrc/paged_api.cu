@@ -41,18 +41,21 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
 
 // Workspace: two areas {steps before each request, partial results}.  The first serves the kernel that a call always has or the
 // only one, the second the tensor-core kernel.  Sizes depend on the head layout alone.
-size_t area_bytes(int workers, int rows, int d) { return PAGED_PREFIX_BYTES + paged_partial_bytes(workers, rows, d); }
-size_t first_area(int g, int d) {
-    // page selection: a unit is a token's g rows
-    return area_bytes(PAGED_SMS * PAGED_PLAIN_CTAS, g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS, d);
+size_t area_bytes(int rows, int d) { return PAGED_PREFIX_BYTES + paged_partial_bytes(rows, d); }
+// The most (workers x rows of a unit) of the first kernels: the plain kernel's units are 16 rows, or a token's g where
+// pages are selected; the warp kernel's 8 or 16 with four workers per SM, 32 or 64 with two.
+int first_rows(int g) {
+    const int plain = PAGED_SMS * PAGED_PLAIN_CTAS * (g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS), warp = PAGED_SMS * 2 * PAGED_WARP_ROWS;
+    return plain > warp ? plain : warp;
 }
-size_t work_bytes(int g, int d) { return first_area(g, d) + area_bytes(PAGED_SMS, PAGED_TC_ROWS, d); }
-PagedWork carve(void* area, int workers, int rows, int d) {
+size_t first_area(int g, int d) { return area_bytes(first_rows(g), d); }
+size_t work_bytes(int g, int d) { return first_area(g, d) + area_bytes(PAGED_SMS * PAGED_TC_ROWS, d); }
+PagedWork carve(void* area, int rows, int d) {
     char* p = (char*)area;
     PagedWork w;
     w.prefix = (long long*)p;
     w.part_o = (float*)(p + PAGED_PREFIX_BYTES);
-    w.part_ml = w.part_o + (size_t)2 * workers * rows * d;
+    w.part_ml = w.part_o + (size_t)2 * rows * d;
     return w;
 }
 
@@ -149,19 +152,20 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     if (n_tokens == 0) return TRIMKV_OK;
     pb.window = window;
     const cudaStream_t st = (cudaStream_t)stream;
-    const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, PAGED_PLAIN_ROWS, pv.d);
+    const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
     if (!is_bf16 || (pv.d != 64 && pv.d != 128)) return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, false, st), "attention");
-    // Requests of up to 16 rows (tokens x query heads of a KV head) stream through the warp kernel, larger ones go to the
-    // tensor cores.  max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
+    // Requests of up to 64 rows (tokens x query heads of a KV head) stream through the warp kernel, larger ones go to the
+    // tcgen05 kernel; of a batch with both, those of up to 32.  max_new may be wrong: every kernel takes any request, and where
+    // both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
     cudaError_t e = cudaSuccess;
     if (most <= PAGED_WARP_ROWS) {
-        e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : 16, INT_MAX, false, st);
+        e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64, INT_MAX, false, st);
     } else {
         const bool equal = max_new > 0 && n_tokens == (int64_t)n_req * max_new;    // every request has max_new tokens: one kernel
-        const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS, PAGED_TC_ROWS, pv.d);
-        e = launch_paged_attention_tc(pv, pb, q, out, scale, w2, equal ? 1 : PAGED_WARP_ROWS + 1, st);
-        if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 16, PAGED_WARP_ROWS, false, st);
+        const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
+        e = launch_paged_attention_tc(pv, pb, q, out, scale, w2, equal ? 1 : 33, st);
+        if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 32, 32, false, st);
     }
     return done(e, "attention");
 }
@@ -191,9 +195,9 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     pb.selected = selected;
     s = done(launch_paged_select(pv, pb, is_bf16, q, selected, (cudaStream_t)stream), "page selection");
     if (s != TRIMKV_OK) return s;
-    const PagedWork w = carve(workspace, PAGED_SMS * PAGED_PLAIN_CTAS, pb.g > PAGED_PLAIN_ROWS ? pb.g : PAGED_PLAIN_ROWS, pv.d);
+    const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
     const bool warp = is_bf16 && (pv.d == 64 || pv.d == 128) && pb.g <= PAGED_WARP_ROWS;
-    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : 16, INT_MAX, true, (cudaStream_t)stream)
+    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, true, (cudaStream_t)stream)
                      : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, true, (cudaStream_t)stream),
                 "attention");
 }

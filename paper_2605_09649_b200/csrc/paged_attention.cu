@@ -198,80 +198,135 @@ paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T*
 }
 
 // ---------------------------------------------------------------- joining the partials
-// One warp per (token, query head): nothing to do where the row's unit was one worker's.  unit_rows: rows of a unit.
-template <typename T>
-__global__ void __launch_bounds__(256)
+// The rows of a (token, KV head) whose unit was shared between workers: M = max m, out = sum e^(m - M) O / sum e^(m - M) l,
+// in worker order, so the result does not depend on timing.  SPLIT warps per row (units with many parts, few rows in all)
+// or SPLIT = 1: a warp walks all g rows of its (token, KV head).  Bound by latency: the request is found by a warp-wide
+// search before the wait for the kernel that wrote the partials.
+template <typename T, int SPLIT>
+__global__ void __launch_bounds__(128)
 paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk, int tile_rows, int min_rows, int max_rows) {
-    const int lane = threadIdx.x & 31, d = pv.d, g = pb.g;
-    const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int t = (int)(item / pb.Hq), hq = (int)(item % pb.Hq);
-    grid_dependency_wait();
+    __shared__ float4 s_sum[SPLIT > 1 ? SPLIT : 1][64];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = pv.d, g = pb.g;
+    const long long item = SPLIT > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 4 + warp;
+    const int heads = SPLIT > 1 ? pb.Hq : pv.H;
+    const int t = (int)(item / heads), rest = (int)(item % heads);
+    const int h = SPLIT > 1 ? rest / g : rest;
     if (t >= pb.T) return;
-    int lo = 0, hi = pb.R - 1;                                    // last r with cu_new[r] <= t
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (pb.cu_new[mid] <= t) lo = mid; else hi = mid - 1;
-    }
-    const PagedReq rq = paged_request(pb, lo);
+    const int r = paged_find_request(pb, t);
+    const PagedReq rq = paged_request(pb, r);
     const int j = t - rq.row0;
     if (j < 0 || j >= rq.n) return;
     const PagedCost c = paged_cost(pb, rq, tile_rows, min_rows, max_rows);
     if (c.U == 0) return;                                         // another kernel's request
-    const long long total = wk.prefix[pb.R];
+    grid_dependency_wait();
+    const long long total = wk.prefix[pb.R], before = wk.prefix[r];
     const int workers = (int)wk.prefix[pb.R + 1];
-    const int h = hq / g, row = j * g + hq % g;
-    const int u = pb.top > 0 ? j : row / tile_rows, unit_rows = pb.top > 0 ? g : tile_rows;
-    const int rr = row - u * unit_rows;
-    const long long a = wk.prefix[lo] + ((long long)h * c.U + paged_unfold(u, c.U)) * c.C, b = a + c.C;
-    const int w0 = paged_owner(total, workers, a), w1 = paged_owner(total, workers, b - 1);
-    if (w0 == w1) return;
-    auto slot_row = [&](int i) {                                  // i-th part of the unit
-        // worker w0 ends inside the unit; it began the unit, so this is its slot 2 w + 1.  The others did not begin it.
-        return (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr;
-    };
-    const int n = w1 - w0 + 1;
-    float M = -INFINITY, L = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        float m = -INFINITY, l = 0.f;
-        if (i0 + lane < n) {
-            const float2 v = *reinterpret_cast<const float2*>(wk.part_ml + slot_row(i0 + lane) * 2);
-            m = v.x; l = v.y;
+    const int unit_rows = pb.top > 0 ? g : tile_rows;
+    int u_now = -1, w0 = 0, n = 0;
+    for (int jj = SPLIT > 1 ? rest % g : 0; jj < g; ++jj) {
+        const int row = j * g + jj, u = pb.top > 0 ? j : row / tile_rows, rr = row - u * unit_rows;
+        if (u != u_now) {
+            const long long a = before + ((long long)h * c.U + paged_unfold(u, c.U)) * c.C;
+            w0 = paged_owner(total, workers, a);
+            n = paged_owner(total, workers, a + c.C - 1) - w0 + 1;
+            u_now = u;
         }
-        float mx = m;
+        if (SPLIT == 1 && n > 1 && n <= 4) {                      // few parts: every load of the row in flight at once
+            float m[4], l[4];
+            float4 v[4][2];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float Mn = fmaxf(M, mx), ref = Mn == -INFINITY ? 0.f : Mn;
-        float s = exp2f(m - ref) * l;
+            for (int i = 0; i < 4; ++i) {
+                m[i] = -INFINITY; l[i] = 0.f;
+                v[i][0] = v[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i < n) {
+                    const size_t pr = (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr;
+                    const float2 ml = *reinterpret_cast<const float2*>(wk.part_ml + pr * 2);
+                    m[i] = ml.x; l[i] = ml.y;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        L = L * exp2f(M - ref) + s;
-        M = Mn;
-    }
-    const float ref = M == -INFINITY ? 0.f : M, inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-    T* o = out + ((size_t)t * pb.Hq + hq) * d;
-    for (int c0 = lane * 4; c0 < d; c0 += 128) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = 0; i0 < n; i0 += 8) {
-            float4 v[8];
-            float f[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                f[i] = 0.f;
-                if (i0 + i < n) {
-                    v[i] = *reinterpret_cast<const float4*>(wk.part_o + slot_row(i0 + i) * d + c0);
-                    f[i] = wk.part_ml[slot_row(i0 + i) * 2];
+                    for (int x = 0; x < 2; ++x)
+                        if (lane * 4 + x * 128 < d) v[i][x] = *reinterpret_cast<const float4*>(wk.part_o + pr * d + lane * 4 + x * 128);
                 }
             }
+            const float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = M == -INFINITY ? 0.f : M;
+            float e[4], L = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = i0 + i < n ? exp2f(f[i] - ref) : 0.f;
-                sum.x = fmaf(e, v[i].x, sum.x); sum.y = fmaf(e, v[i].y, sum.y);
-                sum.z = fmaf(e, v[i].z, sum.z); sum.w = fmaf(e, v[i].w, sum.w);
+            for (int i = 0; i < 4; ++i) { e[i] = exp2f(m[i] - ref); L = fmaf(e[i], l[i], L); }
+            const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+            T* o = out + ((size_t)t * pb.Hq + (size_t)h * g + jj) * d + lane * 4;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (lane * 4 + x * 128 >= d) continue;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum.x = fmaf(e[i], v[i][x].x, sum.x); sum.y = fmaf(e[i], v[i][x].y, sum.y);
+                    sum.z = fmaf(e[i], v[i][x].z, sum.z); sum.w = fmaf(e[i], v[i][x].w, sum.w);
+                }
+                o[x * 128] = from_f32<T>(sum.x * inv); o[x * 128 + 1] = from_f32<T>(sum.y * inv);
+                o[x * 128 + 2] = from_f32<T>(sum.z * inv); o[x * 128 + 3] = from_f32<T>(sum.w * inv);
+            }
+        } else if (n > 1) {
+            // i-th part: worker w0 began the unit and did not end it (its slot 2 w + 1), the others did not begin it
+            auto slot_row = [&](int i) { return (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr; };
+            float M = -INFINITY, L = 0.f;
+            for (int i0 = 0; i0 < n; i0 += 32) {
+                float m = -INFINITY, l = 0.f;
+                if (i0 + lane < n) {
+                    const float2 v = *reinterpret_cast<const float2*>(wk.part_ml + slot_row(i0 + lane) * 2);
+                    m = v.x; l = v.y;
+                }
+                float mx = m;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                const float Mn = fmaxf(M, mx), ref = Mn == -INFINITY ? 0.f : Mn;
+                float s = exp2f(m - ref) * l;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                L = L * exp2f(M - ref) + s;
+                M = Mn;
+            }
+            const float ref = M == -INFINITY ? 0.f : M, inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+            T* o = out + ((size_t)t * pb.Hq + (size_t)h * g + jj) * d;
+            // warp x of SPLIT takes the parts [n x / SPLIT, n (x + 1) / SPLIT)
+            const int i_lo = SPLIT > 1 ? n * warp / SPLIT : 0, i_hi = SPLIT > 1 ? n * (warp + 1) / SPLIT : n;
+            for (int c0 = lane * 4; c0 < d; c0 += 128) {
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int i0 = i_lo; i0 < i_hi; i0 += 8) {
+                    float4 v[8];
+                    float f[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        f[i] = -INFINITY;
+                        if (i0 + i < i_hi) {
+                            v[i] = *reinterpret_cast<const float4*>(wk.part_o + slot_row(i0 + i) * d + c0);
+                            f[i] = wk.part_ml[slot_row(i0 + i) * 2];
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float e = exp2f(f[i] - ref);
+                        sum.x = fmaf(e, v[i].x, sum.x); sum.y = fmaf(e, v[i].y, sum.y);
+                        sum.z = fmaf(e, v[i].z, sum.z); sum.w = fmaf(e, v[i].w, sum.w);
+                    }
+                }
+                if (SPLIT > 1) s_sum[warp][c0 / 4] = sum;
+                else {
+                    o[c0] = from_f32<T>(sum.x * inv); o[c0 + 1] = from_f32<T>(sum.y * inv);
+                    o[c0 + 2] = from_f32<T>(sum.z * inv); o[c0 + 3] = from_f32<T>(sum.w * inv);
+                }
+            }
+            if (SPLIT > 1) {                                      // n is the same for the whole block
+                __syncthreads();
+                for (int cc = threadIdx.x; cc < d; cc += 128) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int x = 0; x < SPLIT; ++x) sum += reinterpret_cast<const float*>(s_sum[x])[cc];
+                    o[cc] = from_f32<T>(sum * inv);
+                }
             }
         }
-        o[c0] = from_f32<T>(sum.x * inv); o[c0 + 1] = from_f32<T>(sum.y * inv);
-        o[c0 + 2] = from_f32<T>(sum.z * inv); o[c0 + 3] = from_f32<T>(sum.w * inv);
+        if (SPLIT > 1) break;
     }
 }
 
@@ -302,19 +357,23 @@ cudaError_t run_plain_d(const PagedView& pv, const PagedBatch& pb, const void* q
 }  // namespace
 
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
-                              int min_rows, int max_rows, cudaStream_t st) {
-    const long long items = (long long)pb.T * pb.Hq;
+                              int min_rows, int max_rows, bool many_rows, cudaStream_t st) {
+    // A block per row while the GPU holds them all at once; beyond that the parts per row are few and a warp walks a
+    // token's rows.
+    const bool split = !many_rows && (long long)pb.T * pb.Hq <= PAGED_SMS * 16;
+    const long long items = (long long)pb.T * (split ? pb.Hq : pv.H);
+    const dim3 grid((unsigned)(split ? items : (items + 3) / 4)), block(128);
     count_launch();
-    const dim3 grid((unsigned)((items + 7) / 8)), block(256);
-    return is_bf16 ? launch_dependent(paged_join_kernel<__nv_bfloat16>, grid, block, 0, st, pv, pb, (__nv_bfloat16*)out, w, tile_rows, min_rows, max_rows)
-                   : launch_dependent(paged_join_kernel<float>, grid, block, 0, st, pv, pb, (float*)out, w, tile_rows, min_rows, max_rows);
+    auto go = [&](auto kernel, auto* o) { return launch_dependent(kernel, grid, block, 0, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
+    if (is_bf16) return split ? go(paged_join_kernel<__nv_bfloat16, 4>, (__nv_bfloat16*)out) : go(paged_join_kernel<__nv_bfloat16, 1>, (__nv_bfloat16*)out);
+    return split ? go(paged_join_kernel<float, 4>, (float*)out) : go(paged_join_kernel<float, 1>, (float*)out);
 }
 
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
                                          float scale, const PagedWork& w, bool dependent, cudaStream_t st) {
     const cudaError_t e = is_bf16 ? run_plain_d<__nv_bfloat16>(pv, pb, q, out, scale, w, dependent, st)
                                   : run_plain_d<float>(pv, pb, q, out, scale, w, dependent, st);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, is_bf16, out, w, PL_ROWS, 1, INT_MAX, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, is_bf16, out, w, PL_ROWS, 1, INT_MAX, false, st);
 }
 
 }  // namespace tkv

@@ -366,7 +366,7 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
     count_launch();
     paged_attn_tc_kernel<D><<<PAGED_SMS, T_THREADS, S::SMEM, st>>>(mk, mv, pv, pb, (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
     e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, true, st);
 }
 
 }  // namespace

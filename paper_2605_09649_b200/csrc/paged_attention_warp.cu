@@ -4,8 +4,11 @@
 // one CTA per SM, four independent warps, each with a ring of its own (48 KB) that TMA fills 32 entries at a time, one
 // or two 64-column boxes of K and of V, 128-byte swizzled so that ldmatrix meets no bank conflict.  A warp takes an equal
 // share of the line of page steps (paged.cuh), computes S^T = K Q^T and O^T += V^T P^T with mma.sync m16n8k16 -- the
-// (token, head) rows are the N dimension, 8 or 16 columns, so a group of 4 to 16 heads wastes little -- and keeps the
-// softmax in registers.  P is rounded to bf16 for the second product, and the sum takes the rounded values, so the weights
+// (token, head) rows are the N dimension, 8 or 16 columns, so little is wasted on padding -- and keeps the
+// softmax in registers.  Units of up to 32 or 64 rows (drafted tokens): teams of four warps share a ring of 96 KB and every
+// tile, each warp with 8 or 16 of the rows.  (One warp with 32 columns took 80 us for 32 requests x 5 tokens x 4 heads over
+// 0.6 to 2.3 K entries: a warp alone on its scheduler waits for each of its own products.)
+// P is rounded to bf16 for the second product, and the sum takes the rounded values, so the weights
 // still add up to one.  Rows behind a request's last entry are zeroed in shared memory (they may hold NaN, and 0 x NaN is
 // NaN).  Every wait is bounded: on expiry the warp latches TRIMKV_E_TIMEOUT, drains its copies and returns.
 #include "async_copy.cuh"
@@ -19,18 +22,21 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int W_TILE = 32;                                            // entries per stage
-constexpr int W_WARPS = PAGED_WARPS;
 
-template <int D>
+// NT: column tiles of 8 rows per warp.  TW: warps of a team, which share a ring and a unit, each with rows of its own.
+template <int D, int NT, int TW>
 struct WarpShape {
+    static constexpr int TEAMS = TW == 1 ? PAGED_WARPS : 2;
+    static constexpr int ROWS = NT * 8 * TW;                          // rows of a unit
     static constexpr int PLANE = W_TILE * 128;                        // 32 entries x 64 columns
     static constexpr int PLANES = D / 64;
     static constexpr int STAGE = 2 * PLANES * PLANE;                  // K planes, V planes
-    static constexpr int STAGES = 48 * 1024 / STAGE;                  // 3 or 6
+    static constexpr int STAGES = 192 * 1024 / TEAMS / STAGE;         // d = 128: 3 (a warp alone) or 6; d = 64: twice that
+    static constexpr int LAG = TW == 1 ? 0 : 1;                       // tiles that the rest of a team may be behind a refill
     static constexpr int RING = STAGES * STAGE;
-    static constexpr int OFF_BAR = W_WARPS * RING;
-    static constexpr int OFF_META = OFF_BAR + W_WARPS * STAGES * 8;
-    static constexpr int OFF_GRP = (OFF_META + W_WARPS * STAGES * 4 + 15) & ~15;
+    static constexpr int OFF_BAR = TEAMS * RING;                      // full and empty barrier of each stage
+    static constexpr int OFF_META = OFF_BAR + TEAMS * STAGES * 16;
+    static constexpr int OFF_GRP = (OFF_META + TEAMS * STAGES * 4 + 15) & ~15;
     static constexpr int SMEM = OFF_GRP + (PAGED_GROUPS + 1) * 8 + 1024;      // 1024: alignment slack
 };
 
@@ -42,32 +48,34 @@ struct WarpCursor {
     bool on;
 };
 
-template <int D, int NT, bool SELECT>
-__global__ void __launch_bounds__(W_WARPS * 32, 1)
+template <int D, int NT, int TW, bool SELECT>
+__global__ void __launch_bounds__(WarpShape<D, NT, TW>::TEAMS * TW * 32, 1)
 paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
                        const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int max_rows) {
-    using S = WarpShape<D>;
+    using S = WarpShape<D, NT, TW>;
     constexpr int KS = D / 16;
     extern __shared__ unsigned char w_smem_raw[];
     unsigned char* smem = w_smem_raw + ((1024u - (smem_u32(w_smem_raw) & 1023u)) & 1023u);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
-    unsigned char* ring = smem + (size_t)warp * S::RING;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + warp * S::STAGES;
-    volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + warp * S::STAGES;      // first entry of the stage's tile; -1: skip
+    const int team = warp / TW, tw = warp % TW;
+    unsigned char* ring = smem + (size_t)team * S::RING;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + team * S::STAGES * 2;
+    uint64_t* empty = bars + S::STAGES;
+    volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + team * S::STAGES;      // first entry of the stage's tile; -1: skip
     long long* grp = reinterpret_cast<long long*>(smem + S::OFF_GRP);
-    const int unit_rows = SELECT ? g : NT * 8;
+    const int unit_rows = SELECT ? g : S::ROWS;
 
-    if (lane == 0)
-        for (int s = 0; s < S::STAGES; ++s) mbar_init(bars + s, 1);
+    if (lane == 0 && tw == 0)
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(bars + s, 1); mbar_init(empty + s, TW); }
     // rows that no copy ever filled are multiplied by weights of zero: they must be finite
-    for (int i = lane * 16; i < S::RING; i += 32 * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = (tw * 32 + lane) * 16; i < S::RING; i += TW * 32 * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, NT * 8, 1, max_rows, (int)gridDim.x * W_WARPS, 4, grp, wk.prefix);
+    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, grp, wk.prefix);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
-    const int w = warp * (int)gridDim.x + (int)blockIdx.x;
+    const int w = team * (int)gridDim.x + (int)blockIdx.x;
     if (w >= tab.workers) return;
     const long long end = paged_share(tab.total, tab.workers, w + 1);
 
@@ -92,7 +100,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     unsigned issued = 0, consumed = 0;
     bool failed = false;
 
-    auto issue_one = [&]() {
+    auto issue_one = [&]() {                                          // the team's first warp
         while (prod.on && prod_tile == prod.ntile) { prod = at(prod.x + prod.it.steps); prod_tile = 0; }
         if (!prod.on) return;
         if ((prod_tile & 63) == 0) {                                  // the next 32 pages
@@ -103,8 +111,9 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         }
         const int src = (prod_tile >> 1) & 31, half = prod_tile & 1;
         const int lp = __shfl_sync(0xffffffffu, log_page, src), pp = __shfl_sync(0xffffffffu, phys_page, src);
+        const unsigned s = issued % S::STAGES;
+        if (TW > 1 && issued >= S::STAGES && !mbar_wait_bounded(empty + s, (issued / S::STAGES - 1) & 1u)) { failed = true; return; }
         if (lane == 0) {
-            const unsigned s = issued % S::STAGES;
             meta[s] = pp < 0 ? -1 : lp * PAGE + half * W_TILE;
             if (pp < 0) {
                 mbar_arrive(bars + s);
@@ -123,7 +132,8 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         ++issued;
         ++prod_tile;
     };
-    for (int s = 0; s < S::STAGES - 1; ++s) issue_one();
+    if (tw == 0)
+        for (int s = 0; s < S::STAGES - 1 - S::LAG; ++s) issue_one();
 
     uint32_t bq[NT][KS][2];
     float o[NT][KS][4];
@@ -131,10 +141,11 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 
     while (cons.on && !failed) {
         const PagedItem& it = cons.it;
-        const int row_first = SELECT ? it.u * g : it.u * NT * 8;
-        const int rows = min(unit_rows, it.q.n * g - row_first);
-        // ---- Q fragments (B operand: k = channel, n = row); the span of entries that each of the thread's columns sees
-        int see_lo[NT][2], see_hi[NT][2];
+        const int unit_first = SELECT ? it.u * g : it.u * S::ROWS;
+        const int unit_n = min(unit_rows, it.q.n * g - unit_first);
+        const int row_first = unit_first + tw * NT * 8;               // this warp's rows
+        const int rows = max(0, min(NT * 8, unit_n - tw * NT * 8));
+        // ---- Q fragments (B operand: k = channel, n = row)
         int all_lo, all_hi;                                           // entries that every row of the unit sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -149,30 +160,27 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int col = nt * 8 + 2 * (lane & 3) + c;
-                see_lo[nt][c] = see_hi[nt][c] = 0;
-                if (col < rows) {
-                    const int pos = it.q.len - it.q.n + (row_first + col) / g;
-                    see_hi[nt][c] = max(pos + 1, 0);
-                    see_lo[nt][c] = pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
-                }
                 m_run[nt][c] = -INFINITY;
                 l_run[nt][c] = 0.f;
             }
         }
-        {                                                             // from the unit's first and last row
+        {                                                             // from the warp's first and last row
             const int p0 = it.q.len - it.q.n + row_first / g, p1 = it.q.len - it.q.n + (row_first + rows - 1) / g;
             all_hi = max(p0 + 1, 0);
             all_lo = pb.window > 0 ? max(p1 + 1 - pb.window, 0) : 0;
         }
 
         for (int tt = 0; tt < cons.ntile; ++tt) {
-            issue_one();                                              // refill the stage that the previous tile freed
+            if (tw == 0) issue_one();                                 // refill the stage freed by the previous tile (a team: the one before)
             const unsigned s = consumed % S::STAGES;
-            if (!mbar_wait_bounded(bars + s, (consumed / S::STAGES) & 1u)) { failed = true; break; }
+            if (failed || !mbar_wait_bounded(bars + s, (consumed / S::STAGES) & 1u)) { failed = true; break; }
             ++consumed;
             const int e0 = meta[s];
-            if (e0 < 0) { __syncwarp(); continue; }
+            if (e0 < 0 || rows == 0) {                                // a page that does not exist; no rows for this warp
+                __syncwarp();
+                if (TW > 1 && lane == 0) mbar_arrive(empty + s);
+                continue;
+            }
             const uint32_t kbase = smem_u32(ring + s * S::STAGE), vbase = kbase + S::PLANES * S::PLANE;
             const int held = it.q.len - e0;                           // entries of the tile, if fewer than 32
             if (held < W_TILE) {
@@ -207,15 +215,27 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float mx[2] = {-INFINITY, -INFINITY};
+                if (edge) {                                           // rows of the column's token see entries lo .. pos
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int col = nt * 8 + 2 * (lane & 3) + c;
+                        const int pos = col < rows ? it.q.len - it.q.n + (row_first + col) / g : -1;
+                        const int lo = pb.window > 0 ? pos + 1 - pb.window : 0;
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                            for (int i = c; i < 4; i += 2) {
+                                const int e = e0 + mt * 16 + (lane >> 2) + (i >> 1) * 8;
+                                if (e > pos || e < lo) sacc[mt][nt][i] = -INFINITY;
+                            }
+                    }
+                }
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int e = e0 + mt * 16 + (lane >> 2) + (i >> 1) * 8;
-                        float v = sacc[mt][nt][i] * scale_log2;
-                        if (edge && (e >= see_hi[nt][i & 1] || e < see_lo[nt][i & 1])) v = -INFINITY;
-                        sacc[mt][nt][i] = v;
-                        mx[i & 1] = fmaxf(mx[i & 1], v);
+                        sacc[mt][nt][i] *= scale_log2;                // > 0
+                        mx[i & 1] = fmaxf(mx[i & 1], sacc[mt][nt][i]);
                     }
                 float f[2], ref[2], ls[2] = {0.f, 0.f};
 #pragma unroll
@@ -258,6 +278,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 }
             }
             __syncwarp();                                             // all lanes are done with the stage before it is refilled
+            if (TW > 1 && lane == 0) mbar_arrive(empty + s);
         }
         if (failed) break;
 
@@ -282,7 +303,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         op[dt * 16 + 8] = __float2bfloat16_rn(o[nt][dt][c + 2] * inv);
                     }
                 } else {
-                    const size_t pr = (size_t)it.slot * unit_rows + col;
+                    const size_t pr = (size_t)it.slot * unit_rows + tw * NT * 8 + col;
                     float* op = wk.part_o + pr * D + dr;
 #pragma unroll
                     for (int dt = 0; dt < KS; ++dt) { op[dt * 16] = o[nt][dt][c]; op[dt * 16 + 8] = o[nt][dt][c + 2]; }
@@ -290,7 +311,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 }
             }
         const long long next = cons.x + it.steps;
-        if (prod.on && prod.x == next) cons = prod; else cons = at(next);
+        if (tw == 0 && prod.on && prod.x == next) cons = prod; else cons = at(next);
     }
     if (failed) {
         if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
@@ -301,28 +322,28 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     }
 }
 
-template <int D, int NT, bool SELECT>
+template <int D, int NT, int TW, bool SELECT>
 cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows,
                      bool dependent, cudaStream_t st) {
-    using S = WarpShape<D>;
+    using S = WarpShape<D, NT, TW>;
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, SELECT>), S::SMEM, done);
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
     e = paged_tensor_map(&mk, pv.k, pv, W_TILE);
     if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, W_TILE);
     if (e != cudaSuccess) return e;
     count_launch();
-    const dim3 grid(PAGED_SMS), block(W_WARPS * 32);
+    const dim3 grid(PAGED_SMS), block(S::TEAMS * TW * 32);
     const __nv_bfloat16* qq = (const __nv_bfloat16*)q;
     __nv_bfloat16* oo = (__nv_bfloat16*)out;
     if (dependent)
-        e = launch_dependent(paged_attn_warp_kernel<D, NT, SELECT>, grid, block, S::SMEM, st, mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
+        e = launch_dependent(paged_attn_warp_kernel<D, NT, TW, SELECT>, grid, block, S::SMEM, st, mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
     else {
-        paged_attn_warp_kernel<D, NT, SELECT><<<grid, block, S::SMEM, st>>>(mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
+        paged_attn_warp_kernel<D, NT, TW, SELECT><<<grid, block, S::SMEM, st>>>(mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
         e = cudaGetLastError();
     }
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, NT * 8, 1, max_rows, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, false, st);
 }
 
 }  // namespace
@@ -342,17 +363,18 @@ cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView
 
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                         int tile_rows, int max_rows, bool dependent, cudaStream_t st) {
-    auto go = [&](auto d, auto nt) {
-        constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-        return pb.top > 0 ? run_warp<D, NT, true>(pv, pb, q, out, scale, w, max_rows, dependent, st)
-                          : run_warp<D, NT, false>(pv, pb, q, out, scale, w, max_rows, dependent, st);
+    auto go = [&](auto d, auto nt, auto tw) {
+        constexpr int D = decltype(d)::value, NT = decltype(nt)::value, TW = decltype(tw)::value;
+        return pb.top > 0 ? run_warp<D, NT, TW, true>(pv, pb, q, out, scale, w, max_rows, dependent, st)
+                          : run_warp<D, NT, TW, false>(pv, pb, q, out, scale, w, max_rows, dependent, st);
     };
-    using One = std::integral_constant<int, 1>;
-    using Two = std::integral_constant<int, 2>;
-    using D64 = std::integral_constant<int, 64>;
-    using D128 = std::integral_constant<int, 128>;
-    if (pv.d == 64) return tile_rows <= 8 ? go(D64{}, One{}) : go(D64{}, Two{});
-    return tile_rows <= 8 ? go(D128{}, One{}) : go(D128{}, Two{});
+    auto rows = [&](auto d) {
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        using Four = std::integral_constant<int, 4>;
+        return tile_rows <= 8 ? go(d, One{}, One{}) : tile_rows <= 16 ? go(d, Two{}, One{}) : tile_rows <= 32 ? go(d, One{}, Four{}) : go(d, Two{}, Four{});
+    };
+    return pv.d == 64 ? rows(std::integral_constant<int, 64>{}) : rows(std::integral_constant<int, 128>{});
 }
 
 }  // namespace tkv

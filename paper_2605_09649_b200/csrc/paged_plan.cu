@@ -13,6 +13,8 @@
 // the page that this same call writes are read from the call's input, so the halves need not wait for one another.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "mma_sync.cuh"
 #include "paged.cuh"
 
@@ -178,7 +180,7 @@ paged_plan_kernel(int R, const int32_t* old_lens, const int32_t* keep_lens, cons
 }
 
 // ---------------------------------------------------------------- append
-constexpr int APP_THREADS = 256;
+constexpr int APP_THREADS = 256, APP_UNROLL = 4;
 
 template <typename T>
 struct MinMax16;                              // channelwise bounds of 16 bytes of keys; NaN in a channel stays NaN
@@ -194,6 +196,11 @@ struct MinMax16<__nv_bfloat16> {
         const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { lo[i] = __hmin2_nan(lo[i], p[i]); hi[i] = __hmax2_nan(hi[i], p[i]); }
+    }
+    __device__ __forceinline__ void join(const uint4& vlo, const uint4& vhi) {
+        const __nv_bfloat162 *a = reinterpret_cast<const __nv_bfloat162*>(&vlo), *b = reinterpret_cast<const __nv_bfloat162*>(&vhi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { lo[i] = __hmin2_nan(lo[i], a[i]); hi[i] = __hmax2_nan(hi[i], b[i]); }
     }
 };
 template <>
@@ -211,99 +218,108 @@ struct MinMax16<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { lo[i] = mn(lo[i], p[i]); hi[i] = mx(hi[i], p[i]); }
     }
+    __device__ __forceinline__ void join(const uint4& vlo, const uint4& vhi) {
+        const float *a = reinterpret_cast<const float*>(&vlo), *b = reinterpret_cast<const float*>(&vhi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { lo[i] = mn(lo[i], a[i]); hi[i] = mx(hi[i], b[i]); }
+    }
 };
 
 // Blocks [0, copy_blocks) copy rows: 16-byte chunk c of the T x H x (d * elt / 16) chunks of k, and the same of v.  The
-// others take 32 tokens x one head per warp and reduce the pages that these tokens complete.
+// others take `group` tokens of one head each and reduce the pages that these tokens complete, eight rows per warp.
 template <typename T>
 __global__ void __launch_bounds__(APP_THREADS)
 paged_append_kernel(char* __restrict__ k_pages, char* __restrict__ v_pages, char* __restrict__ bounds, int n_pages, int H, int d,
                     int T_rows, const char* __restrict__ k, long long k_stride, const char* __restrict__ v, long long v_stride,
-                    const int32_t* __restrict__ slot_map, int32_t* status, int copy_blocks) {
+                    const int32_t* __restrict__ slot_map, int32_t* status, int copy_blocks, int group) {
+    constexpr int WARPS = APP_THREADS / 32;
+    __shared__ uint4 s_part[2][WARPS][16];
     const int rb = d * (int)sizeof(T), cpr = rb / 16;         // bytes, 16-byte chunks per row
     const int slots = n_pages * PAGE;
     if ((int)blockIdx.x < copy_blocks) {
-        const int per_tok = H * cpr;
+        const unsigned per_tok = (unsigned)(H * cpr);
         const long long n = (long long)T_rows * per_tok;
         const long long step = (long long)copy_blocks * APP_THREADS;
-        for (long long c0 = (long long)blockIdx.x * APP_THREADS + threadIdx.x; c0 < n; c0 += 2 * step) {
-            uint4 kv[2], vv[2];
-            size_t dst[2];
-            bool on[2];
+        for (long long c0 = (long long)blockIdx.x * APP_THREADS + threadIdx.x; c0 < n; c0 += APP_UNROLL * step) {
+            int s[APP_UNROLL];
+            unsigned tok[APP_UNROLL], rest[APP_UNROLL];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {                     // two chunks of each in flight per thread
+            for (int u = 0; u < APP_UNROLL; ++u) {
                 const long long c = c0 + u * step;
-                on[u] = c < n;
-                if (!on[u]) continue;
-                const int t = (int)(c / per_tok), rest = (int)(c - (long long)t * per_tok), h = rest / cpr, ch = rest - h * cpr;
-                const int s = slot_map[t];
-                on[u] = s >= 0 && s < slots;
-                if (!on[u]) {
-                    if (s != -1 && rest == 0) latch_error(status, TRIMKV_E_ARG);
+                tok[u] = n < (1LL << 32) ? (unsigned)c / per_tok : (unsigned)(c / per_tok);
+                rest[u] = (unsigned)(c - (long long)tok[u] * per_tok);
+                s[u] = c < n ? slot_map[tok[u]] : -1;
+            }
+            uint4 kv[APP_UNROLL], vv[APP_UNROLL];
+#pragma unroll
+            for (int u = 0; u < APP_UNROLL; ++u) {            // all loads in flight before the first store
+                if (s[u] < 0 || s[u] >= slots) {
+                    if (s[u] != -1 && rest[u] == 0) latch_error(status, TRIMKV_E_ARG);
+                    s[u] = -1;
                     continue;
                 }
-                kv[u] = *reinterpret_cast<const uint4*>(k + ((size_t)t * k_stride) * sizeof(T) + (size_t)rest * 16);
-                vv[u] = *reinterpret_cast<const uint4*>(v + ((size_t)t * v_stride) * sizeof(T) + (size_t)rest * 16);
-                dst[u] = (((size_t)(s / PAGE) * H + h) * PAGE + s % PAGE) * rb + (size_t)ch * 16;
+                kv[u] = *reinterpret_cast<const uint4*>(k + ((size_t)tok[u] * k_stride) * sizeof(T) + (size_t)rest[u] * 16);
+                vv[u] = *reinterpret_cast<const uint4*>(v + ((size_t)tok[u] * v_stride) * sizeof(T) + (size_t)rest[u] * 16);
             }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (on[u]) {
-                    *reinterpret_cast<uint4*>(k_pages + dst[u]) = kv[u];
-                    *reinterpret_cast<uint4*>(v_pages + dst[u]) = vv[u];
+            for (int u = 0; u < APP_UNROLL; ++u)
+                if (s[u] >= 0) {
+                    const unsigned h = rest[u] / (unsigned)cpr, ch = rest[u] - h * cpr;
+                    const size_t dst = (((size_t)(s[u] / PAGE) * H + h) * PAGE + s[u] % PAGE) * rb + (size_t)ch * 16;
+                    *reinterpret_cast<uint4*>(k_pages + dst) = kv[u];
+                    *reinterpret_cast<uint4*>(v_pages + dst) = vv[u];
                 }
         }
         return;
     }
-    const int lane = threadIdx.x & 31;
-    const int item = ((int)blockIdx.x - copy_blocks) * (APP_THREADS / 32) + (threadIdx.x >> 5);
-    const int t0 = (item / H) * 32, h = item % H;
-    if (t0 >= T_rows) return;
-    const int my_slot = t0 + lane < T_rows ? slot_map[t0 + lane] : -1;
-    unsigned full = __ballot_sync(0xffffffffu, my_slot >= 0 && my_slot < slots && my_slot % PAGE == PAGE - 1);
-    while (full) {
-        const int b = __ffs(full) - 1, t = t0 + b;
-        full &= full - 1;
-        const int s = __shfl_sync(0xffffffffu, my_slot, b), page = s / PAGE;
-        // row i of the page is this call's token t - 63 + i if that token was given the row's slot
-        unsigned here[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int item = (int)blockIdx.x - copy_blocks, h = item % H;
+    const long long t_first = (long long)(item / H) * group;
+    for (int g0 = 0; g0 < group && t_first + g0 < T_rows; g0 += 32) {
+        const int t0 = (int)t_first + g0;
+        const int my_slot = g0 + lane < group && t0 + lane < T_rows ? slot_map[t0 + lane] : -1;
+        unsigned full = __ballot_sync(0xffffffffu, my_slot >= 0 && my_slot < slots && my_slot % PAGE == PAGE - 1);
+        while (full) {                                        // the same for every warp of the block
+            const int b = __ffs(full) - 1, t = t0 + b;
+            full &= full - 1;
+            const int s = __shfl_sync(0xffffffffu, my_slot, b), page = s / PAGE;
+            // row i of the page is this call's token t - 63 + i if that token was given the row's slot
+            const int my_row = warp * 8 + (lane & 7), my_tok = t - (PAGE - 1) + my_row;
+            const unsigned here = __ballot_sync(0xffffffffu, my_tok >= 0 && slot_map[max(my_tok, 0)] == page * PAGE + my_row);
+            const char* page_rows = k_pages + ((size_t)page * H + h) * PAGE * (size_t)rb;
+            char* out = bounds + ((size_t)page * H + h) * 2 * rb;
+            for (int c0 = 0; c0 < cpr; c0 += 16) {            // half a warp per row, four rows each
+                const int ch = c0 + (lane & 15), half = lane >> 4;
+                const bool on = ch < cpr;
+                uint4 val[4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int i = u * 32 + lane, ti = t - (PAGE - 1) + i;
-            here[u] = __ballot_sync(0xffffffffu, ti >= 0 && slot_map[max(ti, 0)] == page * PAGE + i);
-        }
-        const char* page_rows = k_pages + ((size_t)page * H + h) * PAGE * (size_t)rb;
-        char* out = bounds + ((size_t)page * H + h) * 2 * rb;
-        for (int c0 = 0; c0 < cpr; c0 += 16) {                // half a warp per row: rows 2 j and 2 j + 1 per step
-            const int ch = c0 + (lane & 15), half = lane >> 4;
-            const bool on = ch < cpr;
-            MinMax16<T> mm;
-#pragma unroll 8
-            for (int j = 0; j < PAGE / 2; ++j) {
-                const int i = 2 * j + half;
-                const bool in_call = (here[i >> 5] >> (i & 31)) & 1u;
-                const char* src = in_call ? k + ((size_t)(t - (PAGE - 1) + i) * k_stride) * sizeof(T) + (size_t)h * rb
-                                          : page_rows + (size_t)i * rb;
-                uint4 val = make_uint4(0u, 0u, 0u, 0u);
-                if (on) val = *reinterpret_cast<const uint4*>(src + (size_t)ch * 16);
-                if (j == 0) mm.start(val); else mm.add(val);
-            }
-            uint4 lo = *reinterpret_cast<uint4*>(mm.lo), hi = *reinterpret_cast<uint4*>(mm.hi);
-            MinMax16<T> other;                                // join the two half-warps
-            uint4 olo, ohi;
-            olo.x = __shfl_xor_sync(0xffffffffu, lo.x, 16); olo.y = __shfl_xor_sync(0xffffffffu, lo.y, 16);
-            olo.z = __shfl_xor_sync(0xffffffffu, lo.z, 16); olo.w = __shfl_xor_sync(0xffffffffu, lo.w, 16);
-            ohi.x = __shfl_xor_sync(0xffffffffu, hi.x, 16); ohi.y = __shfl_xor_sync(0xffffffffu, hi.y, 16);
-            ohi.z = __shfl_xor_sync(0xffffffffu, hi.z, 16); ohi.w = __shfl_xor_sync(0xffffffffu, hi.w, 16);
-            other = mm;
-            other.add(olo);
-            lo = *reinterpret_cast<uint4*>(other.lo);
-            other = mm;
-            other.add(ohi);
-            hi = *reinterpret_cast<uint4*>(other.hi);
-            if (on && half == 0) {
-                *reinterpret_cast<uint4*>(out + (size_t)ch * 16) = lo;
-                *reinterpret_cast<uint4*>(out + rb + (size_t)ch * 16) = hi;
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 2 * j + half, row = warp * 8 + i;
+                    const char* src = (here >> i) & 1u ? k + ((size_t)(t - (PAGE - 1) + row) * k_stride) * sizeof(T) + (size_t)h * rb
+                                                       : page_rows + (size_t)row * rb;
+                    val[j] = on ? *reinterpret_cast<const uint4*>(src + (size_t)ch * 16) : make_uint4(0u, 0u, 0u, 0u);
+                }
+                MinMax16<T> mm;
+                mm.start(val[0]);
+#pragma unroll
+                for (int j = 1; j < 4; ++j) mm.add(val[j]);
+                uint4 lo = *reinterpret_cast<uint4*>(mm.lo), hi = *reinterpret_cast<uint4*>(mm.hi), olo, ohi;
+                olo.x = __shfl_xor_sync(0xffffffffu, lo.x, 16); olo.y = __shfl_xor_sync(0xffffffffu, lo.y, 16);
+                olo.z = __shfl_xor_sync(0xffffffffu, lo.z, 16); olo.w = __shfl_xor_sync(0xffffffffu, lo.w, 16);
+                ohi.x = __shfl_xor_sync(0xffffffffu, hi.x, 16); ohi.y = __shfl_xor_sync(0xffffffffu, hi.y, 16);
+                ohi.z = __shfl_xor_sync(0xffffffffu, hi.z, 16); ohi.w = __shfl_xor_sync(0xffffffffu, hi.w, 16);
+                mm.join(olo, ohi);
+                if (half == 0) {
+                    s_part[0][warp][lane] = *reinterpret_cast<uint4*>(mm.lo);
+                    s_part[1][warp][lane] = *reinterpret_cast<uint4*>(mm.hi);
+                }
+                __syncthreads();
+                if (warp == 0 && half == 0 && on) {
+                    for (int x = 1; x < WARPS; ++x) mm.join(s_part[0][x][lane], s_part[1][x][lane]);
+                    *reinterpret_cast<uint4*>(out + (size_t)ch * 16) = *reinterpret_cast<uint4*>(mm.lo);
+                    *reinterpret_cast<uint4*>(out + rb + (size_t)ch * 16) = *reinterpret_cast<uint4*>(mm.hi);
+                }
+                __syncthreads();
             }
         }
     }
@@ -330,16 +346,20 @@ cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_page
                                 long long k_stride, const void* v, long long v_stride, const int32_t* slot_map, int32_t* status,
                                 cudaStream_t st) {
     const long long chunks = (long long)T * pv.H * (pv.d * (is_bf16 ? 2 : 4) / 16);
-    const int copy_blocks = (int)((chunks + 2 * APP_THREADS - 1) / (2 * APP_THREADS) < PAGED_SMS * 16
-                                      ? (chunks + 2 * APP_THREADS - 1) / (2 * APP_THREADS) : PAGED_SMS * 16);
-    const long long items = bounds ? (long long)((T + 31) / 32) * pv.H : 0;
-    const int blocks = copy_blocks + (int)((items + APP_THREADS / 32 - 1) / (APP_THREADS / 32));
-    if (is_bf16)
-        paged_append_kernel<__nv_bfloat16><<<blocks, APP_THREADS, 0, st>>>(k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k,
-                                                                          k_stride, (const char*)v, v_stride, slot_map, status, copy_blocks);
-    else
-        paged_append_kernel<float><<<blocks, APP_THREADS, 0, st>>>(k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k,
-                                                                  k_stride, (const char*)v, v_stride, slot_map, status, copy_blocks);
+    // one chunk per thread while that leaves the GPU unfilled, then up to APP_UNROLL per thread
+    long long copy_blocks = (chunks + APP_THREADS - 1) / APP_THREADS;
+    if (copy_blocks > PAGED_SMS * 8) copy_blocks = std::max<long long>(PAGED_SMS * 8, std::min<long long>(PAGED_SMS * 64, (copy_blocks + APP_UNROLL - 1) / APP_UNROLL));
+    // tokens per reducing block: few, so that the pages of a decode step (each token may complete one) are reduced side by
+    // side; a prompt completes one page in 64 tokens
+    int group = 1;
+    while (group < 64 && (long long)((T + group - 1) / group) * pv.H > PAGED_SMS * 8) group *= 2;
+    const long long items = bounds ? (long long)((T + group - 1) / group) * pv.H : 0;
+    const unsigned blocks = (unsigned)(copy_blocks + items);
+    auto go = [&](auto kernel) {
+        kernel<<<blocks, APP_THREADS, 0, st>>>(k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k, k_stride, (const char*)v, v_stride,
+                                               slot_map, status, (int)copy_blocks, group);
+    };
+    if (is_bf16) go(paged_append_kernel<__nv_bfloat16>); else go(paged_append_kernel<float>);
     count_launch();
     return cudaGetLastError();
 }

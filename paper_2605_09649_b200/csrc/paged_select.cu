@@ -5,14 +5,23 @@
 // rest of the `top` places go to the largest U, ties to the lower page.  Only full pages before the token's own are ever
 // scored, so the bounds of a page that is still being filled are not looked at.
 //
-// The order of the scores decides which pages are read, so a rounding could change the result altogether: the sums are
-// held in 64 bits.  The term max(q lo, q hi) is q hi where q > 0 and q lo elsewhere: a select and one fp64 fma.  Products of
-// bf16 values are exact there, and the sum's error (128 x 2^-53) is far below the distance of different scores.
+// The order of the scores decides which pages are read, so a rounding could change the result altogether: U is settled in
+// 64 bits, where products of bf16 values are exact and a sum's error (128 x 2^-53) is far below the distance of different
+// scores.  max(q lo, q hi) = min(q, 0) lo + max(q, 0) hi, so U is a product of the page's 2 d bounds, which lie side by
+// side in memory, with the clamped query.
 //
-// One cluster of 1, 2, 4 or 8 CTAs per (token, KV head) -- as many as keep the GPU busy -- shares the pages; eight lanes
-// take a page (16 bytes of lo and of hi per lane and step), the queries wait in shared memory as doubles laid out so that
-// the eight lanes read 128 consecutive bytes.  The first CTA collects the 64-bit order keys in its shared memory and finds
-// the m-th largest by radix descent, eight bits at a time, ending early once a bin holds exactly the places left.
+// bf16 (paged_select_mma_kernel): the tensor cores compute U for 16 pages x 8 rows at a time in fp32, and beside it the
+// sum of the terms' magnitudes A, the same product of absolute values.  An fp32 sum of 2 d <= 512 exact products is off by
+// less than A 2^-14 whatever the order and the rounding of its additions (512 additions of relative error 2^-23).  A
+// bisection over the fp32 scores brackets the m-th largest to [a, b], b - a <= 2 E (E: the largest error of the token's
+// pages); pages above b + 2 E are in, pages below a - 2 E are out, and the few in between are scored again in 64 bits.  If all are in
+// between (equal bounds, infinities, NaN) all are, and a descent over 64-bit keys decides.  Bound by the latency of its
+// chain (table, bounds, descent); the bounds are read once per group of tokens.
+//
+// fp32 (paged_select_kernel): fp64 sums for every page, eight lanes per page.
+//
+// In both, a cluster of 1, 2, 4 or 8 CTAs per unit of tokens and KV head -- as many as fill the GPU -- shares the pages, and
+// its first CTA collects the scores in its shared memory.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -207,6 +216,434 @@ paged_select_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, int32_
     for (int i = tid; i < pb.recent; i += SEL_THREADS) sel[pb.top - pb.recent + i] = np - pb.recent + i;
 }
 
+// ---------------------------------------------------------------- bf16: tensor cores, then 64 bits where it matters
+constexpr int SEL_TOKENS = 4;                 // tokens of one unit, at most
+constexpr int SEL_LIST = 512;                 // pages between the thresholds that are ranked by counting
+constexpr float SEL_EPS = 1.0f / 16384.0f;    // 2^-14, see above
+
+__device__ __forceinline__ uint32_t clamp_neg(uint32_t v) {
+    const __nv_bfloat162 z = __float2bfloat162_rn(0.f), x = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162*>(&v), z);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ uint32_t clamp_pos(uint32_t v) {
+    const __nv_bfloat162 z = __float2bfloat162_rn(0.f), x = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&v), z);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+
+// The 64-bit key of one page, by a whole warp.
+__device__ __forceinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat16* q, int g, int d) {
+    const int lane = threadIdx.x & 31;
+    double best = -INFINITY;
+    bool nan = false;
+    for (int head = 0; head < g; ++head) {
+        double s = 0.0;
+        for (int c = 2 * lane; c < d; c += 64) {
+            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(q + (size_t)head * d + c));
+            const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(b + c));
+            const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(b + d + c));
+            s = fma((double)x.x, (double)(x.x > 0.f ? hi.x : lo.x), s);
+            s = fma((double)x.y, (double)(x.y > 0.f ? hi.y : lo.y), s);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        nan |= s != s;
+        best = fmax(best, s);
+    }
+    return score_key(nan ? (double)NAN : best);
+}
+
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
+
+// Sum over the block of each thread's value, and the sum over the threads before it.
+__device__ __forceinline__ int block_before(int v, int* s_warp, int& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    int before = incl - v;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < SEL_THREADS / 32; ++w) {
+        if (w < warp) before += s_warp[w];
+        total += s_warp[w];
+    }
+    return before;
+}
+
+// One digit of a radix descent: the bin, from the top, in which the count reaches `need`; need and the bin's count by reference.
+__device__ __forceinline__ int pick_digit(const int* s_hist, int* s_pick, int& need, int& count) {
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x < 32) {                                       // lane l: bins 255 - 8 l down to 248 - 8 l
+        int c[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = s_hist[255 - lane * 8 - i]; sum += c[i]; }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        int run = incl - sum;
+        if (run < need && need <= incl) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (run < need && need <= run + c[i]) { s_pick[0] = 255 - lane * 8 - i; s_pick[1] = need - run; s_pick[2] = c[i]; }
+                run += c[i];
+            }
+        }
+    }
+    __syncthreads();
+    need = s_pick[1];
+    count = s_pick[2];
+    return s_pick[0];
+}
+
+// grid = ceil(T / ntok) * H clusters.  Dynamic shared memory: scores [ntok][W] fp32, then 64-bit keys [W].
+template <int DK>      // ceil(d / 32)
+__global__ void __launch_bounds__(SEL_THREADS, DK <= 4 ? 2 : 1)
+paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __restrict__ q, int32_t* __restrict__ selected, int nclust, int ntok) {
+    constexpr int NC = 2;                                         // column tiles (8 rows of q each) per walk over the bounds
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    __shared__ int s_req[SEL_TOKENS], s_np[SEL_TOKENS];           // request of each token (-1: none), pages up to its own
+    __shared__ unsigned s_err[SEL_TOKENS];
+    __shared__ int s_hist[256], s_pick[3], s_warp[SEL_THREADS / 32], s_nlist, s_list[SEL_LIST];
+    __shared__ u64 s_lkey[SEL_LIST];
+    __shared__ uint2 s_cnt[2][SEL_THREADS / 32];
+    grid_dependents_may_launch();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)blockIdx.x % nclust, unit = (int)blockIdx.x / nclust;
+    const int t0 = unit / pv.H * ntok, h = unit % pv.H;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = pb.g, d = pv.d, W = pb.W;
+    u64* s_key = reinterpret_cast<u64*>(s_raw);
+    float* s_c = reinterpret_cast<float*>(s_raw + (size_t)W * sizeof(u64));
+    if (warp < ntok) {
+        const int t = t0 + warp;
+        int req = -1, np = 0;
+        if (t < pb.T) {
+            const int r = paged_find_request(pb, t);
+            const PagedReq rq = paged_request(pb, r);
+            const int j = t - rq.row0;
+            if (j >= 0 && j < rq.n) {                             // else: a row behind the last request, left as it is
+                req = r;
+                const int pos = rq.len - rq.n + j;
+                np = pos < 0 ? 0 : pos / PAGE + 1;
+            }
+        }
+        if (lane == 0) { s_req[warp] = req; s_np[warp] = np; s_err[warp] = 0u; }
+    }
+    __syncthreads();
+    int most = 0;
+    for (int i = 0; i < ntok; ++i) most = max(most, s_np[i]);
+    if (most > pb.top) {                                          // the same for every CTA of the cluster
+        float* c0 = s_c;
+        unsigned* err0 = s_err;
+        if (nclust > 1) {
+            c0 = cluster.map_shared_rank(s_c, 0);
+            err0 = cluster.map_shared_rank(s_err, 0);
+            cluster.sync();                                       // the first CTA runs and has cleared its errors
+        }
+        const int quad = lane & 3, row = lane >> 2;
+        for (int i0 = 0; i0 < ntok;) {                            // runs of tokens of one request
+            const int r = s_req[i0];
+            int i1 = i0 + 1;
+            while (i1 < ntok && s_req[i1] == r) ++i1;
+            int np = 0;
+            for (int i = i0; i < i1; ++i) np = max(np, s_np[i]);
+            const int ncand = np > pb.top ? np - pb.recent - pb.sink : 0, ncol = (i1 - i0) * g;
+            float worst[SEL_TOKENS];
+#pragma unroll
+            for (int i = 0; i < SEL_TOKENS; ++i) worst[i] = 0.f;
+            const int tile0 = rank * (SEL_THREADS / 32) + warp;
+            // Row n of the columns: token t0 + i0 + n / g, head n % g.  The lanes of a quad take 8 channels (16 bytes) each of a
+            // 32-channel block: words x and y are the two k pairs of one product, z and w of the next; q is dealt out alike.
+            uint4 qv[NC][DK];
+            auto load_q = [&](int cb) {
+#pragma unroll
+                for (int nc = 0; nc < NC; ++nc) {
+                    const int n = cb + nc * 8 + row;
+                    const __nv_bfloat16* p = q + (size_t)(t0 + i0 + (n < ncol ? n / g : 0)) * pb.q_stride + (size_t)(h * g + (n < ncol ? n % g : 0)) * d + quad * 8;
+#pragma unroll
+                    for (int k = 0; k < DK; ++k)
+                        qv[nc][k] = n < ncol && k * 32 + quad * 8 < d ? *reinterpret_cast<const uint4*>(p + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+                }
+            };
+            if (tile0 * 16 < ncand) load_q(0);
+            for (int tile = tile0; tile * 16 < ncand; tile += nclust * (SEL_THREADS / 32)) {
+                const int cand = tile * 16 + (lane & 15);
+                const int phys = cand < ncand ? paged_physical(pb, pv, r, pb.sink + cand) : -1;
+                const int pa = __shfl_sync(0xffffffffu, phys, row), pc = __shfl_sync(0xffffffffu, phys, row + 8);
+                const __nv_bfloat16* b = reinterpret_cast<const __nv_bfloat16*>(pv.bounds) + (size_t)h * 2 * d + quad * 8;
+                const __nv_bfloat16 *ba = b + (size_t)max(pa, 0) * pv.H * 2 * d, *bc = b + (size_t)max(pc, 0) * pv.H * 2 * d;
+                float best[SEL_TOKENS][2], mass[SEL_TOKENS][2];
+#pragma unroll
+                for (int i = 0; i < SEL_TOKENS; ++i) { best[i][0] = best[i][1] = -INFINITY; mass[i][0] = mass[i][1] = 0.f; }
+                for (int cb = 0; cb < ncol; cb += NC * 8) {
+                    if (ncol > NC * 8) load_q(cb);
+                    float s[NC][4], m[NC][4];
+#pragma unroll
+                    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[nc][e] = m[nc][e] = 0.f;
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {        // lo with min(q, 0), hi with max(q, 0)
+                        uint4 va[DK], vc[DK];
+#pragma unroll
+                        for (int k = 0; k < DK; ++k) {
+                            const bool on = k * 32 + quad * 8 < d;
+                            va[k] = on && pa >= 0 ? *reinterpret_cast<const uint4*>(ba + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+                            vc[k] = on && pc >= 0 ? *reinterpret_cast<const uint4*>(bc + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+                        }
+#pragma unroll
+                        for (int k = 0; k < DK; ++k) {
+                            const uint32_t a0[4] = {va[k].x, vc[k].x, va[k].y, vc[k].y}, a1[4] = {va[k].z, vc[k].z, va[k].w, vc[k].w};
+                            uint32_t z0[4], z1[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) { z0[e] = a0[e] & 0x7fff7fffu; z1[e] = a1[e] & 0x7fff7fffu; }
+#pragma unroll
+                            for (int nc = 0; nc < NC; ++nc) {
+                                if (cb + nc * 8 >= ncol) continue;
+                                const uint4 x = qv[nc][k];
+                                const uint32_t b0 = part ? clamp_pos(x.x) : clamp_neg(x.x), b1 = part ? clamp_pos(x.y) : clamp_neg(x.y);
+                                const uint32_t b2 = part ? clamp_pos(x.z) : clamp_neg(x.z), b3 = part ? clamp_pos(x.w) : clamp_neg(x.w);
+                                mma_bf16(s[nc], a0, b0, b1);
+                                mma_bf16(s[nc], a1, b2, b3);
+                                mma_bf16(m[nc], z0, b0 & 0x7fff7fffu, b1 & 0x7fff7fffu);
+                                mma_bf16(m[nc], z1, b2 & 0x7fff7fffu, b3 & 0x7fff7fffu);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {             // element e: page row + 8 (e / 2), column 2 quad + e % 2
+                            const int n = cb + nc * 8 + 2 * quad + (e & 1);
+                            if (n >= ncol) continue;
+                            const int tk = n / g;
+#pragma unroll
+                            for (int i = 0; i < SEL_TOKENS; ++i)
+                                if (i == tk) {
+                                    best[i][e >> 1] = fmaxf(best[i][e >> 1], s[nc][e]);
+                                    // what is not finite cannot be bounded
+                                    mass[i][e >> 1] = fmaxf(mass[i][e >> 1], m[nc][e] < 3.0e38f ? m[nc][e] : INFINITY);
+                                }
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < SEL_TOKENS; ++i) {
+                    if (i >= i1 - i0) break;
+#pragma unroll
+                    for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            best[i][e] = fmaxf(best[i][e], __shfl_xor_sync(0xffffffffu, best[i][e], o));
+                            mass[i][e] = fmaxf(mass[i][e], __shfl_xor_sync(0xffffffffu, mass[i][e], o));
+                        }
+                    if (quad < 2) {                               // lane 0 of the quad writes page `row`, lane 1 page `row + 8`
+                        const int cd = tile * 16 + row + 8 * quad;
+                        const int ph = quad ? pc : pa;
+                        if (cd < ncand) {
+                            c0[(size_t)(i0 + i) * W + cd] = ph < 0 ? -INFINITY : quad ? best[i][1] : best[i][0];
+                            if (ph >= 0 && cd < s_np[i0 + i] - pb.recent - pb.sink) worst[i] = fmaxf(worst[i], quad ? mass[i][1] : mass[i][0]);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < SEL_TOKENS; ++i) {
+                if (i >= i1 - i0) break;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) worst[i] = fmaxf(worst[i], __shfl_xor_sync(0xffffffffu, worst[i], o));
+                if (lane == 0 && worst[i] > 0.f) atomicMax(err0 + i0 + i, __float_as_uint(worst[i]));     // both >= 0: ordered as integers
+            }
+            i0 = i1;
+        }
+        if (nclust > 1) cluster.sync(); else __syncthreads();
+    }
+    if (rank != 0) return;
+
+    for (int i = 0; i < ntok; ++i) {
+        const int r = s_req[i], np = s_np[i], t = t0 + i;
+        if (r < 0) continue;
+        int32_t* sel = selected + ((size_t)t * pv.H + h) * pb.top;
+        if (np <= pb.top) {
+            for (int x = tid; x < pb.top; x += SEL_THREADS) sel[x] = x < np ? x : -1;
+            continue;
+        }
+        for (int x = tid; x < pb.sink; x += SEL_THREADS) sel[x] = x;
+        for (int x = tid; x < pb.recent; x += SEL_THREADS) sel[pb.top - pb.recent + x] = np - pb.recent + x;
+        const int m = pb.top - pb.sink - pb.recent, ncand = np - pb.recent - pb.sink;
+        if (m == 0) continue;
+        float* c = s_c + (size_t)i * W;
+        const float mass = __uint_as_float(s_err[i]);
+        const bool unbounded = !(mass < INFINITY);
+        const float e2 = __fadd_ru(__fmul_ru(mass, 2.0f * SEL_EPS), 1e-33f);      // 1e-33: products that underflow
+        // ---- the m-th largest fp32 score, to within e2: [a, b] always holds it.  Three pivots a step, counted by the whole
+        // block; the warps' counts alternate between two buffers, so a step has one barrier.
+        uint32_t a = 0u, b = ~0u;
+        if (!unbounded) {
+            uint32_t kmin = ~0u, kmax = 0u;
+            for (int x = tid; x < ncand; x += SEL_THREADS) {
+                const uint32_t k = orderable_key(c[x]);
+                kmin = min(kmin, k);
+                kmax = max(kmax, k);
+            }
+            kmin = __reduce_min_sync(0xffffffffu, kmin);
+            kmax = __reduce_max_sync(0xffffffffu, kmax);
+            if (lane == 0) s_cnt[0][warp] = make_uint2(kmin, kmax);
+            __syncthreads();
+            a = ~0u; b = 0u;
+#pragma unroll
+            for (int w = 0; w < SEL_THREADS / 32; ++w) { a = min(a, s_cnt[0][w].x); b = max(b, s_cnt[0][w].y); }
+            for (int step = 1; a < b && !(key_value(b) - key_value(a) <= e2); ++step) {
+                const uint32_t quarter = (b - a) / 4 + 1, p1 = a + quarter, p2 = min(b, p1 - 1 + quarter) + 1, p3 = min(b, p2 - 1 + quarter) + 1;
+                uint32_t n12 = 0, n3 = 0;                         // keys >= p1 (low half), >= p2 (high half); >= p3
+                for (int x = tid; x < ncand; x += SEL_THREADS) {
+                    const uint32_t k = orderable_key(c[x]);
+                    n12 += (k >= p1 ? 1u : 0u) + (k >= p2 ? 0x10000u : 0u);
+                    n3 += k >= p3 ? 1u : 0u;
+                }
+                n12 = __reduce_add_sync(0xffffffffu, n12);
+                n3 = __reduce_add_sync(0xffffffffu, n3);
+                uint2* buf = s_cnt[step & 1];
+                if (lane == 0) buf[warp] = make_uint2(n12, n3);
+                __syncthreads();
+                n12 = n3 = 0;
+#pragma unroll
+                for (int w = 0; w < SEL_THREADS / 32; ++w) { n12 += buf[w].x; n3 += buf[w].y; }
+                if ((int)n3 >= m) a = p3;
+                else if ((int)(n12 >> 16) >= m) { a = p2; b = p3 - 1; }
+                else if ((int)(n12 & 0xffffu) >= m) { a = p1; b = p2 - 1; }
+                else b = p1 - 1;
+            }
+            __syncthreads();                                      // the counts' buffers are free for the next token
+        }
+        const float in_above = unbounded ? INFINITY : __fadd_ru(key_value(b), e2), out_below = unbounded ? -INFINITY : __fadd_rd(key_value(a), -e2);
+        auto between = [&](float v) { return unbounded || (v <= in_above && v >= out_below); };
+        // ---- pages that are in for certain, pages in between
+        if (tid == 0) s_nlist = 0;
+        int sure = 0, n_between = 0;
+        __syncthreads();
+        for (int x = tid; x < ncand; x += SEL_THREADS) {
+            const float v = c[x];
+            if (between(v)) {
+                ++n_between;
+                const int at = atomicAdd(&s_nlist, 1);
+                if (at < SEL_LIST) s_list[at] = x;
+            } else if (v > in_above) ++sure;
+        }
+        int all_sure, all_between;
+        block_before(sure, s_warp, all_sure);
+        block_before(n_between, s_warp, all_between);
+        const int left = m - all_sure;                            // places for the pages in between
+        const __nv_bfloat16* bounds = reinterpret_cast<const __nv_bfloat16*>(pv.bounds);
+        const __nv_bfloat16* qt = q + (size_t)t * pb.q_stride + (size_t)h * g * d;
+        auto key_of = [&](int x) {
+            const int phys = paged_physical(pb, pv, r, pb.sink + x);
+            return phys < 0 ? 0ull : exact_key(bounds + ((size_t)phys * pv.H + h) * 2 * d, qt, g, d);
+        };
+        // A page in between is marked +inf (taken) or -inf.
+        if (left >= all_between) {
+            for (int x = tid; x < ncand; x += SEL_THREADS)
+                if (between(c[x])) c[x] = INFINITY;
+        } else if (all_between <= SEL_LIST) {
+            for (int x = warp; x < all_between; x += SEL_THREADS / 32) {
+                const u64 k = key_of(s_list[x]);
+                if (lane == 0) s_lkey[x] = k;
+            }
+            __syncthreads();
+            for (int x = tid; x < all_between; x += SEL_THREADS) {
+                const u64 k = s_lkey[x];
+                const int at = s_list[x];
+                int above = 0;
+                for (int y = 0; y < all_between; ++y) above += s_lkey[y] > k || (s_lkey[y] == k && s_list[y] < at);
+                c[at] = above < left ? INFINITY : -INFINITY;
+            }
+        } else {
+            for (int x = warp; x < ncand; x += SEL_THREADS / 32) {
+                if (!between(c[x])) continue;
+                const u64 k = key_of(x);
+                if (lane == 0) s_key[x] = k;
+            }
+            __syncthreads();
+            u64 kp = 0, km = 0;
+            int kn = left, kc = 0;
+            bool all = left == 0;
+            for (int shift = 56; shift >= 0 && !all; shift -= 8) {
+                for (int x = tid; x < 256; x += SEL_THREADS) s_hist[x] = 0;
+                __syncthreads();
+                for (int x = tid; x < ncand; x += SEL_THREADS)
+                    if (between(c[x]) && (s_key[x] & km) == kp) atomicAdd(&s_hist[(int)(s_key[x] >> shift) & 255], 1);
+                __syncthreads();
+                kp |= (u64)pick_digit(s_hist, s_pick, kn, kc) << shift;
+                km |= 255ull << shift;
+                all = kc == kn;
+                __syncthreads();
+            }
+            // equal keys: the lower pages; a thread takes a run of neighbouring pages, so one sum over the block counts those before
+            const int per = (ncand + SEL_THREADS - 1) / SEL_THREADS, x0 = min(ncand, tid * per), x1 = min(ncand, x0 + per);
+            int equal = 0, total;
+            for (int x = x0; x < x1; ++x) equal += between(c[x]) && (s_key[x] & km) == kp;
+            int before = block_before(equal, s_warp, total);
+            for (int x = x0; x < x1; ++x) {
+                if (!between(c[x])) continue;
+                const u64 k = s_key[x] & km;
+                bool take = left > 0 && k > kp;
+                if (k == kp) { take = left > 0 && before < kn; ++before; }
+                c[x] = take ? INFINITY : -INFINITY;
+            }
+        }
+        __syncthreads();
+        // ---- the pages taken, ascending
+        const int per = (ncand + SEL_THREADS - 1) / SEL_THREADS, x0 = min(ncand, tid * per), x1 = min(ncand, x0 + per);
+        int mine = 0, total;
+        for (int x = x0; x < x1; ++x) mine += c[x] > in_above || c[x] == INFINITY;
+        int at = pb.sink + block_before(mine, s_warp, total);
+        for (int x = x0; x < x1; ++x)
+            if (c[x] > in_above || c[x] == INFINITY) sel[at++] = pb.sink + x;
+        __syncthreads();
+    }
+}
+
+cudaError_t run_select_mma(const PagedView& pv, const PagedBatch& pb, const void* q, int32_t* selected, cudaStream_t st) {
+    // Several tokens of one unit share the walk over the bounds: as many as fill 16 columns, if requests have that many and
+    // enough units are left for the GPU.  Few units: a cluster shares the pages.
+    int ntok = 1;
+    while (ntok < SEL_TOKENS && ntok * 2 * pb.g <= 16 && ntok * 2 <= pb.T / pb.R && (long long)pb.T * pv.H / (ntok * 2) >= 2 * PAGED_SMS &&
+           (size_t)pb.W * (sizeof(u64) + ntok * 2 * sizeof(float)) <= (size_t)PAGED_SELECT_SMEM / 4) ntok *= 2;
+    const long long units = (long long)(pb.T + ntok - 1) / ntok * pv.H;
+    int nclust = 1;
+    while (nclust < 8 && units * nclust < 2 * PAGED_SMS && pb.W > 128 * nclust) nclust *= 2;
+    const size_t smem = (size_t)pb.W * (sizeof(u64) + ntok * sizeof(float));
+    auto go = [&](auto kernel, std::atomic<unsigned long long>& done) {
+        const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(kernel), PAGED_SELECT_SMEM, done);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(units * nclust));
+        cfg.blockDim = dim3(SEL_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = nclust;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        count_launch();
+        return cudaLaunchKernelEx(&cfg, kernel, pv, pb, (const __nv_bfloat16*)q, selected, nclust, ntok);
+    };
+    static std::atomic<unsigned long long> done2{0}, done4{0}, done8{0};
+    if (pv.d <= 64) return go(paged_select_mma_kernel<2>, done2);
+    if (pv.d <= 128) return go(paged_select_mma_kernel<4>, done4);
+    return go(paged_select_mma_kernel<8>, done8);
+}
+
+// ---------------------------------------------------------------- fp32
 template <typename T>
 cudaError_t run_select(const PagedView& pv, const PagedBatch& pb, const void* q, int32_t* selected, cudaStream_t st) {
     constexpr int E = 16 / (int)sizeof(T);
@@ -238,13 +675,13 @@ cudaError_t run_select(const PagedView& pv, const PagedBatch& pb, const void* q,
 }  // namespace
 
 size_t paged_select_smem(int W, int g, int d, int is_bf16) {
-    const int E = is_bf16 ? 8 : 4, chunks = (d / E + 7) / 8;
-    return (size_t)g * chunks * 8 * E * sizeof(double) + (size_t)W * sizeof(u64);
+    if (is_bf16) return (size_t)W * (sizeof(u64) + sizeof(float));
+    return (size_t)g * ((d / 4 + 7) / 8) * 8 * 4 * sizeof(double) + (size_t)W * sizeof(u64);
 }
 
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st) {
-    return is_bf16 ? run_select<__nv_bfloat16>(pv, pb, q, selected, st) : run_select<float>(pv, pb, q, selected, st);
+    return is_bf16 ? run_select_mma(pv, pb, q, selected, st) : run_select<float>(pv, pb, q, selected, st);
 }
 
 }  // namespace tkv

@@ -254,24 +254,54 @@ def test_sparse_attention_long_context(H, g, d, dtype):
     check_attention([3000], [130], H, g, d, dtype, top=8, sink=1, recent=1)
 
 
-def test_sparse_attention_ties_nan_and_infinite_bounds():
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sparse_attention_ties_nan_and_infinite_bounds(dtype):
     H, g, d = 1, 1, 64
-    c = Cache([64 * 40 + 3], H, d, torch.float32, DEV, 2)
-    q, cu = queries([1], 1, d, torch.float32, DEV, 2)
+    c = Cache([64 * 40 + 3], H, d, dtype, DEV, 2)
+    q, cu = queries([1], 1, d, dtype, DEV, 2)
     table = c.table[0].tolist()
     c.bounds[:] = 1.0                                                      # all scores equal: the lower pages win
     args = dict(sink_pages=0, recent_pages=1)
     call = lambda top: binding.paged_sparse_attention(c.k, c.v, c.bounds, q, ints(cu), c.lens, c.table, top, **args)[1][0, 0].tolist()
     assert call(6) == [0, 1, 2, 3, 4, 40]
+    best = int(q[0, 0].float().argmax())
     c.bounds[table[30]] = float("nan")                                     # what cannot be bounded is read
-    c.bounds[table[20], :, 1, int(q[0, 0].argmax())] = float("inf")
-    c.bounds[table[10], :, :, int(q[0, 0].argmax())] = -float("inf")       # the last to be taken
+    c.bounds[table[20], :, 1, best] = float("inf")
+    c.bounds[table[10], :, :, best] = -float("inf")                        # the last to be taken
     assert call(4) == [0, 20, 30, 40]
     assert call(40) == [p for p in range(41) if p != 10]
     assert call(41) == list(range(41))
     c.bounds[:] = -0.0
     c.bounds[table[7]] = 0.0                                               # -0 and +0 are the same score
     assert call(3) == [0, 1, 40]
+
+
+@pytest.mark.parametrize("step", [0.0, 1.0])
+def test_sparse_attention_scores_that_only_64_bits_tell_apart(step):
+    """More pages than the short list ranks, their scores equal (step 0) or apart by less than fp32 sums can tell: one small
+    channel differs, beside channels that cancel to the same large sum."""
+    H, g, d, n = 1, 2, 128, 700
+    c = Cache([64 * n + 1], H, d, torch.bfloat16, DEV, 3)
+    q = torch.ones(1, g, d, dtype=torch.bfloat16, device=DEV)
+    q[0, :, 5] = 2.0 ** -20
+    order = list(range(n))
+    random.Random(1).shuffle(order)
+    c.bounds[:] = 300.0
+    c.bounds[:, :, :, 64:] = -299.0
+    for rank, page in enumerate(order):
+        c.bounds[c.table[0, page].item(), :, :, 5] = step * (rank % 233 + 1) / 256.0 + 1.0
+    for top in (2, 100, 600, 700):
+        sel = binding.paged_sparse_attention(c.k, c.v, c.bounds, q, ints([0, 1]), c.lens, c.table, top)[1][0, 0].tolist()
+        u = {p: float(c.bounds[c.table[0, p].item(), 0, 1, 5]) for p in range(n)}
+        want = sorted(sorted(range(n), key=lambda p: (-u[p], p))[:top - 1]) + [n]
+        assert sel == want
+
+
+def test_sparse_attention_tokens_that_share_a_unit():
+    """Many tokens of few requests: several tokens walk the bounds together; some see fewer pages than they may select."""
+    check_attention([420, 390, 130], [200, 101, 130], 8, 4, 64, torch.bfloat16, top=4, sink=1, recent=1, pad=3)
+    check_attention([500, 260], [260, 255], 6, 7, 128, torch.bfloat16, top=3)
+    check_attention([330], [329], 4, 16, 64, torch.bfloat16, top=2)
 
 
 # ---------------------------------------------------------------- together

@@ -118,14 +118,14 @@ def test_binding_refuses_wrong_tensors():
         binding.paged_append(kp, kp, kp[:1, :, 0], kp[:1, :, 0], i)
     with pytest.raises(ValueError):
         binding.paged_plan(i, i, i, i[None], i, i, i, i, i, i)
-    dev = torch.device("cpu")
+    dev = -1                                                               # what get_device says of a CPU tensor
     for bad in (torch.zeros(3, 4, 64)[:, :, ::2], torch.zeros(3, 8, 32)[:, ::2], torch.zeros(3, 4, 32, dtype=torch.float64), torch.zeros(3, 5, 32), torch.zeros(3, 128)):
         with pytest.raises(ValueError):
             binding._rows(dev, "q", bad, torch.float32, 4, 32)
     assert binding._rows(dev, "q", torch.zeros(3, 6, 32)[:, :4], torch.float32, 4, 32)[1] == 192       # strided tokens
     for bad in (torch.zeros(3, 4)[:, ::2], torch.zeros(4), torch.zeros(3, 4, dtype=torch.int64), torch.zeros(2, 4)):
         with pytest.raises(ValueError):
-            binding._on(dev, "x", bad, torch.float32, 3, 4)
+            binding._on(dev, "x", bad, torch.float32, (3, 4))
 
 
 # ---- the plain statements themselves
