@@ -271,7 +271,7 @@ cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* kee
 cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_pages, char* bounds, int is_bf16, int T, const void* k,
                                 long long k_stride, const void* v, long long v_stride, const int32_t* slot_map, int32_t* status,
                                 cudaStream_t st);
-constexpr int PAGED_SELECT_SMEM = 200 * 1024;
+constexpr int PAGED_SELECT_SMEM = 196 * 1024;
 size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st);

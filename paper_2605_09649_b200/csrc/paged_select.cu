@@ -12,9 +12,10 @@
 //
 // bf16 (paged_select_mma_kernel): the tensor cores compute U for 16 pages x 8 rows at a time in fp32, and beside it the
 // sum of the terms' magnitudes A, the same product of absolute values.  An fp32 sum of 2 d <= 512 exact products is off by
-// less than A 2^-14 whatever the order and the rounding of its additions (512 additions of relative error 2^-23).  A
-// bisection over the fp32 scores brackets the m-th largest to [a, b], b - a <= 2 E (E: the largest error of the token's
-// pages); pages above b + 2 E are in, pages below a - 2 E are out, and the few in between are scored again in 64 bits.  If all are in
+// less than A 2^-14 whatever the order and the rounding of its additions (512 additions of relative error 2^-23).  The
+// m-th largest fp32 score is bracketed to [a, b] (a warp alone: by bisection; the block: by one histogram); pages above
+// b + 2 E are in, pages below a - 2 E are out (E: the largest error of the token's pages), and the few in between
+// are scored again in 64 bits.  If all are in
 // between (equal bounds, infinities, NaN) all are, and a descent over 64-bit keys decides.  Bound by the latency of its
 // chain (table, bounds, descent); the bounds are read once per group of tokens.
 //
@@ -218,7 +219,9 @@ paged_select_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, int32_
 
 // ---------------------------------------------------------------- bf16: tensor cores, then 64 bits where it matters
 constexpr int SEL_TOKENS = 4;                 // tokens of one unit, at most
-constexpr int SEL_LIST = 512;                 // pages between the thresholds that are ranked by counting
+constexpr int SEL_WARP_MAX = 512;             // a warp alone settles a token with up to this many candidates
+constexpr int SEL_WARP_LIST = 32, SEL_LIST = 512;   // pages between the thresholds that are ranked by counting (warp, block)
+constexpr int SEL_BINS = 1024;
 constexpr float SEL_EPS = 1.0f / 16384.0f;    // 2^-14, see above
 
 __device__ __forceinline__ uint32_t clamp_neg(uint32_t v) {
@@ -229,30 +232,38 @@ __device__ __forceinline__ uint32_t clamp_pos(uint32_t v) {
     const __nv_bfloat162 z = __float2bfloat162_rn(0.f), x = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&v), z);
     return *reinterpret_cast<const uint32_t*>(&x);
 }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-// The 64-bit key of one page, by a whole warp.
-__device__ __forceinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat16* q, int g, int d) {
-    const int lane = threadIdx.x & 31;
+// The 64-bit key of one page, by a whole warp: eight lanes per head, 8 channels per lane and step.
+__device__ __noinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat16* q, int g, int d) {
+    const int lane = threadIdx.x & 31, l = lane & 7;
     double best = -INFINITY;
     bool nan = false;
-    for (int head = 0; head < g; ++head) {
+    for (int h0 = 0; h0 < g; h0 += 4) {
+        const int head = h0 + (lane >> 3);
         double s = 0.0;
-        for (int c = 2 * lane; c < d; c += 64) {
-            const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(q + (size_t)head * d + c));
-            const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(b + c));
-            const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(b + d + c));
-            s = fma((double)x.x, (double)(x.x > 0.f ? hi.x : lo.x), s);
-            s = fma((double)x.y, (double)(x.y > 0.f ? hi.y : lo.y), s);
+        for (int c = l * 8; c < d; c += 64) {
+            const uint4 vq = head < g ? *reinterpret_cast<const uint4*>(q + (size_t)head * d + c) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 vlo = *reinterpret_cast<const uint4*>(b + c), vhi = *reinterpret_cast<const uint4*>(b + d + c);
+            const __nv_bfloat16 *xq = reinterpret_cast<const __nv_bfloat16*>(&vq), *xlo = reinterpret_cast<const __nv_bfloat16*>(&vlo),
+                                *xhi = reinterpret_cast<const __nv_bfloat16*>(&vhi);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __bfloat162float(xq[e]);
+                s = fma((double)x, (double)__bfloat162float(x > 0.f ? xhi[e] : xlo[e]), s);
+            }
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        nan |= s != s;
-        best = fmax(best, s);
+        for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (head < g) {
+            nan |= s != s;
+            best = fmax(best, s);
+        }
     }
-    return score_key(nan ? (double)NAN : best);
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1) best = fmax(best, __shfl_xor_sync(0xffffffffu, best, o));
+    return score_key(__any_sync(0xffffffffu, nan) ? (double)NAN : best);
 }
-
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // Sum over the block of each thread's value, and the sum over the threads before it.
 __device__ __forceinline__ int block_before(int v, int* s_warp, int& total) {
@@ -304,17 +315,229 @@ __device__ __forceinline__ int pick_digit(const int* s_hist, int* s_pick, int& n
     return s_pick[0];
 }
 
-// grid = ceil(T / ntok) * H clusters.  Dynamic shared memory: scores [ntok][W] fp32, then 64-bit keys [W].
-template <int DK>      // ceil(d / 32)
+// One token's selection: n candidates (pages sink ..), of which m < n are taken; scores c[n]; the places of the pages
+// taken go to sel[0 .. m), ascending.
+struct SelTask {
+    const PagedView* pv;
+    const PagedBatch* pb;
+    int r, h, n, m;
+    const __nv_bfloat16* q;       // the token's group of query heads
+    float* c;
+    float mass;                   // largest A of the candidates
+    int32_t* sel;
+    __device__ __forceinline__ u64 key(int x) const {
+        const int phys = paged_physical(*pb, *pv, r, pb->sink + x);
+        return phys < 0 ? 0ull : exact_key(reinterpret_cast<const __nv_bfloat16*>(pv->bounds) + ((size_t)phys * pv->H + h) * 2 * pv->d, q, pb->g, pv->d);
+    }
+};
+// The band around the m-th largest fp32 score in which 64 bits decide; above it a page is in, below it out.
+struct SelBand {
+    float below, above;
+    bool everything;              // scores that cannot be bounded: all pages are in the band
+    __device__ __forceinline__ bool holds(float v) const { return everything || (v <= above && v >= below); }
+    __device__ __forceinline__ bool in(float v) const { return !everything && v > above; }
+};
+__device__ __forceinline__ float sel_slack(float mass) { return __fadd_ru(__fmul_ru(mass, 2.0f * SEL_EPS), 1e-33f); }   // 1e-33: products that underflow
+
+// By one warp.  false: too many pages in the band, nothing written.
+__device__ __forceinline__ bool select_by_warp(const SelTask& k, int* list, u64* lkey) {
+    const int lane = threadIdx.x & 31;
+    if (!(k.mass < INFINITY)) return false;
+    const float e2 = sel_slack(k.mass);
+    // [a, b] holds the m-th largest; three pivots a step until it is narrower than the slack
+    uint32_t a = ~0u, b = 0u;
+    for (int x = lane; x < k.n; x += 32) {
+        const uint32_t v = orderable_key(k.c[x]);
+        a = min(a, v);
+        b = max(b, v);
+    }
+    a = __reduce_min_sync(0xffffffffu, a);
+    b = __reduce_max_sync(0xffffffffu, b);
+    while (a < b && !(key_value(b) - key_value(a) <= e2)) {
+        const uint32_t quarter = (b - a) / 4 + 1, p1 = a + quarter, p2 = min(b, p1 - 1 + quarter) + 1, p3 = min(b, p2 - 1 + quarter) + 1;
+        uint32_t n12 = 0, n3 = 0;                                 // keys >= p1 (low half), >= p2 (high half); >= p3
+        for (int x = lane; x < k.n; x += 32) {
+            const uint32_t v = orderable_key(k.c[x]);
+            n12 += (v >= p1 ? 1u : 0u) + (v >= p2 ? 0x10000u : 0u);
+            n3 += v >= p3 ? 1u : 0u;
+        }
+        n12 = __reduce_add_sync(0xffffffffu, n12);
+        n3 = __reduce_add_sync(0xffffffffu, n3);
+        if ((int)n3 >= k.m) a = p3;
+        else if ((int)(n12 >> 16) >= k.m) { a = p2; b = p3 - 1; }
+        else if ((int)(n12 & 0xffffu) >= k.m) { a = p1; b = p2 - 1; }
+        else b = p1 - 1;
+    }
+    const SelBand band = {__fadd_rd(key_value(a), -e2), __fadd_ru(key_value(b), e2), false};
+    int sure = 0, held = 0;
+    for (int x0 = 0; x0 < k.n; x0 += 32) {
+        const float v = x0 + lane < k.n ? k.c[x0 + lane] : -INFINITY;
+        const unsigned hold = __ballot_sync(0xffffffffu, x0 + lane < k.n && band.holds(v));
+        sure += __popc(__ballot_sync(0xffffffffu, x0 + lane < k.n && band.in(v)));
+        const int at = held + __popc(hold & ((1u << lane) - 1u));
+        if (((hold >> lane) & 1u) && at < SEL_WARP_LIST) list[at] = x0 + lane;
+        held += __popc(hold);
+    }
+    const int left = k.m - sure;
+    if (left < held) {
+        if (held > SEL_WARP_LIST) return false;
+        __syncwarp();
+        for (int i = 0; i < held; ++i) {
+            const u64 key = k.key(list[i]);
+            if (lane == 0) lkey[i] = key;
+        }
+        __syncwarp();
+        if (lane < held) {                                        // the list ascends: among equal keys the lower page comes first
+            const u64 key = lkey[lane];
+            int above = 0;
+            for (int i = 0; i < held; ++i) above += lkey[i] > key || (lkey[i] == key && i < lane);
+            k.c[list[lane]] = above < left ? INFINITY : -INFINITY;
+        }
+        __syncwarp();
+    }
+    int at = 0;
+    for (int x0 = 0; x0 < k.n; x0 += 32) {
+        const float v = x0 + lane < k.n ? k.c[x0 + lane] : -INFINITY;
+        // (with places for the whole band its pages are unmarked, else marked +inf or -inf)
+        const bool take = x0 + lane < k.n && (band.in(v) || (left >= held && band.holds(v)));
+        const unsigned t = __ballot_sync(0xffffffffu, take);
+        if (take) k.sel[at + __popc(t & ((1u << lane) - 1u))] = x0 + lane + k.pb->sink;
+        at += __popc(t);
+    }
+    return true;
+}
+
+struct SelShared {
+    int hist[SEL_BINS], pick[3], warp[SEL_THREADS / 32], nlist, list[SEL_LIST];
+    uint2 range[SEL_THREADS / 32];
+    u64 lkey[SEL_LIST];
+};
+
+// By the block; keys: [n] 64-bit words of shared memory.
+__device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u64* keys) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    SelBand band = {-INFINITY, INFINITY, !(k.mass < INFINITY)};
+    __syncthreads();
+    for (int i = tid; i < SEL_BINS; i += SEL_THREADS) sh.hist[i] = 0;
+    if (tid == 0) sh.nlist = 0;
+    if (!band.everything) {
+        // one histogram over [min, max]: the bin in which the count from the top reaches m, widened by the slack
+        uint32_t kmin = ~0u, kmax = 0u;
+        for (int x = tid; x < k.n; x += SEL_THREADS) {
+            const uint32_t v = orderable_key(k.c[x]);
+            kmin = min(kmin, v);
+            kmax = max(kmax, v);
+        }
+        kmin = __reduce_min_sync(0xffffffffu, kmin);
+        kmax = __reduce_max_sync(0xffffffffu, kmax);
+        if (lane == 0) sh.range[warp] = make_uint2(kmin, kmax);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < SEL_THREADS / 32; ++w) { kmin = min(kmin, sh.range[w].x); kmax = max(kmax, sh.range[w].y); }
+        // the bin of a key: monotone in the key, exact integers
+        const uint32_t span = kmax - kmin;
+        const int shift = max(0, 32 - __clz((int)span) - 10);     // span >> shift < 1024 (span = 0: shift 0)
+        for (int x = tid; x < k.n; x += SEL_THREADS) atomicAdd(&sh.hist[(orderable_key(k.c[x]) - kmin) >> shift], 1);
+        __syncthreads();
+        int c[4], sum = 0, total;                                 // thread t: bins 1023 - 4 t down to 1020 - 4 t
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { c[i] = sh.hist[SEL_BINS - 1 - 4 * tid - i]; sum += c[i]; }
+        int run = block_before(sum, sh.warp, total);
+        if (run < k.m && k.m <= run + sum) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (run < k.m && k.m <= run + c[i]) sh.pick[0] = SEL_BINS - 1 - 4 * tid - i;
+                run += c[i];
+            }
+        }
+        __syncthreads();
+        const uint32_t a = kmin + ((uint32_t)sh.pick[0] << shift), b = min(kmax, a + ((1u << shift) - 1u));
+        const float e2 = sel_slack(k.mass);
+        band.below = __fadd_rd(key_value(a), -e2);
+        band.above = __fadd_ru(key_value(b), e2);
+    } else
+        __syncthreads();
+    int sure = 0, held = 0;
+    for (int x = tid; x < k.n; x += SEL_THREADS) {
+        const float v = k.c[x];
+        if (band.holds(v)) {
+            ++held;
+            const int at = atomicAdd(&sh.nlist, 1);
+            if (at < SEL_LIST) sh.list[at] = x;
+        } else if (band.in(v)) ++sure;
+    }
+    int all_sure, all_held;
+    block_before(sure | (held << 16), sh.warp, all_sure);         // n <= 16384: both fit
+    all_held = all_sure >> 16;
+    all_sure &= 0xffff;
+    const int left = k.m - all_sure;                              // places for the pages of the band; marked +inf (taken) or -inf
+    if (left >= all_held) {
+        for (int x = tid; x < k.n; x += SEL_THREADS)
+            if (band.holds(k.c[x])) k.c[x] = INFINITY;
+    } else if (all_held <= SEL_LIST) {
+        for (int x = warp; x < all_held; x += SEL_THREADS / 32) {
+            const u64 key = k.key(sh.list[x]);
+            if (lane == 0) sh.lkey[x] = key;
+        }
+        __syncthreads();
+        for (int x = tid; x < all_held; x += SEL_THREADS) {
+            const u64 key = sh.lkey[x];
+            const int at = sh.list[x];
+            int above = 0;
+            for (int y = 0; y < all_held; ++y) above += sh.lkey[y] > key || (sh.lkey[y] == key && sh.list[y] < at);
+            k.c[at] = above < left ? INFINITY : -INFINITY;
+        }
+    } else {
+        for (int x = warp; x < k.n; x += SEL_THREADS / 32) {
+            if (!band.holds(k.c[x])) continue;
+            const u64 key = k.key(x);
+            if (lane == 0) keys[x] = key;
+        }
+        u64 kp = 0, km = 0;
+        int kn = left, kc = 0;
+        bool all = false;                                         // every key that matches the prefix is taken
+        for (int shift = 56; shift >= 0 && !all; shift -= 8) {
+            __syncthreads();
+            for (int x = tid; x < 256; x += SEL_THREADS) sh.hist[x] = 0;
+            __syncthreads();
+            for (int x = tid; x < k.n; x += SEL_THREADS)
+                if (band.holds(k.c[x]) && (keys[x] & km) == kp) atomicAdd(&sh.hist[(int)(keys[x] >> shift) & 255], 1);
+            __syncthreads();
+            kp |= (u64)pick_digit(sh.hist, sh.pick, kn, kc) << shift;
+            km |= 255ull << shift;
+            all = kc == kn;
+        }
+        // equal keys: the lower pages; a thread takes a run of neighbouring pages, so one sum over the block counts those before
+        const int per = (k.n + SEL_THREADS - 1) / SEL_THREADS, x0 = min(k.n, tid * per), x1 = min(k.n, x0 + per);
+        int equal = 0, total;
+        for (int x = x0; x < x1; ++x) equal += band.holds(k.c[x]) && (keys[x] & km) == kp;
+        int before = block_before(equal, sh.warp, total);
+        for (int x = x0; x < x1; ++x) {
+            if (!band.holds(k.c[x])) continue;
+            const u64 key = keys[x] & km;
+            bool take = key > kp;
+            if (key == kp) { take = before < kn; ++before; }
+            k.c[x] = take ? INFINITY : -INFINITY;
+        }
+    }
+    __syncthreads();
+    const int per = (k.n + SEL_THREADS - 1) / SEL_THREADS, x0 = min(k.n, tid * per), x1 = min(k.n, x0 + per);
+    int mine = 0, total;
+    for (int x = x0; x < x1; ++x) mine += band.in(k.c[x]) || k.c[x] == INFINITY;
+    int at = block_before(mine, sh.warp, total);
+    for (int x = x0; x < x1; ++x)
+        if (band.in(k.c[x]) || k.c[x] == INFINITY) k.sel[at++] = k.pb->sink + x;
+}
+
+// grid = ceil(T / ntok) * H clusters.  Dynamic shared memory: 64-bit keys [W], then scores [ntok][W] fp32.
+// DK: ceil(d / 32).  NTOK: 1, or up to SEL_TOKENS.  NC: column tiles (8 rows of q each) per walk over the bounds.
+template <int DK, int NTOK, int NC>
 __global__ void __launch_bounds__(SEL_THREADS, DK <= 4 ? 2 : 1)
 paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __restrict__ q, int32_t* __restrict__ selected, int nclust, int ntok) {
-    constexpr int NC = 2;                                         // column tiles (8 rows of q each) per walk over the bounds
     extern __shared__ __align__(16) unsigned char s_raw[];
-    __shared__ int s_req[SEL_TOKENS], s_np[SEL_TOKENS];           // request of each token (-1: none), pages up to its own
-    __shared__ unsigned s_err[SEL_TOKENS];
-    __shared__ int s_hist[256], s_pick[3], s_warp[SEL_THREADS / 32], s_nlist, s_list[SEL_LIST];
-    __shared__ u64 s_lkey[SEL_LIST];
-    __shared__ uint2 s_cnt[2][SEL_THREADS / 32];
+    __shared__ int s_req[NTOK], s_np[NTOK], s_hard[NTOK];         // request of each token (-1: none), pages up to its own
+    __shared__ unsigned s_err[NTOK];
+    __shared__ SelShared sh;
     grid_dependents_may_launch();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)blockIdx.x % nclust, unit = (int)blockIdx.x / nclust;
@@ -356,10 +579,9 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
             int np = 0;
             for (int i = i0; i < i1; ++i) np = max(np, s_np[i]);
             const int ncand = np > pb.top ? np - pb.recent - pb.sink : 0, ncol = (i1 - i0) * g;
-            float worst[SEL_TOKENS];
+            float worst[NTOK];
 #pragma unroll
-            for (int i = 0; i < SEL_TOKENS; ++i) worst[i] = 0.f;
-            const int tile0 = rank * (SEL_THREADS / 32) + warp;
+            for (int i = 0; i < NTOK; ++i) worst[i] = 0.f;
             // Row n of the columns: token t0 + i0 + n / g, head n % g.  The lanes of a quad take 8 channels (16 bytes) each of a
             // 32-channel block: words x and y are the two k pairs of one product, z and w of the next; q is dealt out alike.
             uint4 qv[NC][DK];
@@ -373,6 +595,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                         qv[nc][k] = n < ncol && k * 32 + quad * 8 < d ? *reinterpret_cast<const uint4*>(p + k * 32) : make_uint4(0u, 0u, 0u, 0u);
                 }
             };
+            const int tile0 = rank * (SEL_THREADS / 32) + warp;
             if (tile0 * 16 < ncand) load_q(0);
             for (int tile = tile0; tile * 16 < ncand; tile += nclust * (SEL_THREADS / 32)) {
                 const int cand = tile * 16 + (lane & 15);
@@ -380,9 +603,9 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                 const int pa = __shfl_sync(0xffffffffu, phys, row), pc = __shfl_sync(0xffffffffu, phys, row + 8);
                 const __nv_bfloat16* b = reinterpret_cast<const __nv_bfloat16*>(pv.bounds) + (size_t)h * 2 * d + quad * 8;
                 const __nv_bfloat16 *ba = b + (size_t)max(pa, 0) * pv.H * 2 * d, *bc = b + (size_t)max(pc, 0) * pv.H * 2 * d;
-                float best[SEL_TOKENS][2], mass[SEL_TOKENS][2];
+                float best[NTOK][2], mass[NTOK][2];
 #pragma unroll
-                for (int i = 0; i < SEL_TOKENS; ++i) { best[i][0] = best[i][1] = -INFINITY; mass[i][0] = mass[i][1] = 0.f; }
+                for (int i = 0; i < NTOK; ++i) { best[i][0] = best[i][1] = -INFINITY; mass[i][0] = mass[i][1] = 0.f; }
                 for (int cb = 0; cb < ncol; cb += NC * 8) {
                     if (ncol > NC * 8) load_q(cb);
                     float s[NC][4], m[NC][4];
@@ -390,24 +613,26 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                     for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[nc][e] = m[nc][e] = 0.f;
+                    uint4 va[2][DK], vc[2][DK];                   // lo, hi of the two pages of this lane's rows
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) {        // lo with min(q, 0), hi with max(q, 0)
-                        uint4 va[DK], vc[DK];
+                    for (int part = 0; part < 2; ++part)
 #pragma unroll
                         for (int k = 0; k < DK; ++k) {
                             const bool on = k * 32 + quad * 8 < d;
-                            va[k] = on && pa >= 0 ? *reinterpret_cast<const uint4*>(ba + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
-                            vc[k] = on && pc >= 0 ? *reinterpret_cast<const uint4*>(bc + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+                            va[part][k] = on && pa >= 0 ? *reinterpret_cast<const uint4*>(ba + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+                            vc[part][k] = on && pc >= 0 ? *reinterpret_cast<const uint4*>(bc + part * d + k * 32) : make_uint4(0u, 0u, 0u, 0u);
                         }
 #pragma unroll
+                    for (int part = 0; part < 2; ++part)          // lo with min(q, 0), hi with max(q, 0)
+#pragma unroll
                         for (int k = 0; k < DK; ++k) {
-                            const uint32_t a0[4] = {va[k].x, vc[k].x, va[k].y, vc[k].y}, a1[4] = {va[k].z, vc[k].z, va[k].w, vc[k].w};
+                            const uint4 xa = va[part][k], xc = vc[part][k];
+                            const uint32_t a0[4] = {xa.x, xc.x, xa.y, xc.y}, a1[4] = {xa.z, xc.z, xa.w, xc.w};
                             uint32_t z0[4], z1[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) { z0[e] = a0[e] & 0x7fff7fffu; z1[e] = a1[e] & 0x7fff7fffu; }
 #pragma unroll
                             for (int nc = 0; nc < NC; ++nc) {
-                                if (cb + nc * 8 >= ncol) continue;
                                 const uint4 x = qv[nc][k];
                                 const uint32_t b0 = part ? clamp_pos(x.x) : clamp_neg(x.x), b1 = part ? clamp_pos(x.y) : clamp_neg(x.y);
                                 const uint32_t b2 = part ? clamp_pos(x.z) : clamp_neg(x.z), b3 = part ? clamp_pos(x.w) : clamp_neg(x.w);
@@ -417,25 +642,26 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                                 mma_bf16(m[nc], z1, b2 & 0x7fff7fffu, b3 & 0x7fff7fffu);
                             }
                         }
-                    }
 #pragma unroll
                     for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {             // element e: page row + 8 (e / 2), column 2 quad + e % 2
-                            const int n = cb + nc * 8 + 2 * quad + (e & 1);
+                        for (int cc = 0; cc < 2; ++cc) {          // column 2 quad + cc; elements cc, cc + 2: page rows row, row + 8
+                            const int n = cb + nc * 8 + 2 * quad + cc;
                             if (n >= ncol) continue;
-                            const int tk = n / g;
+                            const int tk = NTOK == 1 ? 0 : n / g;
 #pragma unroll
-                            for (int i = 0; i < SEL_TOKENS; ++i)
-                                if (i == tk) {
-                                    best[i][e >> 1] = fmaxf(best[i][e >> 1], s[nc][e]);
-                                    // what is not finite cannot be bounded
-                                    mass[i][e >> 1] = fmaxf(mass[i][e >> 1], m[nc][e] < 3.0e38f ? m[nc][e] : INFINITY);
-                                }
+                            for (int i = 0; i < NTOK; ++i)
+                                if (NTOK == 1 || i == tk)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        best[i][e] = fmaxf(best[i][e], s[nc][cc + 2 * e]);
+                                        // what is not finite cannot be bounded
+                                        mass[i][e] = fmaxf(mass[i][e], m[nc][cc + 2 * e] < 3.0e38f ? m[nc][cc + 2 * e] : INFINITY);
+                                    }
                         }
                 }
 #pragma unroll
-                for (int i = 0; i < SEL_TOKENS; ++i) {
+                for (int i = 0; i < NTOK; ++i) {
                     if (i >= i1 - i0) break;
 #pragma unroll
                     for (int o = 1; o < 4; o <<= 1)
@@ -455,7 +681,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                 }
             }
 #pragma unroll
-            for (int i = 0; i < SEL_TOKENS; ++i) {
+            for (int i = 0; i < NTOK; ++i) {
                 if (i >= i1 - i0) break;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) worst[i] = fmaxf(worst[i], __shfl_xor_sync(0xffffffffu, worst[i], o));
@@ -467,147 +693,38 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
     }
     if (rank != 0) return;
 
-    for (int i = 0; i < ntok; ++i) {
-        const int r = s_req[i], np = s_np[i], t = t0 + i;
-        if (r < 0) continue;
-        int32_t* sel = selected + ((size_t)t * pv.H + h) * pb.top;
-        if (np <= pb.top) {
-            for (int x = tid; x < pb.top; x += SEL_THREADS) sel[x] = x < np ? x : -1;
-            continue;
-        }
-        for (int x = tid; x < pb.sink; x += SEL_THREADS) sel[x] = x;
-        for (int x = tid; x < pb.recent; x += SEL_THREADS) sel[pb.top - pb.recent + x] = np - pb.recent + x;
-        const int m = pb.top - pb.sink - pb.recent, ncand = np - pb.recent - pb.sink;
-        if (m == 0) continue;
-        float* c = s_c + (size_t)i * W;
-        const float mass = __uint_as_float(s_err[i]);
-        const bool unbounded = !(mass < INFINITY);
-        const float e2 = __fadd_ru(__fmul_ru(mass, 2.0f * SEL_EPS), 1e-33f);      // 1e-33: products that underflow
-        // ---- the m-th largest fp32 score, to within e2: [a, b] always holds it.  Three pivots a step, counted by the whole
-        // block; the warps' counts alternate between two buffers, so a step has one barrier.
-        uint32_t a = 0u, b = ~0u;
-        if (!unbounded) {
-            uint32_t kmin = ~0u, kmax = 0u;
-            for (int x = tid; x < ncand; x += SEL_THREADS) {
-                const uint32_t k = orderable_key(c[x]);
-                kmin = min(kmin, k);
-                kmax = max(kmax, k);
-            }
-            kmin = __reduce_min_sync(0xffffffffu, kmin);
-            kmax = __reduce_max_sync(0xffffffffu, kmax);
-            if (lane == 0) s_cnt[0][warp] = make_uint2(kmin, kmax);
-            __syncthreads();
-            a = ~0u; b = 0u;
-#pragma unroll
-            for (int w = 0; w < SEL_THREADS / 32; ++w) { a = min(a, s_cnt[0][w].x); b = max(b, s_cnt[0][w].y); }
-            for (int step = 1; a < b && !(key_value(b) - key_value(a) <= e2); ++step) {
-                const uint32_t quarter = (b - a) / 4 + 1, p1 = a + quarter, p2 = min(b, p1 - 1 + quarter) + 1, p3 = min(b, p2 - 1 + quarter) + 1;
-                uint32_t n12 = 0, n3 = 0;                         // keys >= p1 (low half), >= p2 (high half); >= p3
-                for (int x = tid; x < ncand; x += SEL_THREADS) {
-                    const uint32_t k = orderable_key(c[x]);
-                    n12 += (k >= p1 ? 1u : 0u) + (k >= p2 ? 0x10000u : 0u);
-                    n3 += k >= p3 ? 1u : 0u;
-                }
-                n12 = __reduce_add_sync(0xffffffffu, n12);
-                n3 = __reduce_add_sync(0xffffffffu, n3);
-                uint2* buf = s_cnt[step & 1];
-                if (lane == 0) buf[warp] = make_uint2(n12, n3);
-                __syncthreads();
-                n12 = n3 = 0;
-#pragma unroll
-                for (int w = 0; w < SEL_THREADS / 32; ++w) { n12 += buf[w].x; n3 += buf[w].y; }
-                if ((int)n3 >= m) a = p3;
-                else if ((int)(n12 >> 16) >= m) { a = p2; b = p3 - 1; }
-                else if ((int)(n12 & 0xffffu) >= m) { a = p1; b = p2 - 1; }
-                else b = p1 - 1;
-            }
-            __syncthreads();                                      // the counts' buffers are free for the next token
-        }
-        const float in_above = unbounded ? INFINITY : __fadd_ru(key_value(b), e2), out_below = unbounded ? -INFINITY : __fadd_rd(key_value(a), -e2);
-        auto between = [&](float v) { return unbounded || (v <= in_above && v >= out_below); };
-        // ---- pages that are in for certain, pages in between
-        if (tid == 0) s_nlist = 0;
-        int sure = 0, n_between = 0;
-        __syncthreads();
-        for (int x = tid; x < ncand; x += SEL_THREADS) {
-            const float v = c[x];
-            if (between(v)) {
-                ++n_between;
-                const int at = atomicAdd(&s_nlist, 1);
-                if (at < SEL_LIST) s_list[at] = x;
-            } else if (v > in_above) ++sure;
-        }
-        int all_sure, all_between;
-        block_before(sure, s_warp, all_sure);
-        block_before(n_between, s_warp, all_between);
-        const int left = m - all_sure;                            // places for the pages in between
-        const __nv_bfloat16* bounds = reinterpret_cast<const __nv_bfloat16*>(pv.bounds);
-        const __nv_bfloat16* qt = q + (size_t)t * pb.q_stride + (size_t)h * g * d;
-        auto key_of = [&](int x) {
-            const int phys = paged_physical(pb, pv, r, pb.sink + x);
-            return phys < 0 ? 0ull : exact_key(bounds + ((size_t)phys * pv.H + h) * 2 * d, qt, g, d);
-        };
-        // A page in between is marked +inf (taken) or -inf.
-        if (left >= all_between) {
-            for (int x = tid; x < ncand; x += SEL_THREADS)
-                if (between(c[x])) c[x] = INFINITY;
-        } else if (all_between <= SEL_LIST) {
-            for (int x = warp; x < all_between; x += SEL_THREADS / 32) {
-                const u64 k = key_of(s_list[x]);
-                if (lane == 0) s_lkey[x] = k;
-            }
-            __syncthreads();
-            for (int x = tid; x < all_between; x += SEL_THREADS) {
-                const u64 k = s_lkey[x];
-                const int at = s_list[x];
-                int above = 0;
-                for (int y = 0; y < all_between; ++y) above += s_lkey[y] > k || (s_lkey[y] == k && s_list[y] < at);
-                c[at] = above < left ? INFINITY : -INFINITY;
-            }
-        } else {
-            for (int x = warp; x < ncand; x += SEL_THREADS / 32) {
-                if (!between(c[x])) continue;
-                const u64 k = key_of(x);
-                if (lane == 0) s_key[x] = k;
-            }
-            __syncthreads();
-            u64 kp = 0, km = 0;
-            int kn = left, kc = 0;
-            bool all = left == 0;
-            for (int shift = 56; shift >= 0 && !all; shift -= 8) {
-                for (int x = tid; x < 256; x += SEL_THREADS) s_hist[x] = 0;
-                __syncthreads();
-                for (int x = tid; x < ncand; x += SEL_THREADS)
-                    if (between(c[x]) && (s_key[x] & km) == kp) atomicAdd(&s_hist[(int)(s_key[x] >> shift) & 255], 1);
-                __syncthreads();
-                kp |= (u64)pick_digit(s_hist, s_pick, kn, kc) << shift;
-                km |= 255ull << shift;
-                all = kc == kn;
-                __syncthreads();
-            }
-            // equal keys: the lower pages; a thread takes a run of neighbouring pages, so one sum over the block counts those before
-            const int per = (ncand + SEL_THREADS - 1) / SEL_THREADS, x0 = min(ncand, tid * per), x1 = min(ncand, x0 + per);
-            int equal = 0, total;
-            for (int x = x0; x < x1; ++x) equal += between(c[x]) && (s_key[x] & km) == kp;
-            int before = block_before(equal, s_warp, total);
-            for (int x = x0; x < x1; ++x) {
-                if (!between(c[x])) continue;
-                const u64 k = s_key[x] & km;
-                bool take = left > 0 && k > kp;
-                if (k == kp) { take = left > 0 && before < kn; ++before; }
-                c[x] = take ? INFINITY : -INFINITY;
+    auto task = [&](int i) {
+        SelTask k;
+        k.pv = &pv; k.pb = &pb;
+        k.r = s_req[i]; k.h = h;
+        k.n = s_np[i] - pb.recent - pb.sink;
+        k.m = pb.top - pb.sink - pb.recent;
+        k.q = q + (size_t)(t0 + i) * pb.q_stride + (size_t)h * g * d;
+        k.c = s_c + (size_t)i * W;
+        k.mass = __uint_as_float(s_err[i]);
+        k.sel = selected + ((size_t)(t0 + i) * pv.H + h) * pb.top + pb.sink;
+        return k;
+    };
+    // ---- a warp per token; what is too much for a warp is left to the block
+    if (warp < ntok) {
+        const int np = s_np[warp];
+        bool hard = false;
+        if (s_req[warp] >= 0) {
+            int32_t* sel = selected + ((size_t)(t0 + warp) * pv.H + h) * pb.top;
+            if (np <= pb.top) {
+                for (int x = lane; x < pb.top; x += 32) sel[x] = x < np ? x : -1;
+            } else {
+                for (int x = lane; x < pb.sink; x += 32) sel[x] = x;
+                for (int x = lane; x < pb.recent; x += 32) sel[pb.top - pb.recent + x] = np - pb.recent + x;
+                const SelTask k = task(warp);
+                if (k.m > 0) hard = k.n > SEL_WARP_MAX || !select_by_warp(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST);
             }
         }
-        __syncthreads();
-        // ---- the pages taken, ascending
-        const int per = (ncand + SEL_THREADS - 1) / SEL_THREADS, x0 = min(ncand, tid * per), x1 = min(ncand, x0 + per);
-        int mine = 0, total;
-        for (int x = x0; x < x1; ++x) mine += c[x] > in_above || c[x] == INFINITY;
-        int at = pb.sink + block_before(mine, s_warp, total);
-        for (int x = x0; x < x1; ++x)
-            if (c[x] > in_above || c[x] == INFINITY) sel[at++] = pb.sink + x;
-        __syncthreads();
+        if (lane == 0) s_hard[warp] = hard;
     }
+    __syncthreads();
+    for (int i = 0; i < ntok; ++i)
+        if (s_hard[i]) select_by_block(task(i), sh, s_key);
 }
 
 cudaError_t run_select_mma(const PagedView& pv, const PagedBatch& pb, const void* q, int32_t* selected, cudaStream_t st) {
@@ -618,7 +735,7 @@ cudaError_t run_select_mma(const PagedView& pv, const PagedBatch& pb, const void
            (size_t)pb.W * (sizeof(u64) + ntok * 2 * sizeof(float)) <= (size_t)PAGED_SELECT_SMEM / 4) ntok *= 2;
     const long long units = (long long)(pb.T + ntok - 1) / ntok * pv.H;
     int nclust = 1;
-    while (nclust < 8 && units * nclust < 2 * PAGED_SMS && pb.W > 128 * nclust) nclust *= 2;
+    while (nclust < 8 && units * nclust * 2 <= 2 * PAGED_SMS && pb.W > 128 * nclust) nclust *= 2;
     const size_t smem = (size_t)pb.W * (sizeof(u64) + ntok * sizeof(float));
     auto go = [&](auto kernel, std::atomic<unsigned long long>& done) {
         const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(kernel), PAGED_SELECT_SMEM, done);
@@ -637,10 +754,15 @@ cudaError_t run_select_mma(const PagedView& pv, const PagedBatch& pb, const void
         count_launch();
         return cudaLaunchKernelEx(&cfg, kernel, pv, pb, (const __nv_bfloat16*)q, selected, nclust, ntok);
     };
-    static std::atomic<unsigned long long> done2{0}, done4{0}, done8{0};
-    if (pv.d <= 64) return go(paged_select_mma_kernel<2>, done2);
-    if (pv.d <= 128) return go(paged_select_mma_kernel<4>, done4);
-    return go(paged_select_mma_kernel<8>, done8);
+    auto by_width = [&](auto dk) {
+        constexpr int DK = decltype(dk)::value;
+        static std::atomic<unsigned long long> done[3];
+        if (ntok > 1) return go(paged_select_mma_kernel<DK, SEL_TOKENS, 2>, done[0]);
+        return pb.g <= 8 ? go(paged_select_mma_kernel<DK, 1, 1>, done[1]) : go(paged_select_mma_kernel<DK, 1, 2>, done[2]);
+    };
+    if (pv.d <= 64) return by_width(std::integral_constant<int, 2>{});
+    if (pv.d <= 128) return by_width(std::integral_constant<int, 4>{});
+    return by_width(std::integral_constant<int, 8>{});
 }
 
 // ---------------------------------------------------------------- fp32
