@@ -223,9 +223,12 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     return it;
 }
 
-// Last request r with cu_new[r] <= t, by the whole warp: 32 offsets per step.
-__device__ __forceinline__ int paged_find_request(const PagedBatch& pb, int t) {
-    const int lane = threadIdx.x & 31;
+// The request of token t and what it holds, by the whole warp: the last r with cu_new[r] <= t.  In a decode step token t is
+// request t's, so that is looked at first, its length with it; otherwise 32 offsets per step.
+__device__ __forceinline__ int paged_find_request(const PagedBatch& pb, int t, PagedReq& rq) {
+    const int lane = threadIdx.x & 31, guess = min(t, pb.R - 1);
+    rq = paged_request(pb, guess);
+    if (rq.row0 <= t && t < rq.row0 + rq.n) return guess;
     int lo = 0, n = pb.R;
     while (n > 1) {
         const int step = (n + 31) / 32, i = lane * step;
@@ -234,6 +237,7 @@ __device__ __forceinline__ int paged_find_request(const PagedBatch& pb, int t) {
         lo += k * step;
         n = min(step, n - k * step);
     }
+    rq = paged_request(pb, lo);
     return lo;
 }
 

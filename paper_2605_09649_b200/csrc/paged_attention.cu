@@ -212,8 +212,8 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     const int t = (int)(item / heads), rest = (int)(item % heads);
     const int h = SPLIT > 1 ? rest / g : rest;
     if (t >= pb.T) return;
-    const int r = paged_find_request(pb, t);
-    const PagedReq rq = paged_request(pb, r);
+    PagedReq rq;
+    const int r = paged_find_request(pb, t, rq);
     const int j = t - rq.row0;
     if (j < 0 || j >= rq.n) return;
     const PagedCost c = paged_cost(pb, rq, tile_rows, min_rows, max_rows);

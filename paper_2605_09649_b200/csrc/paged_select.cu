@@ -234,14 +234,15 @@ __device__ __forceinline__ uint32_t clamp_pos(uint32_t v) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-// The 64-bit key of one page, by a whole warp: eight lanes per head, 8 channels per lane and step.
+// The 64-bit key of one page, by a whole warp: eight lanes per head, 8 channels per lane and step, four sums per lane (an
+// fp64 fma waits long for the one before it).
 __device__ __noinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat16* q, int g, int d) {
     const int lane = threadIdx.x & 31, l = lane & 7;
     double best = -INFINITY;
     bool nan = false;
     for (int h0 = 0; h0 < g; h0 += 4) {
         const int head = h0 + (lane >> 3);
-        double s = 0.0;
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
         for (int c = l * 8; c < d; c += 64) {
             const uint4 vq = head < g ? *reinterpret_cast<const uint4*>(q + (size_t)head * d + c) : make_uint4(0u, 0u, 0u, 0u);
             const uint4 vlo = *reinterpret_cast<const uint4*>(b + c), vhi = *reinterpret_cast<const uint4*>(b + d + c);
@@ -250,14 +251,15 @@ __device__ __noinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat1
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = __bfloat162float(xq[e]);
-                s = fma((double)x, (double)__bfloat162float(x > 0.f ? xhi[e] : xlo[e]), s);
+                s[e & 3] = fma((double)x, (double)__bfloat162float(x > 0.f ? xhi[e] : xlo[e]), s[e & 3]);
             }
         }
+        double sum = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (head < g) {
-            nan |= s != s;
-            best = fmax(best, s);
+            nan |= sum != sum;
+            best = fmax(best, sum);
         }
     }
 #pragma unroll
@@ -339,70 +341,87 @@ struct SelBand {
 };
 __device__ __forceinline__ float sel_slack(float mass) { return __fadd_ru(__fmul_ru(mass, 2.0f * SEL_EPS), 1e-33f); }   // 1e-33: products that underflow
 
-// By one warp.  false: too many pages in the band, nothing written.
+// By one warp, KPL scores per lane in registers (n <= 32 KPL).  false: too many pages in the band, nothing written.
+template <int KPL>
 __device__ __forceinline__ bool select_by_warp(const SelTask& k, int* list, u64* lkey) {
     const int lane = threadIdx.x & 31;
     if (!(k.mass < INFINITY)) return false;
     const float e2 = sel_slack(k.mass);
+    float v[KPL];
+    uint32_t key[KPL];
     // [a, b] holds the m-th largest; three pivots a step until it is narrower than the slack
     uint32_t a = ~0u, b = 0u;
-    for (int x = lane; x < k.n; x += 32) {
-        const uint32_t v = orderable_key(k.c[x]);
-        a = min(a, v);
-        b = max(b, v);
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        const int x = i * 32 + lane;
+        v[i] = x < k.n ? k.c[x] : 0.f;
+        key[i] = x < k.n ? orderable_key(v[i]) : 0u;              // 0: below every pivot (a score's key is greater)
+        if (x < k.n) { a = min(a, key[i]); b = max(b, key[i]); }
     }
     a = __reduce_min_sync(0xffffffffu, a);
     b = __reduce_max_sync(0xffffffffu, b);
     while (a < b && !(key_value(b) - key_value(a) <= e2)) {
         const uint32_t quarter = (b - a) / 4 + 1, p1 = a + quarter, p2 = min(b, p1 - 1 + quarter) + 1, p3 = min(b, p2 - 1 + quarter) + 1;
-        uint32_t n12 = 0, n3 = 0;                                 // keys >= p1 (low half), >= p2 (high half); >= p3
-        for (int x = lane; x < k.n; x += 32) {
-            const uint32_t v = orderable_key(k.c[x]);
-            n12 += (v >= p1 ? 1u : 0u) + (v >= p2 ? 0x10000u : 0u);
-            n3 += v >= p3 ? 1u : 0u;
-        }
-        n12 = __reduce_add_sync(0xffffffffu, n12);
-        n3 = __reduce_add_sync(0xffffffffu, n3);
-        if ((int)n3 >= k.m) a = p3;
-        else if ((int)(n12 >> 16) >= k.m) { a = p2; b = p3 - 1; }
-        else if ((int)(n12 & 0xffffu) >= k.m) { a = p1; b = p2 - 1; }
+        uint32_t n123 = 0;                                        // keys >= p1, >= p2, >= p3: ten bits each
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) n123 += (key[i] >= p1 ? 1u : 0u) + (key[i] >= p2 ? 1u << 10 : 0u) + (key[i] >= p3 ? 1u << 20 : 0u);
+        n123 = __reduce_add_sync(0xffffffffu, n123);
+        if ((int)(n123 >> 20) >= k.m) a = p3;
+        else if ((int)((n123 >> 10) & 1023u) >= k.m) { a = p2; b = p3 - 1; }
+        else if ((int)(n123 & 1023u) >= k.m) { a = p1; b = p2 - 1; }
         else b = p1 - 1;
     }
     const SelBand band = {__fadd_rd(key_value(a), -e2), __fadd_ru(key_value(b), e2), false};
+    unsigned in[KPL], hold[KPL];                                  // the pages in for certain, the pages of the band
     int sure = 0, held = 0;
-    for (int x0 = 0; x0 < k.n; x0 += 32) {
-        const float v = x0 + lane < k.n ? k.c[x0 + lane] : -INFINITY;
-        const unsigned hold = __ballot_sync(0xffffffffu, x0 + lane < k.n && band.holds(v));
-        sure += __popc(__ballot_sync(0xffffffffu, x0 + lane < k.n && band.in(v)));
-        const int at = held + __popc(hold & ((1u << lane) - 1u));
-        if (((hold >> lane) & 1u) && at < SEL_WARP_LIST) list[at] = x0 + lane;
-        held += __popc(hold);
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        const bool real = i * 32 + lane < k.n;
+        in[i] = __ballot_sync(0xffffffffu, real && band.in(v[i]));
+        hold[i] = __ballot_sync(0xffffffffu, real && band.holds(v[i]));
+        sure += __popc(in[i]);
+        held += __popc(hold[i]);
     }
     const int left = k.m - sure;
     if (left < held) {
         if (held > SEL_WARP_LIST) return false;
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) {
+            if ((hold[i] >> lane) & 1u) list[at + __popc(hold[i] & ((1u << lane) - 1u))] = i * 32 + lane;
+            at += __popc(hold[i]);
+        }
         __syncwarp();
         for (int i = 0; i < held; ++i) {
-            const u64 key = k.key(list[i]);
-            if (lane == 0) lkey[i] = key;
+            const u64 x = k.key(list[i]);
+            if (lane == 0) lkey[i] = x;
         }
         __syncwarp();
+        bool take = false;
         if (lane < held) {                                        // the list ascends: among equal keys the lower page comes first
-            const u64 key = lkey[lane];
+            const u64 x = lkey[lane];
             int above = 0;
-            for (int i = 0; i < held; ++i) above += lkey[i] > key || (lkey[i] == key && i < lane);
-            k.c[list[lane]] = above < left ? INFINITY : -INFINITY;
+            for (int i = 0; i < held; ++i) above += lkey[i] > x || (lkey[i] == x && i < lane);
+            take = above < left;
         }
-        __syncwarp();
+        // bit j of `taken`: the j-th page of the band
+        const unsigned taken = __ballot_sync(0xffffffffu, take);
+        at = 0;
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) {
+            const int j = at + __popc(hold[i] & ((1u << lane) - 1u));
+            at += __popc(hold[i]);
+            in[i] |= __ballot_sync(0xffffffffu, ((hold[i] >> lane) & 1u) && ((taken >> (j & 31)) & 1u));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) in[i] |= hold[i];
     }
     int at = 0;
-    for (int x0 = 0; x0 < k.n; x0 += 32) {
-        const float v = x0 + lane < k.n ? k.c[x0 + lane] : -INFINITY;
-        // (with places for the whole band its pages are unmarked, else marked +inf or -inf)
-        const bool take = x0 + lane < k.n && (band.in(v) || (left >= held && band.holds(v)));
-        const unsigned t = __ballot_sync(0xffffffffu, take);
-        if (take) k.sel[at + __popc(t & ((1u << lane) - 1u))] = x0 + lane + k.pb->sink;
-        at += __popc(t);
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        if ((in[i] >> lane) & 1u) k.sel[at + __popc(in[i] & ((1u << lane) - 1u))] = i * 32 + lane + k.pb->sink;
+        at += __popc(in[i]);
     }
     return true;
 }
@@ -521,12 +540,23 @@ __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u6
         }
     }
     __syncthreads();
-    const int per = (k.n + SEL_THREADS - 1) / SEL_THREADS, x0 = min(k.n, tid * per), x1 = min(k.n, x0 + per);
-    int mine = 0, total;
-    for (int x = x0; x < x1; ++x) mine += band.in(k.c[x]) || k.c[x] == INFINITY;
-    int at = block_before(mine, sh.warp, total);
-    for (int x = x0; x < x1; ++x)
-        if (band.in(k.c[x]) || k.c[x] == INFINITY) k.sel[at++] = k.pb->sink + x;
+    // ---- the pages taken, ascending: a warp has a run of neighbouring pages
+    const int per = ((k.n + SEL_THREADS - 1) / SEL_THREADS) * 32, x0 = min(k.n, warp * per), x1 = min(k.n, x0 + per);
+    int mine = 0;
+    for (int x = x0; x < x1; x += 32) {
+        const bool t = x + lane < x1 && (band.in(k.c[x + lane]) || k.c[x + lane] == INFINITY);
+        mine += __popc(__ballot_sync(0xffffffffu, t));
+    }
+    if (lane == 0) sh.warp[warp] = mine;
+    __syncthreads();
+    int at = 0;
+    for (int w = 0; w < warp; ++w) at += sh.warp[w];
+    for (int x = x0; x < x1; x += 32) {
+        const bool t = x + lane < x1 && (band.in(k.c[x + lane]) || k.c[x + lane] == INFINITY);
+        const unsigned votes = __ballot_sync(0xffffffffu, t);
+        if (t) k.sel[at + __popc(votes & ((1u << lane) - 1u))] = k.pb->sink + x + lane;
+        at += __popc(votes);
+    }
 }
 
 // grid = ceil(T / ntok) * H clusters.  Dynamic shared memory: 64-bit keys [W], then scores [ntok][W] fp32.
@@ -549,8 +579,8 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
         const int t = t0 + warp;
         int req = -1, np = 0;
         if (t < pb.T) {
-            const int r = paged_find_request(pb, t);
-            const PagedReq rq = paged_request(pb, r);
+            PagedReq rq;
+            const int r = paged_find_request(pb, t, rq);
             const int j = t - rq.row0;
             if (j >= 0 && j < rq.n) {                             // else: a row behind the last request, left as it is
                 req = r;
@@ -569,8 +599,10 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
         if (nclust > 1) {
             c0 = cluster.map_shared_rank(s_c, 0);
             err0 = cluster.map_shared_rank(s_err, 0);
-            cluster.sync();                                       // the first CTA runs and has cleared its errors
+            cluster.barrier_arrive();                             // this CTA runs and has cleared its errors
         }
+        bool arrived = nclust == 1;                               // nothing is written to the first CTA before all have arrived
+        auto all_run = [&]() { if (!arrived) { cluster.barrier_wait(); arrived = true; } };
         const int quad = lane & 3, row = lane >> 2;
         for (int i0 = 0; i0 < ntok;) {                            // runs of tokens of one request
             const int r = s_req[i0];
@@ -660,6 +692,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                                     }
                         }
                 }
+                all_run();
 #pragma unroll
                 for (int i = 0; i < NTOK; ++i) {
                     if (i >= i1 - i0) break;
@@ -689,6 +722,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
             }
             i0 = i1;
         }
+        all_run();
         if (nclust > 1) cluster.sync(); else __syncthreads();
     }
     if (rank != 0) return;
@@ -717,7 +751,8 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                 for (int x = lane; x < pb.sink; x += 32) sel[x] = x;
                 for (int x = lane; x < pb.recent; x += 32) sel[pb.top - pb.recent + x] = np - pb.recent + x;
                 const SelTask k = task(warp);
-                if (k.m > 0) hard = k.n > SEL_WARP_MAX || !select_by_warp(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST);
+                if (k.m > 0) hard = k.n > SEL_WARP_MAX || !(k.n <= 256 ? select_by_warp<8>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST)
+                                                                           : select_by_warp<16>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST));
             }
         }
         if (lane == 0) s_hard[warp] = hard;
