@@ -1,11 +1,13 @@
 // Attention of new tokens over the caller-owned paged cache: the form for any head size and type, and the kernel that joins
 // partial results.
 //
-// Plain form.  A CTA of 128 threads holds 16 (token, query head) rows of one KV head and walks its share of the pages
-// (paged_item): 64 keys at a time, widened to fp32 in shared memory; S = Q K^T with one key per thread and 8 rows in
-// registers, the running maximum and sum of the softmax per row, then O += P V with a column of O per thread.  All sums are
-// fp32.  fp32 caches and head sizes other than 64 and 128 run here; bound by shared-memory reads and FMAs beyond a few
-// rows per page, by the page loads below that.
+// Plain form.  A CTA of 256 threads holds 16 (token, query head) rows of one KV head and walks its share of the pages
+// (paged_item), a page at a time: cp.async brings K and V as they are stored into one of two buffers while the page before
+// is worked on (rows behind the last entry are filled with zeros); S = Q K^T in fp32 with one key and four rows per thread -- a
+// warp has 8 keys x 16 rows, so that a 16-byte read of K serves 16 FMAs and the reads of Q are broadcasts --, the running
+// maximum and sum of the softmax with two rows per warp, then O += P V with a column and 4 to 16 rows of O per thread.  All
+// sums are fp32.  fp32 caches and head sizes other than 64 and 128 run here; bound by shared-memory reads (about 2200 cycles a
+// page at d = 64) beyond a few rows per page, by the page loads below that.
 #include "mma_sync.cuh"
 #include "paged.cuh"
 
@@ -14,58 +16,85 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int PL_THREADS = 128, PL_ROWS = PAGED_PLAIN_ROWS;
+constexpr int PL_THREADS = 256, PL_ROWS = PAGED_PLAIN_ROWS;
 
 // DP: head size rounded up to 64, 128 or 256
 template <typename T, int DP>
 struct PlainShape {
-    static constexpr int KS = DP + 4;                             // row stride of K and Q in shared memory (floats)
-    static constexpr int COLS = DP < PL_THREADS ? DP : PL_THREADS;
-    static constexpr int RG = PL_THREADS / COLS, CPT = DP / COLS; // row groups, columns of O per thread
+    static constexpr int E = 16 / (int)sizeof(T);
+    static constexpr int KS = DP + E;                             // row stride of K (elements): rows 16 bytes apart modulo 128
+    static constexpr int QS = DP + 4;                             // row stride of Q (floats)
+    static constexpr int COLS = DP, RG = PL_THREADS / COLS;       // columns, row groups of O over the threads
     static constexpr int RPT = PL_ROWS / RG;                      // rows of O per thread
-    static constexpr int SMEM = (int)sizeof(float) * (PAGE * KS + PAGE * DP + PL_ROWS * KS + PL_ROWS * PAGE) + 3 * PL_ROWS * 4;
+    static constexpr int STAGE = PAGE * (KS + DP) * (int)sizeof(T);
+    static constexpr int STAGES = STAGE <= 100 * 1024 ? 2 : 1;
+    static constexpr int SMEM = STAGES * STAGE + (int)sizeof(float) * (PL_ROWS * QS + PL_ROWS * PAGE + 3 * PL_ROWS);
+    static constexpr int CTAS = SMEM <= 100 * 1024 ? 2 : 1;       // per SM
 };
 
+template <typename T>
+__device__ __forceinline__ float4 plain_load4(const T* p);
+template <>
+__device__ __forceinline__ float4 plain_load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <>
+__device__ __forceinline__ float4 plain_load4<__nv_bfloat16>(const __nv_bfloat16* p) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+}
+// 16 bytes, or zeros (src is not read).
+__device__ __forceinline__ void plain_copy16(void* dst, const void* src, bool on) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(PL_THREADS)
-paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T* __restrict__ out, float scale_log2, PagedWork wk,
-                        int max_workers) {
+__global__ void __launch_bounds__(PL_THREADS, PlainShape<T, DP>::CTAS)
+paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T* __restrict__ out, float scale_log2, PagedWork wk) {
     using S = PlainShape<T, DP>;
-    extern __shared__ __align__(16) float s_f[];
+    extern __shared__ __align__(16) unsigned char s_pl[];
     __shared__ long long s_grp[PAGED_GROUPS + 1];
-    float* s_k = s_f;                                             // [64][KS]
-    float* s_v = s_k + PAGE * S::KS;                              // [64][DP]
-    float* s_q = s_v + PAGE * DP;                                 // [16][KS]
-    float* s_p = s_q + PL_ROWS * S::KS;                           // [16][64]
+    float* s_q = reinterpret_cast<float*>(s_pl + S::STAGES * S::STAGE);   // [16][QS]
+    float* s_p = s_q + PL_ROWS * S::QS;                           // [16][64]
     float* s_m = s_p + PL_ROWS * PAGE;                            // running maximum, sum, factor of this step
     float* s_l = s_m + PL_ROWS;
     float* s_a = s_l + PL_ROWS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = pv.d, g = pb.g;
-    constexpr int E = 16 / (int)sizeof(T);
-    const int cpr = d / E;
+    const int cpr = d / S::E;
 
     grid_dependency_wait();
     PagedTable tab;
     const int unit_rows = pb.top > 0 ? g : PL_ROWS;               // rows of a unit (top > 0: one token)
-    paged_build_table(tab, pb, pv.H, PL_ROWS, 1, INT_MAX, max_workers, 2, s_grp, wk.prefix);
+    paged_build_table(tab, pb, pv.H, PL_ROWS, 1, INT_MAX, (int)gridDim.x, 2, s_grp, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;
     const long long end = paged_share(tab.total, tab.workers, w + 1);
-    for (int i = tid; i < PL_ROWS * S::KS; i += PL_THREADS) s_q[i] = 0.f;
-    for (int i = tid; i < PAGE * S::KS; i += PL_THREADS) s_k[i] = 0.f;
-    for (int i = tid; i < PAGE * DP; i += PL_THREADS) s_v[i] = 0.f;
 
     for (long long x = paged_share(tab.total, tab.workers, w); x < end;) {
         const PagedItem it = paged_item(tab, pb, x, end, w);
         x += it.steps;
         const int row_first = pb.top > 0 ? it.u * g : it.u * PL_ROWS;    // of the request's n * g rows
         const int unit_n = min(unit_rows, it.q.n * g - row_first);
+        auto load_page = [&](int p) {                            // place p of the unit's pages into buffer (p - p0) % STAGES
+            T* s_k = reinterpret_cast<T*>(s_pl + (p - it.p0) % S::STAGES * S::STAGE);
+            T* s_v = s_k + PAGE * S::KS;
+            const int page = pb.top > 0 ? pb.selected[((size_t)(it.q.row0 + it.u) * pv.H + it.h) * pb.top + p] : p;
+            const int phys = paged_physical(pb, pv, it.r, page);
+            const int held = phys < 0 ? 0 : it.q.len - page * PAGE;      // what lies behind the last entry is not read
+            const size_t off = ((size_t)max(phys, 0) * pv.H + it.h) * PAGE * d;
+            for (int i = tid; i < PAGE * cpr; i += PL_THREADS) {
+                const int e = i / cpr, c = (i - e * cpr) * S::E;
+                plain_copy16(s_k + e * S::KS + c, reinterpret_cast<const T*>(pv.k) + off + (size_t)e * d + c, e < held);
+                plain_copy16(s_v + e * DP + c, reinterpret_cast<const T*>(pv.v) + off + (size_t)e * d + c, e < held);
+            }
+            return phys < 0 ? INT_MAX / 2 : page * PAGE;         // first entry; of a page that does not exist: seen by no row
+        };
         for (int b0 = 0; b0 < unit_n; b0 += PL_ROWS) {           // a token with more than 16 query heads: 16 at a time
             const int rows = min(PL_ROWS, unit_n - b0);
             __syncthreads();
+            int e_next = it.p0 < it.p1 ? load_page(it.p0) : 0;
+            asm volatile("cp.async.commit_group;" ::: "memory");
             for (int i = tid; i < PL_ROWS * cpr; i += PL_THREADS) {
-                const int rr = i / cpr, c = (i - rr * cpr) * E;
+                const int rr = i / cpr, c = (i - rr * cpr) * S::E;
                 uint4 val = make_uint4(0u, 0u, 0u, 0u);
                 if (rr < rows) {
                     const int row = row_first + b0 + rr;
@@ -73,124 +102,118 @@ paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T*
                 }
                 const T* p = reinterpret_cast<const T*>(&val);
 #pragma unroll
-                for (int e = 0; e < E; ++e) s_q[rr * S::KS + c + e] = to_f32<T>(p[e]);
+                for (int e = 0; e < S::E; ++e) s_q[rr * S::QS + c + e] = to_f32<T>(p[e]);
             }
             if (tid < PL_ROWS) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
-            float acc[S::CPT][S::RPT];
+            float acc[S::RPT];
 #pragma unroll
-            for (int c = 0; c < S::CPT; ++c)
+            for (int i = 0; i < S::RPT; ++i) acc[i] = 0.f;
+            // S: this thread's key and first row; the entries its rows see
+            const int key = warp * 8 + (lane & 7), rh = (lane >> 3) * 4;
+            int see_hi[4], see_lo[4];
 #pragma unroll
-                for (int i = 0; i < S::RPT; ++i) acc[c][i] = 0.f;
+            for (int i = 0; i < 4; ++i) {
+                const int pos = rh + i < rows ? it.q.len - it.q.n + (row_first + b0 + rh + i) / g : -1;
+                see_hi[i] = pos;
+                see_lo[i] = pb.window > 0 ? pos + 1 - pb.window : 0;
+            }
+            const int col = tid % S::COLS, r0 = (tid / S::COLS) * S::RPT;
 
             for (int p = it.p0; p < it.p1; ++p) {
-                const int page = pb.top > 0 ? pb.selected[((size_t)(it.q.row0 + it.u) * pv.H + it.h) * pb.top + p] : p;
-                const int phys = paged_physical(pb, pv, it.r, page);
-                if (phys < 0) continue;                          // the same for every thread
-                const int e0 = page * PAGE, held = min(PAGE, it.q.len - e0);   // rows of the page that hold entries
-                __syncthreads();                                  // the last page's products are done
-                const T* kp = reinterpret_cast<const T*>(pv.k) + ((size_t)phys * pv.H + it.h) * PAGE * d;
-                const T* vp = reinterpret_cast<const T*>(pv.v) + ((size_t)phys * pv.H + it.h) * PAGE * d;
-                for (int i = tid; i < PAGE * cpr; i += PL_THREADS) {
-                    const int e = i / cpr, c = (i - e * cpr) * E;
-                    uint4 kv = make_uint4(0u, 0u, 0u, 0u), vv = kv;           // what lies behind the last entry is not read
-                    if (e < held) {
-                        kv = *reinterpret_cast<const uint4*>(kp + (size_t)e * d + c);
-                        vv = *reinterpret_cast<const uint4*>(vp + (size_t)e * d + c);
-                    }
-                    const T* pk = reinterpret_cast<const T*>(&kv);
-                    const T* pvv = reinterpret_cast<const T*>(&vv);
-#pragma unroll
-                    for (int u = 0; u < E; ++u) { s_k[e * S::KS + c + u] = to_f32<T>(pk[u]); s_v[e * DP + c + u] = to_f32<T>(pvv[u]); }
-                }
+                const int e0 = e_next;
+                const T* s_k = reinterpret_cast<const T*>(s_pl + (p - it.p0) % S::STAGES * S::STAGE);
+                const T* s_v = s_k + PAGE * S::KS;
+                if (S::STAGES > 1 && p + 1 < it.p1) e_next = load_page(p + 1);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (S::STAGES > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+                else asm volatile("cp.async.wait_group 0;" ::: "memory");
                 __syncthreads();
-                {                                                 // S: key tid & 63, rows 8 (tid / 64) ..
-                    const int key = tid & 63, rh = (tid >> 6) * (PL_ROWS / 2);
-                    float s[PL_ROWS / 2];
-#pragma unroll
-                    for (int i = 0; i < PL_ROWS / 2; ++i) s[i] = 0.f;
+                {
+                    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
                     for (int c = 0; c < d; c += 4) {
-                        const float4 kk = *reinterpret_cast<const float4*>(s_k + key * S::KS + c);
+                        const float4 kk = plain_load4<T>(s_k + key * S::KS + c);
 #pragma unroll
-                        for (int i = 0; i < PL_ROWS / 2; ++i) {
-                            const float4 qq = *reinterpret_cast<const float4*>(s_q + (rh + i) * S::KS + c);
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 qq = *reinterpret_cast<const float4*>(s_q + (rh + i) * S::QS + c);
                             s[i] = fmaf(qq.x, kk.x, fmaf(qq.y, kk.y, fmaf(qq.z, kk.z, fmaf(qq.w, kk.w, s[i]))));
                         }
                     }
+                    const int at = e0 + key;
 #pragma unroll
-                    for (int i = 0; i < PL_ROWS / 2; ++i) {
-                        const int pos = it.q.len - it.q.n + (row_first + b0 + rh + i) / g, at = e0 + key;
-                        const bool on = rh + i < rows && at <= pos && (pb.window <= 0 || at > pos - pb.window);
-                        s_p[(rh + i) * PAGE + key] = on ? s[i] * scale_log2 : -INFINITY;
-                    }
-                }
-                __syncthreads();
-                for (int rr = warp; rr < PL_ROWS; rr += PL_THREADS / 32) {
-                    const float a = s_p[rr * PAGE + lane], b = s_p[rr * PAGE + 32 + lane];
-                    float mx = fmaxf(a, b);
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                    const float m0 = s_m[rr], mn = fmaxf(m0, mx);
-                    const float ref = mn == -INFINITY ? 0.f : mn; // a row that has seen nothing yet: every weight is 0
-                    const float pa = exp2f(a - ref), pbv = exp2f(b - ref);
-                    float sum = pa + pbv;
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    s_p[rr * PAGE + lane] = pa;
-                    s_p[rr * PAGE + 32 + lane] = pbv;
-                    __syncwarp();
-                    if (lane == 0) {
-                        const float f = exp2f(m0 - ref);
-                        s_a[rr] = f;
-                        s_l[rr] = s_l[rr] * f + sum;
-                        s_m[rr] = mn;
-                    }
-                    __syncwarp();
+                    for (int i = 0; i < 4; ++i) s_p[(rh + i) * PAGE + key] = at <= see_hi[i] && at >= see_lo[i] ? s[i] * scale_log2 : -INFINITY;
                 }
                 __syncthreads();
                 {
-                    const int col = tid % S::COLS, r0 = (tid / S::COLS) * S::RPT;
+                    float a[2], b[2], mx[2], sum[2], m0[2], ref[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int rr = warp * 2 + i;
+                        a[i] = s_p[rr * PAGE + lane];
+                        b[i] = s_p[rr * PAGE + 32 + lane];
+                        m0[i] = s_m[rr];
+                        mx[i] = fmaxf(a[i], b[i]);
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], o));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        mx[i] = fmaxf(m0[i], mx[i]);
+                        ref[i] = mx[i] == -INFINITY ? 0.f : mx[i];       // a row that has seen nothing yet: every weight is 0
+                        a[i] = exp2f(a[i] - ref[i]);
+                        b[i] = exp2f(b[i] - ref[i]);
+                        sum[i] = a[i] + b[i];
+                        s_p[(warp * 2 + i) * PAGE + lane] = a[i];
+                        s_p[(warp * 2 + i) * PAGE + 32 + lane] = b[i];
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+                    if (lane < 2) {
+                        const int rr = warp * 2 + lane;
+                        const float f = exp2f((lane ? m0[1] : m0[0]) - (lane ? ref[1] : ref[0]));
+                        s_a[rr] = f;
+                        s_l[rr] = s_l[rr] * f + (lane ? sum[1] : sum[0]);
+                        s_m[rr] = lane ? mx[1] : mx[0];
+                    }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < S::RPT; ++i) acc[i] *= s_a[r0 + i];
+#pragma unroll 4
+                for (int e = 0; e < PAGE; e += 4) {
+                    float vv[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) vv[u] = to_f32<T>(s_v[(e + u) * DP + col]);
 #pragma unroll
                     for (int i = 0; i < S::RPT; ++i) {
-                        const float f = s_a[r0 + i];
-#pragma unroll
-                        for (int c = 0; c < S::CPT; ++c) acc[c][i] *= f;
+                        const float4 pp = *reinterpret_cast<const float4*>(s_p + (r0 + i) * PAGE + e);
+                        acc[i] = fmaf(pp.x, vv[0], fmaf(pp.y, vv[1], fmaf(pp.z, vv[2], fmaf(pp.w, vv[3], acc[i]))));
                     }
-                    for (int e = 0; e < PAGE; e += 4) {
-                        float vv[S::CPT][4];
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-#pragma unroll
-                            for (int c = 0; c < S::CPT; ++c) vv[c][u] = s_v[(e + u) * DP + col + c * S::COLS];
-#pragma unroll
-                        for (int i = 0; i < S::RPT; ++i) {
-                            const float4 pp = *reinterpret_cast<const float4*>(s_p + (r0 + i) * PAGE + e);
-#pragma unroll
-                            for (int c = 0; c < S::CPT; ++c)
-                                acc[c][i] = fmaf(pp.x, vv[c][0], fmaf(pp.y, vv[c][1], fmaf(pp.z, vv[c][2], fmaf(pp.w, vv[c][3], acc[c][i]))));
-                        }
-                    }
+                }
+                __syncthreads();                                  // the buffer and the weights are free
+                if (S::STAGES == 1 && p + 1 < it.p1) {
+                    e_next = load_page(p + 1);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
                 }
             }
             __syncthreads();
-            const int col = tid % S::COLS, r0 = (tid / S::COLS) * S::RPT;
+            if (col < d) {
 #pragma unroll
-            for (int i = 0; i < S::RPT; ++i) {
-                if (r0 + i >= rows) continue;
-                const int row = row_first + b0 + r0 + i;
-                const float l = s_l[r0 + i], inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-#pragma unroll
-                for (int c = 0; c < S::CPT; ++c) {
-                    const int dd = col + c * S::COLS;
-                    if (dd >= d) continue;
-                    if (it.slot < 0)
-                        out[((size_t)(it.q.row0 + row / g) * pb.Hq + (size_t)(it.h * g + row % g)) * d + dd] = from_f32<T>(acc[c][i] * inv);
-                    else
-                        wk.part_o[((size_t)it.slot * unit_rows + b0 + r0 + i) * d + dd] = acc[c][i];
-                }
-                if (it.slot >= 0 && col == 0) {
-                    float* ml = wk.part_ml + ((size_t)it.slot * unit_rows + b0 + r0 + i) * 2;
-                    ml[0] = s_m[r0 + i];
-                    ml[1] = l;
+                for (int i = 0; i < S::RPT; ++i) {
+                    if (r0 + i >= rows) continue;
+                    const int row = row_first + b0 + r0 + i;
+                    const float l = s_l[r0 + i], inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+                    if (it.slot < 0) {
+                        out[((size_t)(it.q.row0 + row / g) * pb.Hq + (size_t)(it.h * g + row % g)) * d + col] = from_f32<T>(acc[i] * inv);
+                    } else {
+                        const size_t pr = (size_t)it.slot * unit_rows + b0 + r0 + i;
+                        wk.part_o[pr * d + col] = acc[i];
+                        if (col == 0) { wk.part_ml[pr * 2] = s_m[r0 + i]; wk.part_ml[pr * 2 + 1] = l; }
+                    }
                 }
             }
         }
@@ -337,12 +360,11 @@ cudaError_t run_plain(const PagedView& pv, const PagedBatch& pb, const void* q, 
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_plain_kernel<T, DP>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    const int workers = PAGED_SMS * PAGED_PLAIN_CTAS;
+    static_assert(S::CTAS <= PAGED_PLAIN_CTAS, "the workspace holds the workers' partial results");
     count_launch();
-    const dim3 grid(workers), block(PL_THREADS);
-    if (dependent)
-        return launch_dependent(paged_attn_plain_kernel<T, DP>, grid, block, S::SMEM, st, pv, pb, (const T*)q, (T*)out, scale * LOG2E, w, workers);
-    paged_attn_plain_kernel<T, DP><<<grid, block, S::SMEM, st>>>(pv, pb, (const T*)q, (T*)out, scale * LOG2E, w, workers);
+    const dim3 grid(PAGED_SMS * S::CTAS), block(PL_THREADS);
+    if (dependent) return launch_dependent(paged_attn_plain_kernel<T, DP>, grid, block, S::SMEM, st, pv, pb, (const T*)q, (T*)out, scale * LOG2E, w);
+    paged_attn_plain_kernel<T, DP><<<grid, block, S::SMEM, st>>>(pv, pb, (const T*)q, (T*)out, scale * LOG2E, w);
     return cudaGetLastError();
 }
 

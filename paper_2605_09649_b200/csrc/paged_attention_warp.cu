@@ -2,7 +2,7 @@
 //
 // A decode step does 2 g flops per byte of K and V, far below the machine's balance, so the kernel is a stream from HBM:
 // one CTA per SM, four independent warps, each with a ring of its own (48 KB) that TMA fills 32 entries at a time, one
-// or two 64-column boxes of K and of V, 128-byte swizzled so that ldmatrix meets no bank conflict.  A warp takes an equal
+// or two 64-column boxes of K and of V (a team: 64 entries), 128-byte swizzled so that ldmatrix meets no bank conflict.  A warp takes an equal
 // share of the line of page steps (paged.cuh), computes S^T = K Q^T and O^T += V^T P^T with mma.sync m16n8k16 -- the
 // (token, head) rows are the N dimension, 8 or 16 columns, so little is wasted on padding -- and keeps the
 // softmax in registers.  Units of up to 32 or 64 rows (drafted tokens): teams of four warps share a ring of 96 KB and every
@@ -21,17 +21,19 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int W_TILE = 32;                                            // entries per stage
+constexpr float W_RESCALE_STEP = 8.0f;                                // log2 units the reference of the weights may lag behind the maximum
 
 // NT: column tiles of 8 rows per warp.  TW: warps of a team, which share a ring and a unit, each with rows of its own.
 template <int D, int NT, int TW>
 struct WarpShape {
     static constexpr int TEAMS = TW == 1 ? PAGED_WARPS : 2;
     static constexpr int ROWS = NT * 8 * TW;                          // rows of a unit
-    static constexpr int PLANE = W_TILE * 128;                        // 32 entries x 64 columns
+    static constexpr int TILE = TW == 1 ? 32 : 64;                    // entries per stage
+    static constexpr int PER_PAGE = PAGE / TILE;
+    static constexpr int PLANE = TILE * 128;                          // entries x 64 columns
     static constexpr int PLANES = D / 64;
     static constexpr int STAGE = 2 * PLANES * PLANE;                  // K planes, V planes
-    static constexpr int STAGES = 192 * 1024 / TEAMS / STAGE;         // d = 128: 3 (a warp alone) or 6; d = 64: twice that
+    static constexpr int STAGES = 192 * 1024 / TEAMS / STAGE;         // d = 128: 3; d = 64: 6
     static constexpr int LAG = TW == 1 ? 0 : 1;                       // tiles that the rest of a team may be behind a refill
     static constexpr int RING = STAGES * STAGE;
     static constexpr int OFF_BAR = TEAMS * RING;                      // full and empty barrier of each stage
@@ -44,7 +46,7 @@ struct WarpShape {
 struct WarpCursor {
     long long x;
     PagedItem it;
-    int ntile;          // 32-entry tiles to read
+    int ntile;          // tiles to read
     bool on;
 };
 
@@ -53,7 +55,7 @@ __global__ void __launch_bounds__(WarpShape<D, NT, TW>::TEAMS * TW * 32, 1)
 paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
                        const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int max_rows) {
     using S = WarpShape<D, NT, TW>;
-    constexpr int KS = D / 16;
+    constexpr int KS = D / 16, MT = S::TILE / 16;
     extern __shared__ unsigned char w_smem_raw[];
     unsigned char* smem = w_smem_raw + ((1024u - (smem_u32(w_smem_raw) & 1023u)) & 1023u);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
@@ -86,12 +88,12 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         c.on = x < end;
         if (!c.on) return c;
         c.it = paged_item(tab, pb, x, end, w);
-        c.ntile = 2 * (c.it.p1 - c.it.p0);
+        c.ntile = S::PER_PAGE * (c.it.p1 - c.it.p0);
         // the page of the unit's last token: its second half may lie behind what is seen
-        if (c.ntile) {
+        if (S::PER_PAGE == 2 && c.ntile) {
             const int phi = c.it.q.len - c.it.q.n + c.it.tok1, np = phi / PAGE + 1;
             const bool last = SELECT ? c.it.p1 == min(pb.top, np) : c.it.p1 == np;
-            if (last && phi % PAGE < W_TILE) --c.ntile;
+            if (last && phi % PAGE < S::TILE) --c.ntile;
         }
         return c;
     };
@@ -103,23 +105,23 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     auto issue_one = [&]() {                                          // the team's first warp
         while (prod.on && prod_tile == prod.ntile) { prod = at(prod.x + prod.it.steps); prod_tile = 0; }
         if (!prod.on) return;
-        if ((prod_tile & 63) == 0) {                                  // the next 32 pages
-            const int p = prod.it.p0 + (prod_tile >> 1) + lane;
+        if (prod_tile % (32 * S::PER_PAGE) == 0) {                    // the next 32 pages
+            const int p = prod.it.p0 + prod_tile / S::PER_PAGE + lane;
             log_page = -1;
             if (p < prod.it.p1) log_page = SELECT ? pb.selected[((size_t)(prod.it.q.row0 + prod.it.u) * pv.H + prod.it.h) * pb.top + p] : p;
             phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, log_page) : -1;
         }
-        const int src = (prod_tile >> 1) & 31, half = prod_tile & 1;
+        const int src = (prod_tile / S::PER_PAGE) & 31, half = prod_tile % S::PER_PAGE;
         const int lp = __shfl_sync(0xffffffffu, log_page, src), pp = __shfl_sync(0xffffffffu, phys_page, src);
         const unsigned s = issued % S::STAGES;
         if (TW > 1 && issued >= S::STAGES && !mbar_wait_bounded(empty + s, (issued / S::STAGES - 1) & 1u)) { failed = true; return; }
         if (lane == 0) {
-            meta[s] = pp < 0 ? -1 : lp * PAGE + half * W_TILE;
+            meta[s] = pp < 0 ? -1 : lp * PAGE + half * S::TILE;
             if (pp < 0) {
                 mbar_arrive(bars + s);
             } else {
                 const uint32_t dst = smem_u32(ring + s * S::STAGE), bar = smem_u32(bars + s);
-                const int row = (pp * pv.H + prod.it.h) * PAGE + half * W_TILE;
+                const int row = (pp * pv.H + prod.it.h) * PAGE + half * S::TILE;
                 fence_proxy_async_smem();
                 mbar_expect_tx(bars + s, S::STAGE);
 #pragma unroll
@@ -182,9 +184,9 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 continue;
             }
             const uint32_t kbase = smem_u32(ring + s * S::STAGE), vbase = kbase + S::PLANES * S::PLANE;
-            const int held = it.q.len - e0;                           // entries of the tile, if fewer than 32
-            if (held < W_TILE) {
-                for (int i = max(held, 0) * 8 + lane; i < W_TILE * 8; i += 32)
+            const int held = it.q.len - e0;                           // entries of the tile, if it is not full
+            if (held < S::TILE) {
+                for (int i = max(held, 0) * 8 + lane; i < S::TILE * 8; i += 32)
 #pragma unroll
                     for (int p = 0; p < S::PLANES; ++p)
                         *reinterpret_cast<uint4*>(ring + s * S::STAGE + (S::PLANES + p) * S::PLANE + i * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -192,15 +194,15 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 __syncwarp();
             }
             // ---- S^T[entry][row] = K Q^T
-            float sacc[2][NT][4];
+            float sacc[MT][NT][4];
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) sacc[mt][nt][0] = sacc[mt][nt][1] = sacc[mt][nt][2] = sacc[mt][nt][3] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
+                for (int mt = 0; mt < MT; ++mt) {
                     const int row = mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
                     const int c = 2 * ks + (lane >> 4);
                     uint32_t a[4];
@@ -209,12 +211,14 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     for (int nt = 0; nt < NT; ++nt) mma_bf16(sacc[mt][nt], a, bq[nt][ks][0], bq[nt][ks][1]);
                 }
             }
-            // ---- softmax over the entries; this thread owns rows 2 (lane & 3), + 1 of each column tile
-            const bool edge = e0 + W_TILE > all_hi || e0 < all_lo;
-            uint32_t pbf[2][NT][2];
+            // ---- softmax over the entries; this thread owns rows 2 (lane & 3), + 1 of each column tile.  m_ref, the
+            // reference of a row's weights, is raised only when some logit exceeds it by 2^8: until then a tile needs one vote
+            // and no exchange between lanes, and the weights stay below 2^8.
+            const bool edge = e0 + S::TILE > all_hi || e0 < all_lo;
+            float mx[NT][2];
+            bool raise = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float mx[2] = {-INFINITY, -INFINITY};
                 if (edge) {                                           // rows of the column's token see entries lo .. pos
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -222,7 +226,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         const int pos = col < rows ? it.q.len - it.q.n + (row_first + col) / g : -1;
                         const int lo = pb.window > 0 ? pos + 1 - pb.window : 0;
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
+                        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                             for (int i = c; i < 4; i += 2) {
                                 const int e = e0 + mt * 16 + (lane >> 2) + (i >> 1) * 8;
@@ -230,45 +234,54 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             }
                     }
                 }
+                mx[nt][0] = mx[nt][1] = -INFINITY;
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sacc[mt][nt][i] *= scale_log2;                // > 0
-                        mx[i & 1] = fmaxf(mx[i & 1], sacc[mt][nt][i]);
-                    }
-                float f[2], ref[2], ls[2] = {0.f, 0.f};
+                for (int mt = 0; mt < MT; ++mt) {
+                    mx[nt][0] = fmaxf(mx[nt][0], fmaxf(sacc[mt][nt][0], sacc[mt][nt][2]));
+                    mx[nt][1] = fmaxf(mx[nt][1], fmaxf(sacc[mt][nt][1], sacc[mt][nt][3]));
+                }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) mx[c] = fmaxf(mx[c], __shfl_xor_sync(0xffffffffu, mx[c], off));
-                    const float mn = fmaxf(m_run[nt][c], mx[c]);
-                    ref[c] = mn == -INFINITY ? 0.f : mn;              // nothing seen yet: every weight is 0
-                    f[c] = exp2f(m_run[nt][c] - ref[c]);
-                    m_run[nt][c] = mn;
+                    mx[nt][c] *= scale_log2;                          // > 0
+                    raise |= mx[nt][c] > m_run[nt][c] + W_RESCALE_STEP;
                 }
+            }
+            if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    const float* sc = sacc[mt][nt];
-                    const __nv_bfloat162 plo = __floats2bfloat162_rn(exp2f(sc[0] - ref[0]), exp2f(sc[1] - ref[1]));
-                    const __nv_bfloat162 phi = __floats2bfloat162_rn(exp2f(sc[2] - ref[0]), exp2f(sc[3] - ref[1]));
-                    ls[0] += __low2float(plo) + __low2float(phi);     // the sum of what the tensor cores will see
-                    ls[1] += __high2float(plo) + __high2float(phi);
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = mx[nt][c];
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+                        m = fmaxf(m, m_run[nt][c]);
+                        const float f = m == -INFINITY ? 1.f : a_ex2(m_run[nt][c] - m);      // (0 the first time)
+                        m_run[nt][c] = m;
+                        l_run[nt][c] *= f;
+#pragma unroll
+                        for (int dt = 0; dt < KS; ++dt) { o[nt][dt][c] *= f; o[nt][dt][c + 2] *= f; }
+                    }
+            }
+            uint32_t pbf[MT][NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float ref0 = m_run[nt][0] == -INFINITY ? 0.f : m_run[nt][0], ref1 = m_run[nt][1] == -INFINITY ? 0.f : m_run[nt][1];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const float* sc = sacc[mt][nt];                   // (a row that has seen nothing: every weight is 2^-inf = 0)
+                    const __nv_bfloat162 plo = __floats2bfloat162_rn(a_ex2(fmaf(sc[0], scale_log2, -ref0)), a_ex2(fmaf(sc[1], scale_log2, -ref1)));
+                    const __nv_bfloat162 phi = __floats2bfloat162_rn(a_ex2(fmaf(sc[2], scale_log2, -ref0)), a_ex2(fmaf(sc[3], scale_log2, -ref1)));
+                    l_run[nt][0] += __low2float(plo) + __low2float(phi);     // the sum of what the tensor cores will see
+                    l_run[nt][1] += __high2float(plo) + __high2float(phi);
                     pbf[mt][nt][0] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&plo));
                     pbf[mt][nt][1] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&phi));
-                }
-                l_run[nt][0] = l_run[nt][0] * f[0] + ls[0];
-                l_run[nt][1] = l_run[nt][1] * f[1] + ls[1];
-#pragma unroll
-                for (int dt = 0; dt < KS; ++dt) {
-                    o[nt][dt][0] *= f[0]; o[nt][dt][1] *= f[1]; o[nt][dt][2] *= f[0]; o[nt][dt][3] *= f[1];
                 }
             }
             // ---- O^T[channel][row] += V^T P^T
 #pragma unroll
-            for (int dt = 0; dt < KS; ++dt) {
+            for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
+                for (int dt = 0; dt < KS; ++dt) {
                     const int row = mt * 16 + (lane & 7) + (lane >> 4) * 8;
                     const int c = 2 * dt + ((lane >> 3) & 1);
                     uint32_t a[4];
@@ -330,8 +343,8 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    e = paged_tensor_map(&mk, pv.k, pv, W_TILE);
-    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, W_TILE);
+    e = paged_tensor_map(&mk, pv.k, pv, S::TILE);
+    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, S::TILE);
     if (e != cudaSuccess) return e;
     count_launch();
     const dim3 grid(PAGED_SMS), block(S::TEAMS * TW * 32);
