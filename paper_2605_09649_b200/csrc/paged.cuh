@@ -94,40 +94,89 @@ __device__ __forceinline__ PagedCost paged_cost(const PagedBatch& pb, const Page
     return c;
 }
 
-constexpr int PAGED_GROUPS = 1024;            // groups of consecutive requests in the shared-memory table
+// 64-bit quotients are a long routine; nearly all of them have operands of 32 bits.
+__device__ __forceinline__ long long paged_div(long long a, int b) {
+    return (unsigned long long)a >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
+
+constexpr int PAGED_GROUPS = 512;             // groups of consecutive requests in the shared-memory table
+struct PagedTableMem {                        // shared memory of the table
+    long long grp[PAGED_GROUPS + 1];          // steps before a group
+    int4 req[PAGED_GROUPS];                   // {row0, n, len, 0} of each request where a group is one request
+};
 struct PagedTable {
-    long long* grp;                           // shared [PAGED_GROUPS + 1]: steps before a group
+    PagedTableMem* mem;
     int gsz, ngrp, heads;
     int tile_rows, min_rows, max_rows;
     long long total;
     int workers;                              // workers that take part: no share is under min_share steps
+    long long quot;                           // total = quot * workers + rem
+    int rem;
+    // First step of worker w: floor(total w / workers).
+    __device__ __forceinline__ long long share(int w) const { return quot * w + (long long)((unsigned)(rem * w) / (unsigned)workers); }
 };
+
+__device__ __forceinline__ void paged_finish_table(PagedTable& t, int R, int max_workers, int min_share, long long* prefix) {
+    t.total = t.mem->grp[t.ngrp];
+    t.workers = (int)min((long long)max_workers, paged_div(t.total + min_share - 1, min_share));
+    t.quot = t.workers ? paged_div(t.total, t.workers) : 0;
+    t.rem = (int)(t.total - t.quot * t.workers);
+    if (prefix && blockIdx.x == 0 && threadIdx.x == 0) { prefix[R] = t.total; prefix[R + 1] = t.workers; }
+}
 
 // Every thread of the block calls it.  prefix (may be null): steps before each request, [R + 1], written by block 0;
 // prefix[R + 1] = workers.
 __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
-                                                  int max_rows, int max_workers, int min_share, long long* grp, long long* prefix) {
-    t.grp = grp;
+                                                  int max_rows, int max_workers, int min_share, PagedTableMem* mem, long long* prefix) {
+    t.mem = mem;
     t.heads = heads;
     t.tile_rows = tile_rows; t.min_rows = min_rows; t.max_rows = max_rows;
+    if (pb.R <= 32) {                         // one warp, one barrier
+        t.gsz = 1;
+        t.ngrp = pb.R;
+        if (threadIdx.x < 32) {
+            const int r = threadIdx.x;
+            PagedReq q = {0, 0, 0};
+            long long sum = 0;
+            if (r < pb.R) {
+                q = paged_request(pb, r);
+                const PagedCost c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
+                sum = (long long)(c.U * heads) * c.C;
+            }
+            const long long mine = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+                if (r >= o) sum += v;
+            }
+            mem->req[r] = make_int4(q.row0, q.n, q.len, 0);
+            mem->grp[r + 1] = sum;
+            if (r == 0) mem->grp[0] = 0;
+            if (prefix && blockIdx.x == 0 && r < pb.R) prefix[r] = sum - mine;
+        }
+        __syncthreads();
+        paged_finish_table(t, pb.R, max_workers, min_share, prefix);
+        return;
+    }
     t.gsz = (pb.R + PAGED_GROUPS - 1) / PAGED_GROUPS;
-    if (t.gsz < 1) t.gsz = 1;
     t.ngrp = (pb.R + t.gsz - 1) / t.gsz;
     for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
         long long sum = 0;
         for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
-            const PagedCost c = paged_cost(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
-            sum += (long long)c.U * c.C * heads;
+            const PagedReq q = paged_request(pb, r);
+            const PagedCost c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
+            sum += (long long)(c.U * heads) * c.C;
+            if (t.gsz == 1) mem->req[gi] = make_int4(q.row0, q.n, q.len, 0);
         }
-        grp[gi + 1] = sum;
+        mem->grp[gi + 1] = sum;
     }
-    if (threadIdx.x == 0) grp[0] = 0;
+    if (threadIdx.x == 0) mem->grp[0] = 0;
     __syncthreads();
     if (threadIdx.x < 32) {                   // inclusive scan by one warp
         const int lane = threadIdx.x, per = (t.ngrp + 31) / 32;
         const int g0 = min(t.ngrp, lane * per), g1 = min(t.ngrp, g0 + per);
         long long local = 0;
-        for (int gi = g0; gi < g1; ++gi) local += grp[gi + 1];
+        for (int gi = g0; gi < g1; ++gi) local += mem->grp[gi + 1];
         long long incl = local;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -135,31 +184,30 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
             if (lane >= o) incl += v;
         }
         long long run = incl - local;
-        for (int gi = g0; gi < g1; ++gi) { run += grp[gi + 1]; grp[gi + 1] = run; }
+        for (int gi = g0; gi < g1; ++gi) { run += mem->grp[gi + 1]; mem->grp[gi + 1] = run; }
     }
     __syncthreads();
-    t.total = grp[t.ngrp];
-    t.workers = (int)min((long long)max_workers, (t.total + min_share - 1) / min_share);
     if (prefix && blockIdx.x == 0) {
         for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
-            long long run = grp[gi];
+            long long run = mem->grp[gi];
             for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
                 prefix[r] = run;
                 const PagedCost c = paged_cost(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
-                run += (long long)c.U * c.C * heads;
+                run += (long long)(c.U * heads) * c.C;
             }
         }
-        if (threadIdx.x == 0) { prefix[pb.R] = t.total; prefix[pb.R + 1] = t.workers; }
     }
+    paged_finish_table(t, pb.R, max_workers, min_share, prefix);
 }
 
-// First step of worker w; the worker that owns step x.
-__device__ __forceinline__ long long paged_share(long long total, int workers, int w) { return total * w / workers; }
+// The worker whose share holds step x, from the line's total and the number of workers.
 __device__ __forceinline__ int paged_owner(long long total, int workers, long long x) {
-    int w = (int)(((x + 1) * workers - 1) / total);
-    w = min(w, workers - 1);
-    while (w > 0 && paged_share(total, workers, w) > x) --w;
-    while (w + 1 < workers && paged_share(total, workers, w + 1) <= x) ++w;
+    const long long quot = paged_div(total, workers);
+    const int rem = (int)(total - quot * workers);
+    auto share = [&](int w) { return quot * w + (long long)((unsigned)(rem * w) / (unsigned)workers); };
+    int w = min(workers - 1, (int)((float)x / (float)total * (float)workers));       // near; then exact
+    while (w > 0 && share(w) > x) --w;
+    while (w + 1 < workers && share(w + 1) <= x) ++w;
     return w;
 }
 
@@ -183,21 +231,27 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     int lo = 0, hi = t.ngrp - 1;
     while (lo < hi) {                                     // last group that begins at or before x
         const int mid = (lo + hi + 1) >> 1;
-        if (t.grp[mid] <= x) lo = mid; else hi = mid - 1;
+        if (t.mem->grp[mid] <= x) lo = mid; else hi = mid - 1;
     }
-    long long base = t.grp[lo];
+    long long base = t.mem->grp[lo];
     int r = lo * t.gsz;
     PagedReq q;
     PagedCost c;
-    for (;; ++r) {
-        q = paged_request(pb, r);
+    if (t.gsz == 1) {
+        const int4 v = t.mem->req[lo];
+        q.row0 = v.x; q.n = v.y; q.len = v.z;
         c = paged_cost(pb, q, t.tile_rows, t.min_rows, t.max_rows);
-        const long long s = (long long)c.U * c.C * t.heads;
-        if (x < base + s || r + 1 >= pb.R) break;
-        base += s;
+    } else {
+        for (;; ++r) {
+            q = paged_request(pb, r);
+            c = paged_cost(pb, q, t.tile_rows, t.min_rows, t.max_rows);
+            const long long s = (long long)(c.U * t.heads) * c.C;
+            if (x < base + s || r + 1 >= pb.R) break;
+            base += s;
+        }
     }
     const long long off = x - base;
-    const int unit = (int)(off / c.C), v0 = (int)(off - (long long)unit * c.C);
+    const int unit = (int)paged_div(off, c.C), v0 = (int)(off - (long long)unit * c.C);
     it.steps = min((long long)(c.C - v0), end - x);
     const int v1 = v0 + (int)it.steps;
     it.r = r;
@@ -217,8 +271,8 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
         first = pb.window > 0 ? max(0, plo - pb.window + 1) / PAGE : 0;
         count = phi < 0 ? 0 : phi / PAGE + 1 - first;
     }
-    it.p0 = first + (int)((long long)count * v0 / c.C);
-    it.p1 = first + (int)((long long)count * v1 / c.C);
+    it.p0 = first + (count == c.C ? v0 : (int)paged_div((long long)count * v0, c.C));
+    it.p1 = first + (count == c.C ? v1 : (int)paged_div((long long)count * v1, c.C));
     it.slot = (v0 == 0 && v1 == c.C) ? -1 : (v0 == 0 ? 2 * w + 1 : 2 * w);
     return it;
 }
@@ -268,6 +322,29 @@ struct PagedWork {
 };
 
 // ---------------------------------------------------------------- launchers (host)
+// Every kernel of this family is launched as a programmatic dependent of whatever precedes it in the stream: it may be placed
+// (barriers, descriptors) while its predecessor finishes, every one of its threads calls grid_dependency_wait() before it
+// touches memory or returns, and it lets its own successor be placed early.  Behind a kernel that does not take part this is
+// an ordinary launch.  cluster: CTAs per cluster, or 1.
+template <typename... KArgs, typename... Args>
+inline cudaError_t paged_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem_bytes, int cluster, cudaStream_t stream, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem_bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
 cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* keep_lens, const int32_t* new_lens, int32_t* table,
                               int W, int32_t* free_pages, int n_pages, const int32_t* free_count, int32_t* free_count_out,
                               int max_tokens, int32_t* lens_out, int32_t* cu_new, int32_t* slot_map, int32_t* positions,
@@ -283,15 +360,14 @@ cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int i
 // many rows and few parts (the tensor-core kernel's).
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
                               int min_rows, int max_rows, bool many_rows, cudaStream_t st);
-// dependent: launched behind launch_paged_select's kernel as its programmatic dependent.
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
-                                         float scale, const PagedWork& w, bool dependent, cudaStream_t st);
+                                         float scale, const PagedWork& w, cudaStream_t st);
 
-cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows);
+cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows);      // see its definition
 // The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8,
 // 16, 32 or 64 (page selection: g <= 64).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                                        int tile_rows, int max_rows, bool dependent, cudaStream_t st);
+                                        int tile_rows, int max_rows, cudaStream_t st);
 cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                       int min_rows, cudaStream_t st);
 

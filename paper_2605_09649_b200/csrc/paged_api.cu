@@ -153,19 +153,19 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     pb.window = window;
     const cudaStream_t st = (cudaStream_t)stream;
     const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
-    if (!is_bf16 || (pv.d != 64 && pv.d != 128)) return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, false, st), "attention");
+    if (!is_bf16 || (pv.d != 64 && pv.d != 128)) return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st), "attention");
     // Requests of up to 64 rows (tokens x query heads of a KV head) stream through the warp kernel, larger ones go to the
     // tcgen05 kernel; of a batch with both, those of up to 32.  max_new may be wrong: every kernel takes any request, and where
     // both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
     cudaError_t e = cudaSuccess;
     if (most <= PAGED_WARP_ROWS) {
-        e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64, INT_MAX, false, st);
+        e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64, INT_MAX, st);
     } else {
         const bool equal = max_new > 0 && n_tokens == (int64_t)n_req * max_new;    // every request has max_new tokens: one kernel
         const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
         e = launch_paged_attention_tc(pv, pb, q, out, scale, w2, equal ? 1 : 33, st);
-        if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 32, 32, false, st);
+        if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 32, 32, st);
     }
     return done(e, "attention");
 }
@@ -197,8 +197,8 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     if (s != TRIMKV_OK) return s;
     const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
     const bool warp = is_bf16 && (pv.d == 64 || pv.d == 128) && pb.g <= PAGED_WARP_ROWS;
-    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, true, (cudaStream_t)stream)
-                     : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, true, (cudaStream_t)stream),
+    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, (cudaStream_t)stream)
+                     : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, (cudaStream_t)stream),
                 "attention");
 }
 

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(PL_THREADS, PlainShape<T, DP>::CTAS)
 paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T* __restrict__ out, float scale_log2, PagedWork wk) {
     using S = PlainShape<T, DP>;
     extern __shared__ __align__(16) unsigned char s_pl[];
-    __shared__ long long s_grp[PAGED_GROUPS + 1];
+    __shared__ PagedTableMem s_tab;
     float* s_q = reinterpret_cast<float*>(s_pl + S::STAGES * S::STAGE);   // [16][QS]
     float* s_p = s_q + PL_ROWS * S::QS;                           // [16][64]
     float* s_m = s_p + PL_ROWS * PAGE;                            // running maximum, sum, factor of this step
@@ -63,13 +63,13 @@ paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T*
     grid_dependency_wait();
     PagedTable tab;
     const int unit_rows = pb.top > 0 ? g : PL_ROWS;               // rows of a unit (top > 0: one token)
-    paged_build_table(tab, pb, pv.H, PL_ROWS, 1, INT_MAX, (int)gridDim.x, 2, s_grp, wk.prefix);
+    paged_build_table(tab, pb, pv.H, PL_ROWS, 1, INT_MAX, (int)gridDim.x, 2, &s_tab, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;
-    const long long end = paged_share(tab.total, tab.workers, w + 1);
+    const long long end = tab.share(w + 1);
 
-    for (long long x = paged_share(tab.total, tab.workers, w); x < end;) {
+    for (long long x = tab.share(w); x < end;) {
         const PagedItem it = paged_item(tab, pb, x, end, w);
         x += it.steps;
         const int row_first = pb.top > 0 ? it.u * g : it.u * PL_ROWS;    // of the request's n * g rows
@@ -234,14 +234,14 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     const int heads = SPLIT > 1 ? pb.Hq : pv.H;
     const int t = (int)(item / heads), rest = (int)(item % heads);
     const int h = SPLIT > 1 ? rest / g : rest;
-    if (t >= pb.T) return;
+    // cu_new and lens are older than the kernel before this one, which has waited for them
     PagedReq rq;
-    const int r = paged_find_request(pb, t, rq);
+    const int r = paged_find_request(pb, min(t, pb.T - 1), rq);
     const int j = t - rq.row0;
-    if (j < 0 || j >= rq.n) return;
     const PagedCost c = paged_cost(pb, rq, tile_rows, min_rows, max_rows);
-    if (c.U == 0) return;                                         // another kernel's request
+    grid_dependents_may_launch();
     grid_dependency_wait();
+    if (t >= pb.T || j < 0 || j >= rq.n || c.U == 0) return;      // (U = 0: another kernel's request)
     const long long total = wk.prefix[pb.R], before = wk.prefix[r];
     const int workers = (int)wk.prefix[pb.R + 1];
     const int unit_rows = pb.top > 0 ? g : tile_rows;
@@ -249,7 +249,7 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     for (int jj = SPLIT > 1 ? rest % g : 0; jj < g; ++jj) {
         const int row = j * g + jj, u = pb.top > 0 ? j : row / tile_rows, rr = row - u * unit_rows;
         if (u != u_now) {
-            const long long a = before + ((long long)h * c.U + paged_unfold(u, c.U)) * c.C;
+            const long long a = before + (long long)(h * c.U + paged_unfold(u, c.U)) * c.C;
             w0 = paged_owner(total, workers, a);
             n = paged_owner(total, workers, a + c.C - 1) - w0 + 1;
             u_now = u;
@@ -355,25 +355,22 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
 
 template <typename T, int DP>
 cudaError_t run_plain(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                      bool dependent, cudaStream_t st) {
+                      cudaStream_t st) {
     using S = PlainShape<T, DP>;
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_plain_kernel<T, DP>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     static_assert(S::CTAS <= PAGED_PLAIN_CTAS, "the workspace holds the workers' partial results");
-    count_launch();
-    const dim3 grid(PAGED_SMS * S::CTAS), block(PL_THREADS);
-    if (dependent) return launch_dependent(paged_attn_plain_kernel<T, DP>, grid, block, S::SMEM, st, pv, pb, (const T*)q, (T*)out, scale * LOG2E, w);
-    paged_attn_plain_kernel<T, DP><<<grid, block, S::SMEM, st>>>(pv, pb, (const T*)q, (T*)out, scale * LOG2E, w);
-    return cudaGetLastError();
+    return paged_launch(paged_attn_plain_kernel<T, DP>, dim3(PAGED_SMS * S::CTAS), dim3(PL_THREADS), S::SMEM, 1, st, pv, pb, (const T*)q, (T*)out,
+                        scale * LOG2E, w);
 }
 
 template <typename T>
 cudaError_t run_plain_d(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                        bool dependent, cudaStream_t st) {
-    if (pv.d <= 64) return run_plain<T, 64>(pv, pb, q, out, scale, w, dependent, st);
-    if (pv.d <= 128) return run_plain<T, 128>(pv, pb, q, out, scale, w, dependent, st);
-    return run_plain<T, 256>(pv, pb, q, out, scale, w, dependent, st);
+                        cudaStream_t st) {
+    if (pv.d <= 64) return run_plain<T, 64>(pv, pb, q, out, scale, w, st);
+    if (pv.d <= 128) return run_plain<T, 128>(pv, pb, q, out, scale, w, st);
+    return run_plain<T, 256>(pv, pb, q, out, scale, w, st);
 }
 
 }  // namespace
@@ -385,16 +382,15 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
     const bool split = !many_rows && (long long)pb.T * pb.Hq <= PAGED_SMS * 16;
     const long long items = (long long)pb.T * (split ? pb.Hq : pv.H);
     const dim3 grid((unsigned)(split ? items : (items + 3) / 4)), block(128);
-    count_launch();
-    auto go = [&](auto kernel, auto* o) { return launch_dependent(kernel, grid, block, 0, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
+    auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, 0, 1, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
     if (is_bf16) return split ? go(paged_join_kernel<__nv_bfloat16, 4>, (__nv_bfloat16*)out) : go(paged_join_kernel<__nv_bfloat16, 1>, (__nv_bfloat16*)out);
     return split ? go(paged_join_kernel<float, 4>, (float*)out) : go(paged_join_kernel<float, 1>, (float*)out);
 }
 
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
-                                         float scale, const PagedWork& w, bool dependent, cudaStream_t st) {
-    const cudaError_t e = is_bf16 ? run_plain_d<__nv_bfloat16>(pv, pb, q, out, scale, w, dependent, st)
-                                  : run_plain_d<float>(pv, pb, q, out, scale, w, dependent, st);
+                                         float scale, const PagedWork& w, cudaStream_t st) {
+    const cudaError_t e = is_bf16 ? run_plain_d<__nv_bfloat16>(pv, pb, q, out, scale, w, st)
+                                  : run_plain_d<float>(pv, pb, q, out, scale, w, st);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, is_bf16, out, w, PL_ROWS, 1, INT_MAX, false, st);
 }
 

@@ -36,8 +36,8 @@ struct TcShape {
     static constexpr int OFF_Q = STAGES * STAGE;
     static constexpr int OFF_BAR = OFF_Q + Q_BYTES;
     static constexpr int OFF_E0 = OFF_BAR + 256;
-    static constexpr int OFF_GRP = OFF_E0 + T_E0 * 4;
-    static constexpr int SMEM = OFF_GRP + (PAGED_GROUPS + 1) * 8 + 1024;      // 1024: alignment slack
+    static constexpr int OFF_TAB = OFF_E0 + T_E0 * 4;
+    static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 1024;      // 1024: alignment slack
     // D fp32, A and B bf16, M = 128.  S: both K-major, N = 64.  P V: B (V) MN-major, N = D.
     static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -58,7 +58,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(gen + S::OFF_BAR + 240);
     volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 248);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
-    long long* grp_tab = reinterpret_cast<long long*>(gen + S::OFF_GRP);
+    PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(gen + S::OFF_TAB);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
     static_assert(16 * S::STAGES + 64 <= 240, "barriers fit");
 
@@ -72,9 +72,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         }
         *s_fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        a_prefetch_map(&map_k);
+        a_prefetch_map(&map_v);
     }
+    grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, grp_tab, wk.prefix);
+    paged_build_table(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, table_mem, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
@@ -89,10 +92,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     const int grp = (warp >> 2) & 1, wl = warp & 3;
     const int r = wl * 32 + lane, R = grp * T_ROWS + r;               // a softmax thread's row: lane of tensor memory, row of the unit
 
-    const long long end = paged_share(tab.total, tab.workers, w + 1);
+    const long long end = tab.share(w + 1);
     // tiles of the stretches before this one: of the ring, and of group 1, whose barriers rest while it has no rows
     unsigned ct = 0, ct1 = 0;
-    for (long long x = paged_share(tab.total, tab.workers, w); x < end;) {
+    for (long long x = tab.share(w); x < end;) {
         const PagedItem it = paged_item(tab, pb, x, end, w);
         x += it.steps;
         const int ntile = it.p1 - it.p0;
@@ -134,11 +137,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                             const uint32_t dst = base + s * S::STAGE;
                             const int krow = (max(page, 0) * pv.H + it.h) * PAGE;
                             a_bar_expect_tx(full0 + 8 * s, S::STAGE);
-#pragma unroll
-                            for (int p = 0; p < S::PLANES; ++p) {
-                                a_tma_2d(dst + p * T_PLANE, &map_k, p * 64, krow, full0 + 8 * s);
-                                a_tma_2d(dst + (S::PLANES + p) * T_PLANE, &map_v, p * 64, krow, full0 + 8 * s);
-                            }
+                            a_tma_3d(dst, &map_k, 0, krow, 0, full0 + 8 * s);
+                            a_tma_3d(dst + S::PLANES * T_PLANE, &map_v, 0, krow, 0, full0 + 8 * s);
                         }
                     }
                     if (__shfl_sync(0xffffffffu, ok, 0) == 0) {
@@ -363,9 +363,8 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
     e = paged_tensor_map(&mk, pv.k, pv, PAGE);
     if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, PAGE);
     if (e != cudaSuccess) return e;
-    count_launch();
-    paged_attn_tc_kernel<D><<<PAGED_SMS, T_THREADS, S::SMEM, st>>>(mk, mv, pv, pb, (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
-    e = cudaGetLastError();
+    e = paged_launch(paged_attn_tc_kernel<D>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, st, mk, mv, pv, pb, (const __nv_bfloat16*)q, (__nv_bfloat16*)out,
+                     scale * LOG2E, w, min_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, true, st);
 }
 

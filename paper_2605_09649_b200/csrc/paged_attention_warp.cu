@@ -38,8 +38,8 @@ struct WarpShape {
     static constexpr int RING = STAGES * STAGE;
     static constexpr int OFF_BAR = TEAMS * RING;                      // full and empty barrier of each stage
     static constexpr int OFF_META = OFF_BAR + TEAMS * STAGES * 16;
-    static constexpr int OFF_GRP = (OFF_META + TEAMS * STAGES * 4 + 15) & ~15;
-    static constexpr int SMEM = OFF_GRP + (PAGED_GROUPS + 1) * 8 + 1024;      // 1024: alignment slack
+    static constexpr int OFF_TAB = (OFF_META + TEAMS * STAGES * 4 + 15) & ~15;
+    static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 1024;      // 1024: alignment slack
 };
 
 // A place on the line and the stretch of a unit that begins there.
@@ -64,22 +64,21 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + team * S::STAGES * 2;
     uint64_t* empty = bars + S::STAGES;
     volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + team * S::STAGES;      // first entry of the stage's tile; -1: skip
-    long long* grp = reinterpret_cast<long long*>(smem + S::OFF_GRP);
+    PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
     const int unit_rows = SELECT ? g : S::ROWS;
 
     if (lane == 0 && tw == 0)
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(bars + s, 1); mbar_init(empty + s, TW); }
-    // rows that no copy ever filled are multiplied by weights of zero: they must be finite
-    for (int i = (tw * 32 + lane) * 16; i < S::RING; i += TW * 32 * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0u, 0u, 0u, 0u);
+    if (threadIdx.x == 0) { a_prefetch_map(&map_k); a_prefetch_map(&map_v); }
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, grp, wk.prefix);      // (synchronises the block)
+    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, table_mem, wk.prefix);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
     const int w = team * (int)gridDim.x + (int)blockIdx.x;
     if (w >= tab.workers) return;
-    const long long end = paged_share(tab.total, tab.workers, w + 1);
+    const long long end = tab.share(w + 1);
 
     auto at = [&](long long x) {
         WarpCursor c;
@@ -97,7 +96,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         }
         return c;
     };
-    WarpCursor cons = at(paged_share(tab.total, tab.workers, w)), prod = cons;
+    WarpCursor cons = at(tab.share(w)), prod = cons;
     int prod_tile = 0, log_page = 0, phys_page = 0;                   // lane l: page l of the current run of 32
     unsigned issued = 0, consumed = 0;
     bool failed = false;
@@ -122,13 +121,9 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             } else {
                 const uint32_t dst = smem_u32(ring + s * S::STAGE), bar = smem_u32(bars + s);
                 const int row = (pp * pv.H + prod.it.h) * PAGE + half * S::TILE;
-                fence_proxy_async_smem();
-                mbar_expect_tx(bars + s, S::STAGE);
-#pragma unroll
-                for (int p = 0; p < S::PLANES; ++p) {
-                    a_tma_2d(dst + p * S::PLANE, &map_k, p * 64, row, bar);
-                    a_tma_2d(dst + (S::PLANES + p) * S::PLANE, &map_v, p * 64, row, bar);
-                }
+                mbar_expect_tx(bars + s, S::STAGE);                   // (the zeroing of rows below carries its own proxy fence)
+                a_tma_3d(dst, &map_k, 0, row, 0, bar);
+                a_tma_3d(dst + S::PLANES * S::PLANE, &map_v, 0, row, 0, bar);
             }
         }
         ++issued;
@@ -337,7 +332,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 
 template <int D, int NT, int TW, bool SELECT>
 cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows,
-                     bool dependent, cudaStream_t st) {
+                     cudaStream_t st) {
     using S = WarpShape<D, NT, TW>;
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT>), S::SMEM, done);
@@ -346,40 +341,33 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     e = paged_tensor_map(&mk, pv.k, pv, S::TILE);
     if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, S::TILE);
     if (e != cudaSuccess) return e;
-    count_launch();
-    const dim3 grid(PAGED_SMS), block(S::TEAMS * TW * 32);
-    const __nv_bfloat16* qq = (const __nv_bfloat16*)q;
-    __nv_bfloat16* oo = (__nv_bfloat16*)out;
-    if (dependent)
-        e = launch_dependent(paged_attn_warp_kernel<D, NT, TW, SELECT>, grid, block, S::SMEM, st, mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
-    else {
-        paged_attn_warp_kernel<D, NT, TW, SELECT><<<grid, block, S::SMEM, st>>>(mk, mv, pv, pb, qq, oo, scale * LOG2E, w, max_rows);
-        e = cudaGetLastError();
-    }
+    e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, st, mk, mv, pv, pb,
+                     (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, false, st);
 }
 
 }  // namespace
 
-// The pages as a matrix of n_pages x H x 64 rows of d bf16; box 64 columns x box_rows rows, 128-byte swizzle.
+// The pages as n_pages x H x 64 rows of d bf16, their columns cut into planes of 64: dimensions {64, rows, d / 64}; a box is
+// box_rows rows of every plane, each plane 128-byte swizzled, plane after plane.
 cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows) {
     EncodeTiledFnA fn = a_encode_fn();
     if (!fn) return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {(cuuint64_t)pv.d, (cuuint64_t)pv.n_pages * pv.H * PAGE};
-    const cuuint64_t strides[1] = {(cuuint64_t)pv.d * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const cuuint64_t dims[3] = {64, (cuuint64_t)pv.n_pages * pv.H * PAGE, (cuuint64_t)pv.d / 64};
+    const cuuint64_t strides[2] = {(cuuint64_t)pv.d * 2, 128};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)pv.d / 64};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
                ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                                        int tile_rows, int max_rows, bool dependent, cudaStream_t st) {
+                                        int tile_rows, int max_rows, cudaStream_t st) {
     auto go = [&](auto d, auto nt, auto tw) {
         constexpr int D = decltype(d)::value, NT = decltype(nt)::value, TW = decltype(tw)::value;
-        return pb.top > 0 ? run_warp<D, NT, TW, true>(pv, pb, q, out, scale, w, max_rows, dependent, st)
-                          : run_warp<D, NT, TW, false>(pv, pb, q, out, scale, w, max_rows, dependent, st);
+        return pb.top > 0 ? run_warp<D, NT, TW, true>(pv, pb, q, out, scale, w, max_rows, st)
+                          : run_warp<D, NT, TW, false>(pv, pb, q, out, scale, w, max_rows, st);
     };
     auto rows = [&](auto d) {
         using One = std::integral_constant<int, 1>;

@@ -39,7 +39,7 @@ __device__ __forceinline__ int plan_find(const int* at, int n, int x) {
 
 __device__ __forceinline__ int plan_pages(int n) { return (int)(((unsigned)n + PAGE - 1u) / PAGE); }
 
-__global__ void __cluster_dims__(PLAN_CTAS, 1, 1) __launch_bounds__(PLAN_THREADS, 1)
+__global__ void __launch_bounds__(PLAN_THREADS, 1)
 paged_plan_kernel(int R, const int32_t* old_lens, const int32_t* keep_lens, const int32_t* new_lens, int32_t* table, int W,
                   int32_t* free_pages, int n_pages, const int32_t* free_count, int32_t* free_count_out, int max_tokens,
                   int32_t* lens_out, int32_t* cu_new, int32_t* slot_map, int32_t* positions, int32_t* status) {
@@ -55,6 +55,8 @@ paged_plan_kernel(int R, const int32_t* old_lens, const int32_t* keep_lens, cons
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) s_bad = 0;
+    grid_dependency_wait();
+    grid_dependents_may_launch();
     __syncthreads();
 
     // ---- lengths, and their sums: thread i takes the requests [i per, (i + 1) per)
@@ -236,6 +238,8 @@ paged_append_kernel(char* __restrict__ k_pages, char* __restrict__ v_pages, char
     __shared__ uint4 s_part[2][WARPS][16];
     const int rb = d * (int)sizeof(T), cpr = rb / 16;         // bytes, 16-byte chunks per row
     const int slots = n_pages * PAGE;
+    grid_dependency_wait();
+    grid_dependents_may_launch();
     if ((int)blockIdx.x < copy_blocks) {
         const unsigned per_tok = (unsigned)(H * cpr);
         const long long n = (long long)T_rows * per_tok;
@@ -336,10 +340,8 @@ cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* kee
     const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_plan_kernel),
                                            (int)(((size_t)6 * PAGED_MAX_REQ + 3) * sizeof(int)), done);
     if (e != cudaSuccess) return e;
-    paged_plan_kernel<<<PLAN_CTAS, PLAN_THREADS, smem, st>>>(R, old_lens, keep_lens, new_lens, table, W, free_pages, n_pages, free_count,
-                                                             free_count_out, max_tokens, lens_out, cu_new, slot_map, positions, status);
-    count_launch();
-    return cudaGetLastError();
+    return paged_launch(paged_plan_kernel, dim3(PLAN_CTAS), dim3(PLAN_THREADS), smem, PLAN_CTAS, st, R, old_lens, keep_lens, new_lens, table, W, free_pages,
+                        n_pages, free_count, free_count_out, max_tokens, lens_out, cu_new, slot_map, positions, status);
 }
 
 cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_pages, char* bounds, int is_bf16, int T, const void* k,
@@ -356,12 +358,10 @@ cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_page
     const long long items = bounds ? (long long)((T + group - 1) / group) * pv.H : 0;
     const unsigned blocks = (unsigned)(copy_blocks + items);
     auto go = [&](auto kernel) {
-        kernel<<<blocks, APP_THREADS, 0, st>>>(k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k, k_stride, (const char*)v, v_stride,
-                                               slot_map, status, (int)copy_blocks, group);
+        return paged_launch(kernel, dim3(blocks), dim3(APP_THREADS), 0, 1, st, k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k, k_stride,
+                            (const char*)v, v_stride, slot_map, status, (int)copy_blocks, group);
     };
-    if (is_bf16) go(paged_append_kernel<__nv_bfloat16>); else go(paged_append_kernel<float>);
-    count_launch();
-    return cudaGetLastError();
+    return is_bf16 ? go(paged_append_kernel<__nv_bfloat16>) : go(paged_append_kernel<float>);
 }
 
 }  // namespace tkv

@@ -64,6 +64,8 @@ paged_select_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, int32_
     const int t = unit / pv.H, h = unit % pv.H;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t* sel = selected + (size_t)unit * pb.top;
+    grid_dependency_wait();
+    grid_dependents_may_launch();
 
     // the token's request: last r with cu_new[r] <= t
     int lo = 0, hi = pb.R - 1;
@@ -568,6 +570,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
     __shared__ int s_req[NTOK], s_np[NTOK], s_hard[NTOK];         // request of each token (-1: none), pages up to its own
     __shared__ unsigned s_err[NTOK];
     __shared__ SelShared sh;
+    grid_dependency_wait();
     grid_dependents_may_launch();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)blockIdx.x % nclust, unit = (int)blockIdx.x / nclust;
@@ -775,19 +778,7 @@ cudaError_t run_select_mma(const PagedView& pv, const PagedBatch& pb, const void
     auto go = [&](auto kernel, std::atomic<unsigned long long>& done) {
         const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(kernel), PAGED_SELECT_SMEM, done);
         if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(units * nclust));
-        cfg.blockDim = dim3(SEL_THREADS);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = nclust;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        count_launch();
-        return cudaLaunchKernelEx(&cfg, kernel, pv, pb, (const __nv_bfloat16*)q, selected, nclust, ntok);
+        return paged_launch(kernel, dim3((unsigned)(units * nclust)), dim3(SEL_THREADS), smem, nclust, st, pv, pb, (const __nv_bfloat16*)q, selected, nclust, ntok);
     };
     auto by_width = [&](auto dk) {
         constexpr int DK = decltype(dk)::value;
@@ -814,19 +805,7 @@ cudaError_t run_select(const PagedView& pv, const PagedBatch& pb, const void* q,
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_select_kernel<T>), PAGED_SELECT_SMEM, done);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * nclust));
-    cfg.blockDim = dim3(SEL_THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = nclust;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    count_launch();
-    return cudaLaunchKernelEx(&cfg, paged_select_kernel<T>, pv, pb, (const T*)q, selected, nclust, chunks);
+    return paged_launch(paged_select_kernel<T>, dim3((unsigned)(units * nclust)), dim3(SEL_THREADS), smem, nclust, st, pv, pb, (const T*)q, selected, nclust, chunks);
 }
 
 }  // namespace

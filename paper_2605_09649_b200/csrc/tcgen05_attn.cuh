@@ -40,6 +40,15 @@ __device__ __forceinline__ void a_tma_2d(uint32_t dst, const CUtensorMap* map, i
         "l"(map), "r"(c0), "r"(c1), "r"(bar)
         : "memory");
 }
+__device__ __forceinline__ void a_tma_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void a_prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 // Shared-memory matrix descriptor, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart (stride byte
 // offset).  lead_bytes: distance between 64-element blocks along M/N of an MN-major operand (unused for K-major: 16).
 __device__ __forceinline__ uint64_t a_desc(uint32_t saddr, uint32_t lead_bytes) {

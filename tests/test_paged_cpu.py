@@ -91,7 +91,7 @@ def test_sparse_attention_refusals(kw):
 def test_sparse_attention_needs_bounds_and_a_table_that_fits():
     refused("trimkv_paged_sparse_attention", attention_args(cache(key_bounds=None), sparse=True), binding.E_ARG)
     need = binding.paged_workspace_bytes(128, 1, 256)
-    refused("trimkv_paged_sparse_attention", attention_args(cache(kv_heads=1, head_dim=256), sparse=True, hq=128, qs=128 * 256, ws_bytes=need), binding.E_UNSUPPORTED)
+    refused("trimkv_paged_sparse_attention", attention_args(cache(kv_heads=1, head_dim=256, kv_dtype=1), sparse=True, hq=128, qs=128 * 256, ws_bytes=need), binding.E_UNSUPPORTED)
 
 
 def test_calls_without_tokens_launch_nothing():
