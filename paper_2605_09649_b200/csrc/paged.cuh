@@ -46,10 +46,17 @@ struct PagedBatch {
     int window;               // > 0: a token sees the last `window` entries up to its own; 0: all of them
     int top, sink, recent;    // page selection (top = 0: every page is read)
     const int32_t* selected;  // [T][H][top] pages to read, ascending, -1 behind the last
+    // Page selection may run two kernels: pick < 0 marks the one that reads each token's pages for itself (top > 0), pick > 0 the
+    // one that walks the union of a unit's tokens' pages (top = 0, the selection's width in pick_top).  A request goes to the
+    // second if it has at least PAGED_PICK_ROWS rows and at most pick_pages pages.  0: one kernel takes all requests.
+    int pick, pick_top, pick_pages;
     int32_t* status;          // latched status, may be null
 };
 
 constexpr int PAGED_MAX_REQ = 8192;
+constexpr int PAGED_PICK_ROWS = 64;           // see PagedBatch::pick
+constexpr int PAGED_PICK_WORDS = 3968;        // shared memory of the union: bits (tokens of a unit x pages / 32)
+constexpr int PAGED_PICK_PAGES = 1024;        // ... and its list of pages
 
 // Rows and length of request r; a request whose offsets or length are out of range counts as having no rows.
 struct PagedReq { int row0, n, len; };
@@ -78,8 +85,9 @@ struct PagedCost { int U, C; };
 __device__ __forceinline__ PagedCost paged_cost(const PagedBatch& pb, const PagedReq& q, int tile_rows, int min_rows, int max_rows) {
     PagedCost c;
     const int rows = q.n * pb.g;
-    if (q.n == 0 || rows < min_rows || rows > max_rows) { c.U = 0; c.C = 1; return c; }
     int pages = (q.len + PAGE - 1) / PAGE;
+    const bool walks = rows >= PAGED_PICK_ROWS && pages <= pb.pick_pages;
+    if (q.n == 0 || rows < min_rows || rows > max_rows || (pb.pick != 0 && walks != (pb.pick > 0))) { c.U = 0; c.C = 1; return c; }
     if (pb.top > 0) {
         c.U = q.n;
         pages = min(pages, pb.top);
@@ -325,9 +333,9 @@ struct PagedWork {
 // Every kernel of this family is launched as a programmatic dependent of whatever precedes it in the stream: it may be placed
 // (barriers, descriptors) while its predecessor finishes, every one of its threads calls grid_dependency_wait() before it
 // touches memory or returns, and it lets its own successor be placed early.  Behind a kernel that does not take part this is
-// an ordinary launch.  cluster: CTAs per cluster, or 1.
+// an ordinary launch.  cluster: CTAs per cluster, or 1.  early = false: an ordinary launch.
 template <typename... KArgs, typename... Args>
-inline cudaError_t paged_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem_bytes, int cluster, cudaStream_t stream, Args&&... args) {
+inline cudaError_t paged_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem_bytes, int cluster, bool early, cudaStream_t stream, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
@@ -335,7 +343,7 @@ inline cudaError_t paged_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block,
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
@@ -363,7 +371,7 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
                                          float scale, const PagedWork& w, cudaStream_t st);
 
-cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows);      // see its definition
+cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows, int box_planes);      // see its definition
 // The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8,
 // 16, 32 or 64 (page selection: g <= 64).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,

@@ -1,6 +1,8 @@
 // C entry points of the caller-owned paged cache: argument checks, workspace layout, choice of kernels.
 #include <math.h>
 
+#include <algorithm>
+
 #include "paged.cuh"
 
 using namespace tkv;
@@ -195,11 +197,33 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     pb.selected = selected;
     s = done(launch_paged_select(pv, pb, is_bf16, q, selected, (cudaStream_t)stream), "page selection");
     if (s != TRIMKV_OK) return s;
+    const cudaStream_t st = (cudaStream_t)stream;
     const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
-    const bool warp = is_bf16 && (pv.d == 64 || pv.d == 128) && pb.g <= PAGED_WARP_ROWS;
-    return done(warp ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, (cudaStream_t)stream)
-                     : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, (cudaStream_t)stream),
-                "attention");
+    cudaError_t e = cudaSuccess;
+    if (is_bf16 && (pv.d == 64 || pv.d == 128)) {
+        // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
+        // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
+        // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page, and two requests cannot differ in width.
+        const int unit_tokens = PAGED_TC_ROWS / pb.g + 2;
+        const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
+        pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);
+        // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request
+        const bool walk = pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
+        if (walk) {
+            PagedBatch pu = pb;
+            pu.top = 0;
+            pu.pick = 1;
+            pu.pick_top = top_pages;
+            const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
+            e = launch_paged_attention_tc(pv, pu, q, out, scale, w2, 1, st);
+            pb.pick = -1;
+        }
+        if (e == cudaSuccess)
+            e = pb.g <= PAGED_WARP_ROWS ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, st)
+                                        : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st);
+    } else
+        e = launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st);
+    return done(e, "attention");
 }
 
 }  // extern "C"

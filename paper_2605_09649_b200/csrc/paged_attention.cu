@@ -361,7 +361,7 @@ cudaError_t run_plain(const PagedView& pv, const PagedBatch& pb, const void* q, 
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_plain_kernel<T, DP>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     static_assert(S::CTAS <= PAGED_PLAIN_CTAS, "the workspace holds the workers' partial results");
-    return paged_launch(paged_attn_plain_kernel<T, DP>, dim3(PAGED_SMS * S::CTAS), dim3(PL_THREADS), S::SMEM, 1, st, pv, pb, (const T*)q, (T*)out,
+    return paged_launch(paged_attn_plain_kernel<T, DP>, dim3(PAGED_SMS * S::CTAS), dim3(PL_THREADS), S::SMEM, 1, true, st, pv, pb, (const T*)q, (T*)out,
                         scale * LOG2E, w);
 }
 
@@ -382,7 +382,7 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
     const bool split = !many_rows && (long long)pb.T * pb.Hq <= PAGED_SMS * 16;
     const long long items = (long long)pb.T * (split ? pb.Hq : pv.H);
     const dim3 grid((unsigned)(split ? items : (items + 3) / 4)), block(128);
-    auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, 0, 1, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
+    auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, 0, 1, true, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
     if (is_bf16) return split ? go(paged_join_kernel<__nv_bfloat16, 4>, (__nv_bfloat16*)out) : go(paged_join_kernel<__nv_bfloat16, 1>, (__nv_bfloat16*)out);
     return split ? go(paged_join_kernel<float, 4>, (float*)out) : go(paged_join_kernel<float, 1>, (float*)out);
 }

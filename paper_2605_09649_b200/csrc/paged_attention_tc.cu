@@ -1,15 +1,25 @@
 // Attention over the caller-owned paged cache for many query rows, on tcgen05: bf16, head size 64 or 128.
 //
-// A unit is 256 (token, query head) rows of one KV head in two groups of 128 that share every K/V tile; a tile is one page
-// (64 entries).  One persistent CTA per SM takes an equal share of the line of page steps (paged.cuh) and meets a stretch of a
-// unit at a time.  TMA copies the page's K and V as 64-column planes with the 128-byte swizzle: K planes are K-major operands
-// of S = Q K^T, V planes MN-major operands of O += P V.  Warps 0-3 / 4-7 are the softmax warps of group 0 / 1 (a thread owns a
-// row: S from tensor memory, masked, exponentiated, P back to tensor memory as the A operand of P V), warp 8 issues the
-// copies, warps 9 and 10 the products of a group each; S is double-buffered and issued two tiles ahead of the P V that needs the
-// softmax.  The maximum is only raised (and O rescaled) when it grows by more than 2^8.  A third of the exponentials are
-// evaluated on the FMA pipe.  A unit of 128 rows or fewer leaves group 1 idle.  V rows behind a request's last entry are zeroed
-// in shared memory before the product reads them (they may hold NaN).  Every wait is bounded; one that runs out latches
-// TRIMKV_E_TIMEOUT.
+// A unit is 256 (token, query head) rows of one KV head in two groups of 128 that share every K/V tile; a tile is two pages
+// (128 entries; the last of a stretch may be one).  One persistent CTA per SM takes an equal share of the line of page steps
+// (paged.cuh) and meets a stretch of a unit at a time.  TMA copies K and V as 64-column planes with the 128-byte swizzle:
+// K planes (both pages' rows) are K-major operands of S = Q K^T, V planes MN-major operands of O += P V.  Warps 0-7 / 8-15
+// are the softmax warps of group 0 / 1, two threads per row with a page of the tile each (S from tensor memory, masked,
+// exponentiated, P back over it as the A operand of P V; the two exchange their maxima through shared memory and a barrier of
+// their warps), warp 16 issues the copies, warp 17 the products, group 0's and group 1's in turn: the pipe runs P V and the next S
+// of one group while the other group's softmax works on its S.  (With an issuer per group the pipe served both at once, and the
+// groups fell into step: products, then softmax, 5800 cycles a tile.)  The maximum is only raised (and O rescaled) when it
+// grows by more than 2^8.  A third of the exponentials are evaluated on the FMA pipe.  A unit of 128 rows or fewer leaves group
+// 1 idle.  V rows behind a request's last entry are zeroed in shared memory before the product reads them (they may hold
+// NaN).  Every wait is bounded; one that runs out latches TRIMKV_E_TIMEOUT.
+//
+// Why 128 entries: an S of 64 columns reads 6 KB of operands from shared memory for 32 cycles of products, more than the
+// 128 bytes a cycle it delivers, and doubles the hand-overs between the pipes per entry (measured with 64: 610 us for 4 x 512
+// tokens over 16K, the pipe 45 % busy).
+//
+// PICK: attention over selected pages for requests with many tokens.  Tokens next to one another select much the same
+// pages, so a unit walks the union of its tokens' pages once and masks, row by row, the pages that a token did not select
+// (a bit per token and page in shared memory), instead of fetching every token's pages for itself.
 #include "paged.cuh"
 #include "tcgen05_attn.cuh"
 
@@ -21,55 +31,129 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int T_ROWS = 128, T_UNIT = PAGED_TC_ROWS;
 constexpr int T_PLANE = PAGE * 128;                                   // 64 entries x 64 columns
 constexpr int T_QPLANE = T_ROWS * 128;
-constexpr int T_THREADS = 352;
-constexpr int T_TMEM_COLS = 512;      // group g: S of even / odd tiles at columns 128 g, 128 g + 64 (P over the first half); O at 256 + 128 g
+constexpr int T_SOFT = 16;                                            // softmax warps
+constexpr int T_THREADS = (T_SOFT + 2) * 32;
+constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
 constexpr float T_RESCALE_STEP = 8.0f;
-constexpr int T_E0 = 16;              // ring of the tiles' first entries: more than a stage count and two tiles
+constexpr int T_STAGES = 2;           // tiles of K, and of V, in shared memory
+constexpr int T_E0 = 8;               // ring of the tiles' first entries (two pages each): more than the tiles in flight
+constexpr int T_NO_PAGE = INT_MAX / 2;
 
-template <int D>
+template <int D, bool PICK>
 struct TcShape {
     static constexpr int PLANES = D / 64;
-    static constexpr int STAGE = 2 * PLANES * T_PLANE;
-    static constexpr int STAGES = D == 128 ? 4 : 6;
-    static constexpr int Q_BYTES = 2 * PLANES * T_QPLANE;
-    static constexpr int OFF_Q = STAGES * STAGE;
-    static constexpr int OFF_BAR = OFF_Q + Q_BYTES;
+    static constexpr int KPLANE = 2 * T_PLANE;                        // 128 entries x 64 columns
+    static constexpr int TILE = PLANES * KPLANE;                      // K of a tile; V of a tile
+    static constexpr int OFF_V = T_STAGES * TILE;
+    static constexpr int OFF_Q = 2 * T_STAGES * TILE;
+    static constexpr int OFF_BAR = OFF_Q + 2 * PLANES * T_QPLANE;
     static constexpr int OFF_E0 = OFF_BAR + 256;
-    static constexpr int OFF_TAB = OFF_E0 + T_E0 * 4;
-    static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 1024;      // 1024: alignment slack
-    // D fp32, A and B bf16, M = 128.  S: both K-major, N = 64.  P V: B (V) MN-major, N = D.
-    static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [exchange parity][group][half][row] maxima; at the end: sums
+    static constexpr int OFF_TAB = OFF_MX + 2 * 2 * 2 * T_ROWS * 4;
+    static constexpr int OFF_BITS = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;
+    static constexpr int OFF_LIST = OFF_BITS + (PICK ? PAGED_PICK_WORDS * 4 : 0);
+    static constexpr int SMEM = OFF_LIST + (PICK ? PAGED_PICK_PAGES * 2 : 0) + 1024;      // 1024: alignment slack
+    // D fp32, A and B bf16, M = 128.  S: both K-major, N = 64 per page.  P V: B (V) MN-major, N = D.
+    static constexpr uint32_t IDESC_S1 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    static constexpr uint32_t IDESC_S2 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 };
 
-template <int D>
+__device__ __forceinline__ void t_tmem_ld16(uint32_t taddr, uint32_t* t) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(t[0]), "=r"(t[1]), "=r"(t[2]), "=r"(t[3]), "=r"(t[4]), "=r"(t[5]), "=r"(t[6]), "=r"(t[7]), "=r"(t[8]), "=r"(t[9]), "=r"(t[10]),
+          "=r"(t[11]), "=r"(t[12]), "=r"(t[13]), "=r"(t[14]), "=r"(t[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void t_tmem_st16(uint32_t taddr, const uint32_t* t) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(t[0]), "r"(t[1]), "r"(t[2]), "r"(t[3]), "r"(t[4]), "r"(t[5]), "r"(t[6]), "r"(t[7]), "r"(t[8]), "r"(t[9]), "r"(t[10]), "r"(t[11]),
+        "r"(t[12]), "r"(t[13]), "r"(t[14]), "r"(t[15])
+        : "memory");
+}
+__device__ __forceinline__ void t_tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void t_tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Products issued by one lane of a converged warp: every operand is the same in all lanes, so it stays in uniform registers and
+// an instruction costs a few issue slots.  (Behind a branch on the lane each took about 120 cycles beside the softmax warps, more
+// than the 64 of its product.)  Descriptors: the low words change, the high words are t_desc_hi() for both operands.
+constexpr uint32_t T_DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);           // rows in groups of 8, 1024 bytes apart; 128-byte swizzle
+__device__ __forceinline__ uint32_t t_desc_lo(uint32_t saddr, uint32_t lead_bytes) { return ((saddr & 0x3FFFFu) >> 4) | ((lead_bytes >> 4) << 16); }
+__device__ __forceinline__ uint32_t t_elect() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
+}
+__device__ __forceinline__ void t_umma(uint32_t leader, uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 e, %0, 0;\n\t"
+        "mov.b64 a, {%2, %6};\n\t"
+        "mov.b64 b, {%3, %6};\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%1], a, b, %4, p;\n\t}" ::"r"(leader),
+        "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(T_DESC_HI)
+        : "memory");
+}
+__device__ __forceinline__ void t_umma_ts(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "setp.ne.b32 e, %0, 0;\n\t"
+        "mov.b64 b, {%3, %6};\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], b, %4, p;\n\t}" ::"r"(leader),
+        "r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(T_DESC_HI)
+        : "memory");
+}
+__device__ __forceinline__ void t_commit(uint32_t leader, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %0, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(leader), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t t_uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+// Barrier of the two warps that share 32 rows, the n-th time: an mbarrier, so that the wait has a limit.  false: gave up.
+__device__ __forceinline__ bool t_pair_sync(uint32_t bar, unsigned n) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) a_bar_arrive(bar);
+    return __all_sync(0xffffffffu, a_bar_wait(bar, n & 1u));
+}
+
+template <int D, bool PICK>
 __global__ void __launch_bounds__(T_THREADS, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
                      const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int min_rows) {
-    using S = TcShape<D>;
+    using S = TcShape<D, PICK>;
     extern __shared__ unsigned char t_smem_raw[];
     const uint32_t raw = a_smem(t_smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     unsigned char* gen = t_smem_raw + (base - raw);
     const uint32_t bars = base + S::OFF_BAR;
-    const uint32_t full0 = bars, empty0 = bars + 8 * S::STAGES, s_ready0 = empty0 + 8 * S::STAGES /* [group][tile parity] */,
-                   p_ready0 = s_ready0 + 32, pv_done0 = p_ready0 + 16;
+    const uint32_t k_full = bars, k_empty = bars + 16, v_full = bars + 32, v_empty = bars + 48 /* [stage] each */, s_ready0 = bars + 64,
+                   p_ready0 = bars + 80, done0 = bars + 96 /* [group] each */, pair0 = bars + 112 /* [group][32 rows] */;
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(gen + S::OFF_BAR + 240);
-    volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 248);
+    volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 244);
+    volatile int* s_nlist = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 248);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
+    float* s_mx = reinterpret_cast<float*>(gen + S::OFF_MX);
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(gen + S::OFF_TAB);
+    uint32_t* s_bits = reinterpret_cast<uint32_t*>(gen + S::OFF_BITS);
+    uint16_t* s_list = reinterpret_cast<uint16_t*>(gen + S::OFF_LIST);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
-    static_assert(16 * S::STAGES + 64 <= 240, "barriers fit");
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::STAGES; ++s) { a_bar_init(full0 + 8 * s, 1); a_bar_init(empty0 + 8 * s, 2); }   // both issuers free a stage
-        for (int gq = 0; gq < 2; ++gq) {
-            a_bar_init(s_ready0 + 16 * gq, 1);
-            a_bar_init(s_ready0 + 16 * gq + 8, 1);
-            a_bar_init(p_ready0 + 8 * gq, 4);
-            a_bar_init(pv_done0 + 8 * gq, 1);
+        for (int i = 0; i < 2; ++i) {
+            a_bar_init(k_full + 8 * i, 1);
+            a_bar_init(k_empty + 8 * i, 1);
+            a_bar_init(v_full + 8 * i, 1);
+            a_bar_init(v_empty + 8 * i, 1);
+            a_bar_init(s_ready0 + 8 * i, 1);
+            a_bar_init(p_ready0 + 8 * i, T_SOFT / 2);
+            a_bar_init(done0 + 8 * i, 1);
         }
+        for (int i = 0; i < 8; ++i) a_bar_init(pair0 + 8 * i, 2);
         *s_fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         a_prefetch_map(&map_k);
@@ -81,7 +165,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
-    if (warp == 9) {
+    if (warp == T_SOFT + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(a_smem((const void*)s_tmem)), "r"(T_TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -89,29 +173,73 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     __syncthreads();
     a_fence_after();
     const uint32_t tmem = *s_tmem;
-    const int grp = (warp >> 2) & 1, wl = warp & 3;
-    const int r = wl * 32 + lane, R = grp * T_ROWS + r;               // a softmax thread's row: lane of tensor memory, row of the unit
+    // softmax warps: group, half of the tile's entries, 32 rows of the group (a warp reaches the tensor-memory lanes of its number mod 4)
+    const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
+    const int r = wl * 32 + lane, R = grp * T_ROWS + r;               // row: lane of tensor memory, row of the unit
 
     const long long end = tab.share(w + 1);
-    // tiles of the stretches before this one: of the ring, and of group 1, whose barriers rest while it has no rows
-    unsigned ct = 0, ct1 = 0;
+    // tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
+    // stretches with tiles, of group 0 and 1
+    unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
+    unsigned ex = 0;                                                  // exchanges between the halves of a row so far
     for (long long x = tab.share(w); x < end;) {
         const PagedItem it = paged_item(tab, pb, x, end, w);
         x += it.steps;
-        const int ntile = it.p1 - it.p0;
+        int npage = it.p1 - it.p0;
         const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
         const bool both = rows > T_ROWS;
-        const bool valid = warp < 8 && R < rows;
-        const int tok = valid ? (row_first + R) / g : 0, head = valid ? (row_first + R) % g : 0;
+        const bool soft = warp < T_SOFT && (grp == 0 || both);
+        const bool valid = soft && R < rows;
+        const int tok = valid ? (row_first + R) / g : it.tok0, head = valid ? (row_first + R) % g : 0;
         const int pos = it.q.len - it.q.n + tok;
         const int see_hi = valid ? max(pos + 1, 0) : 0;               // entries the row sees: see_lo .. see_hi - 1
         const int see_lo = valid && pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
+        const int w0 = it.p0 >> 5, nw = npage > 0 ? ((it.p1 - 1) >> 5) - w0 + 1 : 0;      // words of the stretch's pages
+        if (PICK && npage > 0) {
+            // ---- which token selected which page of the stretch; the union, ascending
+            const int ntok = it.tok1 - it.tok0 + 1;
+            for (int i = threadIdx.x; i < ntok * nw; i += T_THREADS) s_bits[i] = 0u;
+            __syncthreads();
+            for (int i = threadIdx.x; i < ntok * pb.pick_top; i += T_THREADS) {
+                const int tk = i / pb.pick_top, e = i - tk * pb.pick_top;
+                const int page = pb.selected[((size_t)(it.q.row0 + it.tok0 + tk) * pv.H + it.h) * pb.pick_top + e];
+                if (page >= it.p0 && page < it.p1) atomicOr(&s_bits[tk * nw + (page >> 5) - w0], 1u << (page & 31));
+            }
+            __syncthreads();
+            if (warp == 0) {
+                int at = 0;
+                for (int i0 = 0; i0 < nw; i0 += 32) {
+                    uint32_t any = 0u;
+                    if (i0 + lane < nw)
+                        for (int tk = 0; tk < ntok; ++tk) any |= s_bits[tk * nw + i0 + lane];
+                    int before = __popc(any);
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int v = __shfl_up_sync(0xffffffffu, before, o);
+                        if (lane >= o) before += v;
+                    }
+                    const int all = __shfl_sync(0xffffffffu, before, 31);
+                    int put = at + before - __popc(any);
+                    while (any) {
+                        const int b = __ffs(any) - 1;
+                        any &= any - 1;
+                        s_list[put++] = (uint16_t)((w0 + i0 + lane) * 32 + b);
+                    }
+                    at += all;
+                }
+                if (lane == 0) *s_nlist = at;
+            }
+            __syncthreads();
+            npage = *s_nlist;
+        }
+        const int ntile = (npage + 1) / 2;
         if (ntile > 0) {
-            if (warp < 8 && (grp == 0 || both)) {
+            if (soft) {
                 const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + tok) * pb.q_stride + (size_t)(it.h * g + head) * D);
                 unsigned char* qdst = gen + S::OFF_Q + grp * S::PLANES * T_QPLANE + r * 128;
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
+                for (int i = 0; i < D / 16; ++i) {
+                    const int c = half * (D / 16) + i;
                     const uint4 v = valid ? src[c] : make_uint4(0u, 0u, 0u, 0u);
                     *reinterpret_cast<uint4*>(qdst + (c >> 3) * T_QPLANE + (((c & 7) ^ (r & 7)) << 4)) = v;
                 }
@@ -121,250 +249,302 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             __syncthreads();
             a_fence_after();
 
-            if (warp == 8) {
-                // ---- TMA producer: lane l holds the page of tile l of the current run of 32
-                int phys = 0;
+            if (warp == T_SOFT) {
+                // ---- TMA producer: lane l holds page l of the current run of 32
+                int page = 0, phys = 0;
                 for (int i = 0; i < ntile; ++i) {
-                    if ((i & 31) == 0) phys = i + lane < ntile ? paged_physical(pb, pv, it.r, it.p0 + i + lane) : -1;
-                    const int page = __shfl_sync(0xffffffffu, phys, i & 31);
-                    const unsigned c = ct + i, s = c % S::STAGES;
+                    if ((i & 15) == 0) {
+                        const int e = 2 * i + lane;
+                        page = e < npage ? (PICK ? (int)s_list[e] : it.p0 + e) : -1;
+                        phys = e < npage ? paged_physical(pb, pv, it.r, page) : -1;
+                    }
+                    const int src = (2 * i) & 31;
+                    const int pg0 = __shfl_sync(0xffffffffu, page, src), pg1 = __shfl_sync(0xffffffffu, page, src + 1);
+                    const int ph0 = __shfl_sync(0xffffffffu, phys, src), ph1 = __shfl_sync(0xffffffffu, phys, src + 1);
+                    const unsigned c = ct + i, s = c % T_STAGES;
                     int ok = 1;
                     if (lane == 0) {
-                        if (c >= S::STAGES) ok = a_bar_wait(empty0 + 8 * s, ((c / S::STAGES) - 1) & 1) ? 1 : 0;
+                        const bool two = 2 * i + 1 < npage;
+                        if (c >= T_STAGES) ok = a_bar_wait(k_empty + 8 * s, ((c / T_STAGES) - 1) & 1) ? 1 : 0;
                         if (ok) {
-                            // a page that does not exist: the copy reads page 0 and every row masks the tile
-                            s_e0[c % T_E0] = page < 0 ? INT_MAX / 2 : (it.p0 + i) * PAGE;
-                            const uint32_t dst = base + s * S::STAGE;
-                            const int krow = (max(page, 0) * pv.H + it.h) * PAGE;
-                            a_bar_expect_tx(full0 + 8 * s, S::STAGE);
-                            a_tma_3d(dst, &map_k, 0, krow, 0, full0 + 8 * s);
-                            a_tma_3d(dst + S::PLANES * T_PLANE, &map_v, 0, krow, 0, full0 + 8 * s);
+                            // a page that does not exist: the copy reads page 0 and every row masks the page
+                            s_e0[c % T_E0 * 2] = ph0 < 0 ? T_NO_PAGE : pg0 * PAGE;
+                            s_e0[c % T_E0 * 2 + 1] = !two ? -1 : ph1 < 0 ? T_NO_PAGE : pg1 * PAGE;
+                            const int row0 = (max(ph0, 0) * pv.H + it.h) * PAGE, row1 = (max(ph1, 0) * pv.H + it.h) * PAGE;
+                            const uint32_t kd = base + s * S::TILE, vd = base + S::OFF_V + s * S::TILE;
+                            a_bar_expect_tx(k_full + 8 * s, two ? S::TILE : S::TILE / 2);
+#pragma unroll
+                            for (int p = 0; p < S::PLANES; ++p) {
+                                a_tma_3d(kd + p * S::KPLANE, &map_k, 0, row0, p, k_full + 8 * s);
+                                if (two) a_tma_3d(kd + p * S::KPLANE + T_PLANE, &map_k, 0, row1, p, k_full + 8 * s);
+                            }
+                            if (c >= T_STAGES) ok = a_bar_wait(v_empty + 8 * s, ((c / T_STAGES) - 1) & 1) ? 1 : 0;
+                            if (ok) {
+                                a_bar_expect_tx(v_full + 8 * s, two ? S::TILE : S::TILE / 2);
+                                a_tma_3d(vd, &map_v, 0, row0, 0, v_full + 8 * s);
+                                if (two) a_tma_3d(vd + S::PLANES * T_PLANE, &map_v, 0, row1, 0, v_full + 8 * s);
+                            }
                         }
                     }
                     if (__shfl_sync(0xffffffffu, ok, 0) == 0) {
                         if (lane == 0) *s_fail = 1;
-                        // the copies already issued land before the block leaves (bounded)
-                        for (unsigned k = c >= S::STAGES ? c - S::STAGES : 0; k < c; ++k) a_bar_wait(full0 + 8 * (k % S::STAGES), (k / S::STAGES) & 1);
+                        // the copies already issued land before the block leaves (bounded); K of this tile may be among them
+                        for (unsigned k = c >= T_STAGES ? c - T_STAGES : 0; k <= c; ++k) {
+                            a_bar_wait(k_full + 8 * (k % T_STAGES), (k / T_STAGES) & 1);
+                            if (k < c) a_bar_wait(v_full + 8 * (k % T_STAGES), (k / T_STAGES) & 1);
+                        }
                         break;
                     }
                 }
-            } else if (warp >= 9) {
-                const int gq = warp - 9;
+            } else if (warp > T_SOFT) {
+                // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue
+                // order), for one group after the other
                 bool ok = true;
-                if (gq == 1 && !both) {
-                    // ---- no rows in this group: its share of freeing the stages
-                    for (int i = 0; i < ntile && ok; ++i) {
-                        const unsigned c = ct + i, s = c % S::STAGES;
-                        ok = a_bar_wait(full0 + 8 * s, (c / S::STAGES) & 1);
-                        if (ok && lane == 0) a_bar_arrive(empty0 + 8 * s);
+                const uint32_t leader = t_elect();
+                const uint32_t ub = t_uniform(base), ut = t_uniform(tmem), uct = t_uniform(ct), uct1 = t_uniform(ct1);
+                const int un = (int)t_uniform((uint32_t)ntile), upages = (int)t_uniform((uint32_t)npage), uboth = (int)t_uniform(both ? 1u : 0u);
+                auto issue_s = [&](int i, int gq) {
+                    const uint32_t c = uct + i, s = c % T_STAGES;
+                    ok = __all_sync(0xffffffffu, a_bar_wait(k_full + 8 * s, (c / T_STAGES) & 1));
+                    if (!ok) return;
+                    a_fence_after();
+                    const uint32_t k_lo = t_desc_lo(ub, 16) + s * (S::TILE >> 4), q_lo = t_desc_lo(ub + S::OFF_Q, 16) + gq * (S::PLANES * T_QPLANE >> 4);
+                    const uint32_t idesc = 2 * i + 1 < upages ? S::IDESC_S2 : S::IDESC_S1;
+#pragma unroll
+                    for (int p = 0; p < S::PLANES; ++p)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)                   // 16 channels per instruction, 32 bytes along the row
+                            t_umma(leader, ut + 128 * gq, q_lo + (p * T_QPLANE + j * 32) / 16, k_lo + (p * S::KPLANE + j * 32) / 16, idesc, (p | j) != 0);
+                    t_commit(leader, bars + 64 + 8 * gq);             // S ready (and everything issued before: O up to the last tile)
+                    if (gq == 1 || !uboth) t_commit(leader, k_empty + 8 * s);
+                };
+                auto wait_v = [&](int i) {                            // V of the tile; what lies behind the last entry becomes zero
+                    const uint32_t c = uct + i, s = c % T_STAGES;
+                    ok = __all_sync(0xffffffffu, a_bar_wait(v_full + 8 * s, (c / T_STAGES) & 1));
+                    if (!ok) return;
+                    for (int h = 0; h < 2 && 2 * i + h < upages; ++h) {      // (held <= 0 for a page that does not exist: all of its V)
+                        const int held = it.q.len - s_e0[c % T_E0 * 2 + h];
+                        if (held >= PAGE) continue;
+                        unsigned char* vg = gen + S::OFF_V + s * S::TILE + h * S::PLANES * T_PLANE;
+                        for (int e = max(held, 0) * 8 + lane; e < PAGE * 8; e += 32)
+#pragma unroll
+                            for (int p = 0; p < S::PLANES; ++p) *reinterpret_cast<uint4*>(vg + p * T_PLANE + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                } else {
-                    // ---- MMA issuer of group gq: S of tiles i + 1 and i + 2 are issued before P V of tile i
-                    const uint32_t d_s0 = tmem + 128 * gq, d_o = tmem + 256 + 128 * gq;
-                    const uint32_t qb = base + S::OFF_Q + gq * S::PLANES * T_QPLANE;
-                    const unsigned gt = gq ? ct1 : ct;
-                    auto issue_s = [&](int i) {                       // S = Q K^T of tile i into buffer (gt + i) & 1
-                        const unsigned c = ct + i, s = c % S::STAGES, b = (gt + i) & 1;
-                        ok = __all_sync(0xffffffffu, a_bar_wait(full0 + 8 * s, (c / S::STAGES) & 1));
-                        if (!ok) return;
-                        a_fence_after();
-                        if (lane == 0) {
-                            const uint32_t st = base + s * S::STAGE, d_s = d_s0 + 64 * b;
+                };
+                auto issue_pv = [&](int i, int gq) {
+                    const uint32_t c = uct + i, s = c % T_STAGES;
+                    ok = __all_sync(0xffffffffu, a_bar_wait(p_ready0 + 8 * gq, ((gq ? uct1 : uct) + i) & 1));
+                    if (!ok) return;
+                    a_fence_after();
+                    const uint32_t v_lo = t_desc_lo(ub + S::OFF_V, T_PLANE) + s * (S::TILE >> 4);     // the next 64 channels: one plane further
+                    const uint32_t d_o = ut + 256 + 128 * gq, a_p = ut + 128 * gq;
 #pragma unroll
-                            for (int p = 0; p < S::PLANES; ++p) {
-                                const uint64_t qd = a_desc(qb + p * T_QPLANE, 16), kd = a_desc(st + p * T_PLANE, 16);
+                    for (int j = 0; j < PAGE / 16; ++j)               // 16 entries per instruction: P +8 columns, V +2 row groups
+                        t_umma_ts(leader, d_o, a_p + j * 8, v_lo + j * 128, S::IDESC_PV, i != 0 || j != 0);
+                    if (2 * i + 1 < upages) {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)           // 16 channels per instruction, 32 bytes along the row
-                                    a_umma(d_s, qd + (uint64_t)(j * 32 >> 4), kd + (uint64_t)(j * 32 >> 4), S::IDESC_S, (p | j) != 0);
-                            }
-                            a_commit(s_ready0 + 16 * gq + 8 * b);
-                        }
-                        __syncwarp();
-                    };
-                    auto issue_pv = [&](int i) {                      // O += P V of tile i
-                        const unsigned c = ct + i, s = c % S::STAGES, b = (gt + i) & 1;
-                        const uint32_t st = base + s * S::STAGE, a_p = d_s0 + 64 * b;
-                        const int held = it.q.len - s_e0[c % T_E0];   // (<= 0 for a page that does not exist: all of its V is zeroed)
-                        if (held < PAGE) {
-                            unsigned char* vg = gen + s * S::STAGE + S::PLANES * T_PLANE;
-                            for (int e = max(held, 0) * 8 + lane; e < PAGE * 8; e += 32)
-#pragma unroll
-                                for (int p = 0; p < S::PLANES; ++p) *reinterpret_cast<uint4*>(vg + p * T_PLANE + e * 16) = make_uint4(0u, 0u, 0u, 0u);
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        }
-                        ok = __all_sync(0xffffffffu, a_bar_wait(p_ready0 + 8 * gq, b));
-                        if (!ok) return;
-                        a_fence_after();
-                        if (lane == 0) {
-                            const uint64_t vd = a_desc(st + S::PLANES * T_PLANE, T_PLANE);    // the next 64 channels: one plane further
-#pragma unroll
-                            for (int j = 0; j < PAGE / 16; ++j)       // 16 entries per instruction: P +8 columns, V +2 row groups
-                                a_umma_ts(d_o, a_p + j * 8, vd + (uint64_t)(j * 2048 >> 4), S::IDESC_PV, (i | j) != 0);
-                            a_commit(pv_done0 + 8 * gq);
-                            a_commit(empty0 + 8 * s);                 // this group is done with the stage
-                        }
-                        __syncwarp();
-                    };
-                    issue_s(0);
-                    if (ok && ntile > 1) issue_s(1);
-                    for (int i = 0; i < ntile && ok; ++i) {
-                        issue_pv(i);
-                        if (ok && i + 2 < ntile) issue_s(i + 2);
+                        for (int j = 0; j < PAGE / 16; ++j)
+                            t_umma_ts(leader, d_o, a_p + 64 + j * 8, v_lo + S::PLANES * T_PLANE / 16 + j * 128, S::IDESC_PV, 1u);
                     }
+                    if (gq == 1 || !uboth) t_commit(leader, v_empty + 8 * s);
+                    if (i + 1 == un) t_commit(leader, done0 + 8 * gq);
+                };
+                issue_s(0, 0);
+                if (ok && uboth) issue_s(0, 1);
+                for (int i = 0; i < un && ok; ++i) {
+                    wait_v(i);
+                    if (ok) issue_pv(i, 0);
+                    if (ok && i + 1 < un) issue_s(i + 1, 0);
+                    if (ok && uboth) issue_pv(i, 1);
+                    if (ok && uboth && i + 1 < un) issue_s(i + 1, 1);
                 }
                 if (!ok && lane == 0) *s_fail = 1;
             }
         }
-        if (warp < 8 && (grp == 0 || both)) {
-            // ---- softmax warps
+        if (soft) {
+            // ---- softmax warps: page `half` of every tile
             const uint32_t lane_addr = tmem + ((uint32_t)(wl * 32) << 16);
-            const uint32_t s_col0 = (uint32_t)(128 * grp), o_col = (uint32_t)(256 + 128 * grp);
+            const uint32_t s_addr = lane_addr + (uint32_t)(128 * grp + 64 * half), o_addr = lane_addr + (uint32_t)(256 + 128 * grp + half * (D / 2));
+            const uint32_t pair = pair0 + 8 * (grp * 4 + wl);         // barrier of the two warps of these rows
+            float* mx_mine = s_mx + (grp * 2 + half) * T_ROWS + r;
+            const float* mx_other = s_mx + (grp * 2 + (half ^ 1)) * T_ROWS + r;
+            const unsigned gt = grp ? ct1 : ct;
             float m_used = -INFINITY, l = 0.f;
             bool ok = true;
-            const unsigned gt = grp ? ct1 : ct;
             for (int i = 0; i < ntile; ++i) {
-                const unsigned c = gt + i;                            // of the group's tiles
-                ok = __all_sync(0xffffffffu, a_bar_wait(s_ready0 + 16 * grp + 8 * (c & 1), (c >> 1) & 1));
+                ok = __all_sync(0xffffffffu, a_bar_wait(s_ready0 + 8 * grp, (gt + i) & 1));
                 if (!ok) break;
-                const uint32_t s_col = s_col0 + 64u * (c & 1u);
                 a_fence_after();
-                uint32_t sv[64];
-                a_tmem_ld32(lane_addr + s_col, sv);
-                a_tmem_ld32(lane_addr + s_col + 32, sv + 32);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                const int e0 = s_e0[(ct + i) % T_E0];
-                if (e0 + PAGE > see_hi || e0 < see_lo) {              // the tile crosses the row's limits
-#pragma unroll
-                    for (int e = 0; e < 64; ++e)
-                        if (e0 + e >= see_hi || e0 + e < see_lo) sv[e] = 0xff800000u;        // -inf
+                const int e0 = s_e0[(ct + i) % T_E0 * 2 + half];      // -1: the tile is one page
+                int hi = see_hi;
+                if (PICK) {
+                    const int page = e0 / PAGE;
+                    const bool on = valid && e0 >= 0 && e0 < T_NO_PAGE && ((s_bits[(tok - it.tok0) * nw + (page >> 5) - w0] >> (page & 31)) & 1u);
+                    if (!on) hi = 0;
                 }
-                float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                const bool some = __any_sync(0xffffffffu, e0 >= 0 && e0 < hi && e0 + PAGE > see_lo);      // rows of the warp that see the page
+                const bool edge = e0 + PAGE > hi || e0 < see_lo;
+                uint32_t sv[32];
+                auto load = [&](int k) {                              // entries 32 k .. of the page, masked
+                    a_tmem_ld32(s_addr + 32 * k, sv);
+                    t_tmem_wait_ld();
+                    if (edge) {
 #pragma unroll
-                for (int e = 0; e < 64; e += 8) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mq[k] = a_max3(mq[k], __uint_as_float(sv[e + 2 * k]), __uint_as_float(sv[e + 2 * k + 1]));
-                }
-                const float mx = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
-                const float m_new = mx * scale_log2;                  // scale_log2 > 0
-                const bool resc = __any_sync(0xffffffffu, m_new > m_used + T_RESCALE_STEP);
-                float alpha = 1.0f;
-                if (resc) {
-                    const float mn = fmaxf(m_used, m_new);
-                    alpha = (m_used == -INFINITY) ? 0.0f : exp2f(m_used - mn);
-                    m_used = mn;
-                }
-                const float mref = (m_used == -INFINITY) ? 0.0f : m_used;
-                const uint64_t sc2 = a_pack2(scale_log2, scale_log2), nm2 = a_pack2(-mref, -mref);
-                uint64_t sq[4] = {0ull, 0ull, 0ull, 0ull};
-                uint32_t pk[32];
-#pragma unroll
-                for (int e = 0; e < 64; e += 2) {
-                    const uint64_t x2 = a_fma2(a_pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), sc2, nm2);
-                    float p0, p1;
-                    if ((e >> 1) % T_POLY_EVERY == T_POLY_EVERY - 1) {
-                        a_exp2_fma2(x2, p0, p1);
-                    } else {
-                        float x0, x1;
-                        a_unpack2(x2, x0, x1);
-                        p0 = a_ex2(x0);
-                        p1 = a_ex2(x1);
+                        for (int e = 0; e < 32; ++e)
+                            if (e0 + 32 * k + e >= hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
                     }
-                    sq[(e >> 1) & 3] = a_add2(sq[(e >> 1) & 3], a_pack2(p0, p1));
-                    pk[e >> 1] = a_bf16x2(p0, p1);
+                };
+                float mx = -INFINITY;
+                if (some) {
+                    float mq[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        load(k);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                            mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                        }
+                    }
+                    mx = fmaxf(mq[0], mq[1]);
                 }
-                float a0, a1;
-                a_unpack2(a_add2(a_add2(sq[0], sq[1]), a_add2(sq[2], sq[3])), a0, a1);
-                l = l * alpha + (a0 + a1);
-                if (i > 0) {                                          // O complete up to the previous tile
-                    ok = __all_sync(0xffffffffu, a_bar_wait(pv_done0 + 8 * grp, (c - 1) & 1));
-                    if (!ok) break;
-                    a_fence_after();
-                    if (resc) {
+                mx_mine[(ex & 1) * 4 * T_ROWS] = mx;
+                ok = t_pair_sync(pair, ex);
+                if (!ok) break;
+                const float m_new = fmaxf(mx, mx_other[(ex & 1) * 4 * T_ROWS]) * scale_log2;      // scale_log2 > 0
+                ++ex;
+                if (__any_sync(0xffffffffu, m_new > m_used + T_RESCALE_STEP)) {                   // the same for both warps of the rows
+                    const float mn = fmaxf(m_used, m_new);
+                    const float alpha = (m_used == -INFINITY) ? 0.0f : exp2f(m_used - mn);
+                    m_used = mn;
+                    l *= alpha;
+                    if (i > 0) {                                      // (O is complete up to the previous tile: see the commit of S)
 #pragma unroll
                         for (int k = 0; k < D / 32; ++k) {
-                            uint32_t ov[32];
-                            a_tmem_ld32(lane_addr + o_col + k * 32, ov);
-                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                            uint32_t ov[16];
+                            t_tmem_ld16(o_addr + k * 16, ov);
+                            t_tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-                            a_tmem_st32(lane_addr + o_col + k * 32, ov);
+                            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                            t_tmem_st16(o_addr + k * 16, ov);
                         }
-                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                     }
                 }
-                a_tmem_st32(lane_addr + s_col, pk);
-                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                if (some) {
+                    const float mref = (m_used == -INFINITY) ? 0.0f : m_used;
+                    const uint64_t sc2 = a_pack2(scale_log2, scale_log2), nm2 = a_pack2(-mref, -mref);
+                    uint64_t sq[2] = {0ull, 0ull};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        load(k);
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const uint64_t x2 = a_fma2(a_pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), sc2, nm2);
+                            float p0, p1;
+                            if ((e >> 1) % T_POLY_EVERY == T_POLY_EVERY - 1) {
+                                a_exp2_fma2(x2, p0, p1);
+                            } else {
+                                float x0, x1;
+                                a_unpack2(x2, x0, x1);
+                                p0 = a_ex2(x0);
+                                p1 = a_ex2(x1);
+                            }
+                            sq[(e >> 1) & 1] = a_add2(sq[(e >> 1) & 1], a_pack2(p0, p1));
+                            pk[e >> 1] = a_bf16x2(p0, p1);
+                        }
+                        t_tmem_st16(s_addr + 16 * k, pk);             // P: two entries per column, over the page's first 32 columns of S
+                    }
+                    float a0, a1;
+                    a_unpack2(a_add2(sq[0], sq[1]), a0, a1);
+                    l += a0 + a1;
+                } else if (e0 >= 0) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) pk[e] = 0u;
+                    t_tmem_st16(s_addr, pk);
+                    t_tmem_st16(s_addr + 16, pk);
+                }
+                t_tmem_wait_st();
                 a_fence_before();
                 __syncwarp();
                 if (lane == 0) a_bar_arrive(p_ready0 + 8 * grp);
             }
-            if (ok && ntile > 0) ok = __all_sync(0xffffffffu, a_bar_wait(pv_done0 + 8 * grp, (gt + ntile - 1) & 1));
+            if (ok && ntile > 0) ok = __all_sync(0xffffffffu, a_bar_wait(done0 + 8 * grp, (grp ? st1 : st0) & 1));
+            // the halves' sums, through the buffer that the next tile's maxima would use (its last readers are two exchanges back)
+            mx_mine[(ex & 1) * 4 * T_ROWS] = l;
+            if (ok) ok = t_pair_sync(pair, ex);
             if (!ok) {
                 if (lane == 0) *s_fail = 1;
             } else {
                 a_fence_after();
+                l += mx_other[(ex & 1) * 4 * T_ROWS];
+                ++ex;
                 if (m_used == -INFINITY && !(l != l)) l = 0.f;        // a row that sees nothing (the polynomial gives masked entries 2^-125)
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-                uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * D);
+                uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * D + half * (D / 2));
                 const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
-                float4* po = reinterpret_cast<float4*>(wk.part_o + pr * D);
+                float4* po = reinterpret_cast<float4*>(wk.part_o + pr * D + half * (D / 2));
                 const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
-                    uint32_t ov[32];
+                    uint32_t ov[16];
                     if (ntile > 0) {
-                        a_tmem_ld32(lane_addr + o_col + k * 32, ov);
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        t_tmem_ld16(o_addr + k * 16, ov);
+                        t_tmem_wait_ld();
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) ov[e] = zero ? 0u : ov[e];
+                    for (int e = 0; e < 16; ++e) ov[e] = zero ? 0u : ov[e];
                     if (!valid) continue;
                     if (it.slot < 0) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
+                        for (int e = 0; e < 16; e += 8) {
                             uint32_t v[4];
 #pragma unroll
                             for (int k2 = 0; k2 < 4; ++k2)
                                 v[k2] = a_bf16x2(__uint_as_float(ov[e + 2 * k2]) * inv, __uint_as_float(ov[e + 2 * k2 + 1]) * inv);
-                            op[k * 4 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
+                            op[k * 2 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            po[k * 8 + (e >> 2)] = make_float4(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1]), __uint_as_float(ov[e + 2]), __uint_as_float(ov[e + 3]));
+                        for (int e = 0; e < 16; e += 4)
+                            po[k * 4 + (e >> 2)] = make_float4(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1]), __uint_as_float(ov[e + 2]), __uint_as_float(ov[e + 3]));
                     }
                 }
-                if (valid && it.slot >= 0) {
+                if (valid && it.slot >= 0 && half == 0) {
                     wk.part_ml[pr * 2] = m_used;
                     wk.part_ml[pr * 2 + 1] = l;
                 }
             }
         }
         ct += (unsigned)ntile;
-        if (both) ct1 += (unsigned)ntile;
+        st0 += ntile > 0;
+        if (both) { ct1 += (unsigned)ntile; st1 += ntile > 0; }
         a_fence_before();
-        __syncthreads();                                              // Q and tensor memory are free for the next stretch
+        __syncthreads();                                              // Q, the lists and tensor memory are free for the next stretch
         a_fence_after();
         if (*s_fail) break;
     }
     __syncthreads();
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");
+    if (warp == T_SOFT + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");
     if (threadIdx.x == 0 && *s_fail) latch_error(pb.status, TRIMKV_E_TIMEOUT);
 }
 
-template <int D>
+template <int D, bool PICK>
 cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int min_rows, cudaStream_t st) {
-    using S = TcShape<D>;
+    using S = TcShape<D, PICK>;
+    static_assert(S::SMEM <= 227 * 1024, "shared memory of one SM");
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_tc_kernel<D>), S::SMEM, done);
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_tc_kernel<D, PICK>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    e = paged_tensor_map(&mk, pv.k, pv, PAGE);
-    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, PAGE);
+    e = paged_tensor_map(&mk, pv.k, pv, PAGE, 1);                     // K plane by plane: a tile's plane holds the rows of two pages
+    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, PAGE, pv.d / 64);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged_attn_tc_kernel<D>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, st, mk, mv, pv, pb, (const __nv_bfloat16*)q, (__nv_bfloat16*)out,
-                     scale * LOG2E, w, min_rows);
+    e = paged_launch(paged_attn_tc_kernel<D, PICK>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
+                     (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, true, st);
 }
 
@@ -372,7 +552,8 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
 
 cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                       int min_rows, cudaStream_t st) {
-    return pv.d == 64 ? run_tc<64>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<128>(pv, pb, q, out, scale, w, min_rows, st);
+    if (pb.pick > 0) return pv.d == 64 ? run_tc<64, true>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<128, true>(pv, pb, q, out, scale, w, min_rows, st);
+    return pv.d == 64 ? run_tc<64, false>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<128, false>(pv, pb, q, out, scale, w, min_rows, st);
 }
 
 }  // namespace tkv

@@ -338,10 +338,10 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    e = paged_tensor_map(&mk, pv.k, pv, S::TILE);
-    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, S::TILE);
+    e = paged_tensor_map(&mk, pv.k, pv, S::TILE, S::PLANES);
+    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, S::TILE, S::PLANES);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, st, mk, mv, pv, pb,
+    e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
                      (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, false, st);
 }
@@ -349,13 +349,13 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
 }  // namespace
 
 // The pages as n_pages x H x 64 rows of d bf16, their columns cut into planes of 64: dimensions {64, rows, d / 64}; a box is
-// box_rows rows of every plane, each plane 128-byte swizzled, plane after plane.
-cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows) {
+// box_rows rows of box_planes planes, each plane 128-byte swizzled, plane after plane.
+cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows, int box_planes) {
     EncodeTiledFnA fn = a_encode_fn();
     if (!fn) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {64, (cuuint64_t)pv.n_pages * pv.H * PAGE, (cuuint64_t)pv.d / 64};
     const cuuint64_t strides[2] = {(cuuint64_t)pv.d * 2, 128};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)pv.d / 64};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_planes};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS

@@ -340,7 +340,7 @@ cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* kee
     const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_plan_kernel),
                                            (int)(((size_t)6 * PAGED_MAX_REQ + 3) * sizeof(int)), done);
     if (e != cudaSuccess) return e;
-    return paged_launch(paged_plan_kernel, dim3(PLAN_CTAS), dim3(PLAN_THREADS), smem, PLAN_CTAS, st, R, old_lens, keep_lens, new_lens, table, W, free_pages,
+    return paged_launch(paged_plan_kernel, dim3(PLAN_CTAS), dim3(PLAN_THREADS), smem, PLAN_CTAS, true, st, R, old_lens, keep_lens, new_lens, table, W, free_pages,
                         n_pages, free_count, free_count_out, max_tokens, lens_out, cu_new, slot_map, positions, status);
 }
 
@@ -358,7 +358,7 @@ cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_page
     const long long items = bounds ? (long long)((T + group - 1) / group) * pv.H : 0;
     const unsigned blocks = (unsigned)(copy_blocks + items);
     auto go = [&](auto kernel) {
-        return paged_launch(kernel, dim3(blocks), dim3(APP_THREADS), 0, 1, st, k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k, k_stride,
+        return paged_launch(kernel, dim3(blocks), dim3(APP_THREADS), 0, 1, true, st, k_pages, v_pages, bounds, pv.n_pages, pv.H, pv.d, T, (const char*)k, k_stride,
                             (const char*)v, v_stride, slot_map, status, (int)copy_blocks, group);
     };
     return is_bf16 ? go(paged_append_kernel<__nv_bfloat16>) : go(paged_append_kernel<float>);
