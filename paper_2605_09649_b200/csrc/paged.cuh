@@ -55,7 +55,7 @@ struct PagedBatch {
 
 constexpr int PAGED_MAX_REQ = 8192;
 constexpr int PAGED_PICK_ROWS = 64;           // see PagedBatch::pick
-constexpr int PAGED_PICK_WORDS = 3968;        // shared memory of the union: bits (tokens of a unit x pages / 32)
+constexpr int PAGED_PICK_WORDS = 3456;        // shared memory of the union: bits (tokens of a unit x pages / 32)
 constexpr int PAGED_PICK_PAGES = 1024;        // ... and its list of pages
 
 // Rows and length of request r; a request whose offsets or length are out of range counts as having no rows.

@@ -246,49 +246,64 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     const int workers = (int)wk.prefix[pb.R + 1];
     const int unit_rows = pb.top > 0 ? g : tile_rows;
     int u_now = -1, w0 = 0, n = 0;
-    for (int jj = SPLIT > 1 ? rest % g : 0; jj < g; ++jj) {
-        const int row = j * g + jj, u = pb.top > 0 ? j : row / tile_rows, rr = row - u * unit_rows;
-        if (u != u_now) {
-            const long long a = before + (long long)(h * c.U + paged_unfold(u, c.U)) * c.C;
-            w0 = paged_owner(total, workers, a);
-            n = paged_owner(total, workers, a + c.C - 1) - w0 + 1;
-            u_now = u;
-        }
-        if (SPLIT == 1 && n > 1 && n <= 4) {                      // few parts: every load of the row in flight at once
-            float m[4], l[4];
-            float4 v[4][2];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m[i] = -INFINITY; l[i] = 0.f;
-                v[i][0] = v[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i < n) {
-                    const size_t pr = (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr;
-                    const float2 ml = *reinterpret_cast<const float2*>(wk.part_ml + pr * 2);
-                    m[i] = ml.x; l[i] = ml.y;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        if (lane * 4 + x * 128 < d) v[i][x] = *reinterpret_cast<const float4*>(wk.part_o + pr * d + lane * 4 + x * 128);
-                }
-            }
-            const float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = M == -INFINITY ? 0.f : M;
-            float e[4], L = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { e[i] = exp2f(m[i] - ref); L = fmaf(e[i], l[i], L); }
-            const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-            T* o = out + ((size_t)t * pb.Hq + (size_t)h * g + jj) * d + lane * 4;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (lane * 4 + x * 128 >= d) continue;
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto locate = [&](int u) {                                    // the unit's first worker and number of parts
+        if (u == u_now) return;
+        const long long a = before + (long long)(h * c.U + paged_unfold(u, c.U)) * c.C;
+        w0 = paged_owner(total, workers, a);
+        n = paged_owner(total, workers, a + c.C - 1) - w0 + 1;
+        u_now = u;
+    };
+    if (SPLIT == 1 && pb.top == 0 && (j * g) / tile_rows == (j * g + g - 1) / tile_rows) {
+        // the rows of one unit, in few parts: half a warp per row and every load of the row in flight at once
+        locate(j * g / tile_rows);
+        if (n == 1) return;
+        if (n <= 4) {
+            const int l16 = lane & 15;
+            for (int j0 = 0; j0 < g; j0 += 2) {
+                const int jj = j0 + (lane >> 4);
+                const bool on = jj < g;
+                const int rr = j * g + jj - u_now * tile_rows;
+                float m[4], l[4];
+                float4 v[4][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sum.x = fmaf(e[i], v[i][x].x, sum.x); sum.y = fmaf(e[i], v[i][x].y, sum.y);
-                    sum.z = fmaf(e[i], v[i][x].z, sum.z); sum.w = fmaf(e[i], v[i][x].w, sum.w);
+                    m[i] = -INFINITY; l[i] = 0.f;
+                    if (on && i < n) {
+                        const size_t pr = (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr;
+                        const float2 ml = *reinterpret_cast<const float2*>(wk.part_ml + pr * 2);
+                        m[i] = ml.x; l[i] = ml.y;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (l16 * 4 + x * 64 < d) v[i][x] = *reinterpret_cast<const float4*>(wk.part_o + pr * d + l16 * 4 + x * 64);
+                    }
                 }
-                o[x * 128] = from_f32<T>(sum.x * inv); o[x * 128 + 1] = from_f32<T>(sum.y * inv);
-                o[x * 128 + 2] = from_f32<T>(sum.z * inv); o[x * 128 + 3] = from_f32<T>(sum.w * inv);
+                const float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = M == -INFINITY ? 0.f : M;
+                float e[4], L = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { e[i] = exp2f(m[i] - ref); L = fmaf(e[i], l[i], L); }
+                const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+                T* o = out + ((size_t)t * pb.Hq + (size_t)h * g + jj) * d + l16 * 4;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    if (!on || l16 * 4 + x * 64 >= d) continue;
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < n) {
+                            sum.x = fmaf(e[i], v[i][x].x, sum.x); sum.y = fmaf(e[i], v[i][x].y, sum.y);
+                            sum.z = fmaf(e[i], v[i][x].z, sum.z); sum.w = fmaf(e[i], v[i][x].w, sum.w);
+                        }
+                    o[x * 64] = from_f32<T>(sum.x * inv); o[x * 64 + 1] = from_f32<T>(sum.y * inv);
+                    o[x * 64 + 2] = from_f32<T>(sum.z * inv); o[x * 64 + 3] = from_f32<T>(sum.w * inv);
+                }
             }
-        } else if (n > 1) {
+            return;
+        }
+    }
+    for (int jj = SPLIT > 1 ? rest % g : 0; jj < g; ++jj) {
+        const int row = j * g + jj, u = pb.top > 0 ? j : row / tile_rows, rr = row - u * unit_rows;
+        locate(u);
+        if (n > 1) {
             // i-th part: worker w0 began the unit and did not end it (its slot 2 w + 1), the others did not begin it
             auto slot_row = [&](int i) { return (size_t)(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * unit_rows + rr; };
             float M = -INFINITY, L = 0.f;

@@ -3,15 +3,20 @@
 // A unit is 256 (token, query head) rows of one KV head in two groups of 128 that share every K/V tile; a tile is two pages
 // (128 entries; the last of a stretch may be one).  One persistent CTA per SM takes an equal share of the line of page steps
 // (paged.cuh) and meets a stretch of a unit at a time.  TMA copies K and V as 64-column planes with the 128-byte swizzle:
-// K planes (both pages' rows) are K-major operands of S = Q K^T, V planes MN-major operands of O += P V.  Warps 0-7 / 8-15
-// are the softmax warps of group 0 / 1, two threads per row with a page of the tile each (S from tensor memory, masked,
-// exponentiated, P back over it as the A operand of P V; the two exchange their maxima through shared memory and a barrier of
-// their warps), warp 16 issues the copies, warp 17 the products, group 0's and group 1's in turn: the pipe runs P V and the next S
-// of one group while the other group's softmax works on its S.  (With an issuer per group the pipe served both at once, and the
-// groups fell into step: products, then softmax, 5800 cycles a tile.)  The maximum is only raised (and O rescaled) when it
-// grows by more than 2^8.  A third of the exponentials are evaluated on the FMA pipe.  A unit of 128 rows or fewer leaves group
-// 1 idle.  V rows behind a request's last entry are zeroed in shared memory before the product reads them (they may hold
-// NaN).  Every wait is bounded; one that runs out latches TRIMKV_E_TIMEOUT.
+// K planes (both pages' rows) are K-major operands of S = Q K^T, V planes MN-major operands of O += P V.  Warps 0-7 / 8-15 are
+// the softmax warps of group 0 / 1, two threads per row with a page of the tile each (S from tensor memory, masked,
+// exponentiated, P back over it as the A operand of P V), warp 16 issues the copies, warp 17 the products, group 0's and group
+// 1's in turn: the pipe runs P V and the next S of one group while the other group's softmax works on its S.  (With an issuer
+// per group the pipe served both at once, and the groups fell into step: products, then softmax, 5800 cycles a tile.)
+//
+// The reference m of a row's weights lags: a tile is weighed against the maximum known from the tiles before it, which the two
+// threads of a row exchange through shared memory without a barrier of their own (the hand-over of the tile orders it), and
+// m is raised, and O rescaled, when that maximum exceeds it by more than 2^8.  Only the first tile that a row sees finds its
+// maximum beforehand.  Weights above 2^64, a row whose logits leap by that much within one stretch, send the whole stretch
+// round again with the maximum found first in every tile.  A third of the
+// exponentials are evaluated on the FMA pipe.  A unit of 128 rows or fewer leaves group 1 idle.  V rows behind a request's last
+// entry are zeroed in shared memory before the product reads them (they may hold NaN).  Every wait is bounded; one that runs
+// out latches TRIMKV_E_TIMEOUT.
 //
 // Why 128 entries: an S of 64 columns reads 6 KB of operands from shared memory for 32 cycles of products, more than the
 // 128 bytes a cycle it delivers, and doubles the hand-overs between the pipes per entry (measured with 64: 610 us for 4 x 512
@@ -35,7 +40,7 @@ constexpr int T_SOFT = 16;                                            // softmax
 constexpr int T_THREADS = (T_SOFT + 2) * 32;
 constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
-constexpr float T_RESCALE_STEP = 8.0f;
+constexpr float T_RESCALE_STEP = 8.0f, T_LEAP = 64.0f;
 constexpr int T_STAGES = 2;           // tiles of K, and of V, in shared memory
 constexpr int T_E0 = 8;               // ring of the tiles' first entries (two pages each): more than the tiles in flight
 constexpr int T_NO_PAGE = INT_MAX / 2;
@@ -49,8 +54,8 @@ struct TcShape {
     static constexpr int OFF_Q = 2 * T_STAGES * TILE;
     static constexpr int OFF_BAR = OFF_Q + 2 * PLANES * T_QPLANE;
     static constexpr int OFF_E0 = OFF_BAR + 256;
-    static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [exchange parity][group][half][row] maxima; at the end: sums
-    static constexpr int OFF_TAB = OFF_MX + 2 * 2 * 2 * T_ROWS * 4;
+    static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [tile parity; 2: sums][group][page of the tile][row]: maxima so far
+    static constexpr int OFF_TAB = OFF_MX + 3 * 2 * 2 * T_ROWS * 4;
     static constexpr int OFF_BITS = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;
     static constexpr int OFF_LIST = OFF_BITS + (PICK ? PAGED_PICK_WORDS * 4 : 0);
     static constexpr int SMEM = OFF_LIST + (PICK ? PAGED_PICK_PAGES * 2 : 0) + 1024;      // 1024: alignment slack
@@ -135,6 +140,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                    p_ready0 = bars + 80, done0 = bars + 96 /* [group] each */, pair0 = bars + 112 /* [group][32 rows] */;
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(gen + S::OFF_BAR + 240);
     volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 244);
+    volatile int* s_redo = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 252);
     volatile int* s_nlist = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 248);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
     float* s_mx = reinterpret_cast<float*>(gen + S::OFF_MX);
@@ -155,6 +161,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         }
         for (int i = 0; i < 8; ++i) a_bar_init(pair0 + 8 * i, 2);
         *s_fail = 0;
+        *s_redo = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         a_prefetch_map(&map_k);
         a_prefetch_map(&map_v);
@@ -173,7 +180,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     __syncthreads();
     a_fence_after();
     const uint32_t tmem = *s_tmem;
-    // softmax warps: group, half of the tile's entries, 32 rows of the group (a warp reaches the tensor-memory lanes of its number mod 4)
+    // softmax warps: group, page of the tile, 32 rows of the group (a warp reaches the tensor-memory lanes of its number mod 4)
     const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
     const int r = wl * 32 + lane, R = grp * T_ROWS + r;               // row: lane of tensor memory, row of the unit
 
@@ -181,10 +188,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     // tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
     // stretches with tiles, of group 0 and 1
     unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
-    unsigned ex = 0;                                                  // exchanges between the halves of a row so far
+    unsigned ex = 0;                                                  // barriers of the two warps of a row so far
+    bool careful = false;                                             // this stretch again, every tile's maximum first
     for (long long x = tab.share(w); x < end;) {
         const PagedItem it = paged_item(tab, pb, x, end, w);
-        x += it.steps;
         int npage = it.p1 - it.p0;
         const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
         const bool both = rows > T_ROWS;
@@ -238,8 +245,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + tok) * pb.q_stride + (size_t)(it.h * g + head) * D);
                 unsigned char* qdst = gen + S::OFF_Q + grp * S::PLANES * T_QPLANE + r * 128;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const int c = half * (D / 16) + i;
+                for (int k = 0; k < D / 16; ++k) {
+                    const int c = half * (D / 16) + k;
                     const uint4 v = valid ? src[c] : make_uint4(0u, 0u, 0u, 0u);
                     *reinterpret_cast<uint4*>(qdst + (c >> 3) * T_QPLANE + (((c & 7) ^ (r & 7)) << 4)) = v;
                 }
@@ -335,11 +342,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 };
                 auto issue_pv = [&](int i, int gq) {
                     const uint32_t c = uct + i, s = c % T_STAGES;
+                    const uint32_t v_lo = t_desc_lo(ub + S::OFF_V, T_PLANE) + s * (S::TILE >> 4);     // the next 64 channels: one plane further
+                    const uint32_t d_o = ut + 256 + 128 * gq, a_p = ut + 128 * gq;
                     ok = __all_sync(0xffffffffu, a_bar_wait(p_ready0 + 8 * gq, ((gq ? uct1 : uct) + i) & 1));
                     if (!ok) return;
                     a_fence_after();
-                    const uint32_t v_lo = t_desc_lo(ub + S::OFF_V, T_PLANE) + s * (S::TILE >> 4);     // the next 64 channels: one plane further
-                    const uint32_t d_o = ut + 256 + 128 * gq, a_p = ut + 128 * gq;
 #pragma unroll
                     for (int j = 0; j < PAGE / 16; ++j)               // 16 entries per instruction: P +8 columns, V +2 row groups
                         t_umma_ts(leader, d_o, a_p + j * 8, v_lo + j * 128, S::IDESC_PV, i != 0 || j != 0);
@@ -367,25 +374,39 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             // ---- softmax warps: page `half` of every tile
             const uint32_t lane_addr = tmem + ((uint32_t)(wl * 32) << 16);
             const uint32_t s_addr = lane_addr + (uint32_t)(128 * grp + 64 * half), o_addr = lane_addr + (uint32_t)(256 + 128 * grp + half * (D / 2));
-            const uint32_t pair = pair0 + 8 * (grp * 4 + wl);         // barrier of the two warps of these rows
+            const uint32_t pair = pair0 + 8 * (grp * 4 + wl);
             float* mx_mine = s_mx + (grp * 2 + half) * T_ROWS + r;
             const float* mx_other = s_mx + (grp * 2 + (half ^ 1)) * T_ROWS + r;
+            constexpr int MX = 4 * T_ROWS;                            // from one buffer of maxima to the next
             const unsigned gt = grp ? ct1 : ct;
-            float m_used = -INFINITY, l = 0.f;
+            const uint64_t sc2 = a_pack2(scale_log2, scale_log2);
+            float m_used = -INFINITY, m_mine = -INFINITY, l = 0.f;    // the reference (the same in both threads), this thread's maximum, its sum
             bool ok = true;
+            // entries that every row of the warp sees (rows without a query see whatever the others do); once every row has a
+            // maximum, a tile of two pages in this span needs no look at the rows
+            const int all_hi = PICK ? 0 : __reduce_min_sync(0xffffffffu, valid ? see_hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, see_lo);
+            bool primed = false;
             for (int i = 0; i < ntile; ++i) {
                 ok = __all_sync(0xffffffffu, a_bar_wait(s_ready0 + 8 * grp, (gt + i) & 1));
                 if (!ok) break;
                 a_fence_after();
-                const int e0 = s_e0[(ct + i) % T_E0 * 2 + half];      // -1: the tile is one page
-                int hi = see_hi;
-                if (PICK) {
-                    const int page = e0 / PAGE;
-                    const bool on = valid && e0 >= 0 && e0 < T_NO_PAGE && ((s_bits[(tok - it.tok0) * nw + (page >> 5) - w0] >> (page & 31)) & 1u);
-                    if (!on) hi = 0;
+                // first entries of both pages (-1: the tile is one page); what the row sees of them
+                const int e0 = s_e0[(ct + i) % T_E0 * 2 + half], e1 = s_e0[(ct + i) % T_E0 * 2 + (half ^ 1)];
+                auto sees = [&](int e) {
+                    if (!(valid && e >= 0 && e < see_hi && e + PAGE > see_lo)) return false;
+                    return !PICK || ((s_bits[(tok - it.tok0) * nw + (e / PAGE >> 5) - w0] >> (e / PAGE & 31)) & 1u) != 0u;
+                };
+                const bool inside = primed && !careful && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
+                int hi = INT_MAX;
+                bool some = true, edge = false, first = false;
+                if (!inside) {
+                    const bool mine = sees(e0);
+                    hi = mine ? see_hi : 0;
+                    some = __any_sync(0xffffffffu, mine);             // of the warp's rows
+                    edge = e0 + PAGE > hi || e0 < see_lo;
+                    // the same for both warps of the rows: a row that has seen nothing yet finds its maximum first
+                    first = careful || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
                 }
-                const bool some = __any_sync(0xffffffffu, e0 >= 0 && e0 < hi && e0 + PAGE > see_lo);      // rows of the warp that see the page
-                const bool edge = e0 + PAGE > hi || e0 < see_lo;
                 uint32_t sv[32];
                 auto load = [&](int k) {                              // entries 32 k .. of the page, masked
                     a_tmem_ld32(s_addr + 32 * k, sv);
@@ -396,32 +417,35 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                             if (e0 + 32 * k + e >= hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
                     }
                 };
-                float mx = -INFINITY;
-                if (some) {
-                    float mq[2] = {-INFINITY, -INFINITY};
+                float m_all;
+                if (first) {
+                    if (some) {
+#pragma unroll 1
+                        for (int k = 0; k < 2; ++k) {
+                            load(k);
+                            float mq[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        load(k);
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4) {
-                            mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-                            mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                            for (int e = 0; e < 32; e += 4) {
+                                mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                                mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                            }
+                            m_mine = fmaxf(m_mine, fmaxf(mq[0], mq[1]) * scale_log2);            // scale_log2 > 0
                         }
                     }
-                    mx = fmaxf(mq[0], mq[1]);
-                }
-                mx_mine[(ex & 1) * 4 * T_ROWS] = mx;
-                ok = t_pair_sync(pair, ex);
-                if (!ok) break;
-                const float m_new = fmaxf(mx, mx_other[(ex & 1) * 4 * T_ROWS]) * scale_log2;      // scale_log2 > 0
-                ++ex;
-                if (__any_sync(0xffffffffu, m_new > m_used + T_RESCALE_STEP)) {                   // the same for both warps of the rows
-                    const float mn = fmaxf(m_used, m_new);
+                    mx_mine[(i & 1) * MX] = m_mine;
+                    ok = t_pair_sync(pair, ex);
+                    if (!ok) break;
+                    ++ex;
+                    m_all = fmaxf(m_mine, mx_other[(i & 1) * MX]);
+                } else
+                    m_all = fmaxf(m_mine, mx_other[((i - 1) & 1) * MX]);
+                if (__any_sync(0xffffffffu, m_all > m_used + T_RESCALE_STEP)) {
+                    const float mn = fmaxf(m_used, m_all);
                     const float alpha = (m_used == -INFINITY) ? 0.0f : exp2f(m_used - mn);
                     m_used = mn;
                     l *= alpha;
                     if (i > 0) {                                      // (O is complete up to the previous tile: see the commit of S)
-#pragma unroll
+#pragma unroll 1
                         for (int k = 0; k < D / 32; ++k) {
                             uint32_t ov[16];
                             t_tmem_ld16(o_addr + k * 16, ov);
@@ -432,10 +456,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                         }
                     }
                 }
+                if (!primed) primed = __all_sync(0xffffffffu, m_used > -INFINITY || !valid);
                 if (some) {
                     const float mref = (m_used == -INFINITY) ? 0.0f : m_used;
-                    const uint64_t sc2 = a_pack2(scale_log2, scale_log2), nm2 = a_pack2(-mref, -mref);
+                    const uint64_t nm2 = a_pack2(-mref, -mref);
                     uint64_t sq[2] = {0ull, 0ull};
+                    float mq[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         load(k);
@@ -443,12 +469,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             const uint64_t x2 = a_fma2(a_pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), sc2, nm2);
-                            float p0, p1;
+                            float x0, x1, p0, p1;
+                            a_unpack2(x2, x0, x1);
+                            mq[(e >> 1) & 1] = a_max3(mq[(e >> 1) & 1], x0, x1);
                             if ((e >> 1) % T_POLY_EVERY == T_POLY_EVERY - 1) {
                                 a_exp2_fma2(x2, p0, p1);
                             } else {
-                                float x0, x1;
-                                a_unpack2(x2, x0, x1);
                                 p0 = a_ex2(x0);
                                 p1 = a_ex2(x1);
                             }
@@ -460,6 +486,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     float a0, a1;
                     a_unpack2(a_add2(sq[0], sq[1]), a0, a1);
                     l += a0 + a1;
+                    const float mx = fmaxf(mq[0], mq[1]);
+                    m_mine = fmaxf(m_mine, mref + mx);
+                    if (!first && mx > T_LEAP) *s_redo = 1;
                 } else if (e0 >= 0) {
                     uint32_t pk[16];
 #pragma unroll
@@ -467,28 +496,28 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     t_tmem_st16(s_addr, pk);
                     t_tmem_st16(s_addr + 16, pk);
                 }
+                if (!first) mx_mine[(i & 1) * MX] = m_mine;           // read by the other thread at the next tile
                 t_tmem_wait_st();
                 a_fence_before();
                 __syncwarp();
                 if (lane == 0) a_bar_arrive(p_ready0 + 8 * grp);
             }
             if (ok && ntile > 0) ok = __all_sync(0xffffffffu, a_bar_wait(done0 + 8 * grp, (grp ? st1 : st0) & 1));
-            // the halves' sums, through the buffer that the next tile's maxima would use (its last readers are two exchanges back)
-            mx_mine[(ex & 1) * 4 * T_ROWS] = l;
+            mx_mine[2 * MX] = l;                                      // the two threads' sums
             if (ok) ok = t_pair_sync(pair, ex);
             if (!ok) {
                 if (lane == 0) *s_fail = 1;
             } else {
-                a_fence_after();
-                l += mx_other[(ex & 1) * 4 * T_ROWS];
                 ++ex;
+                a_fence_after();
+                l += mx_other[2 * MX];
                 if (m_used == -INFINITY && !(l != l)) l = 0.f;        // a row that sees nothing (the polynomial gives masked entries 2^-125)
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
                 uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * D + half * (D / 2));
                 const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
                 float4* po = reinterpret_cast<float4*>(wk.part_o + pr * D + half * (D / 2));
                 const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
-#pragma unroll
+#pragma unroll 1
                 for (int k = 0; k < D / 32; ++k) {
                     uint32_t ov[16];
                     if (ntile > 0) {
@@ -526,6 +555,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         __syncthreads();                                              // Q, the lists and tensor memory are free for the next stretch
         a_fence_after();
         if (*s_fail) break;
+        careful = !careful && *s_redo;                                // (a careful stretch sets no flag)
+        if (!careful) x += it.steps;
+        else {
+            __syncthreads();                                          // everyone has read the flag
+            if (threadIdx.x == 0) *s_redo = 0;
+        }
     }
     __syncthreads();
     if (warp == T_SOFT + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");

@@ -207,6 +207,29 @@ def test_attention_strided_queries_padding_and_scale(H, g, d, dtype):
     check_attention([400], [100], H, g, d, dtype, spread=6.0)                                  # large logits
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window", [0, 200])
+def test_attention_logits_that_leap(d, window):
+    """The reference of the softmax weights lags behind the maximum: logits that leap up (by far more than an exponent's range),
+    fall, and rise slowly along the keys, in rows of one call."""
+    H, g, n, new = 1, 4, 1500, 140
+    c = Cache([n], H, d, torch.bfloat16, DEV, 8)
+    q, cu = queries([new], H * g, d, torch.bfloat16, DEV, 8)
+    u = torch.zeros(d)
+    u[3] = 1.0
+    q[:, :, 3] = torch.tensor([2.0, -2.0, 0.5, 0.0]).to(q.dtype).to(DEV)[None, :, None].squeeze(-1)
+    steps = torch.zeros(n)
+    steps[200:] = 40.0
+    steps[450:] = 400.0
+    steps[700:900] = -300.0
+    steps[900:] = torch.linspace(-100, 900, n - 900)
+    for e in range(n):
+        c.k[c.table[0, e // PAGE].item(), :, e % PAGE, 3] = float(steps[e])
+    out = binding.paged_attention(c.k, c.v, q, ints(cu), c.lens, c.table, new, window=window)
+    want, bound, _ = attention(c.k, c.v, q, cu, [n], c.table, d ** -0.5, window)
+    assert ((out.double().cpu() - want).abs() <= bound).all()
+
+
 def test_attention_many_requests_and_mixed_batch():
     rng = random.Random(3)
     lens = [rng.randint(0, 150) for _ in range(1500)]
