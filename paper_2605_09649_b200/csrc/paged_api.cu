@@ -204,7 +204,7 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
         // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
         // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
         // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page, and two requests cannot differ in width.
-        const int unit_tokens = PAGED_TC_ROWS / pb.g + 2;
+        const int unit_tokens = PAGED_TC_ROWS / pb.g + 2 + 1;            // and the union's own row of bits
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
         pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);
         // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request

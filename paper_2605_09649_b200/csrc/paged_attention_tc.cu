@@ -205,20 +205,23 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         if (PICK && npage > 0) {
             // ---- which token selected which page of the stretch; the union, ascending
             const int ntok = it.tok1 - it.tok0 + 1;
-            for (int i = threadIdx.x; i < ntok * nw; i += T_THREADS) s_bits[i] = 0u;
+            for (int i = threadIdx.x; i < (ntok + 1) * nw; i += T_THREADS) s_bits[i] = 0u;      // a row of bits per token, the union last
             __syncthreads();
             for (int i = threadIdx.x; i < ntok * pb.pick_top; i += T_THREADS) {
                 const int tk = i / pb.pick_top, e = i - tk * pb.pick_top;
                 const int page = pb.selected[((size_t)(it.q.row0 + it.tok0 + tk) * pv.H + it.h) * pb.pick_top + e];
-                if (page >= it.p0 && page < it.p1) atomicOr(&s_bits[tk * nw + (page >> 5) - w0], 1u << (page & 31));
+                if (page >= it.p0 && page < it.p1) {
+                    const int word = (page >> 5) - w0;
+                    const uint32_t bit = 1u << (page & 31);
+                    atomicOr(&s_bits[tk * nw + word], bit);
+                    if (!(reinterpret_cast<volatile uint32_t*>(s_bits)[ntok * nw + word] & bit)) atomicOr(&s_bits[ntok * nw + word], bit);
+                }
             }
             __syncthreads();
             if (warp == 0) {
                 int at = 0;
                 for (int i0 = 0; i0 < nw; i0 += 32) {
-                    uint32_t any = 0u;
-                    if (i0 + lane < nw)
-                        for (int tk = 0; tk < ntok; ++tk) any |= s_bits[tk * nw + i0 + lane];
+                    uint32_t any = i0 + lane < nw ? s_bits[ntok * nw + i0 + lane] : 0u;
                     int before = __popc(any);
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
@@ -397,13 +400,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     return !PICK || ((s_bits[(tok - it.tok0) * nw + (e / PAGE >> 5) - w0] >> (e / PAGE & 31)) & 1u) != 0u;
                 };
                 const bool inside = primed && !careful && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
-                int hi = INT_MAX;
-                bool some = true, edge = false, first = false;
+                bool mine = true, some = true, edge = false, first = false;
                 if (!inside) {
-                    const bool mine = sees(e0);
-                    hi = mine ? see_hi : 0;
+                    mine = sees(e0);
                     some = __any_sync(0xffffffffu, mine);             // of the warp's rows
-                    edge = e0 + PAGE > hi || e0 < see_lo;
+                    // a row that sees nothing of the page is weighed to nothing below (mref); only what lies behind the last
+                    // entry has to go, it may be NaN
+                    edge = mine ? e0 + PAGE > see_hi || e0 < see_lo : e0 + PAGE > it.q.len;
                     // the same for both warps of the rows: a row that has seen nothing yet finds its maximum first
                     first = careful || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
                 }
@@ -414,7 +417,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     if (edge) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (e0 + 32 * k + e >= hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
+                            if (e0 + 32 * k + e >= see_hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
                     }
                 };
                 float m_all;
@@ -429,7 +432,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                                 mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
                                 mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
                             }
-                            m_mine = fmaxf(m_mine, fmaxf(mq[0], mq[1]) * scale_log2);            // scale_log2 > 0
+                            if (mine) m_mine = fmaxf(m_mine, fmaxf(mq[0], mq[1]) * scale_log2);  // scale_log2 > 0
                         }
                     }
                     mx_mine[(i & 1) * MX] = m_mine;
@@ -458,7 +461,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 }
                 if (!primed) primed = __all_sync(0xffffffffu, m_used > -INFINITY || !valid);
                 if (some) {
-                    const float mref = (m_used == -INFINITY) ? 0.0f : m_used;
+                    // a row that sees nothing of the page weighs it against +inf: every weight is 0
+                    const float mref = !mine ? INFINITY : (m_used == -INFINITY) ? 0.0f : m_used;
                     const uint64_t nm2 = a_pack2(-mref, -mref);
                     uint64_t sq[2] = {0ull, 0ull};
                     float mq[2] = {-INFINITY, -INFINITY};
@@ -487,8 +491,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                     a_unpack2(a_add2(sq[0], sq[1]), a0, a1);
                     l += a0 + a1;
                     const float mx = fmaxf(mq[0], mq[1]);
-                    m_mine = fmaxf(m_mine, mref + mx);
-                    if (!first && mx > T_LEAP) *s_redo = 1;
+                    if (mine) {
+                        m_mine = fmaxf(m_mine, mref + mx);
+                        if (!first && mx > T_LEAP) *s_redo = 1;
+                    }
                 } else if (e0 >= 0) {
                     uint32_t pk[16];
 #pragma unroll
