@@ -80,7 +80,8 @@ __device__ __forceinline__ PagedReq paged_request(const PagedBatch& pb, int r) {
 // `total` steps, and worker w of N takes the steps [total w / N, total (w + 1) / N): equal shares whatever the lengths, no
 // counters.  A worker's first and last unit may be shared with its neighbours; then it stores a partial result
 // (m, l, O) -- slot 2 w for a unit that it did not begin, slot 2 w + 1 for one that it began and did not end -- and a
-// second kernel joins the partials.
+// second kernel joins the partials.  Where whole units balance about as well (many short ones, or few that are short), a
+// worker takes whole units instead and nothing is joined.
 struct PagedCost { int U, C; };
 __device__ __forceinline__ PagedCost paged_cost(const PagedBatch& pb, const PagedReq& q, int tile_rows, int min_rows, int max_rows) {
     PagedCost c;
@@ -110,7 +111,9 @@ __device__ __forceinline__ long long paged_div(long long a, int b) {
 constexpr int PAGED_GROUPS = 512;             // groups of consecutive requests in the shared-memory table
 struct PagedTableMem {                        // shared memory of the table
     long long grp[PAGED_GROUPS + 1];          // steps before a group
-    int4 req[PAGED_GROUPS];                   // {row0, n, len, 0} of each request where a group is one request
+    int4 req[PAGED_GROUPS];                   // {row0, n, len, units} of each request where a group is one request
+    unsigned long long steps, units;
+    int longest, whole;
 };
 struct PagedTable {
     PagedTableMem* mem;
@@ -118,6 +121,7 @@ struct PagedTable {
     int tile_rows, min_rows, max_rows;
     long long total;
     int workers;                              // workers that take part: no share is under min_share steps
+    bool whole;                               // the line counts whole units, not steps
     long long quot;                           // total = quot * workers + rem
     int rem;
     // First step of worker w: floor(total w / workers).
@@ -126,32 +130,47 @@ struct PagedTable {
 
 __device__ __forceinline__ void paged_finish_table(PagedTable& t, int R, int max_workers, int min_share, long long* prefix) {
     t.total = t.mem->grp[t.ngrp];
-    t.workers = (int)min((long long)max_workers, paged_div(t.total + min_share - 1, min_share));
+    t.workers = (int)min((long long)max_workers, t.whole ? t.total : paged_div(t.total + min_share - 1, min_share));
     t.quot = t.workers ? paged_div(t.total, t.workers) : 0;
     t.rem = (int)(t.total - t.quot * t.workers);
-    if (prefix && blockIdx.x == 0 && threadIdx.x == 0) { prefix[R] = t.total; prefix[R + 1] = t.workers; }
+    if (prefix && blockIdx.x == 0 && threadIdx.x == 0) { prefix[R] = t.total; prefix[R + 1] = t.whole ? 0 : t.workers; }
+}
+// steps, units and the longest unit of all requests: do whole units do?
+// join_steps: what joining parts costs, in steps of the kernel.
+__device__ __forceinline__ bool paged_choose_whole(long long steps, long long units, int longest, int max_workers, int join_steps) {
+    return paged_div(units + max_workers - 1, max_workers) * longest <= paged_div(steps, max_workers) + join_steps;
 }
 
 // Every thread of the block calls it.  prefix (may be null): steps before each request, [R + 1], written by block 0;
-// prefix[R + 1] = workers.
+// prefix[R + 1] = workers, or 0 where the line counts whole units (nothing is joined then).
 __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
-                                                  int max_rows, int max_workers, int min_share, PagedTableMem* mem, long long* prefix) {
+                                                  int max_rows, int max_workers, int min_share, int join_steps, PagedTableMem* mem,
+                                                  long long* prefix) {
     t.mem = mem;
     t.heads = heads;
     t.tile_rows = tile_rows; t.min_rows = min_rows; t.max_rows = max_rows;
-    if (pb.R <= 32) {                         // one warp, one barrier
+    if (pb.R <= 32) {                         // by one warp
         t.gsz = 1;
         t.ngrp = pb.R;
         if (threadIdx.x < 32) {
             const int r = threadIdx.x;
             PagedReq q = {0, 0, 0};
-            long long sum = 0;
+            PagedCost c = {0, 1};
             if (r < pb.R) {
                 q = paged_request(pb, r);
-                const PagedCost c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
-                sum = (long long)(c.U * heads) * c.C;
+                c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
             }
-            const long long mine = sum;
+            const int units = c.U * heads;
+            long long all_steps = (long long)units * c.C, all_units = units;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                all_steps += __shfl_xor_sync(0xffffffffu, all_steps, o);
+                all_units += __shfl_xor_sync(0xffffffffu, all_units, o);
+            }
+            const int longest = __reduce_max_sync(0xffffffffu, c.U ? c.C : 0);
+            t.whole = paged_choose_whole(all_steps, all_units, longest, max_workers, join_steps);
+            const long long mine = t.whole ? units : (long long)units * c.C;
+            long long sum = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long v = __shfl_up_sync(0xffffffffu, sum, o);
@@ -159,27 +178,41 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
             }
             mem->req[r] = make_int4(q.row0, q.n, q.len, 0);
             mem->grp[r + 1] = sum;
-            if (r == 0) mem->grp[0] = 0;
+            if (r == 0) { mem->grp[0] = 0; mem->whole = t.whole; }
             if (prefix && blockIdx.x == 0 && r < pb.R) prefix[r] = sum - mine;
         }
         __syncthreads();
+        t.whole = mem->whole;
         paged_finish_table(t, pb.R, max_workers, min_share, prefix);
         return;
     }
     t.gsz = (pb.R + PAGED_GROUPS - 1) / PAGED_GROUPS;
     t.ngrp = (pb.R + t.gsz - 1) / t.gsz;
+    if (threadIdx.x == 0) { mem->grp[0] = 0; mem->steps = 0; mem->units = 0; mem->longest = 0; }
+    __syncthreads();
     for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
-        long long sum = 0;
+        long long steps = 0, units = 0;
+        int longest = 0;
         for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
             const PagedReq q = paged_request(pb, r);
             const PagedCost c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
-            sum += (long long)(c.U * heads) * c.C;
-            if (t.gsz == 1) mem->req[gi] = make_int4(q.row0, q.n, q.len, 0);
+            units += c.U * heads;
+            steps += (long long)(c.U * heads) * c.C;
+            if (c.U) longest = max(longest, c.C);
+            if (t.gsz == 1) mem->req[gi] = make_int4(q.row0, q.n, q.len, (int)units);
         }
-        mem->grp[gi + 1] = sum;
+        mem->grp[gi + 1] = steps;
+        atomicAdd(&mem->steps, (unsigned long long)steps);        // (sums of integers: any order gives the same)
+        atomicAdd(&mem->units, (unsigned long long)units);
+        atomicMax(&mem->longest, longest);
     }
-    if (threadIdx.x == 0) mem->grp[0] = 0;
     __syncthreads();
+    // (groups of several requests keep to steps: their units are not kept apart)
+    t.whole = t.gsz == 1 && paged_choose_whole((long long)mem->steps, (long long)mem->units, mem->longest, max_workers, join_steps);
+    if (t.whole) {
+        for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) mem->grp[gi + 1] = mem->req[gi].w;
+        __syncthreads();
+    }
     if (threadIdx.x < 32) {                   // inclusive scan by one warp
         const int lane = threadIdx.x, per = (t.ngrp + 31) / 32;
         const int g0 = min(t.ngrp, lane * per), g1 = min(t.ngrp, g0 + per);
@@ -195,7 +228,7 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
         for (int gi = g0; gi < g1; ++gi) { run += mem->grp[gi + 1]; mem->grp[gi + 1] = run; }
     }
     __syncthreads();
-    if (prefix && blockIdx.x == 0) {
+    if (prefix && blockIdx.x == 0 && !t.whole) {
         for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
             long long run = mem->grp[gi];
             for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
@@ -259,9 +292,9 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
         }
     }
     const long long off = x - base;
-    const int unit = (int)paged_div(off, c.C), v0 = (int)(off - (long long)unit * c.C);
-    it.steps = min((long long)(c.C - v0), end - x);
-    const int v1 = v0 + (int)it.steps;
+    const int unit = t.whole ? (int)off : (int)paged_div(off, c.C), v0 = t.whole ? 0 : (int)(off - (long long)unit * c.C);
+    it.steps = t.whole ? 1 : min((long long)(c.C - v0), end - x);
+    const int v1 = t.whole ? c.C : v0 + (int)it.steps;
     it.r = r;
     it.q = q;
     it.h = unit / c.U;
@@ -364,10 +397,9 @@ constexpr int PAGED_SELECT_SMEM = 196 * 1024;
 size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st);
-// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows; many_rows: units of
-// many rows and few parts (the tensor-core kernel's).
+// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows.
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
-                              int min_rows, int max_rows, bool many_rows, cudaStream_t st);
+                              int min_rows, int max_rows, cudaStream_t st);
 cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
                                          float scale, const PagedWork& w, cudaStream_t st);
 

@@ -168,7 +168,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, table_mem, wk.prefix);
+    paged_build_table(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
@@ -586,7 +586,7 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_tc_kernel<D, PICK>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
                      (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, true, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, st);
 }
 
 }  // namespace

@@ -73,7 +73,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, table_mem, wk.prefix);      // (synchronises the block)
+    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem, wk.prefix);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
     const int w = team * (int)gridDim.x + (int)blockIdx.x;
@@ -343,7 +343,7 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
                      (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, false, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, st);
 }
 
 }  // namespace
