@@ -29,6 +29,21 @@ inline cudaError_t paged_allow_smem(const void* kernel, int bytes, std::atomic<u
     return e;
 }
 
+// Division by a number that the host knows, in three instructions (a division by a variable is thirty, and these kernels'
+// short runs are paced by fetching their code): q = (mulhi(n, m) + n) >> s with s = ceil(log2 d), m = floor(2^32 (2^s - d) / d) + 1,
+// for 0 <= n < 2^31 (Granlund and Montgomery, Division by Invariant Integers using Multiplication).
+struct FastDiv {
+    uint32_t m, s, d;
+    static FastDiv by(int d) {
+        FastDiv f = {1u, 0u, (uint32_t)d};
+        while ((1ull << f.s) < (unsigned long long)d) ++f.s;
+        f.m = (uint32_t)((((1ull << f.s) - (unsigned long long)d) << 32) / (unsigned long long)d) + 1u;
+        return f;
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+
 struct PagedView {
     const char* k;
     const char* v;
@@ -45,12 +60,15 @@ struct PagedBatch {
     long long q_stride;       // elements from one token's q to the next
     int window;               // > 0: a token sees the last `window` entries up to its own; 0: all of them
     int top, sink, recent;    // page selection (top = 0: every page is read)
+    int sub;                  // ... units per token: its g rows in blocks of sub_rows
+    int sub_rows;
     const int32_t* selected;  // [T][H][top] pages to read, ascending, -1 behind the last
     // Page selection may run two kernels: pick < 0 marks the one that reads each token's pages for itself (top > 0), pick > 0 the
     // one that walks the union of a unit's tokens' pages (top = 0, the selection's width in pick_top).  A request goes to the
     // second if it has at least PAGED_PICK_ROWS rows and at most pick_pages pages.  0: one kernel takes all requests.
     int pick, pick_top, pick_pages;
     int32_t* status;          // latched status, may be null
+    FastDiv by_g, by_hq, by_h, by_sub, by_sub_rows;
 };
 
 constexpr int PAGED_MAX_REQ = 8192;
@@ -83,19 +101,24 @@ __device__ __forceinline__ PagedReq paged_request(const PagedBatch& pb, int r) {
 // second kernel joins the partials.  Where whole units balance about as well (many short ones, or few that are short), a
 // worker takes whole units instead and nothing is joined.
 struct PagedCost { int U, C; };
+// SEL: whether pages are selected, where a kernel knows it (0, 1); -1: the batch says (top > 0).
+template <int SEL>
+__device__ __forceinline__ bool paged_selects(const PagedBatch& pb) { return SEL < 0 ? pb.top > 0 : SEL != 0; }
+
+template <int SEL>
 __device__ __forceinline__ PagedCost paged_cost(const PagedBatch& pb, const PagedReq& q, int tile_rows, int min_rows, int max_rows) {
     PagedCost c;
     const int rows = q.n * pb.g;
     int pages = (q.len + PAGE - 1) / PAGE;
     const bool walks = rows >= PAGED_PICK_ROWS && pages <= pb.pick_pages;
     if (q.n == 0 || rows < min_rows || rows > max_rows || (pb.pick != 0 && walks != (pb.pick > 0))) { c.U = 0; c.C = 1; return c; }
-    if (pb.top > 0) {
-        c.U = q.n;
+    if (paged_selects<SEL>(pb)) {
+        c.U = q.n * pb.sub;
         pages = min(pages, pb.top);
     } else {
         c.U = (rows + tile_rows - 1) / tile_rows;
         if (pb.window > 0) {                              // entries that the tokens of one unit see, spread over pages
-            const long long span = (long long)pb.window + min(q.n, tile_rows / pb.g + 2);
+            const long long span = (long long)pb.window + min(q.n, pb.by_g.div(tile_rows) + 2);
             pages = (int)min((long long)pages, span / PAGE + 2);
         }
     }
@@ -143,6 +166,7 @@ __device__ __forceinline__ bool paged_choose_whole(long long steps, long long un
 
 // Every thread of the block calls it.  prefix (may be null): steps before each request, [R + 1], written by block 0;
 // prefix[R + 1] = workers, or 0 where the line counts whole units (nothing is joined then).
+template <int SEL>
 __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
                                                   int max_rows, int max_workers, int min_share, int join_steps, PagedTableMem* mem,
                                                   long long* prefix) {
@@ -158,7 +182,7 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
             PagedCost c = {0, 1};
             if (r < pb.R) {
                 q = paged_request(pb, r);
-                c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
+                c = paged_cost<SEL>(pb, q, tile_rows, min_rows, max_rows);
             }
             const int units = c.U * heads;
             long long all_steps = (long long)units * c.C, all_units = units;
@@ -195,7 +219,7 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
         int longest = 0;
         for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
             const PagedReq q = paged_request(pb, r);
-            const PagedCost c = paged_cost(pb, q, tile_rows, min_rows, max_rows);
+            const PagedCost c = paged_cost<SEL>(pb, q, tile_rows, min_rows, max_rows);
             units += c.U * heads;
             steps += (long long)(c.U * heads) * c.C;
             if (c.U) longest = max(longest, c.C);
@@ -233,7 +257,7 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
             long long run = mem->grp[gi];
             for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
                 prefix[r] = run;
-                const PagedCost c = paged_cost(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
+                const PagedCost c = paged_cost<SEL>(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
                 run += (long long)(c.U * heads) * c.C;
             }
         }
@@ -257,6 +281,18 @@ __device__ __forceinline__ int paged_owner(long long total, int workers, long lo
 __device__ __forceinline__ int paged_fold(int v, int U) { return (v & 1) ? v / 2 : U - 1 - v / 2; }
 __device__ __forceinline__ int paged_unfold(int u, int U) { return u >= U - 1 - (U - 1) / 2 ? 2 * (U - 1 - u) : 2 * u + 1; }
 
+// First of the request's n * g (token, query head) rows that belong to unit u, and how many do.
+template <int SEL>
+__device__ __forceinline__ int paged_unit_first(const PagedBatch& pb, int u, int tile_rows) {
+    if (!paged_selects<SEL>(pb)) return u * tile_rows;
+    const int t = pb.by_sub.div(u);
+    return t * pb.g + (u - t * pb.sub) * pb.sub_rows;
+}
+template <int SEL>
+__device__ __forceinline__ int paged_unit_rows(const PagedBatch& pb, int u, int n, int tile_rows) {
+    return paged_selects<SEL>(pb) ? min(pb.sub_rows, pb.g - pb.by_sub.mod(u) * pb.sub_rows) : min(tile_rows, n * pb.g - u * tile_rows);
+}
+
 // One stretch of a unit, as a worker meets it.
 struct PagedItem {
     int r, h, u;            // request, KV head, unit of the request
@@ -267,6 +303,7 @@ struct PagedItem {
     int tok0, tok1;         // tokens (of the request) that the unit's rows belong to, tok1 inclusive
 };
 
+template <int SEL>
 __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const PagedBatch& pb, long long x, long long end, int w) {
     PagedItem it;
     int lo = 0, hi = t.ngrp - 1;
@@ -281,11 +318,11 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     if (t.gsz == 1) {
         const int4 v = t.mem->req[lo];
         q.row0 = v.x; q.n = v.y; q.len = v.z;
-        c = paged_cost(pb, q, t.tile_rows, t.min_rows, t.max_rows);
+        c = paged_cost<SEL>(pb, q, t.tile_rows, t.min_rows, t.max_rows);
     } else {
         for (;; ++r) {
             q = paged_request(pb, r);
-            c = paged_cost(pb, q, t.tile_rows, t.min_rows, t.max_rows);
+            c = paged_cost<SEL>(pb, q, t.tile_rows, t.min_rows, t.max_rows);
             const long long s = (long long)(c.U * t.heads) * c.C;
             if (x < base + s || r + 1 >= pb.R) break;
             base += s;
@@ -300,14 +337,14 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     it.h = unit / c.U;
     it.u = paged_fold(unit - it.h * c.U, c.U);
     int first, count;                                     // the unit's pages
-    if (pb.top > 0) {
-        it.tok0 = it.tok1 = it.u;
-        const int pos = q.len - q.n + it.u;
+    if (paged_selects<SEL>(pb)) {
+        it.tok0 = it.tok1 = pb.by_sub.div(it.u);
+        const int pos = q.len - q.n + it.tok0;
         first = 0;
         count = pos < 0 ? 0 : min(pb.top, pos / PAGE + 1);
     } else {
-        it.tok0 = it.u * t.tile_rows / pb.g;
-        it.tok1 = min(q.n - 1, ((it.u + 1) * t.tile_rows - 1) / pb.g);
+        it.tok0 = pb.by_g.div(it.u * t.tile_rows);
+        it.tok1 = min(q.n - 1, pb.by_g.div((it.u + 1) * t.tile_rows - 1));
         const int plo = q.len - q.n + it.tok0, phi = q.len - q.n + it.tok1;
         first = pb.window > 0 ? max(0, plo - pb.window + 1) / PAGE : 0;
         count = phi < 0 ? 0 : phi / PAGE + 1 - first;
@@ -350,7 +387,7 @@ __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedV
 // [prefix: (PAGED_MAX_REQ + 2) int64][partials of the first kernel][of the second][the second kernel's schedule]
 constexpr int PAGED_SMS = 148;
 constexpr int PAGED_WARP_ROWS = 64, PAGED_WARPS = 4;              // warp kernel: rows per unit at most, workers per SM (2 above 16 rows)
-constexpr int PAGED_PLAIN_ROWS = 16, PAGED_PLAIN_CTAS = 4;        // plain kernel: rows per unit, CTAs per SM at most
+constexpr int PAGED_F32_ROWS = 16, PAGED_F32_CTAS = 2;        // fp32 kernel: rows per unit, CTAs per SM at most
 constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
 constexpr size_t PAGED_PREFIX_BYTES = ((size_t)(PAGED_MAX_REQ + 2) * 8 + 255) & ~(size_t)255;
 // partial results of `rows` rows (workers x rows per unit), two slots each
@@ -400,12 +437,12 @@ cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int i
 // Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows.
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
                               int min_rows, int max_rows, cudaStream_t st);
-cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
-                                         float scale, const PagedWork& w, cudaStream_t st);
-
+// fp32 caches.
+cudaError_t launch_paged_attention_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
+                                       cudaStream_t st);
 cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows, int box_planes);      // see its definition
-// The bf16 forms for head sizes 64 and 128.  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8,
-// 16, 32 or 64 (page selection: g <= 64).  Tensor-core kernel: the requests of more than min_rows - 1 rows.
+// The bf16 forms: head sizes up to 256 (warp kernel) and 128 (tensor-core kernel).  Warp kernel: requests of min_rows = 1 to max_rows rows in units of tile_rows = 8,
+// 16, 32 or 64.  Tensor-core kernel: the requests of more than min_rows - 1 rows.
 cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                         int tile_rows, int max_rows, cudaStream_t st);
 cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,

@@ -44,14 +44,12 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
 // Workspace: two areas {steps before each request, partial results}.  The first serves the kernel that a call always has or the
 // only one, the second the tensor-core kernel.  Sizes depend on the head layout alone.
 size_t area_bytes(int rows, int d) { return PAGED_PREFIX_BYTES + paged_partial_bytes(rows, d); }
-// The most (workers x rows of a unit) of the first kernels: the plain kernel's units are 16 rows, or a token's g where
-// pages are selected; the warp kernel's 8 or 16 with four workers per SM, 32 or 64 with two.
-int first_rows(int g) {
-    const int plain = PAGED_SMS * PAGED_PLAIN_CTAS * (g > PAGED_PLAIN_ROWS ? g : PAGED_PLAIN_ROWS), warp = PAGED_SMS * 2 * PAGED_WARP_ROWS;
-    return plain > warp ? plain : warp;
-}
-size_t first_area(int g, int d) { return area_bytes(first_rows(g), d); }
-size_t work_bytes(int g, int d) { return first_area(g, d) + area_bytes(PAGED_SMS * PAGED_TC_ROWS, d); }
+// The most (workers x rows of a unit) of the first kernels: the fp32 kernel's units are 16 rows; the warp kernel's 8 or 16 with
+// four workers per SM, 32 or 64 with two.
+constexpr int FIRST_ROWS = PAGED_SMS * 2 * PAGED_WARP_ROWS;
+static_assert(PAGED_F32_CTAS * PAGED_F32_ROWS <= 2 * PAGED_WARP_ROWS && PAGED_WARPS * 16 <= 2 * PAGED_WARP_ROWS, "every kernel fits");
+size_t first_area(int d) { return area_bytes(FIRST_ROWS, d); }
+size_t work_bytes(int d) { return first_area(d) + area_bytes(PAGED_SMS * PAGED_TC_ROWS, d); }
 PagedWork carve(void* area, int rows, int d) {
     char* p = (char*)area;
     PagedWork w;
@@ -77,8 +75,7 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
         return refuse(TRIMKV_E_ARG, "cu_new, lens and block_table must be non-NULL and aligned");
     if (!(scale > 0.f) || isinf(scale)) return refuse(TRIMKV_E_ARG, "scale must be positive and finite");
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return refuse(TRIMKV_E_ARG, "workspace must be non-NULL and 256-byte aligned");
-    const int g = q_heads / pv.H;
-    const size_t need = work_bytes(g, pv.d);
+    const size_t need = work_bytes(pv.d);
     if (workspace_bytes < need) return refuse(TRIMKV_E_ARG, "workspace too small: %zu bytes, %zu needed", workspace_bytes, need);
     *pb = PagedBatch{};
     pb->cu_new = cu_new;
@@ -88,7 +85,10 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
     pb->W = table_width;
     pb->T = (int)n_tokens;
     pb->Hq = q_heads;
-    pb->g = g;
+    pb->g = q_heads / pv.H;
+    pb->by_g = FastDiv::by(pb->g);
+    pb->by_hq = FastDiv::by(q_heads);
+    pb->by_h = FastDiv::by(pv.H);
     pb->q_stride = q_stride;
     pb->status = status;
     return TRIMKV_OK;
@@ -135,7 +135,7 @@ trimkv_status trimkv_paged_append(const trimkv_paged_cache* cache, int64_t n_tok
 
 size_t trimkv_paged_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
     if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads || head_dim < 8 || head_dim > 256 || head_dim % 8 || q_heads / kv_heads > 128) return 0;
-    return work_bytes(q_heads / kv_heads, head_dim);
+    return work_bytes(head_dim);
 }
 
 trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t max_new, int32_t q_heads,
@@ -154,18 +154,19 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     if (n_tokens == 0) return TRIMKV_OK;
     pb.window = window;
     const cudaStream_t st = (cudaStream_t)stream;
-    const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
-    if (!is_bf16 || (pv.d != 64 && pv.d != 128)) return done(launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st), "attention");
+    const PagedWork w = carve(workspace, FIRST_ROWS, pv.d);
+    if (!is_bf16) return done(launch_paged_attention_f32(pv, pb, q, out, scale, w, st), "attention");
     // Requests of up to 64 rows (tokens x query heads of a KV head) stream through the warp kernel, larger ones go to the
     // tcgen05 kernel; of a batch with both, those of up to 32.  max_new may be wrong: every kernel takes any request, and where
     // both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
+    const bool tc = pv.d <= 128;
     cudaError_t e = cudaSuccess;
-    if (most <= PAGED_WARP_ROWS) {
+    if (most <= PAGED_WARP_ROWS || !tc) {
         e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64, INT_MAX, st);
     } else {
         const bool equal = max_new > 0 && n_tokens == (int64_t)n_req * max_new;    // every request has max_new tokens: one kernel
-        const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
+        const PagedWork w2 = carve((char*)workspace + first_area(pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
         e = launch_paged_attention_tc(pv, pb, q, out, scale, w2, equal ? 1 : 33, st);
         if (e == cudaSuccess && !equal) e = launch_paged_attention_warp(pv, pb, q, out, scale, w, 32, 32, st);
     }
@@ -198,9 +199,15 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     s = done(launch_paged_select(pv, pb, is_bf16, q, selected, (cudaStream_t)stream), "page selection");
     if (s != TRIMKV_OK) return s;
     const cudaStream_t st = (cudaStream_t)stream;
-    const PagedWork w = carve(workspace, first_rows(pb.g), pv.d);
+    const PagedWork w = carve(workspace, FIRST_ROWS, pv.d);
     cudaError_t e = cudaSuccess;
-    if (is_bf16 && (pv.d == 64 || pv.d == 128)) {
+    // a token's g rows are one unit, or several of the most rows that the kernel holds
+    const int most = is_bf16 ? (pv.d > 128 ? 32 : PAGED_WARP_ROWS) : PAGED_F32_ROWS;
+    pb.sub_rows = pb.g < most ? pb.g : most;
+    pb.sub = (pb.g + pb.sub_rows - 1) / pb.sub_rows;
+    pb.by_sub = FastDiv::by(pb.sub);
+    pb.by_sub_rows = FastDiv::by(pb.sub_rows);
+    if (is_bf16) {
         // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
         // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
         // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page, and two requests cannot differ in width.
@@ -208,21 +215,20 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
         pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);
         // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request
-        const bool walk = pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
+        const bool walk = pv.d <= 128 && pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
         if (walk) {
             PagedBatch pu = pb;
             pu.top = 0;
             pu.pick = 1;
             pu.pick_top = top_pages;
-            const PagedWork w2 = carve((char*)workspace + first_area(pb.g, pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
+            const PagedWork w2 = carve((char*)workspace + first_area(pv.d), PAGED_SMS * PAGED_TC_ROWS, pv.d);
             e = launch_paged_attention_tc(pv, pu, q, out, scale, w2, 1, st);
             pb.pick = -1;
         }
         if (e == cudaSuccess)
-            e = pb.g <= PAGED_WARP_ROWS ? launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, st)
-                                        : launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st);
+            e = launch_paged_attention_warp(pv, pb, q, out, scale, w, pb.g <= 8 ? 8 : pb.g <= 16 ? 16 : pb.g <= 32 ? 32 : 64, INT_MAX, st);
     } else
-        e = launch_paged_attention_plain(pv, pb, is_bf16, q, out, scale, w, st);
+        e = launch_paged_attention_f32(pv, pb, q, out, scale, w, st);
     return done(e, "attention");
 }
 

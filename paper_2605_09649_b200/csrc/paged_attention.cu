@@ -1,13 +1,14 @@
-// Attention of new tokens over the caller-owned paged cache: the form for any head size and type, and the kernel that joins
-// partial results.
+// Attention of new tokens over the caller-owned paged cache: the fp32 form, and the kernel that joins partial results.
 //
-// Plain form.  A CTA of 256 threads holds 16 (token, query head) rows of one KV head and walks its share of the pages
-// (paged_item), a page at a time: cp.async brings K and V as they are stored into one of two buffers while the page before
-// is worked on (rows behind the last entry are filled with zeros); S = Q K^T in fp32 with one key and four rows per thread -- a
-// warp has 8 keys x 16 rows, so that a 16-byte read of K serves 16 FMAs and the reads of Q are broadcasts --, the running
-// maximum and sum of the softmax with two rows per warp, then O += P V with a column and 4 to 16 rows of O per thread.  All
-// sums are fp32.  fp32 caches and head sizes other than 64 and 128 run here; bound by shared-memory reads (about 2200 cycles a
-// page at d = 64) beyond a few rows per page, by the page loads below that.
+// fp32 form.  A CTA of 256 threads holds 16 (token, query head) rows of one KV head and walks its share of the pages
+// (paged_item), a page at a time: cp.async brings K and V into one of two buffers while the page before is worked on (rows
+// behind the last entry are filled with zeros).  The products run on the tensor cores in three TF32 parts: a value is split
+// x = hi + lo with hi and lo rounded to 11 bits, and hi hi + hi lo + lo hi leaves out 2^-22 of a product, as fp32 does; the
+// parts go to accumulators of their own (short chains) and are added up at the end of a page.  S = Q K^T: a warp has 8 keys
+// x 16 rows, its K fragments come by ldmatrix and Q waits in registers (head sizes up to 128); the running maximum and sum of
+// the softmax with two rows per warp; O += P V: a warp has an eighth of the columns.  Plain fp32 FMAs were bound by shared
+// memory (a 16-byte read per 4 products: 5100 cycles a page at d = 64); this is bound by the page loads for the few rows of a
+// decode step, by the latency of a page's three phases otherwise.
 #include "mma_sync.cuh"
 #include "paged.cuh"
 
@@ -16,206 +17,252 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int PL_THREADS = 256, PL_ROWS = PAGED_PLAIN_ROWS;
+constexpr int F_THREADS = 256, F_ROWS = PAGED_F32_ROWS;
 
-// DP: head size rounded up to 64, 128 or 256
-template <typename T, int DP>
-struct PlainShape {
-    static constexpr int E = 16 / (int)sizeof(T);
-    static constexpr int KS = DP + E;                             // row stride of K (elements): rows 16 bytes apart modulo 128
-    static constexpr int QS = DP + 4;                             // row stride of Q (floats)
-    static constexpr int COLS = DP, RG = PL_THREADS / COLS;       // columns, row groups of O over the threads
-    static constexpr int RPT = PL_ROWS / RG;                      // rows of O per thread
-    static constexpr int STAGE = PAGE * (KS + DP) * (int)sizeof(T);
-    static constexpr int STAGES = STAGE <= 100 * 1024 ? 2 : 1;
-    static constexpr int SMEM = STAGES * STAGE + (int)sizeof(float) * (PL_ROWS * QS + PL_ROWS * PAGE + 3 * PL_ROWS);
-    static constexpr int CTAS = SMEM <= 100 * 1024 ? 2 : 1;       // per SM
+// DP: head size rounded up to 64, 128 or 256.  Row strides: ldmatrix reads 8 rows of 16 bytes (16 bytes apart modulo 128), the V
+// fragments 4 rows of 8 words (8 words apart modulo 32).
+template <int DP>
+struct F32Shape {
+    static constexpr int KS = DP + 4, VS = DP + 8, QS = DP + 4, PS = PAGE + 4;
+    static constexpr int STAGE = PAGE * (KS + VS);                // floats
+    static constexpr int STAGES = DP == 256 ? 1 : 2;
+    static constexpr bool Q_REG = DP <= 128;
+    static constexpr int SMEM = (int)sizeof(float) * (STAGES * STAGE + 2 * F_ROWS * QS + F_ROWS * PS + 3 * F_ROWS);
+    static constexpr int CTAS = DP == 64 ? 2 : 1;                 // per SM
 };
 
-template <typename T>
-__device__ __forceinline__ float4 plain_load4(const T* p);
-template <>
-__device__ __forceinline__ float4 plain_load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <>
-__device__ __forceinline__ float4 plain_load4<__nv_bfloat16>(const __nv_bfloat16* p) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-}
 // 16 bytes, or zeros (src is not read).
-__device__ __forceinline__ void plain_copy16(void* dst, const void* src, bool on) {
+__device__ __forceinline__ void f32_copy16(void* dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ uint32_t f32_tf32(float x) {
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void f32_split(uint32_t x, uint32_t& hi, uint32_t& lo) {
+    hi = f32_tf32(__uint_as_float(x));
+    lo = f32_tf32(__uint_as_float(x) - __uint_as_float(hi));
+}
+__device__ __forceinline__ void f32_mma(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(PL_THREADS, PlainShape<T, DP>::CTAS)
-paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T* __restrict__ out, float scale_log2, PagedWork wk) {
-    using S = PlainShape<T, DP>;
-    extern __shared__ __align__(16) unsigned char s_pl[];
+template <int DP>
+__global__ void __launch_bounds__(F_THREADS, F32Shape<DP>::CTAS)
+paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* __restrict__ q, float* __restrict__ out, float scale_log2, PagedWork wk) {
+    using S = F32Shape<DP>;
+    constexpr int KSTEPS = DP / 8, NT = DP / 64;                  // k steps of S; 8-column tiles of O per warp
+    extern __shared__ __align__(16) float s_f32[];
     __shared__ PagedTableMem s_tab;
-    float* s_q = reinterpret_cast<float*>(s_pl + S::STAGES * S::STAGE);   // [16][QS]
-    float* s_p = s_q + PL_ROWS * S::QS;                           // [16][64]
-    float* s_m = s_p + PL_ROWS * PAGE;                            // running maximum, sum, factor of this step
-    float* s_l = s_m + PL_ROWS;
-    float* s_a = s_l + PL_ROWS;
+    float* s_qh = s_f32 + S::STAGES * S::STAGE;                   // [16][QS]: the two parts of Q
+    float* s_ql = s_qh + F_ROWS * S::QS;
+    float* s_p = s_ql + F_ROWS * S::QS;                          // [16][PS]
+    float* s_m = s_p + F_ROWS * S::PS;                           // running maximum, sum, factor of this step
+    float* s_l = s_m + F_ROWS;
+    float* s_a = s_l + F_ROWS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = pv.d, g = pb.g;
-    const int cpr = d / S::E;
+    const int cpr = d / 4;
 
     grid_dependency_wait();
     PagedTable tab;
-    const int unit_rows = pb.top > 0 ? g : PL_ROWS;               // rows of a unit (top > 0: one token)
-    paged_build_table(tab, pb, pv.H, PL_ROWS, 1, INT_MAX, (int)gridDim.x, 2, 2, &s_tab, wk.prefix);
+    const int unit_rows = pb.top > 0 ? pb.sub_rows : F_ROWS;
+    paged_build_table<-1>(tab, pb, pv.H, F_ROWS, 1, INT_MAX, (int)gridDim.x, 2, 4, &s_tab, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;
     const long long end = tab.share(w + 1);
+    const int lrow = (lane & 7) + ((lane >> 3) & 1) * 8, lcol = (lane >> 4) * 4;      // this lane's row and column of an A fragment's ldmatrix
 
     for (long long x = tab.share(w); x < end;) {
-        const PagedItem it = paged_item(tab, pb, x, end, w);
+        const PagedItem it = paged_item<-1>(tab, pb, x, end, w);
         x += it.steps;
-        const int row_first = pb.top > 0 ? it.u * g : it.u * PL_ROWS;    // of the request's n * g rows
-        const int unit_n = min(unit_rows, it.q.n * g - row_first);
+        const int row_first = paged_unit_first<-1>(pb, it.u, F_ROWS), rows = paged_unit_rows<-1>(pb, it.u, it.q.n, F_ROWS);
         auto load_page = [&](int p) {                            // place p of the unit's pages into buffer (p - p0) % STAGES
-            T* s_k = reinterpret_cast<T*>(s_pl + (p - it.p0) % S::STAGES * S::STAGE);
-            T* s_v = s_k + PAGE * S::KS;
-            const int page = pb.top > 0 ? pb.selected[((size_t)(it.q.row0 + it.u) * pv.H + it.h) * pb.top + p] : p;
+            float* s_k = s_f32 + (p - it.p0) % S::STAGES * S::STAGE;
+            float* s_v = s_k + PAGE * S::KS;
+            const int page = pb.top > 0 ? pb.selected[((size_t)(it.q.row0 + it.tok0) * pv.H + it.h) * pb.top + p] : p;
             const int phys = paged_physical(pb, pv, it.r, page);
             const int held = phys < 0 ? 0 : it.q.len - page * PAGE;      // what lies behind the last entry is not read
             const size_t off = ((size_t)max(phys, 0) * pv.H + it.h) * PAGE * d;
-            for (int i = tid; i < PAGE * cpr; i += PL_THREADS) {
-                const int e = i / cpr, c = (i - e * cpr) * S::E;
-                plain_copy16(s_k + e * S::KS + c, reinterpret_cast<const T*>(pv.k) + off + (size_t)e * d + c, e < held);
-                plain_copy16(s_v + e * DP + c, reinterpret_cast<const T*>(pv.v) + off + (size_t)e * d + c, e < held);
+            for (int i = tid; i < PAGE * cpr; i += F_THREADS) {
+                const int e = i / cpr, c = (i - e * cpr) * 4;
+                f32_copy16(s_k + e * S::KS + c, reinterpret_cast<const float*>(pv.k) + off + (size_t)e * d + c, e < held);
+                f32_copy16(s_v + e * S::VS + c, reinterpret_cast<const float*>(pv.v) + off + (size_t)e * d + c, e < held);
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
             return phys < 0 ? INT_MAX / 2 : page * PAGE;         // first entry; of a page that does not exist: seen by no row
         };
-        for (int b0 = 0; b0 < unit_n; b0 += PL_ROWS) {           // a token with more than 16 query heads: 16 at a time
-            const int rows = min(PL_ROWS, unit_n - b0);
+        __syncthreads();                                          // the last unit's buffers and rows are done with
+        int e_next = it.p0 < it.p1 ? load_page(it.p0) : 0;
+        for (int i = tid; i < F_ROWS * cpr; i += F_THREADS) {
+            const int rr = i / cpr, c = (i - rr * cpr) * 4;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u), hi, lo;
+            if (rr < rows) {
+                const int row = row_first + rr;
+                const int qt = pb.by_g.div(row);
+                v = *reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + row - qt * g) * d + c);
+            }
+            f32_split(v.x, hi.x, lo.x); f32_split(v.y, hi.y, lo.y); f32_split(v.z, hi.z, lo.z); f32_split(v.w, hi.w, lo.w);
+            *reinterpret_cast<uint4*>(s_qh + rr * S::QS + c) = hi;
+            *reinterpret_cast<uint4*>(s_ql + rr * S::QS + c) = lo;
+        }
+        if (tid < F_ROWS) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
+        float o[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[nt][0] = o[nt][1] = o[nt][2] = o[nt][3] = 0.f;
+        // S: this thread has rows lane / 4 and + 8, keys 8 warp + 2 (lane % 4) and + 1 of a page; the entries its rows see
+        int see_hi[2], see_lo[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int rr = (lane >> 2) + 8 * i;
+            const int pos = rr < rows ? it.q.len - it.q.n + pb.by_g.div(row_first + rr) : -1;
+            see_hi[i] = pos;
+            see_lo[i] = pb.window > 0 ? pos + 1 - pb.window : 0;
+        }
+        uint32_t qh[S::Q_REG ? KSTEPS : 1][4], ql[S::Q_REG ? KSTEPS : 1][4];
+        auto load_q = [&](int ks, uint32_t (&h)[4], uint32_t (&l)[4]) {
+            const int at = lrow * S::QS + ks * 8 + lcol;
+            ldsm_x4(h, (uint32_t)__cvta_generic_to_shared(s_qh + at));
+            ldsm_x4(l, (uint32_t)__cvta_generic_to_shared(s_ql + at));
+        };
+        if (S::Q_REG) {
             __syncthreads();
-            int e_next = it.p0 < it.p1 ? load_page(it.p0) : 0;
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            for (int i = tid; i < PL_ROWS * cpr; i += PL_THREADS) {
-                const int rr = i / cpr, c = (i - rr * cpr) * S::E;
-                uint4 val = make_uint4(0u, 0u, 0u, 0u);
-                if (rr < rows) {
-                    const int row = row_first + b0 + rr;
-                    val = *reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + row / g) * pb.q_stride + (size_t)(it.h * g + row % g) * d + c);
-                }
-                const T* p = reinterpret_cast<const T*>(&val);
 #pragma unroll
-                for (int e = 0; e < S::E; ++e) s_q[rr * S::QS + c + e] = to_f32<T>(p[e]);
-            }
-            if (tid < PL_ROWS) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
-            float acc[S::RPT];
-#pragma unroll
-            for (int i = 0; i < S::RPT; ++i) acc[i] = 0.f;
-            // S: this thread's key and first row; the entries its rows see
-            const int key = warp * 8 + (lane & 7), rh = (lane >> 3) * 4;
-            int see_hi[4], see_lo[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int pos = rh + i < rows ? it.q.len - it.q.n + (row_first + b0 + rh + i) / g : -1;
-                see_hi[i] = pos;
-                see_lo[i] = pb.window > 0 ? pos + 1 - pb.window : 0;
-            }
-            const int col = tid % S::COLS, r0 = (tid / S::COLS) * S::RPT;
+            for (int ks = 0; ks < KSTEPS; ++ks)
+                if (ks * 8 < d) load_q(ks, qh[S::Q_REG ? ks : 0], ql[S::Q_REG ? ks : 0]);
+        }
 
-            for (int p = it.p0; p < it.p1; ++p) {
-                const int e0 = e_next;
-                const T* s_k = reinterpret_cast<const T*>(s_pl + (p - it.p0) % S::STAGES * S::STAGE);
-                const T* s_v = s_k + PAGE * S::KS;
-                if (S::STAGES > 1 && p + 1 < it.p1) e_next = load_page(p + 1);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (S::STAGES > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-                else asm volatile("cp.async.wait_group 0;" ::: "memory");
-                __syncthreads();
-                {
-                    float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-                    for (int c = 0; c < d; c += 4) {
-                        const float4 kk = plain_load4<T>(s_k + key * S::KS + c);
+        for (int p = it.p0; p < it.p1; ++p) {
+            const int e0 = e_next;
+            const float* s_k = s_f32 + (p - it.p0) % S::STAGES * S::STAGE;
+            const float* s_v = s_k + PAGE * S::KS;
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                      // the page is here, and the page before is done with
+            if (S::STAGES > 1 && p + 1 < it.p1) e_next = load_page(p + 1);
+            {
+                float acc[3][2][4];                               // hi hi, lo hi, hi lo; even and odd steps
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 qq = *reinterpret_cast<const float4*>(s_q + (rh + i) * S::QS + c);
-                            s[i] = fmaf(qq.x, kk.x, fmaf(qq.y, kk.y, fmaf(qq.z, kk.z, fmaf(qq.w, kk.w, s[i]))));
-                        }
-                    }
-                    const int at = e0 + key;
+                for (int i = 0; i < 24; ++i) (&acc[0][0][0])[i] = 0.f;
+                const uint32_t kaddr = (uint32_t)__cvta_generic_to_shared(s_k + (warp * 8 + (lane & 7)) * S::KS + (lane >> 3) * 4);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s_p[(rh + i) * PAGE + key] = at <= see_hi[i] && at >= see_lo[i] ? s[i] * scale_log2 : -INFINITY;
-                }
-                __syncthreads();
-                {
-                    float a[2], b[2], mx[2], sum[2], m0[2], ref[2];
+                for (int ks = 0; ks < KSTEPS; ks += 2) {
+                    if (ks * 8 >= d) break;
+                    uint32_t kb[4];                               // k 0-3, 4-7 of this step and of the next
+                    ldsm_x4(kb, kaddr + ks * 32);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int rr = warp * 2 + i;
-                        a[i] = s_p[rr * PAGE + lane];
-                        b[i] = s_p[rr * PAGE + 32 + lane];
-                        m0[i] = s_m[rr];
-                        mx[i] = fmaxf(a[i], b[i]);
-                    }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], o));
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        mx[i] = fmaxf(m0[i], mx[i]);
-                        ref[i] = mx[i] == -INFINITY ? 0.f : mx[i];       // a row that has seen nothing yet: every weight is 0
-                        a[i] = exp2f(a[i] - ref[i]);
-                        b[i] = exp2f(b[i] - ref[i]);
-                        sum[i] = a[i] + b[i];
-                        s_p[(warp * 2 + i) * PAGE + lane] = a[i];
-                        s_p[(warp * 2 + i) * PAGE + 32 + lane] = b[i];
-                    }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
-                    if (lane < 2) {
-                        const int rr = warp * 2 + lane;
-                        const float f = exp2f((lane ? m0[1] : m0[0]) - (lane ? ref[1] : ref[0]));
-                        s_a[rr] = f;
-                        s_l[rr] = s_l[rr] * f + (lane ? sum[1] : sum[0]);
-                        s_m[rr] = lane ? mx[1] : mx[0];
+                    for (int e = 0; e < 2; ++e) {
+                        if ((ks + e) * 8 >= d) break;
+                        uint32_t h0, l0, h1, l1, th[4], tl[4];
+                        f32_split(kb[2 * e], h0, l0);
+                        f32_split(kb[2 * e + 1], h1, l1);
+                        if (!S::Q_REG) load_q(ks + e, th, tl);
+                        const uint32_t* ah = S::Q_REG ? qh[S::Q_REG ? ks + e : 0] : th;
+                        const uint32_t* al = S::Q_REG ? ql[S::Q_REG ? ks + e : 0] : tl;
+                        f32_mma(acc[0][e], ah, h0, h1);
+                        f32_mma(acc[1][e], al, h0, h1);
+                        f32_mma(acc[2][e], ah, l0, l1);
                     }
                 }
-                __syncthreads();
+                const int key = warp * 8 + 2 * (lane & 3);
 #pragma unroll
-                for (int i = 0; i < S::RPT; ++i) acc[i] *= s_a[r0 + i];
-#pragma unroll 4
-                for (int e = 0; e < PAGE; e += 4) {
-                    float vv[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) vv[u] = to_f32<T>(s_v[(e + u) * DP + col]);
-#pragma unroll
-                    for (int i = 0; i < S::RPT; ++i) {
-                        const float4 pp = *reinterpret_cast<const float4*>(s_p + (r0 + i) * PAGE + e);
-                        acc[i] = fmaf(pp.x, vv[0], fmaf(pp.y, vv[1], fmaf(pp.z, vv[2], fmaf(pp.w, vv[3], acc[i]))));
-                    }
-                }
-                __syncthreads();                                  // the buffer and the weights are free
-                if (S::STAGES == 1 && p + 1 < it.p1) {
-                    e_next = load_page(p + 1);
-                    asm volatile("cp.async.commit_group;" ::: "memory");
+                for (int i = 0; i < 4; ++i) {
+                    const int at = e0 + key + (i & 1), rr = (lane >> 2) + 8 * (i >> 1);
+                    const float v = (acc[0][0][i] + acc[0][1][i]) + ((acc[1][0][i] + acc[1][1][i]) + (acc[2][0][i] + acc[2][1][i]));
+                    s_p[rr * S::PS + key + (i & 1)] = at <= see_hi[i >> 1] && at >= see_lo[i >> 1] ? v * scale_log2 : -INFINITY;
                 }
             }
             __syncthreads();
-            if (col < d) {
+            {
+                float a[2], b[2], mx[2], sum[2], m0[2], ref[2];
 #pragma unroll
-                for (int i = 0; i < S::RPT; ++i) {
-                    if (r0 + i >= rows) continue;
-                    const int row = row_first + b0 + r0 + i;
-                    const float l = s_l[r0 + i], inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-                    if (it.slot < 0) {
-                        out[((size_t)(it.q.row0 + row / g) * pb.Hq + (size_t)(it.h * g + row % g)) * d + col] = from_f32<T>(acc[i] * inv);
-                    } else {
-                        const size_t pr = (size_t)it.slot * unit_rows + b0 + r0 + i;
-                        wk.part_o[pr * d + col] = acc[i];
-                        if (col == 0) { wk.part_ml[pr * 2] = s_m[r0 + i]; wk.part_ml[pr * 2 + 1] = l; }
-                    }
+                for (int i = 0; i < 2; ++i) {
+                    const int rr = warp * 2 + i;
+                    a[i] = s_p[rr * S::PS + lane];
+                    b[i] = s_p[rr * S::PS + 32 + lane];
+                    m0[i] = s_m[rr];
+                    mx[i] = fmaxf(a[i], b[i]);
+                }
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], off));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    mx[i] = fmaxf(m0[i], mx[i]);
+                    ref[i] = mx[i] == -INFINITY ? 0.f : mx[i];           // a row that has seen nothing yet: every weight is 0
+                    a[i] = exp2f(a[i] - ref[i]);
+                    b[i] = exp2f(b[i] - ref[i]);
+                    sum[i] = a[i] + b[i];
+                    s_p[(warp * 2 + i) * S::PS + lane] = a[i];
+                    s_p[(warp * 2 + i) * S::PS + 32 + lane] = b[i];
+                }
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], off);
+                if (lane < 2) {
+                    const int rr = warp * 2 + lane;
+                    const float f = exp2f((lane ? m0[1] : m0[0]) - (lane ? ref[1] : ref[0]));
+                    s_a[rr] = f;
+                    s_l[rr] = s_l[rr] * f + (lane ? sum[1] : sum[0]);
+                    s_m[rr] = lane ? mx[1] : mx[0];
                 }
             }
+            __syncthreads();
+            {
+                float acc[NT][3][4];
+#pragma unroll
+                for (int i = 0; i < NT * 12; ++i) (&acc[0][0][0])[i] = 0.f;
+                const uint32_t paddr = (uint32_t)__cvta_generic_to_shared(s_p + lrow * S::PS + lcol);
+                const float* vb = s_v + (lane & 3) * S::VS + warp * (DP / 8) + (lane >> 2);
+#pragma unroll
+                for (int ks = 0; ks < PAGE / 8; ++ks) {
+                    uint32_t pr[4], ph[4], pl[4];
+                    ldsm_x4(pr, paddr + ks * 32);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f32_split(pr[i], ph[i], pl[i]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        uint32_t h0, l0, h1, l1;
+                        f32_split(__float_as_uint(vb[ks * 8 * S::VS + nt * 8]), h0, l0);
+                        f32_split(__float_as_uint(vb[(ks * 8 + 4) * S::VS + nt * 8]), h1, l1);
+                        f32_mma(acc[nt][0], ph, h0, h1);
+                        f32_mma(acc[nt][1], pl, h0, h1);
+                        f32_mma(acc[nt][2], ph, l0, l1);
+                    }
+                }
+                const float f0 = s_a[lane >> 2], f1 = s_a[(lane >> 2) + 8];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nt][i] = fmaf(o[nt][i], i < 2 ? f0 : f1, acc[nt][0][i] + (acc[nt][1][i] + acc[nt][2][i]));
+            }
+            if (S::STAGES == 1 && p + 1 < it.p1) {
+                __syncthreads();                                  // the only buffer is free
+                e_next = load_page(p + 1);
+            }
+        }
+        __syncthreads();                                          // the last sums are written
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int rr = (lane >> 2) + 8 * i;
+            if (rr >= rows) continue;
+            const int row = row_first + rr, qt = pb.by_g.div(row);
+            const float l = s_l[rr], inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+            float* op = out + ((size_t)(it.q.row0 + qt) * pb.Hq + (size_t)(it.h * g + row - qt * g)) * d;
+            const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * unit_rows + rr;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int col = warp * (DP / 8) + nt * 8 + 2 * (lane & 3);
+                if (col >= d) continue;
+                if (it.slot < 0) *reinterpret_cast<float2*>(op + col) = make_float2(o[nt][2 * i] * inv, o[nt][2 * i + 1] * inv);
+                else *reinterpret_cast<float2*>(wk.part_o + pr * d + col) = make_float2(o[nt][2 * i], o[nt][2 * i + 1]);
+            }
+            if (it.slot >= 0 && warp == 0 && (lane & 3) == 0) { wk.part_ml[pr * 2] = s_m[rr]; wk.part_ml[pr * 2 + 1] = l; }
         }
     }
 }
@@ -225,26 +272,26 @@ paged_attn_plain_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, T*
 // in worker order, so the result does not depend on timing.  SPLIT warps per row (units with many parts, few rows in all)
 // or SPLIT = 1: a warp walks all g rows of its (token, KV head).  Bound by latency: the request is found by a warp-wide
 // search before the wait for the kernel that wrote the partials.
-template <typename T, int SPLIT>
+template <typename T, int SPLIT, int SEL>
 __global__ void __launch_bounds__(128)
 paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk, int tile_rows, int min_rows, int max_rows) {
     __shared__ float4 s_sum[SPLIT > 1 ? SPLIT : 1][64];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = pv.d, g = pb.g;
-    const long long item = SPLIT > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 4 + warp;
-    const int heads = SPLIT > 1 ? pb.Hq : pv.H;
-    const int t = (int)(item / heads), rest = (int)(item % heads);
-    const int h = SPLIT > 1 ? rest / g : rest;
+    // (n_tokens x q_heads <= 2^30)
+    const int item = SPLIT > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + warp;
+    const int t = SPLIT > 1 ? pb.by_hq.div(item) : pb.by_h.div(item), rest = item - t * (SPLIT > 1 ? pb.Hq : pv.H);
+    const int h = SPLIT > 1 ? pb.by_g.div(rest) : rest;
     // cu_new and lens are older than the kernel before this one, which has waited for them
     PagedReq rq;
     const int r = paged_find_request(pb, min(t, pb.T - 1), rq);
     const int j = t - rq.row0;
-    const PagedCost c = paged_cost(pb, rq, tile_rows, min_rows, max_rows);
+    const PagedCost c = paged_cost<SEL>(pb, rq, tile_rows, min_rows, max_rows);
     grid_dependents_may_launch();
     grid_dependency_wait();
     const int workers = (int)wk.prefix[pb.R + 1];                 // 0: the workers had whole units
     if (workers == 0 || t >= pb.T || j < 0 || j >= rq.n || c.U == 0) return;      // (U = 0: another kernel's request)
     const long long total = wk.prefix[pb.R], before = wk.prefix[r];
-    const int unit_rows = pb.top > 0 ? g : tile_rows;
+    const int unit_rows = SEL ? pb.sub_rows : tile_rows, tile_shift = __ffs(tile_rows) - 1;      // tile_rows: a power of two
     int u_now = -1, w0 = 0, n = 0;
     auto locate = [&](int u) {                                    // the unit's first worker and number of parts
         if (u == u_now) return;
@@ -253,9 +300,9 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
         n = paged_owner(total, workers, a + c.C - 1) - w0 + 1;
         u_now = u;
     };
-    if (SPLIT == 1 && pb.top == 0 && (j * g) / tile_rows == (j * g + g - 1) / tile_rows) {
+    if (SPLIT == 1 && !SEL && (j * g) >> tile_shift == (j * g + g - 1) >> tile_shift) {
         // the rows of one unit, in few parts: half a warp per row and every load of the row in flight at once
-        locate(j * g / tile_rows);
+        locate((j * g) >> tile_shift);
         if (n == 1) return;
         if (n <= 4) {
             const int l16 = lane & 15;
@@ -300,8 +347,9 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
             return;
         }
     }
-    for (int jj = SPLIT > 1 ? rest % g : 0; jj < g; ++jj) {
-        const int row = j * g + jj, u = pb.top > 0 ? j : row / tile_rows, rr = row - u * unit_rows;
+    for (int jj = SPLIT > 1 ? rest - h * g : 0; jj < g; ++jj) {
+        const int row = j * g + jj, block = SEL ? pb.by_sub_rows.div(jj) : 0;
+        const int u = SEL ? j * pb.sub + block : row >> tile_shift, rr = SEL ? jj - block * pb.sub_rows : row - u * tile_rows;
         locate(u);
         if (n > 1) {
             // i-th part: worker w0 began the unit and did not end it (its slot 2 w + 1), the others did not begin it
@@ -368,24 +416,16 @@ paged_join_kernel(PagedView pv, PagedBatch pb, T* __restrict__ out, PagedWork wk
     }
 }
 
-template <typename T, int DP>
-cudaError_t run_plain(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                      cudaStream_t st) {
-    using S = PlainShape<T, DP>;
+template <int DP>
+cudaError_t run_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, cudaStream_t st) {
+    using S = F32Shape<DP>;
+    static_assert(S::CTAS <= PAGED_F32_CTAS, "the workspace holds the workers' partial results");
+    static_assert((S::SMEM + (int)sizeof(PagedTableMem) + 1024) * S::CTAS <= 228 * 1024, "shared memory of one SM");
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_plain_kernel<T, DP>), S::SMEM, done);
+    const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_f32_kernel<DP>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    static_assert(S::CTAS <= PAGED_PLAIN_CTAS, "the workspace holds the workers' partial results");
-    return paged_launch(paged_attn_plain_kernel<T, DP>, dim3(PAGED_SMS * S::CTAS), dim3(PL_THREADS), S::SMEM, 1, true, st, pv, pb, (const T*)q, (T*)out,
+    return paged_launch(paged_attn_f32_kernel<DP>, dim3(PAGED_SMS * S::CTAS), dim3(F_THREADS), S::SMEM, 1, true, st, pv, pb, (const float*)q, (float*)out,
                         scale * LOG2E, w);
-}
-
-template <typename T>
-cudaError_t run_plain_d(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
-                        cudaStream_t st) {
-    if (pv.d <= 64) return run_plain<T, 64>(pv, pb, q, out, scale, w, st);
-    if (pv.d <= 128) return run_plain<T, 128>(pv, pb, q, out, scale, w, st);
-    return run_plain<T, 256>(pv, pb, q, out, scale, w, st);
 }
 
 }  // namespace
@@ -398,15 +438,20 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
     const long long items = (long long)pb.T * (split ? pb.Hq : pv.H);
     const dim3 grid((unsigned)(split ? items : (items + 3) / 4)), block(128);
     auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, 0, 1, true, st, pv, pb, o, w, tile_rows, min_rows, max_rows); };
-    if (is_bf16) return split ? go(paged_join_kernel<__nv_bfloat16, 4>, (__nv_bfloat16*)out) : go(paged_join_kernel<__nv_bfloat16, 1>, (__nv_bfloat16*)out);
-    return split ? go(paged_join_kernel<float, 4>, (float*)out) : go(paged_join_kernel<float, 1>, (float*)out);
+    auto typed = [&](auto* o) {
+        using T = std::remove_pointer_t<decltype(o)>;
+        if (pb.top > 0) return split ? go(paged_join_kernel<T, 4, 1>, o) : go(paged_join_kernel<T, 1, 1>, o);
+        return split ? go(paged_join_kernel<T, 4, 0>, o) : go(paged_join_kernel<T, 1, 0>, o);
+    };
+    return is_bf16 ? typed((__nv_bfloat16*)out) : typed((float*)out);
 }
 
-cudaError_t launch_paged_attention_plain(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, void* out,
-                                         float scale, const PagedWork& w, cudaStream_t st) {
-    const cudaError_t e = is_bf16 ? run_plain_d<__nv_bfloat16>(pv, pb, q, out, scale, w, st)
-                                  : run_plain_d<float>(pv, pb, q, out, scale, w, st);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, is_bf16, out, w, PL_ROWS, 1, INT_MAX, st);
+cudaError_t launch_paged_attention_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
+                                       cudaStream_t st) {
+    const cudaError_t e = pv.d <= 64    ? run_f32<64>(pv, pb, q, out, scale, w, st)
+                          : pv.d <= 128 ? run_f32<128>(pv, pb, q, out, scale, w, st)
+                                        : run_f32<256>(pv, pb, q, out, scale, w, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 0, out, w, F_ROWS, 1, INT_MAX, st);
 }
 
 }  // namespace tkv

@@ -1,4 +1,5 @@
-// Attention over the caller-owned paged cache for many query rows, on tcgen05: bf16, head size 64 or 128.
+// Attention over the caller-owned paged cache for many query rows, on tcgen05: bf16, head sizes up to 128 (padded to 64 or 128 in
+// shared memory, the missing columns zero).
 //
 // A unit is 256 (token, query head) rows of one KV head in two groups of 128 that share every K/V tile; a tile is two pages
 // (128 entries; the last of a stretch may be one).  One persistent CTA per SM takes an equal share of the line of page steps
@@ -126,7 +127,8 @@ __device__ __forceinline__ bool t_pair_sync(uint32_t bar, unsigned n) {
     return __all_sync(0xffffffffu, a_bar_wait(bar, n & 1u));
 }
 
-template <int D, bool PICK>
+// EXACT: the head size is D; otherwise smaller, and the columns from pv.d on are zeros in shared memory.
+template <int D, bool PICK, bool EXACT>
 __global__ void __launch_bounds__(T_THREADS, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
                      const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int min_rows) {
@@ -147,7 +149,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(gen + S::OFF_TAB);
     uint32_t* s_bits = reinterpret_cast<uint32_t*>(gen + S::OFF_BITS);
     uint16_t* s_list = reinterpret_cast<uint16_t*>(gen + S::OFF_LIST);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = EXACT ? D : pv.d;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -168,7 +170,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem, wk.prefix);
+    paged_build_table<0>(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem, wk.prefix);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
@@ -191,13 +193,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     unsigned ex = 0;                                                  // barriers of the two warps of a row so far
     bool careful = false;                                             // this stretch again, every tile's maximum first
     for (long long x = tab.share(w); x < end;) {
-        const PagedItem it = paged_item(tab, pb, x, end, w);
+        const PagedItem it = paged_item<0>(tab, pb, x, end, w);
         int npage = it.p1 - it.p0;
         const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
         const bool both = rows > T_ROWS;
         const bool soft = warp < T_SOFT && (grp == 0 || both);
         const bool valid = soft && R < rows;
-        const int tok = valid ? (row_first + R) / g : it.tok0, head = valid ? (row_first + R) % g : 0;
+        const int tok = valid ? pb.by_g.div(row_first + R) : it.tok0, head = valid ? row_first + R - tok * g : 0;
         const int pos = it.q.len - it.q.n + tok;
         const int see_hi = valid ? max(pos + 1, 0) : 0;               // entries the row sees: see_lo .. see_hi - 1
         const int see_lo = valid && pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
@@ -245,12 +247,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const int ntile = (npage + 1) / 2;
         if (ntile > 0) {
             if (soft) {
-                const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + tok) * pb.q_stride + (size_t)(it.h * g + head) * D);
+                const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + tok) * pb.q_stride + (size_t)(it.h * g + head) * d);
                 unsigned char* qdst = gen + S::OFF_Q + grp * S::PLANES * T_QPLANE + r * 128;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const int c = half * (D / 16) + k;
-                    const uint4 v = valid ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 v = valid && c * 8 < d ? src[c] : make_uint4(0u, 0u, 0u, 0u);
                     *reinterpret_cast<uint4*>(qdst + (c >> 3) * T_QPLANE + (((c & 7) ^ (r & 7)) << 4)) = v;
                 }
             }
@@ -262,6 +264,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             if (warp == T_SOFT) {
                 // ---- TMA producer: lane l holds page l of the current run of 32
                 int page = 0, phys = 0;
+                auto copy = [&](uint32_t dst, const CUtensorMap* map, int plane, int row, uint32_t bar) {    // a page's plane
+                    if (EXACT || d % 64 == 0) a_tma_3d(dst, map, 0, row, plane, bar);
+                    else a_tma_2d(dst, map, plane * 64, row, bar);    // the last plane's missing columns arrive as zeros
+                };
                 for (int i = 0; i < ntile; ++i) {
                     if ((i & 15) == 0) {
                         const int e = 2 * i + lane;
@@ -285,14 +291,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                             a_bar_expect_tx(k_full + 8 * s, two ? S::TILE : S::TILE / 2);
 #pragma unroll
                             for (int p = 0; p < S::PLANES; ++p) {
-                                a_tma_3d(kd + p * S::KPLANE, &map_k, 0, row0, p, k_full + 8 * s);
-                                if (two) a_tma_3d(kd + p * S::KPLANE + T_PLANE, &map_k, 0, row1, p, k_full + 8 * s);
+                                copy(kd + p * S::KPLANE, &map_k, p, row0, k_full + 8 * s);
+                                if (two) copy(kd + p * S::KPLANE + T_PLANE, &map_k, p, row1, k_full + 8 * s);
                             }
                             if (c >= T_STAGES) ok = a_bar_wait(v_empty + 8 * s, ((c / T_STAGES) - 1) & 1) ? 1 : 0;
                             if (ok) {
                                 a_bar_expect_tx(v_full + 8 * s, two ? S::TILE : S::TILE / 2);
-                                a_tma_3d(vd, &map_v, 0, row0, 0, v_full + 8 * s);
-                                if (two) a_tma_3d(vd + S::PLANES * T_PLANE, &map_v, 0, row1, 0, v_full + 8 * s);
+#pragma unroll
+                                for (int p = 0; p < S::PLANES; ++p) {
+                                    copy(vd + p * T_PLANE, &map_v, p, row0, v_full + 8 * s);
+                                    if (two) copy(vd + (S::PLANES + p) * T_PLANE, &map_v, p, row1, v_full + 8 * s);
+                                }
                             }
                         }
                     }
@@ -519,9 +528,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 l += mx_other[2 * MX];
                 if (m_used == -INFINITY && !(l != l)) l = 0.f;        // a row that sees nothing (the polynomial gives masked entries 2^-125)
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-                uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * D + half * (D / 2));
+                uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * d + half * (D / 2));
                 const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
-                float4* po = reinterpret_cast<float4*>(wk.part_o + pr * D + half * (D / 2));
+                float4* po = reinterpret_cast<float4*>(wk.part_o + pr * d + half * (D / 2));
                 const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
 #pragma unroll 1
                 for (int k = 0; k < D / 32; ++k) {
@@ -540,12 +549,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
 #pragma unroll
                             for (int k2 = 0; k2 < 4; ++k2)
                                 v[k2] = a_bf16x2(__uint_as_float(ov[e + 2 * k2]) * inv, __uint_as_float(ov[e + 2 * k2 + 1]) * inv);
-                            op[k * 2 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
+                            if (half * (D / 2) + k * 16 + e < d) op[k * 2 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
                         }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; e += 4)
-                            po[k * 4 + (e >> 2)] = make_float4(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1]), __uint_as_float(ov[e + 2]), __uint_as_float(ov[e + 3]));
+                            if (half * (D / 2) + k * 16 + e < d) po[k * 4 + (e >> 2)] = make_float4(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1]), __uint_as_float(ov[e + 2]), __uint_as_float(ov[e + 3]));
                     }
                 }
                 if (valid && it.slot >= 0 && half == 0) {
@@ -573,18 +582,18 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     if (threadIdx.x == 0 && *s_fail) latch_error(pb.status, TRIMKV_E_TIMEOUT);
 }
 
-template <int D, bool PICK>
+template <int D, bool PICK, bool EXACT>
 cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int min_rows, cudaStream_t st) {
     using S = TcShape<D, PICK>;
     static_assert(S::SMEM <= 227 * 1024, "shared memory of one SM");
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_tc_kernel<D, PICK>), S::SMEM, done);
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_tc_kernel<D, PICK, EXACT>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    e = paged_tensor_map(&mk, pv.k, pv, PAGE, 1);                     // K plane by plane: a tile's plane holds the rows of two pages
-    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, PAGE, pv.d / 64);
+    e = paged_tensor_map(&mk, pv.k, pv, PAGE, 1);                     // plane by plane: a tile's plane of K holds the rows of two pages
+    if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, PAGE, 1);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged_attn_tc_kernel<D, PICK>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
+    e = paged_launch(paged_attn_tc_kernel<D, PICK, EXACT>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
                      (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, st);
 }
@@ -593,8 +602,15 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
 
 cudaError_t launch_paged_attention_tc(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                       int min_rows, cudaStream_t st) {
-    if (pb.pick > 0) return pv.d == 64 ? run_tc<64, true>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<128, true>(pv, pb, q, out, scale, w, min_rows, st);
-    return pv.d == 64 ? run_tc<64, false>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<128, false>(pv, pb, q, out, scale, w, min_rows, st);
+    auto go = [&](auto d, auto pick) {
+        constexpr int D = decltype(d)::value;
+        constexpr bool PICK = decltype(pick)::value;
+        return pv.d == D ? run_tc<D, PICK, true>(pv, pb, q, out, scale, w, min_rows, st) : run_tc<D, PICK, false>(pv, pb, q, out, scale, w, min_rows, st);
+    };
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (pb.pick > 0) return pv.d <= 64 ? go(D64{}, std::true_type{}) : go(D128{}, std::true_type{});
+    return pv.d <= 64 ? go(D64{}, std::false_type{}) : go(D128{}, std::false_type{});
 }
 
 }  // namespace tkv

@@ -1,4 +1,5 @@
-// Attention over the caller-owned paged cache for few query rows: bf16, head size 64 or 128.
+// Attention over the caller-owned paged cache for few query rows: bf16, head sizes up to 256 (padded to 64, 128 or 256 in shared
+// memory, the missing columns zero).
 //
 // A decode step does 2 g flops per byte of K and V, far below the machine's balance, so the kernel is a stream from HBM:
 // one CTA per SM, four independent warps, each with a ring of its own (48 KB) that TMA fills 32 entries at a time, one
@@ -28,12 +29,12 @@ template <int D, int NT, int TW>
 struct WarpShape {
     static constexpr int TEAMS = TW == 1 ? PAGED_WARPS : 2;
     static constexpr int ROWS = NT * 8 * TW;                          // rows of a unit
-    static constexpr int TILE = TW == 1 ? 32 : 64;                    // entries per stage
+    static constexpr int TILE = (TW == 1 ? 32 : 64) / (D == 256 ? 2 : 1);       // entries per stage
     static constexpr int PER_PAGE = PAGE / TILE;
     static constexpr int PLANE = TILE * 128;                          // entries x 64 columns
     static constexpr int PLANES = D / 64;
     static constexpr int STAGE = 2 * PLANES * PLANE;                  // K planes, V planes
-    static constexpr int STAGES = 192 * 1024 / TEAMS / STAGE;         // d = 128: 3; d = 64: 6
+    static constexpr int STAGES = 192 * 1024 / TEAMS / STAGE;         // 3; d = 64: 6
     static constexpr int LAG = TW == 1 ? 0 : 1;                       // tiles that the rest of a team may be behind a refill
     static constexpr int RING = STAGES * STAGE;
     static constexpr int OFF_BAR = TEAMS * RING;                      // full and empty barrier of each stage
@@ -50,7 +51,8 @@ struct WarpCursor {
     bool on;
 };
 
-template <int D, int NT, int TW, bool SELECT>
+// EXACT: the head size is D; otherwise smaller, and the columns from pv.d on are zeros in shared memory.
+template <int D, int NT, int TW, bool SELECT, bool EXACT>
 __global__ void __launch_bounds__(WarpShape<D, NT, TW>::TEAMS * TW * 32, 1)
 paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
                        const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int max_rows) {
@@ -65,7 +67,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     uint64_t* empty = bars + S::STAGES;
     volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + team * S::STAGES;      // first entry of the stage's tile; -1: skip
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
-    const int unit_rows = SELECT ? g : S::ROWS;
+    const int unit_rows = SELECT ? pb.sub_rows : S::ROWS, d = EXACT ? D : pv.d;
 
     if (lane == 0 && tw == 0)
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(bars + s, 1); mbar_init(empty + s, TW); }
@@ -73,7 +75,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem, wk.prefix);      // (synchronises the block)
+    paged_build_table<SELECT>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem, wk.prefix);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
     const int w = team * (int)gridDim.x + (int)blockIdx.x;
@@ -86,13 +88,13 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         c.ntile = 0;
         c.on = x < end;
         if (!c.on) return c;
-        c.it = paged_item(tab, pb, x, end, w);
+        c.it = paged_item<SELECT>(tab, pb, x, end, w);
         c.ntile = S::PER_PAGE * (c.it.p1 - c.it.p0);
-        // the page of the unit's last token: its second half may lie behind what is seen
-        if (S::PER_PAGE == 2 && c.ntile) {
+        // the page of the unit's last token: its last tiles may lie behind what is seen
+        if (S::PER_PAGE > 1 && c.ntile) {
             const int phi = c.it.q.len - c.it.q.n + c.it.tok1, np = phi / PAGE + 1;
             const bool last = SELECT ? c.it.p1 == min(pb.top, np) : c.it.p1 == np;
-            if (last && phi % PAGE < S::TILE) --c.ntile;
+            if (last) c.ntile -= S::PER_PAGE - 1 - phi % PAGE / S::TILE;
         }
         return c;
     };
@@ -107,7 +109,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         if (prod_tile % (32 * S::PER_PAGE) == 0) {                    // the next 32 pages
             const int p = prod.it.p0 + prod_tile / S::PER_PAGE + lane;
             log_page = -1;
-            if (p < prod.it.p1) log_page = SELECT ? pb.selected[((size_t)(prod.it.q.row0 + prod.it.u) * pv.H + prod.it.h) * pb.top + p] : p;
+            if (p < prod.it.p1) log_page = SELECT ? pb.selected[((size_t)(prod.it.q.row0 + prod.it.tok0) * pv.H + prod.it.h) * pb.top + p] : p;
             phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, log_page) : -1;
         }
         const int src = (prod_tile / S::PER_PAGE) & 31, half = prod_tile % S::PER_PAGE;
@@ -122,8 +124,16 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 const uint32_t dst = smem_u32(ring + s * S::STAGE), bar = smem_u32(bars + s);
                 const int row = (pp * pv.H + prod.it.h) * PAGE + half * S::TILE;
                 mbar_expect_tx(bars + s, S::STAGE);                   // (the zeroing of rows below carries its own proxy fence)
-                a_tma_3d(dst, &map_k, 0, row, 0, bar);
-                a_tma_3d(dst + S::PLANES * S::PLANE, &map_v, 0, row, 0, bar);
+                if (EXACT || d % 64 == 0) {
+                    a_tma_3d(dst, &map_k, 0, row, 0, bar);
+                    a_tma_3d(dst + S::PLANES * S::PLANE, &map_v, 0, row, 0, bar);
+                } else {                                              // the last plane's missing columns arrive as zeros
+#pragma unroll
+                    for (int p = 0; p < S::PLANES; ++p) {
+                        a_tma_2d(dst + p * S::PLANE, &map_k, p * 64, row, bar);
+                        a_tma_2d(dst + (S::PLANES + p) * S::PLANE, &map_v, p * 64, row, bar);
+                    }
+                }
             }
         }
         ++issued;
@@ -138,8 +148,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 
     while (cons.on && !failed) {
         const PagedItem& it = cons.it;
-        const int unit_first = SELECT ? it.u * g : it.u * S::ROWS;
-        const int unit_n = min(unit_rows, it.q.n * g - unit_first);
+        const int unit_first = paged_unit_first<SELECT>(pb, it.u, S::ROWS), unit_n = paged_unit_rows<SELECT>(pb, it.u, it.q.n, S::ROWS);
         const int row_first = unit_first + tw * NT * 8;               // this warp's rows
         const int rows = max(0, min(NT * 8, unit_n - tw * NT * 8));
         // ---- Q fragments (B operand: k = channel, n = row)
@@ -148,11 +157,12 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         for (int nt = 0; nt < NT; ++nt) {
             const int row = nt * 8 + (lane >> 2);
             const int qr = row_first + row;
-            const __nv_bfloat16* p = q + (size_t)(it.q.row0 + (row < rows ? qr / g : 0)) * pb.q_stride + (size_t)(it.h * g + (row < rows ? qr % g : 0)) * D + 2 * (lane & 3);
+            const int qt = row < rows ? pb.by_g.div(qr) : 0, qj = row < rows ? qr - qt * g : 0;
+            const __nv_bfloat16* p = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + 2 * (lane & 3);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                bq[nt][ks][0] = row < rows ? *reinterpret_cast<const uint32_t*>(p + ks * 16) : 0u;
-                bq[nt][ks][1] = row < rows ? *reinterpret_cast<const uint32_t*>(p + ks * 16 + 8) : 0u;
+                bq[nt][ks][0] = row < rows && ks * 16 < d ? *reinterpret_cast<const uint32_t*>(p + ks * 16) : 0u;
+                bq[nt][ks][1] = row < rows && ks * 16 + 8 < d ? *reinterpret_cast<const uint32_t*>(p + ks * 16 + 8) : 0u;
                 o[nt][ks][0] = o[nt][ks][1] = o[nt][ks][2] = o[nt][ks][3] = 0.f;
             }
 #pragma unroll
@@ -162,7 +172,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             }
         }
         {                                                             // from the warp's first and last row
-            const int p0 = it.q.len - it.q.n + row_first / g, p1 = it.q.len - it.q.n + (row_first + rows - 1) / g;
+            const int p0 = it.q.len - it.q.n + pb.by_g.div(row_first), p1 = it.q.len - it.q.n + pb.by_g.div(max(row_first + rows - 1, 0));
             all_hi = max(p0 + 1, 0);
             all_lo = pb.window > 0 ? max(p1 + 1 - pb.window, 0) : 0;
         }
@@ -218,7 +228,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int col = nt * 8 + 2 * (lane & 3) + c;
-                        const int pos = col < rows ? it.q.len - it.q.n + (row_first + col) / g : -1;
+                        const int pos = col < rows ? it.q.len - it.q.n + pb.by_g.div(row_first + col) : -1;
                         const int lo = pb.window > 0 ? pos + 1 - pb.window : 0;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -303,18 +313,21 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 const int dr = lane >> 2;
                 if (it.slot < 0) {
                     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-                    const int qr = row_first + col;
-                    __nv_bfloat16* op = out + ((size_t)(it.q.row0 + qr / g) * pb.Hq + (size_t)(it.h * g + qr % g)) * D + dr;
+                    const int qt = pb.by_g.div(row_first + col), qj = row_first + col - qt * g;
+                    __nv_bfloat16* op = out + ((size_t)(it.q.row0 + qt) * pb.Hq + (size_t)(it.h * g + qj)) * d + dr;
 #pragma unroll
                     for (int dt = 0; dt < KS; ++dt) {
-                        op[dt * 16] = __float2bfloat16_rn(o[nt][dt][c] * inv);
-                        op[dt * 16 + 8] = __float2bfloat16_rn(o[nt][dt][c + 2] * inv);
+                        if (dt * 16 < d) op[dt * 16] = __float2bfloat16_rn(o[nt][dt][c] * inv);
+                        if (dt * 16 + 8 < d) op[dt * 16 + 8] = __float2bfloat16_rn(o[nt][dt][c + 2] * inv);
                     }
                 } else {
                     const size_t pr = (size_t)it.slot * unit_rows + tw * NT * 8 + col;
-                    float* op = wk.part_o + pr * D + dr;
+                    float* op = wk.part_o + pr * d + dr;
 #pragma unroll
-                    for (int dt = 0; dt < KS; ++dt) { op[dt * 16] = o[nt][dt][c]; op[dt * 16 + 8] = o[nt][dt][c + 2]; }
+                    for (int dt = 0; dt < KS; ++dt) {
+                        if (dt * 16 < d) op[dt * 16] = o[nt][dt][c];
+                        if (dt * 16 + 8 < d) op[dt * 16 + 8] = o[nt][dt][c + 2];
+                    }
                     if (dr == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
                 }
             }
@@ -330,34 +343,37 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     }
 }
 
-template <int D, int NT, int TW, bool SELECT>
+template <int D, int NT, int TW, bool SELECT, bool EXACT>
 cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows,
                      cudaStream_t st) {
     using S = WarpShape<D, NT, TW>;
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT>), S::SMEM, done);
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_attn_warp_kernel<D, NT, TW, SELECT, EXACT>), S::SMEM, done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
     e = paged_tensor_map(&mk, pv.k, pv, S::TILE, S::PLANES);
     if (e == cudaSuccess) e = paged_tensor_map(&mv, pv.v, pv, S::TILE, S::PLANES);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
+    e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT, EXACT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
                      (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
     return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, st);
 }
 
 }  // namespace
 
-// The pages as n_pages x H x 64 rows of d bf16, their columns cut into planes of 64: dimensions {64, rows, d / 64}; a box is
-// box_rows rows of box_planes planes, each plane 128-byte swizzled, plane after plane.
+// The pages as n_pages x H x 64 rows of d bf16.  d a multiple of 64: columns cut into planes of 64, dimensions {64, rows, d / 64}; a
+// box is box_rows rows of box_planes planes, each plane 128-byte swizzled, plane after plane.  Otherwise: dimensions {d, rows}, a
+// box is 64 columns (those behind d are filled with zeros) of box_rows rows.
 cudaError_t paged_tensor_map(CUtensorMap* map, const char* base, const PagedView& pv, int box_rows, int box_planes) {
     EncodeTiledFnA fn = a_encode_fn();
     if (!fn) return cudaErrorNotSupported;
-    const cuuint64_t dims[3] = {64, (cuuint64_t)pv.n_pages * pv.H * PAGE, (cuuint64_t)pv.d / 64};
-    const cuuint64_t strides[2] = {(cuuint64_t)pv.d * 2, 128};
+    const cuuint64_t rows = (cuuint64_t)pv.n_pages * pv.H * PAGE, row_bytes = (cuuint64_t)pv.d * 2;
+    const bool planes = pv.d % 64 == 0;
+    const cuuint64_t dims[3] = {planes ? 64 : (cuuint64_t)pv.d, rows, (cuuint64_t)pv.d / 64};
+    const cuuint64_t strides[2] = {row_bytes, 128};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_planes};
     const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, planes ? 3 : 2, const_cast<char*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
                ? cudaSuccess : cudaErrorInvalidValue;
 }
@@ -366,8 +382,11 @@ cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& p
                                         int tile_rows, int max_rows, cudaStream_t st) {
     auto go = [&](auto d, auto nt, auto tw) {
         constexpr int D = decltype(d)::value, NT = decltype(nt)::value, TW = decltype(tw)::value;
-        return pb.top > 0 ? run_warp<D, NT, TW, true>(pv, pb, q, out, scale, w, max_rows, st)
-                          : run_warp<D, NT, TW, false>(pv, pb, q, out, scale, w, max_rows, st);
+        if (pv.d == D)
+            return pb.top > 0 ? run_warp<D, NT, TW, true, true>(pv, pb, q, out, scale, w, max_rows, st)
+                              : run_warp<D, NT, TW, false, true>(pv, pb, q, out, scale, w, max_rows, st);
+        return pb.top > 0 ? run_warp<D, NT, TW, true, false>(pv, pb, q, out, scale, w, max_rows, st)
+                          : run_warp<D, NT, TW, false, false>(pv, pb, q, out, scale, w, max_rows, st);
     };
     auto rows = [&](auto d) {
         using One = std::integral_constant<int, 1>;
@@ -375,7 +394,12 @@ cudaError_t launch_paged_attention_warp(const PagedView& pv, const PagedBatch& p
         using Four = std::integral_constant<int, 4>;
         return tile_rows <= 8 ? go(d, One{}, One{}) : tile_rows <= 16 ? go(d, Two{}, One{}) : tile_rows <= 32 ? go(d, One{}, Four{}) : go(d, Two{}, Four{});
     };
-    return pv.d == 64 ? rows(std::integral_constant<int, 64>{}) : rows(std::integral_constant<int, 128>{});
+    if (pv.d <= 64) return rows(std::integral_constant<int, 64>{});
+    if (pv.d <= 128) return rows(std::integral_constant<int, 128>{});
+    // the accumulators of 16 rows of 256 do not fit the registers of a warp: 8 rows, or a team's 32
+    using D256 = std::integral_constant<int, 256>;
+    return tile_rows <= 8 ? go(D256{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
+                          : go(D256{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
 }
 
 }  // namespace tkv
