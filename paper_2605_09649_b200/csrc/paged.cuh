@@ -18,13 +18,14 @@ namespace tkv {
 
 // Opts the kernel in to `bytes` of dynamic shared memory on the current device, once per device.  The bit is set after the
 // call has succeeded, so a thread that finds it set may launch; two threads that race both make the call.
-inline cudaError_t paged_allow_smem(const void* kernel, int bytes, std::atomic<unsigned long long>& done) {
+inline cudaError_t paged_allow_smem(const void* kernel, int bytes, std::atomic<unsigned long long>& done, bool wide_cluster = false) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
     if (bit & done.load(std::memory_order_acquire)) return cudaSuccess;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && wide_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
     return e;
 }

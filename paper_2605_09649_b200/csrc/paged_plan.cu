@@ -3,10 +3,11 @@
 // Plan.  Request r goes from ceil(old / 64) to ceil(new / 64) pages; tokens keep .. new - 1 are the call's new ones.  Pages
 // given back are pushed on the free stack in (request, page) order, then the missing ones are popped in (request, page)
 // order, so the result is a pure function of the inputs: three prefix sums over the requests (tokens, pages taken, pages
-// given back) place everything.  One cluster of 8 CTAs does it in one launch: every CTA computes the sums for itself from
+// given back) place everything.  One cluster of 16 CTAs does it in one launch: every CTA computes the sums for itself from
 // shared memory (3 x R words), the cluster barrier separates the last read of an input from the first write (inputs and
-// outputs may be the same arrays), and the output is dealt out over all 8192 threads.  Bound by latency: at 64 requests
-// the kernel moves 22 KB.
+// outputs may be the same arrays), and the output is dealt out over all 16384 threads.  Bound by latency: 7.3 us for 64
+// requests with one token each (22 KB), whatever the cluster's size; 11.3 us for 256 requests of up to 1024 new tokens (1.6 MB),
+// where clusters of 1, 2, 4 and 8 CTAs take 96, 50, 28 and 17 us: each token costs its search in shared memory.
 //
 // Append.  A copy of k and v rows to their slots, 16 bytes per thread and step, bound by HBM; the grid's second half looks
 // for tokens that complete a page (slot % 64 = 63) and reduces the page's 64 keys to its channelwise bounds.  Rows of
@@ -24,7 +25,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int PLAN_CTAS = 8, PLAN_THREADS = 1024;
+constexpr int PLAN_CTAS = 16, PLAN_THREADS = 1024;
 
 // Last r with at[r] <= x (at ascending, at[0] = 0, x < at[n]).  Empty requests are passed over: their successor has the
 // same offset.
@@ -338,10 +339,10 @@ cudaError_t launch_paged_plan(int R, const int32_t* old_lens, const int32_t* kee
     const size_t smem = ((size_t)6 * R + 3) * sizeof(int);
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_plan_kernel),
-                                           (int)(((size_t)6 * PAGED_MAX_REQ + 3) * sizeof(int)), done);
+                                           (int)(((size_t)6 * PAGED_MAX_REQ + 3) * sizeof(int)), done, true);
     if (e != cudaSuccess) return e;
-    return paged_launch(paged_plan_kernel, dim3(PLAN_CTAS), dim3(PLAN_THREADS), smem, PLAN_CTAS, true, st, R, old_lens, keep_lens, new_lens, table, W, free_pages,
-                        n_pages, free_count, free_count_out, max_tokens, lens_out, cu_new, slot_map, positions, status);
+    return paged_launch(paged_plan_kernel, dim3(PLAN_CTAS), dim3(PLAN_THREADS), smem, PLAN_CTAS, true, st, R, old_lens, keep_lens, new_lens,
+                        table, W, free_pages, n_pages, free_count, free_count_out, max_tokens, lens_out, cu_new, slot_map, positions, status);
 }
 
 cudaError_t launch_paged_append(const PagedView& pv, char* k_pages, char* v_pages, char* bounds, int is_bf16, int T, const void* k,

@@ -322,16 +322,20 @@ __device__ __forceinline__ int pick_digit(const int* s_hist, int* s_pick, int& n
 // One token's selection: n candidates (pages sink ..), of which m < n are taken; scores c[n]; the places of the pages
 // taken go to sel[0 .. m), ascending.
 struct SelTask {
-    const PagedView* pv;
-    const PagedBatch* pb;
-    int r, h, n, m;
+    const __nv_bfloat16* bounds;  // of the KV head, page 0
+    const int32_t* table;         // the request's row
+    int32_t* status;
+    int n_pages, page_stride;     // pages; elements from one page's bounds to the next
+    int first, n, m, g, d;        // first candidate page
     const __nv_bfloat16* q;       // the token's group of query heads
     float* c;
     float mass;                   // largest A of the candidates
     int32_t* sel;
     __device__ __forceinline__ u64 key(int x) const {
-        const int phys = paged_physical(*pb, *pv, r, pb->sink + x);
-        return phys < 0 ? 0ull : exact_key(reinterpret_cast<const __nv_bfloat16*>(pv->bounds) + ((size_t)phys * pv->H + h) * 2 * pv->d, q, pb->g, pv->d);
+        const int phys = table[first + x];
+        if (phys >= 0 && phys < n_pages) return exact_key(bounds + (size_t)phys * page_stride, q, g, d);
+        latch_error(status, TRIMKV_E_ARG);
+        return 0ull;
     }
 };
 // The band around the m-th largest fp32 score in which 64 bits decide; above it a page is in, below it out.
@@ -422,7 +426,7 @@ __device__ __forceinline__ bool select_by_warp(const SelTask& k, int* list, u64*
     int at = 0;
 #pragma unroll
     for (int i = 0; i < KPL; ++i) {
-        if ((in[i] >> lane) & 1u) k.sel[at + __popc(in[i] & ((1u << lane) - 1u))] = i * 32 + lane + k.pb->sink;
+        if ((in[i] >> lane) & 1u) k.sel[at + __popc(in[i] & ((1u << lane) - 1u))] = i * 32 + lane + k.first;
         at += __popc(in[i]);
     }
     return true;
@@ -556,7 +560,7 @@ __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u6
     for (int x = x0; x < x1; x += 32) {
         const bool t = x + lane < x1 && (band.in(k.c[x + lane]) || k.c[x + lane] == INFINITY);
         const unsigned votes = __ballot_sync(0xffffffffu, t);
-        if (t) k.sel[at + __popc(votes & ((1u << lane) - 1u))] = k.pb->sink + x + lane;
+        if (t) k.sel[at + __popc(votes & ((1u << lane) - 1u))] = k.first + x + lane;
         at += __popc(votes);
     }
 }
@@ -574,7 +578,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
     grid_dependents_may_launch();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)blockIdx.x % nclust, unit = (int)blockIdx.x / nclust;
-    const int t0 = unit / pv.H * ntok, h = unit % pv.H;
+    const int unit_t = pb.by_h.div(unit), t0 = unit_t * ntok, h = unit - unit_t * pv.H;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = pb.g, d = pv.d, W = pb.W;
     u64* s_key = reinterpret_cast<u64*>(s_raw);
     float* s_c = reinterpret_cast<float*>(s_raw + (size_t)W * sizeof(u64));
@@ -624,7 +628,8 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
 #pragma unroll
                 for (int nc = 0; nc < NC; ++nc) {
                     const int n = cb + nc * 8 + row;
-                    const __nv_bfloat16* p = q + (size_t)(t0 + i0 + (n < ncol ? n / g : 0)) * pb.q_stride + (size_t)(h * g + (n < ncol ? n % g : 0)) * d + quad * 8;
+                    const int tk = NTOK == 1 || n >= ncol ? 0 : pb.by_g.div(n), head = n >= ncol ? 0 : n - tk * g;
+                    const __nv_bfloat16* p = q + (size_t)(t0 + i0 + tk) * pb.q_stride + (size_t)(h * g + head) * d + quad * 8;
 #pragma unroll
                     for (int k = 0; k < DK; ++k)
                         qv[nc][k] = n < ncol && k * 32 + quad * 8 < d ? *reinterpret_cast<const uint4*>(p + k * 32) : make_uint4(0u, 0u, 0u, 0u);
@@ -683,7 +688,7 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
                         for (int cc = 0; cc < 2; ++cc) {          // column 2 quad + cc; elements cc, cc + 2: page rows row, row + 8
                             const int n = cb + nc * 8 + 2 * quad + cc;
                             if (n >= ncol) continue;
-                            const int tk = NTOK == 1 ? 0 : n / g;
+                            const int tk = NTOK == 1 ? 0 : pb.by_g.div(n);
 #pragma unroll
                             for (int i = 0; i < NTOK; ++i)
                                 if (NTOK == 1 || i == tk)
@@ -732,8 +737,13 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
 
     auto task = [&](int i) {
         SelTask k;
-        k.pv = &pv; k.pb = &pb;
-        k.r = s_req[i]; k.h = h;
+        k.bounds = reinterpret_cast<const __nv_bfloat16*>(pv.bounds) + (size_t)h * 2 * d;
+        k.table = pb.table + (size_t)s_req[i] * W;
+        k.status = pb.status;
+        k.n_pages = pv.n_pages;
+        k.page_stride = pv.H * 2 * d;
+        k.first = pb.sink;
+        k.g = g; k.d = d;
         k.n = s_np[i] - pb.recent - pb.sink;
         k.m = pb.top - pb.sink - pb.recent;
         k.q = q + (size_t)(t0 + i) * pb.q_stride + (size_t)h * g * d;
