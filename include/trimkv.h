@@ -347,7 +347,7 @@ TRIMKV_API trimkv_status trimkv_select_topk_static(const float* scores, int64_t 
  * of different lengths.  (No counterpart in the paper.)  They take no handle and allocate nothing: every buffer is the
  * caller's device memory.
  *   pages        k_pages, v_pages [n_pages, kv_heads, 64, head_dim]: entry e of a request lies in row e % 64 of page
- *                block_table[request][e / 64]. 
+ *                block_table[request][e / 64].  n_pages x kv_heads x 64 is below 2^31.
  *   key_bounds   [n_pages, kv_heads, 2, head_dim]: the channelwise smallest and largest key of each FULL page, kept by
  *                trimkv_paged_append, read by trimkv_paged_sparse_attention.  May be NULL where neither is needed.
  *   block_table  int32 [n_req, table_width] physical pages; entries behind a request's last page are not read.
@@ -360,6 +360,7 @@ TRIMKV_API trimkv_status trimkv_select_topk_static(const float* scores, int64_t 
  *                page or slot too), E_NOMEM where the plan finds too few free pages, E_TIMEOUT where a bounded wait gave up.
  * Lengths and tables live on the device, so a captured graph serves every step.  Two calls that may overlap on the GPU
  * need workspaces (and outputs) of their own; contents of a workspace are ignored and may be overwritten after the call.
+ * Outputs and workspace overlap no input, but where a call says so.
  * At most TRIMKV_PAGED_MAX_REQ requests, 64 x TRIMKV_PAGED_MAX_WIDTH entries per request. */
 #define TRIMKV_PAGED_MAX_REQ 8192
 #define TRIMKV_PAGED_MAX_WIDTH 16384

@@ -1,4 +1,5 @@
 // C entry points of the caller-owned paged cache: argument checks, workspace layout, choice of kernels.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -31,6 +32,8 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
     if (c->n_pages < 1 || c->n_pages > TRIMKV_PAGED_MAX_PAGES) return refuse(TRIMKV_E_ARG, "n_pages must be in [1, %d]", TRIMKV_PAGED_MAX_PAGES);
     if (c->kv_heads < 1 || c->kv_heads > 1024) return refuse(TRIMKV_E_ARG, "kv_heads must be in [1, 1024]");
     if (c->head_dim < 8 || c->head_dim % 8 || c->head_dim > 256) return refuse(TRIMKV_E_UNSUPPORTED, "head_dim must be a multiple of 8 up to 256");
+    // rows of the tensor maps and slots are 32-bit numbers
+    if ((long long)c->n_pages * c->kv_heads * PAGE > INT_MAX) return refuse(TRIMKV_E_UNSUPPORTED, "n_pages x kv_heads x %d must be below 2^31", PAGE);
     if (!ok16(c->k_pages) || !ok16(c->v_pages) || !ok16(c->key_bounds)) return refuse(TRIMKV_E_ARG, "k_pages, v_pages and key_bounds must be 16-byte aligned");
     pv->k = (const char*)c->k_pages;
     pv->v = (const char*)c->v_pages;
@@ -70,6 +73,10 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
         if (!q || !out || !ok16(q) || !ok16(out)) return refuse(TRIMKV_E_ARG, "q and out must be non-NULL and 16-byte aligned");
         if (q_stride < (int64_t)q_heads * pv.d || q_stride > (1LL << 31) || (q_stride * (is_bf16 ? 2 : 4)) % 16)
             return refuse(TRIMKV_E_ARG, "q_stride must cover a token's q and be a multiple of 16 bytes");
+        // several workers read a row of q, and any of them may be the first to write its part of out
+        const size_t elt = is_bf16 ? 2 : 4, row = (size_t)q_heads * pv.d * elt;
+        const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
+        if (q0 < o0 + n_tokens * row && o0 < q0 + (n_tokens - 1) * (size_t)q_stride * elt + row) return refuse(TRIMKV_E_ARG, "out must not overlap q");
     }
     if (!cu_new || !lens || !block_table || !ok4(cu_new) || !ok4(lens) || !ok4(block_table) || !ok4(status))
         return refuse(TRIMKV_E_ARG, "cu_new, lens and block_table must be non-NULL and aligned");
@@ -210,7 +217,7 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     if (is_bf16) {
         // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
         // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
-        // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page, and two requests cannot differ in width.
+        // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page.
         const int unit_tokens = PAGED_TC_ROWS / pb.g + 2 + 1;            // and the union's own row of bits
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
         pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);

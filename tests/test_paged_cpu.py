@@ -33,7 +33,7 @@ def attention_args(cache_=None, sparse=False, **kw):
     need = binding.paged_workspace_bytes(4, 2, 64)
     a = dict(cache=cache_ or cache(), r=1, t=1, max_new=1, hq=4, q=OK16, qs=256, cu=OK16, lens=OK16, table=OK16, width=4, scale=0.125)
     a.update(dict(top=3, sink=1, recent=1, selected=OK16) if sparse else dict(window=0))
-    a.update(out=OK16, ws=OK16, ws_bytes=need, status=OK16, stream=None)
+    a.update(out=OK16 + (1 << 28), ws=OK16, ws_bytes=need, status=OK16, stream=None)
     if sparse:
         del a["max_new"]
     assert set(kw) <= set(a), kw
@@ -49,7 +49,7 @@ BAD_CACHES = [(dict(k_pages=None), binding.E_ARG), (dict(v_pages=None), binding.
               (dict(key_bounds=OK16 + 2), binding.E_ARG), (dict(n_pages=0), binding.E_ARG), (dict(n_pages=(1 << 24) + 1), binding.E_ARG),
               (dict(kv_heads=0), binding.E_ARG), (dict(kv_heads=1025), binding.E_ARG), (dict(head_dim=0), binding.E_UNSUPPORTED),
               (dict(head_dim=12), binding.E_UNSUPPORTED), (dict(head_dim=264), binding.E_UNSUPPORTED), (dict(kv_dtype=2), binding.E_ARG),
-              (dict(page_size=32), binding.E_UNSUPPORTED), (dict(reserved=1), binding.E_ARG)]
+              (dict(n_pages=1 << 20, kv_heads=32), binding.E_UNSUPPORTED), (dict(page_size=32), binding.E_UNSUPPORTED), (dict(reserved=1), binding.E_ARG)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_CACHES)
@@ -75,7 +75,7 @@ def test_append_refusals(kw):
 
 COMMON = [dict(r=0), dict(r=8193), dict(t=-1), dict(t=1 << 29), dict(hq=1), dict(hq=3), dict(hq=258), dict(q=None), dict(q=OK16 + 2), dict(qs=255), dict(qs=260),
           dict(cu=None), dict(lens=None), dict(table=None), dict(width=0), dict(width=16385), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
-          dict(scale=float("inf")), dict(out=None), dict(out=OK16 + 4), dict(ws=None), dict(ws=OK16 + 16), dict(ws_bytes=0), dict(cu=OK16 + 1), dict(status=OK16 + 2)]
+          dict(scale=float("inf")), dict(out=None), dict(out=OK16 + 4), dict(out=OK16), dict(t=3, out=OK16 + 2 * 512 + 256), dict(q=OK16 + (1 << 28) + 256), dict(ws=None), dict(ws=OK16 + 16), dict(ws_bytes=0), dict(cu=OK16 + 1), dict(status=OK16 + 2)]
 
 
 @pytest.mark.parametrize("kw", COMMON + [dict(window=-1), dict(window=(1 << 30) + 1), dict(max_new=-1)])
