@@ -152,12 +152,11 @@ struct PagedTable {
     __device__ __forceinline__ long long share(int w) const { return quot * w + (long long)((unsigned)(rem * w) / (unsigned)workers); }
 };
 
-__device__ __forceinline__ void paged_finish_table(PagedTable& t, int R, int max_workers, int min_share, long long* prefix) {
+__device__ __forceinline__ void paged_finish_table(PagedTable& t, int max_workers, int min_share) {
     t.total = t.mem->grp[t.ngrp];
     t.workers = (int)min((long long)max_workers, t.whole ? t.total : paged_div(t.total + min_share - 1, min_share));
     t.quot = t.workers ? paged_div(t.total, t.workers) : 0;
     t.rem = (int)(t.total - t.quot * t.workers);
-    if (prefix && blockIdx.x == 0 && threadIdx.x == 0) { prefix[R] = t.total; prefix[R + 1] = t.whole ? 0 : t.workers; }
 }
 // steps, units and the longest unit of all requests: do whole units do?
 // join_steps: what joining parts costs, in steps of the kernel.
@@ -165,12 +164,10 @@ __device__ __forceinline__ bool paged_choose_whole(long long steps, long long un
     return paged_div(units + max_workers - 1, max_workers) * longest <= paged_div(steps, max_workers) + join_steps;
 }
 
-// Every thread of the block calls it.  prefix (may be null): steps before each request, [R + 1], written by block 0;
-// prefix[R + 1] = workers, or 0 where the line counts whole units (nothing is joined then).
+// Every thread of the block calls it.
 template <int SEL>
 __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
-                                                  int max_rows, int max_workers, int min_share, int join_steps, PagedTableMem* mem,
-                                                  long long* prefix) {
+                                                  int max_rows, int max_workers, int min_share, int join_steps, PagedTableMem* mem) {
     t.mem = mem;
     t.heads = heads;
     t.tile_rows = tile_rows; t.min_rows = min_rows; t.max_rows = max_rows;
@@ -204,11 +201,10 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
             mem->req[r] = make_int4(q.row0, q.n, q.len, 0);
             mem->grp[r + 1] = sum;
             if (r == 0) { mem->grp[0] = 0; mem->whole = t.whole; }
-            if (prefix && blockIdx.x == 0 && r < pb.R) prefix[r] = sum - mine;
         }
         __syncthreads();
         t.whole = mem->whole;
-        paged_finish_table(t, pb.R, max_workers, min_share, prefix);
+        paged_finish_table(t, max_workers, min_share);
         return;
     }
     t.gsz = (pb.R + PAGED_GROUPS - 1) / PAGED_GROUPS;
@@ -253,17 +249,7 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
         for (int gi = g0; gi < g1; ++gi) { run += mem->grp[gi + 1]; mem->grp[gi + 1] = run; }
     }
     __syncthreads();
-    if (prefix && blockIdx.x == 0 && !t.whole) {
-        for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
-            long long run = mem->grp[gi];
-            for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
-                prefix[r] = run;
-                const PagedCost c = paged_cost<SEL>(pb, paged_request(pb, r), tile_rows, min_rows, max_rows);
-                run += (long long)(c.U * heads) * c.C;
-            }
-        }
-    }
-    paged_finish_table(t, pb.R, max_workers, min_share, prefix);
+    paged_finish_table(t, max_workers, min_share);
 }
 
 // The worker whose share holds step x, from the line's total and the number of workers.
@@ -280,7 +266,6 @@ __device__ __forceinline__ int paged_owner(long long total, int workers, long lo
 // Order of a request's units on the line: last, first, last but one, second, ...  Later units see more entries, so pairs of
 // neighbours cost about the same and equal shares of the line stay equal shares of the work.
 __device__ __forceinline__ int paged_fold(int v, int U) { return (v & 1) ? v / 2 : U - 1 - v / 2; }
-__device__ __forceinline__ int paged_unfold(int u, int U) { return u >= U - 1 - (U - 1) / 2 ? 2 * (U - 1 - u) : 2 * u + 1; }
 
 // First of the request's n * g (token, query head) rows that belong to unit u, and how many do.
 template <int SEL>
@@ -301,6 +286,7 @@ struct PagedItem {
     int p0, p1;             // first page and one past the last (of the unit's pages, or places in its list of selected pages)
     long long steps;        // steps of the line that it covers
     int slot;               // -1: the whole unit (the result is final); else 2 w or 2 w + 1, see above
+    int cost;               // steps of the unit
     int tok0, tok1;         // tokens (of the request) that the unit's rows belong to, tok1 inclusive
 };
 
@@ -335,6 +321,7 @@ __device__ __forceinline__ PagedItem paged_item(const PagedTable& t, const Paged
     const int v1 = t.whole ? c.C : v0 + (int)it.steps;
     it.r = r;
     it.q = q;
+    it.cost = c.C;
     it.h = unit / c.U;
     it.u = paged_fold(unit - it.h * c.U, c.U);
     int first, count;                                     // the unit's pages
@@ -385,20 +372,29 @@ __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedV
 }
 
 // ---------------------------------------------------------------- workspace
-// [prefix: (PAGED_MAX_REQ + 2) int64][partials of the first kernel][of the second][the second kernel's schedule]
+// Of each kernel: [shared units, one per worker: int4][partial results, two slots per worker].
 constexpr int PAGED_SMS = 148;
 constexpr int PAGED_WARP_ROWS = 64, PAGED_WARPS = 4;              // warp kernel: rows per unit at most, workers per SM (2 above 16 rows)
 constexpr int PAGED_F32_ROWS = 16, PAGED_F32_CTAS = 2;        // fp32 kernel: rows per unit, CTAs per SM at most
 constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
-constexpr size_t PAGED_PREFIX_BYTES = ((size_t)(PAGED_MAX_REQ + 2) * 8 + 255) & ~(size_t)255;
+constexpr size_t PAGED_SHARED_BYTES = (size_t)PAGED_SMS * PAGED_WARPS * 16;      // the warp kernel has the most workers
 // partial results of `rows` rows (workers x rows per unit), two slots each
 constexpr size_t paged_partial_bytes(int rows, int d) { return ((size_t)2 * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
 
 struct PagedWork {
-    long long* prefix;
+    int4* shared;             // [workers]: see paged_note_shared
     float* part_o;            // [slots][rows][d]
     float* part_ml;           // [slots][rows][2]: running maximum (log2 units) and sum
 };
+
+// The unit that worker w began, at step x of the line, and did not end: {row0 of its request, its first row, rows | parts << 12,
+// KV head}; worker w's own part is in slot 2 w + 1, the next workers' in slots 2 (w + 1), 2 (w + 2), ...  Workers without
+// such a unit leave zeros (paged_note_none).
+__device__ __forceinline__ void paged_note_none(const PagedWork& wk, int w) { wk.shared[w] = make_int4(0, 0, 0, 0); }
+__device__ __forceinline__ void paged_note_shared(const PagedWork& wk, const PagedTable& t, const PagedItem& it, long long x, int w, int first, int rows) {
+    const int parts = paged_owner(t.total, t.workers, x + it.cost - 1) - w + 1;
+    wk.shared[w] = make_int4(it.q.row0, first, rows | parts << 12, it.h);
+}
 
 // ---------------------------------------------------------------- launchers (host)
 // Every kernel of this family is launched as a programmatic dependent of whatever precedes it in the stream: it may be placed
@@ -435,9 +431,9 @@ constexpr int PAGED_SELECT_SMEM = 196 * 1024;
 size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st);
-// Joins the partial results of a kernel whose requests have min_rows .. max_rows (token, query head) rows.
-cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int tile_rows,
-                              int min_rows, int max_rows, cudaStream_t st);
+// Joins the partial results of a kernel of `workers` workers whose units have up to unit_rows rows.
+cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int unit_rows,
+                              int workers, cudaStream_t st);
 // fp32 caches.
 cudaError_t launch_paged_attention_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                        cudaStream_t st);

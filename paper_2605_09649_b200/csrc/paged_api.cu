@@ -44,9 +44,9 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
     return TRIMKV_OK;
 }
 
-// Workspace: two areas {steps before each request, partial results}.  The first serves the kernel that a call always has or the
+// Workspace: two areas {shared units, partial results}.  The first serves the kernel that a call always has or the
 // only one, the second the tensor-core kernel.  Sizes depend on the head layout alone.
-size_t area_bytes(int rows, int d) { return PAGED_PREFIX_BYTES + paged_partial_bytes(rows, d); }
+size_t area_bytes(int rows, int d) { return PAGED_SHARED_BYTES + paged_partial_bytes(rows, d); }
 // The most (workers x rows of a unit) of the first kernels: the fp32 kernel's units are 16 rows; the warp kernel's 8 or 16 with
 // four workers per SM, 32 or 64 with two.
 constexpr int FIRST_ROWS = PAGED_SMS * 2 * PAGED_WARP_ROWS;
@@ -56,8 +56,8 @@ size_t work_bytes(int d) { return first_area(d) + area_bytes(PAGED_SMS * PAGED_T
 PagedWork carve(void* area, int rows, int d) {
     char* p = (char*)area;
     PagedWork w;
-    w.prefix = (long long*)p;
-    w.part_o = (float*)(p + PAGED_PREFIX_BYTES);
+    w.shared = (int4*)p;
+    w.part_o = (float*)(p + PAGED_SHARED_BYTES);
     w.part_ml = w.part_o + (size_t)2 * rows * d;
     return w;
 }

@@ -170,9 +170,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table<0>(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem, wk.prefix);
+    paged_build_table<0>(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
+    if (threadIdx.x == 0) paged_note_none(wk, w);
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
     if (warp == T_SOFT + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(a_smem((const void*)s_tmem)), "r"(T_TMEM_COLS) : "memory");
@@ -571,7 +572,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         a_fence_after();
         if (*s_fail) break;
         careful = !careful && *s_redo;                                // (a careful stretch sets no flag)
-        if (!careful) x += it.steps;
+        if (!careful) {
+            if (it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0) paged_note_shared(wk, tab, it, x, w, row_first, rows);
+            x += it.steps;
+        }
         else {
             __syncthreads();                                          // everyone has read the flag
             if (threadIdx.x == 0) *s_redo = 0;
@@ -595,7 +599,7 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_tc_kernel<D, PICK, EXACT>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
                      (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, min_rows, INT_MAX, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, PAGED_SMS, st);
 }
 
 }  // namespace

@@ -75,10 +75,11 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table<SELECT>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem, wk.prefix);      // (synchronises the block)
+    paged_build_table<SELECT>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
     const int w = team * (int)gridDim.x + (int)blockIdx.x;
+    if (lane == 0 && tw == 0) paged_note_none(wk, w);
     if (w >= tab.workers) return;
     const long long end = tab.share(w + 1);
 
@@ -331,6 +332,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     if (dr == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
                 }
             }
+        if (it.slot >= 0 && (it.slot & 1) && lane == 0 && tw == 0) paged_note_shared(wk, tab, it, cons.x, w, unit_first, unit_n);
         const long long next = cons.x + it.steps;
         if (tw == 0 && prod.on && prod.x == next) cons = prod; else cons = at(next);
     }
@@ -356,7 +358,7 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT, EXACT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
                      (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, S::ROWS, 1, max_rows, st);
+    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, SELECT ? pb.sub_rows : S::ROWS, PAGED_SMS * S::TEAMS, st);
 }
 
 }  // namespace
