@@ -221,6 +221,7 @@ paged_select_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, int32_
 
 // ---------------------------------------------------------------- bf16: tensor cores, then 64 bits where it matters
 constexpr int SEL_TOKENS = 4;                 // tokens of one unit, at most
+constexpr int SEL_KPL = 8;                    // a block alone settles one with up to 8 per thread in registers
 constexpr int SEL_WARP_MAX = 512;             // a warp alone settles a token with up to this many candidates
 constexpr int SEL_WARP_LIST = 32, SEL_LIST = 512;   // pages between the thresholds that are ranked by counting (warp, block)
 constexpr int SEL_BINS = 1024;
@@ -237,19 +238,29 @@ __device__ __forceinline__ uint32_t clamp_pos(uint32_t v) {
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // The 64-bit key of one page, by a whole warp: eight lanes per head, 8 channels per lane and step, four sums per lane (an
-// fp64 fma waits long for the one before it).
+// fp64 fma waits long for the one before it).  The bounds are loaded once, all at the same time.
 __device__ __noinline__ u64 exact_key(const __nv_bfloat16* b, const __nv_bfloat16* q, int g, int d) {
-    const int lane = threadIdx.x & 31, l = lane & 7;
+    const int lane = threadIdx.x & 31, c0 = (lane & 7) * 8;
+    uint4 vlo[4], vhi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        vlo[i] = vhi[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (c0 + i * 64 < d) {
+            vlo[i] = *reinterpret_cast<const uint4*>(b + c0 + i * 64);
+            vhi[i] = *reinterpret_cast<const uint4*>(b + d + c0 + i * 64);
+        }
+    }
     double best = -INFINITY;
     bool nan = false;
     for (int h0 = 0; h0 < g; h0 += 4) {
         const int head = h0 + (lane >> 3);
         double s[4] = {0.0, 0.0, 0.0, 0.0};
-        for (int c = l * 8; c < d; c += 64) {
-            const uint4 vq = head < g ? *reinterpret_cast<const uint4*>(q + (size_t)head * d + c) : make_uint4(0u, 0u, 0u, 0u);
-            const uint4 vlo = *reinterpret_cast<const uint4*>(b + c), vhi = *reinterpret_cast<const uint4*>(b + d + c);
-            const __nv_bfloat16 *xq = reinterpret_cast<const __nv_bfloat16*>(&vq), *xlo = reinterpret_cast<const __nv_bfloat16*>(&vlo),
-                                *xhi = reinterpret_cast<const __nv_bfloat16*>(&vhi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i * 64 >= d) break;
+            const uint4 vq = head < g && c0 + i * 64 < d ? *reinterpret_cast<const uint4*>(q + (size_t)head * d + c0 + i * 64) : make_uint4(0u, 0u, 0u, 0u);
+            const __nv_bfloat16 *xq = reinterpret_cast<const __nv_bfloat16*>(&vq), *xlo = reinterpret_cast<const __nv_bfloat16*>(&vlo[i]),
+                                *xhi = reinterpret_cast<const __nv_bfloat16*>(&vhi[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float x = __bfloat162float(xq[e]);
@@ -434,9 +445,122 @@ __device__ __forceinline__ bool select_by_warp(const SelTask& k, int* list, u64*
 
 struct SelShared {
     int hist[SEL_BINS], pick[3], warp[SEL_THREADS / 32], nlist, list[SEL_LIST];
-    uint2 range[SEL_THREADS / 32];
+    uint2 range[2][SEL_THREADS / 32];
     u64 lkey[SEL_LIST];
 };
+
+// By the block, KPL scores per thread in registers (n <= KPL x SEL_THREADS): the same bisection, its counts summed over the warps in
+// shared memory.  A warp has a run of neighbouring candidates.  false, for the whole block: as above.
+template <int KPL>
+__device__ __forceinline__ bool select_in_registers(const SelTask& k, SelShared& sh) {
+    constexpr int WARPS = SEL_THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (!(k.mass < INFINITY)) return false;
+    const float e2 = sel_slack(k.mass);
+    const int per = (k.n + SEL_THREADS - 1) / SEL_THREADS, x0 = warp * per * 32 + lane;
+    float v[KPL];
+    uint32_t key[KPL];
+    uint32_t a = ~0u, b = 0u;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        const bool real = i < per && x0 + i * 32 < k.n;
+        v[i] = real ? k.c[x0 + i * 32] : 0.f;
+        key[i] = real ? orderable_key(v[i]) : 0u;
+        if (real) { a = min(a, key[i]); b = max(b, key[i]); }
+    }
+    a = __reduce_min_sync(0xffffffffu, a);
+    b = __reduce_max_sync(0xffffffffu, b);
+    if (lane == 0) sh.range[0][warp] = make_uint2(a, b);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) { a = min(a, sh.range[0][w].x); b = max(b, sh.range[0][w].y); }
+    // (two buffers in turn: whoever writes one again has passed the barrier behind which everybody has read it)
+    for (int turn = 1; a < b && !(key_value(b) - key_value(a) <= e2); turn ^= 1) {
+        const uint32_t quarter = (b - a) / 4 + 1, p1 = a + quarter, p2 = min(b, p1 - 1 + quarter) + 1, p3 = min(b, p2 - 1 + quarter) + 1;
+        uint32_t n12 = 0, n3 = 0;                                 // keys >= p1 and >= p2, 16 bits each; >= p3
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) {
+            n12 += (key[i] >= p1 ? 1u : 0u) + (key[i] >= p2 ? 1u << 16 : 0u);
+            n3 += key[i] >= p3 ? 1u : 0u;
+        }
+        n12 = __reduce_add_sync(0xffffffffu, n12);
+        n3 = __reduce_add_sync(0xffffffffu, n3);
+        if (lane == 0) sh.range[turn][warp] = make_uint2(n12, n3);
+        __syncthreads();
+        n12 = n3 = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) { n12 += sh.range[turn][w].x; n3 += sh.range[turn][w].y; }
+        if ((int)n3 >= k.m) a = p3;
+        else if ((int)(n12 >> 16) >= k.m) { a = p2; b = p3 - 1; }
+        else if ((int)(n12 & 0xffffu) >= k.m) { a = p1; b = p2 - 1; }
+        else b = p1 - 1;
+    }
+    const SelBand band = {__fadd_rd(key_value(a), -e2), __fadd_ru(key_value(b), e2), false};
+    unsigned in[KPL], hold[KPL];
+    int sure = 0, held = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        const bool real = i < per && x0 + i * 32 < k.n;
+        in[i] = __ballot_sync(0xffffffffu, real && band.in(v[i]));
+        hold[i] = __ballot_sync(0xffffffffu, real && band.holds(v[i]));
+        sure += __popc(in[i]);
+        held += __popc(hold[i]);
+    }
+    __syncthreads();
+    if (lane == 0) sh.range[0][warp] = make_uint2((unsigned)sure, (unsigned)held);
+    __syncthreads();
+    sure = held = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        if (w == warp) before = held;
+        sure += (int)sh.range[0][w].x;
+        held += (int)sh.range[0][w].y;
+    }
+    const int left = k.m - sure;
+    const bool some = left < held;
+    if (some) {
+        if (held > SEL_LIST) return false;
+        int at = before;
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) {
+            if ((hold[i] >> lane) & 1u) sh.list[at + __popc(hold[i] & ((1u << lane) - 1u))] = x0 + i * 32;
+            at += __popc(hold[i]);
+        }
+        __syncthreads();
+        for (int x = warp; x < held; x += WARPS) {
+            const u64 y = k.key(sh.list[x]);
+            if (lane == 0) sh.lkey[x] = y;
+        }
+        __syncthreads();
+        for (int x = tid; x < held; x += SEL_THREADS) {           // the list ascends: among equal keys the lower page comes first
+            const u64 y = sh.lkey[x];
+            int above = 0;
+            for (int i = 0; i < held; ++i) above += sh.lkey[i] > y || (sh.lkey[i] == y && i < x);
+            sh.hist[x] = above < left;
+        }
+        __syncthreads();
+    }
+    int at = before, mine = 0;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        if (hold[i]) {
+            const bool h = (hold[i] >> lane) & 1u;
+            in[i] |= some ? __ballot_sync(0xffffffffu, h && sh.hist[at + __popc(hold[i] & ((1u << lane) - 1u))]) : hold[i];
+            at += __popc(hold[i]);
+        }
+        mine += __popc(in[i]);
+    }
+    if (lane == 0) sh.warp[warp] = mine;
+    __syncthreads();
+    at = 0;
+    for (int w = 0; w < warp; ++w) at += sh.warp[w];
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+        if ((in[i] >> lane) & 1u) k.sel[at + __popc(in[i] & ((1u << lane) - 1u))] = x0 + i * 32 + k.first;
+        at += __popc(in[i]);
+    }
+    return true;
+}
 
 // By the block; keys: [n] 64-bit words of shared memory.
 __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u64* keys) {
@@ -455,10 +579,10 @@ __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u6
         }
         kmin = __reduce_min_sync(0xffffffffu, kmin);
         kmax = __reduce_max_sync(0xffffffffu, kmax);
-        if (lane == 0) sh.range[warp] = make_uint2(kmin, kmax);
+        if (lane == 0) sh.range[0][warp] = make_uint2(kmin, kmax);
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < SEL_THREADS / 32; ++w) { kmin = min(kmin, sh.range[w].x); kmax = max(kmax, sh.range[w].y); }
+        for (int w = 0; w < SEL_THREADS / 32; ++w) { kmin = min(kmin, sh.range[0][w].x); kmax = max(kmax, sh.range[0][w].y); }
         // the bin of a key: monotone in the key, exact integers
         const uint32_t span = kmax - kmin;
         const int shift = max(0, 32 - __clz((int)span) - 10);     // span >> shift < 1024 (span = 0: shift 0)
@@ -752,21 +876,31 @@ paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __rest
         k.sel = selected + ((size_t)(t0 + i) * pv.H + h) * pb.top + pb.sink;
         return k;
     };
-    // ---- a warp per token; what is too much for a warp is left to the block
+    // pages that are always read; whether any are left to choose
+    auto always = [&](int i, int x0, int step) {
+        const int np = s_np[i];
+        int32_t* sel = selected + ((size_t)(t0 + i) * pv.H + h) * pb.top;
+        if (np <= pb.top) {
+            for (int x = x0; x < pb.top; x += step) sel[x] = x < np ? x : -1;
+            return false;
+        }
+        for (int x = x0; x < pb.sink; x += step) sel[x] = x;
+        for (int x = x0; x < pb.recent; x += step) sel[pb.top - pb.recent + x] = np - pb.recent + x;
+        return pb.top > pb.sink + pb.recent;
+    };
+    if (NTOK == 1) {                                              // the block has one token
+        if (s_req[0] < 0 || !always(0, tid, SEL_THREADS)) return;
+        const SelTask k = task(0);
+        if (k.n > SEL_KPL * SEL_THREADS || !select_in_registers<SEL_KPL>(k, sh)) select_by_block(k, sh, s_key);
+        return;
+    }
+    // a warp per token; what is too much for a warp is left to the block
     if (warp < ntok) {
-        const int np = s_np[warp];
         bool hard = false;
-        if (s_req[warp] >= 0) {
-            int32_t* sel = selected + ((size_t)(t0 + warp) * pv.H + h) * pb.top;
-            if (np <= pb.top) {
-                for (int x = lane; x < pb.top; x += 32) sel[x] = x < np ? x : -1;
-            } else {
-                for (int x = lane; x < pb.sink; x += 32) sel[x] = x;
-                for (int x = lane; x < pb.recent; x += 32) sel[pb.top - pb.recent + x] = np - pb.recent + x;
-                const SelTask k = task(warp);
-                if (k.m > 0) hard = k.n > SEL_WARP_MAX || !(k.n <= 256 ? select_by_warp<8>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST)
-                                                                           : select_by_warp<16>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST));
-            }
+        if (s_req[warp] >= 0 && always(warp, lane, 32)) {
+            const SelTask k = task(warp);
+            hard = k.n > SEL_WARP_MAX || !(k.n <= 256 ? select_by_warp<8>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST)
+                                                      : select_by_warp<16>(k, sh.list + warp * SEL_WARP_LIST, sh.lkey + warp * SEL_WARP_LIST));
         }
         if (lane == 0) s_hard[warp] = hard;
     }
