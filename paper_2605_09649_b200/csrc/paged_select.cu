@@ -11,11 +11,11 @@
 // side in memory, with the clamped query.
 //
 // bf16 (paged_select_mma_kernel): the tensor cores compute U for 16 pages x 8 rows at a time in fp32, and beside it the
-// sum of the terms' magnitudes A, the same product of absolute values.  An fp32 sum of 2 d <= 512 exact products is off by
-// less than A 2^-14 whatever the order and the rounding of its additions (512 additions of relative error 2^-23).  The
-// m-th largest fp32 score is bracketed to [a, b] (a warp alone: by bisection; the block: by one histogram); pages above
-// b + 2 E are in, pages below a - 2 E are out (E: the largest error of the token's pages), and the few in between
-// are scored again in 64 bits.  If all are in
+// sum of the terms' magnitudes A, the same product of absolute values.  An fp32 sum of 2 d exact products is off by less than
+// E = A 2 d 2^-23 whatever the order and the rounding of its additions (each off by 2^-23 of a partial sum at most).  The
+// m-th largest fp32 score is bracketed to [a, b], by bisection on scores in registers or, for very many, by one histogram;
+// pages above b + 2 E are in, pages below a - 2 E are out (E: the largest error of the token's pages), and the few in
+// between are scored again in 64 bits.  If all are in
 // between (equal bounds, infinities, NaN) all are, and a descent over 64-bit keys decides.  Bound by the latency of its
 // chain (table, bounds, descent); the bounds are read once per group of tokens.
 //
@@ -225,7 +225,6 @@ constexpr int SEL_KPL = 8;                    // a block alone settles one with 
 constexpr int SEL_WARP_MAX = 512;             // a warp alone settles a token with up to this many candidates
 constexpr int SEL_WARP_LIST = 32, SEL_LIST = 512;   // pages between the thresholds that are ranked by counting (warp, block)
 constexpr int SEL_BINS = 1024;
-constexpr float SEL_EPS = 1.0f / 16384.0f;    // 2^-14, see above
 
 __device__ __forceinline__ uint32_t clamp_neg(uint32_t v) {
     const __nv_bfloat162 z = __float2bfloat162_rn(0.f), x = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162*>(&v), z);
@@ -356,14 +355,15 @@ struct SelBand {
     __device__ __forceinline__ bool holds(float v) const { return everything || (v <= above && v >= below); }
     __device__ __forceinline__ bool in(float v) const { return !everything && v > above; }
 };
-__device__ __forceinline__ float sel_slack(float mass) { return __fadd_ru(__fmul_ru(mass, 2.0f * SEL_EPS), 1e-33f); }   // 1e-33: products that underflow
+// Twice the error of a score, see above; one addition more pays for the rounding of `mass` itself, 1e-33 for products that underflow.
+__device__ __forceinline__ float sel_slack(float mass, int d) { return __fadd_ru(__fmul_ru(mass, (float)(2 * d + 1) * (2.0f / 8388608.0f)), 1e-33f); }
 
 // By one warp, KPL scores per lane in registers (n <= 32 KPL).  false: too many pages in the band, nothing written.
 template <int KPL>
 __device__ __forceinline__ bool select_by_warp(const SelTask& k, int* list, u64* lkey) {
     const int lane = threadIdx.x & 31;
     if (!(k.mass < INFINITY)) return false;
-    const float e2 = sel_slack(k.mass);
+    const float e2 = sel_slack(k.mass, k.d);
     float v[KPL];
     uint32_t key[KPL];
     // [a, b] holds the m-th largest; three pivots a step until it is narrower than the slack
@@ -456,7 +456,7 @@ __device__ __forceinline__ bool select_in_registers(const SelTask& k, SelShared&
     constexpr int WARPS = SEL_THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (!(k.mass < INFINITY)) return false;
-    const float e2 = sel_slack(k.mass);
+    const float e2 = sel_slack(k.mass, k.d);
     const int per = (k.n + SEL_THREADS - 1) / SEL_THREADS, x0 = warp * per * 32 + lane;
     float v[KPL];
     uint32_t key[KPL];
@@ -480,6 +480,7 @@ __device__ __forceinline__ bool select_in_registers(const SelTask& k, SelShared&
         uint32_t n12 = 0, n3 = 0;                                 // keys >= p1 and >= p2, 16 bits each; >= p3
 #pragma unroll
         for (int i = 0; i < KPL; ++i) {
+            if (i >= per) break;
             n12 += (key[i] >= p1 ? 1u : 0u) + (key[i] >= p2 ? 1u << 16 : 0u);
             n3 += key[i] >= p3 ? 1u : 0u;
         }
@@ -601,7 +602,7 @@ __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u6
         }
         __syncthreads();
         const uint32_t a = kmin + ((uint32_t)sh.pick[0] << shift), b = min(kmax, a + ((1u << shift) - 1u));
-        const float e2 = sel_slack(k.mass);
+        const float e2 = sel_slack(k.mass, k.d);
         band.below = __fadd_rd(key_value(a), -e2);
         band.above = __fadd_ru(key_value(b), e2);
     } else
