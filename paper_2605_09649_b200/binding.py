@@ -429,6 +429,13 @@ def _rows(index: int, name: str, t: torch.Tensor, dtype, heads: int, d: int):
                      f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
+def _small(**numbers):
+    """Numbers that the call takes as 32 bits (ctypes would cut a larger one down without a word)."""
+    for name, x in numbers.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise ValueError(f"{name} = {x} is out of range")
+
+
 def _paged_cache(k_pages, v_pages, key_bounds):
     if not k_pages.is_cuda:
         raise ValueError("expected a CUDA tensor")
@@ -515,6 +522,7 @@ def _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspa
 def paged_attention(k_pages, v_pages, q, cu_new, lens, block_table, max_new: int = 0, *, scale: Optional[float] = None,
                     window: int = 0, out=None, workspace=None, status=None):
     """Causal attention of the new tokens q [tokens, Hq, d] over a caller-owned paged cache (trimkv_paged_attention)."""
+    _small(max_new=max_new, window=window)
     cache, n, dt = _paged_cache(k_pages, v_pages, None)
     r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
     _launch(lib().trimkv_paged_attention, n, C.byref(cache), r, t, max_new, hq, *batch, window, *tail)
@@ -526,6 +534,7 @@ def paged_sparse_attention(k_pages, v_pages, key_bounds, q, cu_new, lens, block_
                            status=None):
     """Attention over the top_pages pages that each token selects by their key bounds (trimkv_paged_sparse_attention).
     Returns (out, selected [tokens, H, top_pages])."""
+    _small(top_pages=top_pages, sink_pages=sink_pages, recent_pages=recent_pages)
     cache, n, dt = _paged_cache(k_pages, v_pages, key_bounds)
     r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
     if selected is None:

@@ -428,3 +428,74 @@ def test_two_streams_at_once_and_repeatable():
     torch.cuda.synchronize()
     for i, o in enumerate(outs):                                           # no atomics: the same bits every time
         assert torch.equal(o, first if i < 4 else firsts)
+
+
+@pytest.mark.parametrize("dtype,n_pages", [(torch.bfloat16, 70000), (torch.float32, 35000)])
+def test_pages_behind_32_bit_offsets(dtype, n_pages):
+    """Arrays of more than 2^32 (bf16) and 2^31 elements, 9.2 GB each: pages anywhere in them give the bits that pages in a small
+    cache give."""
+    H, g, d = 8, 4, 128
+    lens, new = [900, 130, 64], [70, 1, 3]
+    c = Cache(lens, H, d, dtype, DEV, 6)
+    q, cu = queries(new, H * g, d, dtype, DEV, 6)
+    cu = ints(cu)
+    far = n_pages - 1 - torch.arange(c.n_pages, device=DEV) * (n_pages // c.n_pages)
+    far[-1] = 0
+    k, v = (torch.empty(n_pages, H, PAGE, d, dtype=dtype, device=DEV) for _ in range(2))
+    b = torch.empty(n_pages, H, 2, d, dtype=dtype, device=DEV)
+    k[far], v[far], b[far] = c.k, c.v, c.bounds
+    table = torch.where(c.table < c.n_pages, far[c.table.clamp(max=c.n_pages - 1).long()].to(I32), c.table)
+    st = status_word()
+    want = binding.paged_attention(c.k, c.v, q, cu, c.lens, c.table, 70)
+    assert torch.equal(binding.paged_attention(k, v, q, cu, c.lens, table, 70, status=st), want)
+    want, chosen = binding.paged_sparse_attention(c.k, c.v, c.bounds, q, cu, c.lens, c.table, 3)
+    got, sel = binding.paged_sparse_attention(k, v, b, q, cu, c.lens, table, 3, status=st)
+    assert torch.equal(got, want) and torch.equal(sel, chosen)
+    x = torch.randn(PAGE + 1, H, d, device=DEV).to(dtype)
+    slots = torch.arange(PAGE + 1, dtype=I32, device=DEV) + (n_pages - 1) * PAGE
+    slots[PAGE] = 5
+    binding.paged_append(k, v, x, -x, slots, key_bounds=b, status=st)
+    assert torch.equal(k[n_pages - 1], x[:PAGE].transpose(0, 1)) and torch.equal(v[n_pages - 1], -x[:PAGE].transpose(0, 1))
+    assert torch.equal(k[0, :, 5], x[PAGE]) and torch.equal(b[n_pages - 1, :, 1], x[:PAGE].amax(0)) and st.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sparse_attention_widest_table(dtype):
+    check_attention([1 << 20], [1], 1, 2, 8, dtype, top=20, sink=1, recent=2)
+
+
+def test_calls_that_share_a_workspace_in_turn():
+    """Different calls one after the other on one stream, and two captured graphs, with one workspace: each gives what it gives alone."""
+    H, g, d = 2, 4, 128
+    c = Cache([3000, 40, 900, 2500], H, d, torch.bfloat16, DEV, 14)
+    ws = torch.full((binding.paged_workspace_bytes(H * g, H, d),), 255, dtype=torch.uint8, device=DEV)
+    calls = []
+    for new, top in (([1, 1, 1, 1], 0), ([2, 1, 150, 300], 0), ([1, 1, 1, 1], 9), ([5, 5, 5, 5], 0), ([200, 1, 2, 130], 6)):
+        q, cu = queries(new, H * g, d, torch.bfloat16, DEV, 14)
+        cu, out = ints(cu), torch.empty_like(q)
+        def call(q=q, cu=cu, out=out, new=new, top=top):
+            if top:
+                binding.paged_sparse_attention(c.k, c.v, c.bounds, q, cu, c.lens, c.table, top, out=out, workspace=ws)
+            else:
+                binding.paged_attention(c.k, c.v, q, cu, c.lens, c.table, max(new), out=out, workspace=ws)
+            return out
+        call()
+        torch.cuda.synchronize()
+        calls.append((call, call().clone(), out))
+    graphs = []
+    for half in (calls[:3], calls[3:]):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            for call, _, _ in half:
+                call()
+    for order in range(6):
+        for _, _, out in calls:
+            out.fill_(float("nan"))
+        if order % 2:
+            for graph in graphs:
+                graph.replay()
+        else:
+            for call, _, _ in calls[order:] + calls[:order]:
+                call()
+        for _, want, out in calls:
+            assert torch.equal(out, want)

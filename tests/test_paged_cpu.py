@@ -130,6 +130,16 @@ def test_binding_refuses_wrong_tensors():
 
 # ---- the plain statements themselves
 
+def test_binding_refuses_numbers_that_do_not_fit_32_bits():
+    z = torch.zeros(1)
+    for kw in (dict(window=(1 << 32) + 5), dict(max_new=1 << 31)):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            binding.paged_attention(z, z, z, z, z, z, **kw)
+    for kw in (dict(top_pages=(1 << 32) + 3), dict(top_pages=3, sink_pages=1 << 32), dict(top_pages=3, recent_pages=(1 << 32) + 1)):
+        with pytest.raises(ValueError, match=list(kw)[-1]):
+            binding.paged_sparse_attention(z, z, z, z, z, z, z, **kw)
+
+
 def test_plain_plan_by_hand():
     got = plan([70, 130, 0], [70, 60, 0], [129, 61, 2], [[9, 8, 0], [7, 6, 5], [0, 0, 0]], [1, 2, 0, 0, 0, 0], 2, 64)
     # request 1 gives back 6 and 5; request 0 pops 5, request 2 pops 6
