@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -127,7 +128,7 @@ def lib() -> C.CDLL:
     L.trimkv_select_workspace_bytes.restype = C.c_size_t
     L.trimkv_select_topk.argtypes = [vp, i64, i64, vp, vp, C.c_size_t, vp, vp]
     L.trimkv_select_topk_static.argtypes = [vp, i64, i64, vp, vp, vp]
-    pc, sz = C.POINTER(PagedCache), C.c_size_t
+    pc, sz = C.c_void_p, C.c_size_t          # pc: trimkv_paged_cache*, byref(PagedCache(...)) or its bytes
     L.trimkv_paged_plan.argtypes = [i32, vp, vp, vp, vp, i32, vp, i32, vp, vp, i64, vp, vp, vp, vp, vp, vp]
     L.trimkv_paged_append.argtypes = [pc, i64, vp, i64, vp, i64, vp, vp, vp]
     L.trimkv_paged_workspace_bytes.argtypes = [i32, i32, i32]
@@ -410,21 +411,29 @@ PAGE_SIZE = 64
 _KV_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
 
 
-def _on(index: int, name: str, t: torch.Tensor, dtype, shape) -> int:
-    """Address of a contiguous tensor of device `index`, type and shape (None: any one-dimensional shape)."""
-    if t.dtype is dtype and t.get_device() == index and (t.shape == shape if shape is not None else t.dim() == 1) and t.is_contiguous():
+# (These calls are short and a decode step makes several, so the checks are made with few attribute reads each.)
+def _ints(index: int, name: str, t: torch.Tensor, n: int) -> int:
+    """Address of n contiguous int32 on device `index`."""
+    if t.dtype is torch.int32 and t.get_device() == index and t.numel() == n and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous {dtype} tensor {'(any length)' if shape is None else tuple(shape)} on cuda:{index}, "
+    raise ValueError(f"{name}: expected {n} contiguous int32 on cuda:{index}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _on(index: int, name: str, t: torch.Tensor, dtype, shape) -> int:
+    """Address of a contiguous tensor of device `index`, type and shape."""
+    if t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on cuda:{index}, "
                      f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
 def _rows(index: int, name: str, t: torch.Tensor, dtype, heads: int, d: int):
-    """(address, elements between tokens) of a [tokens, heads, d] tensor whose rows [heads, d] are contiguous."""
+    """(address, elements between tokens, tokens) of a [tokens, heads, d] tensor whose rows [heads, d] are contiguous."""
     if t.dim() == 3 and t.dtype is dtype and t.get_device() == index:
         n, h, e = t.shape
         step, sh, sd = t.stride()
         if h == heads and e == d and (n == 0 or ((sd == 1 or d == 1) and (sh == d or heads == 1))):
-            return t.data_ptr(), (step if n > 1 else heads * d)
+            return t.data_ptr(), (step if n > 1 else heads * d), n
     raise ValueError(f"{name}: expected {dtype} [tokens, {heads}, {d}] on cuda:{index}, the {heads} x {d} values of a token contiguous, "
                      f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
@@ -436,17 +445,20 @@ def _small(**numbers):
             raise ValueError(f"{name} = {x} is out of range")
 
 
+_pack_cache = struct.Struct("PPPiiiiii").pack      # PagedCache, field by field
+
+
 def _paged_cache(k_pages, v_pages, key_bounds):
-    if not k_pages.is_cuda:
+    """(trimkv_paged_cache as bytes, device, dtype, kv_heads, head_dim)"""
+    index, dt, shape = k_pages.get_device(), k_pages.dtype, k_pages.shape
+    if index < 0:
         raise ValueError("expected a CUDA tensor")
-    dt = k_pages.dtype
-    if k_pages.dim() != 4 or dt not in _KV_DTYPES:
+    if len(shape) != 4 or dt not in _KV_DTYPES:
         raise ValueError("k_pages: expected bf16 or fp32 [n_pages, kv_heads, 64, head_dim]")
-    index, shape = k_pages.get_device(), k_pages.shape
     n, h, page, d = shape
-    return PagedCache(_on(index, "k_pages", k_pages, dt, shape), _on(index, "v_pages", v_pages, dt, shape),
-                      None if key_bounds is None else _on(index, "key_bounds", key_bounds, dt, (n, h, 2, d)),
-                      n, h, d, _KV_DTYPES[dt], page, 0), index, dt
+    return _pack_cache(_on(index, "k_pages", k_pages, dt, shape), _on(index, "v_pages", v_pages, dt, shape),
+                       0 if key_bounds is None else _on(index, "key_bounds", key_bounds, dt, (n, h, 2, d)),
+                       n, h, d, _KV_DTYPES[dt], page, 0), index, dt, h, d
 
 
 # The raw handle of a device's current stream and the current device's number, without the wrapper objects where torch
@@ -471,51 +483,56 @@ def paged_plan(old_lens, keep_lens, new_lens, block_table, free_pages, free_coun
     """Block tables and slot maps from request lengths (trimkv_paged_plan).  int32 tensors: old_lens, keep_lens (or None),
     new_lens, lens_out [R], block_table [R, W], free_pages [n_pages], free_count and free_count_out [1], cu_new [R + 1],
     slot_map and positions (or None) [max_tokens], status [1].  Works in place; returns nothing."""
-    if not old_lens.is_cuda:
+    n = old_lens.get_device()
+    if n < 0:
         raise ValueError("expected a CUDA tensor")
-    n, i, one = old_lens.get_device(), torch.int32, (1,)
-    r, w, m = old_lens.numel(), block_table.shape[-1], slot_map.numel()
-    per = (r,)
-    _launch(lib().trimkv_paged_plan, n, r, _on(n, "old_lens", old_lens, i, per),
-            None if keep_lens is None else _on(n, "keep_lens", keep_lens, i, per), _on(n, "new_lens", new_lens, i, per),
-            _on(n, "block_table", block_table, i, (r, w)), w, _on(n, "free_pages", free_pages, i, None), free_pages.numel(),
-            _on(n, "free_count", free_count, i, one), _on(n, "free_count_out", free_count_out, i, one), m,
-            _on(n, "lens_out", lens_out, i, per), _on(n, "cu_new", cu_new, i, (r + 1,)), _on(n, "slot_map", slot_map, i, (m,)),
-            None if positions is None else _on(n, "positions", positions, i, (m,)),
-            None if status is None else _on(n, "status", status, i, one))
+    r, m, pages = old_lens.numel(), slot_map.numel(), free_pages.numel()
+    rows, w = block_table.shape
+    if rows != r:
+        raise ValueError(f"block_table: expected {r} rows, got {rows}")
+    _launch(lib().trimkv_paged_plan, n, r, _ints(n, "old_lens", old_lens, r),
+            None if keep_lens is None else _ints(n, "keep_lens", keep_lens, r), _ints(n, "new_lens", new_lens, r),
+            _ints(n, "block_table", block_table, r * w), w, _ints(n, "free_pages", free_pages, pages), pages,
+            _ints(n, "free_count", free_count, 1), _ints(n, "free_count_out", free_count_out, 1), m,
+            _ints(n, "lens_out", lens_out, r), _ints(n, "cu_new", cu_new, r + 1), _ints(n, "slot_map", slot_map, m),
+            None if positions is None else _ints(n, "positions", positions, m),
+            None if status is None else _ints(n, "status", status, 1))
 
 
 def paged_append(k_pages, v_pages, k, v, slot_map, key_bounds=None, status=None):
     """Writes k and v [tokens, H, d] (rows may be strided) to the slots of slot_map [tokens] (trimkv_paged_append)."""
-    cache, n, dt = _paged_cache(k_pages, v_pages, key_bounds)
-    t = k.shape[0]
-    kp, ks = _rows(n, "k", k, dt, cache.kv_heads, cache.head_dim)
-    vp, vs = _rows(n, "v", v, dt, cache.kv_heads, cache.head_dim)
-    if v.shape[0] != t:
+    cache, n, dt, h, d = _paged_cache(k_pages, v_pages, key_bounds)
+    kp, ks, t = _rows(n, "k", k, dt, h, d)
+    vp, vs, tv = _rows(n, "v", v, dt, h, d)
+    if tv != t:
         raise ValueError("k and v hold different numbers of tokens")
-    _launch(lib().trimkv_paged_append, n, C.byref(cache), t, kp, ks, vp, vs, _on(n, "slot_map", slot_map, torch.int32, (t,)),
-            None if status is None else _on(n, "status", status, torch.int32, (1,)))
+    _launch(lib().trimkv_paged_append, n, cache, t, kp, ks, vp, vs, _ints(n, "slot_map", slot_map, t),
+            None if status is None else _ints(n, "status", status, 1))
 
 
 def paged_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().trimkv_paged_workspace_bytes(q_heads, kv_heads, head_dim))
 
 
-def _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status):
+def _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspace, status):
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, q_heads, head_dim]")
-    i = torch.int32
-    t, hq, d = q.shape[0], q.shape[1], cache.head_dim
-    qp, qs = _rows(n, "q", q, dt, hq, d)
-    r, w = lens.numel(), block_table.shape[-1]
+    shape = q.shape
+    hq = shape[1]
+    qp, qs, t = _rows(n, "q", q, dt, hq, d)
+    r = lens.numel()
+    rows, w = block_table.shape
+    if rows != r:
+        raise ValueError(f"block_table: expected {r} rows, got {rows}")
     if out is None:
-        out = torch.empty((t, hq, d), dtype=dt, device=q.device)
+        out = torch.empty(shape, dtype=dt, device=q.device)
     if workspace is None:
-        workspace = torch.empty(max(256, paged_workspace_bytes(hq, cache.kv_heads, d)), dtype=torch.uint8, device=q.device)
-    batch = (qp, qs, _on(n, "cu_new", cu_new, i, (r + 1,)), _on(n, "lens", lens, i, (r,)), _on(n, "block_table", block_table, i, (r, w)), w,
+        workspace = torch.empty(max(256, paged_workspace_bytes(hq, h, d)), dtype=torch.uint8, device=q.device)
+    size = workspace.numel()
+    batch = (qp, qs, _ints(n, "cu_new", cu_new, r + 1), _ints(n, "lens", lens, r), _ints(n, "block_table", block_table, r * w), w,
              d ** -0.5 if scale is None else scale)
-    tail = (_on(n, "out", out, dt, (t, hq, d)), _on(n, "workspace", workspace, torch.uint8, None), workspace.numel(),
-            None if status is None else _on(n, "status", status, i, (1,)))
+    tail = (_on(n, "out", out, dt, shape), _on(n, "workspace", workspace, torch.uint8, (size,)), size,
+            None if status is None else _ints(n, "status", status, 1))
     return r, t, hq, batch, tail, out
 
 
@@ -523,9 +540,9 @@ def paged_attention(k_pages, v_pages, q, cu_new, lens, block_table, max_new: int
                     window: int = 0, out=None, workspace=None, status=None):
     """Causal attention of the new tokens q [tokens, Hq, d] over a caller-owned paged cache (trimkv_paged_attention)."""
     _small(max_new=max_new, window=window)
-    cache, n, dt = _paged_cache(k_pages, v_pages, None)
-    r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
-    _launch(lib().trimkv_paged_attention, n, C.byref(cache), r, t, max_new, hq, *batch, window, *tail)
+    cache, n, dt, h, d = _paged_cache(k_pages, v_pages, None)
+    r, t, hq, batch, tail, out = _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspace, status)
+    _launch(lib().trimkv_paged_attention, n, cache, r, t, max_new, hq, *batch, window, *tail)
     return out
 
 
@@ -535,10 +552,10 @@ def paged_sparse_attention(k_pages, v_pages, key_bounds, q, cu_new, lens, block_
     """Attention over the top_pages pages that each token selects by their key bounds (trimkv_paged_sparse_attention).
     Returns (out, selected [tokens, H, top_pages])."""
     _small(top_pages=top_pages, sink_pages=sink_pages, recent_pages=recent_pages)
-    cache, n, dt = _paged_cache(k_pages, v_pages, key_bounds)
-    r, t, hq, batch, tail, out = _paged_batch(cache, n, dt, q, cu_new, lens, block_table, scale, out, workspace, status)
+    cache, n, dt, h, d = _paged_cache(k_pages, v_pages, key_bounds)
+    r, t, hq, batch, tail, out = _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspace, status)
     if selected is None:
-        selected = torch.empty((t, cache.kv_heads, max(top_pages, 0)), dtype=torch.int32, device=q.device)
-    sel = _on(n, "selected", selected, torch.int32, (t, cache.kv_heads, top_pages))
-    _launch(lib().trimkv_paged_sparse_attention, n, C.byref(cache), r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel, *tail)
+        selected = torch.empty((t, h, max(top_pages, 0)), dtype=torch.int32, device=q.device)
+    sel = _on(n, "selected", selected, torch.int32, (t, h, top_pages))
+    _launch(lib().trimkv_paged_sparse_attention, n, cache, r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel, *tail)
     return out, selected
