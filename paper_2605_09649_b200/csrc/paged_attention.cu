@@ -8,7 +8,7 @@
 // x 16 rows, its K fragments come by ldmatrix and Q waits in registers (head sizes up to 128); the running maximum and sum of
 // the softmax with two rows per warp; O += P V: a warp has an eighth of the columns.  Plain fp32 FMAs were bound by shared
 // memory (a 16-byte read per 4 products: 5100 cycles a page at d = 64); this is bound by the page loads for the few rows of a
-// decode step, by the latency of a page's three phases otherwise.
+// decode step, by the latency of a page's three phases otherwise (a prompt of 512 tokens, 4 heads of 64: 23.4 us with the join, 38 with plain FMAs).
 #include "mma_sync.cuh"
 #include "paged.cuh"
 
@@ -273,7 +273,8 @@ paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* __restrict__ q, 
 // A unit that several workers shared: M = max m, out = sum e^(m - M) O / sum e^(m - M) l over its parts, in worker order, so
 // the result does not depend on timing.  Block (w, y): rows y * chunk .. of the unit that worker w began.  Bound by latency, and short
 // enough to be paced by fetching its code: one loop takes up to J_BATCH parts at a time, m, l and O in flight together, with a running
-// maximum; a row of many parts is dealt out over several warps.
+// maximum; a row of many parts is dealt out over several warps.  5 to 6 us for a decode step, 18 us for the 38 MB of parts of 4 x
+// 512 tokens x 32 heads.  (Every row searching for its request and its workers by itself took 7 to 11 and 31 us.)
 constexpr int J_THREADS = 512, J_WARPS = J_THREADS / 32, J_BATCH = 6;
 
 __device__ __forceinline__ void join_store(__nv_bfloat16* o, const float4& v, float f) {

@@ -9,6 +9,9 @@
 // softmax in registers.  Units of up to 32 or 64 rows (drafted tokens): teams of four warps share a ring of 96 KB and every
 // tile, each warp with 8 or 16 of the rows.  (One warp with 32 columns took 80 us for 32 requests x 5 tokens x 4 heads over
 // 0.6 to 2.3 K entries: a warp alone on its scheduler waits for each of its own products.)
+// Measured: 1.07 GB of K and V of a decode step (8 requests of up to 32 K) in 170 us, 0.98 of the measured copy rate; 81 MB (4
+// of up to 16 K) in 26 us and the 184 MB of those drafts in 42 us, of which about 10 are the launch, the table of requests,
+// the first pages' way here and the join.
 // P is rounded to bf16 for the second product, and the sum takes the rounded values, so the weights
 // still add up to one.  Rows behind a request's last entry are zeroed in shared memory (they may hold NaN, and 0 x NaN is
 // NaN).  Every wait is bounded: on expiry the warp latches TRIMKV_E_TIMEOUT, drains its copies and returns.

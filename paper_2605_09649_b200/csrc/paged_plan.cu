@@ -9,9 +9,12 @@
 // requests with one token each (22 KB), whatever the cluster's size; 11.3 us for 256 requests of up to 1024 new tokens (1.6 MB),
 // where clusters of 1, 2, 4 and 8 CTAs take 96, 50, 28 and 17 us: each token costs its search in shared memory.
 //
-// Append.  A copy of k and v rows to their slots, 16 bytes per thread and step, bound by HBM; the grid's second half looks
+// Append.  A copy of k and v rows to their slots, 16 bytes per thread and step; the grid's second half looks
 // for tokens that complete a page (slot % 64 = 63) and reduces the page's 64 keys to its channelwise bounds.  Rows of
-// the page that this same call writes are read from the call's input, so the halves need not wait for one another.
+// the page that this same call writes are read from the call's input, so the halves need not wait for one another.  One
+// token for each of 32 requests (8 heads of 128, bf16) takes 2.2 us, the latency of a launch and two dependent reads; 32
+// chunks of up to 512 move 106 MB in 23.8 us, 0.69 of the measured copy rate: the copy is short, its first and last loads stand
+// alone (two or eight rows in flight per thread: 27 and 31 us; 888 to 9472 blocks: 23.4 to 30 us).
 #include <cooperative_groups.h>
 
 #include <algorithm>
