@@ -9,6 +9,7 @@
 
 #include <cuda.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -79,18 +80,18 @@ constexpr int PAGED_PICK_PAGES = 1024;        // ... and its list of pages
 
 // Rows and length of request r; a request whose offsets or length are out of range counts as having no rows.
 struct PagedReq { int row0, n, len; };
-__device__ __forceinline__ PagedReq paged_request(const PagedBatch& pb, int r) {
+__device__ __forceinline__ PagedReq paged_checked(const PagedBatch& pb, int row0, int end, int len) {
     PagedReq q;
-    q.row0 = pb.cu_new[r];
-    const int end = pb.cu_new[r + 1];
-    q.len = pb.lens[r];
-    q.n = end - q.row0;
-    if (q.row0 < 0 || end < q.row0 || end > pb.T || q.len < 0 || q.len > pb.W * (long long)PAGE) {
+    q.row0 = row0;
+    q.len = len;
+    q.n = end - row0;
+    if (row0 < 0 || end < row0 || end > pb.T || len < 0 || len > pb.W * (long long)PAGE) {
         latch_error(pb.status, TRIMKV_E_ARG);
         q.row0 = q.n = q.len = 0;
     }
     return q;
 }
+__device__ __forceinline__ PagedReq paged_request(const PagedBatch& pb, int r) { return paged_checked(pb, pb.cu_new[r], pb.cu_new[r + 1], pb.lens[r]); }
 
 // ---------------------------------------------------------------- work split
 // A request has U units per KV head -- blocks of `tile_rows` of its n * g (token, query head) rows, or single tokens when
@@ -132,12 +133,22 @@ __device__ __forceinline__ long long paged_div(long long a, int b) {
     return (unsigned long long)a >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
 
-constexpr int PAGED_GROUPS = 512;             // groups of consecutive requests in the shared-memory table
-struct PagedTableMem {                        // shared memory of the table
+// Where the host can tell that every batch of these sizes is dealt out in whole units (paged_choose_whole): a unit for each worker, none
+// longer than a join is worth.  Then no join is launched (2.5 us of a short call's host time).
+constexpr int PAGED_GROUPS = 480;
+inline bool paged_always_whole(const PagedBatch& pb, int H, int tile_rows, int workers, int join_steps) {
+    const long long per_token = pb.top > 0 ? pb.sub : (pb.g + tile_rows - 1) / tile_rows;
+    long long longest = pb.top > 0 && pb.top < pb.W ? pb.top : pb.W;
+    if (pb.window > 0) longest = std::min(longest, ((long long)pb.window + tile_rows / pb.g + 2) / PAGE + 2);      // as paged_cost
+    return pb.R <= PAGED_GROUPS && pb.T * per_token * H <= workers && longest <= join_steps;
+}
+
+// Shared memory of the table: PAGED_GROUPS groups of consecutive requests.
+struct PagedTableMem {
     long long grp[PAGED_GROUPS + 1];          // steps before a group
     int4 req[PAGED_GROUPS];                   // {row0, n, len, units} of each request where a group is one request
-    unsigned long long steps, units;
-    int longest, whole;
+    long long steps[18], units[18];           // of the requests of each warp (the tensor-core kernel has 18)
+    int longest[18], whole;
 };
 struct PagedTable {
     PagedTableMem* mem;
@@ -207,47 +218,57 @@ __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatc
         paged_finish_table(t, max_workers, min_share);
         return;
     }
+    // a thread takes neighbouring groups; sums over the threads by shuffles and one sum per warp in shared memory
     t.gsz = (pb.R + PAGED_GROUPS - 1) / PAGED_GROUPS;
     t.ngrp = (pb.R + t.gsz - 1) / t.gsz;
-    if (threadIdx.x == 0) { mem->grp[0] = 0; mem->steps = 0; mem->units = 0; mem->longest = 0; }
-    __syncthreads();
-    for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    if (t.gsz == 1) {                         // every load in flight at once
+        for (int r = threadIdx.x; r < pb.R; r += blockDim.x) mem->req[r] = make_int4(pb.cu_new[r], pb.cu_new[r + 1], pb.lens[r], 0);
+        __syncthreads();
+    }
+    const int per = (t.ngrp + (int)blockDim.x - 1) / (int)blockDim.x;
+    const int g0 = min(t.ngrp, (int)threadIdx.x * per), g1 = min(t.ngrp, g0 + per);
+    long long my_steps = 0, my_units = 0;
+    int my_longest = 0;
+    for (int gi = g0; gi < g1; ++gi) {
         long long steps = 0, units = 0;
-        int longest = 0;
         for (int r = gi * t.gsz; r < min(pb.R, (gi + 1) * t.gsz); ++r) {
-            const PagedReq q = paged_request(pb, r);
+            PagedReq q;
+            if (t.gsz == 1) { const int4 v = mem->req[r]; q = paged_checked(pb, v.x, v.y, v.z); } else q = paged_request(pb, r);
             const PagedCost c = paged_cost<SEL>(pb, q, tile_rows, min_rows, max_rows);
             units += c.U * heads;
             steps += (long long)(c.U * heads) * c.C;
-            if (c.U) longest = max(longest, c.C);
+            if (c.U) my_longest = max(my_longest, c.C);
             if (t.gsz == 1) mem->req[gi] = make_int4(q.row0, q.n, q.len, (int)units);
         }
         mem->grp[gi + 1] = steps;
-        atomicAdd(&mem->steps, (unsigned long long)steps);        // (sums of integers: any order gives the same)
-        atomicAdd(&mem->units, (unsigned long long)units);
-        atomicMax(&mem->longest, longest);
+        my_steps += steps;
+        my_units += units;
     }
-    __syncthreads();
-    // (groups of several requests keep to steps: their units are not kept apart)
-    t.whole = t.gsz == 1 && paged_choose_whole((long long)mem->steps, (long long)mem->units, mem->longest, max_workers, join_steps);
-    if (t.whole) {
-        for (int gi = threadIdx.x; gi < t.ngrp; gi += blockDim.x) mem->grp[gi + 1] = mem->req[gi].w;
-        __syncthreads();
-    }
-    if (threadIdx.x < 32) {                   // inclusive scan by one warp
-        const int lane = threadIdx.x, per = (t.ngrp + 31) / 32;
-        const int g0 = min(t.ngrp, lane * per), g1 = min(t.ngrp, g0 + per);
-        long long local = 0;
-        for (int gi = g0; gi < g1; ++gi) local += mem->grp[gi + 1];
-        long long incl = local;
+    long long steps_to = my_steps, units_to = my_units;           // of the warp's threads up to this one
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        long long run = incl - local;
-        for (int gi = g0; gi < g1; ++gi) { run += mem->grp[gi + 1]; mem->grp[gi + 1] = run; }
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long a = __shfl_up_sync(0xffffffffu, steps_to, o), b = __shfl_up_sync(0xffffffffu, units_to, o);
+        if (lane >= o) { steps_to += a; units_to += b; }
     }
+    my_longest = __reduce_max_sync(0xffffffffu, my_longest);
+    if (lane == 31) { mem->steps[warp] = steps_to; mem->units[warp] = units_to; mem->longest[warp] = my_longest; }
+    __syncthreads();
+    long long steps = 0, units = 0;
+    for (int x = 0; x < warps; ++x) {
+        if (x == warp) { steps_to += steps; units_to += units; }
+        steps += mem->steps[x];
+        units += mem->units[x];
+        my_longest = max(my_longest, mem->longest[x]);
+    }
+    // (groups of several requests keep to steps: their units are not kept apart)
+    t.whole = t.gsz == 1 && paged_choose_whole(steps, units, my_longest, max_workers, join_steps);
+    long long run = t.whole ? units_to - my_units : steps_to - my_steps;
+    for (int gi = g0; gi < g1; ++gi) {
+        run += t.whole ? (long long)mem->req[gi].w : mem->grp[gi + 1];
+        mem->grp[gi + 1] = run;
+    }
+    if (threadIdx.x == 0) mem->grp[0] = 0;
     __syncthreads();
     paged_finish_table(t, max_workers, min_share);
 }

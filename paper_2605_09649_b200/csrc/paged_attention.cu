@@ -17,7 +17,7 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int F_THREADS = 256, F_ROWS = PAGED_F32_ROWS;
+constexpr int F_THREADS = 256, F_ROWS = PAGED_F32_ROWS, F_JOIN_STEPS = 4;
 
 // DP: head size rounded up to 64, 128 or 256.  Row strides: ldmatrix reads 8 rows of 16 bytes (16 bytes apart modulo 128), the V
 // fragments 4 rows of 8 words (8 words apart modulo 32).
@@ -70,7 +70,7 @@ paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* __restrict__ q, 
     grid_dependency_wait();
     PagedTable tab;
     const int unit_rows = pb.top > 0 ? pb.sub_rows : F_ROWS;
-    paged_build_table<-1>(tab, pb, pv.H, F_ROWS, 1, INT_MAX, (int)gridDim.x, 2, 4, &s_tab);
+    paged_build_table<-1>(tab, pb, pv.H, F_ROWS, 1, INT_MAX, (int)gridDim.x, 2, F_JOIN_STEPS, &s_tab);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (tid == 0) paged_note_none(wk, w);
@@ -372,7 +372,8 @@ cudaError_t run_f32(const PagedView& pv, const PagedBatch& pb, const void* q, vo
     const int workers = PAGED_SMS * S::CTAS;
     const cudaError_t e2 = paged_launch(paged_attn_f32_kernel<DP>, dim3(workers), dim3(F_THREADS), S::SMEM, 1, true, st, pv, pb, (const float*)q, (float*)out,
                                         scale * LOG2E, w);
-    return e2 != cudaSuccess ? e2 : launch_paged_join(pv, pb, 0, out, w, pb.top > 0 ? pb.sub_rows : F_ROWS, workers, st);
+    if (e2 != cudaSuccess || paged_always_whole(pb, pv.H, F_ROWS, workers, F_JOIN_STEPS)) return e2;
+    return launch_paged_join(pv, pb, 0, out, w, pb.top > 0 ? pb.sub_rows : F_ROWS, workers, st);
 }
 
 }  // namespace

@@ -48,6 +48,7 @@ constexpr int T_SOFT = 16;                                            // softmax
 constexpr int T_THREADS = (T_SOFT + 2) * 32;
 constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
+constexpr int T_JOIN_STEPS = 4;       // what a join costs, in pages
 constexpr float T_RESCALE_STEP = 8.0f, T_LEAP = 64.0f;
 constexpr int T_STAGES = 2;           // tiles of K, and of V, in shared memory
 constexpr int T_E0 = 8;               // ring of the tiles' first entries (two pages each): more than the tiles in flight
@@ -177,7 +178,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table<0>(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, 4, table_mem);
+    paged_build_table<0>(tab, pb, pv.H, T_UNIT, min_rows, INT_MAX, (int)gridDim.x, 4, T_JOIN_STEPS, table_mem);
     grid_dependents_may_launch();
     const int w = blockIdx.x;
     if (threadIdx.x == 0) paged_note_none(wk, w);
@@ -613,7 +614,8 @@ cudaError_t run_tc(const PagedView& pv, const PagedBatch& pb, const void* q, voi
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_tc_kernel<D, PICK, EXACT>, dim3(PAGED_SMS), dim3(T_THREADS), S::SMEM, 1, true, st, mk, mv, pv, pb, (const __nv_bfloat16*)q,
                      (__nv_bfloat16*)out, scale * LOG2E, w, min_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, T_UNIT, PAGED_SMS, st);
+    if (e != cudaSuccess || paged_always_whole(pb, pv.H, T_UNIT, PAGED_SMS, T_JOIN_STEPS)) return e;
+    return launch_paged_join(pv, pb, 1, out, w, T_UNIT, PAGED_SMS, st);
 }
 
 }  // namespace

@@ -25,6 +25,7 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int W_JOIN_STEPS = 8;                                       // what a join costs, in pages
 constexpr float W_RESCALE_STEP = 8.0f;                                // log2 units the reference of the weights may lag behind the maximum
 
 // NT: column tiles of 8 rows per warp.  TW: warps of a team, which share a ring and a unit, each with rows of its own.
@@ -78,7 +79,7 @@ paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
-    paged_build_table<SELECT>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, 8, table_mem);      // (synchronises the block)
+    paged_build_table<SELECT>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::TEAMS, 4, W_JOIN_STEPS, table_mem);      // (synchronises the block)
     grid_dependents_may_launch();
     // workers are spread over the SMs first, so that a short line uses many of them
     const int w = team * (int)gridDim.x + (int)blockIdx.x;
@@ -361,7 +362,8 @@ cudaError_t run_warp(const PagedView& pv, const PagedBatch& pb, const void* q, v
     if (e != cudaSuccess) return e;
     e = paged_launch(paged_attn_warp_kernel<D, NT, TW, SELECT, EXACT>, dim3(PAGED_SMS), dim3(S::TEAMS * TW * 32), S::SMEM, 1, true, st, mk, mv, pv, pb,
                      (const __nv_bfloat16*)q, (__nv_bfloat16*)out, scale * LOG2E, w, max_rows);
-    return e != cudaSuccess ? e : launch_paged_join(pv, pb, 1, out, w, SELECT ? pb.sub_rows : S::ROWS, PAGED_SMS * S::TEAMS, st);
+    if (e != cudaSuccess || paged_always_whole(pb, pv.H, S::ROWS, PAGED_SMS * S::TEAMS, W_JOIN_STEPS)) return e;
+    return launch_paged_join(pv, pb, 1, out, w, SELECT ? pb.sub_rows : S::ROWS, PAGED_SMS * S::TEAMS, st);
 }
 
 }  // namespace
