@@ -137,10 +137,12 @@ __device__ __forceinline__ long long paged_div(long long a, int b) {
 // longer than a join is worth.  Then no join is launched (2.5 us of a short call's host time).
 constexpr int PAGED_GROUPS = 480;
 inline bool paged_always_whole(const PagedBatch& pb, int H, int tile_rows, int workers, int join_steps) {
-    const long long per_token = pb.top > 0 ? pb.sub : (pb.g + tile_rows - 1) / tile_rows;
+    // units of one KV head: whole ones per token, or those that the tokens fill and a last one of each request
+    const long long units = pb.top > 0 ? (long long)pb.T * pb.sub
+                                       : std::min((long long)pb.T * ((pb.g + tile_rows - 1) / tile_rows), (long long)pb.T * pb.g / tile_rows + pb.R);
     long long longest = pb.top > 0 && pb.top < pb.W ? pb.top : pb.W;
     if (pb.window > 0) longest = std::min(longest, ((long long)pb.window + tile_rows / pb.g + 2) / PAGE + 2);      // as paged_cost
-    return pb.R <= PAGED_GROUPS && pb.T * per_token * H <= workers && longest <= join_steps;
+    return pb.R <= PAGED_GROUPS && units * H <= workers && longest <= join_steps;
 }
 
 // Shared memory of the table: PAGED_GROUPS groups of consecutive requests.
