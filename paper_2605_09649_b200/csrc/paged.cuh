@@ -401,6 +401,7 @@ constexpr int PAGED_WARP_ROWS = 64, PAGED_WARPS = 4;              // warp kernel
 constexpr int PAGED_F32_ROWS = 16, PAGED_F32_CTAS = 2;        // fp32 kernel: rows per unit, CTAs per SM at most
 constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
 constexpr size_t PAGED_SHARED_BYTES = (size_t)PAGED_SMS * PAGED_WARPS * 16;      // the warp kernel has the most workers
+static_assert(PAGED_SHARED_BYTES % 256 == 0, "partial results are aligned");
 // partial results of `rows` rows (workers x rows per unit), two slots each
 constexpr size_t paged_partial_bytes(int rows, int d) { return ((size_t)2 * rows * (d + 2) * 4 + 255) & ~(size_t)255; }
 

@@ -127,6 +127,12 @@ __device__ __forceinline__ void t_commit(uint32_t leader, uint32_t bar) {
         "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(leader), "r"(bar)
         : "memory");
 }
+// 32 bytes, a whole sector per lane: rows lie d floats apart, and two stores of 16 bytes would each move half a sector.
+__device__ __forceinline__ void t_store32(float* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 __device__ __forceinline__ uint32_t t_uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 // Barrier of the two warps that share 32 rows, the n-th time: an mbarrier, so that the wait has a limit.  false: gave up.
 __device__ __forceinline__ bool t_pair_sync(uint32_t bar, unsigned n) {
@@ -263,18 +269,21 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const int ntile = (npage + 1) / 2;
         if (ntile > 0) {
             if (soft) {
-                const uint4* src = reinterpret_cast<const uint4*>(q + (size_t)(it.q.row0 + tok) * pb.q_stride + (size_t)(it.h * g + head) * d);
-                unsigned char* qdst = gen + S::OFF_Q + grp * S::PLANES * T_QPLANE + r * 128;
+                // neighbouring lanes have neighbouring 16 bytes of a row (a row per lane: 32 cache lines per load, 4100 cycles in all)
+                constexpr int CPR = D / 16;                           // 16-byte chunks of half a row
+                const int c = half * CPR + lane % CPR;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const int c = half * (D / 16) + k;
-                    const uint4 v = valid && c * 8 < d ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4*>(qdst + (c >> 3) * T_QPLANE + (((c & 7) ^ (r & 7)) << 4)) = v;
+                for (int k = 0; k < CPR; ++k) {
+                    const int rq = wl * 32 + k * (32 / CPR) + lane / CPR, row = row_first + grp * T_ROWS + rq, qt = pb.by_g.div(row);
+                    const __nv_bfloat16* src = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + row - qt * g) * d + c * 8;
+                    const uint4 v = grp * T_ROWS + rq < rows && c * 8 < d ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(gen + S::OFF_Q + (grp * S::PLANES + (c >> 3)) * T_QPLANE + rq * 128 + (((c & 7) ^ (rq & 7)) << 4)) = v;
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // Q and the barriers, before the async proxy uses them
             a_fence_before();
-            __syncthreads();
+            // everyone but the warp that copies K and V: its rings are free since the end of the stretch before
+            if (warp != T_SOFT) asm volatile("bar.sync 1, %0;" ::"n"(T_THREADS - 32) : "memory");
             a_fence_after();
 
             if (warp == T_SOFT) {
@@ -546,7 +555,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
                 uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * d + half * (D / 2));
                 const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
-                float4* po = reinterpret_cast<float4*>(wk.part_o + pr * d + half * (D / 2));
+                float* po = wk.part_o + pr * d + half * (D / 2);
                 const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
 #pragma unroll 1
                 for (int k = 0; k < D / 32; ++k) {
@@ -569,8 +578,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                         }
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4)
-                            if (half * (D / 2) + k * 16 + e < d) po[k * 4 + (e >> 2)] = make_float4(__uint_as_float(ov[e]), __uint_as_float(ov[e + 1]), __uint_as_float(ov[e + 2]), __uint_as_float(ov[e + 3]));
+                        for (int e = 0; e < 16; e += 8)
+                            if (half * (D / 2) + k * 16 + e < d) t_store32(po + k * 16 + e, ov + e);
                     }
                 }
                 if (valid && it.slot >= 0 && half == 0) {
