@@ -423,8 +423,9 @@ __device__ __forceinline__ void paged_note_shared(const PagedWork& wk, const Pag
 // ---------------------------------------------------------------- launchers (host)
 // Every kernel of this family is launched as a programmatic dependent of whatever precedes it in the stream: it may be placed
 // (barriers, descriptors) while its predecessor finishes, every one of its threads calls grid_dependency_wait() before it
-// touches memory or returns, and it lets its own successor be placed early.  Behind a kernel that does not take part this is
-// an ordinary launch.  cluster: CTAs per cluster, or 1.  early = false: an ordinary launch.
+// touches memory or returns, and it lets its own successor be placed early.  Their parameters carry no __restrict__: it would
+// promise that the memory does not change from the kernel's start on, so a load could be moved before that wait.  Behind a kernel
+// that does not take part this is an ordinary launch.  cluster: CTAs per cluster, or 1.  early = false: an ordinary launch.
 template <typename... KArgs, typename... Args>
 inline cudaError_t paged_launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem_bytes, int cluster, bool early, cudaStream_t stream, Args&&... args) {
     cudaLaunchConfig_t cfg = {};

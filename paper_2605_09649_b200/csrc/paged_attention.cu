@@ -53,7 +53,7 @@ __device__ __forceinline__ void f32_mma(float (&c)[4], const uint32_t* a, uint32
 
 template <int DP>
 __global__ void __launch_bounds__(F_THREADS, F32Shape<DP>::CTAS)
-paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* __restrict__ q, float* __restrict__ out, float scale_log2, PagedWork wk) {
+paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* q, float* out, float scale_log2, PagedWork wk) {
     using S = F32Shape<DP>;
     constexpr int KSTEPS = DP / 8, NT = DP / 64;                  // k steps of S; 8-column tiles of O per warp
     extern __shared__ __align__(16) float s_f32[];
@@ -289,7 +289,7 @@ __device__ __forceinline__ float join_factor(float l) { return l > 0.f ? 1.f / l
 
 template <typename T>
 __global__ void __launch_bounds__(J_THREADS, 2)
-paged_join_kernel(T* __restrict__ out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_rows, int chunk) {
+paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_rows, int chunk) {
     extern __shared__ __align__(16) float4 s_sum[];               // [J_WARPS][d / 4]
     __shared__ float2 s_ml[J_WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w = blockIdx.x, g = (int)by_g.d;

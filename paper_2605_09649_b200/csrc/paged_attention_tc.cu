@@ -145,7 +145,7 @@ __device__ __forceinline__ bool t_pair_sync(uint32_t bar, unsigned n) {
 template <int D, bool PICK, bool EXACT>
 __global__ void __launch_bounds__(T_THREADS, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
-                     const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int min_rows) {
+                     const __nv_bfloat16* q, __nv_bfloat16* out, float scale_log2, PagedWork wk, int min_rows) {
     using S = TcShape<D, PICK>;
     extern __shared__ unsigned char t_smem_raw[];
     const uint32_t raw = a_smem(t_smem_raw);

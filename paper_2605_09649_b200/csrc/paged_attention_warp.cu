@@ -59,7 +59,7 @@ struct WarpCursor {
 template <int D, int NT, int TW, bool SELECT, bool EXACT>
 __global__ void __launch_bounds__(WarpShape<D, NT, TW>::TEAMS * TW * 32, 1)
 paged_attn_warp_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PagedView pv, PagedBatch pb,
-                       const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float scale_log2, PagedWork wk, int max_rows) {
+                       const __nv_bfloat16* q, __nv_bfloat16* out, float scale_log2, PagedWork wk, int max_rows) {
     using S = WarpShape<D, NT, TW>;
     constexpr int KS = D / 16, MT = S::TILE / 16;
     extern __shared__ unsigned char w_smem_raw[];

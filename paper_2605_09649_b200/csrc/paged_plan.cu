@@ -235,9 +235,8 @@ struct MinMax16<float> {
 // others take `group` tokens of one head each and reduce the pages that these tokens complete, eight rows per warp.
 template <typename T>
 __global__ void __launch_bounds__(APP_THREADS)
-paged_append_kernel(char* __restrict__ k_pages, char* __restrict__ v_pages, char* __restrict__ bounds, int n_pages, int H, int d,
-                    int T_rows, const char* __restrict__ k, long long k_stride, const char* __restrict__ v, long long v_stride,
-                    const int32_t* __restrict__ slot_map, int32_t* status, int copy_blocks, int group) {
+paged_append_kernel(char* k_pages, char* v_pages, char* bounds, int n_pages, int H, int d, int T_rows, const char* k, long long k_stride,
+                    const char* v, long long v_stride, const int32_t* slot_map, int32_t* status, int copy_blocks, int group) {
     constexpr int WARPS = APP_THREADS / 32;
     __shared__ uint4 s_part[2][WARPS][16];
     const int rb = d * (int)sizeof(T), cpr = rb / 16;         // bytes, 16-byte chunks per row

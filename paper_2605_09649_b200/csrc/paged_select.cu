@@ -57,7 +57,7 @@ __device__ __forceinline__ void widen16(const uint4& v, double (&x)[16 / sizeof(
 // grid = T * H clusters.  Shared memory: queries [g][chunks][E / 2][8] double2, then keys [W], then the flags of the pages.
 template <typename T>
 __global__ void __launch_bounds__(SEL_THREADS)
-paged_select_kernel(PagedView pv, PagedBatch pb, const T* __restrict__ q, int32_t* __restrict__ selected, int nclust, int chunks) {
+paged_select_kernel(PagedView pv, PagedBatch pb, const T* q, int32_t* selected, int nclust, int chunks) {
     extern __shared__ __align__(16) unsigned char s_raw[];
     constexpr int E = 16 / (int)sizeof(T);                        // channels of a 16-byte chunk
     __shared__ int s_hist[256];
@@ -696,7 +696,7 @@ __device__ __noinline__ void select_by_block(const SelTask& k, SelShared& sh, u6
 // DK: ceil(d / 32).  NTOK: 1, or up to SEL_TOKENS.  NC: column tiles (8 rows of q each) per walk over the bounds.
 template <int DK, int NTOK, int NC>
 __global__ void __launch_bounds__(SEL_THREADS, DK <= 4 ? 2 : 1)
-paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* __restrict__ q, int32_t* __restrict__ selected, int nclust, int ntok) {
+paged_select_mma_kernel(PagedView pv, PagedBatch pb, const __nv_bfloat16* q, int32_t* selected, int nclust, int ntok) {
     extern __shared__ __align__(16) unsigned char s_raw[];
     __shared__ int s_req[NTOK], s_np[NTOK], s_hard[NTOK];         // request of each token (-1: none), pages up to its own
     __shared__ unsigned s_err[NTOK];
