@@ -129,8 +129,7 @@ flat_gather_kernel(const float* __restrict__ s, long long n, int cap, u64* __res
 // after they part each key still matches at most one of the two prefixes, so a sweep costs the same.
 template <int PER>
 __global__ void __launch_bounds__(1024)
-flat_bracket_kernel(const u64* __restrict__ samples, long long n, long long k_evict, FlatState* __restrict__ st,
-                    long long* __restrict__ stats, float sigmas, int distrust) {
+flat_bracket_kernel(const u64* samples, long long n, long long k_evict, FlatState* st, long long* stats, float sigmas, int distrust) {
     constexpr int DB = 11, NBIN = 1 << DB, CAP = 1024 * PER;
     __shared__ unsigned hAB[NBIN];          // low half-word: keys under the lower end's prefix; high: the upper end's
     __shared__ unsigned wtot[32];
@@ -297,8 +296,7 @@ flat_bracket_kernel(const u64* __restrict__ samples, long long n, long long k_ev
 // first one unchanged; the exact stages after it check whatever they are given.
 constexpr int REFINE_CTAS = 128, REFINE_THREADS = 256, REFINE_PER = 8;     // 2^18 samples
 __global__ void __launch_bounds__(REFINE_THREADS)
-flat_refine_kernel(const float* __restrict__ s, long long n, long long k_evict, FlatState* __restrict__ st,
-                   uint32_t* __restrict__ hist2, long long* __restrict__ stats, float sigmas) {
+flat_refine_kernel(const float* __restrict__ s, long long n, long long k_evict, FlatState* st, uint32_t* hist2, long long* stats, float sigmas) {
     __shared__ uint32_t sh[FB];
     __shared__ unsigned long long wt[REFINE_THREADS / 32];
     __shared__ int s_bin[3];
@@ -763,9 +761,8 @@ __device__ __forceinline__ void flat_main_body(const float* __restrict__ s, long
 }
 
 __global__ void __launch_bounds__(MAIN_THREADS, 1)
-flat_main_kernel(const float* __restrict__ s, long long n, long long k_evict, FlatState* __restrict__ st,
-                 uint32_t* __restrict__ hist, u64* __restrict__ cand, long long cand_cap, u64* __restrict__ keep_bits,
-                 long long* __restrict__ stats, int32_t* __restrict__ status) {
+flat_main_kernel(const float* __restrict__ s, long long n, long long k_evict, FlatState* st, uint32_t* hist, u64* cand, long long cand_cap,
+                 u64* keep_bits, long long* stats, int32_t* status) {
     extern __shared__ __align__(128) unsigned char fm_smem[];
     __shared__ int s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -940,8 +937,7 @@ __device__ void flat_resolve(FlatState* st, const u64* cand2, u64* keep_bits, lo
 }
 
 __global__ void __launch_bounds__(1024)
-flat_cand_kernel(FlatState* __restrict__ st, const u64* __restrict__ cand, u64* __restrict__ cand2,
-                 u64* __restrict__ keep_bits, long long* __restrict__ stats) {
+flat_cand_kernel(FlatState* st, const u64* cand, u64* cand2, u64* keep_bits, long long* stats) {
     __shared__ int s_last;
     grid_dependency_wait();                                   // the list and its bin come from the kernel before
     if (st->mode != MODE_DONE) return;                        // the exact fallback over all scores takes over
@@ -1166,7 +1162,8 @@ cudaError_t launch_select_flat(const float* scores, long long n, long long k_kee
         u64* samples = cand2 + FB / 2;          // behind the refinement round's histogram, which shares the space of cand2
         const int cap = refine ? 4096 : 8192;
         flat_gather_kernel<<<cap / 256, 256, 0, stream>>>(scores, n, cap, samples, hist, status);
-        // every kernel after the first is a dependent launch: it is placed and set up while its predecessor finishes
+        // every kernel after the first is a dependent launch: it is placed and set up while its predecessor finishes, so only the
+        // scores, which none of them writes, are __restrict__ there
         if (refine) launch_dependent(flat_bracket_kernel<4>, dim3(1), dim3(1024), 0, stream, samples, n, k_evict, st, stats, sigmas, distrust);
         else launch_dependent(flat_bracket_kernel<8>, dim3(1), dim3(1024), 0, stream, samples, n, k_evict, st, stats, sigmas, distrust);
         ++launches;

@@ -35,3 +35,11 @@ def test_paged_kernels_promise_nothing_about_memory():
     assert {"paged_plan_kernel", "paged_append_kernel", "paged_attn_f32_kernel", "paged_join_kernel", "paged_attn_warp_kernel", "paged_attn_tc_kernel",
             "paged_select_kernel", "paged_select_mma_kernel"} <= {name for name, _ in found}
     assert [name for name, params in found if "__restrict__" in params] == []
+
+
+def test_selection_kernels_promise_it_of_the_scores_alone():
+    """(no kernel of the selection writes the scores, and the first is an ordinary launch behind whatever wrote them)"""
+    found = _waiting("select")
+    assert {"flat_bracket_kernel", "flat_refine_kernel", "flat_main_kernel", "flat_cand_kernel"} <= {name for name, _ in found}
+    for name, params in found:
+        assert [p.strip() for p in params.split(",") if "__restrict__" in p] in ([], ["const float* __restrict__ s"]), name
