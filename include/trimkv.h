@@ -384,6 +384,7 @@ typedef struct trimkv_paged_cache {
  * keep < old takes rejected drafts back before the next ones.  0 <= keep <= min(old, new) <= 64 x table_width.
  * free_pages: int32 [n_pages], a stack of free pages of which the first *free_count are live.  Pages given back are pushed in
  * (request, page) order, then the missing ones are popped in (request, page) order; memory above the top is left as it is.
+ * Where the table holds no page (E_ARG), -1 is pushed; who pops it gets -1 in its table and slots (E_ARG again).
  * Table entries behind a request's last page are left as they are.
  * Written: block_table, free_pages, free_count_out [1], lens_out [n_req] (= new_lens), cu_new [n_req + 1], and for each of
  * the max_tokens places slot_map (page x 64 + row) and positions (may be NULL), -1 behind the last token.  free_count_out may

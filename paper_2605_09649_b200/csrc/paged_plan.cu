@@ -144,8 +144,12 @@ paged_plan_kernel(int R, const int32_t* old_lens, const int32_t* keep_lens, cons
         const int p = s >= fc ? given_back(s - fc) : free_pages[s];
         return (p >= 0 && p < n_pages) ? p : -1;
     };
-    for (int i = gt; i < (int)back; i += GT) free_pages[fc + i] = given_back(i);
     bool wrong = false;
+    for (int i = gt; i < (int)back; i += GT) {    // (a table entry that is no page keeps its place on the stack, as -1)
+        const int p = given_back(i);
+        free_pages[fc + i] = p >= 0 && p < n_pages ? p : -1;
+        wrong |= p < 0 || p >= n_pages;
+    }
     for (int i = gt; i < (int)taken; i += GT) {
         const int r = plan_find(s_take, R, i), p = taken_page(i);
         table[(size_t)r * W + plan_pages(s_old[r]) + (i - s_take[r])] = p;

@@ -94,6 +94,18 @@ def test_plan_bad_page_in_the_free_list_or_table():
     assert got[0] == [[-1], [99]] and got[5] == [-1, -1, -1, -1]
 
 
+def test_plan_bad_page_given_back():
+    """The call that takes a bad entry from a table reports it, not the request that meets it on the stack later."""
+    for bad in (-1, 5, 1 << 29, -(1 << 31)):
+        got, st = run_plan([130, 3], None, [10, 3], [[0, bad, 2], [1, -3, -3]], [3, 4, -4, -4, -4], 2, 4)      # five pages exist
+        assert st == binding.E_ARG
+        assert got[0] == [[0, bad, 2], [1, -3, -3]] and got[1] == [3, 4, -1, 2, -4] and got[2] == 4
+        assert got[3:] == [[10, 3], [0, 0, 0], [-1] * 4, [-1] * 4]
+    got, st = run_plan([64, 0], None, [0, 65], [[7, -3], [-3, -3]], [1, -4, -4], 1, 65)        # given back and taken in one call
+    assert st == binding.E_ARG
+    assert got[0] == [[7, -3], [-1, 1]] and got[5] == [-1] * 64 + [64]
+
+
 # ---------------------------------------------------------------- append
 
 @pytest.mark.parametrize("H,d,dtype", [(2, 64, torch.float32), (8, 128, torch.bfloat16), (3, 8, torch.bfloat16), (1, 256, torch.float32), (5, 96, torch.bfloat16), (4, 200, torch.bfloat16)])
