@@ -399,7 +399,7 @@ __device__ __forceinline__ int paged_physical(const PagedBatch& pb, const PagedV
 constexpr int PAGED_SMS = 148;
 constexpr int PAGED_WARP_ROWS = 64, PAGED_WARPS = 4;              // warp kernel: rows per unit at most, workers per SM (2 above 16 rows)
 constexpr int PAGED_F32_ROWS = 16, PAGED_F32_CTAS = 2;        // fp32 kernel: rows per unit, CTAs per SM at most
-constexpr int PAGED_TC_ROWS = 256;                                // tensor-core kernel: rows per unit, one CTA per SM
+constexpr int PAGED_TC_ROWS = 256, PAGED_TC_HEAD = 128;           // tensor-core kernel: rows per unit, one CTA per SM; largest head size
 constexpr size_t PAGED_SHARED_BYTES = (size_t)PAGED_SMS * PAGED_WARPS * 16;      // the warp kernel has the most workers
 static_assert(PAGED_SHARED_BYTES % 256 == 0, "partial results are aligned");
 // partial results of `rows` rows (workers x rows per unit), two slots each

@@ -45,14 +45,14 @@ trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
 }
 
 // Workspace: two areas {shared units, partial results}.  The first serves the kernel that a call always has or the
-// only one, the second the tensor-core kernel.  Sizes depend on the head layout alone.
+// only one, the second the tensor-core kernel, where the head size has one.  Sizes depend on the head size alone.
 size_t area_bytes(int rows, int d) { return PAGED_SHARED_BYTES + paged_partial_bytes(rows, d); }
 // The most (workers x rows of a unit) of the first kernels: the fp32 kernel's units are 16 rows; the warp kernel's 8 or 16 with
 // four workers per SM, 32 or 64 with two.
 constexpr int FIRST_ROWS = PAGED_SMS * 2 * PAGED_WARP_ROWS;
 static_assert(PAGED_F32_CTAS * PAGED_F32_ROWS <= 2 * PAGED_WARP_ROWS && PAGED_WARPS * 16 <= 2 * PAGED_WARP_ROWS, "every kernel fits");
 size_t first_area(int d) { return area_bytes(FIRST_ROWS, d); }
-size_t work_bytes(int d) { return first_area(d) + area_bytes(PAGED_SMS * PAGED_TC_ROWS, d); }
+size_t work_bytes(int d) { return first_area(d) + (d <= PAGED_TC_HEAD ? area_bytes(PAGED_SMS * PAGED_TC_ROWS, d) : 0); }
 PagedWork carve(void* area, int rows, int d) {
     char* p = (char*)area;
     PagedWork w;
@@ -167,7 +167,7 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     // tcgen05 kernel; of a batch with both, those of up to 32.  max_new may be wrong: every kernel takes any request, and where
     // both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
-    const bool tc = pv.d <= 128;
+    const bool tc = pv.d <= PAGED_TC_HEAD;
     cudaError_t e = cudaSuccess;
     if (most <= PAGED_WARP_ROWS || !tc) {
         e = launch_paged_attention_warp(pv, pb, q, out, scale, w, most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64, INT_MAX, st);
@@ -222,7 +222,7 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
         pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);
         // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request
-        const bool walk = pv.d <= 128 && pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
+        const bool walk = pv.d <= PAGED_TC_HEAD && pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
         if (walk) {
             PagedBatch pu = pb;
             pu.top = 0;

@@ -109,6 +109,16 @@ def test_workspace_bytes():
         assert binding.paged_workspace_bytes(*bad) == 0
 
 
+def test_workspace_bytes_hold_what_a_head_size_can_use():
+    """Of each kernel: a note of 16 bytes per worker and two partial results (m, l, O in fp32) per row of its workers' units: 148 x 2 x 64
+    rows everywhere, 148 x 256 more where the tensor-core kernel takes the head size (up to 128)."""
+    part = lambda rows, d: 148 * 4 * 16 + 2 * rows * (d + 2) * 4
+    for d in (8, 64, 96, 128):
+        assert 0 <= binding.paged_workspace_bytes(16, 4, d) - part(148 * 128, d) - part(148 * 256, d) < 512, d
+    for d in (136, 192, 256):
+        assert 0 <= binding.paged_workspace_bytes(16, 4, d) - part(148 * 128, d) < 256, d
+
+
 def test_binding_refuses_wrong_tensors():
     kp = torch.zeros(2, 2, PAGE, 64)
     i = torch.zeros(1, dtype=torch.int32)
