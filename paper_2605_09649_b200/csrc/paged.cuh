@@ -70,7 +70,7 @@ struct PagedBatch {
     // second if it has at least PAGED_PICK_ROWS rows and at most pick_pages pages.  0: one kernel takes all requests.
     int pick, pick_top, pick_pages;
     int32_t* status;          // latched status, may be null
-    FastDiv by_g, by_hq, by_h, by_sub, by_sub_rows;
+    FastDiv by_g, by_h, by_sub;
 };
 
 constexpr int PAGED_MAX_REQ = 8192;

@@ -94,7 +94,6 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
     pb->Hq = q_heads;
     pb->g = q_heads / pv.H;
     pb->by_g = FastDiv::by(pb->g);
-    pb->by_hq = FastDiv::by(q_heads);
     pb->by_h = FastDiv::by(pv.H);
     pb->q_stride = q_stride;
     pb->status = status;
@@ -213,7 +212,6 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     pb.sub_rows = pb.g < most ? pb.g : most;
     pb.sub = (pb.g + pb.sub_rows - 1) / pb.sub_rows;
     pb.by_sub = FastDiv::by(pb.sub);
-    pb.by_sub_rows = FastDiv::by(pb.sub_rows);
     if (is_bf16) {
         // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
         // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
