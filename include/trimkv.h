@@ -288,10 +288,13 @@ TRIMKV_API trimkv_status trimkv_shard_compact(trimkv_t* h, int64_t* local_entrie
  *   TRIMKV_TEST_ATTENTION_NO_COPY    the tensor-core decode attention kernel issues none of its asynchronous K/V copies
  *                                    and uses a short limit for its waits: every wait runs out, the kernel latches
  *                                    TRIMKV_E_TIMEOUT and returns with nothing in flight (its output is not written).
- * h != NULL sets the switches of that handle; h == NULL those of the handle-less calls (trimkv_select_topk and
- * trimkv_select_topk_static) for the whole process.  flags = 0 restores normal operation.  Synchronises. */
+ *   TRIMKV_TEST_UNION_OF_PAGES       trimkv_paged_sparse_attention takes the kernel for requests with many tokens wherever it can,
+ *                                    however little it pays.  Outputs are as accurate, the selected pages the same.
+ * h != NULL sets the switches of that handle; h == NULL those of the handle-less calls (trimkv_select_topk,
+ * trimkv_select_topk_static and trimkv_paged_sparse_attention) for the whole process.  flags = 0 restores normal operation.  Synchronises. */
 #define TRIMKV_TEST_DISTRUST_SAMPLE 1
 #define TRIMKV_TEST_ATTENTION_NO_COPY 2
+#define TRIMKV_TEST_UNION_OF_PAGES 4
 TRIMKV_API trimkv_status trimkv_set_test_hooks(trimkv_t* h, int flags);
 
 /* Message of the calling thread's last failed call; never NULL. */

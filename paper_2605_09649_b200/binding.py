@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libtrimkv.so")
 OK, E_ARG, E_STATE, E_NOMEM, E_CUDA, E_NONFINITE, E_TIMEOUT, E_UNSUPPORTED = range(8)
 STATUS_NAMES = ["OK", "E_ARG", "E_STATE", "E_NOMEM", "E_CUDA", "E_NONFINITE", "E_TIMEOUT", "E_UNSUPPORTED"]
 DTYPE_BF16, DTYPE_F32 = 0, 1
-TEST_DISTRUST_SAMPLE, TEST_ATTENTION_NO_COPY = 1, 2     # testing aids, see trimkv_set_test_hooks
+TEST_DISTRUST_SAMPLE, TEST_ATTENTION_NO_COPY, TEST_UNION_OF_PAGES = 1, 2, 4     # testing aids, see trimkv_set_test_hooks
 
 EXPORTS = [
     "trimkv_default_config", "trimkv_create", "trimkv_create_ex", "trimkv_destroy", "trimkv_reset", "trimkv_set_gate",
@@ -366,7 +366,7 @@ class TrimKV:
 
 
 def set_global_test_hooks(flags: int):
-    """Testing aids of the handle-less calls (select_topk, select_topk_static); 0 = normal operation."""
+    """Testing aids of the handle-less calls (select_topk, select_topk_static, paged_sparse_attention); 0 = normal operation."""
     _check(lib().trimkv_set_test_hooks(None, int(flags)))
 
 

@@ -213,12 +213,19 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     pb.sub = (pb.g + pb.sub_rows - 1) / pb.sub_rows;
     pb.by_sub = FastDiv::by(pb.sub);
     if (is_bf16) {
-        // A token's own pages cost their bytes from L2 (measured: 32 KB in about 6 ns over the GPU), a page of a unit's union costs
-        // 256 rows of tensor work (about 6 ns): the union pays while the pages of a request are fewer than top x (tokens
-        // of a unit) = top x 256 / g.  It needs a bit per token of the unit and page.
+        // A token that reads its own pages costs 2.7 ns a page and KV head (out of L2; up to 4.5 from HBM), a unit that walks the union of its
+        // tokens' pages 4 ns for each page up to the request's last, and 30 us a call to begin with, of which every token bears its part:
+        // a request walks the union while its pages are at most pick_pages.  (Fitted to 172 calls: one or two requests of 16 to 512
+        // tokens over 32 to 1024 pages, 1 to 16 query heads per KV head, 8 to 48 pages each, queries independent or alike.  It takes the
+        // faster way or one at most 15 % slower, 1 % on average.  2 x 512 tokens, 8 x 4 heads, top 32, over 256 pages: 412 us, token by token 849;
+        // 2 x 128 tokens, 2 x 8 heads, over 1024 pages: 175, token by token 111.)
+        const long long OWN = 27, UNION = 40, START = 300000;            // tenths of a nanosecond
+        const long long heads = n_tokens * pv.H, gain = heads * std::min(top_pages, table_width) * OWN - START;
+        const bool forced = (global_test_hooks() & TRIMKV_TEST_UNION_OF_PAGES) != 0;
+        // The union needs a bit per token of the unit and page, and room for its list.
         const int unit_tokens = PAGED_TC_ROWS / pb.g + 2 + 1;            // and the union's own row of bits
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
-        pb.pick_pages = (int)std::min<long long>(fit, (long long)top_pages * PAGED_TC_ROWS / pb.g);
+        pb.pick_pages = (int)(forced ? fit : std::min(fit, gain > 0 ? gain * PAGED_TC_ROWS / (heads * UNION * pb.g) : 0LL));
         // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request
         const bool walk = pv.d <= PAGED_TC_HEAD && pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
         if (walk) {

@@ -1030,7 +1030,7 @@ trimkv_status trimkv_shard_compact(trimkv_t* h, int64_t* local_entries_out_host,
 }
 
 trimkv_status trimkv_set_test_hooks(trimkv_t* h, int flags) {
-    if (flags & ~(TRIMKV_TEST_DISTRUST_SAMPLE | TRIMKV_TEST_ATTENTION_NO_COPY)) return fail(TRIMKV_E_ARG, "unknown test hook");
+    if (flags & ~(TRIMKV_TEST_DISTRUST_SAMPLE | TRIMKV_TEST_ATTENTION_NO_COPY | TRIMKV_TEST_UNION_OF_PAGES)) return fail(TRIMKV_E_ARG, "unknown test hook");
     CUDA_TRY(cudaDeviceSynchronize());
     if (h) h->test_hooks = flags;
     else tkv::g_test_hooks.store(flags, std::memory_order_relaxed);

@@ -339,6 +339,48 @@ def test_sparse_attention_tokens_that_share_a_unit():
     check_attention([330], [329], 4, 16, 64, torch.bfloat16, top=2)
 
 
+@pytest.fixture
+def union_forced():
+    binding.set_global_test_hooks(binding.TEST_UNION_OF_PAGES)
+    yield
+    binding.set_global_test_hooks(0)
+
+
+@pytest.mark.parametrize("H,g,d", [(h, g, d) for h, g, d, dtype in LAYOUTS if dtype == torch.bfloat16])
+@pytest.mark.parametrize("top,sink,recent", [(1, 0, 1), (4, 1, 2), (5, 0, 1)])
+def test_sparse_attention_union_of_pages(union_forced, H, g, d, top, sink, recent):
+    """The kernel for requests with many tokens, at sizes where it does not pay by itself."""
+    check_attention([500, 6, 330], [70, 8, 64], H, g, d, torch.bfloat16, top=top, sink=sink, recent=recent, pad=2, stride=True)
+    check_attention([700, 64, 65, 1], [66, 64, 1, 1], H, g, d, torch.bfloat16, top=top, sink=sink, recent=recent)
+
+
+def test_sparse_attention_union_of_pages_over_long_contexts(union_forced):
+    check_attention([3000], [130], 1, 4, 128, torch.bfloat16, top=8, sink=1, recent=1)
+    check_attention([9001, 4000, 12345], [70, 2, 65], 1, 4, 64, torch.bfloat16, top=33)
+    check_attention([420, 390, 130], [200, 101, 130], 2, 4, 64, torch.bfloat16, top=4, sink=1, recent=1, pad=3)
+
+
+def launches(lens, new, H, g, d, top, dtype=torch.bfloat16, seed=11):
+    c = Cache(lens, H, d, dtype, DEV, seed)
+    q, cu = queries(new, H * g, d, dtype, DEV, seed)
+    before = binding.kernel_launches()
+    out, sel = binding.paged_sparse_attention(c.k, c.v, c.bounds, q, ints(cu), c.lens, c.table, top)
+    return binding.kernel_launches() - before, out, sel
+
+
+def test_sparse_attention_union_of_pages_only_where_it_pays():
+    """A short chunk is served by the kernels that serve as many single tokens; a long one by those that the hook asks for, and right."""
+    assert launches([6400], [40], 1, 4, 64, 4)[0] == launches([640] * 40, [1] * 40, 1, 4, 64, 4)[0]
+    few, out, sel = launches([2200], [200], 8, 4, 64, 32)
+    binding.set_global_test_hooks(binding.TEST_UNION_OF_PAGES)
+    try:
+        forced, same, _ = launches([2200], [200], 8, 4, 64, 32)
+    finally:
+        binding.set_global_test_hooks(0)
+    assert few == forced and torch.equal(out, same)
+    check_attention([2200], [200], 8, 4, 64, torch.bfloat16, top=32)
+
+
 # ---------------------------------------------------------------- together
 
 def serve(dtype, H, g, d, top, graph):
