@@ -226,8 +226,14 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
         const int unit_tokens = PAGED_TC_ROWS / pb.g + 2 + 1;            // and the union's own row of bits
         const long long fit = std::min<long long>(PAGED_PICK_PAGES, 32LL * (PAGED_PICK_WORDS / unit_tokens - 1));
         pb.pick_pages = (int)(forced ? fit : std::min(fit, gain > 0 ? gain * PAGED_TC_ROWS / (heads * UNION * pb.g) : 0LL));
-        // some request may have PAGED_PICK_ROWS rows only if the tokens leave it that many beside one for each other request
-        const bool walk = pv.d <= PAGED_TC_HEAD && pb.pick_pages > 0 && (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS;
+        // The host sees no lengths.  Some request surely may have PAGED_PICK_ROWS rows if the tokens leave it that many beside one for each
+        // other request.  Fewer tokens may be a decode step, where the union's kernel finds nothing to do (7 us), or a chunk among requests
+        // without new tokens: it is launched where that is two hundredths of the call (256 single tokens over 2048 entries each 345 to 352 us,
+        // over 8192 408 to 417; 200 tokens of one of 256 requests 152 to 63, 197 to 124), not where it is ten (64 single tokens 92 to
+        // 100; 64 tokens of one of 64 requests would go from 60 to 39 us, over 8192 entries from 76 to 77).
+        const long long DOUBT = 1300000;
+        const bool likely = (n_tokens - n_req + 1) * pb.g >= PAGED_PICK_ROWS || (gain >= DOUBT - START && n_tokens * pb.g >= PAGED_PICK_ROWS);
+        const bool walk = pv.d <= PAGED_TC_HEAD && pb.pick_pages > 0 && likely;
         if (walk) {
             PagedBatch pu = pb;
             pu.top = 0;

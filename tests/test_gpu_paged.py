@@ -381,6 +381,13 @@ def test_sparse_attention_union_of_pages_only_where_it_pays():
     check_attention([2200], [200], 8, 4, 64, torch.bfloat16, top=32)
 
 
+def test_sparse_attention_chunk_among_idle_requests():
+    """Requests without new tokens do not change which kernels serve a chunk."""
+    alone, out, sel = launches([2200], [200], 8, 4, 64, 32)
+    among, out2, sel2 = launches([2200] + [0] * 255, [200] + [0] * 255, 8, 4, 64, 32)
+    assert among == alone and torch.equal(out2, out) and torch.equal(sel2, sel)
+
+
 # ---------------------------------------------------------------- together
 
 def serve(dtype, H, g, d, top, graph):
