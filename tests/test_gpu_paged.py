@@ -1,12 +1,13 @@
 """The caller-owned paged cache on the GPU: plan, append, attention, attention over selected pages, each against a plain
 64-bit statement (tests/util_paged.py), and a run of them together."""
+import math
 import random
 
 import pytest
 import torch
 
 from paper_2605_09649_b200 import binding
-from util_paged import PAGE, Cache, attention, pages, plan, queries
+from util_paged import PAGE, Cache, attention, pages, plan, queries, slack
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -273,6 +274,106 @@ def test_attention_bad_requests_and_pages_are_skipped():
             assert st.item() == binding.E_ARG
 
 
+WIDE = [(2, 4, 256), (1, 8, 192), (3, 5, 136), (1, 40, 200)]                # head sizes above 128, bf16
+
+
+@pytest.mark.parametrize("lens,new", BATCHES)
+@pytest.mark.parametrize("H,g,d", WIDE)
+def test_attention_wide_heads(H, g, d, lens, new):
+    check_attention(lens, new, H, g, d, torch.bfloat16)
+
+
+@pytest.mark.parametrize("H,g,d", WIDE)
+def test_attention_wide_heads_shared_out(H, g, d):
+    """Long requests, whose units several workers share: single tokens, drafts, a chunk, windows."""
+    check_attention([5000, 1], [1, 1], H, g, d, torch.bfloat16, pad=1, stride=True)
+    check_attention([4000, 2100], [3, 1], H, g, d, torch.bfloat16, max_new=0)
+    check_attention([2500], [20], H, g, d, torch.bfloat16, window=1000)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [5, 2, 3]])
+@pytest.mark.parametrize("H,g,d,dtype", [(2, 2, 64, torch.float32), (1, 3, 256, torch.float32), (2, 4, 128, torch.bfloat16), (2, 4, 64, torch.bfloat16), (1, 7, 96, torch.bfloat16)])
+def test_attention_window_over_shared_units(H, g, d, dtype, new):
+    """Windows of many pages: their units are dealt out by pages, and a unit's pages are not as many as the line counts for it."""
+    for window in (1500, 4031):
+        check_attention([9000, 5000, 700], new, H, g, d, dtype, window=window)
+
+
+def without_page(c, q, cu, lens, r_bad, page, scale):
+    """(out, bound) in fp64 where the entries of one page of one request do not count."""
+    H, d = c.k.shape[1], c.k.shape[3]
+    g = q.shape[1] // H
+    out, bound = (torch.zeros(q.shape, dtype=torch.float64) for _ in range(2))
+    for r, total in enumerate(lens):
+        at = torch.arange(total)
+        keep = torch.ones(total, dtype=torch.bool) if r != r_bad else at // PAGE != page
+        phys = torch.where(keep, c.table[r].cpu()[at // PAGE].long(), 0)
+        for h in range(H):
+            k, v = (torch.where(keep[:, None], x.cpu()[phys, h, at % PAGE].double(), 0.0) for x in (c.k, c.v))
+            for t in range(cu[r], cu[r + 1]):
+                see = keep & (at <= total - (cu[r + 1] - t))
+                qq = q[t, h * g:(h + 1) * g].double().cpu()
+                if not see.any():
+                    continue
+                w = torch.softmax((qq @ k.T * scale).masked_fill(~see, -math.inf), -1)
+                o = w @ v
+                out[t, h * g:(h + 1) * g] = o
+                bound[t, h * g:(h + 1) * g] = slack(q.dtype, o, w @ v.abs(), (qq.abs() @ k.abs().T * scale).amax(-1, keepdim=True), total, d)
+    return out, bound
+
+
+@pytest.mark.parametrize("H,g,d,dtype", [(2, 2, 64, torch.float32), (2, 4, 128, torch.bfloat16), (2, 4, 40, torch.bfloat16), (1, 4, 256, torch.bfloat16)])
+@pytest.mark.parametrize("new", [[5, 1], [100, 40], [200, 1]])
+def test_attention_bad_page_of_a_chunk(H, g, d, dtype, new):
+    """An entry of the table that is no page, first, in the middle and last, in drafts and chunks: its entries do not count, the rest does;
+    what the cache's first page holds (NaN here) reaches nobody."""
+    lens = [300, 129]
+    for page, value in ((0, -1), (2, 1 << 29), (4, None)):
+        c = Cache(lens, H, d, dtype, DEV, 31)
+        q, cu = queries(new, H * g, d, dtype, DEV, 31)
+        c.table[0, page] = c.n_pages if value is None else value
+        spare = next(p for p in range(1, c.n_pages) if p not in c.table.flatten().tolist())
+        c.k[spare], c.v[spare] = c.k[0], c.v[0]
+        c.table[c.table == 0] = spare
+        c.k[0], c.v[0] = float("nan"), float("nan")
+        out, st = torch.full(q.shape, 7.0, dtype=dtype, device=DEV), status_word()
+        binding.paged_attention(c.k, c.v, q, ints(cu), c.lens, c.table, max(new), out=out, status=st)
+        want, bound = without_page(c, q, cu, lens, 0, page, d ** -0.5)
+        assert st.item() == binding.E_ARG
+        assert ((out.double().cpu() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_bad_offsets_leave_the_other_requests_right(dtype):
+    H, g, d, lens = 1, 2, 64, [100, 90, 80, 70]
+    c = Cache(lens, H, d, dtype, DEV, 1)
+    q, _ = queries([1, 1, 1, 1], H * g, d, dtype, DEV, 1)
+    # offsets, and the requests with good ones: (request, its rows); rows of no good request stay as they are
+    cases = [([0, 1, 2, 9, 4], [(0, [0]), (1, [1])]),                      # request 2 ends behind the last row, request 3 descends
+             ([0, 1, 3, 2, 4], [(0, [0]), (1, [1, 2]), (3, [2, 3])]),      # request 2 descends; row 2 is claimed twice
+             ([-1, 1, 2, 3, 4], [(1, [1]), (2, [2]), (3, [3])]),           # request 0 begins in front of the first row
+             ([5, 6, 2, 3, 4], [(2, [2]), (3, [3])])]                      # requests 0 and 1 lie behind the last row
+    for cu, good in cases:
+        out, st = torch.full(q.shape, 7.0, dtype=dtype, device=DEV), status_word()
+        binding.paged_attention(c.k, c.v, q, ints(cu), c.lens, c.table, 1, out=out, status=st)
+        assert st.item() == binding.E_ARG, cu
+        owners = {}
+        for r, rows in good:
+            for row in rows:
+                owners.setdefault(row, []).append(r)
+        for row in range(4):
+            if row not in owners:
+                assert (out[row] == 7).all(), (cu, row)
+            elif len(owners[row]) == 1:
+                r = owners[row][0]
+                mine = dict(good)[r]
+                # the request by itself: its rows are the new tokens of a batch of one
+                alone = Cache(lens, H, d, dtype, DEV, 1)
+                want, bound, _ = attention(alone.k, alone.v, q[mine], [0, len(mine)], [lens[r]], alone.table[r:r + 1], d ** -0.5)
+                i = mine.index(row)
+                assert ((out[row].double().cpu() - want[i]).abs() <= bound[i]).all(), (cu, row)
+
+
 # ---------------------------------------------------------------- attention over selected pages
 
 @pytest.mark.parametrize("H,g,d,dtype", LAYOUTS)
@@ -339,6 +440,19 @@ def test_sparse_attention_tokens_that_share_a_unit():
     check_attention([330], [329], 4, 16, 64, torch.bfloat16, top=2)
 
 
+@pytest.mark.parametrize("H,g,d", WIDE)
+@pytest.mark.parametrize("top,sink,recent", [(1, 0, 1), (4, 1, 2), (5, 0, 1)])
+def test_sparse_attention_wide_heads(H, g, d, top, sink, recent):
+    check_attention([700, 64, 0, 1, 65, 257], [1, 1, 0, 1, 1, 1], H, g, d, torch.bfloat16, top=top, sink=sink, recent=recent)
+    check_attention([500, 6, 330], [5, 8, 70], H, g, d, torch.bfloat16, top=top, sink=sink, recent=recent, pad=2, stride=True)
+
+
+def test_sparse_attention_wide_heads_over_long_contexts():
+    check_attention([20000], [1], 1, 8, 256, torch.bfloat16, top=40, sink=2, recent=3)
+    check_attention([9001, 4000, 12345], [1, 2, 1], 2, 4, 192, torch.bfloat16, top=33)
+    check_attention([420, 390, 130], [200, 101, 130], 8, 2, 136, torch.bfloat16, top=4, sink=1, recent=1, pad=3)      # tokens share a unit
+
+
 @pytest.fixture
 def union_forced():
     binding.set_global_test_hooks(binding.TEST_UNION_OF_PAGES)
@@ -379,6 +493,32 @@ def test_sparse_attention_union_of_pages_only_where_it_pays():
         binding.set_global_test_hooks(0)
     assert few == forced and torch.equal(out, same)
     check_attention([2200], [200], 8, 4, 64, torch.bfloat16, top=32)
+
+
+@pytest.mark.parametrize("forced", [False, True])
+@pytest.mark.parametrize("H,g,d,dtype", [(2, 2, 64, torch.float32), (2, 4, 128, torch.bfloat16), (2, 4, 40, torch.bfloat16)])
+def test_sparse_attention_bad_page(H, g, d, dtype, forced):
+    """Among the pages that are always read, an entry that is no page counts for nothing; among the others it is chosen last."""
+    lens, new = [300, 129], [80, 1]
+    for page in (0, 2):
+        c = Cache(lens, H, d, dtype, DEV, 32)
+        q, cu = queries(new, H * g, d, dtype, DEV, 32)
+        c.table[0, page] = 1 << 29
+        st = status_word()
+        binding.set_global_test_hooks(binding.TEST_UNION_OF_PAGES if forced else 0)
+        try:
+            out, sel = binding.paged_sparse_attention(c.k, c.v, c.bounds, q, ints(cu), c.lens, c.table, 5, sink_pages=1, status=st)
+            out4, sel4 = binding.paged_sparse_attention(c.k, c.v, c.bounds, q, ints(cu), c.lens, c.table, 4, sink_pages=1, status=st)
+        finally:
+            binding.set_global_test_hooks(0)
+        assert st.item() == binding.E_ARG
+        want, bound = without_page(c, q, cu, lens, 0, page, d ** -0.5)     # five pages are all there are
+        assert ((out.double().cpu() - want).abs() <= bound).all()
+        if page == 2:                                                      # of pages 1 to 3 of a token on page 4 two are read, 2 is not
+            late = sel4[36:80].cpu()                                       # (positions 256 to 299)
+            assert (late == torch.tensor([0, 1, 3, 4], dtype=I32)).all()
+            see = without_page(c, q, cu, lens, 0, page, d ** -0.5)
+            assert ((out4[36:80].double().cpu() - see[0][36:80]).abs() <= see[1][36:80]).all()
 
 
 def test_sparse_attention_chunk_among_idle_requests():
