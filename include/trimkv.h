@@ -360,7 +360,10 @@ TRIMKV_API trimkv_status trimkv_select_topk_static(const float* scores, int64_t 
  *                padding: neither read nor written.
  *   status       device int32, may be NULL: latched (written only while 0) with what a kernel finds wrong: E_ARG for
  *                lengths, offsets, slots or pages out of range (a request with bad lengths or offsets is skipped, a bad
- *                page or slot too), E_NOMEM where the plan finds too few free pages, E_TIMEOUT where a bounded wait gave up.
+ *                page or slot too; rows that two requests claim are undefined), E_NOMEM where the plan finds too few free
+ *                pages, E_TIMEOUT where a bounded wait gave up.
+ * k, v, q, out, slot_map and positions are 16-byte aligned, strides between tokens are multiples of 16 bytes, the other arrays are
+ * 4-byte aligned.
  * Lengths and tables live on the device, so a captured graph serves every step.  Two calls that may overlap on the GPU
  * need workspaces (and outputs) of their own; contents of a workspace are ignored and may be overwritten after the call.
  * Outputs and workspace overlap no input, but where a call says so.
@@ -415,7 +418,11 @@ TRIMKV_API size_t trimkv_paged_workspace_bytes(int32_t q_heads, int32_t kv_heads
  * zeros.  q: rows of [q_heads, head_dim], q_stride elements apart; out [n_tokens, q_heads, head_dim].  max_new: the most new
  * tokens of one request as far as the host knows; it only guides the choice of kernels (0: not known).
  * Rows of a page behind a request's last entry may hold anything, also NaN.  A NaN or infinity in an entry of the request
- * itself may reach every token that the same call computes for it.  workspace: at least trimkv_paged_workspace_bytes, 256-byte aligned. */
+ * itself may reach every token that the same call computes for it, or weigh nothing; finite values of v are below 2^43.
+ * Sums, softmax statistics and partial results are fp32.  bf16: weights are rounded to bf16 for their product with v (off by
+ * 2^-8 at most, like the output's own rounding), and a third of them may come from a polynomial off by 7.5e-5.  fp32: three
+ * TF32 products for each, 2^-22 relative.  Which kernel serves a request depends on the batch that it is in, and its last bits
+ * with it.  workspace: at least trimkv_paged_workspace_bytes, 256-byte aligned. */
 TRIMKV_API trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t max_new,
                                      int32_t q_heads, const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
                                      const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,
@@ -426,7 +433,12 @@ TRIMKV_API trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache,
  *     U(page) = max over the query heads of the group of sum_c max(q_c lo_c, q_c hi_c)        (lo, hi: key_bounds)
  * -- no key of the page has a larger q . k --, ties to the lower page, NaN first.  U is summed in 64 bits.  A token with at
  * most top_pages pages reads them all.  sink_pages + recent_pages <= top_pages.  selected: int32 [n_tokens, kv_heads,
- * top_pages], the pages read (places in the block-table row), ascending, -1 behind the last. */
+ * top_pages], the pages read (places in the block-table row), ascending, -1 behind the last.
+ * fp32 is refused (E_UNSUPPORTED) where 8 bytes per place of the table and 8 per query head of the group and channel (head_dim
+ * rounded up to 32) exceed 196 KB.
+ * This pays for single tokens over long contexts.  The tokens of a chunk select different pages, most of the context between them,
+ * and reading all of it (trimkv_paged_attention) is the faster call for them up to some hundred pages: for 2 x 512 tokens with
+ * 4 query heads per KV head and 32 pages each up to 512 pages where their queries are alike, still at 1024 where they are not. */
 TRIMKV_API trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int32_t n_req, int64_t n_tokens, int32_t q_heads,
                                             const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
                                             const int32_t* block_table, int32_t table_width, float scale, int32_t top_pages,

@@ -15,7 +15,8 @@
 // m is raised, and O rescaled, when that maximum exceeds it by more than 2^8.  Only the first tile that a row sees finds its
 // maximum beforehand.  Weights above 2^64, a row whose logits leap by that much within one stretch, send the whole stretch
 // round again with the maximum found first in every tile.  A third of the
-// exponentials are evaluated on the FMA pipe.  A unit of 128 rows or fewer leaves group 1 idle.  V rows behind a request's last
+// exponentials are evaluated on the FMA pipe (7.5e-5 relative).  P is rounded to V's type, which both operands of a product share: off
+// by 2^-8 at most, as the output's own rounding; the sum takes the unrounded weights, which are at hand.  A unit of 128 rows or fewer leaves group 1 idle.  V rows behind a request's last
 // entry are zeroed in shared memory before the product reads them (they may hold NaN).  Every wait is bounded; one that runs
 // out latches TRIMKV_E_TIMEOUT.
 //

@@ -274,6 +274,18 @@ def test_attention_bad_requests_and_pages_are_skipped():
             assert st.item() == binding.E_ARG
 
 
+@pytest.mark.parametrize("dtype,d,new", [(torch.bfloat16, 64, 140), (torch.bfloat16, 128, 140), (torch.bfloat16, 128, 3), (torch.bfloat16, 256, 40), (torch.float32, 64, 40)])
+def test_attention_large_values(dtype, d, new):
+    """Values up to 2^43 (randn, times 2^40), with logits that leap: no weight times a value overflows, whatever its reference is."""
+    H, g, n = 1, 4, 900
+    c = Cache([n], H, d, dtype, DEV, 18, spread=4.0)
+    c.v *= 2.0 ** 40
+    q, cu = queries([new], H * g, d, dtype, DEV, 18)
+    out = binding.paged_attention(c.k, c.v, q, ints(cu), c.lens, c.table, new)
+    want, bound, _ = attention(c.k, c.v, q, cu, [n], c.table, d ** -0.5)
+    assert ((out.double().cpu() - want).abs() <= bound).all()
+
+
 WIDE = [(2, 4, 256), (1, 8, 192), (3, 5, 136), (1, 40, 200)]                # head sizes above 128, bf16
 
 
