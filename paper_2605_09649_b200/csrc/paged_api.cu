@@ -217,8 +217,8 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
         // tokens' pages 4 ns for each page up to the request's last, and 30 us a call to begin with, of which every token bears its part:
         // a request walks the union while its pages are at most pick_pages.  (Fitted to 172 calls: one or two requests of 16 to 512
         // tokens over 32 to 1024 pages, 1 to 16 query heads per KV head, 8 to 48 pages each, queries independent or alike.  It takes the
-        // faster way or one at most 15 % slower, 1 % on average.  2 x 512 tokens, 8 x 4 heads, top 32, over 256 pages: 412 us, token by token 849;
-        // 2 x 128 tokens, 2 x 8 heads, over 1024 pages: 175, token by token 111.)
+        // faster way or one at most 15 % slower, 1 % on average.  2 x 512 tokens, 8 x 4 heads, top 32, over 256 pages: 411 us, token by token 827;
+        // 2 x 128 tokens, 2 x 8 heads, over 1024 pages: 173, token by token 111.)
         const long long OWN = 27, UNION = 40, START = 300000;            // tenths of a nanosecond
         const long long heads = n_tokens * pv.H, gain = heads * std::min(top_pages, table_width) * OWN - START;
         const bool forced = (global_test_hooks() & TRIMKV_TEST_UNION_OF_PAGES) != 0;

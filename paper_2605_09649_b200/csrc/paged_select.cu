@@ -19,7 +19,7 @@
 // between (equal bounds, infinities, NaN) all are, and a descent over 64-bit keys decides.  Bound by the latency of its
 // chain (request, table, bounds, descent: 33000 cycles for one token with the scores in shared memory, 26000 in registers); the
 // bounds are read once per group of tokens.  18 us for one token over 2048 pages x 8 heads, 16 us for 32 tokens over up to 256
-// pages (33 MB of bounds: 5 us), 31 us for 256 tokens.
+// pages (33 MB of bounds: 5 us), 30 us for 232 tokens over up to 133.
 //
 // fp32 (paged_select_kernel): fp64 sums for every page, eight lanes per page.
 //
