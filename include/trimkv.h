@@ -362,8 +362,8 @@ TRIMKV_API trimkv_status trimkv_select_topk_static(const float* scores, int64_t 
  *                lengths, offsets, slots or pages out of range (a request with bad lengths or offsets is skipped, a bad
  *                page or slot too; rows that two requests claim are undefined), E_NOMEM where the plan finds too few free
  *                pages, E_TIMEOUT where a bounded wait gave up.
- * k, v, q, out, slot_map and positions are 16-byte aligned, strides between tokens are multiples of 16 bytes, the other arrays are
- * 4-byte aligned.
+ * k, v, q, out, slot_map and positions are 16-byte aligned, strides between tokens are multiples of 16 bytes, the other int32 arrays
+ * are 4-byte aligned.
  * Lengths and tables live on the device, so a captured graph serves every step.  Two calls that may overlap on the GPU
  * need workspaces (and outputs) of their own; contents of a workspace are ignored and may be overwritten after the call.
  * Outputs and workspace overlap no input, but where a call says so.
