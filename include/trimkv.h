@@ -445,6 +445,53 @@ TRIMKV_API trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache*
                                             int32_t sink_pages, int32_t recent_pages, int32_t* selected, void* out, void* workspace,
                                             size_t workspace_bytes, int32_t* status, void* stream);
 
+/* ---- the paged cache in 4 bits -----------------------------------------------------------------------
+ * The same pages, tables, lengths, slot maps and rules as above, with keys and values held in 4.5 bits.  (No counterpart in the paper.)
+ * 16 neighbouring channels of an entry and KV head share a scale; a value is  code x scale x 2^shift,  code one of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 with a sign (e2m1), scale an e4m3 number.
+ *   codes    uint8 [n_pages, kv_heads, 64, head_dim / 2]: channel 2 i in the low half of byte i, channel 2 i + 1 in the high half
+ *   scales   e4m3 bytes [n_pages, kv_heads, 64, head_dim / 16]
+ *   shift    int32 [kv_heads], device memory, or NULL (0): the powers of two that bring a head's values, largest over 16 channels, into
+ *            the range of the scales (0.1 to 2688 with full precision).  Taken as -64 or 64 beyond these.
+ * A fifth to a quarter of the bytes of bf16: 0.28.  The values of a block are off by a quarter of the scale where they are
+ * small (code x scale up to 2), by a half or a whole one above: scale is a sixth of the block's largest magnitude. */
+typedef struct trimkv_paged4_cache {
+    void* k_codes;             /* these four 16-byte aligned */
+    void* k_scales;
+    void* v_codes;
+    void* v_scales;
+    const int32_t* k_shift;    /* or NULL */
+    const int32_t* v_shift;
+    int32_t n_pages;
+    int32_t kv_heads;
+    int32_t head_dim;          /* a multiple of 32, at most 256 */
+    int32_t page_size;         /* must be 64 */
+    int32_t reserved;          /* must be 0 */
+} trimkv_paged4_cache;
+
+/* Rounds k and v (dtype TRIMKV_DTYPE_BF16 or TRIMKV_DTYPE_F32; rows and strides as in trimkv_paged_append) into slot slot_map[t] of the
+ * cache; -1 skips a token; no slot is given twice.  With x' = x 2^-shift: scale = e4m3(max |x'| / 6), the quotient in fp32, to nearest even, at most 448;
+ * code = e2m1(x' / scale), to nearest, ties to the code whose mantissa is 0, at most 6 in magnitude; codes 0 where the
+ * scale is 0.  A block that holds a NaN becomes NaN; infinities become the largest value. */
+TRIMKV_API trimkv_status trimkv_paged4_append(const trimkv_paged4_cache* cache, int32_t dtype, int64_t n_tokens, const void* k, int64_t k_stride,
+                                   const void* v, int64_t v_stride, const int32_t* slot_map, int32_t* status, void* stream);
+
+/* The values that slots hold: k and v [n_slots, kv_heads, head_dim] in dtype, 16-byte aligned; exact in either (up to where a value times
+ * 2^shift leaves fp32's range).  -1: zeros.  A slot may be given any number of times. */
+TRIMKV_API trimkv_status trimkv_paged4_read(const trimkv_paged4_cache* cache, int32_t dtype, int64_t n_slots, const int32_t* slot_map, void* k,
+                                 void* v, int32_t* status, void* stream);
+
+/* Scratch of trimkv_paged4_attention, in bytes; 0 for a head layout that it refuses. */
+TRIMKV_API size_t trimkv_paged4_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+
+/* trimkv_paged_attention over a cache in 4 bits: the same arguments and rules, q and out in dtype.  The values of the cache enter the
+ * products exactly.  q is below 2^70.  bf16: weights are rounded to fp16 for their product with v (off by 2^-11 at most; weights below
+ * 2^-21 of a row's largest by 2^-32 of that).  fp32: q and the weights in two fp16 parts each, 2^-22 relative. */
+TRIMKV_API trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t dtype, int32_t n_req, int64_t n_tokens, int32_t max_new,
+                                      int32_t q_heads, const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
+                                      const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,
+                                      void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

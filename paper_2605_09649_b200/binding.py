@@ -31,6 +31,7 @@ EXPORTS = [
     "trimkv_shard_resolve", "trimkv_shard_hist", "trimkv_shard_digit", "trimkv_shard_mark", "trimkv_shard_compact",
     "trimkv_paged_plan", "trimkv_paged_append", "trimkv_paged_workspace_bytes", "trimkv_paged_attention",
     "trimkv_paged_sparse_attention",
+    "trimkv_paged4_append", "trimkv_paged4_read", "trimkv_paged4_workspace_bytes", "trimkv_paged4_attention",
 ]
 
 
@@ -57,6 +58,15 @@ class PagedCache(C.Structure):
         ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("key_bounds", C.c_void_p), ("n_pages", C.c_int32),
         ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32), ("page_size", C.c_int32),
         ("reserved", C.c_int32),
+    ]
+
+
+class Paged4CacheFields(C.Structure):
+    """trimkv_paged4_cache: the arrays of a caller-owned cache in 4 bits."""
+    _fields_ = [
+        ("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+        ("k_shift", C.c_void_p), ("v_shift", C.c_void_p), ("n_pages", C.c_int32), ("kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("page_size", C.c_int32), ("reserved", C.c_int32),
     ]
 
 
@@ -134,6 +144,11 @@ def lib() -> C.CDLL:
     L.trimkv_paged_workspace_bytes.argtypes = [i32, i32, i32]
     L.trimkv_paged_workspace_bytes.restype = sz
     L.trimkv_paged_attention.argtypes = [pc, i32, i64, i32, i32, vp, i64, vp, vp, vp, i32, f32, i32, vp, vp, sz, vp, vp]
+    L.trimkv_paged4_append.argtypes = [pc, i32, i64, vp, i64, vp, i64, vp, vp, vp]      # pc: trimkv_paged4_cache* likewise
+    L.trimkv_paged4_read.argtypes = [pc, i32, i64, vp, vp, vp, vp, vp]
+    L.trimkv_paged4_workspace_bytes.argtypes = [i32, i32, i32]
+    L.trimkv_paged4_workspace_bytes.restype = sz
+    L.trimkv_paged4_attention.argtypes = [pc, i32, i32, i64, i32, i32, vp, i64, vp, vp, vp, i32, f32, i32, vp, vp, sz, vp, vp]
     L.trimkv_paged_sparse_attention.argtypes = [pc, i32, i64, i32, vp, i64, vp, vp, vp, i32, f32, i32, i32, i32, vp, vp, vp,
                                                 sz, vp, vp]
     for name in ("trimkv_create_ex", "trimkv_reset", "trimkv_set_gate", "trimkv_set_shared_projection", "trimkv_gate",
@@ -514,7 +529,7 @@ def paged_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().trimkv_paged_workspace_bytes(q_heads, kv_heads, head_dim))
 
 
-def _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspace, status):
+def _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspace, status, workspace_bytes=paged_workspace_bytes):
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, q_heads, head_dim]")
     shape = q.shape
@@ -527,7 +542,7 @@ def _paged_batch(n, dt, h, d, q, cu_new, lens, block_table, scale, out, workspac
     if out is None:
         out = torch.empty(shape, dtype=dt, device=q.device)
     if workspace is None:
-        workspace = torch.empty(max(256, paged_workspace_bytes(hq, h, d)), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(256, workspace_bytes(hq, h, d)), dtype=torch.uint8, device=q.device)
     size = workspace.numel()
     batch = (qp, qs, _ints(n, "cu_new", cu_new, r + 1), _ints(n, "lens", lens, r), _ints(n, "block_table", block_table, r * w), w,
              d ** -0.5 if scale is None else scale)
@@ -559,3 +574,78 @@ def paged_sparse_attention(k_pages, v_pages, key_bounds, q, cu_new, lens, block_
     sel = _on(n, "selected", selected, torch.int32, (t, h, top_pages))
     _launch(lib().trimkv_paged_sparse_attention, n, cache, r, t, hq, *batch, top_pages, sink_pages, recent_pages, sel, *tail)
     return out, selected
+
+
+# ---- the caller-owned paged cache in 4 bits (trimkv_paged4_*)
+_pack_cache4 = struct.Struct("PPPPPPiiiii4x").pack      # Paged4CacheFields, field by field
+
+
+class Paged4Cache:
+    """A layer's cache in 4 bits: k_codes, v_codes uint8 [n_pages, H, 64, d / 2], k_scales, v_scales float8_e4m3fn (or their bytes)
+    [n_pages, H, 64, d / 16], k_shift, v_shift int32 [H] or None.  Holds the tensors; checked once, here."""
+
+    __slots__ = ("fields", "index", "heads", "head_dim", "tensors")
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, k_shift=None, v_shift=None):
+        index, shape = k_codes.get_device(), k_codes.shape
+        if index < 0:
+            raise ValueError("expected a CUDA tensor")
+        if len(shape) != 4:
+            raise ValueError("k_codes: expected uint8 [n_pages, kv_heads, 64, head_dim / 2]")
+        n, h, page, half = shape
+        scales = (n, h, page, half // 8)
+
+        def bytes_of(name, t):
+            return _on(index, name, t, torch.float8_e4m3fn if t.dtype is torch.float8_e4m3fn else torch.uint8, scales)
+
+        self.fields = _pack_cache4(_on(index, "k_codes", k_codes, torch.uint8, shape), bytes_of("k_scales", k_scales),
+                                   _on(index, "v_codes", v_codes, torch.uint8, shape), bytes_of("v_scales", v_scales),
+                                   0 if k_shift is None else _ints(index, "k_shift", k_shift, h),
+                                   0 if v_shift is None else _ints(index, "v_shift", v_shift, h), n, h, 2 * half, page, 0)
+        self.index, self.heads, self.head_dim = index, h, 2 * half
+        self.tensors = (k_codes, k_scales, v_codes, v_scales, k_shift, v_shift)
+
+
+def _value_dtype(name, t):
+    if t.dtype not in _KV_DTYPES:
+        raise ValueError(f"{name}: expected bf16 or fp32, got {t.dtype}")
+    return t.dtype
+
+
+def paged4_append(cache: Paged4Cache, k, v, slot_map, status=None):
+    """Rounds k and v [tokens, H, d] (bf16 or fp32, rows may be strided) into the slots of slot_map [tokens] (trimkv_paged4_append)."""
+    n, h, d, dt = cache.index, cache.heads, cache.head_dim, _value_dtype("k", k)
+    kp, ks, t = _rows(n, "k", k, dt, h, d)
+    vp, vs, tv = _rows(n, "v", v, dt, h, d)
+    if tv != t:
+        raise ValueError("k and v hold different numbers of tokens")
+    _launch(lib().trimkv_paged4_append, n, cache.fields, _KV_DTYPES[dt], t, kp, ks, vp, vs, _ints(n, "slot_map", slot_map, t),
+            None if status is None else _ints(n, "status", status, 1))
+
+
+def paged4_read(cache: Paged4Cache, slot_map, k=None, v=None, *, dtype=torch.bfloat16, status=None):
+    """The values that the slots of slot_map [n] hold (trimkv_paged4_read): (k, v) [n, H, d]."""
+    n, t, device = cache.index, slot_map.numel(), slot_map.device
+    if k is not None:
+        dtype = _value_dtype("k", k)
+    shape = (t, cache.heads, cache.head_dim)
+    k = torch.empty(shape, dtype=dtype, device=device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=device) if v is None else v
+    _launch(lib().trimkv_paged4_read, n, cache.fields, _KV_DTYPES[_value_dtype("k", k)], t, _ints(n, "slot_map", slot_map, t), _on(n, "k", k, dtype, shape),
+            _on(n, "v", v, dtype, shape), None if status is None else _ints(n, "status", status, 1))
+    return k, v
+
+
+def paged4_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().trimkv_paged4_workspace_bytes(q_heads, kv_heads, head_dim))
+
+
+def paged4_attention(cache: Paged4Cache, q, cu_new, lens, block_table, max_new: int = 0, *, scale: Optional[float] = None, window: int = 0,
+                     out=None, workspace=None, status=None):
+    """Causal attention of the new tokens q [tokens, Hq, d] (bf16 or fp32) over a caller-owned paged cache in 4 bits (trimkv_paged4_attention)."""
+    _small(max_new=max_new, window=window)
+    n, dt = cache.index, _value_dtype("q", q)
+    r, t, hq, batch, tail, out = _paged_batch(n, dt, cache.heads, cache.head_dim, q, cu_new, lens, block_table, scale, out, workspace, status,
+                                              paged4_workspace_bytes)
+    _launch(lib().trimkv_paged4_attention, n, cache.fields, _KV_DTYPES[dt], r, t, max_new, hq, *batch, window, *tail)
+    return out

@@ -1,0 +1,102 @@
+// C entry points of the paged cache held in 4 bits: argument checks, workspace layout, choice of kernels.
+#include <limits.h>
+
+#include "paged4.cuh"
+#include "paged_check.cuh"
+
+using namespace tkv;
+
+namespace {
+
+trimkv_status check_cache4(const trimkv_paged4_cache* c, int32_t dtype, Paged4View* v) {
+    if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return refuse(TRIMKV_E_ARG, "cache, codes and scales must not be NULL");
+    if (c->reserved != 0) return refuse(TRIMKV_E_ARG, "reserved must be 0");
+    if (dtype != TRIMKV_DTYPE_BF16 && dtype != TRIMKV_DTYPE_F32) return refuse(TRIMKV_E_ARG, "unknown dtype %d", dtype);
+    if (c->page_size != PAGE) return refuse(TRIMKV_E_UNSUPPORTED, "page_size must be %d", PAGE);
+    if (c->n_pages < 1 || c->n_pages > TRIMKV_PAGED_MAX_PAGES) return refuse(TRIMKV_E_ARG, "n_pages must be in [1, %d]", TRIMKV_PAGED_MAX_PAGES);
+    if (c->kv_heads < 1 || c->kv_heads > 1024) return refuse(TRIMKV_E_ARG, "kv_heads must be in [1, 1024]");
+    if (c->head_dim < 32 || c->head_dim % 32 || c->head_dim > 256) return refuse(TRIMKV_E_UNSUPPORTED, "head_dim must be a multiple of 32 up to 256");
+    if ((long long)c->n_pages * c->kv_heads * PAGE > INT_MAX) return refuse(TRIMKV_E_UNSUPPORTED, "n_pages x kv_heads x %d must be below 2^31", PAGE);
+    if (!ok16(c->k_codes) || !ok16(c->k_scales) || !ok16(c->v_codes) || !ok16(c->v_scales)) return refuse(TRIMKV_E_ARG, "codes and scales must be 16-byte aligned");
+    if (!ok4(c->k_shift) || !ok4(c->v_shift)) return refuse(TRIMKV_E_ARG, "shifts must be 4-byte aligned");
+    *v = Paged4View{};
+    v->pv.n_pages = c->n_pages;
+    v->pv.H = c->kv_heads;
+    v->pv.d = c->head_dim;
+    v->codes[0] = (const uint8_t*)c->k_codes;
+    v->codes[1] = (const uint8_t*)c->v_codes;
+    v->scales[0] = (const uint8_t*)c->k_scales;
+    v->scales[1] = (const uint8_t*)c->v_scales;
+    v->shift[0] = c->k_shift;
+    v->shift[1] = c->v_shift;
+    return TRIMKV_OK;
+}
+
+// Workspace: {shared units, partial results} of the warp kernel.
+size_t work_bytes4(int d) { return P4_SHARED_BYTES + paged_partial_bytes(P4_WORKER_ROWS, d); }
+PagedWork carve4(void* area, size_t shared_bytes, int rows, int d) {
+    PagedWork w;
+    w.shared = (int4*)area;
+    w.part_o = (float*)((char*)area + shared_bytes);
+    w.part_ml = w.part_o + (size_t)2 * rows * d;
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+trimkv_status trimkv_paged4_append(const trimkv_paged4_cache* cache, int32_t dtype, int64_t n_tokens, const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, const int32_t* slot_map, int32_t* status, void* stream) {
+    Paged4View c;
+    const trimkv_status s = check_cache4(cache, dtype, &c);
+    if (s != TRIMKV_OK) return s;
+    if (n_tokens < 0 || n_tokens * c.pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
+    if (n_tokens == 0) return TRIMKV_OK;
+    const int elt = dtype == TRIMKV_DTYPE_BF16 ? 2 : 4;
+    if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
+    const int64_t row = (int64_t)c.pv.H * c.pv.d;
+    if (k_stride < row || v_stride < row || k_stride > (1LL << 31) || v_stride > (1LL << 31) || (k_stride * elt) % 16 || (v_stride * elt) % 16)
+        return refuse(TRIMKV_E_ARG, "k_stride and v_stride must cover a token's row and be multiples of 16 bytes");
+    return done(launch_paged4_append(c, elt == 2, (int)n_tokens, k, k_stride, v, v_stride, slot_map, status, (cudaStream_t)stream), "append");
+}
+
+trimkv_status trimkv_paged4_read(const trimkv_paged4_cache* cache, int32_t dtype, int64_t n_slots, const int32_t* slot_map, void* k, void* v, int32_t* status,
+                                 void* stream) {
+    Paged4View c;
+    const trimkv_status s = check_cache4(cache, dtype, &c);
+    if (s != TRIMKV_OK) return s;
+    if (n_slots < 0 || n_slots * c.pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_slots x kv_heads must be in [0, 2^30]");
+    if (n_slots == 0) return TRIMKV_OK;
+    if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
+    return done(launch_paged4_read(c, dtype == TRIMKV_DTYPE_BF16, (int)n_slots, slot_map, k, v, status, (cudaStream_t)stream), "read");
+}
+
+size_t trimkv_paged4_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+    if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads || head_dim < 32 || head_dim > 256 || head_dim % 32 || q_heads / kv_heads > 128) return 0;
+    return work_bytes4(head_dim);
+}
+
+trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t dtype, int32_t n_req, int64_t n_tokens, int32_t max_new, int32_t q_heads,
+                                      const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens, const int32_t* block_table,
+                                      int32_t table_width, float scale, int32_t window, void* out, void* workspace, size_t workspace_bytes,
+                                      int32_t* status, void* stream) {
+    Paged4View c;
+    PagedBatch pb;
+    trimkv_status s = check_cache4(cache, dtype, &c);
+    if (s != TRIMKV_OK) return s;
+    const int is_bf16 = dtype == TRIMKV_DTYPE_BF16;
+    s = paged_check_batch(c.pv, is_bf16, work_bytes4(c.pv.d), n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace,
+                          workspace_bytes, status, &pb);
+    if (s != TRIMKV_OK) return s;
+    if (window < 0 || window > (1 << 30)) return refuse(TRIMKV_E_ARG, "window must be in [0, 2^30]");
+    if (max_new < 0) return refuse(TRIMKV_E_ARG, "max_new must not be negative");
+    if (n_tokens == 0) return TRIMKV_OK;
+    pb.window = window;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const PagedWork w = carve4(workspace, P4_SHARED_BYTES, P4_WORKER_ROWS, c.pv.d);
+    const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
+    return done(launch_paged4_attention_warp(c, pb, is_bf16, q, out, scale, w, most <= 8 ? 8 : 16, INT_MAX, st), "attention");
+}
+
+}  // extern "C"

@@ -1,0 +1,493 @@
+// Attention over the paged cache held in 4 bits, for few query rows (and for fp32 and head sizes above 128, any number).
+//
+// One CTA per SM, independent warps, each with a ring of its own in shared memory that bulk copies fill with 32 entries at a time: codes
+// and scales of K and of V.  A warp takes an equal share of the line of page steps (paged.cuh) and computes S^T = K Q^T and
+// O^T += V^T P^T with mma.sync m16n8k16 in fp16, the (token, head) rows as the N dimension: fp16 holds every value of the cache
+// exactly (paged4.cuh), and Q once each row is scaled by a power of two (its largest value in 2^10 .. 2^11; what is lost of the
+// smallest ones is 2^-35 of the largest).  fp32: Q and P in two fp16 parts each, 2^-22 relative, and sums of a tile apart.
+//
+// The operands are made in registers.  K (A operand, rows = entries): a thread takes d / 4 neighbouring channels of an entry, so the order of
+// channels along k is a permutation, which Q follows; a word of codes is the A registers of two products.  V (A operand, rows =
+// channels): a thread takes d / 8 neighbouring channels of entries in pairs, and three-input logic puts the codes of one channel
+// of two entries into a byte, which one conversion makes the register.  Each register is then multiplied by its scale (of two entries for V).
+// A thread's 2 x 32 channels and scales of 16 entries cost about 200 instructions.
+//
+// The reference of a row's weights lags its maximum by up to 2^8, and weights are 2^7 times their value: at most 2^15, and what
+// fp16 cannot hold is below 2^-32 of the row's largest weight.
+// Entries behind the request's last one: any code is finite, so only their scales are put to zero (for V; K's products are masked).
+// Every wait is bounded: on expiry the warp latches TRIMKV_E_TIMEOUT, drains its copies and returns.
+#include "async_copy.cuh"
+#include "mma_sync.cuh"
+#include "paged4.cuh"
+#include "tcgen05_attn.cuh"
+
+namespace tkv {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
+constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
+
+template <int D, int NT>
+struct Warp4Shape {
+    static constexpr int WARPS = P4_WARPS;
+    static constexpr int ROWS = NT * 8;                               // rows of a unit
+    static constexpr int TILE = 32;                                   // entries per stage
+    static constexpr int STAGE = TILE * (D / 2 + D / 16) * 2;         // K codes, K scales, V codes, V scales
+    static constexpr int STAGES = D == 256 ? 2 : D == 128 ? 5 : 8;
+    static constexpr int OFF_BAR = WARPS * STAGES * STAGE;
+    static constexpr int OFF_META = OFF_BAR + WARPS * STAGES * 8;
+    static constexpr int OFF_TAB = (OFF_META + WARPS * STAGES * 4 + 15) & ~15;
+    static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 128;       // 128: alignment slack
+    static_assert(SMEM <= 227 * 1024, "shared memory of one SM");
+    static_assert(WARPS * ROWS * PAGED_SMS <= P4_WORKER_ROWS, "the workspace holds the workers' partial results");
+};
+
+__device__ __forceinline__ void w4_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Entry that row r (0 .. 15) of a product's 16 stands for: neighbours and every second row fall on both halves of the 32 banks.
+__device__ __forceinline__ int w4_entry(int r) { return r ^ ((r >> 1) & 1); }
+template <int BYTES>
+__device__ __forceinline__ void w4_load(uint32_t* w, const unsigned char* p) {
+    if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    if constexpr (BYTES == 8) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
+    if constexpr (BYTES == 16) { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+}
+__device__ __forceinline__ float w4_exp2(float x, std::false_type) { return a_ex2(x); }
+__device__ __forceinline__ float w4_exp2(float x, std::true_type) { return exp2f(x); }
+__device__ __forceinline__ void w4_load8(float (&v)[8], const __nv_bfloat16* p) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(&u)[i >> 1];
+        v[i] = __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    }
+}
+__device__ __forceinline__ void w4_load8(float (&v)[8], const float* p) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void w4_store8(__nv_bfloat16* p, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void w4_store8(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// A place on the line and the stretch of a unit that begins there.
+struct Warp4Cursor {
+    long long x;
+    PagedItem it;
+    int ntile;          // tiles to read
+    bool on;
+};
+
+// Head size pv.d, a multiple of 32, at most D.  T: type of q and out.
+template <int D, int NT, typename T>
+__global__ void __launch_bounds__(Warp4Shape<D, NT>::WARPS * 32, 1)
+paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, float scale_log2, PagedWork wk, int max_rows) {
+    using S = Warp4Shape<D, NT>;
+    constexpr bool F32 = sizeof(T) == 4;
+    using Exact = std::integral_constant<bool, F32>;
+    constexpr int KS = D / 16, MT = S::TILE / 16, PARTS = F32 ? 2 : 1;
+    constexpr int KW = D / 32, VW = D / 64;                           // words of codes that a thread takes of an entry's K, and of its V
+    extern __shared__ unsigned char w4_smem_raw[];
+    unsigned char* smem = w4_smem_raw + ((128u - (smem_u32(w4_smem_raw) & 127u)) & 127u);
+    const PagedView& pv = cache.pv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = pv.d, gq = lane >> 2, tq = lane & 3;
+    unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + warp * S::STAGES;
+    volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + warp * S::STAGES;      // first entry of the stage's tile; -1: skip
+    PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
+    const int code_row = d / 2, scale_row = d / 16;
+    const int off_ks = S::TILE * code_row, off_vc = off_ks + S::TILE * scale_row, off_vs = off_vc + off_ks;       // within a stage
+
+    if (lane == 0)
+        for (int s = 0; s < S::STAGES; ++s) mbar_init(bars + s, 1);
+    fence_proxy_async_smem();
+    grid_dependency_wait();
+    PagedTable tab;
+    paged_build_table<0>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::WARPS, 4, W4_JOIN_STEPS, table_mem);      // (synchronises the block)
+    grid_dependents_may_launch();
+    const int w = warp * (int)gridDim.x + (int)blockIdx.x;            // workers are spread over the SMs first
+    if (lane == 0) paged_note_none(wk, w);
+    if (w >= tab.workers) return;
+    const long long end = tab.share(w + 1);
+
+    auto at = [&](long long x) {
+        Warp4Cursor c;
+        c.x = x;
+        c.ntile = 0;
+        c.on = x < end;
+        if (!c.on) return c;
+        c.it = paged_item<0>(tab, pb, x, end, w);
+        c.ntile = 2 * (c.it.p1 - c.it.p0);
+        if (c.ntile) {                                                // the second half of the last token's page may lie behind what is seen
+            const int phi = c.it.q.len - c.it.q.n + c.it.tok1;
+            if (c.it.p1 == phi / PAGE + 1 && phi % PAGE < S::TILE) --c.ntile;
+        }
+        return c;
+    };
+    Warp4Cursor cons = at(tab.share(w)), prod = cons;
+    int prod_tile = 0, phys_page = 0;                                 // lane l: page l of the current run of 32
+    unsigned issued = 0, consumed = 0;
+    bool failed = false;
+
+    auto issue_one = [&]() {
+        while (prod.on && prod_tile == prod.ntile) { prod = at(prod.x + prod.it.steps); prod_tile = 0; }
+        if (!prod.on) return;
+        if (prod_tile % 64 == 0) {                                    // the next 32 pages
+            const int p = prod.it.p0 + prod_tile / 2 + lane;
+            phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, p) : -1;
+        }
+        const int pp = __shfl_sync(0xffffffffu, phys_page, (prod_tile / 2) & 31), half = prod_tile & 1;
+        const unsigned s = issued % S::STAGES;
+        if (lane == 0) {
+            meta[s] = pp < 0 ? -1 : (prod.it.p0 + prod_tile / 2) * PAGE + half * S::TILE;
+            if (pp < 0) {
+                mbar_arrive(bars + s);
+            } else {
+                unsigned char* dst = ring + s * S::STAGE;
+                const size_t row = ((size_t)pp * pv.H + prod.it.h) * PAGE + half * S::TILE;
+                mbar_expect_tx(bars + s, 2 * off_vc);                 // (the zeroing of scales below carries its own proxy fence)
+                bulk_g2s(dst, cache.codes[0] + row * code_row, off_ks, bars + s);
+                bulk_g2s(dst + off_ks, cache.scales[0] + row * scale_row, S::TILE * scale_row, bars + s);
+                bulk_g2s(dst + off_vc, cache.codes[1] + row * code_row, off_ks, bars + s);
+                bulk_g2s(dst + off_vs, cache.scales[1] + row * scale_row, S::TILE * scale_row, bars + s);
+            }
+        }
+        ++issued;
+        ++prod_tile;
+    };
+    for (int s = 0; s < S::STAGES - 1; ++s) issue_one();
+
+    uint32_t bq[NT][PARTS][KS][2];
+    float o[NT][KS][4];
+    float m_run[NT][2], l_run[NT][2], to_log2[NT][2];
+
+    while (cons.on && !failed) {
+        const PagedItem& it = cons.it;
+        const int row_first = paged_unit_first<0>(pb, it.u, S::ROWS), rows = paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS);
+        const int ksh = p4_shift(cache, 0, it.h);
+        // ---- Q fragments (B operand: k = channel, n = row): row gq of a column tile, channels tq d / 4 ..
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = nt * 8 + gq, qr = row_first + row;
+            const int qt = row < rows ? pb.by_g.div(qr) : 0, qj = row < rows ? qr - qt * g : 0;
+            const T* p = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + tq * (D / 4);
+            float top = 0.f;
+            auto load = [&](float (&v)[8], int c) {
+                if (row < rows && tq * (D / 4) + c < d) w4_load8(v, p + c);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            };
+#pragma unroll
+            for (int c = 0; c < D / 4; c += 8) {
+                float v[8];
+                load(v, c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int up = top > 0.f ? max(-60, min(60, 137 - (int)(__float_as_uint(top) >> 23))) : 0;
+            const float f = p4_pow2(up);
+#pragma unroll
+            for (int c = 0; c < D / 4; c += 8) {
+                float v[8];
+                load(v, c);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float x0 = v[e] * f, x1 = v[e + 1] * f;
+                    const uint32_t hi = p4_f16x2(x0, x1);
+                    bq[nt][0][c / 4 + e / 4][(e >> 1) & 1] = hi;
+                    if constexpr (F32) {
+                        const float2 b = p4_float2(hi);
+                        bq[nt][1][c / 4 + e / 4][(e >> 1) & 1] = p4_f16x2(x0 - b.x, x1 - b.y);
+                    }
+                }
+            }
+            const float back = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));      // of row gq; this thread's columns are 2 tq, + 1
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                to_log2[nt][c] = __shfl_sync(0xffffffffu, back, (2 * tq + c) * 4);
+                m_run[nt][c] = -INFINITY;
+                l_run[nt][c] = 0.f;
+            }
+#pragma unroll
+            for (int dt = 0; dt < KS; ++dt) o[nt][dt][0] = o[nt][dt][1] = o[nt][dt][2] = o[nt][dt][3] = 0.f;
+        }
+        int all_lo, all_hi;                                           // entries that every row of the unit sees, from its first and last row
+        {
+            const int p0 = it.q.len - it.q.n + pb.by_g.div(row_first), p1 = it.q.len - it.q.n + pb.by_g.div(max(row_first + rows - 1, 0));
+            all_hi = max(p0 + 1, 0);
+            all_lo = pb.window > 0 ? max(p1 + 1 - pb.window, 0) : 0;
+        }
+
+        for (int tt = 0; tt < cons.ntile; ++tt) {
+            issue_one();                                              // refill the stage freed by the previous tile
+            const unsigned s = consumed % S::STAGES;
+            if (!mbar_wait_bounded(bars + s, (consumed / S::STAGES) & 1u)) { failed = true; break; }
+            ++consumed;
+            const int e0 = meta[s];
+            if (e0 < 0) { __syncwarp(); continue; }                   // a page that does not exist
+            unsigned char* tile = ring + s * S::STAGE;
+            const int held = it.q.len - e0;                           // entries of the tile, if it is not full
+            if (held < S::TILE) {
+                for (int i = max(held, 0) * scale_row + lane; i < S::TILE * scale_row; i += 32) tile[off_vs + i] = 0;
+                fence_proxy_async_smem();                             // before a later copy into this stage
+                __syncwarp();
+            }
+            // ---- S^T[entry][row] = K Q^T
+            float sacc[MT][NT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) sacc[mt][nt][0] = sacc[mt][nt][1] = sacc[mt][nt][2] = sacc[mt][nt][3] = 0.f;
+                uint32_t kw[2][KW], ks[2][(KW + 3) / 4 * 2];           // rows gq and gq + 8: codes; scales, both halves of a register alike
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int e = mt * 16 + i * 8 + w4_entry(gq);
+                    const unsigned char* cp = tile + e * code_row + tq * (D / 8);
+                    const unsigned char* sp = tile + off_ks + e * scale_row + tq * (D / 64);
+#pragma unroll
+                    for (int c = 0; c < KW; c += 4) {                 // (KW = 2 for heads of 64)
+                        const bool on = tq * (D / 4) + c * 8 < d;     // the padded channels: codes 0
+#pragma unroll
+                        for (int x = 0; x < 4 && c + x < KW; ++x) kw[i][c + x] = 0u;
+                        uint32_t two = 0u;
+                        if (on) {
+                            w4_load<KW == 2 ? 8 : 16>(&kw[i][c], cp + c * 4);
+                            two = KW == 2 ? (uint32_t)sp[0] : (uint32_t)*reinterpret_cast<const uint16_t*>(sp + c / 2);
+                        }
+                        const uint32_t sc = p4_scales(two);
+                        ks[i][c / 2] = p4_both_low(sc);
+                        if (KW > 2) ks[i][c / 2 + 1] = p4_both_high(sc);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < KW; ++x) {                        // a word of each row: two products
+                    uint32_t r0[4], r1[4];
+                    p4_codes(kw[0][x], r0);
+                    p4_codes(kw[1][x], r1);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t a[4];
+                        a[0] = p4_mul(r0[2 * j], ks[0][x / 2]);
+                        a[1] = p4_mul(r1[2 * j], ks[1][x / 2]);
+                        a[2] = p4_mul(r0[2 * j + 1], ks[0][x / 2]);
+                        a[3] = p4_mul(r1[2 * j + 1], ks[1][x / 2]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int part = 0; part < PARTS; ++part) w4_mma(sacc[mt][nt], a, bq[nt][part][2 * x + j][0], bq[nt][part][2 * x + j][1]);
+                    }
+                }
+            }
+            // ---- softmax over the entries; this thread owns rows 2 tq, + 1 of each column tile.  The reference of a row's
+            // weights is raised only when some logit exceeds it by 2^8: until then a tile needs one vote and no exchange.
+            const bool edge = e0 + S::TILE > all_hi || e0 < all_lo;
+            float mx[NT][2];
+            bool raise = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (edge) {                                           // rows of the column's token see entries lo .. pos
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int col = nt * 8 + 2 * tq + c;
+                        const int pos = col < rows ? it.q.len - it.q.n + pb.by_g.div(row_first + col) : -1;
+                        const int lo = pb.window > 0 ? pos + 1 - pb.window : 0;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int i = c; i < 4; i += 2) {
+                                const int e = e0 + mt * 16 + w4_entry(gq) + (i >> 1) * 8;
+                                if (e > pos || e < lo) sacc[mt][nt][i] = -INFINITY;
+                            }
+                    }
+                }
+                mx[nt][0] = mx[nt][1] = -INFINITY;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    mx[nt][0] = fmaxf(mx[nt][0], fmaxf(sacc[mt][nt][0], sacc[mt][nt][2]));
+                    mx[nt][1] = fmaxf(mx[nt][1], fmaxf(sacc[mt][nt][1], sacc[mt][nt][3]));
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    mx[nt][c] *= to_log2[nt][c];                      // > 0
+                    raise |= mx[nt][c] > m_run[nt][c] + W4_RESCALE_STEP;
+                }
+            }
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = mx[nt][c];
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+                        m = fmaxf(m, m_run[nt][c]);
+                        const float f = m == -INFINITY ? 1.f : w4_exp2(m_run[nt][c] - m, Exact{});      // (0 the first time)
+                        m_run[nt][c] = m;
+                        l_run[nt][c] *= f;
+#pragma unroll
+                        for (int dt = 0; dt < KS; ++dt) { o[nt][dt][c] *= f; o[nt][dt][c + 2] *= f; }
+                    }
+            }
+            uint32_t pf[MT][NT][PARTS][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                // (a row that has seen nothing: every weight is 2^-inf = 0)
+                const float ref0 = m_run[nt][0] == -INFINITY ? 0.f : W4_OFFSET - m_run[nt][0], ref1 = m_run[nt][1] == -INFINITY ? 0.f : W4_OFFSET - m_run[nt][1];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const float* sc = sacc[mt][nt];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float p0 = w4_exp2(fmaf(sc[2 * i], to_log2[nt][0], ref0), Exact{}), p1 = w4_exp2(fmaf(sc[2 * i + 1], to_log2[nt][1], ref1), Exact{});
+                        l_run[nt][0] += p0;
+                        l_run[nt][1] += p1;
+                        const uint32_t hi = p4_f16x2(p0, p1);
+                        pf[mt][nt][0][i] = movmatrix_trans(hi);
+                        if constexpr (F32) {
+                            const float2 b = p4_float2(hi);
+                            pf[mt][nt][PARTS - 1][i] = movmatrix_trans(p4_f16x2(p0 - b.x, p1 - b.y));
+                        }
+                    }
+                }
+            }
+            // ---- O^T[channel][row] += V^T P^T: this thread's channels are gq d / 8 .., its entries 2 tq, 2 tq + 1 and 8 further
+            const bool v_on = gq * (D / 8) < d;
+#pragma unroll
+            for (int x = 0; x < VW; ++x) {
+                float acc[F32 ? NT : 1][4][4];
+                if constexpr (F32)
+#pragma unroll
+                    for (int i = 0; i < NT * 16; ++i) (&acc[0][0][0])[i] = 0.f;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    uint32_t vw[4], sp[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int ea = mt * 16 + i * 8 + w4_entry(2 * tq), eb = mt * 16 + i * 8 + w4_entry(2 * tq + 1);
+                        const unsigned char* c0 = tile + off_vc + gq * (D / 16) + x * 4;
+                        const unsigned char* s0 = tile + off_vs + gq * D / 128 + x / 2;
+                        uint32_t a = 0u, b = 0u, two = 0u;
+                        if (v_on) {
+                            a = *reinterpret_cast<const uint32_t*>(c0 + ea * code_row);
+                            b = *reinterpret_cast<const uint32_t*>(c0 + eb * code_row);
+                            two = (uint32_t)s0[ea * scale_row] | (uint32_t)s0[eb * scale_row] << 8;
+                        }
+                        sp[i] = p4_scales(two);
+                        vw[2 * i] = (a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u);            // even channels of both entries
+                        vw[2 * i + 1] = ((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);        // odd ones
+                    }
+                    uint32_t r[4][4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p4_codes(vw[i], r[i]);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        uint32_t a[4];
+                        a[0] = p4_mul(r[0][b], sp[0]);
+                        a[1] = p4_mul(r[1][b], sp[0]);
+                        a[2] = p4_mul(r[2][b], sp[1]);
+                        a[3] = p4_mul(r[3][b], sp[1]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int part = 0; part < PARTS; ++part) {
+                                if constexpr (F32) w4_mma(acc[nt][b], a, pf[mt][nt][part][0], pf[mt][nt][part][1]);
+                                else w4_mma(o[nt][4 * x + b], a, pf[mt][nt][part][0], pf[mt][nt][part][1]);
+                            }
+                    }
+                }
+                if constexpr (F32)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[nt][4 * x + b][i] += acc[nt][b][i];
+            }
+            __syncwarp();                                             // all lanes are done with the stage before it is refilled
+        }
+        if (failed) break;
+
+        // ---- the unit's result, or this worker's part of it.  o[nt][4 x + b]: channels 8 x + 2 b (c) and + 1 (c + 2) of the thread's
+        const float v_up = p4_pow2(p4_shift(cache, 1, it.h));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float l = l_run[nt][c];
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+                const int col = nt * 8 + 2 * tq + c;
+                if (col >= rows) continue;
+                const float f = it.slot < 0 ? (l > 0.f ? v_up / l : (l == 0.f ? 0.f : l)) : v_up;
+                const int qt = pb.by_g.div(row_first + col), qj = row_first + col - qt * g;
+                T* op = out + ((size_t)(it.q.row0 + qt) * pb.Hq + (size_t)(it.h * g + qj)) * d + gq * (D / 8);
+                const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * S::ROWS + col;
+                float* po = wk.part_o + pr * d + gq * (D / 8);
+                if (gq * (D / 8) < d) {
+#pragma unroll
+                    for (int x = 0; x < VW; ++x) {
+                        float v[8];
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            v[2 * b] = o[nt][4 * x + b][c] * f;
+                            v[2 * b + 1] = o[nt][4 * x + b][c + 2] * f;
+                        }
+                        if (it.slot < 0) w4_store8(op + 8 * x, v);
+                        else w4_store8(po + 8 * x, v);
+                    }
+                }
+                if (it.slot >= 0 && gq == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
+            }
+        if (it.slot >= 0 && (it.slot & 1) && lane == 0) paged_note_shared(wk, tab, it, cons.x, w, row_first, rows);
+        const long long next = cons.x + it.steps;
+        if (prod.on && prod.x == next) cons = prod; else cons = at(next);
+    }
+    if (failed) {
+        if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
+        while (consumed < issued) {                                   // wait (bounded) for the copies still in flight
+            mbar_wait_bounded(bars + consumed % S::STAGES, (consumed / S::STAGES) & 1u);
+            ++consumed;
+        }
+    }
+}
+
+template <int D, int NT, typename T>
+cudaError_t run_warp4(const Paged4View& c, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows, cudaStream_t st) {
+    using S = Warp4Shape<D, NT>;
+    static std::atomic<unsigned long long> done{0};
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, T>), S::SMEM, done);
+    if (e != cudaSuccess) return e;
+    e = paged_launch(paged4_attn_warp_kernel<D, NT, T>, dim3(PAGED_SMS), dim3(S::WARPS * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
+                     max_rows);
+    if (e != cudaSuccess || paged_always_whole(pb, c.pv.H, S::ROWS, PAGED_SMS * S::WARPS, W4_JOIN_STEPS)) return e;
+    return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st);
+}
+
+}  // namespace
+
+cudaError_t launch_paged4_attention_warp(const Paged4View& c, const PagedBatch& pb, int is_bf16, const void* q, void* out, float scale, const PagedWork& w,
+                                         int tile_rows, int max_rows, cudaStream_t st) {
+    auto go = [&](auto d, auto nt) {
+        constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+        return is_bf16 ? run_warp4<D, NT, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, float>(c, pb, q, out, scale, w, max_rows, st);
+    };
+    auto rows = [&](auto d) { return tile_rows <= 8 ? go(d, std::integral_constant<int, 1>{}) : go(d, std::integral_constant<int, 2>{}); };
+    return c.pv.d <= 64    ? rows(std::integral_constant<int, 64>{})
+           : c.pv.d <= 128 ? rows(std::integral_constant<int, 128>{})
+                           : go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+}
+
+}  // namespace tkv

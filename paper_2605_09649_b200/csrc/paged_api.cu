@@ -4,25 +4,11 @@
 
 #include <algorithm>
 
-#include "paged.cuh"
+#include "paged_check.cuh"
 
 using namespace tkv;
 
 namespace {
-
-template <typename... A>
-trimkv_status refuse(trimkv_status s, const char* fmt, A... args) {
-    set_last_error(fmt, args...);
-    return s;
-}
-bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool ok4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-trimkv_status done(cudaError_t e, const char* what) {
-    if (e == cudaSuccess) return TRIMKV_OK;
-    cudaGetLastError();
-    return refuse(TRIMKV_E_CUDA, "%s launch failed: %s", what, cudaGetErrorString(e));
-}
 
 trimkv_status check_cache(const trimkv_paged_cache* c, PagedView* pv) {
     if (!c || !c->k_pages || !c->v_pages) return refuse(TRIMKV_E_ARG, "cache, k_pages and v_pages must not be NULL");
@@ -62,9 +48,11 @@ PagedWork carve(void* area, int rows, int d) {
     return w;
 }
 
-trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64_t n_tokens, int32_t q_heads, const void* q, int64_t q_stride,
-                          const int32_t* cu_new, const int32_t* lens, const int32_t* block_table, int32_t table_width, float scale,
-                          const void* out, const void* workspace, size_t workspace_bytes, int32_t* status, PagedBatch* pb) {
+}  // namespace
+
+trimkv_status tkv::paged_check_batch(const PagedView& pv, int is_bf16, size_t need, int32_t n_req, int64_t n_tokens, int32_t q_heads, const void* q,
+                                     int64_t q_stride, const int32_t* cu_new, const int32_t* lens, const int32_t* block_table, int32_t table_width, float scale,
+                                     const void* out, const void* workspace, size_t workspace_bytes, int32_t* status, PagedBatch* pb) {
     if (n_req < 1 || n_req > PAGED_MAX_REQ) return refuse(TRIMKV_E_ARG, "n_req must be in [1, %d]", PAGED_MAX_REQ);
     if (table_width < 1 || table_width > TRIMKV_PAGED_MAX_WIDTH) return refuse(TRIMKV_E_ARG, "table_width must be in [1, %d]", TRIMKV_PAGED_MAX_WIDTH);
     if (q_heads < pv.H || q_heads % pv.H || q_heads / pv.H > 128) return refuse(TRIMKV_E_ARG, "q_heads must be kv_heads times 1 to 128");
@@ -82,7 +70,6 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
         return refuse(TRIMKV_E_ARG, "cu_new, lens and block_table must be non-NULL and aligned");
     if (!(scale > 0.f) || isinf(scale)) return refuse(TRIMKV_E_ARG, "scale must be positive and finite");
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return refuse(TRIMKV_E_ARG, "workspace must be non-NULL and 256-byte aligned");
-    const size_t need = work_bytes(pv.d);
     if (workspace_bytes < need) return refuse(TRIMKV_E_ARG, "workspace too small: %zu bytes, %zu needed", workspace_bytes, need);
     *pb = PagedBatch{};
     pb->cu_new = cu_new;
@@ -99,8 +86,6 @@ trimkv_status check_batch(const PagedView& pv, int is_bf16, int32_t n_req, int64
     pb->status = status;
     return TRIMKV_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -153,7 +138,7 @@ trimkv_status trimkv_paged_attention(const trimkv_paged_cache* cache, int32_t n_
     trimkv_status s = check_cache(cache, &pv);
     if (s != TRIMKV_OK) return s;
     const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16;
-    s = check_batch(pv, is_bf16, n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
+    s = paged_check_batch(pv, is_bf16, work_bytes(pv.d), n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
     if (s != TRIMKV_OK) return s;
     if (window < 0 || window > (1 << 30)) return refuse(TRIMKV_E_ARG, "window must be in [0, 2^30]");
     if (max_new < 0) return refuse(TRIMKV_E_ARG, "max_new must not be negative");
@@ -189,7 +174,7 @@ trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache* cache, int
     trimkv_status s = check_cache(cache, &pv);
     if (s != TRIMKV_OK) return s;
     const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16;
-    s = check_batch(pv, is_bf16, n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
+    s = paged_check_batch(pv, is_bf16, work_bytes(pv.d), n_req, n_tokens, q_heads, q, q_stride, cu_new, lens, block_table, table_width, scale, out, workspace, workspace_bytes, status, &pb);
     if (s != TRIMKV_OK) return s;
     if (!pv.bounds) return refuse(TRIMKV_E_ARG, "the cache has no key_bounds");
     if (sink_pages < 0 || recent_pages < 1 || top_pages > TRIMKV_PAGED_MAX_WIDTH || sink_pages > top_pages || recent_pages > top_pages - sink_pages)
