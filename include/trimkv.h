@@ -492,6 +492,63 @@ TRIMKV_API trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cach
                                       const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,
                                       void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
 
+/* ---- rows that share pages, and dropped entries -------------------------------------------------------
+ * For any of the paged caches above: these calls deal with tables and page numbers, and with rows as bytes.  (No counterpart in the
+ * paper, whose budgeted cache drops entries by itself.)
+ *   page_refs    int32 [n_pages]: how many rows of the table hold each page, and whatever the program counts beside them; 0 for free
+ *                ones.  A prefix that no request is using right now is kept by a row of its own.
+ * Outputs are apart from inputs: table_out is another array than block_table; refs_out may be page_refs, free_out free_pages and
+ * free_count_out free_count; otherwise no output overlaps an input.  Table entries behind a row's last page are neither read nor written.
+ * What moves: move_src, move_dst int32 [max_moves], *move_count pairs of slots (page x 64 + row) in ascending order of row and entry, -1
+ * behind them: rows to be copied, in every array of every layer, by trimkv_paged_move, before the call's new tokens are appended.  No
+ * destination is a source, and none is given twice.
+ * If something is wrong (E_ARG, E_NOMEM in status) nothing changes hands: the outputs say what the inputs said, with no new tokens
+ * and no moves.  Only pages that do not exist do not stop a call: they are latched, and -1 stands for them in tables and slots. */
+
+/* Row r goes on with the first keep_lens[r] entries of row source[r] (itself; another row: a fork, or a beam that goes on from
+ * another; -1 and keep 0: with nothing) and grows to new_lens[r]: its new tokens are positions keep_lens[r] .. new_lens[r] - 1, as in
+ * trimkv_paged_plan.  0 <= keep_lens[r] <= min(old_lens[source[r]], new_lens[r]); lengths are at most 64 x table_width.  Full pages are shared.  A partly filled
+ * page that a row will write is copied (its rows are listed) where another row or holder goes on with it; of several rows that
+ * will write it the lowest keeps it, if nobody else does.  new_lens = 0 ends a row.
+ * Pages whose count becomes 0 are pushed on the stack in (row, place) order, of the lowest row that let go of them; fresh pages are then
+ * popped in (row, place) order.  At most 63 moves a row. */
+TRIMKV_API trimkv_status trimkv_paged_share(int32_t n_req, const int32_t* source, const int32_t* old_lens, const int32_t* keep_lens,
+                                 const int32_t* new_lens, const int32_t* block_table, int32_t* table_out, int32_t table_width,
+                                 const int32_t* page_refs, int32_t* refs_out, const int32_t* free_pages, int32_t* free_out, int32_t n_pages,
+                                 const int32_t* free_count, int32_t* free_count_out, int64_t max_tokens, int32_t* lens_out, int32_t* cu_new,
+                                 int32_t* slot_map, int32_t* positions, int64_t max_moves, int32_t* move_src, int32_t* move_dst,
+                                 int32_t* move_count, int32_t* status, void* stream);
+
+/* Row r keeps the entries whose bits are set in keep_bits [n_req, table_width] (entry e: bit e % 64 of word e / 64, as
+ * trimkv_select_topk writes them; bits from lens[r] on are ignored), in their order.  Pages up to the first dropped entry's stay;
+ * what is kept from there on is listed to be moved to fresh pages, and the old pages are let go of; nothing moves if only a row's end
+ * is dropped.  Fresh pages come from the stack as it was (popped in (row, place) order), pages whose count becomes 0 are pushed after that.
+ * page_refs, refs_out: both NULL where no page has two holders. */
+TRIMKV_API trimkv_status trimkv_paged_compact(int32_t n_req, const int32_t* lens, const uint64_t* keep_bits, const int32_t* block_table,
+                                   int32_t* table_out, int32_t table_width, const int32_t* page_refs, int32_t* refs_out,
+                                   const int32_t* free_pages, int32_t* free_out, int32_t n_pages, const int32_t* free_count,
+                                   int32_t* free_count_out, int32_t* lens_out, int64_t max_moves, int32_t* move_src, int32_t* move_dst,
+                                   int32_t* move_count, int32_t* status, void* stream);
+
+/* An array of pages [n_pages, heads, 64, row_bytes]: pages, codes or scales of one layer. */
+#define TRIMKV_PAGED_MAX_ARRAYS 1024
+typedef struct trimkv_paged_rows {
+    void* pages;               /* 16-byte aligned */
+    void* key_bounds;          /* or NULL: [n_pages, heads, 2, row_bytes], made anew for pages whose row 63 is a destination; 16-byte aligned,
+                                  row_bytes a multiple of 16 */
+    int32_t heads;
+    int32_t row_bytes;         /* 1 to 4096 */
+    int32_t dtype;             /* of keys that have bounds; else ignored */
+    int32_t reserved;          /* must be 0 */
+} trimkv_paged_rows;
+
+/* Copies row move_src[i] to row move_dst[i] of every head of every array (a host array of n_arrays descriptions, copied by the call), for
+ * the first *move_count (device) of at most max_moves pairs; -1, -1 skips a pair, one outside the pages is skipped and latched.
+ * Destinations are no sources, and none is given twice. */
+TRIMKV_API trimkv_status trimkv_paged_move(int32_t n_arrays, const trimkv_paged_rows* arrays, int32_t n_pages, int64_t max_moves,
+                                const int32_t* move_src, const int32_t* move_dst, const int32_t* move_count, int32_t* status,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

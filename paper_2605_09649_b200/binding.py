@@ -32,6 +32,7 @@ EXPORTS = [
     "trimkv_paged_plan", "trimkv_paged_append", "trimkv_paged_workspace_bytes", "trimkv_paged_attention",
     "trimkv_paged_sparse_attention",
     "trimkv_paged4_append", "trimkv_paged4_read", "trimkv_paged4_workspace_bytes", "trimkv_paged4_attention",
+    "trimkv_paged_share", "trimkv_paged_compact", "trimkv_paged_move",
 ]
 
 
@@ -67,6 +68,14 @@ class Paged4CacheFields(C.Structure):
         ("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
         ("k_shift", C.c_void_p), ("v_shift", C.c_void_p), ("n_pages", C.c_int32), ("kv_heads", C.c_int32),
         ("head_dim", C.c_int32), ("page_size", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class PagedRows(C.Structure):
+    """trimkv_paged_rows: an array of pages whose rows are moved."""
+    _fields_ = [
+        ("pages", C.c_void_p), ("key_bounds", C.c_void_p), ("heads", C.c_int32), ("row_bytes", C.c_int32),
+        ("dtype", C.c_int32), ("reserved", C.c_int32),
     ]
 
 
@@ -149,6 +158,9 @@ def lib() -> C.CDLL:
     L.trimkv_paged4_workspace_bytes.argtypes = [i32, i32, i32]
     L.trimkv_paged4_workspace_bytes.restype = sz
     L.trimkv_paged4_attention.argtypes = [pc, i32, i32, i64, i32, i32, vp, i64, vp, vp, vp, i32, f32, i32, vp, vp, sz, vp, vp]
+    L.trimkv_paged_share.argtypes = [i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    L.trimkv_paged_compact.argtypes = [i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp]
+    L.trimkv_paged_move.argtypes = [i32, pc, i32, i64, vp, vp, vp, vp, vp]      # pc: trimkv_paged_rows*, PagedRows array or its bytes
     L.trimkv_paged_sparse_attention.argtypes = [pc, i32, i64, i32, vp, i64, vp, vp, vp, i32, f32, i32, i32, i32, vp, vp, vp,
                                                 sz, vp, vp]
     for name in ("trimkv_create_ex", "trimkv_reset", "trimkv_set_gate", "trimkv_set_shared_projection", "trimkv_gate",
@@ -649,3 +661,81 @@ def paged4_attention(cache: Paged4Cache, q, cu_new, lens, block_table, max_new: 
                                               paged4_workspace_bytes)
     _launch(lib().trimkv_paged4_attention, n, cache.fields, _KV_DTYPES[dt], r, t, max_new, hq, *batch, window, *tail)
     return out
+
+
+# ---- rows that share pages, dropped entries, and the rows that move (trimkv_paged_share, _compact, _move)
+def _table_pair(n, r, block_table, table_out):
+    rows, w = block_table.shape
+    if rows != r:
+        raise ValueError(f"block_table: expected {r} rows, got {rows}")
+    return _ints(n, "block_table", block_table, r * w), _ints(n, "table_out", table_out, r * w), w
+
+
+def paged_share(source, old_lens, keep_lens, new_lens, block_table, table_out, page_refs, refs_out, free_pages, free_out, free_count,
+                free_count_out, lens_out, cu_new, slot_map, positions, move_src, move_dst, move_count, status=None):
+    """Forks, growth and release of rows that share pages (trimkv_paged_share).  int32 tensors: source, old_lens, keep_lens, new_lens,
+    lens_out [R], block_table and table_out [R, W], page_refs, refs_out, free_pages, free_out [n_pages], free_count, free_count_out,
+    move_count, status [1], cu_new [R + 1], slot_map and positions (or None) [max_tokens], move_src and move_dst [max_moves]."""
+    n = old_lens.get_device()
+    if n < 0:
+        raise ValueError("expected a CUDA tensor")
+    r, m, pages, moves = old_lens.numel(), slot_map.numel(), free_pages.numel(), move_src.numel()
+    table, out, w = _table_pair(n, r, block_table, table_out)
+    _launch(lib().trimkv_paged_share, n, r, _ints(n, "source", source, r), _ints(n, "old_lens", old_lens, r), _ints(n, "keep_lens", keep_lens, r),
+            _ints(n, "new_lens", new_lens, r), table, out, w, _ints(n, "page_refs", page_refs, pages), _ints(n, "refs_out", refs_out, pages),
+            _ints(n, "free_pages", free_pages, pages), _ints(n, "free_out", free_out, pages), pages, _ints(n, "free_count", free_count, 1),
+            _ints(n, "free_count_out", free_count_out, 1), m, _ints(n, "lens_out", lens_out, r), _ints(n, "cu_new", cu_new, r + 1),
+            _ints(n, "slot_map", slot_map, m), None if positions is None else _ints(n, "positions", positions, m), moves,
+            _ints(n, "move_src", move_src, moves), _ints(n, "move_dst", move_dst, moves), _ints(n, "move_count", move_count, 1),
+            None if status is None else _ints(n, "status", status, 1))
+
+
+def paged_compact(lens, keep_bits, block_table, table_out, page_refs, refs_out, free_pages, free_out, free_count, free_count_out, lens_out,
+                  move_src, move_dst, move_count, status=None):
+    """Rows without the entries whose bits in keep_bits (int64 [R, W]) are clear (trimkv_paged_compact).  int32 tensors as in
+    paged_share; page_refs and refs_out may both be None."""
+    n = lens.get_device()
+    if n < 0:
+        raise ValueError("expected a CUDA tensor")
+    r, pages, moves = lens.numel(), free_pages.numel(), move_src.numel()
+    table, out, w = _table_pair(n, r, block_table, table_out)
+    _launch(lib().trimkv_paged_compact, n, r, _ints(n, "lens", lens, r), _on(n, "keep_bits", keep_bits, torch.int64, (r, w)), table, out, w,
+            None if page_refs is None else _ints(n, "page_refs", page_refs, pages), None if refs_out is None else _ints(n, "refs_out", refs_out, pages),
+            _ints(n, "free_pages", free_pages, pages), _ints(n, "free_out", free_out, pages), pages, _ints(n, "free_count", free_count, 1),
+            _ints(n, "free_count_out", free_count_out, 1), _ints(n, "lens_out", lens_out, r), moves, _ints(n, "move_src", move_src, moves),
+            _ints(n, "move_dst", move_dst, moves), _ints(n, "move_count", move_count, 1), None if status is None else _ints(n, "status", status, 1))
+
+
+_pack_rows = struct.Struct("PPiiii").pack       # PagedRows, field by field
+
+
+def paged_move(arrays, move_src, move_dst, move_count, key_bounds=None, status=None):
+    """Copies rows move_src to rows move_dst [max_moves], the first move_count [1] pairs, in every array (trimkv_paged_move).  arrays: contiguous
+    tensors [n_pages, H, 64, ...] of any type, of all layers; key_bounds: per array None or its bounds [n_pages, H, 2, d], or None."""
+    n = move_src.get_device()
+    if n < 0:
+        raise ValueError("expected a CUDA tensor")
+    moves, pages, rows = move_src.numel(), None, []
+    if key_bounds is not None and len(key_bounds) != len(arrays):
+        raise ValueError(f"key_bounds: expected one entry for each of {len(arrays)} arrays, got {len(key_bounds)}")
+    for i, t in enumerate(arrays):
+        shape = t.shape
+        if len(shape) < 3 or shape[2] != PAGE_SIZE or t.get_device() != n or not t.is_contiguous():
+            raise ValueError(f"arrays[{i}]: expected a contiguous tensor [n_pages, kv_heads, {PAGE_SIZE}, ...] on cuda:{n}, got {tuple(shape)} with strides {t.stride()} on {t.device}")
+        if pages is None:
+            pages = shape[0]
+        elif shape[0] != pages:
+            raise ValueError(f"arrays[{i}]: expected {pages} pages, got {shape[0]}")
+        row = t.stride(1) // PAGE_SIZE * t.element_size()
+        bounds = None if key_bounds is None else key_bounds[i]
+        if bounds is None:
+            rows.append(_pack_rows(t.data_ptr(), 0, shape[1], row, 0, 0))
+        else:
+            if t.dtype not in _KV_DTYPES or len(shape) != 4:
+                raise ValueError(f"arrays[{i}]: bounds want bf16 or fp32 keys [n_pages, kv_heads, {PAGE_SIZE}, head_dim]")
+            rows.append(_pack_rows(t.data_ptr(), _on(n, f"key_bounds[{i}]", bounds, t.dtype, (shape[0], shape[1], 2, shape[3])), shape[1], row,
+                                   _KV_DTYPES[t.dtype], 0))
+    if pages is None:
+        return
+    _launch(lib().trimkv_paged_move, n, len(rows), b"".join(rows), pages, moves, _ints(n, "move_src", move_src, moves), _ints(n, "move_dst", move_dst, moves),
+            _ints(n, "move_count", move_count, 1), None if status is None else _ints(n, "status", status, 1))

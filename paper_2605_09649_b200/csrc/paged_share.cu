@@ -1,0 +1,571 @@
+// Rows of a block table that share pages: forks, growth and release by reference counts, and dropping entries by keep bits.
+//
+// Both are one launch of one cluster of 16 CTAs, 512 warps.  Page numbers are dealt out in (row, place) order, so the result is a pure function of
+// the inputs although the counts are kept with atomics: counts are sums of whole numbers, and who of several rows keeps or
+// returns a page is settled by a minimum over row numbers, taken in the count itself (a count of 0 becomes r - R < 0 while it is
+// in dispute).  The cluster barrier orders the steps; per-row and per-stretch counts go to every CTA's shared memory
+// through the cluster, and every CTA computes the prefix sums that place things for itself.
+//
+// Share: refs_out = refs - the rows' old holds + those that go on; a partly filled page that a row will write stays with the lowest such
+// row if no other holds it, the others take a fresh page and list its rows to be copied; pages left without a holder go
+// on the stack; fresh pages come from its top.
+// Compact: a row's pages up to the first dropped entry's stay, the entries kept from there on are listed to be moved to fresh pages, the old pages are
+// released.  Fresh pages are taken before any is released, so no listed source is a destination.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "paged.cuh"
+#include "paged_share.cuh"
+
+namespace tkv {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int SH_CTAS = 16, SH_THREADS = 1024, SH_WARPS = SH_CTAS * SH_THREADS / 32;
+constexpr int SH_TASKS = 1024;                // stretches of rows, if there are fewer rows than that
+
+__device__ __forceinline__ int sh_pages(int n) { return (int)(((unsigned)n + PAGE - 1u) / PAGE); }
+__device__ __forceinline__ int sh_ld(const int32_t* p) { return __ldcg(p); }      // written by other CTAs
+
+// A row's table places are cut into nseg stretches of seg places (a multiple of 32); stretch t belongs to row t / nseg.
+struct ShareCut { int nseg, seg, tasks; };
+__host__ __device__ inline ShareCut share_cut(int R, int W) {
+    ShareCut c;
+    const int most = (W + 31) / 32;
+    int n = R >= SH_TASKS ? 1 : SH_TASKS / R;
+    n = n < most ? n : most;
+    c.seg = ((W + n - 1) / n + 31) / 32 * 32;
+    c.nseg = (W + c.seg - 1) / c.seg;
+    c.tasks = R * c.nseg;
+    return c;
+}
+
+// v[0 .. n] = sums before each of v[0 .. n - 1]; the block calls it.  Sums fit 32 bits.  w: 33 ints of shared memory.
+__device__ __forceinline__ void share_scan(int* v, int n, int* w) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (n + SH_THREADS - 1) / SH_THREADS;
+    const int i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+    int mine = 0;
+    for (int i = i0; i < i1; ++i) mine += v[i];
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+    }
+    __syncthreads();
+    if (lane == 31) w[warp] = incl;
+    __syncthreads();
+    if (warp == 0) {
+        int x = w[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += u;
+        }
+        w[lane] = x;
+    }
+    __syncthreads();
+    int run = (warp ? w[warp - 1] : 0) + incl - mine;
+    for (int i = i0; i < i1; ++i) { const int x = v[i]; v[i] = run; run += x; }
+    if (threadIdx.x == 0) v[n] = w[31];
+    __syncthreads();
+}
+
+// Last r with at[r] <= x (at ascending, at[0] = 0, x < at[n]); rows without any are passed over.
+__device__ __forceinline__ int share_find(const int* at, int n, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (at[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ void share_tell(cg::cluster_group& cluster, int* slot, int v) {      // *slot = v in every CTA
+    for (int i = 0; i < SH_CTAS; ++i) *cluster.map_shared_rank(slot, i) = v;
+}
+
+// Counts and the live part of the stack, where they are kept apart from the inputs.
+__device__ __forceinline__ void share_copy(const ShareArgs& a, int fc, int gt, int GT) {
+    if (a.refs_out != a.refs)
+        for (int i = gt; i < a.n_pages; i += GT) a.refs_out[i] = a.refs[i];
+    if (a.free_out != a.free_pages)
+        for (int i = gt; i < min(max(fc, 0), a.n_pages); i += GT) a.free_out[i] = a.free_pages[i];
+}
+
+__device__ __forceinline__ void share_none_moved(const ShareArgs& a, int from, int gt, int GT) {
+    for (int i = from + gt; i < a.max_moves; i += GT) { a.move_src[i] = -1; a.move_dst[i] = -1; }
+    if (gt == 0) *a.move_count = from;
+}
+
+// ---------------------------------------------------------------- share
+
+// What row r of a share is.
+struct ShareRow {
+    int source, old, keep, now;
+    int stay;                                 // pages that it goes on holding without writing them
+    bool writes;                              // page keep / 64 of its source is partly filled and will be written
+};
+__device__ __forceinline__ ShareRow share_row(const ShareArgs& a, int r) {
+    ShareRow s;
+    s.source = a.source[r]; s.old = a.old_lens[r]; s.keep = a.keep_lens[r]; s.now = a.new_lens[r];
+    s.writes = s.keep % PAGE != 0 && s.now > s.keep;
+    s.stay = s.writes ? s.keep / PAGE : sh_pages(s.keep);
+    return s;
+}
+
+__global__ void __launch_bounds__(SH_THREADS, 1)
+paged_share_kernel(ShareArgs a) {
+    extern __shared__ int s_share[];
+    __shared__ int s_w[33], s_bad;
+    __shared__ long long s_total;
+    const int R = a.R, W = a.W;
+    const ShareCut cut = share_cut(R, W);
+    int* s_tok = s_share;                     // [R + 1] each: per row, then sums before it
+    int* s_take = s_tok + R + 1;
+    int* s_move = s_take + R + 1;
+    int* s_back = s_move + R + 1;             // [tasks + 1]
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster.block_rank();
+    const int gt = rank * SH_THREADS + tid, GT = SH_CTAS * SH_THREADS, gw = rank * (SH_THREADS / 32) + (tid >> 5);
+    if (tid == 0) { s_bad = 0; s_total = 0; }
+    grid_dependency_wait();
+    grid_dependents_may_launch();
+    __syncthreads();
+    const int fc = *a.free_count;
+
+    // ---- lengths
+    const int cap = W * PAGE;
+    long long tokens_mine = 0;
+    for (int r = tid; r < R; r += SH_THREADS) {
+        const int src = a.source[r], o = a.old_lens[r], k = a.keep_lens[r], n = a.new_lens[r];
+        const int so = src >= 0 && src < R ? a.old_lens[src] : 0;
+        if (src < -1 || src >= R || o < 0 || o > cap || n < 0 || n > cap || k < 0 || k > so || k > n) { s_bad = TRIMKV_E_ARG; continue; }
+        tokens_mine += n - k;
+        s_tok[r] = n - k;
+        s_take[r] = sh_pages(n) - sh_pages(k);        // and one more where a page is copied
+        s_move[r] = 0;
+    }
+    for (int o = 16; o > 0; o >>= 1) tokens_mine += __shfl_xor_sync(0xffffffffu, tokens_mine, o);
+    if (lane == 0 && tokens_mine) atomicAdd(reinterpret_cast<unsigned long long*>(&s_total), (unsigned long long)tokens_mine);
+    share_copy(a, fc, gt, GT);
+    __syncthreads();
+    int bad = s_bad;
+    if (!bad && (fc < 0 || fc > a.n_pages || s_total > a.max_tokens)) bad = TRIMKV_E_ARG;
+    cluster.sync();                           // copies are made, every CTA's shared memory is set up
+    bool wrong = false;                       // a page that does not exist
+    auto page_at = [&](int r, int j) {
+        const int p = a.table[(size_t)r * W + j];
+        return p >= 0 && p < a.n_pages ? p : -1;
+    };
+    // places of row r that it lets go of: those it holds and does not go on with
+    auto each_dropped = [&](auto&& f) {
+        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+            const ShareRow s = share_row(a, r);
+            const int from = s.source == r ? s.stay : 0, to = sh_pages(s.old);
+            f(t, r, max(j0, from / 32 * 32), from, min(to, j0 + cut.seg));
+        }
+    };
+    auto each_gained = [&](auto&& f) {        // holds of a page of another row
+        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+            const ShareRow s = share_row(a, r);
+            if (s.source < 0 || s.source == r) continue;
+            for (int j = j0 + lane; j < min(s.stay, j0 + cut.seg); j += 32) f(page_at(s.source, j));
+        }
+    };
+    auto add = [&](int sign) {
+        each_dropped([&](int, int r, int j0, int from, int to) {
+            for (int j = j0 + lane; j < to; j += 32) {
+                const int p = j >= from ? page_at(r, j) : -1;
+                if (p >= 0) atomicAdd(a.refs_out + p, -sign);
+                else wrong |= j >= from;
+            }
+        });
+        each_gained([&](int p) {
+            if (p >= 0) atomicAdd(a.refs_out + p, sign);
+            else wrong = true;
+        });
+    };
+    if (!bad) {
+        add(1);
+        __threadfence();
+        cluster.sync();
+        // ---- pages that rows go on writing: counts are of the holders that do not
+        for (int r = gt; r < R; r += GT) {
+            const ShareRow s = share_row(a, r);
+            const int p = s.writes ? page_at(s.source, s.keep / PAGE) : -1;
+            if (p >= 0 && sh_ld(a.refs_out + p) <= 0) atomicMin(a.refs_out + p, r - R);
+        }
+        __threadfence();
+        cluster.sync();
+        for (int r = gt; r < R; r += GT) {
+            const ShareRow s = share_row(a, r);
+            const int p = s.writes ? page_at(s.source, s.keep / PAGE) : -1;
+            if (p < 0) { wrong |= s.writes; continue; }
+            if (sh_ld(a.refs_out + p) == r - R) {
+                a.refs_out[p] = 1;            // (others who read it now see this or the minimum: not theirs)
+            } else {
+                share_tell(cluster, s_take + r, sh_pages(s.now) - sh_pages(s.keep) + 1);
+                share_tell(cluster, s_move + r, s.keep % PAGE);
+            }
+        }
+        __threadfence();
+        cluster.sync();
+        // ---- pages that nobody holds: the lowest row that let go of one gives it back
+        each_dropped([&](int, int r, int j0, int from, int to) {
+            for (int j = j0 + lane; j < to; j += 32) {
+                const int p = j >= from ? page_at(r, j) : -1;
+                if (p >= 0 && sh_ld(a.refs_out + p) <= 0) atomicMin(a.refs_out + p, r - R);
+            }
+        });
+        __threadfence();
+        cluster.sync();
+        each_dropped([&](int t, int r, int j0, int from, int to) {
+            int n = 0;
+            for (int j = j0; j < to; j += 32) {
+                const int p = j + lane >= from && j + lane < to ? page_at(r, j + lane) : -1;
+                n += __popc(__ballot_sync(0xffffffffu, p >= 0 && sh_ld(a.refs_out + p) == r - R));
+            }
+            if (lane < SH_CTAS) *cluster.map_shared_rank(s_back + t, lane) = n;
+        });
+        cluster.sync();
+        share_scan(s_tok, R, s_w);
+        share_scan(s_take, R, s_w);
+        share_scan(s_move, R, s_w);
+        share_scan(s_back, cut.tasks, s_w);
+        if (fc + s_back[cut.tasks] > a.n_pages || s_move[R] > a.max_moves) bad = TRIMKV_E_ARG;
+        else if (fc + s_back[cut.tasks] < s_take[R]) bad = TRIMKV_E_NOMEM;
+        if (bad) {                            // the counts as they were
+            each_dropped([&](int, int r, int j0, int from, int to) {
+                for (int j = j0 + lane; j < to; j += 32) {
+                    const int p = j >= from ? page_at(r, j) : -1;
+                    if (p >= 0 && sh_ld(a.refs_out + p) == r - R) a.refs_out[p] = 0;
+                }
+            });
+            __threadfence();
+            cluster.sync();
+            for (int r = gt; r < R; r += GT) {
+                const ShareRow s = share_row(a, r);
+                const int p = s.writes && s_move[r + 1] == s_move[r] ? page_at(s.source, s.keep / PAGE) : -1;
+                if (p >= 0) atomicAdd(a.refs_out + p, -1);
+            }
+            add(-1);
+        }
+    }
+    if (bad) {                                // nothing changes hands; the call's tokens are none
+        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+            for (int j = j0 + lane; j < min(min(sh_pages(max(a.old_lens[r], 0)), W), j0 + cut.seg); j += 32) a.table_out[(size_t)r * W + j] = a.table[(size_t)r * W + j];
+        }
+        for (int r = gt; r <= R; r += GT) {
+            a.cu_new[r] = 0;
+            if (r < R) a.lens_out[r] = a.old_lens[r];
+        }
+        for (int i = gt; i < a.max_tokens; i += GT) { a.slot_map[i] = -1; if (a.positions) a.positions[i] = -1; }
+        share_none_moved(a, 0, gt, GT);
+        if (gt == 0) { *a.free_count_out = fc; latch_error(a.status, bad); }      // (a barrier ago everyone had read the free count)
+        return;
+    }
+    const int back = s_back[cut.tasks], taken = s_take[R], tokens = s_tok[R], moves = s_move[R];
+    // ---- given back, in (row, place) order
+    each_dropped([&](int t, int r, int j0, int from, int to) {
+        int at = fc + s_back[t];
+        for (int j = j0; j < to; j += 32) {
+            const int p = j + lane >= from && j + lane < to ? page_at(r, j + lane) : -1;
+            const bool mine = p >= 0 && sh_ld(a.refs_out + p) == r - R;
+            const unsigned all = __ballot_sync(0xffffffffu, mine);
+            const int i = at + __popc(all & ((1u << lane) - 1u));
+            if (mine) {
+                if (i < a.n_pages) a.free_out[i] = p;
+                a.refs_out[p] = 0;
+            }
+            at += __popc(all);
+        }
+    });
+    __threadfence();
+    cluster.sync();
+    // ---- the new rows: what they go on with, then fresh pages from the top of the stack
+    for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+        const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+        const ShareRow s = share_row(a, r);
+        const int has = sh_pages(s.now), begin = has - (s_take[r + 1] - s_take[r]);
+        for (int j = j0 + lane; j < min(has, j0 + cut.seg); j += 32) {
+            int p;
+            if (j < begin) {
+                p = page_at(s.source, j);
+            } else {
+                p = sh_ld(a.free_out + (fc + back - 1 - (s_take[r] + j - begin)));
+                if (p < 0 || p >= a.n_pages) p = -1;
+                else a.refs_out[p] = 1;
+            }
+            wrong |= p < 0;
+            a.table_out[(size_t)r * W + j] = p;
+        }
+    }
+    __threadfence();
+    cluster.sync();
+    for (int r = gt; r <= R; r += GT) {
+        a.cu_new[r] = s_tok[r];
+        if (r < R) a.lens_out[r] = a.new_lens[r];
+    }
+    if (gt == 0) *a.free_count_out = fc + back - taken;
+    for (int i = gt; i < a.max_tokens; i += GT) {
+        int slot = -1, pos = -1;
+        if (i < tokens) {
+            const int r = share_find(s_tok, R, i);
+            pos = a.keep_lens[r] + (i - s_tok[r]);
+            const int p = sh_ld(a.table_out + (size_t)r * W + pos / PAGE);
+            if (p >= 0) slot = p * PAGE + pos % PAGE;
+        }
+        a.slot_map[i] = slot;
+        if (a.positions) a.positions[i] = pos;
+    }
+    for (int i = gt; i < moves; i += GT) {
+        const int r = share_find(s_move, R, i), e = i - s_move[r], page = a.keep_lens[r] / PAGE;
+        const int from = page_at(a.source[r], page), to = sh_ld(a.table_out + (size_t)r * W + page);
+        a.move_src[i] = to >= 0 ? from * PAGE + e : -1;
+        a.move_dst[i] = to >= 0 ? to * PAGE + e : -1;
+    }
+    share_none_moved(a, moves, gt, GT);
+    if (wrong) latch_error(a.status, TRIMKV_E_ARG);
+}
+
+// ---------------------------------------------------------------- compact
+
+__global__ void __launch_bounds__(SH_THREADS, 1)
+paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
+    extern __shared__ int s_share[];
+    __shared__ int s_w[33], s_bad, s_cnt, s_first, s_last;
+    const int R = a.R, W = a.W;
+    const ShareCut cut = share_cut(R, W);
+    int* s_len = s_share;                     // [R]: entries kept
+    int* s_stay = s_len + R;                  // [R]: pages that stay
+    int* s_take = s_stay + R;                 // [R + 1] each: per row, then sums before it
+    int* s_move = s_take + R + 1;
+    int* s_back = s_move + R + 1;             // [tasks + 1]
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster.block_rank();
+    const int gt = rank * SH_THREADS + tid, GT = SH_CTAS * SH_THREADS, gw = rank * (SH_THREADS / 32) + (tid >> 5);
+    if (tid == 0) s_bad = 0;
+    grid_dependency_wait();
+    grid_dependents_may_launch();
+    __syncthreads();
+    const int fc = *a.free_count;
+    for (int r = tid; r < R; r += SH_THREADS) {
+        const int n = a.old_lens[r];
+        if (n < 0 || n > W * PAGE) s_bad = TRIMKV_E_ARG;
+    }
+    share_copy(a, fc, gt, GT);
+    __syncthreads();
+    int bad = s_bad;
+    if (!bad && (fc < 0 || fc > a.n_pages)) bad = TRIMKV_E_ARG;
+    cluster.sync();                           // copies are made, every CTA's shared memory is set up
+    // Word w of row r: which of its entries are kept, and which are dropped.
+    auto kept = [&](int r, int w, int n) {
+        const u64 in = n - w * PAGE >= PAGE ? ~0ull : n > w * PAGE ? (1ull << (n - w * PAGE)) - 1ull : 0ull;
+        return keep_bits[(size_t)r * W + w] & in;
+    };
+    bool wrong = false;
+    auto page_at = [&](int r, int j) {
+        const int p = a.table[(size_t)r * W + j];
+        return p >= 0 && p < a.n_pages ? p : -1;
+    };
+    if (!bad) {
+        // ---- of each row: entries kept, the first dropped, the last kept
+        auto look = [&](int r, int n, int id, int step, int& cnt, int& first, int& last) {
+#pragma unroll 4
+            for (int w = id; w < sh_pages(n); w += step) {
+                const u64 k = kept(r, w, n), gone = ~k;
+                cnt += __popcll(k);
+                if (k) last = w * PAGE + 63 - __clzll((long long)k);
+                const int f = gone ? w * PAGE + __ffsll((long long)gone) - 1 : n;
+                first = min(first, f);
+            }
+            cnt = __reduce_add_sync(0xffffffffu, cnt);
+            first = __reduce_min_sync(0xffffffffu, first);
+            last = __reduce_max_sync(0xffffffffu, last);
+        };
+        auto tell = [&](int r, int to, int cnt, int first, int last) {        // CTA `to`
+            const bool moves = last > first;
+            const int stay = moves ? first / PAGE : sh_pages(cnt);
+            *cluster.map_shared_rank(s_len + r, to) = cnt;
+            *cluster.map_shared_rank(s_stay + r, to) = stay;
+            *cluster.map_shared_rank(s_take + r, to) = sh_pages(cnt) - stay;
+            *cluster.map_shared_rank(s_move + r, to) = moves ? cnt - stay * PAGE : 0;
+        };
+        if (W <= 2048 || R >= SH_WARPS / 8) {                 // by a warp: at most 64 words a lane, or enough rows to fill an eighth of the warps
+            for (int r = gw; r < R; r += SH_WARPS) {
+                const int n = a.old_lens[r];
+                int cnt = 0, first = n, last = -1;
+                look(r, n, lane, 32, cnt, first, last);
+                if (lane < SH_CTAS) tell(r, lane, cnt, first, last);
+            }
+        } else {
+            for (int r = rank; r < R; r += SH_CTAS) {
+                const int n = a.old_lens[r];
+                if (tid == 0) { s_cnt = 0; s_first = n; s_last = -1; }
+                __syncthreads();
+                int cnt = 0, first = n, last = -1;
+                look(r, n, tid, SH_THREADS, cnt, first, last);
+                if (lane == 0) {
+                    atomicAdd(&s_cnt, cnt);
+                    atomicMin(&s_first, first);
+                    atomicMax(&s_last, last);
+                }
+                __syncthreads();
+                if (tid < SH_CTAS) tell(r, tid, s_cnt, s_first, s_last);
+                __syncthreads();
+            }
+        }
+        cluster.sync();
+        share_scan(s_take, R, s_w);
+        share_scan(s_move, R, s_w);
+        if (s_move[R] > a.max_moves) bad = TRIMKV_E_ARG;
+        else if (s_take[R] > fc) bad = TRIMKV_E_NOMEM;
+    }
+    if (bad) {                                // nothing changes hands
+        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+            for (int j = j0 + lane; j < min(min(sh_pages(max(a.old_lens[r], 0)), W), j0 + cut.seg); j += 32) a.table_out[(size_t)r * W + j] = a.table[(size_t)r * W + j];
+        }
+        for (int r = gt; r < R; r += GT) a.lens_out[r] = a.old_lens[r];
+        share_none_moved(a, 0, gt, GT);
+        if (gt == 0) { *a.free_count_out = fc; latch_error(a.status, bad); }      // (a barrier ago everyone had read the free count)
+        return;
+    }
+    const int taken = s_take[R], moves = s_move[R];
+    auto each_dropped = [&](auto&& f) {
+        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg, from = s_stay[r];
+            f(t, r, max(j0, from / 32 * 32), from, min(sh_pages(a.old_lens[r]), j0 + cut.seg));
+        }
+    };
+    // ---- the new rows, and one holder less for what they leave
+    for (int t = gw; t < cut.tasks; t += SH_WARPS) {
+        const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg, has = sh_pages(s_len[r]), stay = s_stay[r];
+        for (int j = j0 + lane; j < min(has, j0 + cut.seg); j += 32) {
+            int p;
+            if (j < stay) {
+                p = page_at(r, j);
+            } else {
+                p = a.free_pages[fc - 1 - (s_take[r] + j - stay)];
+                if (p < 0 || p >= a.n_pages) p = -1;
+                else if (a.refs_out) a.refs_out[p] = 1;
+            }
+            wrong |= p < 0;
+            a.table_out[(size_t)r * W + j] = p;
+        }
+    }
+    each_dropped([&](int, int r, int j0, int from, int to) {
+        for (int j = j0 + lane; j < to; j += 32) {
+            const int p = j >= from ? page_at(r, j) : -1;
+            if (p >= 0 && a.refs_out) atomicAdd(a.refs_out + p, -1);
+            wrong |= j >= from && p < 0;
+        }
+    });
+    __threadfence();
+    cluster.sync();
+    if (a.refs_out) {
+        each_dropped([&](int, int r, int j0, int from, int to) {
+            for (int j = j0 + lane; j < to; j += 32) {
+                const int p = j >= from ? page_at(r, j) : -1;
+                if (p >= 0 && sh_ld(a.refs_out + p) <= 0) atomicMin(a.refs_out + p, r - R);
+            }
+        });
+        __threadfence();
+        cluster.sync();
+    }
+    auto returns = [&](int r, int p) { return p >= 0 && (!a.refs_out || sh_ld(a.refs_out + p) == r - R); };
+    each_dropped([&](int t, int r, int j0, int from, int to) {
+        int n = 0;
+        for (int j = j0; j < to; j += 32) {
+            const int p = j + lane >= from && j + lane < to ? page_at(r, j + lane) : -1;
+            n += __popc(__ballot_sync(0xffffffffu, returns(r, p)));
+        }
+        if (lane < SH_CTAS) *cluster.map_shared_rank(s_back + t, lane) = n;
+    });
+    cluster.sync();
+    share_scan(s_back, cut.tasks, s_w);
+    each_dropped([&](int t, int r, int j0, int from, int to) {
+        int at = fc - taken + s_back[t];
+        for (int j = j0; j < to; j += 32) {
+            const int p = j + lane >= from && j + lane < to ? page_at(r, j + lane) : -1;
+            const bool mine = returns(r, p);
+            const unsigned all = __ballot_sync(0xffffffffu, mine);
+            const int i = at + __popc(all & ((1u << lane) - 1u));
+            if (mine) {
+                if (i < a.n_pages) a.free_out[i] = p;
+                if (a.refs_out) a.refs_out[p] = 0;
+            }
+            at += __popc(all);
+        }
+    });
+    for (int r = gt; r < R; r += GT) a.lens_out[r] = s_len[r];
+    if (gt == 0) *a.free_count_out = min(fc - taken + s_back[cut.tasks], a.n_pages);
+    // ---- the entries that move: a warp takes 32 words of a row
+    const int nwarp = (W + 31) / 32;
+    for (long long t = gw; t < (long long)R * nwarp; t += SH_WARPS) {
+        const int r = (int)(t / nwarp), w0 = (int)(t - (long long)r * nwarp) * 32, stay = s_stay[r];
+        const int n = a.old_lens[r], count = s_move[r + 1] - s_move[r];
+        if (count == 0 || w0 + 32 <= stay || w0 >= sh_pages(n)) continue;
+        int before = 0;                       // entries kept in the row's earlier words
+        for (int w = lane; w < w0; w += 32) before += __popcll(kept(r, w, n));
+        before = __reduce_add_sync(0xffffffffu, before);
+        const bool on = w0 + lane < sh_pages(n);
+        const u64 bits = on ? kept(r, w0 + lane, n) : 0ull;
+        const int from = on ? page_at(r, w0 + lane) : -1;
+        int sum = __popcll(bits);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += u;
+        }
+        const int total = __shfl_sync(0xffffffffu, sum, 31), base = before + sum - __popcll(bits);
+        const int d0 = before / PAGE, d1 = total ? (before + total - 1) / PAGE : d0;       // destination pages: at most 33
+        const int to_mine = d0 + lane <= d1 ? sh_ld(a.table_out + (size_t)r * W + d0 + lane) : -1;
+        const int to_last = d0 + 32 <= d1 ? sh_ld(a.table_out + (size_t)r * W + d0 + 32) : -1;
+        for (int i = max(0, stay - w0); i < 32; ++i) {
+            const u64 b = __shfl_sync(0xffffffffu, bits, i);
+            const int fp = __shfl_sync(0xffffffffu, from, i), at = __shfl_sync(0xffffffffu, base, i);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int bit = half * 32 + lane, rank_in = at + __popcll(b & ((1ull << bit) - 1ull));
+                const int tp = __shfl_sync(0xffffffffu, to_mine, (rank_in / PAGE - d0) & 31), to = rank_in / PAGE - d0 == 32 ? to_last : tp;
+                if ((b >> bit) & 1ull) {
+                    const int m = s_move[r] + rank_in - stay * PAGE;
+                    a.move_src[m] = fp >= 0 && to >= 0 ? fp * PAGE + bit : -1;
+                    a.move_dst[m] = fp >= 0 && to >= 0 ? to * PAGE + rank_in % PAGE : -1;
+                }
+            }
+        }
+    }
+    share_none_moved(a, moves, gt, GT);
+    if (wrong) latch_error(a.status, TRIMKV_E_ARG);
+}
+
+size_t share_ints(int R, int W) { return (size_t)4 * R + 4 + share_cut(R, W).tasks + 1; }
+constexpr int SH_MOST_SMEM = (5 * PAGED_MAX_REQ + 8) * (int)sizeof(int);          // (fewer tasks than rows above SH_TASKS rows)
+static_assert(PAGED_MAX_REQ >= SH_TASKS, "tasks are at most the larger of the two");
+
+}  // namespace
+
+cudaError_t launch_paged_share(const ShareArgs& a, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready{0};
+    const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_share_kernel), SH_MOST_SMEM, ready, true);
+    if (e != cudaSuccess) return e;
+    return paged_launch(paged_share_kernel, dim3(SH_CTAS), dim3(SH_THREADS), share_ints(a.R, a.W) * sizeof(int), SH_CTAS, true, st, a);
+}
+
+cudaError_t launch_paged_compact(const ShareArgs& a, const unsigned long long* keep_bits, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready{0};
+    const cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged_compact_kernel), SH_MOST_SMEM, ready, true);
+    if (e != cudaSuccess) return e;
+    return paged_launch(paged_compact_kernel, dim3(SH_CTAS), dim3(SH_THREADS), share_ints(a.R, a.W) * sizeof(int), SH_CTAS, true, st, a, keep_bits);
+}
+
+}  // namespace tkv
