@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtrimkv.so")
-SOURCES = ["trimkv_runtime.cu", "gate.cu", "gate_tc.cu", "cache.cu", "select.cu", "select_flat.cu", "select_static.cu", "attention.cu", "prefill_attention.cu", "prefill_attention_tc.cu", "paged_plan.cu", "paged_select.cu", "paged_attention.cu", "paged_attention_warp.cu", "paged_attention_tc.cu", "paged_api.cu", "paged4_append.cu", "paged4_attention.cu", "paged4_api.cu", "paged_share.cu", "paged_move.cu", "paged_share_api.cu"]
+SOURCES = ["trimkv_runtime.cu", "gate.cu", "gate_tc.cu", "cache.cu", "select.cu", "select_flat.cu", "select_static.cu", "attention.cu", "prefill_attention.cu", "prefill_attention_tc.cu", "paged_plan.cu", "paged_select.cu", "paged_attention.cu", "paged_attention_warp.cu", "paged_attention_tc.cu", "paged_api.cu", "paged4_append.cu", "paged4_attention.cu", "paged4_attention_tc.cu", "paged4_api.cu", "paged_share.cu", "paged_move.cu", "paged_share_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
@@ -33,7 +33,7 @@ def _stale(target: str, deps) -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu to an object and link libtrimkv.so next to this file.  Returns the library path."""
     nvcc = _nvcc()
-    headers = [os.path.join(CSRC, "trimkv_internal.cuh"), os.path.join(CSRC, "async_copy.cuh"), os.path.join(CSRC, "mma_sync.cuh"), os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "paged_check.cuh"), os.path.join(CSRC, "paged4.cuh"), os.path.join(CSRC, "paged_share.cuh"), os.path.join(CSRC, "paged_bounds.cuh"), os.path.join(CSRC, "tcgen05_attn.cuh"), os.path.join(ROOT, "include", "trimkv.h"), __file__]
+    headers = [os.path.join(CSRC, "trimkv_internal.cuh"), os.path.join(CSRC, "async_copy.cuh"), os.path.join(CSRC, "mma_sync.cuh"), os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "paged_check.cuh"), os.path.join(CSRC, "paged4.cuh"), os.path.join(CSRC, "paged_tc.cuh"), os.path.join(CSRC, "paged_share.cuh"), os.path.join(CSRC, "paged_bounds.cuh"), os.path.join(CSRC, "tcgen05_attn.cuh"), os.path.join(ROOT, "include", "trimkv.h"), __file__]
     objs = []
     procs = []
     for src in SOURCES:

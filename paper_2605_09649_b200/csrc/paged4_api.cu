@@ -32,8 +32,9 @@ trimkv_status check_cache4(const trimkv_paged4_cache* c, int32_t dtype, Paged4Vi
     return TRIMKV_OK;
 }
 
-// Workspace: {shared units, partial results} of the warp kernel.
-size_t work_bytes4(int d) { return P4_SHARED_BYTES + paged_partial_bytes(P4_WORKER_ROWS, d); }
+// Workspace: {shared units, partial results} of the warp kernel, then of the tensor-core kernel, where the head size has one.
+size_t first_bytes4(int d) { return P4_SHARED_BYTES + paged_partial_bytes(P4_WORKER_ROWS, d); }
+size_t work_bytes4(int d) { return first_bytes4(d) + (d <= PAGED_TC_HEAD ? PAGED_SHARED_BYTES + paged_partial_bytes(PAGED_SMS * PAGED_TC_ROWS, d) : 0); }
 PagedWork carve4(void* area, size_t shared_bytes, int rows, int d) {
     PagedWork w;
     w.shared = (int4*)area;
@@ -95,8 +96,20 @@ trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t 
     pb.window = window;
     const cudaStream_t st = (cudaStream_t)stream;
     const PagedWork w = carve4(workspace, P4_SHARED_BYTES, P4_WORKER_ROWS, c.pv.d);
+    // Requests of up to 32 rows (tokens x query heads of a KV head) go to the warp kernel, larger ones to the tcgen05 kernel, where there is
+    // one.  max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
-    return done(launch_paged4_attention_warp(c, pb, is_bf16, q, out, scale, w, most <= 8 ? 8 : 16, INT_MAX, st), "attention");
+    const int tile = most <= 8 ? 8 : 16;
+    cudaError_t e = cudaSuccess;
+    if (most <= 32 || !is_bf16 || c.pv.d > PAGED_TC_HEAD) {
+        e = launch_paged4_attention_warp(c, pb, is_bf16, q, out, scale, w, tile, INT_MAX, st);
+    } else {
+        const bool equal = max_new > 0 && n_tokens == (int64_t)n_req * max_new;    // every request has max_new tokens: one kernel
+        const PagedWork w2 = carve4((char*)workspace + first_bytes4(c.pv.d), PAGED_SHARED_BYTES, PAGED_SMS * PAGED_TC_ROWS, c.pv.d);
+        e = launch_paged4_attention_tc(c, pb, q, out, scale, w2, equal ? 1 : 33, st);
+        if (e == cudaSuccess && !equal) e = launch_paged4_attention_warp(c, pb, is_bf16, q, out, scale, w, tile, 32, st);
+    }
+    return done(e, "attention");
 }
 
 }  // extern "C"
