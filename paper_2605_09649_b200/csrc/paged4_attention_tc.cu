@@ -2,10 +2,12 @@
 // shared memory, the missing columns zero).
 //
 // The chunk kernel of the bf16 cache (paged_attention_tc.cu: units of 256 rows in two groups, tiles of two pages, 16 softmax warps, one issuing
-// warp, the order of a worker's stretches) with another producer: three warps read codes and scales, a piece of 32 channels of an entry
-// a lane, into registers one tile ahead, turn them into fp16 (exact, see paged4.cuh) and store them where TMA would have put a
-// bf16 tile: rows of 128 bytes, 128-byte swizzled, 64-column planes.  Eight neighbouring lanes take eight neighbouring rows, so the
-// stores meet no bank conflict.  Three and not four: with 20 warps a thread may have 96 registers, with 21 80.
+// warp, the order of a worker's stretches) with another producer: one warp copies codes and scales of a page into a ring of three, six
+// warps turn them into fp16 (exact, see paged4.cuh) and store them where TMA would have put a bf16 tile: rows of 128 bytes,
+// 128-byte swizzled, 64-column planes.  Eight neighbouring lanes take four rows and two parts, so the stores meet no bank conflict.
+// Each kind of warp walks the line in code of its own, and they divide the block's registers: a step of a feeding warp is a chain
+// of 300 to 600 cycles, so what feeds a tile in time is their number.  (4 x 512 tokens over 16K: three warps with loads of their own
+// 1683 us, 1180 with the loads of four steps in flight, 1062 with seven warps, 864 with copies by the copy engine.)
 // Both products are fp16: Q's rows are scaled by powers of two (largest value in 2^10 .. 2^11) and P by 2^4: weights may exceed their
 // reference by 2^11 before a stretch goes round again (fp16 ends at 2^16), and what is lost of a small one is 2^-29 of the reference.
 // V behind a request's last entry, and pages that do not exist, are stored as zeros.
@@ -20,8 +22,12 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int T_ROWS = 128, T_UNIT = PAGED_TC_ROWS;
 constexpr int T_PLANE = PAGE * 128;                                   // 64 entries x 64 columns
 constexpr int T_QPLANE = T_ROWS * 128;
-constexpr int T_SOFT = 16, T_FEED = 3;                                // softmax warps; warps that bring K and V
-constexpr int T_THREADS = (T_SOFT + T_FEED + 1) * 32;
+constexpr int T_SOFT = 16, T_FEED = 6;                                // softmax warps; warps that make K and V; then one that copies, one that issues
+constexpr int T_THREADS = (T_SOFT + T_FEED + 2) * 32;
+constexpr int T_REGS = 80, T_SOFT_REGS = 96, T_REST_REGS = 48;        // a thread's registers at the launch, and as the warps divide them
+static_assert(T_SOFT * T_SOFT_REGS + (T_FEED + 2) * T_REST_REGS <= (T_SOFT + T_FEED + 2) * T_REGS, "no more than the block was launched with");
+static_assert(T_THREADS / 32 <= 24, "the table of requests has room for that many warps");
+static_assert(T_SOFT % 4 == 0 && (T_FEED + 2) % 4 == 0, "registers are divided by groups of four warps");
 constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
 constexpr int T_JOIN_STEPS = 4;       // what a join costs, in pages
@@ -29,6 +35,17 @@ constexpr float T_RESCALE_STEP = 4.0f, T_OFFSET = 4.0f, T_LEAP = 15.0f;      // 
 constexpr int T_STAGES = 2;           // tiles of K, and of V, in shared memory
 constexpr int T_E0 = 8;               // ring of the tiles' first entries (two pages each): more than the tiles in flight
 constexpr int T_NO_PAGE = INT_MAX / 2;
+
+// The feed.  TMA brings codes and scales of a page's K or V, page after page, into a ring of T_RAW places; a step turns ROWS of its rows into fp16, 32
+// channels a lane.
+constexpr int T_RAW = 3;
+template <int D>
+struct Feed {
+    static constexpr int PARTS = D / 32, ROWS = 32 / PARTS, STEPS = PAGE / ROWS, RAW = PAGE * (D / 2 + D / 16);
+};
+__device__ __forceinline__ void t_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
 template <int D>
 struct Tc4Shape {
@@ -42,24 +59,16 @@ struct Tc4Shape {
     static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [tile parity; 2: sums][group][page of the tile][row]: maxima so far
     static constexpr int OFF_TAB = OFF_MX + 3 * 2 * 2 * T_ROWS * 4;
     static constexpr int OFF_UP = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;      // from a row's S to log2 units
-    static constexpr int SMEM = OFF_UP + T_UNIT * 4 + 1024;           // 1024: alignment slack
+    static constexpr int OFF_RAW = OFF_UP + T_UNIT * 4;
+    static constexpr int SMEM = OFF_RAW + T_RAW * Feed<D>::RAW + 1024;      // 1024: alignment slack
     // D fp32, A and B fp16, M = 128.  S: both K-major, N = 64 per page.  P V: B (V) MN-major, N = D.
     static constexpr uint32_t IDESC_S1 = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_S2 = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 };
 
-// Rows of codes of a page that a warp turns into fp16 at a time: 8 (or 16 for heads of 64), 32 channels a lane.
 template <int D>
-struct Feed {
-    static constexpr int QUARTERS = D / 32, ROWS = 32 / QUARTERS, STEPS = 2 * PAGE / ROWS;       // steps of a tile of K, or of V
-    static constexpr int MINE = (STEPS + T_FEED - 1) / T_FEED;
-    uint4 code[MINE];
-    uint16_t scale[MINE];
-};
-
-template <int D>
-__global__ void __launch_bounds__(T_THREADS, 1)
+__global__ void __launch_bounds__(T_THREADS, 1) /* T_REGS registers */
 paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, __nv_bfloat16* out, float scale_log2, PagedWork wk, int min_rows) {
     using S = Tc4Shape<D>;
     const PagedView& pv = cache.pv;
@@ -69,9 +78,11 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     unsigned char* gen = t_smem_raw + (base - raw);
     const uint32_t bars = base + S::OFF_BAR;
     const uint32_t k_full = bars, k_empty = bars + 16, v_full = bars + 32, v_empty = bars + 48 /* [stage] each */, s_ready0 = bars + 64,
-                   p_ready0 = bars + 80, done0 = bars + 96 /* [group] each */, pair0 = bars + 112 /* [group][32 rows] */;
+                   p_ready0 = bars + 80, done0 = bars + 96 /* [group] each */, pair0 = bars + 112 /* [group][32 rows] */,
+                   raw_full = bars + 176, raw_empty = bars + 200 /* [place] each */;
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(gen + S::OFF_BAR + 240);
     volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 244);
+    volatile int* s_real = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 224);      // [place]: whether the page exists
     volatile int* s_redo = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 252);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
     float* s_mx = reinterpret_cast<float*>(gen + S::OFF_MX);
@@ -90,6 +101,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             a_bar_init(done0 + 8 * i, 1);
         }
         for (int i = 0; i < 8; ++i) a_bar_init(pair0 + 8 * i, 2);
+        for (int i = 0; i < T_RAW; ++i) { a_bar_init(raw_full + 8 * i, 1); a_bar_init(raw_empty + 8 * i, T_FEED); }
         *s_fail = 0;
         *s_redo = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -101,7 +113,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     const int w = blockIdx.x;
     if (threadIdx.x == 0) paged_note_none(wk, w);
     if (w >= tab.workers) return;                                     // the whole block, before it holds tensor memory
-    if (warp == T_SOFT + T_FEED) {
+    if (warp == T_SOFT + T_FEED + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(a_smem((const void*)s_tmem)), "r"(T_TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -109,148 +121,388 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     __syncthreads();
     a_fence_after();
     const uint32_t tmem = *s_tmem;
-    // softmax warps: group, page of the tile, 32 rows of the group (a warp reaches the tensor-memory lanes of its number mod 4)
-    const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
-    const int r = wl * 32 + lane, R = grp * T_ROWS + r;               // row: lane of tensor memory, row of the unit
-
+    // The line as every warp walks it, at its own place in the code.  The rest of a unit that another worker began comes last: the workers then
+    // begin units at their first page at the same time, and those of one KV head read the same pages from L2.
     const long long begin = tab.share(w);
-    long long end = tab.share(w + 1);
-    // tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
-    // stretches with tiles, of group 0 and 1
-    unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
-    unsigned ex = 0;                                                  // barriers of the two warps of a row so far
+    long long x = begin, end = tab.share(w + 1), last = 0;            // last: end of that rest, if it was put off
     bool careful = false;                                             // this stretch again, every tile's maximum first
-    // The rest of a unit that another worker began comes last: the workers then begin units at their first page at the same time, and
-    // those of one KV head read the same pages from L2.
-    long long last = 0;                                               // end of that rest, if it was put off
-    for (long long x = begin; x < end || last;) {
-        if (x >= end) { x = begin; end = last; }
-        const PagedItem it = paged_item<0>(tab, pb, x, end, w);
-        if (x == begin && !last && it.slot == 2 * w && x + it.steps < end) { last = x += it.steps; continue; }
-        if (end == last) last = 0;
-        const int npage = it.p1 - it.p0;
-        const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
-        const bool both = rows > T_ROWS;
-        const bool soft = warp < T_SOFT && (grp == 0 || both);
-        const bool valid = soft && R < rows;
-        const int tok = valid ? pb.by_g.div(row_first + R) : it.tok0, head = valid ? row_first + R - tok * g : 0;
-        const int pos = it.q.len - it.q.n + tok;
-        const int see_hi = valid ? max(pos + 1, 0) : 0;               // entries the row sees: see_lo .. see_hi - 1
-        const int see_lo = valid && pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
-        const int ntile = (npage + 1) / 2;
-        if (ntile > 0) {
-            if (soft) {
-                // neighbouring lanes have neighbouring 16 bytes of a row; the two warps of 32 rows take 16 each
-                constexpr int CPR = D / 8;                            // 16-byte chunks of a row
-                const int c = lane % CPR, ksh = p4_shift(cache, 0, it.h);
-#pragma unroll 2
-                for (int k = 0; k < CPR / 2; ++k) {
-                    const int rq = wl * 32 + half * 16 + k * (32 / CPR) + lane / CPR, row = row_first + grp * T_ROWS + rq, qt = pb.by_g.div(row);
-                    const __nv_bfloat16* src = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + row - qt * g) * d + c * 8;
-                    const uint4 v = grp * T_ROWS + rq < rows && c * 8 < d ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
-                    const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
-                    float top = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(vw[e] << 16)), fabsf(__uint_as_float(vw[e] & 0xffff0000u))));
-#pragma unroll
-                    for (int o = 1; o < CPR; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const int up = top > 0.f ? max(-60, min(60, 137 - (int)(__float_as_uint(top) >> 23))) : 0;
-                    const float f = p4_pow2(up);
-                    uint32_t w4[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w4[e] = p4_f16x2(__uint_as_float(vw[e] << 16) * f, __uint_as_float(vw[e] & 0xffff0000u) * f);
-                    *reinterpret_cast<uint4*>(gen + S::OFF_Q + (grp * S::PLANES + (c >> 3)) * T_QPLANE + rq * 128 + (((c & 7) ^ (rq & 7)) << 4)) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
-                    if (c == 0) s_up[grp * T_ROWS + rq] = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // Q and the barriers, before the async proxy uses them
-            a_fence_before();
-            // everyone but the warps that bring K and V: their rings are free since the end of the stretch before
-            if (warp < T_SOFT || warp == T_SOFT + T_FEED) asm volatile("bar.sync 1, %0;" ::"n"(T_THREADS - 32 * T_FEED) : "memory");
-            a_fence_after();
+    PagedItem it;
+    auto next_stretch = [&]() {
+        while (x < end || last) {
+            if (x >= end) { x = begin; end = last; }
+            it = paged_item<0>(tab, pb, x, end, w);
+            if (x == begin && !last && it.slot == 2 * w && x + it.steps < end) { last = x += it.steps; continue; }
+            if (end == last) last = 0;
+            return true;
+        }
+        return false;
+    };
+    auto end_stretch = [&]() {                                        // false: a wait gave up
+        a_fence_before();
+        __syncthreads();                                              // Q and tensor memory are free for the next stretch
+        a_fence_after();
+        if (*s_fail) return false;
+        careful = !careful && *s_redo;                                // (a careful stretch sets no flag)
+        if (!careful) {
+            x += it.steps;
+        } else {
+            __syncthreads();                                          // everyone has read the flag
+            if (threadIdx.x == 0) *s_redo = 0;
+        }
+        return true;
+    };
+    // Tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
+    // stretches with tiles, of group 0 and 1.
+    unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
 
-            if (warp >= T_SOFT && warp < T_SOFT + T_FEED) {
-                // ---- K and V: lane l holds page l of the current run of 32.  Step j of a tile of K or V (rows j ROWS .. of its two pages) is
-                // warp j mod T_FEED's for K, and the steps of V begin where those of K ended.
-                using F = Feed<D>;
-                const int fw = warp - T_SOFT, part = lane / 8 % F::QUARTERS, lrow = lane % 8 + 8 * (lane / 8 / F::QUARTERS);
-                const bool on = part * 32 < d;                        // not a missing column
-                int phys = 0;
-                F kf, vf;
-                auto begin = [&](int kv) { return kv ? (fw + T_FEED - F::STEPS % T_FEED) % T_FEED : fw; };
-                auto pages = [&](int i, int h) { return __shfl_sync(0xffffffffu, phys, (2 * i + h) & 31); };
-                auto fetch = [&](int kv, int i, F& f) {
-                    const int ph[2] = {pages(i, 0), 2 * i + 1 < npage ? pages(i, 1) : -1};
+    if (warp < T_SOFT) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(T_SOFT_REGS));
+        // group, page of the tile, 32 rows of the group (a warp reaches the tensor-memory lanes of its number mod 4)
+        const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
+        const int r = wl * 32 + lane, R = grp * T_ROWS + r;           // row: lane of tensor memory, row of the unit
+        unsigned ex = 0;                                              // barriers of the two warps of a row so far
+        while (next_stretch()) {
+            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+            const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
+            const bool both = rows > T_ROWS, soft = grp == 0 || both;
+            const bool valid = soft && R < rows;
+            const int tok = valid ? pb.by_g.div(row_first + R) : it.tok0, head = valid ? row_first + R - tok * g : 0;
+            const int pos = it.q.len - it.q.n + tok;
+            const int see_hi = valid ? max(pos + 1, 0) : 0;           // entries the row sees: see_lo .. see_hi - 1
+            const int see_lo = valid && pb.window > 0 ? max(pos + 1 - pb.window, 0) : 0;
+            if (ntile > 0) {
+                if (soft) {
+                    // neighbouring lanes have neighbouring 16 bytes of a row; the two warps of 32 rows take 16 each
+                    constexpr int CPR = D / 8;                            // 16-byte chunks of a row
+                    const int c = lane % CPR, ksh = p4_shift(cache, 0, it.h);
+#pragma unroll 2
+                    for (int k = 0; k < CPR / 2; ++k) {
+                        const int rq = wl * 32 + half * 16 + k * (32 / CPR) + lane / CPR, row = row_first + grp * T_ROWS + rq, qt = pb.by_g.div(row);
+                        const __nv_bfloat16* src = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + row - qt * g) * d + c * 8;
+                        const uint4 v = grp * T_ROWS + rq < rows && c * 8 < d ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+                        const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+                        float top = 0.f;
 #pragma unroll
-                    for (int n = 0; n < F::MINE; ++n) {
-                        const int j = begin(kv) + n * T_FEED, row = j * F::ROWS + lrow, h = row / PAGE, p = h ? ph[1] : ph[0];
-                        f.code[n] = make_uint4(0u, 0u, 0u, 0u);
-                        f.scale[n] = 0;
-                        // V behind the last entry stays zero: its weights are, but its scales may be NaN
-                        if (j < F::STEPS && p >= 0 && on && (kv == 0 || (it.p0 + 2 * i) * PAGE + row < it.q.len)) {
-                            const size_t at = ((size_t)p * pv.H + it.h) * PAGE + row % PAGE;
-                            f.code[n] = *reinterpret_cast<const uint4*>(cache.codes[kv] + at * (d / 2) + part * 16);
-                            f.scale[n] = *reinterpret_cast<const uint16_t*>(cache.scales[kv] + at * (d / 16) + part * 2);
+                        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(vw[e] << 16)), fabsf(__uint_as_float(vw[e] & 0xffff0000u))));
+#pragma unroll
+                        for (int o = 1; o < CPR; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const int up = top > 0.f ? max(-60, min(60, 137 - (int)(__float_as_uint(top) >> 23))) : 0;
+                        const float f = p4_pow2(up);
+                        uint32_t w4[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w4[e] = p4_f16x2(__uint_as_float(vw[e] << 16) * f, __uint_as_float(vw[e] & 0xffff0000u) * f);
+                        *reinterpret_cast<uint4*>(gen + S::OFF_Q + (grp * S::PLANES + (c >> 3)) * T_QPLANE + rq * 128 + (((c & 7) ^ (rq & 7)) << 4)) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+                        if (c == 0) s_up[grp * T_ROWS + rq] = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // Q, before the async proxy uses it
+                a_fence_before();
+                asm volatile("bar.sync 1, %0;" ::"n"((T_SOFT + 1) * 32) : "memory");      // with the issuing warp
+                a_fence_after();
+            }
+            if (soft) {
+                // ---- softmax warps: page `half` of every tile
+                const uint32_t lane_addr = tmem + ((uint32_t)(wl * 32) << 16);
+                const uint32_t s_addr = lane_addr + (uint32_t)(128 * grp + 64 * half), o_addr = lane_addr + (uint32_t)(256 + 128 * grp + half * (D / 2));
+                const uint32_t pair = pair0 + 8 * (grp * 4 + wl);
+                float* mx_mine = s_mx + (grp * 2 + half) * T_ROWS + r;
+                const float* mx_other = s_mx + (grp * 2 + (half ^ 1)) * T_ROWS + r;
+                constexpr int MX = 4 * T_ROWS;                            // from one buffer of maxima to the next
+                const unsigned gt = grp ? ct1 : ct;
+                const float to_log2 = ntile > 0 ? s_up[R] : 0.f;
+                const uint64_t sc2 = a_pack2(to_log2, to_log2);
+                float m_used = -INFINITY, m_mine = -INFINITY, l = 0.f;    // the reference (the same in both threads), this thread's maximum, its sum
+                bool ok = true;
+                // entries that every row of the warp sees (rows without a query see whatever the others do); once every row has a
+                // maximum, a tile of two pages in this span needs no look at the rows
+                const int all_hi = __reduce_min_sync(0xffffffffu, valid ? see_hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, see_lo);
+                bool primed = false;
+                for (int i = 0; i < ntile; ++i) {
+                    ok = __all_sync(0xffffffffu, a_bar_wait(s_ready0 + 8 * grp, (gt + i) & 1));
+                    if (!ok) break;
+                    a_fence_after();
+                    // first entries of both pages (-1: the tile is one page); what the row sees of them
+                    const int e0 = s_e0[(ct + i) % T_E0 * 2 + half], e1 = s_e0[(ct + i) % T_E0 * 2 + (half ^ 1)];
+                    auto sees = [&](int e) {
+                        return valid && e >= 0 && e < see_hi && e + PAGE > see_lo;
+                    };
+                    const bool inside = primed && !careful && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
+                    bool mine = true, some = true, edge = false, first = false;
+                    if (!inside) {
+                        mine = sees(e0);
+                        some = __any_sync(0xffffffffu, mine);             // of the warp's rows
+                        // a row that sees nothing of the page is weighed to nothing below (mref); only what lies behind the last
+                        // entry has to go, it may be NaN
+                        edge = mine ? e0 + PAGE > see_hi || e0 < see_lo : e0 + PAGE > it.q.len;
+                        // the same for both warps of the rows: a row that has seen nothing yet finds its maximum first
+                        first = careful || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
+                    }
+                    uint32_t sv[32];
+                    auto load = [&](int k) {                              // entries 32 k .. of the page, masked
+                        a_tmem_ld32(s_addr + 32 * k, sv);
+                        t_tmem_wait_ld();
+                        if (edge) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (e0 + 32 * k + e >= see_hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
+                        }
+                    };
+                    float m_all;
+                    if (first) {
+                        if (some) {
+#pragma unroll 1
+                            for (int k = 0; k < 2; ++k) {
+                                load(k);
+                                float mq[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                                for (int e = 0; e < 32; e += 4) {
+                                    mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                                    mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                                }
+                                if (mine) m_mine = fmaxf(m_mine, fmaxf(mq[0], mq[1]) * to_log2);     // to_log2 > 0
+                            }
+                        }
+                        mx_mine[(i & 1) * MX] = m_mine;
+                        ok = t_pair_sync(pair, ex);
+                        if (!ok) break;
+                        ++ex;
+                        m_all = fmaxf(m_mine, mx_other[(i & 1) * MX]);
+                    } else
+                        m_all = fmaxf(m_mine, mx_other[((i - 1) & 1) * MX]);
+                    if (__any_sync(0xffffffffu, m_all > m_used + T_RESCALE_STEP)) {
+                        const float mn = fmaxf(m_used, m_all);
+                        const float alpha = (m_used == -INFINITY) ? 0.0f : exp2f(m_used - mn);
+                        m_used = mn;
+                        l *= alpha;
+                        if (i > 0) {                                      // (O is complete up to the previous tile: see the commit of S)
+#pragma unroll 1
+                            for (int k = 0; k < D / 32; ++k) {
+                                uint32_t ov[16];
+                                t_tmem_ld16(o_addr + k * 16, ov);
+                                t_tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                                t_tmem_st16(o_addr + k * 16, ov);
+                            }
                         }
                     }
-                };
-                auto put = [&](int kv, int i, unsigned s, const F& f) {
+                    if (!primed) primed = __all_sync(0xffffffffu, m_used > -INFINITY || !valid);
+                    if (some) {
+                        // a row that sees nothing of the page weighs it against +inf: every weight is 0
+                        const float mref = !mine ? INFINITY : (m_used == -INFINITY) ? 0.0f : m_used;
+                        const uint64_t nm2 = a_pack2(T_OFFSET - mref, T_OFFSET - mref);
+                        uint64_t sq[2] = {0ull, 0ull};
+                        float mq[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int n = 0; n < F::MINE; ++n) {
-                        const int j = begin(kv) + n * T_FEED, row = j * F::ROWS + lrow;
-                        if (j >= F::STEPS || 2 * i + row / PAGE >= npage) continue;       // (a tile of one page: the other half is not read)
-                        // K: a plane holds the rows of both pages; V: planes of a page, then of the next
-                        unsigned char* plane = gen + s * S::TILE + (kv ? S::OFF_V + (row / PAGE * S::PLANES + part / 2) * T_PLANE + row % PAGE * 128
-                                                                       : part / 2 * S::KPLANE + row * 128);
-                        const uint32_t sc = p4_scales(f.scale[n]), lo = p4_both_low(sc), hi = p4_both_high(sc);
-                        const uint32_t word[4] = {f.code[n].x, f.code[n].y, f.code[n].z, f.code[n].w};
+                        for (int k = 0; k < 2; ++k) {
+                            load(k);
+                            uint32_t pk[16];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            uint32_t r4[4];
-                            p4_codes(word[x], r4);
-                            const uint32_t by = x < 2 ? lo : hi;
-                            *reinterpret_cast<uint4*>(plane + ((part % 2 * 4 + x) ^ (row & 7)) * 16) = make_uint4(p4_mul(r4[0], by), p4_mul(r4[1], by), p4_mul(r4[2], by), p4_mul(r4[3], by));
+                            for (int e = 0; e < 32; e += 2) {
+                                const uint64_t x2 = a_fma2(a_pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), sc2, nm2);
+                                float x0, x1, p0, p1;
+                                a_unpack2(x2, x0, x1);
+                                mq[(e >> 1) & 1] = a_max3(mq[(e >> 1) & 1], x0, x1);
+                                if ((e >> 1) % T_POLY_EVERY == T_POLY_EVERY - 1) {
+                                    a_exp2_fma2(x2, p0, p1);
+                                } else {
+                                    p0 = a_ex2(x0);
+                                    p1 = a_ex2(x1);
+                                }
+                                sq[(e >> 1) & 1] = a_add2(sq[(e >> 1) & 1], a_pack2(p0, p1));
+                                pk[e >> 1] = p4_f16x2(p0, p1);
+                            }
+                            t_tmem_st16(s_addr + 16 * k, pk);             // P: two entries per column, over the page's first 32 columns of S
                         }
+                        float a0, a1;
+                        a_unpack2(a_add2(sq[0], sq[1]), a0, a1);
+                        l += a0 + a1;
+                        const float mx = fmaxf(mq[0], mq[1]);
+                        if (mine) {
+                            m_mine = fmaxf(m_mine, mref - T_OFFSET + mx);
+                            if (!first && mx > T_LEAP) *s_redo = 1;
+                        }
+                    } else if (e0 >= 0) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = 0u;
+                        t_tmem_st16(s_addr, pk);
+                        t_tmem_st16(s_addr + 16, pk);
+                    }
+                    if (!first) mx_mine[(i & 1) * MX] = m_mine;           // read by the other thread at the next tile
+                    t_tmem_wait_st();
+                    a_fence_before();
+                    __syncwarp();
+                    if (lane == 0) a_bar_arrive(p_ready0 + 8 * grp);
+                }
+                if (ok && ntile > 0) ok = __all_sync(0xffffffffu, a_bar_wait(done0 + 8 * grp, (grp ? st1 : st0) & 1));
+                mx_mine[2 * MX] = l;                                      // the two threads' sums
+                if (ok) ok = t_pair_sync(pair, ex);
+                if (!ok) {
+                    if (lane == 0) *s_fail = 1;
+                } else {
+                    ++ex;
+                    a_fence_after();
+                    l += mx_other[2 * MX];
+                    if (m_used == -INFINITY && !(l != l)) l = 0.f;        // a row that sees nothing (the polynomial gives masked entries 2^-125)
+                    const float v_up = p4_pow2(p4_shift(cache, 1, it.h)), inv = l > 0.f ? v_up / l : (l == 0.f ? 0.f : l);
+                    uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * d + half * (D / 2));
+                    const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
+                    float* po = wk.part_o + pr * d + half * (D / 2);
+                    const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
+#pragma unroll 1
+                    for (int k = 0; k < D / 32; ++k) {
+                        uint32_t ov[16];
+                        if (ntile > 0) {
+                            t_tmem_ld16(o_addr + k * 16, ov);
+                            t_tmem_wait_ld();
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) ov[e] = zero ? 0u : it.slot < 0 ? ov[e] : __float_as_uint(__uint_as_float(ov[e]) * v_up);
+                        if (!valid) continue;
+                        if (it.slot < 0) {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 8) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int k2 = 0; k2 < 4; ++k2)
+                                    v[k2] = a_bf16x2(__uint_as_float(ov[e + 2 * k2]) * inv, __uint_as_float(ov[e + 2 * k2 + 1]) * inv);
+                                if (half * (D / 2) + k * 16 + e < d) op[k * 2 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; e += 8)
+                                if (half * (D / 2) + k * 16 + e < d) t_store32(po + k * 16 + e, ov + e);
+                        }
+                    }
+                    if (valid && it.slot >= 0 && half == 0) {
+                        wk.part_ml[pr * 2] = m_used;
+                        wk.part_ml[pr * 2 + 1] = l;
+                    }
+                }
+            }
+            ct += (unsigned)ntile;
+            st0 += ntile > 0;
+            if (both) { ct1 += (unsigned)ntile; st1 += ntile > 0; }
+            const long long at = x;
+            if (!end_stretch()) break;
+            if (!careful && it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0) paged_note_shared(wk, tab, it, at, w, row_first, rows);
+        }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(T_REST_REGS));      // (one instruction for the four warps of a group)
+    if (warp < T_SOFT + T_FEED) {
+        // ---- K and V
+        // Lanes: eight neighbours store four rows and two parts, all 32 banks.
+        using F = Feed<D>;
+        const int fw = warp - T_SOFT, part = (lane & 1) | (F::PARTS == 4 ? lane >> 4 << 1 : 0), lrow = (lane >> 1) % F::ROWS;
+        const int code_row = d / 2, scale_row = d / 16;
+        const bool on = part * 32 < d;                                // not a missing column
+        const uint32_t out0 = base + lrow * 128 + ((part % 2 * 4) ^ (lrow & 7)) * 16;
+        const uint32_t code0 = base + S::OFF_RAW + lrow * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + lrow * scale_row + (on ? part * 2 : 0);
+        unsigned rc = 0;                                              // pages of K and V before this one: the ring
+        bool ok = true;
+        while (next_stretch()) {
+            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+#pragma unroll 1
+            for (int i = 0; i < ntile && ok; ++i) {
+                const unsigned c = ct + i, s = c % T_STAGES;
+                const int two = 2 * i + 1 < npage;
+#pragma unroll 1
+                for (int kv = 0; kv < 2 && ok; ++kv) {
+                    if (c >= T_STAGES) ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
+                    // Steps of both pages, one line; warp fw takes every T_FEED-th, V's going on where K's ended.
+                    int j = kv ? (fw + T_FEED - 2 * F::STEPS % T_FEED) % T_FEED : fw;
+#pragma unroll 1
+                    for (int h = 0; h <= two && ok; ++h, ++rc) {
+                        const unsigned slot = rc % T_RAW;
+                        ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, (rc / T_RAW) & 1));
+                        if (!ok) break;
+                        // V behind the last entry is zero: its weights are, but its scales may be NaN
+                        const int real = !on || !s_real[slot] ? 0 : kv ? it.q.len - (it.p0 + 2 * i + h) * PAGE : PAGE;
+                        // K: a plane holds the rows of both pages; V: planes of a page, then of the next
+                        const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
+#pragma unroll 2
+                        for (; j < (h + 1) * F::STEPS; j += T_FEED) {
+                            const int row0 = j % F::STEPS * F::ROWS;
+                            uint32_t word[4], scale;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(word[0]), "=r"(word[1]), "=r"(word[2]), "=r"(word[3]) : "r"(code0 + slot * F::RAW + row0 * code_row));
+                            asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(scale) : "r"(scale0 + slot * F::RAW + row0 * scale_row));
+                            const uint32_t sc = p4_scales(row0 + lrow < real ? scale : 0u), lo = p4_both_low(sc), hi = p4_both_high(sc);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {             // (chunk x lies 16 x further, but for the swizzle)
+                                uint32_t r4[4];
+                                p4_codes(word[x], r4);
+                                const uint32_t by = x < 2 ? lo : hi;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((out + row0 * 128) ^ (x * 16)), "r"(p4_mul(r4[0], by)), "r"(p4_mul(r4[1], by)),
+                                             "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) a_bar_arrive(raw_empty + 8 * slot);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                };
-                auto look = [&](int i) {                              // the next 32 pages
-                    if ((i & 15) == 0) phys = 2 * i + lane < npage ? paged_physical(pb, pv, it.r, it.p0 + 2 * i + lane) : -1;
-                };
-                look(0);
-                fetch(0, 0, kf);
-                for (int i = 0; i < ntile; ++i) {
-                    const unsigned c = ct + i, s = c % T_STAGES;
-                    bool ok = true;
-                    fetch(1, i, vf);
-                    if (c >= T_STAGES) ok = __all_sync(0xffffffffu, a_bar_wait(k_empty + 8 * s, ((c / T_STAGES) - 1) & 1));
-                    if (ok) {
-                        if (fw == 0) {                                // a page that does not exist: every row masks it
-                            const int ph0 = pages(i, 0), ph1 = pages(i, 1);
-                            if (lane == 0) {
-                                s_e0[c % T_E0 * 2] = ph0 < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
-                                s_e0[c % T_E0 * 2 + 1] = 2 * i + 1 >= npage ? -1 : ph1 < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
-                            }
-                        }
-                        put(0, i, s, kf);
-                        if (lane == 0) a_bar_arrive(k_full + 8 * s);
-                        if (i + 1 < ntile) {
-                            look(i + 1);
-                            fetch(0, i + 1, kf);
-                        }
-                        if (c >= T_STAGES) ok = __all_sync(0xffffffffu, a_bar_wait(v_empty + 8 * s, ((c / T_STAGES) - 1) & 1));
-                    }
-                    if (!ok) {
-                        if (lane == 0) *s_fail = 1;
-                        break;
-                    }
-                    put(1, i, s, vf);
-                    if (lane == 0) a_bar_arrive(v_full + 8 * s);
+                    if (lane == 0 && ok) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
                 }
-            } else if (warp == T_SOFT + T_FEED) {
-                // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue
-                // order), for one group after the other
+            }
+            if (!ok && lane == 0) *s_fail = 1;
+            ct += (unsigned)ntile;
+            if (!end_stretch()) break;
+        }
+    } else if (warp == T_SOFT + T_FEED) {
+        // ---- copies: lane l holds page l of the current run of 32
+        unsigned rc = 0;
+        bool ok = true;
+        while (next_stretch()) {
+            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+            int phys = -1;
+#pragma unroll 1
+            for (int i = 0; i < ntile && ok; ++i) {
+                if ((i & 15) == 0) phys = 2 * i + lane < npage ? paged_physical(pb, pv, it.r, it.p0 + 2 * i + lane) : -1;
+                const int two = 2 * i + 1 < npage, page[2] = {__shfl_sync(0xffffffffu, phys, (2 * i) & 31), __shfl_sync(0xffffffffu, phys, (2 * i + 1) & 31)};
+                if (lane == 0) {                                      // a page that does not exist: every row masks it
+                    const unsigned c = ct + i;
+                    s_e0[c % T_E0 * 2] = page[0] < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
+                    s_e0[c % T_E0 * 2 + 1] = !two ? -1 : page[1] < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
+                }
+#pragma unroll 1
+                for (int n = 0; n < 2 * (1 + two) && ok; ++n, ++rc) {
+                    const int kv = n > two, p = page[two ? n & 1 : 0];
+                    const unsigned slot = rc % T_RAW;
+                    if (rc >= T_RAW) ok = __all_sync(0xffffffffu, a_bar_wait(raw_empty + 8 * slot, ((rc / T_RAW) - 1) & 1));
+                    if (!ok) break;
+                    if (lane == 0) {
+                        s_real[slot] = p >= 0;
+                        if (p < 0) {
+                            a_bar_arrive(raw_full + 8 * slot);
+                        } else {
+                            const size_t row = ((size_t)p * pv.H + it.h) * PAGE;
+                            const uint32_t dst = base + S::OFF_RAW + slot * Feed<D>::RAW;
+                            a_bar_expect_tx(raw_full + 8 * slot, PAGE * (d / 2 + d / 16));
+                            t_bulk(dst, cache.codes[kv] + row * (d / 2), PAGE * (d / 2), raw_full + 8 * slot);
+                            t_bulk(dst + PAGE * (d / 2), cache.scales[kv] + row * (d / 16), PAGE * (d / 16), raw_full + 8 * slot);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok && lane == 0) *s_fail = 1;
+            ct += (unsigned)ntile;
+            if (!end_stretch()) {                                     // copies in flight land before the block leaves (bounded)
+                for (unsigned k = rc > T_RAW ? rc - T_RAW : 0; k < rc; ++k) a_bar_wait(raw_full + 8 * (k % T_RAW), (k / T_RAW) & 1);
+                break;
+            }
+        }
+    } else {
+        // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue order), for one group
+        // after the other
+        while (next_stretch()) {
+            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+            const bool both = min(T_UNIT, it.q.n * g - it.u * T_UNIT) > T_ROWS;
+            if (ntile > 0) {
+                a_fence_before();
+                asm volatile("bar.sync 1, %0;" ::"n"((T_SOFT + 1) * 32) : "memory");      // Q is there
+                a_fence_after();
                 bool ok = true;
                 const uint32_t leader = t_elect();
                 const uint32_t ub = t_uniform(base), ut = t_uniform(tmem), uct = t_uniform(ct), uct1 = t_uniform(ct1);
@@ -303,207 +555,14 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                 }
                 if (!ok && lane == 0) *s_fail = 1;
             }
-        }
-        if (soft) {
-            // ---- softmax warps: page `half` of every tile
-            const uint32_t lane_addr = tmem + ((uint32_t)(wl * 32) << 16);
-            const uint32_t s_addr = lane_addr + (uint32_t)(128 * grp + 64 * half), o_addr = lane_addr + (uint32_t)(256 + 128 * grp + half * (D / 2));
-            const uint32_t pair = pair0 + 8 * (grp * 4 + wl);
-            float* mx_mine = s_mx + (grp * 2 + half) * T_ROWS + r;
-            const float* mx_other = s_mx + (grp * 2 + (half ^ 1)) * T_ROWS + r;
-            constexpr int MX = 4 * T_ROWS;                            // from one buffer of maxima to the next
-            const unsigned gt = grp ? ct1 : ct;
-            const float to_log2 = ntile > 0 ? s_up[R] : 0.f;
-            const uint64_t sc2 = a_pack2(to_log2, to_log2);
-            float m_used = -INFINITY, m_mine = -INFINITY, l = 0.f;    // the reference (the same in both threads), this thread's maximum, its sum
-            bool ok = true;
-            // entries that every row of the warp sees (rows without a query see whatever the others do); once every row has a
-            // maximum, a tile of two pages in this span needs no look at the rows
-            const int all_hi = __reduce_min_sync(0xffffffffu, valid ? see_hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, see_lo);
-            bool primed = false;
-            for (int i = 0; i < ntile; ++i) {
-                ok = __all_sync(0xffffffffu, a_bar_wait(s_ready0 + 8 * grp, (gt + i) & 1));
-                if (!ok) break;
-                a_fence_after();
-                // first entries of both pages (-1: the tile is one page); what the row sees of them
-                const int e0 = s_e0[(ct + i) % T_E0 * 2 + half], e1 = s_e0[(ct + i) % T_E0 * 2 + (half ^ 1)];
-                auto sees = [&](int e) {
-                    return valid && e >= 0 && e < see_hi && e + PAGE > see_lo;
-                };
-                const bool inside = primed && !careful && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
-                bool mine = true, some = true, edge = false, first = false;
-                if (!inside) {
-                    mine = sees(e0);
-                    some = __any_sync(0xffffffffu, mine);             // of the warp's rows
-                    // a row that sees nothing of the page is weighed to nothing below (mref); only what lies behind the last
-                    // entry has to go, it may be NaN
-                    edge = mine ? e0 + PAGE > see_hi || e0 < see_lo : e0 + PAGE > it.q.len;
-                    // the same for both warps of the rows: a row that has seen nothing yet finds its maximum first
-                    first = careful || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
-                }
-                uint32_t sv[32];
-                auto load = [&](int k) {                              // entries 32 k .. of the page, masked
-                    a_tmem_ld32(s_addr + 32 * k, sv);
-                    t_tmem_wait_ld();
-                    if (edge) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (e0 + 32 * k + e >= see_hi || e0 + 32 * k + e < see_lo) sv[e] = 0xff800000u;        // -inf
-                    }
-                };
-                float m_all;
-                if (first) {
-                    if (some) {
-#pragma unroll 1
-                        for (int k = 0; k < 2; ++k) {
-                            load(k);
-                            float mq[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                mq[0] = a_max3(mq[0], __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-                                mq[1] = a_max3(mq[1], __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
-                            }
-                            if (mine) m_mine = fmaxf(m_mine, fmaxf(mq[0], mq[1]) * to_log2);     // to_log2 > 0
-                        }
-                    }
-                    mx_mine[(i & 1) * MX] = m_mine;
-                    ok = t_pair_sync(pair, ex);
-                    if (!ok) break;
-                    ++ex;
-                    m_all = fmaxf(m_mine, mx_other[(i & 1) * MX]);
-                } else
-                    m_all = fmaxf(m_mine, mx_other[((i - 1) & 1) * MX]);
-                if (__any_sync(0xffffffffu, m_all > m_used + T_RESCALE_STEP)) {
-                    const float mn = fmaxf(m_used, m_all);
-                    const float alpha = (m_used == -INFINITY) ? 0.0f : exp2f(m_used - mn);
-                    m_used = mn;
-                    l *= alpha;
-                    if (i > 0) {                                      // (O is complete up to the previous tile: see the commit of S)
-#pragma unroll 1
-                        for (int k = 0; k < D / 32; ++k) {
-                            uint32_t ov[16];
-                            t_tmem_ld16(o_addr + k * 16, ov);
-                            t_tmem_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-                            t_tmem_st16(o_addr + k * 16, ov);
-                        }
-                    }
-                }
-                if (!primed) primed = __all_sync(0xffffffffu, m_used > -INFINITY || !valid);
-                if (some) {
-                    // a row that sees nothing of the page weighs it against +inf: every weight is 0
-                    const float mref = !mine ? INFINITY : (m_used == -INFINITY) ? 0.0f : m_used;
-                    const uint64_t nm2 = a_pack2(T_OFFSET - mref, T_OFFSET - mref);
-                    uint64_t sq[2] = {0ull, 0ull};
-                    float mq[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        load(k);
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const uint64_t x2 = a_fma2(a_pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), sc2, nm2);
-                            float x0, x1, p0, p1;
-                            a_unpack2(x2, x0, x1);
-                            mq[(e >> 1) & 1] = a_max3(mq[(e >> 1) & 1], x0, x1);
-                            if ((e >> 1) % T_POLY_EVERY == T_POLY_EVERY - 1) {
-                                a_exp2_fma2(x2, p0, p1);
-                            } else {
-                                p0 = a_ex2(x0);
-                                p1 = a_ex2(x1);
-                            }
-                            sq[(e >> 1) & 1] = a_add2(sq[(e >> 1) & 1], a_pack2(p0, p1));
-                            pk[e >> 1] = p4_f16x2(p0, p1);
-                        }
-                        t_tmem_st16(s_addr + 16 * k, pk);             // P: two entries per column, over the page's first 32 columns of S
-                    }
-                    float a0, a1;
-                    a_unpack2(a_add2(sq[0], sq[1]), a0, a1);
-                    l += a0 + a1;
-                    const float mx = fmaxf(mq[0], mq[1]);
-                    if (mine) {
-                        m_mine = fmaxf(m_mine, mref - T_OFFSET + mx);
-                        if (!first && mx > T_LEAP) *s_redo = 1;
-                    }
-                } else if (e0 >= 0) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) pk[e] = 0u;
-                    t_tmem_st16(s_addr, pk);
-                    t_tmem_st16(s_addr + 16, pk);
-                }
-                if (!first) mx_mine[(i & 1) * MX] = m_mine;           // read by the other thread at the next tile
-                t_tmem_wait_st();
-                a_fence_before();
-                __syncwarp();
-                if (lane == 0) a_bar_arrive(p_ready0 + 8 * grp);
-            }
-            if (ok && ntile > 0) ok = __all_sync(0xffffffffu, a_bar_wait(done0 + 8 * grp, (grp ? st1 : st0) & 1));
-            mx_mine[2 * MX] = l;                                      // the two threads' sums
-            if (ok) ok = t_pair_sync(pair, ex);
-            if (!ok) {
-                if (lane == 0) *s_fail = 1;
-            } else {
-                ++ex;
-                a_fence_after();
-                l += mx_other[2 * MX];
-                if (m_used == -INFINITY && !(l != l)) l = 0.f;        // a row that sees nothing (the polynomial gives masked entries 2^-125)
-                const float v_up = p4_pow2(p4_shift(cache, 1, it.h)), inv = l > 0.f ? v_up / l : (l == 0.f ? 0.f : l);
-                uint4* op = reinterpret_cast<uint4*>(out + ((size_t)(it.q.row0 + tok) * pb.Hq + (size_t)(it.h * g + head)) * d + half * (D / 2));
-                const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * T_UNIT + R;
-                float* po = wk.part_o + pr * d + half * (D / 2);
-                const bool zero = l == 0.f;                           // (also a stretch without tiles, whose O was never written)
-#pragma unroll 1
-                for (int k = 0; k < D / 32; ++k) {
-                    uint32_t ov[16];
-                    if (ntile > 0) {
-                        t_tmem_ld16(o_addr + k * 16, ov);
-                        t_tmem_wait_ld();
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) ov[e] = zero ? 0u : it.slot < 0 ? ov[e] : __float_as_uint(__uint_as_float(ov[e]) * v_up);
-                    if (!valid) continue;
-                    if (it.slot < 0) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 8) {
-                            uint32_t v[4];
-#pragma unroll
-                            for (int k2 = 0; k2 < 4; ++k2)
-                                v[k2] = a_bf16x2(__uint_as_float(ov[e + 2 * k2]) * inv, __uint_as_float(ov[e + 2 * k2 + 1]) * inv);
-                            if (half * (D / 2) + k * 16 + e < d) op[k * 2 + (e >> 3)] = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 8)
-                            if (half * (D / 2) + k * 16 + e < d) t_store32(po + k * 16 + e, ov + e);
-                    }
-                }
-                if (valid && it.slot >= 0 && half == 0) {
-                    wk.part_ml[pr * 2] = m_used;
-                    wk.part_ml[pr * 2 + 1] = l;
-                }
-            }
-        }
-        ct += (unsigned)ntile;
-        st0 += ntile > 0;
-        if (both) { ct1 += (unsigned)ntile; st1 += ntile > 0; }
-        a_fence_before();
-        __syncthreads();                                              // Q, the lists and tensor memory are free for the next stretch
-        a_fence_after();
-        if (*s_fail) break;
-        careful = !careful && *s_redo;                                // (a careful stretch sets no flag)
-        if (!careful) {
-            if (it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0) paged_note_shared(wk, tab, it, x, w, row_first, rows);
-            x += it.steps;
-        }
-        else {
-            __syncthreads();                                          // everyone has read the flag
-            if (threadIdx.x == 0) *s_redo = 0;
+            ct += (unsigned)ntile;
+            if (both) ct1 += (unsigned)ntile;
+            if (!end_stretch()) break;
         }
     }
+    }
     __syncthreads();
-    if (warp == T_SOFT + T_FEED) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");
+    if (warp == T_SOFT + T_FEED + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");
     if (threadIdx.x == 0 && *s_fail) latch_error(pb.status, TRIMKV_E_TIMEOUT);
 }
 

@@ -277,3 +277,33 @@ def test_streams_graphs_and_workspaces():
         for c, out in zip(caches, outs):
             want, bound = attention(c.k, c.v, q, cu, lens, c.table, d ** -0.5)
             assert ((out.double().cpu() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_chunks_of_many_requests(d):
+    """More requests than one warp lays out, long and short chunks and single tokens among them."""
+    rng = random.Random(d)
+    lens = [rng.choice([1, 64, 100, 300, 513]) for _ in range(70)]
+    new = [min(n, rng.choice([0, 1, 1, 40, 130, 257])) for n in lens]
+    check(lens, new, 1, 4, d, torch.bfloat16, seed=12)
+
+
+def test_a_chunk_over_a_long_request():
+    check([4200, 3], [300, 1], 1, 8, 128, torch.bfloat16, seed=13)
+    check([4200], [300], 2, 2, 96, torch.bfloat16, seed=14, window=1000)
+
+
+def test_chunk_rows_that_leap_late():
+    """A few late entries outweigh all before by far more than fp16 holds: their stretch is computed again, maxima first."""
+    H, g, d = 1, 2, 128
+    c = Cache4([1200], H, d, seed=15)
+    q, cu = queries([200], H * g, d, torch.bfloat16, seed=15)
+    kc, ks = c.arrays[0], c.arrays[1]
+    for e in (700, 1010, 1150):                               # these entries' keys become 64 times as large
+        page = int(c.table[0, e // PAGE])
+        ks[page, 0, e % PAGE] = torch.clamp(ks[page, 0, e % PAGE].int() + 48, max=126).to(torch.uint8)
+        c.k[page, 0, e % PAGE] = values(kc[page, :, e % PAGE, None], ks[page, :, e % PAGE, None], c.arrays[2])[0, 0]
+    out, st = run(c, q, cu, 200)
+    assert st == 0
+    want, bound = attention(c.k, c.v, q, cu, [1200], c.table, d ** -0.5)
+    assert ((out.double().cpu() - want).abs() <= bound).all()
