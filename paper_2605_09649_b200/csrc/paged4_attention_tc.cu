@@ -47,6 +47,14 @@ __device__ __forceinline__ void t_bulk(uint32_t dst, const void* src, uint32_t b
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// A worker's share of the line, as each kind of warp walks it at its own place in the code.  The rest of a unit that another worker began comes
+// last: the workers then begin units at their first page at the same time, and those of one KV head read the same pages from L2.
+// (In shared memory, a copy for each warp, and the table's own fields beside them: registers that the loops do without.)
+struct Line {
+    long long begin, x, end, last;            // last: end of that rest, if it was put off
+    int careful;                              // this stretch again, every tile's maximum first
+};
+
 template <int D>
 struct Tc4Shape {
     static constexpr int PLANES = D / 64;
@@ -59,13 +67,50 @@ struct Tc4Shape {
     static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [tile parity; 2: sums][group][page of the tile][row]: maxima so far
     static constexpr int OFF_TAB = OFF_MX + 3 * 2 * 2 * T_ROWS * 4;
     static constexpr int OFF_UP = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;      // from a row's S to log2 units
-    static constexpr int OFF_RAW = OFF_UP + T_UNIT * 4;
+    static constexpr int OFF_LINE = OFF_UP + T_UNIT * 4;
+    static constexpr int OFF_RAW = (OFF_LINE + T_THREADS / 32 * (int)sizeof(Line) + (int)sizeof(PagedTable) + 15) & ~15;
     static constexpr int SMEM = OFF_RAW + T_RAW * Feed<D>::RAW + 1024;      // 1024: alignment slack
     // D fp32, A and B fp16, M = 128.  S: both K-major, N = 64 per page.  P V: B (V) MN-major, N = D.
     static constexpr uint32_t IDESC_S1 = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_S2 = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 };
+
+__device__ __forceinline__ bool line_next(volatile Line* mem, const PagedTable* s_tab, const PagedBatch& pb, int w, PagedItem& it) {
+    const PagedTable tab = *s_tab;
+    long long x = mem->x, end = mem->end, last = mem->last;
+    const long long begin = mem->begin;
+    while (x < end || last) {
+        if (x >= end) { x = begin; end = last; }
+        it = paged_item<0>(tab, pb, x, end, w);
+        if (x == begin && !last && it.slot == 2 * w && x + it.steps < end) { last = x += it.steps; continue; }
+        if (end == last) last = 0;
+        __syncwarp();
+        mem->x = x;
+        mem->end = end;
+        mem->last = last;
+        return true;
+    }
+    return false;
+}
+__device__ __forceinline__ bool line_done(volatile Line* mem, long long steps, volatile int* s_fail, volatile int* s_redo) {      // false: a wait gave up
+    a_fence_before();
+    __syncthreads();                          // Q and tensor memory are free for the next stretch
+    a_fence_after();
+    if (*s_fail) return false;
+    const bool careful = !mem->careful && *s_redo;        // (a careful stretch sets no flag)
+    const long long x = mem->x;
+    __syncwarp();
+    mem->careful = careful;
+    if (!careful) {
+        mem->x = x + steps;
+    } else {
+        __syncthreads();                      // everyone has read the flag
+        if (threadIdx.x == 0) *s_redo = 0;
+    }
+    __syncwarp();
+    return true;
+}
 
 template <int D>
 __global__ void __launch_bounds__(T_THREADS, 1) /* T_REGS registers */
@@ -121,36 +166,17 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     __syncthreads();
     a_fence_after();
     const uint32_t tmem = *s_tmem;
-    // The line as every warp walks it, at its own place in the code.  The rest of a unit that another worker began comes last: the workers then
-    // begin units at their first page at the same time, and those of one KV head read the same pages from L2.
-    const long long begin = tab.share(w);
-    long long x = begin, end = tab.share(w + 1), last = 0;            // last: end of that rest, if it was put off
-    bool careful = false;                                             // this stretch again, every tile's maximum first
-    PagedItem it;
-    auto next_stretch = [&]() {
-        while (x < end || last) {
-            if (x >= end) { x = begin; end = last; }
-            it = paged_item<0>(tab, pb, x, end, w);
-            if (x == begin && !last && it.slot == 2 * w && x + it.steps < end) { last = x += it.steps; continue; }
-            if (end == last) last = 0;
-            return true;
-        }
-        return false;
-    };
-    auto end_stretch = [&]() {                                        // false: a wait gave up
-        a_fence_before();
-        __syncthreads();                                              // Q and tensor memory are free for the next stretch
-        a_fence_after();
-        if (*s_fail) return false;
-        careful = !careful && *s_redo;                                // (a careful stretch sets no flag)
-        if (!careful) {
-            x += it.steps;
-        } else {
-            __syncthreads();                                          // everyone has read the flag
-            if (threadIdx.x == 0) *s_redo = 0;
-        }
-        return true;
-    };
+    volatile Line* line = reinterpret_cast<Line*>(gen + S::OFF_LINE) + warp;
+    PagedTable* s_tab = reinterpret_cast<PagedTable*>(gen + S::OFF_LINE + T_THREADS / 32 * sizeof(Line));
+    if (threadIdx.x == 0) *s_tab = tab;
+    if (lane == 0) {
+        volatile Line* l = line;
+        l->begin = l->x = tab.share(w);
+        l->end = tab.share(w + 1);
+        l->last = 0;
+        l->careful = 0;
+    }
+    __syncthreads();
     // Tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
     // stretches with tiles, of group 0 and 1.
     unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
@@ -161,7 +187,9 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
         const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
         const int r = wl * 32 + lane, R = grp * T_ROWS + r;           // row: lane of tensor memory, row of the unit
         unsigned ex = 0;                                              // barriers of the two warps of a row so far
-        while (next_stretch()) {
+        PagedItem it;
+        while (line_next(line, s_tab, pb, w, it)) {
+            const bool again = line->careful != 0;
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
             const bool both = rows > T_ROWS, soft = grp == 0 || both;
@@ -226,7 +254,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                     auto sees = [&](int e) {
                         return valid && e >= 0 && e < see_hi && e + PAGE > see_lo;
                     };
-                    const bool inside = primed && !careful && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
+                    const bool inside = primed && !again && min(e0, e1) >= all_lo && max(e0, e1) + PAGE <= all_hi;      // (e1 < 0: not inside)
                     bool mine = true, some = true, edge = false, first = false;
                     if (!inside) {
                         mine = sees(e0);
@@ -235,7 +263,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                         // entry has to go, it may be NaN
                         edge = mine ? e0 + PAGE > see_hi || e0 < see_lo : e0 + PAGE > it.q.len;
                         // the same for both warps of the rows: a row that has seen nothing yet finds its maximum first
-                        first = careful || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
+                        first = again || i == 0 || __any_sync(0xffffffffu, m_used == -INFINITY && (mine || sees(e1)));
                     }
                     uint32_t sv[32];
                     auto load = [&](int k) {                              // entries 32 k .. of the page, masked
@@ -384,9 +412,9 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             ct += (unsigned)ntile;
             st0 += ntile > 0;
             if (both) { ct1 += (unsigned)ntile; st1 += ntile > 0; }
-            const long long at = x;
-            if (!end_stretch()) break;
-            if (!careful && it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0) paged_note_shared(wk, tab, it, at, w, row_first, rows);
+            const long long at = line->x;
+            if (!line_done(line, it.steps, s_fail, s_redo)) break;
+            if (it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0 && !line->careful) paged_note_shared(wk, *s_tab, it, at, w, row_first, rows);
         }
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(T_REST_REGS));      // (one instruction for the four warps of a group)
@@ -401,7 +429,8 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
         const uint32_t code0 = base + S::OFF_RAW + lrow * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + lrow * scale_row + (on ? part * 2 : 0);
         unsigned rc = 0;                                              // pages of K and V before this one: the ring
         bool ok = true;
-        while (next_stretch()) {
+        PagedItem it;
+        while (line_next(line, s_tab, pb, w, it)) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
 #pragma unroll 1
             for (int i = 0; i < ntile && ok; ++i) {
@@ -447,27 +476,28 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             }
             if (!ok && lane == 0) *s_fail = 1;
             ct += (unsigned)ntile;
-            if (!end_stretch()) break;
+            if (!line_done(line, it.steps, s_fail, s_redo)) break;
         }
     } else if (warp == T_SOFT + T_FEED) {
         // ---- copies: lane l holds page l of the current run of 32
         unsigned rc = 0;
         bool ok = true;
-        while (next_stretch()) {
+        PagedItem it;
+        while (line_next(line, s_tab, pb, w, it)) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             int phys = -1;
 #pragma unroll 1
             for (int i = 0; i < ntile && ok; ++i) {
                 if ((i & 15) == 0) phys = 2 * i + lane < npage ? paged_physical(pb, pv, it.r, it.p0 + 2 * i + lane) : -1;
-                const int two = 2 * i + 1 < npage, page[2] = {__shfl_sync(0xffffffffu, phys, (2 * i) & 31), __shfl_sync(0xffffffffu, phys, (2 * i + 1) & 31)};
+                const int two = 2 * i + 1 < npage, page0 = __shfl_sync(0xffffffffu, phys, (2 * i) & 31), page1 = __shfl_sync(0xffffffffu, phys, (2 * i + 1) & 31);
                 if (lane == 0) {                                      // a page that does not exist: every row masks it
                     const unsigned c = ct + i;
-                    s_e0[c % T_E0 * 2] = page[0] < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
-                    s_e0[c % T_E0 * 2 + 1] = !two ? -1 : page[1] < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
+                    s_e0[c % T_E0 * 2] = page0 < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
+                    s_e0[c % T_E0 * 2 + 1] = !two ? -1 : page1 < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
                 }
 #pragma unroll 1
                 for (int n = 0; n < 2 * (1 + two) && ok; ++n, ++rc) {
-                    const int kv = n > two, p = page[two ? n & 1 : 0];
+                    const int kv = n > two, p = two && (n & 1) ? page1 : page0;
                     const unsigned slot = rc % T_RAW;
                     if (rc >= T_RAW) ok = __all_sync(0xffffffffu, a_bar_wait(raw_empty + 8 * slot, ((rc / T_RAW) - 1) & 1));
                     if (!ok) break;
@@ -488,7 +518,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             }
             if (!ok && lane == 0) *s_fail = 1;
             ct += (unsigned)ntile;
-            if (!end_stretch()) {                                     // copies in flight land before the block leaves (bounded)
+            if (!line_done(line, it.steps, s_fail, s_redo)) {                                     // copies in flight land before the block leaves (bounded)
                 for (unsigned k = rc > T_RAW ? rc - T_RAW : 0; k < rc; ++k) a_bar_wait(raw_full + 8 * (k % T_RAW), (k / T_RAW) & 1);
                 break;
             }
@@ -496,7 +526,8 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     } else {
         // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue order), for one group
         // after the other
-        while (next_stretch()) {
+        PagedItem it;
+        while (line_next(line, s_tab, pb, w, it)) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             const bool both = min(T_UNIT, it.q.n * g - it.u * T_UNIT) > T_ROWS;
             if (ntile > 0) {
@@ -557,7 +588,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             }
             ct += (unsigned)ntile;
             if (both) ct1 += (unsigned)ntile;
-            if (!end_stretch()) break;
+            if (!line_done(line, it.steps, s_fail, s_redo)) break;
         }
     }
     }
