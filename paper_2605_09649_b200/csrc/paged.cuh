@@ -149,8 +149,8 @@ inline bool paged_always_whole(const PagedBatch& pb, int H, int tile_rows, int w
 struct PagedTableMem {
     long long grp[PAGED_GROUPS + 1];          // steps before a group
     int4 req[PAGED_GROUPS];                   // {row0, n, len, units} of each request where a group is one request
-    long long steps[24], units[24];           // of the requests of each warp (the 4-bit tensor-core kernel has 24)
-    int longest[24], whole;
+    long long steps[28], units[28];           // of the requests of each warp (the 4-bit tensor-core kernel has 28)
+    int longest[28], whole;
 };
 struct PagedTable {
     PagedTableMem* mem;

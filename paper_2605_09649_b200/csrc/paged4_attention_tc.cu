@@ -22,12 +22,12 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int T_ROWS = 128, T_UNIT = PAGED_TC_ROWS;
 constexpr int T_PLANE = PAGE * 128;                                   // 64 entries x 64 columns
 constexpr int T_QPLANE = T_ROWS * 128;
-constexpr int T_SOFT = 16, T_FEED = 6;                                // softmax warps; warps that make K and V; then one that copies, one that issues
-constexpr int T_THREADS = (T_SOFT + T_FEED + 2) * 32;
-constexpr int T_REGS = 80, T_SOFT_REGS = 96, T_REST_REGS = 48;        // a thread's registers at the launch, and as the warps divide them
-static_assert(T_SOFT * T_SOFT_REGS + (T_FEED + 2) * T_REST_REGS <= (T_SOFT + T_FEED + 2) * T_REGS, "no more than the block was launched with");
-static_assert(T_THREADS / 32 <= 24, "the table of requests has room for that many warps");
-static_assert(T_SOFT % 4 == 0 && (T_FEED + 2) % 4 == 0, "registers are divided by groups of four warps");
+constexpr int T_SOFT = 16, T_FEED = 8;                                // softmax warps; warps that make K and V; then one that copies, one that issues, two to fill the group
+constexpr int T_THREADS = (T_SOFT + T_FEED + 4) * 32;
+constexpr int T_REGS = 72, T_SOFT_REGS = 96, T_REST_REGS = 40;        // a thread's registers at the launch, and as the warps divide them
+static_assert(T_SOFT * T_SOFT_REGS + (T_THREADS / 32 - T_SOFT) * T_REST_REGS <= T_THREADS / 32 * T_REGS, "no more than the block was launched with");
+static_assert(T_THREADS / 32 <= 28, "the table of requests has room for that many warps");
+static_assert(T_SOFT % 4 == 0 && T_THREADS / 32 % 4 == 0, "registers are divided by groups of four warps");
 constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
 constexpr int T_JOIN_STEPS = 4;       // what a join costs, in pages
@@ -42,16 +42,20 @@ constexpr int T_RAW = 3;
 template <int D>
 struct Feed {
     static constexpr int PARTS = D / 32, ROWS = 32 / PARTS, STEPS = PAGE / ROWS, RAW = PAGE * (D / 2 + D / 16);
+    static_assert(T_FEED % STEPS == 0 && T_FEED <= 2 * STEPS, "a warp has one step of a page, or of one of a tile's two");
 };
 __device__ __forceinline__ void t_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// A worker's share of the line, as each kind of warp walks it at its own place in the code.  The rest of a unit that another worker began comes
-// last: the workers then begin units at their first page at the same time, and those of one KV head read the same pages from L2.
-// (In shared memory, a copy for each warp, and the table's own fields beside them: registers that the loops do without.)
-struct Line {
+// A worker's share of the line and the stretch of it that the block is at, in shared memory: one warp moves it on between two barriers of the block,
+// the others keep none of it in registers.  The rest of a unit that another worker began comes last: the workers then begin units
+// at their first page at the same time, and those of one KV head read the same pages from L2.
+struct Walk {
+    PagedTable tab;
     long long begin, x, end, last;            // last: end of that rest, if it was put off
+    PagedItem it;
+    int more;                                 // whether there is a stretch
     int careful;                              // this stretch again, every tile's maximum first
 };
 
@@ -67,8 +71,8 @@ struct Tc4Shape {
     static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [tile parity; 2: sums][group][page of the tile][row]: maxima so far
     static constexpr int OFF_TAB = OFF_MX + 3 * 2 * 2 * T_ROWS * 4;
     static constexpr int OFF_UP = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;      // from a row's S to log2 units
-    static constexpr int OFF_LINE = OFF_UP + T_UNIT * 4;
-    static constexpr int OFF_RAW = (OFF_LINE + T_THREADS / 32 * (int)sizeof(Line) + (int)sizeof(PagedTable) + 15) & ~15;
+    static constexpr int OFF_WALK = OFF_UP + T_UNIT * 4;
+    static constexpr int OFF_RAW = (OFF_WALK + (int)sizeof(Walk) + 15) & ~15;
     static constexpr int SMEM = OFF_RAW + T_RAW * Feed<D>::RAW + 1024;      // 1024: alignment slack
     // D fp32, A and B fp16, M = 128.  S: both K-major, N = 64 per page.  P V: B (V) MN-major, N = D.
     static constexpr uint32_t IDESC_S1 = (1u << 4) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -76,40 +80,37 @@ struct Tc4Shape {
     static constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 };
 
-__device__ __forceinline__ bool line_next(volatile Line* mem, const PagedTable* s_tab, const PagedBatch& pb, int w, PagedItem& it) {
-    const PagedTable tab = *s_tab;
-    long long x = mem->x, end = mem->end, last = mem->last;
-    const long long begin = mem->begin;
-    while (x < end || last) {
+// By one warp: the first stretch, or the one behind that which is done (or the same again).
+__device__ __forceinline__ void walk_on(Walk* k, bool begun, const PagedBatch& pb, const PagedWork& wk, int w, int unit_rows, volatile int* s_redo) {
+    const PagedTable tab = k->tab;
+    const long long begin = k->begin;
+    long long x = k->x, end = k->end, last = k->last;
+    PagedItem it = k->it;
+    const bool again = begun && !k->careful && *s_redo;       // (a careful stretch sets no flag)
+    bool more = again;
+    if (begun && !again) {
+        if (it.slot >= 0 && (it.slot & 1) && (threadIdx.x & 31) == 0)
+            paged_note_shared(wk, tab, it, x, w, it.u * unit_rows, min(unit_rows, it.q.n * pb.g - it.u * unit_rows));
+        x += it.steps;
+    }
+    while (!again && (x < end || last)) {
         if (x >= end) { x = begin; end = last; }
         it = paged_item<0>(tab, pb, x, end, w);
         if (x == begin && !last && it.slot == 2 * w && x + it.steps < end) { last = x += it.steps; continue; }
         if (end == last) last = 0;
-        __syncwarp();
-        mem->x = x;
-        mem->end = end;
-        mem->last = last;
-        return true;
-    }
-    return false;
-}
-__device__ __forceinline__ bool line_done(volatile Line* mem, long long steps, volatile int* s_fail, volatile int* s_redo) {      // false: a wait gave up
-    a_fence_before();
-    __syncthreads();                          // Q and tensor memory are free for the next stretch
-    a_fence_after();
-    if (*s_fail) return false;
-    const bool careful = !mem->careful && *s_redo;        // (a careful stretch sets no flag)
-    const long long x = mem->x;
-    __syncwarp();
-    mem->careful = careful;
-    if (!careful) {
-        mem->x = x + steps;
-    } else {
-        __syncthreads();                      // everyone has read the flag
-        if (threadIdx.x == 0) *s_redo = 0;
+        more = true;
+        break;
     }
     __syncwarp();
-    return true;
+    if ((threadIdx.x & 31) == 0) {
+        k->x = x;
+        k->end = end;
+        k->last = last;
+        k->it = it;
+        k->more = more;
+        k->careful = again;
+        *s_redo = 0;
+    }
 }
 
 template <int D>
@@ -127,7 +128,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                    raw_full = bars + 176, raw_empty = bars + 200 /* [place] each */;
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(gen + S::OFF_BAR + 240);
     volatile int* s_fail = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 244);
-    volatile int* s_real = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 224);      // [place]: whether the page exists
+    volatile int* s_real = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 224);      // [place]: rows of the page that count
     volatile int* s_redo = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 252);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
     float* s_mx = reinterpret_cast<float*>(gen + S::OFF_MX);
@@ -166,17 +167,27 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     __syncthreads();
     a_fence_after();
     const uint32_t tmem = *s_tmem;
-    volatile Line* line = reinterpret_cast<Line*>(gen + S::OFF_LINE) + warp;
-    PagedTable* s_tab = reinterpret_cast<PagedTable*>(gen + S::OFF_LINE + T_THREADS / 32 * sizeof(Line));
-    if (threadIdx.x == 0) *s_tab = tab;
-    if (lane == 0) {
-        volatile Line* l = line;
-        l->begin = l->x = tab.share(w);
-        l->end = tab.share(w + 1);
-        l->last = 0;
-        l->careful = 0;
+    Walk* walk = reinterpret_cast<Walk*>(gen + S::OFF_WALK);
+    if (threadIdx.x == 0) {
+        walk->tab = tab;
+        walk->begin = walk->x = tab.share(w);
+        walk->end = tab.share(w + 1);
+        walk->last = 0;
+        walk->careful = 0;
     }
+    __syncwarp();
+    if (warp == 0) walk_on(walk, false, pb, wk, w, T_UNIT, s_redo);
     __syncthreads();
+    const PagedItem& it = walk->it;
+    auto stretch_done = [&]() {                                       // false: a wait gave up
+        a_fence_before();
+        __syncthreads();                                              // Q and tensor memory are free for the next stretch
+        a_fence_after();
+        if (*s_fail) return false;
+        if (warp == 0) walk_on(walk, true, pb, wk, w, T_UNIT, s_redo);
+        __syncthreads();
+        return true;
+    };
     // Tiles of the stretches before this one: of the rings, and of group 1, whose barriers rest while it has no rows; and the
     // stretches with tiles, of group 0 and 1.
     unsigned ct = 0, ct1 = 0, st0 = 0, st1 = 0;
@@ -187,9 +198,8 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
         const int grp = (warp >> 3) & 1, half = (warp >> 2) & 1, wl = warp & 3;
         const int r = wl * 32 + lane, R = grp * T_ROWS + r;           // row: lane of tensor memory, row of the unit
         unsigned ex = 0;                                              // barriers of the two warps of a row so far
-        PagedItem it;
-        while (line_next(line, s_tab, pb, w, it)) {
-            const bool again = line->careful != 0;
+        while (walk->more) {
+            const bool again = walk->careful != 0;
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             const int row_first = it.u * T_UNIT, rows = min(T_UNIT, it.q.n * g - row_first);
             const bool both = rows > T_ROWS, soft = grp == 0 || both;
@@ -412,9 +422,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             ct += (unsigned)ntile;
             st0 += ntile > 0;
             if (both) { ct1 += (unsigned)ntile; st1 += ntile > 0; }
-            const long long at = line->x;
-            if (!line_done(line, it.steps, s_fail, s_redo)) break;
-            if (it.slot >= 0 && (it.slot & 1) && threadIdx.x == 0 && !line->careful) paged_note_shared(wk, *s_tab, it, at, w, row_first, rows);
+            if (!stretch_done()) break;
         }
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(T_REST_REGS));      // (one instruction for the four warps of a group)
@@ -425,65 +433,72 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
         const int fw = warp - T_SOFT, part = (lane & 1) | (F::PARTS == 4 ? lane >> 4 << 1 : 0), lrow = (lane >> 1) % F::ROWS;
         const int code_row = d / 2, scale_row = d / 16;
         const bool on = part * 32 < d;                                // not a missing column
-        const uint32_t out0 = base + lrow * 128 + ((part % 2 * 4) ^ (lrow & 7)) * 16;
-        const uint32_t code0 = base + S::OFF_RAW + lrow * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + lrow * scale_row + (on ? part * 2 : 0);
-        unsigned rc = 0;                                              // pages of K and V before this one: the ring
+        const uint32_t out0 = base + (fw % F::STEPS * F::ROWS + lrow) * 128 + ((part % 2 * 4) ^ (lrow & 7)) * 16;
+        const uint32_t code0 = base + S::OFF_RAW + (fw % F::STEPS * F::ROWS + lrow) * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + (fw % F::STEPS * F::ROWS + lrow) * scale_row + (on ? part * 2 : 0);
+        const int row0 = fw % F::STEPS * F::ROWS;                     // this warp's step of a page; (heads of 64: of every other page)
+        unsigned slot = 0, phase = 0;                                 // place in the ring of the page that is read next
         bool ok = true;
-        PagedItem it;
-        while (line_next(line, s_tab, pb, w, it)) {
+        while (walk->more) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+            uint32_t word[4], scale;
+            int real;
+            auto take = [&](uint32_t (&wd)[4], uint32_t& sc, int& n) {
+                ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3]) : "r"(code0 + slot * F::RAW));
+                asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(sc) : "r"(scale0 + slot * F::RAW));
+                n = s_real[slot];
+            };
+            if (npage > 0) take(word, scale, real);
+            unsigned c = ct;
+            int kv = 0, h = 0, left = npage;                          // page h of K or V of tile c; pages of the tile and those behind it
 #pragma unroll 1
-            for (int i = 0; i < ntile && ok; ++i) {
-                const unsigned c = ct + i, s = c % T_STAGES;
-                const int two = 2 * i + 1 < npage;
-#pragma unroll 1
-                for (int kv = 0; kv < 2 && ok; ++kv) {
-                    if (c >= T_STAGES) ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
-                    // Steps of both pages, one line; warp fw takes every T_FEED-th, V's going on where K's ended.
-                    int j = kv ? (fw + T_FEED - 2 * F::STEPS % T_FEED) % T_FEED : fw;
-#pragma unroll 1
-                    for (int h = 0; h <= two && ok; ++h, ++rc) {
-                        const unsigned slot = rc % T_RAW;
-                        ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, (rc / T_RAW) & 1));
-                        if (!ok) break;
-                        // V behind the last entry is zero: its weights are, but its scales may be NaN
-                        const int real = !on || !s_real[slot] ? 0 : kv ? it.q.len - (it.p0 + 2 * i + h) * PAGE : PAGE;
-                        // K: a plane holds the rows of both pages; V: planes of a page, then of the next
-                        const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
-#pragma unroll 2
-                        for (; j < (h + 1) * F::STEPS; j += T_FEED) {
-                            const int row0 = j % F::STEPS * F::ROWS;
-                            uint32_t word[4], scale;
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(word[0]), "=r"(word[1]), "=r"(word[2]), "=r"(word[3]) : "r"(code0 + slot * F::RAW + row0 * code_row));
-                            asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(scale) : "r"(scale0 + slot * F::RAW + row0 * scale_row));
-                            const uint32_t sc = p4_scales(row0 + lrow < real ? scale : 0u), lo = p4_both_low(sc), hi = p4_both_high(sc);
+            for (int n = 0; n < 2 * npage && ok; ++n) {
+                __syncwarp();
+                if (lane == 0) a_bar_arrive(raw_empty + 8 * slot);    // in registers
+                if (++slot == T_RAW) { slot = 0; phase ^= 1; }
+                uint32_t next[4] = {0u, 0u, 0u, 0u}, next_scale = 0u;
+                int next_real = 0;
+                if (n + 1 < 2 * npage) take(next, next_scale, next_real);
+                const unsigned s = c % T_STAGES;
+                if (h == 0 && c >= T_STAGES && ok) ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
+                if (!ok) break;
+                if (F::STEPS == T_FEED || fw / F::STEPS == h) {
+                    // K: a plane holds the rows of both pages; V: planes of a page, then of the next
+                    const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
+                    const uint32_t sc = p4_scales(on && row0 + lrow < real ? scale : 0u), lo = p4_both_low(sc), hi = p4_both_high(sc);
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {             // (chunk x lies 16 x further, but for the swizzle)
-                                uint32_t r4[4];
-                                p4_codes(word[x], r4);
-                                const uint32_t by = x < 2 ? lo : hi;
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((out + row0 * 128) ^ (x * 16)), "r"(p4_mul(r4[0], by)), "r"(p4_mul(r4[1], by)),
-                                             "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
-                            }
-                        }
-                        __syncwarp();
-                        if (lane == 0) a_bar_arrive(raw_empty + 8 * slot);
+                    for (int x = 0; x < 4; ++x) {                     // (chunk x lies 16 x further, but for the swizzle)
+                        uint32_t r4[4];
+                        p4_codes(word[x], r4);
+                        const uint32_t by = x < 2 ? lo : hi;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out ^ (x * 16)), "r"(p4_mul(r4[0], by)), "r"(p4_mul(r4[1], by)),
+                                     "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
                     }
+                }
+                if (h == 1 || left == 1) {                            // the tile's last page
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0 && ok) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
+                    if (lane == 0) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
+                    h = 0;
+                    if (kv) { ++c; left -= 2; }
+                    kv ^= 1;
+                } else {
+                    h = 1;
                 }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) word[x] = next[x];
+                scale = next_scale;
+                real = next_real;
             }
             if (!ok && lane == 0) *s_fail = 1;
             ct += (unsigned)ntile;
-            if (!line_done(line, it.steps, s_fail, s_redo)) break;
+            if (!stretch_done()) break;
         }
     } else if (warp == T_SOFT + T_FEED) {
         // ---- copies: lane l holds page l of the current run of 32
         unsigned rc = 0;
         bool ok = true;
-        PagedItem it;
-        while (line_next(line, s_tab, pb, w, it)) {
+        while (walk->more) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             int phys = -1;
 #pragma unroll 1
@@ -502,7 +517,8 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                     if (rc >= T_RAW) ok = __all_sync(0xffffffffu, a_bar_wait(raw_empty + 8 * slot, ((rc / T_RAW) - 1) & 1));
                     if (!ok) break;
                     if (lane == 0) {
-                        s_real[slot] = p >= 0;
+                        // none of a page that does not exist; of V those up to the last entry (their weights are 0, but scales may be NaN)
+                        s_real[slot] = p < 0 ? 0 : kv ? it.q.len - (it.p0 + 2 * i + (two ? n & 1 : 0)) * PAGE : PAGE;
                         if (p < 0) {
                             a_bar_arrive(raw_full + 8 * slot);
                         } else {
@@ -518,16 +534,17 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             }
             if (!ok && lane == 0) *s_fail = 1;
             ct += (unsigned)ntile;
-            if (!line_done(line, it.steps, s_fail, s_redo)) {                                     // copies in flight land before the block leaves (bounded)
+            if (!stretch_done()) {                                     // copies in flight land before the block leaves (bounded)
                 for (unsigned k = rc > T_RAW ? rc - T_RAW : 0; k < rc; ++k) a_bar_wait(raw_full + 8 * (k % T_RAW), (k / T_RAW) & 1);
                 break;
             }
         }
+    } else if (warp > T_SOFT + T_FEED + 1) {
+        while (walk->more && stretch_done()) {}
     } else {
         // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue order), for one group
         // after the other
-        PagedItem it;
-        while (line_next(line, s_tab, pb, w, it)) {
+        while (walk->more) {
             const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
             const bool both = min(T_UNIT, it.q.n * g - it.u * T_UNIT) > T_ROWS;
             if (ntile > 0) {
@@ -588,7 +605,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             }
             ct += (unsigned)ntile;
             if (both) ct1 += (unsigned)ntile;
-            if (!line_done(line, it.steps, s_fail, s_redo)) break;
+            if (!stretch_done()) break;
         }
     }
     }
