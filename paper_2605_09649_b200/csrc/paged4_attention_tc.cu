@@ -44,6 +44,14 @@ struct Feed {
     static constexpr int PARTS = D / 32, ROWS = 32 / PARTS, STEPS = PAGE / ROWS, RAW = PAGE * (D / 2 + D / 16);
     static_assert(T_FEED % STEPS == 0 && T_FEED <= 2 * STEPS, "a warp has one step of a page, or of one of a tile's two");
 };
+// Whether the phase is over, without waiting: asked well before the answer is used, it hides the way to shared memory and back, which
+// takes some 200 cycles beside the tensor cores' own reads.
+__device__ __forceinline__ uint32_t t_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
 __device__ __forceinline__ void t_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -443,12 +451,15 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             uint32_t word[4], scale;
             int real;
             auto take = [&](uint32_t (&wd)[4], uint32_t& sc, int& n) {
-                ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3]) : "r"(code0 + slot * F::RAW));
                 asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(sc) : "r"(scale0 + slot * F::RAW));
                 n = s_real[slot];
             };
-            if (npage > 0) take(word, scale, real);
+            if (npage > 0) {
+                ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
+                take(word, scale, real);
+            }
+            uint32_t raw_ready = 0u, stage_ready = 0u;                // of the page behind, of the part behind
             unsigned c = ct;
             int kv = 0, h = 0, left = npage;                          // page h of K or V of tile c; pages of the tile and those behind it
 #pragma unroll 1
@@ -458,10 +469,20 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                 if (++slot == T_RAW) { slot = 0; phase ^= 1; }
                 uint32_t next[4] = {0u, 0u, 0u, 0u}, next_scale = 0u;
                 int next_real = 0;
-                if (n + 1 < 2 * npage) take(next, next_scale, next_real);
+                if (n + 1 < 2 * npage) {
+                    if (!__all_sync(0xffffffffu, raw_ready != 0u)) ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
+                    take(next, next_scale, next_real);
+                }
+                raw_ready = t_test(raw_full + (slot + 1 == T_RAW ? 0u : 8 * (slot + 1)), slot + 1 == T_RAW ? phase ^ 1u : phase);
                 const unsigned s = c % T_STAGES;
-                if (h == 0 && c >= T_STAGES && ok) ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
+                if (h == 0 && c >= T_STAGES && ok && !__all_sync(0xffffffffu, stage_ready != 0u))
+                    ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
                 if (!ok) break;
+                const bool last_page = h == 1 || left == 1;           // of the tile
+                if (last_page) {
+                    const unsigned nc = c + kv;                       // the next part: V of this tile, or K of the next
+                    stage_ready = t_test((kv ? k_empty : v_empty) + 8 * (nc % T_STAGES), ((nc / T_STAGES) - 1) & 1);
+                }
                 if (F::STEPS == T_FEED || fw / F::STEPS == h) {
                     // K: a plane holds the rows of both pages; V: planes of a page, then of the next
                     const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
@@ -475,7 +496,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                                      "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
                     }
                 }
-                if (h == 1 || left == 1) {                            // the tile's last page
+                if (last_page) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
