@@ -29,13 +29,13 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
 constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
 
-template <int D, int NT>
+template <int D, int NT, bool F32>
 struct Warp4Shape {
-    static constexpr int WARPS = P4_WARPS;
+    static constexpr int WARPS = D <= 128 && NT == 1 && !F32 ? 16 : 8;         // as the registers allow: 128 or 255 a thread
     static constexpr int ROWS = NT * 8;                               // rows of a unit
     static constexpr int TILE = 32;                                   // entries per stage
     static constexpr int STAGE = TILE * (D / 2 + D / 16) * 2;         // K codes, K scales, V codes, V scales
-    static constexpr int STAGES = D == 256 ? 2 : D == 128 ? 5 : 8;
+    static constexpr int STAGES = (212 * 1024 / WARPS / STAGE) < 8 ? 212 * 1024 / WARPS / STAGE : 8;
     static constexpr int OFF_BAR = WARPS * STAGES * STAGE;
     static constexpr int OFF_META = OFF_BAR + WARPS * STAGES * 8;
     static constexpr int OFF_TAB = (OFF_META + WARPS * STAGES * 4 + 15) & ~15;
@@ -88,11 +88,11 @@ struct Warp4Cursor {
     bool on;
 };
 
-// Head size pv.d, a multiple of 32, at most D.  T: type of q and out.
-template <int D, int NT, typename T>
-__global__ void __launch_bounds__(Warp4Shape<D, NT>::WARPS * 32, 1)
+// EXACT: the head size is D; otherwise smaller, a multiple of 32.  T: type of q and out.
+template <int D, int NT, bool EXACT, typename T>
+__global__ void __launch_bounds__(Warp4Shape<D, NT, sizeof(T) == 4>::WARPS * 32, 1)
 paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, float scale_log2, PagedWork wk, int max_rows) {
-    using S = Warp4Shape<D, NT>;
+    using S = Warp4Shape<D, NT, sizeof(T) == 4>;
     constexpr bool F32 = sizeof(T) == 4;
     using Exact = std::integral_constant<bool, F32>;
     constexpr int KS = D / 16, MT = S::TILE / 16, PARTS = F32 ? 2 : 1;
@@ -100,7 +100,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     extern __shared__ unsigned char w4_smem_raw[];
     unsigned char* smem = w4_smem_raw + ((128u - (smem_u32(w4_smem_raw) & 127u)) & 127u);
     const PagedView& pv = cache.pv;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = pv.d, gq = lane >> 2, tq = lane & 3;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = EXACT ? D : pv.d, gq = lane >> 2, tq = lane & 3;
     unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + warp * S::STAGES;
     volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + warp * S::STAGES;      // first entry of the stage's tile; -1: skip
@@ -120,6 +120,11 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     if (w >= tab.workers) return;
     const long long end = tab.share(w + 1);
 
+    // this thread's places in a tile: codes and scales of K (entry of row gq, channels tq d / 4 ..), of V (entries of rows 2 tq and + 1, channels gq d / 8 ..)
+    const int k_codes = w4_entry(gq) * code_row + tq * (D / 8), k_scales = off_ks + w4_entry(gq) * scale_row + tq * (D / 64);
+    const int v_codes[2] = {off_vc + w4_entry(2 * tq) * code_row + gq * (D / 16), off_vc + w4_entry(2 * tq + 1) * code_row + gq * (D / 16)};
+    const int v_scales[2] = {off_vs + w4_entry(2 * tq) * scale_row + gq * D / 128, off_vs + w4_entry(2 * tq + 1) * scale_row + gq * D / 128};
+
     auto at = [&](long long x) {
         Warp4Cursor c;
         c.x = x;
@@ -136,7 +141,8 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     };
     Warp4Cursor cons = at(tab.share(w)), prod = cons;
     int prod_tile = 0, phys_page = 0;                                 // lane l: page l of the current run of 32
-    unsigned issued = 0, consumed = 0;
+    unsigned issued = 0, consumed = 0;                                // tiles; place in the ring of the next one
+    unsigned in = 0, at_stage = 0, parity = 0;
     bool failed = false;
 
     auto issue_one = [&]() {
@@ -147,7 +153,8 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
             phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, p) : -1;
         }
         const int pp = __shfl_sync(0xffffffffu, phys_page, (prod_tile / 2) & 31), half = prod_tile & 1;
-        const unsigned s = issued % S::STAGES;
+        const unsigned s = in;
+        if (++in == S::STAGES) in = 0;
         if (lane == 0) {
             meta[s] = pp < 0 ? -1 : (prod.it.p0 + prod_tile / 2) * PAGE + half * S::TILE;
             if (pp < 0) {
@@ -233,9 +240,10 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
 
         for (int tt = 0; tt < cons.ntile; ++tt) {
             issue_one();                                              // refill the stage freed by the previous tile
-            const unsigned s = consumed % S::STAGES;
-            if (!mbar_wait_bounded(bars + s, (consumed / S::STAGES) & 1u)) { failed = true; break; }
+            const unsigned s = at_stage;
+            if (!mbar_wait_bounded(bars + s, parity)) { failed = true; break; }
             ++consumed;
+            if (++at_stage == S::STAGES) { at_stage = 0; parity ^= 1u; }
             const int e0 = meta[s];
             if (e0 < 0) { __syncwarp(); continue; }                   // a page that does not exist
             unsigned char* tile = ring + s * S::STAGE;
@@ -254,19 +262,17 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 uint32_t kw[2][KW], ks[2][(KW + 3) / 4 * 2];           // rows gq and gq + 8: codes; scales, both halves of a register alike
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int e = mt * 16 + i * 8 + w4_entry(gq);
-                    const unsigned char* cp = tile + e * code_row + tq * (D / 8);
-                    const unsigned char* sp = tile + off_ks + e * scale_row + tq * (D / 64);
+                    const unsigned char* cp = tile + k_codes + (mt * 16 + i * 8) * code_row;
+                    const unsigned char* sp = tile + k_scales + (mt * 16 + i * 8) * scale_row;
 #pragma unroll
                     for (int c = 0; c < KW; c += 4) {                 // (KW = 2 for heads of 64)
-                        const bool on = tq * (D / 4) + c * 8 < d;     // the padded channels: codes 0
-#pragma unroll
-                        for (int x = 0; x < 4 && c + x < KW; ++x) kw[i][c + x] = 0u;
                         uint32_t two = 0u;
-                        if (on) {
+                        if (EXACT || tq * (D / 4) + c * 8 < d) {
                             w4_load<KW == 2 ? 8 : 16>(&kw[i][c], cp + c * 4);
                             two = KW == 2 ? (uint32_t)sp[0] : (uint32_t)*reinterpret_cast<const uint16_t*>(sp + c / 2);
-                        }
+                        } else                                        // missing channels: Q has zeros there
+#pragma unroll
+                            for (int x = 0; x < 4 && c + x < KW; ++x) kw[i][c + x] = 0u;
                         const uint32_t sc = p4_scales(two);
                         ks[i][c / 2] = p4_both_low(sc);
                         if (KW > 2) ks[i][c / 2 + 1] = p4_both_high(sc);
@@ -364,58 +370,56 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 }
             }
             // ---- O^T[channel][row] += V^T P^T: this thread's channels are gq d / 8 .., its entries 2 tq, 2 tq + 1 and 8 further
-            const bool v_on = gq * (D / 8) < d;
+            const bool v_on = EXACT || gq * (D / 8) < d;              // otherwise these channels are missing: nothing is written from them
+            float acc[F32 ? NT : 1][F32 ? KS : 1][4];
+            if constexpr (F32)
 #pragma unroll
-            for (int x = 0; x < VW; ++x) {
-                float acc[F32 ? NT : 1][4][4];
-                if constexpr (F32)
+                for (int i = 0; i < NT * KS * 4; ++i) (&acc[0][0][0])[i] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < NT * 16; ++i) (&acc[0][0][0])[i] = 0.f;
+            for (int mt = 0; mt < MT; ++mt) {
+                uint32_t a[2][VW], b[2][VW], sp[2][(VW + 1) / 2];     // rows 2 tq + 8 i, and 2 tq + 8 i + 1: codes; scales of both
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    uint32_t vw[4], sp[2];
+                for (int i = 0; i < 2; ++i) {
+                    if (v_on) {
+                        w4_load<VW * 4>(a[i], tile + v_codes[0] + (mt * 16 + i * 8) * code_row);
+                        w4_load<VW * 4>(b[i], tile + v_codes[1] + (mt * 16 + i * 8) * code_row);
+                    } else
+#pragma unroll
+                        for (int x = 0; x < VW; ++x) a[i][x] = b[i][x] = 0u;
+#pragma unroll
+                    for (int x = 0; x < (VW + 1) / 2; ++x) {
+                        const uint32_t s0 = v_on ? tile[v_scales[0] + (mt * 16 + i * 8) * scale_row + x] : 0, s1 = v_on ? tile[v_scales[1] + (mt * 16 + i * 8) * scale_row + x] : 0;
+                        sp[i][x] = p4_scales(__byte_perm(s0, s1, 0x0040));
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < VW; ++x) {
+                    uint32_t r[4][4];                                 // even channels of both entries, odd ones; the same 8 entries on
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int ea = mt * 16 + i * 8 + w4_entry(2 * tq), eb = mt * 16 + i * 8 + w4_entry(2 * tq + 1);
-                        const unsigned char* c0 = tile + off_vc + gq * (D / 16) + x * 4;
-                        const unsigned char* s0 = tile + off_vs + gq * D / 128 + x / 2;
-                        uint32_t a = 0u, b = 0u, two = 0u;
-                        if (v_on) {
-                            a = *reinterpret_cast<const uint32_t*>(c0 + ea * code_row);
-                            b = *reinterpret_cast<const uint32_t*>(c0 + eb * code_row);
-                            two = (uint32_t)s0[ea * scale_row] | (uint32_t)s0[eb * scale_row] << 8;
-                        }
-                        sp[i] = p4_scales(two);
-                        vw[2 * i] = (a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u);            // even channels of both entries
-                        vw[2 * i + 1] = ((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);        // odd ones
+                        p4_codes((a[i][x] & 0x0f0f0f0fu) | ((b[i][x] << 4) & 0xf0f0f0f0u), r[2 * i]);
+                        p4_codes(((a[i][x] >> 4) & 0x0f0f0f0fu) | (b[i][x] & 0xf0f0f0f0u), r[2 * i + 1]);
                     }
-                    uint32_t r[4][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p4_codes(vw[i], r[i]);
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        uint32_t a[4];
-                        a[0] = p4_mul(r[0][b], sp[0]);
-                        a[1] = p4_mul(r[1][b], sp[0]);
-                        a[2] = p4_mul(r[2][b], sp[1]);
-                        a[3] = p4_mul(r[3][b], sp[1]);
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t af[4] = {p4_mul(r[0][c], sp[0][x / 2]), p4_mul(r[1][c], sp[0][x / 2]), p4_mul(r[2][c], sp[1][x / 2]), p4_mul(r[3][c], sp[1][x / 2])};
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int part = 0; part < PARTS; ++part) {
-                                if constexpr (F32) w4_mma(acc[nt][b], a, pf[mt][nt][part][0], pf[mt][nt][part][1]);
-                                else w4_mma(o[nt][4 * x + b], a, pf[mt][nt][part][0], pf[mt][nt][part][1]);
+                                if constexpr (F32) w4_mma(acc[nt][4 * x + c], af, pf[mt][nt][part][0], pf[mt][nt][part][1]);
+                                else w4_mma(o[nt][4 * x + c], af, pf[mt][nt][part][0], pf[mt][nt][part][1]);
                             }
                     }
                 }
-                if constexpr (F32)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int b = 0; b < 4; ++b)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[nt][4 * x + b][i] += acc[nt][b][i];
             }
+            if constexpr (F32)                                        // a tile's sum apart: short chains
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int dt = 0; dt < KS; ++dt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[nt][dt][i] += acc[nt][dt][i];
             __syncwarp();                                             // all lanes are done with the stage before it is refilled
         }
         if (failed) break;
@@ -458,19 +462,19 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     if (failed) {
         if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
         while (consumed < issued) {                                   // wait (bounded) for the copies still in flight
-            mbar_wait_bounded(bars + consumed % S::STAGES, (consumed / S::STAGES) & 1u);
+            mbar_wait_bounded(bars + consumed % S::STAGES, (consumed / S::STAGES) & 1u);      // (once: the ring's place follows from the count)
             ++consumed;
         }
     }
 }
 
-template <int D, int NT, typename T>
+template <int D, int NT, bool EXACT, typename T>
 cudaError_t run_warp4(const Paged4View& c, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w, int max_rows, cudaStream_t st) {
-    using S = Warp4Shape<D, NT>;
+    using S = Warp4Shape<D, NT, sizeof(T) == 4>;
     static std::atomic<unsigned long long> done{0};
-    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, T>), S::SMEM, done);
+    cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, EXACT, T>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged4_attn_warp_kernel<D, NT, T>, dim3(PAGED_SMS), dim3(S::WARPS * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
+    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3(S::WARPS * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
                      max_rows);
     if (e != cudaSuccess || paged_always_whole(pb, c.pv.H, S::ROWS, PAGED_SMS * S::WARPS, W4_JOIN_STEPS)) return e;
     return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st);
@@ -482,7 +486,8 @@ cudaError_t launch_paged4_attention_warp(const Paged4View& c, const PagedBatch& 
                                          int tile_rows, int max_rows, cudaStream_t st) {
     auto go = [&](auto d, auto nt) {
         constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-        return is_bf16 ? run_warp4<D, NT, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, float>(c, pb, q, out, scale, w, max_rows, st);
+        if (c.pv.d == D) return is_bf16 ? run_warp4<D, NT, true, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, true, float>(c, pb, q, out, scale, w, max_rows, st);
+        return is_bf16 ? run_warp4<D, NT, false, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, false, float>(c, pb, q, out, scale, w, max_rows, st);
     };
     auto rows = [&](auto d) { return tile_rows <= 8 ? go(d, std::integral_constant<int, 1>{}) : go(d, std::integral_constant<int, 2>{}); };
     return c.pv.d <= 64    ? rows(std::integral_constant<int, 64>{})
