@@ -61,7 +61,7 @@ cudaError_t launch_paged4_read(const Paged4View& c, int is_bf16, int n, const in
 
 // Warp kernel: workers per SM and the most rows that they hold in all (workers x rows of a unit).
 constexpr int P4_WARPS = 16;
-constexpr int P4_WORKER_ROWS = PAGED_SMS * 8 * 16;
+constexpr int P4_WORKER_ROWS = PAGED_SMS * 11 * 16;
 constexpr size_t P4_SHARED_BYTES = (size_t)PAGED_SMS * P4_WARPS * 16;
 static_assert(P4_SHARED_BYTES % 256 == 0, "partial results are aligned");
 // Units of tile_rows = 8 or 16 rows of the requests of up to max_rows rows.

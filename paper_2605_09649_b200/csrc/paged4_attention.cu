@@ -26,19 +26,30 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr unsigned W4_IDLE_LIMIT = 1u << 22, W4_NAP = 64;             // rounds without progress, and ns between them
 constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
 constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
 
+// A tile as it lies in a stage of a ring, and the stretch of a unit that it belongs to.
+constexpr int TILE_FIRST = 1, TILE_LAST = 2, TILE_END = 4;            // of the stretch; nothing more to do
+struct __align__(16) Tile4 {
+    int e0, flags;                                                    // first entry; -1: nothing to read
+    int row0, n, len, row_first, rows, h, slot;                       // see PagedItem, paged_unit_first, paged_unit_rows
+    int pad[3];
+};
+
 template <int D, int NT, bool F32>
 struct Warp4Shape {
-    static constexpr int WARPS = D <= 128 && NT == 1 && !F32 ? 16 : 8;         // as the registers allow: 128 or 255 a thread
+    // Warps that compute; one more brings their tiles.  As the registers allow: 168 a thread with 12 in all, 255 with 8.
+    static constexpr int WARPS = (D <= 128 && !F32 ? 12 : 8) - 1;
     static constexpr int ROWS = NT * 8;                               // rows of a unit
-    static constexpr int TILE = 32;                                   // entries per stage
+    static constexpr int TILE = D == 256 ? 32 : 64, STEP = 32;        // entries per stage; entries that are worked on at a time
+    static constexpr int PER_PAGE = PAGE / TILE;
     static constexpr int STAGE = TILE * (D / 2 + D / 16) * 2;         // K codes, K scales, V codes, V scales
     static constexpr int STAGES = (212 * 1024 / WARPS / STAGE) < 8 ? 212 * 1024 / WARPS / STAGE : 8;
     static constexpr int OFF_BAR = WARPS * STAGES * STAGE;
-    static constexpr int OFF_META = OFF_BAR + WARPS * STAGES * 8;
-    static constexpr int OFF_TAB = (OFF_META + WARPS * STAGES * 4 + 15) & ~15;
+    static constexpr int OFF_DESC = (OFF_BAR + WARPS * STAGES * 16 + 15) & ~15;
+    static constexpr int OFF_TAB = OFF_DESC + WARPS * STAGES * (int)sizeof(Tile4);
     static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 128;       // 128: alignment slack
     static_assert(SMEM <= 227 * 1024, "shared memory of one SM");
     static_assert(WARPS * ROWS * PAGED_SMS <= P4_WORKER_ROWS, "the workspace holds the workers' partial results");
@@ -49,6 +60,11 @@ __device__ __forceinline__ void w4_mma(float (&c)[4], const uint32_t (&a)[4], ui
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ bool w4_test(uint64_t* bar, uint32_t parity) {      // whether the phase is over, without waiting
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
 }
 // Entry that row r (0 .. 15) of a product's 16 stands for: neighbours and every second row fall on both halves of the 32 banks.
 __device__ __forceinline__ int w4_entry(int r) { return r ^ ((r >> 1) & 1); }
@@ -80,114 +96,148 @@ __device__ __forceinline__ void w4_store8(float* p, const float (&v)[8]) {
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// A place on the line and the stretch of a unit that begins there.
-struct Warp4Cursor {
-    long long x;
-    PagedItem it;
-    int ntile;          // tiles to read
-    bool on;
-};
-
 // EXACT: the head size is D; otherwise smaller, a multiple of 32.  T: type of q and out.
 template <int D, int NT, bool EXACT, typename T>
-__global__ void __launch_bounds__(Warp4Shape<D, NT, sizeof(T) == 4>::WARPS * 32, 1)
+__global__ void __launch_bounds__((Warp4Shape<D, NT, sizeof(T) == 4>::WARPS + 1) * 32, 1)
 paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, float scale_log2, PagedWork wk, int max_rows) {
     using S = Warp4Shape<D, NT, sizeof(T) == 4>;
     constexpr bool F32 = sizeof(T) == 4;
     using Exact = std::integral_constant<bool, F32>;
-    constexpr int KS = D / 16, MT = S::TILE / 16, PARTS = F32 ? 2 : 1;
+    constexpr int KS = D / 16, MT = S::STEP / 16, PARTS = F32 ? 2 : 1;
     constexpr int KW = D / 32, VW = D / 64;                           // words of codes that a thread takes of an entry's K, and of its V
     extern __shared__ unsigned char w4_smem_raw[];
     unsigned char* smem = w4_smem_raw + ((128u - (smem_u32(w4_smem_raw) & 127u)) & 127u);
     const PagedView& pv = cache.pv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = EXACT ? D : pv.d, gq = lane >> 2, tq = lane & 3;
-    unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR) + warp * S::STAGES;
-    volatile int* meta = reinterpret_cast<volatile int*>(smem + S::OFF_META) + warp * S::STAGES;      // first entry of the stage's tile; -1: skip
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);      // [warp][stage]
+    uint64_t* empty = full + S::WARPS * S::STAGES;
+    Tile4* desc = reinterpret_cast<Tile4*>(smem + S::OFF_DESC);
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
     const int code_row = d / 2, scale_row = d / 16;
     const int off_ks = S::TILE * code_row, off_vc = off_ks + S::TILE * scale_row, off_vs = off_vc + off_ks;       // within a stage
 
-    if (lane == 0)
-        for (int s = 0; s < S::STAGES; ++s) mbar_init(bars + s, 1);
+    if (threadIdx.x < S::WARPS * S::STAGES) { mbar_init(full + threadIdx.x, 1); mbar_init(empty + threadIdx.x, 1); }
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
     paged_build_table<0>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::WARPS, 4, W4_JOIN_STEPS, table_mem);      // (synchronises the block)
     grid_dependents_may_launch();
-    const int w = warp * (int)gridDim.x + (int)blockIdx.x;            // workers are spread over the SMs first
-    if (lane == 0) paged_note_none(wk, w);
-    if (w >= tab.workers) return;
-    const long long end = tab.share(w + 1);
+    if (warp == S::WARPS) {
+        // ---- the warp that brings tiles: lane l those of warp l, each at its own place on the line
+        const int w = lane * (int)gridDim.x + (int)blockIdx.x;        // workers are spread over the SMs first
+        bool done = lane >= S::WARPS;
+        if (!done) paged_note_none(wk, w);
+        unsigned char* ring = smem + (size_t)(done ? 0 : lane) * S::STAGES * S::STAGE;
+        uint64_t* my_full = full + (done ? 0 : lane) * S::STAGES;
+        uint64_t* my_empty = empty + (done ? 0 : lane) * S::STAGES;
+        Tile4* my_desc = desc + (done ? 0 : lane) * S::STAGES;
+        const long long end = !done && w < tab.workers ? tab.share(w + 1) : 0;
+        long long x = !done && w < tab.workers ? tab.share(w) : 0;
+        PagedItem it;
+        int ntile = 0, tile = 0, phys = -1;
+        auto begin = [&]() {                                          // the stretch at x
+            it = paged_item<0>(tab, pb, x, end, w);
+            tile = 0;
+            ntile = S::PER_PAGE * (it.p1 - it.p0);
+            if (ntile) {
+                // the second half of the last token's page may lie behind what is seen
+                const int phi = it.q.len - it.q.n + it.tok1;
+                if (S::PER_PAGE == 2 && it.p1 == phi / PAGE + 1 && phi % PAGE < S::TILE) --ntile;
+                phys = paged_physical(pb, pv, it.r, it.p0);
+            }
+            if (it.slot >= 0 && (it.slot & 1)) paged_note_shared(wk, tab, it, x, w, paged_unit_first<0>(pb, it.u, S::ROWS), paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS));
+        };
+        if (x < end) begin();
+        unsigned issued = 0, s = 0, parity = 1;                       // (the first round of a ring finds it empty)
+        unsigned idle = 0;
+        while (__any_sync(0xffffffffu, !done)) {
+            const bool go = !done && (issued < S::STAGES || w4_test(my_empty + s, parity));
+            if (go) {
+                Tile4* t = my_desc + s;
+                uint64_t* bar = my_full + s;
+                if (x >= end) {
+                    t->flags = TILE_END;
+                    mbar_arrive(bar);
+                    done = true;
+                } else {
+                    const int sub = tile % S::PER_PAGE, page = it.p0 + tile / S::PER_PAGE;
+                    const bool last = tile + 1 >= ntile, real = ntile > 0 && phys >= 0;
+                    t->e0 = real ? page * PAGE + sub * S::TILE : -1;
+                    t->flags = (tile == 0 ? TILE_FIRST : 0) | (last ? TILE_LAST : 0);
+                    if (tile == 0 || last) {                          // (at the first tile all of it is read, at the last where the result goes)
+                        t->row0 = it.q.row0; t->n = it.q.n; t->len = it.q.len;
+                        t->row_first = paged_unit_first<0>(pb, it.u, S::ROWS);
+                        t->rows = paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS);
+                        t->h = it.h; t->slot = it.slot;
+                    }
+                    if (real) {
+                        unsigned char* dst = ring + s * S::STAGE;
+                        const size_t row = ((size_t)phys * pv.H + it.h) * PAGE + sub * S::TILE;
+                        mbar_expect_tx(bar, 2 * off_vc);              // (the zeroing of scales below carries its own proxy fence)
+                        bulk_g2s(dst, cache.codes[0] + row * code_row, off_ks, bar);
+                        bulk_g2s(dst + off_ks, cache.scales[0] + row * scale_row, S::TILE * scale_row, bar);
+                        bulk_g2s(dst + off_vc, cache.codes[1] + row * code_row, off_ks, bar);
+                        bulk_g2s(dst + off_vs, cache.scales[1] + row * scale_row, S::TILE * scale_row, bar);
+                    } else {
+                        mbar_arrive(bar);
+                    }
+                    ++tile;
+                    if (last) {
+                        x += it.steps;
+                        if (x < end) begin();
+                    } else if (sub == S::PER_PAGE - 1) {
+                        phys = paged_physical(pb, pv, it.r, page + 1);
+                    }
+                }
+                ++issued;
+                if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+            }
+            if (__any_sync(0xffffffffu, go)) idle = 0;
+            else if (++idle > W4_IDLE_LIMIT) break;
+            else __nanosleep(W4_NAP);
+        }
+        if (!done) {                                                  // a warp gave up: the copies in flight land before this one leaves (bounded)
+            latch_error(pb.status, TRIMKV_E_TIMEOUT);
+            for (unsigned k = issued > S::STAGES ? issued - S::STAGES : 0; k < issued; ++k) mbar_wait_bounded(my_full + k % S::STAGES, (k / S::STAGES) & 1u);
+        }
+        return;
+    }
 
+    // ---- the warps that compute
+    const unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
+    full += warp * S::STAGES;
+    empty += warp * S::STAGES;
+    desc += warp * S::STAGES;
     // this thread's places in a tile: codes and scales of K (entry of row gq, channels tq d / 4 ..), of V (entries of rows 2 tq and + 1, channels gq d / 8 ..)
     const int k_codes = w4_entry(gq) * code_row + tq * (D / 8), k_scales = off_ks + w4_entry(gq) * scale_row + tq * (D / 64);
     const int v_codes[2] = {off_vc + w4_entry(2 * tq) * code_row + gq * (D / 16), off_vc + w4_entry(2 * tq + 1) * code_row + gq * (D / 16)};
     const int v_scales[2] = {off_vs + w4_entry(2 * tq) * scale_row + gq * D / 128, off_vs + w4_entry(2 * tq + 1) * scale_row + gq * D / 128};
-
-    auto at = [&](long long x) {
-        Warp4Cursor c;
-        c.x = x;
-        c.ntile = 0;
-        c.on = x < end;
-        if (!c.on) return c;
-        c.it = paged_item<0>(tab, pb, x, end, w);
-        c.ntile = 2 * (c.it.p1 - c.it.p0);
-        if (c.ntile) {                                                // the second half of the last token's page may lie behind what is seen
-            const int phi = c.it.q.len - c.it.q.n + c.it.tok1;
-            if (c.it.p1 == phi / PAGE + 1 && phi % PAGE < S::TILE) --c.ntile;
-        }
-        return c;
-    };
-    Warp4Cursor cons = at(tab.share(w)), prod = cons;
-    int prod_tile = 0, phys_page = 0;                                 // lane l: page l of the current run of 32
-    unsigned issued = 0, consumed = 0;                                // tiles; place in the ring of the next one
-    unsigned in = 0, at_stage = 0, parity = 0;
-    bool failed = false;
-
-    auto issue_one = [&]() {
-        while (prod.on && prod_tile == prod.ntile) { prod = at(prod.x + prod.it.steps); prod_tile = 0; }
-        if (!prod.on) return;
-        if (prod_tile % 64 == 0) {                                    // the next 32 pages
-            const int p = prod.it.p0 + prod_tile / 2 + lane;
-            phys_page = p < prod.it.p1 ? paged_physical(pb, pv, prod.it.r, p) : -1;
-        }
-        const int pp = __shfl_sync(0xffffffffu, phys_page, (prod_tile / 2) & 31), half = prod_tile & 1;
-        const unsigned s = in;
-        if (++in == S::STAGES) in = 0;
-        if (lane == 0) {
-            meta[s] = pp < 0 ? -1 : (prod.it.p0 + prod_tile / 2) * PAGE + half * S::TILE;
-            if (pp < 0) {
-                mbar_arrive(bars + s);
-            } else {
-                unsigned char* dst = ring + s * S::STAGE;
-                const size_t row = ((size_t)pp * pv.H + prod.it.h) * PAGE + half * S::TILE;
-                mbar_expect_tx(bars + s, 2 * off_vc);                 // (the zeroing of scales below carries its own proxy fence)
-                bulk_g2s(dst, cache.codes[0] + row * code_row, off_ks, bars + s);
-                bulk_g2s(dst + off_ks, cache.scales[0] + row * scale_row, S::TILE * scale_row, bars + s);
-                bulk_g2s(dst + off_vc, cache.codes[1] + row * code_row, off_ks, bars + s);
-                bulk_g2s(dst + off_vs, cache.scales[1] + row * scale_row, S::TILE * scale_row, bars + s);
-            }
-        }
-        ++issued;
-        ++prod_tile;
-    };
-    for (int s = 0; s < S::STAGES - 1; ++s) issue_one();
+    int row_first = 0, rows = 0, pos0 = 0, len = 0, all_lo = 0, all_hi = 0, all_end = 0;       // of the stretch; pos0: position of its request's first token
 
     uint32_t bq[NT][PARTS][KS][2];
     float o[NT][KS][4];
     float m_run[NT][2], l_run[NT][2], to_log2[NT][2];
 
-    while (cons.on && !failed) {
-        const PagedItem& it = cons.it;
-        const int row_first = paged_unit_first<0>(pb, it.u, S::ROWS), rows = paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS);
+    for (unsigned stage = 0, parity = 0;;) {
+        if (!mbar_wait_bounded(full + stage, parity)) {
+            if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
+            return;
+        }
+        const Tile4& it = desc[stage];
+        const int flags = it.flags, e0 = it.e0;
+        if (flags & TILE_END) return;
+        if (flags & TILE_FIRST) {
+        row_first = it.row_first;
+        rows = it.rows;
+        len = it.len;
+        pos0 = it.len - it.n;
         const int ksh = p4_shift(cache, 0, it.h);
         // ---- Q fragments (B operand: k = channel, n = row): row gq of a column tile, channels tq d / 4 ..
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = nt * 8 + gq, qr = row_first + row;
             const int qt = row < rows ? pb.by_g.div(qr) : 0, qj = row < rows ? qr - qt * g : 0;
-            const T* p = q + (size_t)(it.q.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + tq * (D / 4);
+            const T* p = q + (size_t)(it.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + tq * (D / 4);
             float top = 0.f;
             auto load = [&](float (&v)[8], int c) {
                 if (row < rows && tq * (D / 4) + c < d) w4_load8(v, p + c);
@@ -231,28 +281,25 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
 #pragma unroll
             for (int dt = 0; dt < KS; ++dt) o[nt][dt][0] = o[nt][dt][1] = o[nt][dt][2] = o[nt][dt][3] = 0.f;
         }
-        int all_lo, all_hi;                                           // entries that every row of the unit sees, from its first and last row
-        {
-            const int p0 = it.q.len - it.q.n + pb.by_g.div(row_first), p1 = it.q.len - it.q.n + pb.by_g.div(max(row_first + rows - 1, 0));
-            all_hi = max(p0 + 1, 0);
-            all_lo = pb.window > 0 ? max(p1 + 1 - pb.window, 0) : 0;
+        // entries that every row of the unit sees, from its first and last row
+        all_hi = max(pos0 + pb.by_g.div(row_first) + 1, 0);
+        all_end = pos0 + pb.by_g.div(row_first + rows - 1) + 1;        // none sees an entry from here on
+        all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
         }
 
-        for (int tt = 0; tt < cons.ntile; ++tt) {
-            issue_one();                                              // refill the stage freed by the previous tile
-            const unsigned s = at_stage;
-            if (!mbar_wait_bounded(bars + s, parity)) { failed = true; break; }
-            ++consumed;
-            if (++at_stage == S::STAGES) { at_stage = 0; parity ^= 1u; }
-            const int e0 = meta[s];
-            if (e0 < 0) { __syncwarp(); continue; }                   // a page that does not exist
-            unsigned char* tile = ring + s * S::STAGE;
-            const int held = it.q.len - e0;                           // entries of the tile, if it is not full
+        if (e0 >= 0) {
+            unsigned char* whole = const_cast<unsigned char*>(ring) + stage * S::STAGE;
+            const int held = len - e0;                                // entries of the tile, if it is not full
             if (held < S::TILE) {
-                for (int i = max(held, 0) * scale_row + lane; i < S::TILE * scale_row; i += 32) tile[off_vs + i] = 0;
+                for (int i = max(held, 0) * scale_row + lane; i < S::TILE * scale_row; i += 32) whole[off_vs + i] = 0;
                 fence_proxy_async_smem();                             // before a later copy into this stage
                 __syncwarp();
             }
+#pragma unroll 1
+            for (int at = 0; at < S::TILE && e0 + at < all_end; at += S::STEP) {
+            const int es = e0 + at;                                   // entries es .. es + 31
+            const unsigned char *kc = whole + k_codes + at * code_row, *ks_at = whole + k_scales + at * scale_row, *vc0 = whole + v_codes[0] + at * code_row,
+                                *vc1 = whole + v_codes[1] + at * code_row, *vs0 = whole + v_scales[0] + at * scale_row, *vs1 = whole + v_scales[1] + at * scale_row;
             // ---- S^T[entry][row] = K Q^T
             float sacc[MT][NT][4];
 #pragma unroll
@@ -262,8 +309,8 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 uint32_t kw[2][KW], ks[2][(KW + 3) / 4 * 2];           // rows gq and gq + 8: codes; scales, both halves of a register alike
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const unsigned char* cp = tile + k_codes + (mt * 16 + i * 8) * code_row;
-                    const unsigned char* sp = tile + k_scales + (mt * 16 + i * 8) * scale_row;
+                    const unsigned char* cp = kc + (mt * 16 + i * 8) * code_row;
+                    const unsigned char* sp = ks_at + (mt * 16 + i * 8) * scale_row;
 #pragma unroll
                     for (int c = 0; c < KW; c += 4) {                 // (KW = 2 for heads of 64)
                         uint32_t two = 0u;
@@ -299,7 +346,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
             }
             // ---- softmax over the entries; this thread owns rows 2 tq, + 1 of each column tile.  The reference of a row's
             // weights is raised only when some logit exceeds it by 2^8: until then a tile needs one vote and no exchange.
-            const bool edge = e0 + S::TILE > all_hi || e0 < all_lo;
+            const bool edge = es + S::STEP > all_hi || es < all_lo;
             float mx[NT][2];
             bool raise = false;
 #pragma unroll
@@ -308,13 +355,13 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int col = nt * 8 + 2 * tq + c;
-                        const int pos = col < rows ? it.q.len - it.q.n + pb.by_g.div(row_first + col) : -1;
+                        const int pos = col < rows ? pos0 + pb.by_g.div(row_first + col) : -1;
                         const int lo = pb.window > 0 ? pos + 1 - pb.window : 0;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                             for (int i = c; i < 4; i += 2) {
-                                const int e = e0 + mt * 16 + w4_entry(gq) + (i >> 1) * 8;
+                                const int e = es + mt * 16 + w4_entry(gq) + (i >> 1) * 8;
                                 if (e > pos || e < lo) sacc[mt][nt][i] = -INFINITY;
                             }
                     }
@@ -381,14 +428,14 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (v_on) {
-                        w4_load<VW * 4>(a[i], tile + v_codes[0] + (mt * 16 + i * 8) * code_row);
-                        w4_load<VW * 4>(b[i], tile + v_codes[1] + (mt * 16 + i * 8) * code_row);
+                        w4_load<VW * 4>(a[i], vc0 + (mt * 16 + i * 8) * code_row);
+                        w4_load<VW * 4>(b[i], vc1 + (mt * 16 + i * 8) * code_row);
                     } else
 #pragma unroll
                         for (int x = 0; x < VW; ++x) a[i][x] = b[i][x] = 0u;
 #pragma unroll
                     for (int x = 0; x < (VW + 1) / 2; ++x) {
-                        const uint32_t s0 = v_on ? tile[v_scales[0] + (mt * 16 + i * 8) * scale_row + x] : 0, s1 = v_on ? tile[v_scales[1] + (mt * 16 + i * 8) * scale_row + x] : 0;
+                        const uint32_t s0 = v_on ? vs0[(mt * 16 + i * 8) * scale_row + x] : 0, s1 = v_on ? vs1[(mt * 16 + i * 8) * scale_row + x] : 0;
                         sp[i][x] = p4_scales(__byte_perm(s0, s1, 0x0040));
                     }
                 }
@@ -420,12 +467,16 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                     for (int dt = 0; dt < KS; ++dt)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[nt][dt][i] += acc[nt][dt][i];
-            __syncwarp();                                             // all lanes are done with the stage before it is refilled
+            }
         }
-        if (failed) break;
+        const int row0 = it.row0, h = it.h, slot = it.slot;
+        __syncwarp();                                                 // all lanes are done with the stage before it is refilled
+        if (lane == 0) mbar_arrive(empty + stage);
+        if (++stage == S::STAGES) { stage = 0; parity ^= 1u; }
+        if (!(flags & TILE_LAST)) continue;
 
         // ---- the unit's result, or this worker's part of it.  o[nt][4 x + b]: channels 8 x + 2 b (c) and + 1 (c + 2) of the thread's
-        const float v_up = p4_pow2(p4_shift(cache, 1, it.h));
+        const float v_up = p4_pow2(p4_shift(cache, 1, h));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -435,10 +486,10 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
                 const int col = nt * 8 + 2 * tq + c;
                 if (col >= rows) continue;
-                const float f = it.slot < 0 ? (l > 0.f ? v_up / l : (l == 0.f ? 0.f : l)) : v_up;
+                const float f = slot < 0 ? (l > 0.f ? v_up / l : (l == 0.f ? 0.f : l)) : v_up;
                 const int qt = pb.by_g.div(row_first + col), qj = row_first + col - qt * g;
-                T* op = out + ((size_t)(it.q.row0 + qt) * pb.Hq + (size_t)(it.h * g + qj)) * d + gq * (D / 8);
-                const size_t pr = (size_t)(it.slot < 0 ? 0 : it.slot) * S::ROWS + col;
+                T* op = out + ((size_t)(row0 + qt) * pb.Hq + (size_t)(h * g + qj)) * d + gq * (D / 8);
+                const size_t pr = (size_t)(slot < 0 ? 0 : slot) * S::ROWS + col;
                 float* po = wk.part_o + pr * d + gq * (D / 8);
                 if (gq * (D / 8) < d) {
 #pragma unroll
@@ -449,22 +500,12 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                             v[2 * b] = o[nt][4 * x + b][c] * f;
                             v[2 * b + 1] = o[nt][4 * x + b][c + 2] * f;
                         }
-                        if (it.slot < 0) w4_store8(op + 8 * x, v);
+                        if (slot < 0) w4_store8(op + 8 * x, v);
                         else w4_store8(po + 8 * x, v);
                     }
                 }
-                if (it.slot >= 0 && gq == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
+                if (slot >= 0 && gq == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
             }
-        if (it.slot >= 0 && (it.slot & 1) && lane == 0) paged_note_shared(wk, tab, it, cons.x, w, row_first, rows);
-        const long long next = cons.x + it.steps;
-        if (prod.on && prod.x == next) cons = prod; else cons = at(next);
-    }
-    if (failed) {
-        if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
-        while (consumed < issued) {                                   // wait (bounded) for the copies still in flight
-            mbar_wait_bounded(bars + consumed % S::STAGES, (consumed / S::STAGES) & 1u);      // (once: the ring's place follows from the count)
-            ++consumed;
-        }
     }
 }
 
@@ -474,7 +515,7 @@ cudaError_t run_warp4(const Paged4View& c, const PagedBatch& pb, const void* q, 
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, EXACT, T>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3(S::WARPS * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
+    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3((S::WARPS + 1) * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
                      max_rows);
     if (e != cudaSuccess || paged_always_whole(pb, c.pv.H, S::ROWS, PAGED_SMS * S::WARPS, W4_JOIN_STEPS)) return e;
     return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st);
