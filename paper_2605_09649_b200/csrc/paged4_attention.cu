@@ -30,7 +30,9 @@ constexpr unsigned W4_IDLE_LIMIT = 1u << 22, W4_NAP = 64;             // rounds 
 constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
 constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
 
-// A tile as it lies in a stage of a ring, and the stretch of a unit that it belongs to.
+// A tile that a warp is to read, and the stretch of a unit that it belongs to.
+constexpr int W4_FEED = 2;                                            // warps that bring tiles to the others
+constexpr int W4_AHEAD = 4, W4_MOST_STAGES = 4;                       // pages that are described to a warp at most; places of its ring
 constexpr int TILE_FIRST = 1, TILE_LAST = 2, TILE_END = 4;            // of the stretch; nothing more to do
 struct __align__(16) Tile4 {
     int e0, flags;                                                    // first entry; -1: nothing to read
@@ -40,16 +42,17 @@ struct __align__(16) Tile4 {
 
 template <int D, int NT, bool F32>
 struct Warp4Shape {
-    // Warps that compute; one more brings their tiles.  As the registers allow: 168 a thread with 12 in all, 255 with 8.
-    static constexpr int WARPS = (D <= 128 && !F32 ? 12 : 8) - 1;
+    // Warps that compute, beside those that feed them.  As the registers allow: 128 a thread with 16 in all, 168 with 12, 255 with 8.
+    static constexpr int WARPS = (D <= 128 && NT == 1 && !F32 ? 16 : D <= 128 && !F32 ? 12 : 8) - W4_FEED;
+    static constexpr int EACH = (WARPS + W4_FEED - 1) / W4_FEED;      // warps that one feeds
     static constexpr int ROWS = NT * 8;                               // rows of a unit
-    static constexpr int TILE = D == 256 ? 32 : 64, STEP = 32;        // entries per stage; entries that are worked on at a time
-    static constexpr int PER_PAGE = PAGE / TILE;
-    static constexpr int STAGE = TILE * (D / 2 + D / 16) * 2;         // K codes, K scales, V codes, V scales
-    static constexpr int STAGES = (212 * 1024 / WARPS / STAGE) < 8 ? 212 * 1024 / WARPS / STAGE : 8;
+    static constexpr int STEP = 32;                                   // entries that are worked on at a time
+    static constexpr int STAGE = PAGE * (D / 2 + D / 16);             // codes and scales of a page's K, or of its V
+    static constexpr int STAGES = 208 * 1024 / WARPS / STAGE < W4_MOST_STAGES ? 208 * 1024 / WARPS / STAGE : W4_MOST_STAGES;
+    static_assert(STAGES >= 3 && (STAGES + 1) / 2 + 1 <= W4_AHEAD, "a description stays while its page is in the ring");
     static constexpr int OFF_BAR = WARPS * STAGES * STAGE;
     static constexpr int OFF_DESC = (OFF_BAR + WARPS * STAGES * 16 + 15) & ~15;
-    static constexpr int OFF_TAB = OFF_DESC + WARPS * STAGES * (int)sizeof(Tile4);
+    static constexpr int OFF_TAB = OFF_DESC + WARPS * W4_AHEAD * (int)sizeof(Tile4);
     static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 128;       // 128: alignment slack
     static_assert(SMEM <= 227 * 1024, "shared memory of one SM");
     static_assert(WARPS * ROWS * PAGED_SMS <= P4_WORKER_ROWS, "the workspace holds the workers' partial results");
@@ -98,7 +101,7 @@ __device__ __forceinline__ void w4_store8(float* p, const float (&v)[8]) {
 
 // EXACT: the head size is D; otherwise smaller, a multiple of 32.  T: type of q and out.
 template <int D, int NT, bool EXACT, typename T>
-__global__ void __launch_bounds__((Warp4Shape<D, NT, sizeof(T) == 4>::WARPS + 1) * 32, 1)
+__global__ void __launch_bounds__((Warp4Shape<D, NT, sizeof(T) == 4>::WARPS + W4_FEED) * 32, 1)
 paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, float scale_log2, PagedWork wk, int max_rows) {
     using S = Warp4Shape<D, NT, sizeof(T) == 4>;
     constexpr bool F32 = sizeof(T) == 4;
@@ -114,7 +117,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     Tile4* desc = reinterpret_cast<Tile4*>(smem + S::OFF_DESC);
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
     const int code_row = d / 2, scale_row = d / 16;
-    const int off_ks = S::TILE * code_row, off_vc = off_ks + S::TILE * scale_row, off_vs = off_vc + off_ks;       // within a stage
+    const int off_scale = PAGE * code_row;                            // within a stage
 
     if (threadIdx.x < S::WARPS * S::STAGES) { mbar_init(full + threadIdx.x, 1); mbar_init(empty + threadIdx.x, 1); }
     fence_proxy_async_smem();
@@ -122,15 +125,12 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     PagedTable tab;
     paged_build_table<0>(tab, pb, pv.H, S::ROWS, 1, max_rows, (int)gridDim.x * S::WARPS, 4, W4_JOIN_STEPS, table_mem);      // (synchronises the block)
     grid_dependents_may_launch();
-    if (warp == S::WARPS) {
-        // ---- the warp that brings tiles: lane l those of warp l, each at its own place on the line
-        const int w = lane * (int)gridDim.x + (int)blockIdx.x;        // workers are spread over the SMs first
-        bool done = lane >= S::WARPS;
+    if (warp >= S::WARPS) {
+        // ---- the warps that bring tiles: each lane those of one warp, at a place of its own on the line
+        const int c = (warp - S::WARPS) * S::EACH + lane;
+        bool done = lane >= S::EACH || c >= S::WARPS;
+        const int w = c * (int)gridDim.x + (int)blockIdx.x;           // workers are spread over the SMs first
         if (!done) paged_note_none(wk, w);
-        unsigned char* ring = smem + (size_t)(done ? 0 : lane) * S::STAGES * S::STAGE;
-        uint64_t* my_full = full + (done ? 0 : lane) * S::STAGES;
-        uint64_t* my_empty = empty + (done ? 0 : lane) * S::STAGES;
-        Tile4* my_desc = desc + (done ? 0 : lane) * S::STAGES;
         const long long end = !done && w < tab.workers ? tab.share(w + 1) : 0;
         long long x = !done && w < tab.workers ? tab.share(w) : 0;
         PagedItem it;
@@ -138,59 +138,59 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
         auto begin = [&]() {                                          // the stretch at x
             it = paged_item<0>(tab, pb, x, end, w);
             tile = 0;
-            ntile = S::PER_PAGE * (it.p1 - it.p0);
-            if (ntile) {
-                // the second half of the last token's page may lie behind what is seen
-                const int phi = it.q.len - it.q.n + it.tok1;
-                if (S::PER_PAGE == 2 && it.p1 == phi / PAGE + 1 && phi % PAGE < S::TILE) --ntile;
-                phys = paged_physical(pb, pv, it.r, it.p0);
-            }
-            if (it.slot >= 0 && (it.slot & 1)) paged_note_shared(wk, tab, it, x, w, paged_unit_first<0>(pb, it.u, S::ROWS), paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS));
+            ntile = it.p1 - it.p0;
+            phys = ntile ? paged_physical(pb, pv, it.r, it.p0) : -1;
         };
         if (x < end) begin();
-        unsigned issued = 0, s = 0, parity = 1;                       // (the first round of a ring finds it empty)
-        unsigned idle = 0;
+        // Part p is K (p even) or V of page p / 2, and lies in place p mod STAGES of the ring.
+        unsigned n = 0, part = 0, place = 0, parity = 1, idle = 0;    // page; (the first round of a ring finds it empty)
         while (__any_sync(0xffffffffu, !done)) {
-            const bool go = !done && (issued < S::STAGES || w4_test(my_empty + s, parity));
+            const unsigned at = (done ? 0 : c) * S::STAGES + place;
+            const bool go = !done && (part < (unsigned)S::STAGES || w4_test(empty + at, parity));
             if (go) {
-                Tile4* t = my_desc + s;
-                uint64_t* bar = my_full + s;
-                if (x >= end) {
-                    t->flags = TILE_END;
-                    mbar_arrive(bar);
-                    done = true;
-                } else {
-                    const int sub = tile % S::PER_PAGE, page = it.p0 + tile / S::PER_PAGE;
-                    const bool last = tile + 1 >= ntile, real = ntile > 0 && phys >= 0;
-                    t->e0 = real ? page * PAGE + sub * S::TILE : -1;
-                    t->flags = (tile == 0 ? TILE_FIRST : 0) | (last ? TILE_LAST : 0);
-                    if (tile == 0 || last) {                          // (at the first tile all of it is read, at the last where the result goes)
-                        t->row0 = it.q.row0; t->n = it.q.n; t->len = it.q.len;
-                        t->row_first = paged_unit_first<0>(pb, it.u, S::ROWS);
-                        t->rows = paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS);
-                        t->h = it.h; t->slot = it.slot;
-                    }
-                    if (real) {
-                        unsigned char* dst = ring + s * S::STAGE;
-                        const size_t row = ((size_t)phys * pv.H + it.h) * PAGE + sub * S::TILE;
-                        mbar_expect_tx(bar, 2 * off_vc);              // (the zeroing of scales below carries its own proxy fence)
-                        bulk_g2s(dst, cache.codes[0] + row * code_row, off_ks, bar);
-                        bulk_g2s(dst + off_ks, cache.scales[0] + row * scale_row, S::TILE * scale_row, bar);
-                        bulk_g2s(dst + off_vc, cache.codes[1] + row * code_row, off_ks, bar);
-                        bulk_g2s(dst + off_vs, cache.scales[1] + row * scale_row, S::TILE * scale_row, bar);
+                Tile4* t = desc + c * W4_AHEAD + n % W4_AHEAD;
+                const int kv = part & 1;
+                const bool last = tile + 1 >= ntile;
+                if (!kv) {
+                    if (x >= end) {
+                        t->flags = TILE_END;
+                        mbar_arrive(full + at);
+                        done = true;
                     } else {
-                        mbar_arrive(bar);
-                    }
-                    ++tile;
-                    if (last) {
-                        x += it.steps;
-                        if (x < end) begin();
-                    } else if (sub == S::PER_PAGE - 1) {
-                        phys = paged_physical(pb, pv, it.r, page + 1);
+                        t->e0 = phys >= 0 ? (it.p0 + tile) * PAGE : -1;
+                        t->flags = (tile == 0 ? TILE_FIRST : 0) | (last ? TILE_LAST : 0);
+                        if (tile == 0 || last) {                      // (at the first page all of it is read, at the last where the result goes)
+                            t->row0 = it.q.row0; t->n = it.q.n; t->len = it.q.len;
+                            t->row_first = paged_unit_first<0>(pb, it.u, S::ROWS);
+                            t->rows = paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS);
+                            t->h = it.h; t->slot = it.slot;
+                        }
                     }
                 }
-                ++issued;
-                if (++s == S::STAGES) { s = 0; parity ^= 1u; }
+                if (!done) {
+                    if (phys < 0) {
+                        mbar_arrive(full + at);
+                    } else {
+                        unsigned char* dst = smem + (size_t)at * S::STAGE;
+                        const size_t row = ((size_t)phys * pv.H + it.h) * PAGE;
+                        mbar_expect_tx(full + at, PAGE * (code_row + scale_row));      // (the zeroing of scales below carries its own proxy fence)
+                        bulk_g2s(dst, (kv ? cache.codes[1] : cache.codes[0]) + row * code_row, off_scale, full + at);
+                        bulk_g2s(dst + off_scale, (kv ? cache.scales[1] : cache.scales[0]) + row * scale_row, PAGE * scale_row, full + at);
+                    }
+                    if (kv) {                                         // what comes next
+                        ++n;
+                        if (tile == 0 && it.slot >= 0 && (it.slot & 1))
+                            paged_note_shared(wk, tab, it, x, w, paged_unit_first<0>(pb, it.u, S::ROWS), paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS));
+                        if (++tile >= ntile) {
+                            x += it.steps;
+                            if (x < end) begin();
+                        } else {
+                            phys = paged_physical(pb, pv, it.r, it.p0 + tile);
+                        }
+                    }
+                    ++part;
+                    if (++place == S::STAGES) { place = 0; parity ^= 1u; }
+                }
             }
             if (__any_sync(0xffffffffu, go)) idle = 0;
             else if (++idle > W4_IDLE_LIMIT) break;
@@ -198,7 +198,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
         }
         if (!done) {                                                  // a warp gave up: the copies in flight land before this one leaves (bounded)
             latch_error(pb.status, TRIMKV_E_TIMEOUT);
-            for (unsigned k = issued > S::STAGES ? issued - S::STAGES : 0; k < issued; ++k) mbar_wait_bounded(my_full + k % S::STAGES, (k / S::STAGES) & 1u);
+            for (unsigned k = part > S::STAGES ? part - S::STAGES : 0; k < part; ++k) mbar_wait_bounded(full + c * S::STAGES + k % S::STAGES, (k / S::STAGES) & 1u);
         }
         return;
     }
@@ -207,23 +207,23 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     const unsigned char* ring = smem + (size_t)warp * S::STAGES * S::STAGE;
     full += warp * S::STAGES;
     empty += warp * S::STAGES;
-    desc += warp * S::STAGES;
+    desc += warp * W4_AHEAD;
     // this thread's places in a tile: codes and scales of K (entry of row gq, channels tq d / 4 ..), of V (entries of rows 2 tq and + 1, channels gq d / 8 ..)
-    const int k_codes = w4_entry(gq) * code_row + tq * (D / 8), k_scales = off_ks + w4_entry(gq) * scale_row + tq * (D / 64);
-    const int v_codes[2] = {off_vc + w4_entry(2 * tq) * code_row + gq * (D / 16), off_vc + w4_entry(2 * tq + 1) * code_row + gq * (D / 16)};
-    const int v_scales[2] = {off_vs + w4_entry(2 * tq) * scale_row + gq * D / 128, off_vs + w4_entry(2 * tq + 1) * scale_row + gq * D / 128};
+    const int k_codes = w4_entry(gq) * code_row + tq * (D / 8), k_scales = off_scale + w4_entry(gq) * scale_row + tq * (D / 64);
+    const int v_codes[2] = {w4_entry(2 * tq) * code_row + gq * (D / 16), w4_entry(2 * tq + 1) * code_row + gq * (D / 16)};
+    const int v_scales[2] = {off_scale + w4_entry(2 * tq) * scale_row + gq * D / 128, off_scale + w4_entry(2 * tq + 1) * scale_row + gq * D / 128};
     int row_first = 0, rows = 0, pos0 = 0, len = 0, all_lo = 0, all_hi = 0, all_end = 0;       // of the stretch; pos0: position of its request's first token
 
     uint32_t bq[NT][PARTS][KS][2];
     float o[NT][KS][4];
     float m_run[NT][2], l_run[NT][2], to_log2[NT][2];
 
-    for (unsigned stage = 0, parity = 0;;) {
-        if (!mbar_wait_bounded(full + stage, parity)) {
-            if (lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);
-            return;
-        }
-        const Tile4& it = desc[stage];
+    unsigned stage = 0, parity = 0;
+    bool ok = true;
+    for (unsigned tile_n = 0;; ++tile_n) {
+        ok = mbar_wait_bounded(full + stage, parity);
+        if (!ok) break;
+        const Tile4& it = desc[tile_n % W4_AHEAD];
         const int flags = it.flags, e0 = it.e0;
         if (flags & TILE_END) return;
         if (flags & TILE_FIRST) {
@@ -287,21 +287,20 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
         all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
         }
 
-        if (e0 >= 0) {
-            unsigned char* whole = const_cast<unsigned char*>(ring) + stage * S::STAGE;
-            const int held = len - e0;                                // entries of the tile, if it is not full
-            if (held < S::TILE) {
-                for (int i = max(held, 0) * scale_row + lane; i < S::TILE * scale_row; i += 32) whole[off_vs + i] = 0;
-                fence_proxy_async_smem();                             // before a later copy into this stage
-                __syncwarp();
-            }
+        const unsigned k_stage = stage;
+        if (++stage == S::STAGES) { stage = 0; parity ^= 1u; }
+        const unsigned char* k_tile = ring + k_stage * S::STAGE;
+        unsigned char* v_tile = const_cast<unsigned char*>(ring) + stage * S::STAGE;
+        bool v_here = false;
+        const bool any = e0 >= 0;
 #pragma unroll 1
-            for (int at = 0; at < S::TILE && e0 + at < all_end; at += S::STEP) {
+        for (int at = 0; at < PAGE; at += S::STEP) {
             const int es = e0 + at;                                   // entries es .. es + 31
-            const unsigned char *kc = whole + k_codes + at * code_row, *ks_at = whole + k_scales + at * scale_row, *vc0 = whole + v_codes[0] + at * code_row,
-                                *vc1 = whole + v_codes[1] + at * code_row, *vs0 = whole + v_scales[0] + at * scale_row, *vs1 = whole + v_scales[1] + at * scale_row;
-            // ---- S^T[entry][row] = K Q^T
+            const bool work = any && es < all_end;
             float sacc[MT][NT][4];
+            if (work) {
+            const unsigned char *kc = k_tile + k_codes + at * code_row, *ks_at = k_tile + k_scales + at * scale_row;
+            // ---- S^T[entry][row] = K Q^T
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -344,6 +343,25 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                     }
                 }
             }
+            }
+            if (at + S::STEP >= PAGE) {                               // K is done with
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty + k_stage);
+            }
+            if (!v_here) {
+                ok = ok && mbar_wait_bounded(full + stage, parity);
+                if (!ok) break;
+                v_here = true;
+                const int held = len - e0;                            // entries of the page, if it is not full
+                if (any && held < PAGE) {
+                    for (int i = max(held, 0) * scale_row + lane; i < PAGE * scale_row; i += 32) v_tile[off_scale + i] = 0;
+                    fence_proxy_async_smem();                         // before a later copy into this stage
+                    __syncwarp();
+                }
+            }
+            if (!work) continue;
+            const unsigned char *vc0 = v_tile + v_codes[0] + at * code_row, *vc1 = v_tile + v_codes[1] + at * code_row, *vs0 = v_tile + v_scales[0] + at * scale_row,
+                                *vs1 = v_tile + v_scales[1] + at * scale_row;
             // ---- softmax over the entries; this thread owns rows 2 tq, + 1 of each column tile.  The reference of a row's
             // weights is raised only when some logit exceeds it by 2^8: until then a tile needs one vote and no exchange.
             const bool edge = es + S::STEP > all_hi || es < all_lo;
@@ -467,10 +485,10 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                     for (int dt = 0; dt < KS; ++dt)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[nt][dt][i] += acc[nt][dt][i];
-            }
         }
+        if (!ok) break;
         const int row0 = it.row0, h = it.h, slot = it.slot;
-        __syncwarp();                                                 // all lanes are done with the stage before it is refilled
+        __syncwarp();                                                 // all lanes are done with V, and with the description
         if (lane == 0) mbar_arrive(empty + stage);
         if (++stage == S::STAGES) { stage = 0; parity ^= 1u; }
         if (!(flags & TILE_LAST)) continue;
@@ -507,6 +525,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 if (slot >= 0 && gq == 0) { wk.part_ml[pr * 2] = m_run[nt][c]; wk.part_ml[pr * 2 + 1] = l; }
             }
     }
+    if (!ok && lane == 0) latch_error(pb.status, TRIMKV_E_TIMEOUT);   // (who brings the tiles waits for the copies in flight)
 }
 
 template <int D, int NT, bool EXACT, typename T>
@@ -515,7 +534,7 @@ cudaError_t run_warp4(const Paged4View& c, const PagedBatch& pb, const void* q, 
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, EXACT, T>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3((S::WARPS + 1) * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
+    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3((S::WARPS + W4_FEED) * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
                      max_rows);
     if (e != cudaSuccess || paged_always_whole(pb, c.pv.H, S::ROWS, PAGED_SMS * S::WARPS, W4_JOIN_STEPS)) return e;
     return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st);

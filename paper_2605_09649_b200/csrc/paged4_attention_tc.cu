@@ -546,8 +546,8 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
                             const size_t row = ((size_t)p * pv.H + it.h) * PAGE;
                             const uint32_t dst = base + S::OFF_RAW + slot * Feed<D>::RAW;
                             a_bar_expect_tx(raw_full + 8 * slot, PAGE * (d / 2 + d / 16));
-                            t_bulk(dst, cache.codes[kv] + row * (d / 2), PAGE * (d / 2), raw_full + 8 * slot);
-                            t_bulk(dst + PAGE * (d / 2), cache.scales[kv] + row * (d / 16), PAGE * (d / 16), raw_full + 8 * slot);
+                            t_bulk(dst, (kv ? cache.codes[1] : cache.codes[0]) + row * (d / 2), PAGE * (d / 2), raw_full + 8 * slot);
+                            t_bulk(dst + PAGE * (d / 2), (kv ? cache.scales[1] : cache.scales[0]) + row * (d / 16), PAGE * (d / 16), raw_full + 8 * slot);
                         }
                     }
                     __syncwarp();
