@@ -456,9 +456,10 @@ constexpr int PAGED_SELECT_SMEM = 196 * 1024;
 size_t paged_select_smem(int W, int g, int d, int is_bf16);        // must not exceed PAGED_SELECT_SMEM
 cudaError_t launch_paged_select(const PagedView& pv, const PagedBatch& pb, int is_bf16, const void* q, int32_t* selected,
                                 cudaStream_t st);
-// Joins the partial results of a kernel of `workers` workers whose units have up to unit_rows rows.
+// Joins the partial results of a kernel of `workers` workers whose units have up to unit_rows rows; blocks: 0 or, for very many workers, how
+// many blocks look through their notes (at least a sixteenth of them).
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int unit_rows,
-                              int workers, cudaStream_t st);
+                              int workers, cudaStream_t st, int blocks = 0);
 // fp32 caches.
 cudaError_t launch_paged_attention_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
                                        cudaStream_t st);

@@ -26,32 +26,38 @@ namespace tkv {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr unsigned W4_IDLE_LIMIT = 1u << 22, W4_NAP = 64;             // rounds without progress, and ns between them
+constexpr unsigned W4_IDLE_LIMIT = 1u << 22, W4_NAP = 20;             // rounds without progress, and ns between them
 constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
 constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
 
 // A tile that a warp is to read, and the stretch of a unit that it belongs to.
-constexpr int W4_FEED = 2;                                            // warps that bring tiles to the others
 constexpr int W4_AHEAD = 4, W4_MOST_STAGES = 4;                       // pages that are described to a warp at most; places of its ring
 constexpr int TILE_FIRST = 1, TILE_LAST = 2, TILE_END = 4;            // of the stretch; nothing more to do
 struct __align__(16) Tile4 {
-    int e0, flags;                                                    // first entry; -1: nothing to read
+    int e0, flags;                                                    // first entry
+    int real;                                                         // whether there is something to read; written last, with the copy
     int row0, n, len, row_first, rows, h, slot;                       // see PagedItem, paged_unit_first, paged_unit_rows
-    int pad[3];
+    int pad[2];
 };
 
 template <int D, int NT, bool F32>
 struct Warp4Shape {
-    // Warps that compute, beside those that feed them.  As the registers allow: 128 a thread with 16 in all, 168 with 12, 255 with 8.
-    static constexpr int WARPS = (D <= 128 && NT == 1 && !F32 ? 16 : D <= 128 && !F32 ? 12 : 8) - W4_FEED;
-    static constexpr int EACH = (WARPS + W4_FEED - 1) / W4_FEED;      // warps that one feeds
+    // Warps that bring tiles, and those that compute.  As the registers allow: 128 a thread with 16 in all, 168 with 12, 255 with 8.  One warp feeds
+    // up to 11 in time (a page costs it some 500 cycles).
+    static constexpr int FEED = D <= 128 && NT == 1 && !F32 ? 2 : 1;
+    static constexpr int WARPS = (D > 128 || F32 ? 8 : NT == 2 ? 12 : 16) - FEED;
+    static constexpr int EACH = (WARPS + FEED - 1) / FEED;            // warps that one feeds
     static constexpr int ROWS = NT * 8;                               // rows of a unit
     static constexpr int STEP = 32;                                   // entries that are worked on at a time
-    static constexpr int STAGE = PAGE * (D / 2 + D / 16);             // codes and scales of a page's K, or of its V
-    static constexpr int STAGES = 208 * 1024 / WARPS / STAGE < W4_MOST_STAGES ? 208 * 1024 / WARPS / STAGE : W4_MOST_STAGES;
-    static_assert(STAGES >= 3 && (STAGES + 1) / 2 + 1 <= W4_AHEAD, "a description stays while its page is in the ring");
+    // A place of a ring holds a page's codes and scales of K and of V, or, where that leaves too few places, of one of them.
+    static constexpr bool WHOLE = D <= 128 && (NT > 1 || F32);
+    static constexpr int HALF = PAGE * (D / 2 + D / 16), STAGE = WHOLE ? 2 * HALF : HALF;
+    static constexpr int MOST = WHOLE ? W4_MOST_STAGES - 1 : W4_MOST_STAGES;
+    static constexpr int STAGES = 208 * 1024 / WARPS / STAGE < MOST ? 208 * 1024 / WARPS / STAGE : MOST;
+    static_assert(STAGES >= (WHOLE ? 2 : 3) && (WHOLE ? STAGES : (STAGES + 1) / 2) + 1 <= W4_AHEAD, "a description stays while its page is in the ring");
     static constexpr int OFF_BAR = WARPS * STAGES * STAGE;
-    static constexpr int OFF_DESC = (OFF_BAR + WARPS * STAGES * 16 + 15) & ~15;
+    static constexpr int OFF_TOLD = OFF_BAR + WARPS * STAGES * 16;    // pages described to each warp
+    static constexpr int OFF_DESC = (OFF_TOLD + WARPS * 4 + 15) & ~15;
     static constexpr int OFF_TAB = OFF_DESC + WARPS * W4_AHEAD * (int)sizeof(Tile4);
     static constexpr int SMEM = OFF_TAB + (int)sizeof(PagedTableMem) + 128;       // 128: alignment slack
     static_assert(SMEM <= 227 * 1024, "shared memory of one SM");
@@ -101,7 +107,7 @@ __device__ __forceinline__ void w4_store8(float* p, const float (&v)[8]) {
 
 // EXACT: the head size is D; otherwise smaller, a multiple of 32.  T: type of q and out.
 template <int D, int NT, bool EXACT, typename T>
-__global__ void __launch_bounds__((Warp4Shape<D, NT, sizeof(T) == 4>::WARPS + W4_FEED) * 32, 1)
+__global__ void __launch_bounds__((Warp4Shape<D, NT, sizeof(T) == 4>::WARPS + Warp4Shape<D, NT, sizeof(T) == 4>::FEED) * 32, 1)
 paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, float scale_log2, PagedWork wk, int max_rows) {
     using S = Warp4Shape<D, NT, sizeof(T) == 4>;
     constexpr bool F32 = sizeof(T) == 4;
@@ -114,12 +120,14 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = EXACT ? D : pv.d, gq = lane >> 2, tq = lane & 3;
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);      // [warp][stage]
     uint64_t* empty = full + S::WARPS * S::STAGES;
+    volatile unsigned* told = reinterpret_cast<volatile unsigned*>(smem + S::OFF_TOLD);
     Tile4* desc = reinterpret_cast<Tile4*>(smem + S::OFF_DESC);
     PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(smem + S::OFF_TAB);
     const int code_row = d / 2, scale_row = d / 16;
     const int off_scale = PAGE * code_row;                            // within a stage
 
     if (threadIdx.x < S::WARPS * S::STAGES) { mbar_init(full + threadIdx.x, 1); mbar_init(empty + threadIdx.x, 1); }
+    if (threadIdx.x < S::WARPS) told[threadIdx.x] = 0u;
     fence_proxy_async_smem();
     grid_dependency_wait();
     PagedTable tab;
@@ -134,30 +142,30 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
         const long long end = !done && w < tab.workers ? tab.share(w + 1) : 0;
         long long x = !done && w < tab.workers ? tab.share(w) : 0;
         PagedItem it;
-        int ntile = 0, tile = 0, phys = -1;
+        int ntile = 0, tile = 0, entry = -1, phys = -1;               // entry: the table's, on its way
+        auto table_entry = [&](int page) { return page < pb.W ? pb.table[(size_t)it.r * pb.W + page] : -1; };
         auto begin = [&]() {                                          // the stretch at x
             it = paged_item<0>(tab, pb, x, end, w);
             tile = 0;
             ntile = it.p1 - it.p0;
-            phys = ntile ? paged_physical(pb, pv, it.r, it.p0) : -1;
+            entry = ntile ? table_entry(it.p0) : -1;
         };
         if (x < end) begin();
-        // Part p is K (p even) or V of page p / 2, and lies in place p mod STAGES of the ring.
+        // Part p is K (p even) or V of page p / 2, or page p where a place holds both, and lies in place p mod STAGES of the ring.
         unsigned n = 0, part = 0, place = 0, parity = 1, idle = 0;    // page; (the first round of a ring finds it empty)
         while (__any_sync(0xffffffffu, !done)) {
             const unsigned at = (done ? 0 : c) * S::STAGES + place;
             const bool go = !done && (part < (unsigned)S::STAGES || w4_test(empty + at, parity));
             if (go) {
                 Tile4* t = desc + c * W4_AHEAD + n % W4_AHEAD;
-                const int kv = part & 1;
+                const int kv = S::WHOLE ? 0 : part & 1;
                 const bool last = tile + 1 >= ntile;
                 if (!kv) {
                     if (x >= end) {
                         t->flags = TILE_END;
-                        mbar_arrive(full + at);
                         done = true;
                     } else {
-                        t->e0 = phys >= 0 ? (it.p0 + tile) * PAGE : -1;
+                        t->e0 = (it.p0 + tile) * PAGE;
                         t->flags = (tile == 0 ? TILE_FIRST : 0) | (last ? TILE_LAST : 0);
                         if (tile == 0 || last) {                      // (at the first page all of it is read, at the last where the result goes)
                             t->row0 = it.q.row0; t->n = it.q.n; t->len = it.q.len;
@@ -166,6 +174,13 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                             t->h = it.h; t->slot = it.slot;
                         }
                     }
+                    __threadfence_block();
+                    told[c] = n + 1;
+                    if (!done) {
+                        phys = entry >= 0 && entry < pv.n_pages ? entry : -1;
+                        if (phys < 0 && ntile > 0) latch_error(pb.status, TRIMKV_E_ARG);
+                        t->real = phys >= 0;
+                    }
                 }
                 if (!done) {
                     if (phys < 0) {
@@ -173,11 +188,16 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                     } else {
                         unsigned char* dst = smem + (size_t)at * S::STAGE;
                         const size_t row = ((size_t)phys * pv.H + it.h) * PAGE;
-                        mbar_expect_tx(full + at, PAGE * (code_row + scale_row));      // (the zeroing of scales below carries its own proxy fence)
+                        // (the zeroing of scales below carries its own proxy fence)
+                        mbar_expect_tx(full + at, (S::WHOLE ? 2 : 1) * PAGE * (code_row + scale_row));
                         bulk_g2s(dst, (kv ? cache.codes[1] : cache.codes[0]) + row * code_row, off_scale, full + at);
                         bulk_g2s(dst + off_scale, (kv ? cache.scales[1] : cache.scales[0]) + row * scale_row, PAGE * scale_row, full + at);
+                        if (S::WHOLE) {
+                            bulk_g2s(dst + S::HALF, cache.codes[1] + row * code_row, off_scale, full + at);
+                            bulk_g2s(dst + S::HALF + off_scale, cache.scales[1] + row * scale_row, PAGE * scale_row, full + at);
+                        }
                     }
-                    if (kv) {                                         // what comes next
+                    if (kv || S::WHOLE) {                             // what comes next
                         ++n;
                         if (tile == 0 && it.slot >= 0 && (it.slot & 1))
                             paged_note_shared(wk, tab, it, x, w, paged_unit_first<0>(pb, it.u, S::ROWS), paged_unit_rows<0>(pb, it.u, it.q.n, S::ROWS));
@@ -185,7 +205,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                             x += it.steps;
                             if (x < end) begin();
                         } else {
-                            phys = paged_physical(pb, pv, it.r, it.p0 + tile);
+                            entry = table_entry(it.p0 + tile);
                         }
                     }
                     ++part;
@@ -221,8 +241,8 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     unsigned stage = 0, parity = 0;
     bool ok = true;
     for (unsigned tile_n = 0;; ++tile_n) {
-        ok = mbar_wait_bounded(full + stage, parity);
-        if (!ok) break;
+        for (unsigned k = 0; (ok = (int)(told[warp] - tile_n) > 0) == false && k < W4_IDLE_LIMIT; ++k) __nanosleep(W4_NAP);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         const Tile4& it = desc[tile_n % W4_AHEAD];
         const int flags = it.flags, e0 = it.e0;
         if (flags & TILE_END) return;
@@ -287,12 +307,14 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
         all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
         }
 
+        ok = mbar_wait_bounded(full + stage, parity);
+        if (!ok) break;
         const unsigned k_stage = stage;
-        if (++stage == S::STAGES) { stage = 0; parity ^= 1u; }
+        if (!S::WHOLE && ++stage == S::STAGES) { stage = 0; parity ^= 1u; }
         const unsigned char* k_tile = ring + k_stage * S::STAGE;
-        unsigned char* v_tile = const_cast<unsigned char*>(ring) + stage * S::STAGE;
+        unsigned char* v_tile = const_cast<unsigned char*>(ring) + stage * S::STAGE + (S::WHOLE ? S::HALF : 0);
         bool v_here = false;
-        const bool any = e0 >= 0;
+        const bool any = it.real != 0;
 #pragma unroll 1
         for (int at = 0; at < PAGE; at += S::STEP) {
             const int es = e0 + at;                                   // entries es .. es + 31
@@ -344,12 +366,12 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 }
             }
             }
-            if (at + S::STEP >= PAGE) {                               // K is done with
+            if (!S::WHOLE && at + S::STEP >= PAGE) {                  // K is done with
                 __syncwarp();
                 if (lane == 0) mbar_arrive(empty + k_stage);
             }
             if (!v_here) {
-                ok = ok && mbar_wait_bounded(full + stage, parity);
+                if (!S::WHOLE) ok = mbar_wait_bounded(full + stage, parity);
                 if (!ok) break;
                 v_here = true;
                 const int held = len - e0;                            // entries of the page, if it is not full
@@ -534,10 +556,10 @@ cudaError_t run_warp4(const Paged4View& c, const PagedBatch& pb, const void* q, 
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = paged_allow_smem(reinterpret_cast<const void*>(paged4_attn_warp_kernel<D, NT, EXACT, T>), S::SMEM, done);
     if (e != cudaSuccess) return e;
-    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3((S::WARPS + W4_FEED) * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
+    e = paged_launch(paged4_attn_warp_kernel<D, NT, EXACT, T>, dim3(PAGED_SMS), dim3((S::WARPS + S::FEED) * 32), S::SMEM, 1, true, st, c, pb, (const T*)q, (T*)out, scale * LOG2E, w,
                      max_rows);
     if (e != cudaSuccess || paged_always_whole(pb, c.pv.H, S::ROWS, PAGED_SMS * S::WARPS, W4_JOIN_STEPS)) return e;
-    return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st);
+    return launch_paged_join(c.pv, pb, sizeof(T) == 2, out, w, S::ROWS, PAGED_SMS * S::WARPS, st, NT == 1 ? PAGED_SMS * 2 : 0);
 }
 
 }  // namespace
@@ -549,7 +571,9 @@ cudaError_t launch_paged4_attention_warp(const Paged4View& c, const PagedBatch& 
         if (c.pv.d == D) return is_bf16 ? run_warp4<D, NT, true, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, true, float>(c, pb, q, out, scale, w, max_rows, st);
         return is_bf16 ? run_warp4<D, NT, false, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, false, float>(c, pb, q, out, scale, w, max_rows, st);
     };
-    auto rows = [&](auto d) { return tile_rows <= 8 ? go(d, std::integral_constant<int, 1>{}) : go(d, std::integral_constant<int, 2>{}); };
+    auto rows = [&](auto d) {
+        return tile_rows <= 8 ? go(d, std::integral_constant<int, 1>{}) : go(d, std::integral_constant<int, 2>{});
+    };
     return c.pv.d <= 64    ? rows(std::integral_constant<int, 64>{})
            : c.pv.d <= 128 ? rows(std::integral_constant<int, 128>{})
                            : go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});

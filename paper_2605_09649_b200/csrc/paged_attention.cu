@@ -276,7 +276,7 @@ paged_attn_f32_kernel(PagedView pv, PagedBatch pb, const float* q, float* out, f
 // enough to be paced by fetching its code: one loop takes up to J_BATCH parts at a time, m, l and O in flight together, with a running
 // maximum; a row of many parts is dealt out over several warps.  5 to 6 us for a decode step, 18 us for the 38 MB of parts of 4 x
 // 512 tokens x 32 heads.  (Every row searching for its request and its workers by itself took 7 to 11 and 31 us.)
-constexpr int J_THREADS = 512, J_WARPS = J_THREADS / 32, J_BATCH = 6;
+constexpr int J_THREADS = 512, J_WARPS = J_THREADS / 32, J_BATCH = 6, J_NOTES = 16;
 
 __device__ __forceinline__ void join_store(__nv_bfloat16* o, const float4& v, float f) {
     const __nv_bfloat162 a = __floats2bfloat162_rn(v.x * f, v.y * f), b = __floats2bfloat162_rn(v.z * f, v.w * f);
@@ -290,15 +290,23 @@ __device__ __forceinline__ float join_factor(float l) { return l > 0.f ? 1.f / l
 
 template <typename T>
 __global__ void __launch_bounds__(J_THREADS, 2)
-paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_rows, int chunk) {
+paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_rows, int chunk, int workers) {
     extern __shared__ __align__(16) float4 s_sum[];               // [J_WARPS][d / 4]
     __shared__ float2 s_ml[J_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w = blockIdx.x, g = (int)by_g.d;
+    __shared__ int4 s_unit[J_NOTES];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = (int)by_g.d;
     grid_dependents_may_launch();
     grid_dependency_wait();
-    const int4 unit = wk.shared[w];
+    // the units of workers blockIdx.x, + gridDim.x, ...: all notes at once where there is more than one
+    if ((int)gridDim.x < workers) {
+        const int at = (int)(blockIdx.x + threadIdx.x * gridDim.x);
+        if (threadIdx.x < J_NOTES) s_unit[threadIdx.x] = at < workers ? wk.shared[at] : make_int4(0, 0, 0, 0);
+        __syncthreads();
+    }
+    for (int w = blockIdx.x, note = 0; w < workers; w += (int)gridDim.x, ++note) {
+    const int4 unit = (int)gridDim.x < workers ? s_unit[note] : wk.shared[w];
     const int r0 = (int)blockIdx.y * chunk, nr = min(chunk, (unit.z & 4095) - r0), n = unit.z >> 12;
-    if (nr <= 0) return;
+    if (nr <= 0) continue;
     int shift = 0;                                                // 2^shift warps per row
     while ((2 << shift) * nr <= J_WARPS && (J_BATCH << shift) < n) ++shift;
     const int way = warp & ((1 << shift) - 1), i_lo = n * way >> shift, i_hi = n * (way + 1) >> shift;
@@ -345,10 +353,10 @@ paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_ro
             }
         }
     }
-    if (shift == 0) return;
+    if (shift == 0) continue;
     __syncthreads();
     const int rr = warp >> shift;
-    if (way != 0 || rr >= nr) return;
+    if (way == 0 && rr < nr) {
     const int row = unit.y + r0 + rr, t = by_g.div(row);
     T* o = out + ((size_t)(unit.x + t) * Hq + (size_t)(unit.w * g + row - t * g)) * d;
     float M = -INFINITY, L = 0.f;
@@ -359,6 +367,9 @@ paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_ro
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int x = 0; x < 1 << shift; ++x) join_add(sum, exp2f(s_ml[warp + x].x - ref), s_sum[(warp + x) * (d / 4) + c0 / 4]);
         join_store(o + c0, sum, join_factor(L));
+    }
+    }
+    __syncthreads();                                              // the sums are read
     }
 }
 
@@ -380,13 +391,14 @@ cudaError_t run_f32(const PagedView& pv, const PagedBatch& pb, const void* q, vo
 }  // namespace
 
 cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_bf16, void* out, const PagedWork& w, int unit_rows,
-                              int workers, cudaStream_t st) {
+                              int workers, cudaStream_t st, int blocks) {
     // Units of few rows are those with many parts: four rows leave four warps to each (measured for 4 requests x 4 heads of 7 rows in
     // 37 parts: 25.9 us with the kernel before it, eight rows to a block 28.6); otherwise two rows per warp.
     const int chunk = std::min(unit_rows, unit_rows <= 8 ? 4 : 2 * J_WARPS);
-    const dim3 grid((unsigned)workers, (unsigned)((unit_rows + chunk - 1) / chunk)), block(J_THREADS);
+    if (blocks <= 0 || blocks * J_NOTES < workers) blocks = workers;
+    const dim3 grid((unsigned)std::min(blocks, workers), (unsigned)((unit_rows + chunk - 1) / chunk)), block(J_THREADS);
     const size_t smem = (size_t)J_WARPS * pv.d * sizeof(float);
-    auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, smem, 1, true, st, o, w, pb.by_g, pb.Hq, pv.d, unit_rows, chunk); };
+    auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, smem, 1, true, st, o, w, pb.by_g, pb.Hq, pv.d, unit_rows, chunk, workers); };
     return is_bf16 ? go(paged_join_kernel<__nv_bfloat16>, (__nv_bfloat16*)out) : go(paged_join_kernel<float>, (float*)out);
 }
 
