@@ -18,7 +18,7 @@ namespace tkv {
 
 namespace {
 
-constexpr int A4_THREADS = 256;
+constexpr int A4_THREADS = 256, R4_UNROLL = 4;
 
 __device__ __forceinline__ float max_nan(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
 __device__ __forceinline__ uint32_t a4_scale(float amax) {                // of max |x'|
@@ -113,59 +113,96 @@ paged4_append_kernel(Paged4View c, uint8_t* k_codes, uint8_t* k_scales, uint8_t*
     }
 }
 
-__device__ __forceinline__ void r4_store(__nv_bfloat16* p, const float2* v) {       // 32 values
+// 32 bytes, a whole sector.
+__device__ __forceinline__ void r4_store32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]),
+                 "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ void r4_store(__nv_bfloat16* p, const float2 (&v)[8]) {       // 16 values
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[i * 4 + e].x, v[i * 4 + e].y);
-            w[e] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        reinterpret_cast<uint4*>(p)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int e = 0; e < 8; ++e) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[e].x, v[e].y);
+        w[e] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+        r4_store32(p, w);
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
 }
-__device__ __forceinline__ void r4_store(float* p, const float2* v) {
+__device__ __forceinline__ void r4_store(float* p, const float2 (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
+    for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(A4_THREADS)
 paged4_read_kernel(Paged4View c, long long items, const int32_t* slot_map, T* k, T* v, int32_t* status) {
     const int kv = blockIdx.y, H = c.pv.H, d = c.pv.d, per_head = d / 32, per_tok = H * per_head;
+    const uint8_t* codes = kv ? c.codes[1] : c.codes[0];
+    const uint8_t* scales = kv ? c.scales[1] : c.scales[0];
     T* out = kv ? v : k;
+    const long long step = (long long)gridDim.x * A4_THREADS;
     grid_dependency_wait();
     grid_dependents_may_launch();
-    for (long long i = (long long)blockIdx.x * A4_THREADS + threadIdx.x; i < items; i += (long long)gridDim.x * A4_THREADS) {
-        const int tok = (int)(i / per_tok), rest = (int)(i - (long long)tok * per_tok), h = rest / per_head, part = rest - h * per_head;
-        const int slot = slot_map[tok];
-        float2 val[16];
-        if (slot < 0 || slot >= c.pv.n_pages * PAGE) {
-            if (slot != -1 && rest == 0) latch_error(status, TRIMKV_E_ARG);
+    for (long long i0 = (long long)blockIdx.x * A4_THREADS + threadIdx.x; i0 < items; i0 += R4_UNROLL * step) {
+        uint4 code[R4_UNROLL];
+        uint32_t scale[R4_UNROLL];
+        int head[R4_UNROLL];
+        bool wrong = false;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) val[e] = make_float2(0.f, 0.f);
-        } else {
-            const long long row = ((long long)(slot / PAGE) * H + h) * PAGE + slot % PAGE;
-            const uint4 code = *reinterpret_cast<const uint4*>(c.codes[kv] + row * (d / 2) + part * 16);
-            const uint32_t s2 = p4_scales(*reinterpret_cast<const uint16_t*>(c.scales[kv] + row * (d / 16) + part * 2));
-            const float up = p4_pow2(p4_shift(c, kv, h));
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t r[4];
-                p4_codes(reinterpret_cast<const uint32_t*>(&code)[w], r);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = p4_float2(p4_mul(r[e], w < 2 ? p4_both_low(s2) : p4_both_high(s2)));
-                    val[w * 4 + e] = make_float2(f.x * up, f.y * up);
-                }
+        for (int u = 0; u < R4_UNROLL; ++u) {                             // all loads in flight
+            const long long i = i0 + u * step;
+            const int tok = (unsigned long long)i >> 32 ? (int)(i / per_tok) : (int)((unsigned)i / (unsigned)per_tok);
+            const unsigned rest = (unsigned)(i - (long long)tok * per_tok);
+            head[u] = (int)(rest / (unsigned)per_head);
+            const int part = (int)(rest - (unsigned)head[u] * (unsigned)per_head);
+            const int slot = i < items ? slot_map[tok] : -1;
+            code[u] = make_uint4(0u, 0u, 0u, 0u);                         // a slot that is none: zeros
+            scale[u] = 0u;
+            if (slot >= 0 && slot < c.pv.n_pages * PAGE) {
+                const long long row = ((long long)(slot / PAGE) * H + head[u]) * PAGE + slot % PAGE;
+                code[u] = *reinterpret_cast<const uint4*>(codes + row * (d / 2) + part * 16);
+                scale[u] = *reinterpret_cast<const uint16_t*>(scales + row * (d / 16) + part * 2);
+            } else {
+                wrong |= slot != -1;
             }
         }
-        r4_store(out + (long long)tok * H * d + (long long)h * d + part * 32, val);
+        if (wrong) latch_error(status, TRIMKV_E_ARG);
+#pragma unroll
+        for (int u = 0; u < R4_UNROLL; ++u) {
+            const long long i = i0 + u * step;
+            if (i >= items) continue;
+            const uint32_t s2 = p4_scales(scale[u]);
+            const float up = p4_pow2(p4_shift(c, kv, head[u]));
+            const uint32_t word[4] = {code[u].x, code[u].y, code[u].z, code[u].w};
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t by = b ? p4_both_high(s2) : p4_both_low(s2);
+                float2 val[8];
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    uint32_t r[4];
+                    p4_codes(word[2 * b + w], r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = p4_float2(p4_mul(r[e], by));
+                        val[w * 4 + e] = make_float2(f.x * up, f.y * up);
+                    }
+                }
+                r4_store(out + i * 32 + b * 16, val);                     // (items lie in the output's order)
+            }
+        }
     }
 }
 
-unsigned a4_blocks(long long items) { return (unsigned)std::min<long long>((items + A4_THREADS - 1) / A4_THREADS, PAGED_SMS * 32); }
+unsigned a4_blocks(long long items, int each) {      // `each` items per thread, fewer while that leaves the GPU unfilled
+    const long long one = (items + A4_THREADS - 1) / A4_THREADS;
+    return (unsigned)std::max<long long>(std::min<long long>(one, PAGED_SMS * 4), std::min<long long>((one + each - 1) / each, PAGED_SMS * 64));
+}
 
 }  // namespace
 
@@ -173,7 +210,7 @@ cudaError_t launch_paged4_append(const Paged4View& c, int is_bf16, int T, const 
                                  const int32_t* slot_map, int32_t* status, cudaStream_t st) {
     const long long items = (long long)T * c.pv.H * (c.pv.d / 32);
     auto go = [&](auto kernel, auto* type) {
-        return paged_launch(kernel, dim3(a4_blocks(items), 2), dim3(A4_THREADS), 0, 1, true, st, c, const_cast<uint8_t*>(c.codes[0]), const_cast<uint8_t*>(c.scales[0]),
+        return paged_launch(kernel, dim3(a4_blocks(items, 1), 2), dim3(A4_THREADS), 0, 1, true, st, c, const_cast<uint8_t*>(c.codes[0]), const_cast<uint8_t*>(c.scales[0]),
                             const_cast<uint8_t*>(c.codes[1]), const_cast<uint8_t*>(c.scales[1]), items, (decltype(type))k, k_stride, (decltype(type))v, v_stride,
                             slot_map, status);
     };
@@ -183,7 +220,7 @@ cudaError_t launch_paged4_append(const Paged4View& c, int is_bf16, int T, const 
 cudaError_t launch_paged4_read(const Paged4View& c, int is_bf16, int n, const int32_t* slot_map, void* k, void* v, int32_t* status, cudaStream_t st) {
     const long long items = (long long)n * c.pv.H * (c.pv.d / 32);
     auto go = [&](auto kernel, auto* type) {
-        return paged_launch(kernel, dim3(a4_blocks(items), 2), dim3(A4_THREADS), 0, 1, true, st, c, items, slot_map, (decltype(type))k, (decltype(type))v, status);
+        return paged_launch(kernel, dim3(a4_blocks(items, R4_UNROLL), 2), dim3(A4_THREADS), 0, 1, true, st, c, items, slot_map, (decltype(type))k, (decltype(type))v, status);
     };
     return is_bf16 ? go(paged4_read_kernel<__nv_bfloat16>, (__nv_bfloat16*)nullptr) : go(paged4_read_kernel<float>, (float*)nullptr);
 }
