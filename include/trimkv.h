@@ -453,8 +453,8 @@ TRIMKV_API trimkv_status trimkv_paged_sparse_attention(const trimkv_paged_cache*
  *   scales   e4m3 bytes [n_pages, kv_heads, 64, head_dim / 16]
  *   shift    int32 [kv_heads], device memory, or NULL (0): the powers of two that bring a head's values, largest over 16 channels, into
  *            the range of the scales (0.1 to 2688 with full precision).  Taken as -64 or 64 beyond these.
- * A fifth to a quarter of the bytes of bf16: 0.28.  The values of a block are off by a quarter of the scale where they are
- * small (code x scale up to 2), by a half or a whole one above: scale is a sixth of the block's largest magnitude. */
+ * That is 0.28 of the bytes of bf16.  A value is off by a quarter of its block's scale at most up to twice the scale, by half of it up to
+ * four times, by the whole of it above; the scale is a sixth of the block's largest magnitude, give or take a sixteenth. */
 typedef struct trimkv_paged4_cache {
     void* k_codes;             /* these four 16-byte aligned */
     void* k_scales;
@@ -486,7 +486,8 @@ TRIMKV_API size_t trimkv_paged4_workspace_bytes(int32_t q_heads, int32_t kv_head
 
 /* trimkv_paged_attention over a cache in 4 bits: the same arguments and rules, q and out in dtype.  The values of the cache enter the
  * products exactly.  q is below 2^70.  bf16: weights are rounded to fp16 for their product with v (off by 2^-11 at most; weights below
- * 2^-21 of a row's largest by 2^-32 of that).  fp32: q and the weights in two fp16 parts each, 2^-22 relative. */
+ * 2^-21 of a row's largest by 2^-32 of that).  fp32: q and the weights in two fp16 parts each, 2^-22 relative.
+ * The tables, lengths and slots are trimkv_paged_plan's or trimkv_paged_share's.  There is no selection of pages (no key_bounds) here. */
 TRIMKV_API trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t dtype, int32_t n_req, int64_t n_tokens, int32_t max_new,
                                       int32_t q_heads, const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,
                                       const int32_t* block_table, int32_t table_width, float scale, int32_t window, void* out,

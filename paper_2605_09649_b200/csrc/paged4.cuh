@@ -64,7 +64,7 @@ constexpr int P4_WARPS = 16;
 constexpr int P4_WORKER_ROWS = PAGED_SMS * 11 * 16;
 constexpr size_t P4_SHARED_BYTES = (size_t)PAGED_SMS * P4_WARPS * 16;
 static_assert(P4_SHARED_BYTES % 256 == 0, "partial results are aligned");
-// Units of tile_rows = 8 or 16 rows (head sizes above 128: 8) of the requests of up to max_rows rows.
+// Units of tile_rows = 8 or 16 rows (fp32 and head sizes above 128: 8) of the requests of up to max_rows rows.
 cudaError_t launch_paged4_attention_warp(const Paged4View& c, const PagedBatch& pb, int is_bf16, const void* q, void* out, float scale, const PagedWork& w,
                                          int tile_rows, int max_rows, cudaStream_t st);
 // Tensor-core kernel, bf16 and head sizes up to PAGED_TC_HEAD: units of PAGED_TC_ROWS rows of the requests of more than min_rows - 1.

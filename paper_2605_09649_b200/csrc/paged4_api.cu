@@ -99,7 +99,7 @@ trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t 
     // Requests of up to 32 rows (tokens x query heads of a KV head) go to the warp kernel, larger ones to the tcgen05 kernel, where there is
     // one.  max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
-    const int tile = most <= 8 ? 8 : 16;
+    const int tile = most <= 8 || (c.pv.d > PAGED_TC_HEAD && most <= PAGED_WARP_ROWS) ? 8 : 16;
     cudaError_t e = cudaSuccess;
     if (most <= 32 || !is_bf16 || c.pv.d > PAGED_TC_HEAD) {
         e = launch_paged4_attention_warp(c, pb, is_bf16, q, out, scale, w, tile, INT_MAX, st);

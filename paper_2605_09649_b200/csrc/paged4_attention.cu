@@ -1,16 +1,23 @@
 // Attention over the paged cache held in 4 bits, for few query rows (and for fp32 and head sizes above 128, any number).
 //
-// One CTA per SM, independent warps, each with a ring of its own in shared memory that bulk copies fill with 32 entries at a time: codes
-// and scales of K and of V.  A warp takes an equal share of the line of page steps (paged.cuh) and computes S^T = K Q^T and
-// O^T += V^T P^T with mma.sync m16n8k16 in fp16, the (token, head) rows as the N dimension: fp16 holds every value of the cache
-// exactly (paged4.cuh), and Q once each row is scaled by a power of two (its largest value in 2^10 .. 2^11; what is lost of the
-// smallest ones is 2^-35 of the largest).  fp32: Q and P in two fp16 parts each, 2^-22 relative, and sums of a tile apart.
+// One CTA per SM.  Its warps are independent, each with a ring of its own in shared memory and an equal share of the line of page steps
+// (paged.cuh); one or two more walk those shares for them, a lane for each warp: they describe a page, then have the copy engine
+// bring its codes and scales.  A computing warp forms S^T = K Q^T and O^T += V^T P^T with mma.sync m16n8k16 in fp16, 32 entries at a
+// time, the (token, head) rows as the N dimension: fp16 holds every value of the cache exactly (paged4.cuh), and Q once each row
+// is scaled by a power of two (its largest value in 2^10 .. 2^11; what is lost of the smallest ones is 2^-35 of the largest).  fp32:
+// Q and P in two fp16 parts each, 2^-22 relative, and the sums of 32 entries apart.
 //
 // The operands are made in registers.  K (A operand, rows = entries): a thread takes d / 4 neighbouring channels of an entry, so the order of
 // channels along k is a permutation, which Q follows; a word of codes is the A registers of two products.  V (A operand, rows =
 // channels): a thread takes d / 8 neighbouring channels of entries in pairs, and three-input logic puts the codes of one channel
 // of two entries into a byte, which one conversion makes the register.  Each register is then multiplied by its scale (of two entries for V).
-// A thread's 2 x 32 channels and scales of 16 entries cost about 200 instructions.
+// 16 entries of heads of 128 cost a warp 270 instructions, 122 of them on the ALU (64 conversions) and 95 on the FMA pipe (64 products
+// with scales).
+//
+// What bounds it: 302 MB of a decode step (8 requests of 32 K, 8 x 4 heads of 128) take 73 us, 19 of which no length changes (launch, table of
+// requests, first pages, join) and the rest 5.2 TB/s, 0.8 of the copy rate; without the conversions, or without the products with
+// scales, it takes 9 us less.  Steps: 8 warps that fetch for themselves 121 us, 16 of them 100, head size known at compile time 82, 11 warps fed by
+// another 77.6, 14 fed by two 77.1, descriptions ahead of the copies and a join of 296 blocks 74.5.
 //
 // The reference of a row's weights lags its maximum by up to 2^8, and weights are 2^7 times their value: at most 2^15, and what
 // fp16 cannot hold is below 2^-32 of the row's largest weight.
@@ -242,69 +249,71 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
     bool ok = true;
     for (unsigned tile_n = 0;; ++tile_n) {
         for (unsigned k = 0; (ok = (int)(told[warp] - tile_n) > 0) == false && k < W4_IDLE_LIMIT; ++k) __nanosleep(W4_NAP);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        __syncwarp();                                                 // the description is read after the count
         const Tile4& it = desc[tile_n % W4_AHEAD];
         const int flags = it.flags, e0 = it.e0;
         if (flags & TILE_END) return;
         if (flags & TILE_FIRST) {
-        row_first = it.row_first;
-        rows = it.rows;
-        len = it.len;
-        pos0 = it.len - it.n;
-        const int ksh = p4_shift(cache, 0, it.h);
-        // ---- Q fragments (B operand: k = channel, n = row): row gq of a column tile, channels tq d / 4 ..
+            row_first = it.row_first;
+            rows = it.rows;
+            len = it.len;
+            pos0 = it.len - it.n;
+            const int ksh = p4_shift(cache, 0, it.h);
+            // ---- Q fragments (B operand: k = channel, n = row): row gq of a column tile, channels tq d / 4 ..
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int row = nt * 8 + gq, qr = row_first + row;
-            const int qt = row < rows ? pb.by_g.div(qr) : 0, qj = row < rows ? qr - qt * g : 0;
-            const T* p = q + (size_t)(it.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + tq * (D / 4);
-            float top = 0.f;
-            auto load = [&](float (&v)[8], int c) {
-                if (row < rows && tq * (D / 4) + c < d) w4_load8(v, p + c);
-                else
+            for (int nt = 0; nt < NT; ++nt) {
+                const int row = nt * 8 + gq, qr = row_first + row;
+                const int qt = row < rows ? pb.by_g.div(qr) : 0, qj = row < rows ? qr - qt * g : 0;
+                const T* p = q + (size_t)(it.row0 + qt) * pb.q_stride + (size_t)(it.h * g + qj) * d + tq * (D / 4);
+                float top = 0.f;
+                auto load = [&](float (&v)[8], int c) {
+                    if (row < rows && tq * (D / 4) + c < d) w4_load8(v, p + c);
+                    else
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-            };
+                        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+                };
 #pragma unroll
-            for (int c = 0; c < D / 4; c += 8) {
-                float v[8];
-                load(v, c);
+                for (int c = 0; c < D / 4; c += 8) {
+                    float v[8];
+                    load(v, c);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-            }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int up = top > 0.f ? max(-60, min(60, 137 - (int)(__float_as_uint(top) >> 23))) : 0;
-            const float f = p4_pow2(up);
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int up = top > 0.f ? max(-60, min(60, 137 - (int)(__float_as_uint(top) >> 23))) : 0;
+                const float f = p4_pow2(up);
 #pragma unroll
-            for (int c = 0; c < D / 4; c += 8) {
-                float v[8];
-                load(v, c);
+                for (int c = 0; c < D / 4; c += 8) {
+                    float v[8];
+                    load(v, c);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float x0 = v[e] * f, x1 = v[e + 1] * f;
-                    const uint32_t hi = p4_f16x2(x0, x1);
-                    bq[nt][0][c / 4 + e / 4][(e >> 1) & 1] = hi;
-                    if constexpr (F32) {
-                        const float2 b = p4_float2(hi);
-                        bq[nt][1][c / 4 + e / 4][(e >> 1) & 1] = p4_f16x2(x0 - b.x, x1 - b.y);
+                    for (int e = 0; e < 8; e += 2) {
+                        const float x0 = v[e] * f, x1 = v[e + 1] * f;
+                        const uint32_t hi = p4_f16x2(x0, x1);
+                        bq[nt][0][c / 4 + e / 4][(e >> 1) & 1] = hi;
+                        if constexpr (F32) {
+                            const float2 b = p4_float2(hi);
+                            bq[nt][1][c / 4 + e / 4][(e >> 1) & 1] = p4_f16x2(x0 - b.x, x1 - b.y);
+                        }
                     }
                 }
-            }
-            const float back = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));      // of row gq; this thread's columns are 2 tq, + 1
+                const float back = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));      // of row gq; this thread's columns are 2 tq, + 1
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                to_log2[nt][c] = __shfl_sync(0xffffffffu, back, (2 * tq + c) * 4);
-                m_run[nt][c] = -INFINITY;
-                l_run[nt][c] = 0.f;
-            }
+                for (int c = 0; c < 2; ++c) {
+                    to_log2[nt][c] = __shfl_sync(0xffffffffu, back, (2 * tq + c) * 4);
+                    m_run[nt][c] = -INFINITY;
+                    l_run[nt][c] = 0.f;
+                }
 #pragma unroll
-            for (int dt = 0; dt < KS; ++dt) o[nt][dt][0] = o[nt][dt][1] = o[nt][dt][2] = o[nt][dt][3] = 0.f;
-        }
-        // entries that every row of the unit sees, from its first and last row
-        all_hi = max(pos0 + pb.by_g.div(row_first) + 1, 0);
-        all_end = pos0 + pb.by_g.div(row_first + rows - 1) + 1;        // none sees an entry from here on
-        all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
+                for (int dt = 0; dt < KS; ++dt) o[nt][dt][0] = o[nt][dt][1] = o[nt][dt][2] = o[nt][dt][3] = 0.f;
+            }
+            // entries that every row of the unit sees, from its first and last row
+            all_hi = max(pos0 + pb.by_g.div(row_first) + 1, 0);
+            all_end = pos0 + pb.by_g.div(row_first + rows - 1) + 1;        // none sees an entry from here on
+            all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
         }
 
         ok = mbar_wait_bounded(full + stage, parity);
@@ -321,50 +330,50 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
             const bool work = any && es < all_end;
             float sacc[MT][NT][4];
             if (work) {
-            const unsigned char *kc = k_tile + k_codes + at * code_row, *ks_at = k_tile + k_scales + at * scale_row;
-            // ---- S^T[entry][row] = K Q^T
+                const unsigned char *kc = k_tile + k_codes + at * code_row, *ks_at = k_tile + k_scales + at * scale_row;
+                // ---- S^T[entry][row] = K Q^T
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+                for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) sacc[mt][nt][0] = sacc[mt][nt][1] = sacc[mt][nt][2] = sacc[mt][nt][3] = 0.f;
-                uint32_t kw[2][KW], ks[2][(KW + 3) / 4 * 2];           // rows gq and gq + 8: codes; scales, both halves of a register alike
+                    for (int nt = 0; nt < NT; ++nt) sacc[mt][nt][0] = sacc[mt][nt][1] = sacc[mt][nt][2] = sacc[mt][nt][3] = 0.f;
+                    uint32_t kw[2][KW], ks[2][(KW + 3) / 4 * 2];           // rows gq and gq + 8: codes; scales, both halves of a register alike
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const unsigned char* cp = kc + (mt * 16 + i * 8) * code_row;
-                    const unsigned char* sp = ks_at + (mt * 16 + i * 8) * scale_row;
+                    for (int i = 0; i < 2; ++i) {
+                        const unsigned char* cp = kc + (mt * 16 + i * 8) * code_row;
+                        const unsigned char* sp = ks_at + (mt * 16 + i * 8) * scale_row;
 #pragma unroll
-                    for (int c = 0; c < KW; c += 4) {                 // (KW = 2 for heads of 64)
-                        uint32_t two = 0u;
-                        if (EXACT || tq * (D / 4) + c * 8 < d) {
-                            w4_load<KW == 2 ? 8 : 16>(&kw[i][c], cp + c * 4);
-                            two = KW == 2 ? (uint32_t)sp[0] : (uint32_t)*reinterpret_cast<const uint16_t*>(sp + c / 2);
-                        } else                                        // missing channels: Q has zeros there
+                        for (int c = 0; c < KW; c += 4) {                 // (KW = 2 for heads of 64)
+                            uint32_t two = 0u;
+                            if (EXACT || tq * (D / 4) + c * 8 < d) {
+                                w4_load<KW == 2 ? 8 : 16>(&kw[i][c], cp + c * 4);
+                                two = KW == 2 ? (uint32_t)sp[0] : (uint32_t)*reinterpret_cast<const uint16_t*>(sp + c / 2);
+                            } else                                        // missing channels: Q has zeros there
 #pragma unroll
-                            for (int x = 0; x < 4 && c + x < KW; ++x) kw[i][c + x] = 0u;
-                        const uint32_t sc = p4_scales(two);
-                        ks[i][c / 2] = p4_both_low(sc);
-                        if (KW > 2) ks[i][c / 2 + 1] = p4_both_high(sc);
+                                for (int x = 0; x < 4 && c + x < KW; ++x) kw[i][c + x] = 0u;
+                            const uint32_t sc = p4_scales(two);
+                            ks[i][c / 2] = p4_both_low(sc);
+                            if (KW > 2) ks[i][c / 2 + 1] = p4_both_high(sc);
+                        }
+                    }
+#pragma unroll
+                    for (int x = 0; x < KW; ++x) {                        // a word of each row: two products
+                        uint32_t r0[4], r1[4];
+                        p4_codes(kw[0][x], r0);
+                        p4_codes(kw[1][x], r1);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t a[4];
+                            a[0] = p4_mul(r0[2 * j], ks[0][x / 2]);
+                            a[1] = p4_mul(r1[2 * j], ks[1][x / 2]);
+                            a[2] = p4_mul(r0[2 * j + 1], ks[0][x / 2]);
+                            a[3] = p4_mul(r1[2 * j + 1], ks[1][x / 2]);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int part = 0; part < PARTS; ++part) w4_mma(sacc[mt][nt], a, bq[nt][part][2 * x + j][0], bq[nt][part][2 * x + j][1]);
+                        }
                     }
                 }
-#pragma unroll
-                for (int x = 0; x < KW; ++x) {                        // a word of each row: two products
-                    uint32_t r0[4], r1[4];
-                    p4_codes(kw[0][x], r0);
-                    p4_codes(kw[1][x], r1);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t a[4];
-                        a[0] = p4_mul(r0[2 * j], ks[0][x / 2]);
-                        a[1] = p4_mul(r1[2 * j], ks[1][x / 2]);
-                        a[2] = p4_mul(r0[2 * j + 1], ks[0][x / 2]);
-                        a[3] = p4_mul(r1[2 * j + 1], ks[1][x / 2]);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int part = 0; part < PARTS; ++part) w4_mma(sacc[mt][nt], a, bq[nt][part][2 * x + j][0], bq[nt][part][2 * x + j][1]);
-                    }
-                }
-            }
             }
             if (!S::WHOLE && at + S::STEP >= PAGE) {                  // K is done with
                 __syncwarp();
@@ -571,12 +580,17 @@ cudaError_t launch_paged4_attention_warp(const Paged4View& c, const PagedBatch& 
         if (c.pv.d == D) return is_bf16 ? run_warp4<D, NT, true, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, true, float>(c, pb, q, out, scale, w, max_rows, st);
         return is_bf16 ? run_warp4<D, NT, false, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<D, NT, false, float>(c, pb, q, out, scale, w, max_rows, st);
     };
+    auto two256 = [&] {
+        return c.pv.d == 256 ? run_warp4<256, 2, true, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st) : run_warp4<256, 2, false, __nv_bfloat16>(c, pb, q, out, scale, w, max_rows, st);
+    };
     auto rows = [&](auto d) {
         return tile_rows <= 8 ? go(d, std::integral_constant<int, 1>{}) : go(d, std::integral_constant<int, 2>{});
     };
     return c.pv.d <= 64    ? rows(std::integral_constant<int, 64>{})
            : c.pv.d <= 128 ? rows(std::integral_constant<int, 128>{})
-                           : go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+                           // 16 rows of 256 spill: they pay for chunks, whose passes over the cache they halve (2 x 512 tokens over 8K, 4 x 4 heads:
+                           // 930 to 724 us), not for 32 rows (80 to 87)
+                           : is_bf16 && tile_rows > 8 ? two256() : go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
 }
 
 }  // namespace tkv

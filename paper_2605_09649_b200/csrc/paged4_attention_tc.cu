@@ -2,15 +2,19 @@
 // shared memory, the missing columns zero).
 //
 // The chunk kernel of the bf16 cache (paged_attention_tc.cu: units of 256 rows in two groups, tiles of two pages, 16 softmax warps, one issuing
-// warp, the order of a worker's stretches) with another producer: one warp copies codes and scales of a page into a ring of three, six
-// warps turn them into fp16 (exact, see paged4.cuh) and store them where TMA would have put a bf16 tile: rows of 128 bytes,
-// 128-byte swizzled, 64-column planes.  Eight neighbouring lanes take four rows and two parts, so the stores meet no bank conflict.
-// Each kind of warp walks the line in code of its own, and they divide the block's registers: a step of a feeding warp is a chain
-// of 300 to 600 cycles, so what feeds a tile in time is their number.  (4 x 512 tokens over 16K: three warps with loads of their own
-// 1683 us, 1180 with the loads of four steps in flight, 1062 with seven warps, 864 with copies by the copy engine.)
+// warp, the order of a worker's stretches) with another producer: one warp has the copy engine bring codes and scales of a page into a
+// ring of three, eight warps turn them into fp16 (exact, see paged4.cuh) and store them where TMA would have put a bf16 tile:
+// rows of 128 bytes, 128-byte swizzled, 64-column planes.  Eight neighbouring lanes take four rows and two parts, so the stores meet
+// no bank conflict.  Each kind of warp has its loop in code of its own, and they divide the block's registers; the place on the line is
+// kept in shared memory, since local memory has almost no cache beside it.
 // Both products are fp16: Q's rows are scaled by powers of two (largest value in 2^10 .. 2^11) and P by 2^4: weights may exceed their
 // reference by 2^11 before a stretch goes round again (fp16 ends at 2^16), and what is lost of a small one is 2^-29 of the reference.
 // V behind a request's last entry, and pages that do not exist, are stored as zeros.
+//
+// What bounds it: the feed.  Beside the products' own reads a way to shared memory and back takes some 200 cycles, and a page of K or V costs a
+// feeding warp several of them in turn.  4 x 512 tokens over 16K, 8 x 4 heads of 128: 622 to 660 us, 0.82 to 0.87 PFLOP/s of useful products (the bf16 cache's
+// kernel, fed by TMA alone: 521).  Steps: three warps with loads of their own 1683 us, the loads of four steps in flight 1180, seven
+// warps 1062, copies by the copy engine 864, the place on the line in shared memory 703, a page ahead in registers 635, barriers asked ahead 627.
 #include "paged4.cuh"
 #include "paged_tc.cuh"
 

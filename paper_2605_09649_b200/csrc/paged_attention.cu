@@ -304,72 +304,72 @@ paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_ro
         __syncthreads();
     }
     for (int w = blockIdx.x, note = 0; w < workers; w += (int)gridDim.x, ++note) {
-    const int4 unit = (int)gridDim.x < workers ? s_unit[note] : wk.shared[w];
-    const int r0 = (int)blockIdx.y * chunk, nr = min(chunk, (unit.z & 4095) - r0), n = unit.z >> 12;
-    if (nr <= 0) continue;
-    int shift = 0;                                                // 2^shift warps per row
-    while ((2 << shift) * nr <= J_WARPS && (J_BATCH << shift) < n) ++shift;
-    const int way = warp & ((1 << shift) - 1), i_lo = n * way >> shift, i_hi = n * (way + 1) >> shift;
-    for (int rr = warp >> shift; rr < nr; rr += J_WARPS >> shift) {       // (several warps per row: one round)
-        const int row = unit.y + r0 + rr, t = by_g.div(row);
-        T* o = out + ((size_t)(unit.x + t) * Hq + (size_t)(unit.w * g + row - t * g)) * d;
+        const int4 unit = (int)gridDim.x < workers ? s_unit[note] : wk.shared[w];
+        const int r0 = (int)blockIdx.y * chunk, nr = min(chunk, (unit.z & 4095) - r0), n = unit.z >> 12;
+        if (nr <= 0) continue;
+        int shift = 0;                                                // 2^shift warps per row
+        while ((2 << shift) * nr <= J_WARPS && (J_BATCH << shift) < n) ++shift;
+        const int way = warp & ((1 << shift) - 1), i_lo = n * way >> shift, i_hi = n * (way + 1) >> shift;
+        for (int rr = warp >> shift; rr < nr; rr += J_WARPS >> shift) {       // (several warps per row: one round)
+            const int row = unit.y + r0 + rr, t = by_g.div(row);
+            T* o = out + ((size_t)(unit.x + t) * Hq + (size_t)(unit.w * g + row - t * g)) * d;
 #pragma unroll 1
-        for (int c0 = lane * 4; c0 < d; c0 += 128) {
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float M = -INFINITY, L = 0.f;
+            for (int c0 = lane * 4; c0 < d; c0 += 128) {
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                float M = -INFINITY, L = 0.f;
 #pragma unroll 1
-            for (int i0 = i_lo; i0 < i_hi; i0 += J_BATCH) {
-                float4 v[J_BATCH];
-                float2 ml[J_BATCH];
-                float top = M;
+                for (int i0 = i_lo; i0 < i_hi; i0 += J_BATCH) {
+                    float4 v[J_BATCH];
+                    float2 ml[J_BATCH];
+                    float top = M;
 #pragma unroll
-                for (int i = 0; i < J_BATCH; ++i) {
-                    // part 0: worker w began the unit and did not end it; the others did not begin it
-                    const size_t p = (size_t)(2 * (w + i0 + i) + (i0 + i == 0)) * unit_rows + r0 + rr;
-                    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    ml[i] = make_float2(-INFINITY, 0.f);
-                    if (i0 + i < i_hi) {
-                        v[i] = *reinterpret_cast<const float4*>(wk.part_o + p * d + c0);
-                        ml[i] = *reinterpret_cast<const float2*>(wk.part_ml + p * 2);
+                    for (int i = 0; i < J_BATCH; ++i) {
+                        // part 0: worker w began the unit and did not end it; the others did not begin it
+                        const size_t p = (size_t)(2 * (w + i0 + i) + (i0 + i == 0)) * unit_rows + r0 + rr;
+                        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        ml[i] = make_float2(-INFINITY, 0.f);
+                        if (i0 + i < i_hi) {
+                            v[i] = *reinterpret_cast<const float4*>(wk.part_o + p * d + c0);
+                            ml[i] = *reinterpret_cast<const float2*>(wk.part_ml + p * 2);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < J_BATCH; ++i) top = fmaxf(top, ml[i].x);
+                    const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
+                    M = top;
+                    L *= keep;
+                    sum.x *= keep; sum.y *= keep; sum.z *= keep; sum.w *= keep;
+#pragma unroll
+                    for (int i = 0; i < J_BATCH; ++i) {
+                        const float e = exp2f(ml[i].x - ref);
+                        L = fmaf(e, ml[i].y, L);
+                        join_add(sum, e, v[i]);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < J_BATCH; ++i) top = fmaxf(top, ml[i].x);
-                const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
-                M = top;
-                L *= keep;
-                sum.x *= keep; sum.y *= keep; sum.z *= keep; sum.w *= keep;
-#pragma unroll
-                for (int i = 0; i < J_BATCH; ++i) {
-                    const float e = exp2f(ml[i].x - ref);
-                    L = fmaf(e, ml[i].y, L);
-                    join_add(sum, e, v[i]);
+                if (shift == 0) join_store(o + c0, sum, join_factor(L));
+                else {
+                    s_sum[warp * (d / 4) + c0 / 4] = sum;
+                    s_ml[warp] = make_float2(M, L);
                 }
             }
-            if (shift == 0) join_store(o + c0, sum, join_factor(L));
-            else {
-                s_sum[warp * (d / 4) + c0 / 4] = sum;
-                s_ml[warp] = make_float2(M, L);
-            }
         }
-    }
-    if (shift == 0) continue;
-    __syncthreads();
-    const int rr = warp >> shift;
-    if (way == 0 && rr < nr) {
-    const int row = unit.y + r0 + rr, t = by_g.div(row);
-    T* o = out + ((size_t)(unit.x + t) * Hq + (size_t)(unit.w * g + row - t * g)) * d;
-    float M = -INFINITY, L = 0.f;
-    for (int x = 0; x < 1 << shift; ++x) M = fmaxf(M, s_ml[warp + x].x);
-    const float ref = M == -INFINITY ? 0.f : M;
-    for (int x = 0; x < 1 << shift; ++x) L = fmaf(exp2f(s_ml[warp + x].x - ref), s_ml[warp + x].y, L);
-    for (int c0 = lane * 4; c0 < d; c0 += 128) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int x = 0; x < 1 << shift; ++x) join_add(sum, exp2f(s_ml[warp + x].x - ref), s_sum[(warp + x) * (d / 4) + c0 / 4]);
-        join_store(o + c0, sum, join_factor(L));
-    }
-    }
-    __syncthreads();                                              // the sums are read
+        if (shift == 0) continue;
+        __syncthreads();
+        const int rr = warp >> shift;
+        if (way == 0 && rr < nr) {
+            const int row = unit.y + r0 + rr, t = by_g.div(row);
+            T* o = out + ((size_t)(unit.x + t) * Hq + (size_t)(unit.w * g + row - t * g)) * d;
+            float M = -INFINITY, L = 0.f;
+            for (int x = 0; x < 1 << shift; ++x) M = fmaxf(M, s_ml[warp + x].x);
+            const float ref = M == -INFINITY ? 0.f : M;
+            for (int x = 0; x < 1 << shift; ++x) L = fmaf(exp2f(s_ml[warp + x].x - ref), s_ml[warp + x].y, L);
+            for (int c0 = lane * 4; c0 < d; c0 += 128) {
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int x = 0; x < 1 << shift; ++x) join_add(sum, exp2f(s_ml[warp + x].x - ref), s_sum[(warp + x) * (d / 4) + c0 / 4]);
+                join_store(o + c0, sum, join_factor(L));
+        }
+        }
+        __syncthreads();                                              // the sums are read
     }
 }
 
