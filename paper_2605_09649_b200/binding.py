@@ -7,6 +7,7 @@ been built, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 from typing import Optional
@@ -726,7 +727,7 @@ def paged_move(arrays, move_src, move_dst, move_count, key_bounds=None, status=N
             pages = shape[0]
         elif shape[0] != pages:
             raise ValueError(f"arrays[{i}]: expected {pages} pages, got {shape[0]}")
-        row = t.stride(1) // PAGE_SIZE * t.element_size()
+        row = math.prod(shape[3:]) * t.element_size()
         bounds = None if key_bounds is None else key_bounds[i]
         if bounds is None:
             rows.append(_pack_rows(t.data_ptr(), 0, shape[1], row, 0, 0))

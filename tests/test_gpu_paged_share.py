@@ -298,6 +298,16 @@ def test_move_skips_what_does_not_exist():
         assert st.item() == binding.E_ARG and torch.equal(b[0, 0, 9], a[1, 0, 6] if count > 0 else a[0, 0, 9])
 
 
+def test_move_takes_rows_by_shape_where_a_dimension_is_one():
+    """One head: its stride says nothing about the rows."""
+    a = torch.randn(4, PAGE, 1, 128, device=DEV).transpose(1, 2)
+    assert a.is_contiguous() and a.stride(1) != PAGE * 128
+    want = a.clone()
+    want[3, :, 9] = a[1, :, 6]
+    binding.paged_move([a], ints([PAGE + 6]), ints([3 * PAGE + 9]), ints([1]))
+    assert torch.equal(a, want)
+
+
 # ---------------------------------------------------------------- together
 
 def test_fork_append_attend_compact_over_a_cache_in_4_bits():
