@@ -20,6 +20,7 @@ trimkv_status check_rows(const ShareArgs& a, int64_t max_tokens, int64_t max_mov
         (max_moves > 0 && (!a.move_src || !a.move_dst)))
         return refuse(TRIMKV_E_ARG, "NULL buffer");
     if (a.table_out == a.table) return refuse(TRIMKV_E_ARG, "table_out must not be the table");
+    if (a.lens_out == a.old_lens || a.lens_out == a.keep_lens || a.lens_out == a.new_lens || a.lens_out == a.source) return refuse(TRIMKV_E_ARG, "lens_out must not be an input");
     const void* all[] = {a.source, a.old_lens, a.keep_lens, a.new_lens, a.table, a.table_out, a.refs, a.refs_out, a.free_pages, a.free_out, a.free_count,
                          a.free_count_out, a.lens_out, a.cu_new, a.slot_map, a.positions, a.move_src, a.move_dst, a.move_count, a.status};
     for (const void* p : all)

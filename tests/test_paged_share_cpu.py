@@ -130,3 +130,12 @@ def test_lists_neither_lose_nor_double_a_page(seed):
         count[p] += 1
     assert got2 == count and sorted(live2) == [p for p in range(n2) if count[p] == 0] and lens2 == [len(k) for k in kept]
     assert not {a // PAGE for a, _ in moves2} & {b // PAGE for _, b in moves2}
+
+
+@pytest.mark.parametrize("name", ["source", "old", "keep", "new"])
+def test_lengths_are_not_written_over_what_is_read(name):
+    refused("trimkv_paged_share", share_args(**{name: OUT}))
+
+
+def test_kept_lengths_are_not_written_over_what_is_read():
+    refused("trimkv_paged_compact", compact_args(lens_in=OUT))
