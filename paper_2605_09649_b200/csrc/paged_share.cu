@@ -12,8 +12,8 @@
 // Compact: a row's pages up to the first dropped entry's stay, the entries kept from there on are listed to be moved to fresh pages, the old pages are
 // released.  Fresh pages are taken before any is released, so no listed source is a destination.
 // Both are bound by latency, five to six cluster barriers and the way to memory between them: a share of 64 beams of 2.3 K entries 18.1 us, of 128
-// samples of 8 prompts of up to 16 K 21.0 us (with three barriers more 20.4 and 24.7); a compact of one request of 4 K entries 15.5 us, of 32 of
-// up to 32 K (1 MB of listed rows) 34.5 us.
+// samples of 8 prompts of up to 16 K 21.0 us (with three barriers more 20.4 and 24.7); a compact of one request of 4 K entries 11.5 us, of 32 of
+// up to 32 K (1 MB of listed rows) 27.5 us.  (A warp to each row's bits, and 32 words at a time in exchanges of registers: 15.9 and 34.8.)
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -347,7 +347,8 @@ paged_share_kernel(ShareArgs a) {
 __global__ void __launch_bounds__(SH_THREADS, 1)
 paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
     extern __shared__ int s_share[];
-    __shared__ int s_w[33], s_bad, s_cnt, s_first, s_last;
+    __shared__ int s_w[33], s_bad, s_cnt[SH_THREADS / 32], s_first[SH_THREADS / 32], s_last[SH_THREADS / 32];
+    __shared__ uint4 s_word[SH_THREADS / 32][32][2];      // see the entries that move
     const int R = a.R, W = a.W;
     const ShareCut cut = share_cut(R, W);
     int* s_len = s_share;                     // [R]: entries kept
@@ -405,29 +406,29 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
             *cluster.map_shared_rank(s_take + r, to) = sh_pages(cnt) - stay;
             *cluster.map_shared_rank(s_move + r, to) = moves ? cnt - stay * PAGE : 0;
         };
-        if (W <= 2048 || R >= SH_WARPS / 8) {                 // by a warp: at most 64 words a lane, or enough rows to fill an eighth of the warps
-            for (int r = gw; r < R; r += SH_WARPS) {
-                const int n = a.old_lens[r];
-                int cnt = 0, first = n, last = -1;
-                look(r, n, lane, 32, cnt, first, last);
-                if (lane < SH_CTAS) tell(r, lane, cnt, first, last);
-            }
-        } else {
-            for (int r = rank; r < R; r += SH_CTAS) {
-                const int n = a.old_lens[r];
-                if (tid == 0) { s_cnt = 0; s_first = n; s_last = -1; }
+        // a CTA takes every 16th row, `team` warps each: as many as there are, or as find four words a lane
+        const int mine = (R - rank + SH_CTAS - 1) / SH_CTAS, most = min(max(mine, 1), SH_THREADS / 32);
+        const int team = min(SH_THREADS / 32 / most, (W + 127) / 128), teams = SH_THREADS / 32 / team, warp = tid >> 5, tm = warp / team;
+        for (int i0 = 0; i0 < mine; i0 += teams) {
+            const int i = i0 + tm, r = rank + i * SH_CTAS;
+            const bool on = tm < teams && i < mine;
+            const int n = on ? a.old_lens[r] : 0;
+            int cnt = 0, first = n, last = -1;
+            if (team > 1) {
+                if (on && warp == tm * team && lane == 0) { s_cnt[tm] = 0; s_first[tm] = n; s_last[tm] = -1; }
                 __syncthreads();
-                int cnt = 0, first = n, last = -1;
-                look(r, n, tid, SH_THREADS, cnt, first, last);
-                if (lane == 0) {
-                    atomicAdd(&s_cnt, cnt);
-                    atomicMin(&s_first, first);
-                    atomicMax(&s_last, last);
+            }
+            if (on) look(r, n, tid - tm * team * 32, team * 32, cnt, first, last);
+            if (team > 1) {
+                if (on && lane == 0) {
+                    atomicAdd(&s_cnt[tm], cnt);
+                    atomicMin(&s_first[tm], first);
+                    atomicMax(&s_last[tm], last);
                 }
                 __syncthreads();
-                if (tid < SH_CTAS) tell(r, tid, s_cnt, s_first, s_last);
-                __syncthreads();
+                if (on && warp == tm * team) { cnt = s_cnt[tm]; first = s_first[tm]; last = s_last[tm]; }
             }
+            if (on && warp == tm * team && lane < SH_CTAS) tell(r, lane, cnt, first, last);
         }
         cluster.sync();
         share_scan(s_take, R, s_w);
@@ -514,42 +515,47 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
     });
     for (int r = gt; r < R; r += GT) a.lens_out[r] = s_len[r];
     if (gt == 0) *a.free_count_out = min(fc - taken + s_back[cut.tasks], a.n_pages);
-    // ---- the entries that move: a warp takes 32 words of a row
-    const int nwarp = (W + 31) / 32;
-    for (long long t = gw; t < (long long)R * nwarp; t += SH_WARPS) {
-        const int r = (int)(t / nwarp), w0 = (int)(t - (long long)r * nwarp) * 32, stay = s_stay[r];
-        const int n = a.old_lens[r], count = s_move[r + 1] - s_move[r];
-        if (count == 0 || w0 + 32 <= stay || w0 >= sh_pages(n)) continue;
+    // ---- the entries that move: a warp takes up to 32 words of a row, a lane describes one, then all lanes list the entries of each in turn
+    const int span = (int)min(32ll, max(2ll, ((long long)R * W + SH_WARPS - 1) / SH_WARPS)), per_row = (W + span - 1) / span;
+    uint4(*desc)[2] = s_word[tid >> 5];
+    for (long long t = gw; t < (long long)R * per_row; t += SH_WARPS) {
+        const int r = (int)(t / per_row), w0 = (int)(t - (long long)r * per_row) * span, stay = s_stay[r];
+        const int n = a.old_lens[r], count = s_move[r + 1] - s_move[r], end = min(w0 + span, sh_pages(n));
+        if (count == 0 || end <= stay || w0 >= end) continue;
         int before = 0;                       // entries kept in the row's earlier words
+#pragma unroll 4
         for (int w = lane; w < w0; w += 32) before += __popcll(kept(r, w, n));
-        before = __reduce_add_sync(0xffffffffu, before);
-        const bool on = w0 + lane < sh_pages(n);
-        const u64 bits = on ? kept(r, w0 + lane, n) : 0ull;
-        const int from = on ? page_at(r, w0 + lane) : -1;
+        const int w = w0 + lane;
+        const u64 bits = w < end ? kept(r, w, n) : 0ull;
         int sum = __popcll(bits);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int u = __shfl_up_sync(0xffffffffu, sum, o);
             if (lane >= o) sum += u;
         }
-        const int total = __shfl_sync(0xffffffffu, sum, 31), base = before + sum - __popcll(bits);
-        const int d0 = before / PAGE, d1 = total ? (before + total - 1) / PAGE : d0;       // destination pages: at most 33
-        const int to_mine = d0 + lane <= d1 ? sh_ld(a.table_out + (size_t)r * W + d0 + lane) : -1;
-        const int to_last = d0 + 32 <= d1 ? sh_ld(a.table_out + (size_t)r * W + d0 + 32) : -1;
-        for (int i = max(0, stay - w0); i < 32; ++i) {
-            const u64 b = __shfl_sync(0xffffffffu, bits, i);
-            const int fp = __shfl_sync(0xffffffffu, from, i), at = __shfl_sync(0xffffffffu, base, i);
+        const int base = __reduce_add_sync(0xffffffffu, before) + sum - __popcll(bits);
+        if (bits && w >= stay) {              // its entries go to one page, or to two
+            const int32_t* to = a.table_out + (size_t)r * W + base / PAGE;
+            const int from = page_at(r, w), to0 = sh_ld(to), to1 = base % PAGE + __popcll(bits) > PAGE ? sh_ld(to + 1) : -1;
+            auto slot = [&](int page, int other) { return page >= 0 && other >= 0 ? page * PAGE : -1; };
+            desc[lane][0] = make_uint4((uint32_t)bits, (uint32_t)(bits >> 32), (uint32_t)(s_move[r] + base - stay * PAGE), (uint32_t)(base % PAGE));
+            desc[lane][1] = make_uint4((uint32_t)slot(from, to0), (uint32_t)slot(to0, from), (uint32_t)slot(from, to1), (uint32_t)slot(to1, from));
+        }
+        __syncwarp();
+        for (unsigned todo = __ballot_sync(0xffffffffu, bits && w >= stay); todo; todo &= todo - 1) {
+            const uint4 d0 = desc[__ffs(todo) - 1][0], d1 = desc[__ffs(todo) - 1][1];
+            const unsigned below = (1u << lane) - 1u;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int bit = half * 32 + lane, rank_in = at + __popcll(b & ((1ull << bit) - 1ull));
-                const int tp = __shfl_sync(0xffffffffu, to_mine, (rank_in / PAGE - d0) & 31), to = rank_in / PAGE - d0 == 32 ? to_last : tp;
-                if ((b >> bit) & 1ull) {
-                    const int m = s_move[r] + rank_in - stay * PAGE;
-                    a.move_src[m] = fp >= 0 && to >= 0 ? fp * PAGE + bit : -1;
-                    a.move_dst[m] = fp >= 0 && to >= 0 ? to * PAGE + rank_in % PAGE : -1;
+                const unsigned word = half ? d0.y : d0.x;
+                const int k = __popc(word & below) + (half ? __popc(d0.x) : 0), at = (int)d0.w + k, m = (int)d0.z + k;
+                if ((word >> lane) & 1u) {    // (-1 with any row is -1)
+                    a.move_src[m] = (int)(at < PAGE ? d1.x : d1.z) | (half * 32 + lane);
+                    a.move_dst[m] = (int)(at < PAGE ? d1.y : d1.w) | (at % PAGE);
                 }
             }
         }
+        __syncwarp();
     }
     share_none_moved(a, moves, gt, GT);
     if (wrong) latch_error(a.status, TRIMKV_E_ARG);

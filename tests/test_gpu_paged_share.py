@@ -210,6 +210,20 @@ def test_compact_equals_the_lists(groups, per_group, longest, seed, width, with_
         assert got["moves"] == len(mv) and got["src"] == [a for a, _ in mv] + [-1] * (moves - len(mv)) and got["dst"] == [b for _, b in mv] + [-1] * (moves - len(mv))
 
 
+@pytest.mark.parametrize("rows,longest,width,seed", [(16, 130 * 64, 140, 0), (17, 2000, 260, 1), (40, 260 * 64, 300, 2), (150, 900, 130, 3), (513, 100, 129, 4)])
+def test_compact_of_rows_by_several_warps(rows, longest, width, seed):
+    rng = random.Random(seed)
+    s = Rows(rng, rows, 1, longest, spare=0, shared=False, holders=False, width=width)
+    kept = [random_kept(rng, n) for n in s.lens]
+    room = sum(pages(n) for n in s.lens)
+    stack, n_pages = s.stack + [s.n_pages + i for i in range(room)], s.n_pages + room
+    after, _, live, lens, mv, memory = compact(s.lens, kept, s.table, None, stack, n_pages, width)
+    got, st = run_compact(s.lens, kept, s.table, None, stack, n_pages, width, len(mv))
+    assert st == 0 and got["lens"] == lens and got["count"] == len(live) and got["free"][:len(memory)] == memory
+    assert got["table"] == [row + [-5] * (width - len(row)) for row in after]
+    assert got["moves"] == len(mv) and got["src"] == [a for a, _ in mv] and got["dst"] == [b for _, b in mv]
+
+
 def test_compact_refused_as_a_whole():
     table, lens, kept = [[3, 1, 5], [0, -9, -9]], [150, 20], [list(range(2, 150)), [3, 4]]
     refs, stack = [1, 1, 0, 1, 0, 1, 0, 0], [2, 4, 6, 7]
