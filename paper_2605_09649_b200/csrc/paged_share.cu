@@ -11,9 +11,10 @@
 // on the stack; fresh pages come from its top.
 // Compact: a row's pages up to the first dropped entry's stay, the entries kept from there on are listed to be moved to fresh pages, the old pages are
 // released.  Fresh pages are taken before any is released, so no listed source is a destination.
-// Both are bound by latency, five to six cluster barriers and the way to memory between them: a share of 64 beams of 2.3 K entries 18.1 us, of 128
-// samples of 8 prompts of up to 16 K 21.0 us (with three barriers more 20.4 and 24.7); a compact of one request of 4 K entries 11.5 us, of 32 of
-// up to 32 K (1 MB of listed rows) 27.5 us.  (A warp to each row's bits, and 32 words at a time in exchanges of registers: 15.9 and 34.8.)
+// Both are bound by latency, five to six cluster barriers and the way to memory between them: a share of 64 beams of 2.3 K entries 13.2 us, of 128
+// samples of 8 prompts of up to 16 K 16.0 us (losses and gains apart, rows and tokens by the same warps as stretches, lists summed one by
+// one: 17.9 and 21.0; three barriers more: 20.4 and 24.7); a compact of one request of 4 K entries 10.7 us, of 32 of up to 32 K (1 MB of
+// listed rows) 26.7 us.  (A warp to each row's bits, and 32 words at a time in exchanges of registers: 15.9 and 34.8.)
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -28,7 +29,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int SH_CTAS = 16, SH_THREADS = 1024, SH_WARPS = SH_CTAS * SH_THREADS / 32;
-constexpr int SH_TASKS = 1024;                // stretches of rows, if there are fewer rows than that
+constexpr int SH_TASKS = 512;                 // stretches of rows, if there are fewer rows than that: one for each warp
 constexpr int SH_FIRST = 2 * PAGED_MAX_REQ;   // see the dispute over pages that nobody holds
 
 __device__ __forceinline__ int sh_pages(int n) { return (int)(((unsigned)n + PAGE - 1u) / PAGE); }
@@ -47,10 +48,15 @@ __host__ __device__ inline ShareCut share_cut(int R, int W) {
     return c;
 }
 
-// v[0 .. n] = sums before each of v[0 .. n - 1]; the block calls it.  Sums fit 32 bits.  w: 33 ints of shared memory.
-__device__ __forceinline__ void share_scan(int* v, int n, int* w) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (n + SH_THREADS - 1) / SH_THREADS;
-    const int i0 = min(n, (int)threadIdx.x * per), i1 = min(n, i0 + per);
+// Up to four lists at once, a quarter of the block each: v[0 .. n] = sums before each of v[0 .. n - 1]; the block calls it.  Sums fit 32
+// bits.  w: 32 ints of shared memory.
+struct ShareList { int* v; int n; };          // null: none
+__device__ __forceinline__ void share_scan(int* w, ShareList a, ShareList b = {nullptr, 0}, ShareList c = {nullptr, 0}, ShareList d = {nullptr, 0}) {
+    constexpr int QUARTER = SH_THREADS / 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = threadIdx.x / QUARTER, id = threadIdx.x % QUARTER;
+    const ShareList mine_of = q == 0 ? a : q == 1 ? b : q == 2 ? c : d;
+    int* v = mine_of.v;
+    const int n = v ? mine_of.n : 0, per = (n + QUARTER - 1) / QUARTER, i0 = min(n, id * per), i1 = min(n, i0 + per);
     int mine = 0;
     for (int i = i0; i < i1; ++i) mine += v[i];
     int incl = mine;
@@ -59,22 +65,12 @@ __device__ __forceinline__ void share_scan(int* v, int n, int* w) {
         const int u = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += u;
     }
-    __syncthreads();
     if (lane == 31) w[warp] = incl;
     __syncthreads();
-    if (warp == 0) {
-        int x = w[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += u;
-        }
-        w[lane] = x;
-    }
-    __syncthreads();
-    int run = (warp ? w[warp - 1] : 0) + incl - mine;
+    int run = incl - mine;                    // and the quarter's warps before this one
+    for (int k = q * (QUARTER / 32); k < warp; ++k) run += w[k];
     for (int i = i0; i < i1; ++i) { const int x = v[i]; v[i] = run; run += x; }
-    if (threadIdx.x == 0) v[n] = w[31];
+    if (id == QUARTER - 1 && v) v[n] = run;
     __syncthreads();
 }
 
@@ -124,7 +120,7 @@ __device__ __forceinline__ ShareRow share_row(const ShareArgs& a, int r) {
 __global__ void __launch_bounds__(SH_THREADS, 1)
 paged_share_kernel(ShareArgs a) {
     extern __shared__ int s_share[];
-    __shared__ int s_w[33], s_bad;
+    __shared__ int s_w[32], s_bad;
     __shared__ long long s_total;
     const int R = a.R, W = a.W;
     const ShareCut cut = share_cut(R, W);
@@ -135,6 +131,7 @@ paged_share_kernel(ShareArgs a) {
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, rank = (int)cluster.block_rank();
     const int gt = rank * SH_THREADS + tid, GT = SH_CTAS * SH_THREADS, gw = rank * (SH_THREADS / 32) + (tid >> 5);
+    const int gt_row = GT - 1 - gt, gt_move = gt ^ (GT / 2);      // rows and tokens, and moves, go to warps without stretches first
     if (tid == 0) { s_bad = 0; s_total = 0; }
     grid_dependency_wait();
     grid_dependents_may_launch();
@@ -174,25 +171,17 @@ paged_share_kernel(ShareArgs a) {
             f(t, r, max(j0, from / 32 * 32), from, min(to, j0 + cut.seg));
         }
     };
-    auto each_gained = [&](auto&& f) {        // holds of a page of another row
-        for (int t = gw; t < cut.tasks; t += SH_WARPS) {
-            const int r = t / cut.nseg, j0 = (t - r * cut.nseg) * cut.seg;
+    auto add = [&](int sign) {                // holds let go of, and holds of a page of another row
+        each_dropped([&](int t, int r, int, int from, int to) {
             const ShareRow s = share_row(a, r);
-            if (s.source < 0 || s.source == r) continue;
-            for (int j = j0 + lane; j < min(s.stay, j0 + cut.seg); j += 32) f(page_at(s.source, j));
-        }
-    };
-    auto add = [&](int sign) {
-        each_dropped([&](int, int r, int j0, int from, int to) {
-            for (int j = j0 + lane; j < to; j += 32) {
-                const int p = j >= from ? page_at(r, j) : -1;
+            const int j0 = (t - r * cut.nseg) * cut.seg, gains = s.source < 0 || s.source == r ? 0 : min(s.stay, j0 + cut.seg);
+            for (int j = j0 + lane; j < max(to, gains); j += 32) {
+                const bool loss = j >= from && j < to, gain = j < gains;
+                const int p = loss ? page_at(r, j) : -1, u = gain ? page_at(s.source, j) : -1;
                 if (p >= 0) atomicAdd(a.refs_out + p, -sign);
-                else wrong |= j >= from;
+                if (u >= 0) atomicAdd(a.refs_out + u, sign);
+                wrong |= (loss && p < 0) || (gain && u < 0);
             }
-        });
-        each_gained([&](int p) {
-            if (p >= 0) atomicAdd(a.refs_out + p, sign);
-            else wrong = true;
         });
     };
     if (!bad) {
@@ -201,7 +190,7 @@ paged_share_kernel(ShareArgs a) {
         cluster.sync();
         // ---- counts are now of the holders that do not write.  Pages that nobody holds are in dispute: among the rows that will write one, and
         // if there is none among those that let go of it; the lowest of either gets it, and writers go first by SH_FIRST.
-        for (int r = gt; r < R; r += GT) {
+        for (int r = gt_row; r < R; r += GT) {
             const ShareRow s = share_row(a, r);
             const int p = s.writes ? page_at(s.source, s.keep / PAGE) : -1;
             if (p >= 0 && sh_ld(a.refs_out + p) <= 0) atomicMin(a.refs_out + p, r - R - SH_FIRST);
@@ -214,7 +203,7 @@ paged_share_kernel(ShareArgs a) {
         });
         __threadfence();
         cluster.sync();
-        for (int r = gt; r < R; r += GT) {
+        for (int r = gt_row; r < R; r += GT) {
             const ShareRow s = share_row(a, r);
             const int p = s.writes ? page_at(s.source, s.keep / PAGE) : -1;
             if (p < 0) { wrong |= s.writes; continue; }
@@ -236,10 +225,7 @@ paged_share_kernel(ShareArgs a) {
         });
         __threadfence();
         cluster.sync();
-        share_scan(s_tok, R, s_w);
-        share_scan(s_take, R, s_w);
-        share_scan(s_move, R, s_w);
-        share_scan(s_back, cut.tasks, s_w);
+        share_scan(s_w, {s_tok, R}, {s_take, R}, {s_move, R}, {s_back, cut.tasks});
         if (fc + s_back[cut.tasks] > a.n_pages || s_move[R] > a.max_moves) bad = TRIMKV_E_ARG;
         else if (fc + s_back[cut.tasks] < s_take[R]) bad = TRIMKV_E_NOMEM;
         if (bad) {                            // the counts as they were
@@ -316,12 +302,12 @@ paged_share_kernel(ShareArgs a) {
             a.table_out[(size_t)r * W + j] = p;
         }
     }
-    for (int r = gt; r <= R; r += GT) {
+    for (int r = gt_row; r <= R; r += GT) {
         a.cu_new[r] = s_tok[r];
         if (r < R) a.lens_out[r] = a.new_lens[r];
     }
     if (gt == 0) *a.free_count_out = fc + back - taken;
-    for (int i = gt; i < a.max_tokens; i += GT) {
+    for (int i = gt_row; i < a.max_tokens; i += GT) {
         int slot = -1, pos = -1;
         if (i < tokens) {
             const int r = share_find(s_tok, R, i);
@@ -332,7 +318,7 @@ paged_share_kernel(ShareArgs a) {
         a.slot_map[i] = slot;
         if (a.positions) a.positions[i] = pos;
     }
-    for (int i = gt; i < moves; i += GT) {
+    for (int i = gt_move; i < moves; i += GT) {
         const int r = share_find(s_move, R, i), e = i - s_move[r], page = a.keep_lens[r] / PAGE;
         const int from = page_at(a.source[r], page), to = new_page(r, page);
         a.move_src[i] = to >= 0 ? from * PAGE + e : -1;
@@ -347,7 +333,7 @@ paged_share_kernel(ShareArgs a) {
 __global__ void __launch_bounds__(SH_THREADS, 1)
 paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
     extern __shared__ int s_share[];
-    __shared__ int s_w[33], s_bad, s_cnt[SH_THREADS / 32], s_first[SH_THREADS / 32], s_last[SH_THREADS / 32];
+    __shared__ int s_w[32], s_bad, s_cnt[SH_THREADS / 32], s_first[SH_THREADS / 32], s_last[SH_THREADS / 32];
     __shared__ uint4 s_word[SH_THREADS / 32][32][2];      // see the entries that move
     const int R = a.R, W = a.W;
     const ShareCut cut = share_cut(R, W);
@@ -431,8 +417,7 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
             if (on && warp == tm * team && lane < SH_CTAS) tell(r, lane, cnt, first, last);
         }
         cluster.sync();
-        share_scan(s_take, R, s_w);
-        share_scan(s_move, R, s_w);
+        share_scan(s_w, {s_take, R}, {s_move, R});
         if (s_move[R] > a.max_moves) bad = TRIMKV_E_ARG;
         else if (s_take[R] > fc) bad = TRIMKV_E_NOMEM;
     }
@@ -498,7 +483,7 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
         if (lane < SH_CTAS) *cluster.map_shared_rank(s_back + t, lane) = n;
     });
     cluster.sync();
-    share_scan(s_back, cut.tasks, s_w);
+    share_scan(s_w, {s_back, cut.tasks});
     each_dropped([&](int t, int r, int j0, int from, int to) {
         int at = fc - taken + s_back[t];
         for (int j = j0; j < to; j += 32) {
