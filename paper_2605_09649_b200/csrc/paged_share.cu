@@ -13,8 +13,8 @@
 // released.  Fresh pages are taken before any is released, so no listed source is a destination.
 // Both are bound by latency, five to six cluster barriers and the way to memory between them: a share of 64 beams of 2.3 K entries 13.2 us, of 128
 // samples of 8 prompts of up to 16 K 16.0 us (losses and gains apart, rows and tokens by the same warps as stretches, lists summed one by
-// one: 17.9 and 21.0; three barriers more: 20.4 and 24.7); a compact of one request of 4 K entries 10.7 us, of 32 of up to 32 K (1 MB of
-// listed rows) 26.7 us.  (A warp to each row's bits, and 32 words at a time in exchanges of registers: 15.9 and 34.8.)
+// one: 17.9 and 21.0; three barriers more: 20.4 and 24.7); a compact of one request of 4 K entries 10.1 us, of 32 of up to 32 K (1 MB of
+// listed rows) 22.0 us.  (A warp to each row's bits, and 32 words at a time in exchanges of registers: 15.9 and 34.8.)
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -30,6 +30,9 @@ namespace cg = cooperative_groups;
 
 constexpr int SH_CTAS = 16, SH_THREADS = 1024, SH_WARPS = SH_CTAS * SH_THREADS / 32;
 constexpr int SH_TASKS = 512;                 // stretches of rows, if there are fewer rows than that: one for each warp
+// Kept entries of a word of 64 up to which lanes look for theirs: 32 rows of 32 K entries, an eighth kept, 21.4 us that way and 26.7 with a
+// word after another; a quarter 25.6 and 26.8; 0.4 30.5 and 26.8.
+constexpr int SH_SPARSE = 16;
 constexpr int SH_FIRST = 2 * PAGED_MAX_REQ;   // see the dispute over pages that nobody holds
 
 __device__ __forceinline__ int sh_pages(int n) { return (int)(((unsigned)n + PAGE - 1u) / PAGE); }
@@ -500,7 +503,8 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
     });
     for (int r = gt; r < R; r += GT) a.lens_out[r] = s_len[r];
     if (gt == 0) *a.free_count_out = min(fc - taken + s_back[cut.tasks], a.n_pages);
-    // ---- the entries that move: a warp takes up to 32 words of a row, a lane describes one, then all lanes list the entries of each in turn
+    // ---- the entries that move: a warp takes up to 32 words of a row, a lane describes one; then a lane looks for the word and bit of an
+    // entry, or, of many, all lanes list those of a word after another
     const int span = (int)min(32ll, max(2ll, ((long long)R * W + SH_WARPS - 1) / SH_WARPS)), per_row = (W + span - 1) / span;
     uint4(*desc)[2] = s_word[tid >> 5];
     for (long long t = gw; t < (long long)R * per_row; t += SH_WARPS) {
@@ -527,7 +531,34 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
             desc[lane][1] = make_uint4((uint32_t)slot(from, to0), (uint32_t)slot(to0, from), (uint32_t)slot(from, to1), (uint32_t)slot(to1, from));
         }
         __syncwarp();
-        for (unsigned todo = __ballot_sync(0xffffffffu, bits && w >= stay); todo; todo &= todo - 1) {
+        const unsigned words = __ballot_sync(0xffffffffu, bits && w >= stay);
+        const int base0 = words ? __shfl_sync(0xffffffffu, base, __ffs(words) - 1) : 0, listed = words ? __shfl_sync(0xffffffffu, base + __popcll(bits), 31) - base0 : 0;
+        if (listed <= SH_SPARSE * __popc(words)) {            // few entries a word: a lane finds the word and the bit of its entry
+            const int at = w >= stay ? base - base0 : 0;      // entries listed of the words before (words before `stay` come first)
+            for (int i0 = 0; i0 < listed; i0 += 32) {
+                const int i = i0 + lane;
+                int k = 0;
+#pragma unroll
+                for (int step = 16; step; step >>= 1)         // the last word with at <= i
+                    if (__shfl_sync(0xffffffffu, at, k + step) <= i) k += step;
+                int nth = i - __shfl_sync(0xffffffffu, at, k);
+                if (i < listed) {
+                    const uint4 d0 = desc[k][0], d1 = desc[k][1];
+                    const int to = (int)d0.w + nth, m = (int)d0.z + nth, low = __popc(d0.x);
+                    unsigned rest = nth < low ? d0.x : d0.y;
+                    int bit = nth < low ? 0 : 32;
+                    nth -= nth < low ? 0 : low;
+#pragma unroll
+                    for (int half = 16; half; half >>= 1) {   // the nth bit of a word
+                        const int c = __popc(rest & ((1u << half) - 1u));
+                        if (nth >= c) { nth -= c; bit += half; rest >>= half; }
+                    }
+                    a.move_src[m] = (int)(to < PAGE ? d1.x : d1.z) | bit;
+                    a.move_dst[m] = (int)(to < PAGE ? d1.y : d1.w) | (to % PAGE);
+                }
+            }
+        }
+        for (unsigned todo = listed <= SH_SPARSE * __popc(words) ? 0u : words; todo; todo &= todo - 1) {
             const uint4 d0 = desc[__ffs(todo) - 1][0], d1 = desc[__ffs(todo) - 1][1];
             const unsigned below = (1u << lane) - 1u;
 #pragma unroll
