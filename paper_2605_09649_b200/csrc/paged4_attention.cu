@@ -22,7 +22,7 @@
 // The reference of a row's weights lags its maximum by up to 2^8, and weights are 2^7 times their value: at most 2^15, and what
 // fp16 cannot hold is below 2^-32 of the row's largest weight.
 // Entries behind the request's last one: any code is finite, so only their scales are put to zero (for V; K's products are masked).
-// Every wait is bounded: on expiry the warp latches TRIMKV_E_TIMEOUT, drains its copies and returns.
+// Every wait is bounded: on expiry a warp latches TRIMKV_E_TIMEOUT and returns, those that bring tiles once their copies have landed.
 #include "async_copy.cuh"
 #include "mma_sync.cuh"
 #include "paged4.cuh"

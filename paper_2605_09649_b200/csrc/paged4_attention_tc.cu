@@ -437,202 +437,202 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
             if (!stretch_done()) break;
         }
     } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(T_REST_REGS));      // (one instruction for the four warps of a group)
-    if (warp < T_SOFT + T_FEED) {
-        // ---- K and V
-        // Lanes: eight neighbours store four rows and two parts, all 32 banks.
-        using F = Feed<D>;
-        const int fw = warp - T_SOFT, part = (lane & 1) | (F::PARTS == 4 ? lane >> 4 << 1 : 0), lrow = (lane >> 1) % F::ROWS;
-        const int code_row = d / 2, scale_row = d / 16;
-        const bool on = part * 32 < d;                                // not a missing column
-        const uint32_t out0 = base + (fw % F::STEPS * F::ROWS + lrow) * 128 + ((part % 2 * 4) ^ (lrow & 7)) * 16;
-        const uint32_t code0 = base + S::OFF_RAW + (fw % F::STEPS * F::ROWS + lrow) * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + (fw % F::STEPS * F::ROWS + lrow) * scale_row + (on ? part * 2 : 0);
-        const int row0 = fw % F::STEPS * F::ROWS;                     // this warp's step of a page; (heads of 64: of every other page)
-        unsigned slot = 0, phase = 0;                                 // place in the ring of the page that is read next
-        bool ok = true;
-        while (walk->more) {
-            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
-            uint32_t word[4], scale;
-            int real;
-            auto take = [&](uint32_t (&wd)[4], uint32_t& sc, int& n) {
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3]) : "r"(code0 + slot * F::RAW));
-                asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(sc) : "r"(scale0 + slot * F::RAW));
-                n = s_real[slot];
-            };
-            if (npage > 0) {
-                ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
-                take(word, scale, real);
-            }
-            uint32_t raw_ready = 0u, stage_ready = 0u;                // of the page behind, of the part behind
-            unsigned c = ct;
-            int kv = 0, h = 0, left = npage;                          // page h of K or V of tile c; pages of the tile and those behind it
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(T_REST_REGS));      // (one instruction for the four warps of a group)
+        if (warp < T_SOFT + T_FEED) {
+            // ---- K and V
+            // Lanes: eight neighbours store four rows and two parts, all 32 banks.
+            using F = Feed<D>;
+            const int fw = warp - T_SOFT, part = (lane & 1) | (F::PARTS == 4 ? lane >> 4 << 1 : 0), lrow = (lane >> 1) % F::ROWS;
+            const int code_row = d / 2, scale_row = d / 16;
+            const bool on = part * 32 < d;                                // not a missing column
+            const uint32_t out0 = base + (fw % F::STEPS * F::ROWS + lrow) * 128 + ((part % 2 * 4) ^ (lrow & 7)) * 16;
+            const uint32_t code0 = base + S::OFF_RAW + (fw % F::STEPS * F::ROWS + lrow) * code_row + (on ? part * 16 : 0), scale0 = base + S::OFF_RAW + PAGE * code_row + (fw % F::STEPS * F::ROWS + lrow) * scale_row + (on ? part * 2 : 0);
+            const int row0 = fw % F::STEPS * F::ROWS;                     // this warp's step of a page; (heads of 64: of every other page)
+            unsigned slot = 0, phase = 0;                                 // place in the ring of the page that is read next
+            bool ok = true;
+            while (walk->more) {
+                const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+                uint32_t word[4], scale;
+                int real;
+                auto take = [&](uint32_t (&wd)[4], uint32_t& sc, int& n) {
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3]) : "r"(code0 + slot * F::RAW));
+                    asm volatile("{\n\t.reg .b16 t;\n\tld.shared.b16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(sc) : "r"(scale0 + slot * F::RAW));
+                    n = s_real[slot];
+                };
+                if (npage > 0) {
+                    ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
+                    take(word, scale, real);
+                }
+                uint32_t raw_ready = 0u, stage_ready = 0u;                // of the page behind, of the part behind
+                unsigned c = ct;
+                int kv = 0, h = 0, left = npage;                          // page h of K or V of tile c; pages of the tile and those behind it
 #pragma unroll 1
-            for (int n = 0; n < 2 * npage && ok; ++n) {
-                __syncwarp();
-                if (lane == 0) a_bar_arrive(raw_empty + 8 * slot);    // in registers
-                if (++slot == T_RAW) { slot = 0; phase ^= 1; }
-                uint32_t next[4] = {0u, 0u, 0u, 0u}, next_scale = 0u;
-                int next_real = 0;
-                if (n + 1 < 2 * npage) {
-                    if (!__all_sync(0xffffffffu, raw_ready != 0u)) ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
-                    take(next, next_scale, next_real);
-                }
-                raw_ready = t_test(raw_full + (slot + 1 == T_RAW ? 0u : 8 * (slot + 1)), slot + 1 == T_RAW ? phase ^ 1u : phase);
-                const unsigned s = c % T_STAGES;
-                if (h == 0 && c >= T_STAGES && ok && !__all_sync(0xffffffffu, stage_ready != 0u))
-                    ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
-                if (!ok) break;
-                const bool last_page = h == 1 || left == 1;           // of the tile
-                if (last_page) {
-                    const unsigned nc = c + kv;                       // the next part: V of this tile, or K of the next
-                    stage_ready = t_test((kv ? k_empty : v_empty) + 8 * (nc % T_STAGES), ((nc / T_STAGES) - 1) & 1);
-                }
-                if (F::STEPS == T_FEED || fw / F::STEPS == h) {
-                    // K: a plane holds the rows of both pages; V: planes of a page, then of the next
-                    const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
-                    const uint32_t sc = p4_scales(on && row0 + lrow < real ? scale : 0u), lo = p4_both_low(sc), hi = p4_both_high(sc);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {                     // (chunk x lies 16 x further, but for the swizzle)
-                        uint32_t r4[4];
-                        p4_codes(word[x], r4);
-                        const uint32_t by = x < 2 ? lo : hi;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out ^ (x * 16)), "r"(p4_mul(r4[0], by)), "r"(p4_mul(r4[1], by)),
-                                     "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
-                    }
-                }
-                if (last_page) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                for (int n = 0; n < 2 * npage && ok; ++n) {
                     __syncwarp();
-                    if (lane == 0) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
-                    h = 0;
-                    if (kv) { ++c; left -= 2; }
-                    kv ^= 1;
-                } else {
-                    h = 1;
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) word[x] = next[x];
-                scale = next_scale;
-                real = next_real;
-            }
-            if (!ok && lane == 0) *s_fail = 1;
-            ct += (unsigned)ntile;
-            if (!stretch_done()) break;
-        }
-    } else if (warp == T_SOFT + T_FEED) {
-        // ---- copies: lane l holds page l of the current run of 32
-        unsigned rc = 0;
-        bool ok = true;
-        while (walk->more) {
-            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
-            int phys = -1;
-#pragma unroll 1
-            for (int i = 0; i < ntile && ok; ++i) {
-                if ((i & 15) == 0) phys = 2 * i + lane < npage ? paged_physical(pb, pv, it.r, it.p0 + 2 * i + lane) : -1;
-                const int two = 2 * i + 1 < npage, page0 = __shfl_sync(0xffffffffu, phys, (2 * i) & 31), page1 = __shfl_sync(0xffffffffu, phys, (2 * i + 1) & 31);
-                if (lane == 0) {                                      // a page that does not exist: every row masks it
-                    const unsigned c = ct + i;
-                    s_e0[c % T_E0 * 2] = page0 < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
-                    s_e0[c % T_E0 * 2 + 1] = !two ? -1 : page1 < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
-                }
-#pragma unroll 1
-                for (int n = 0; n < 2 * (1 + two) && ok; ++n, ++rc) {
-                    const int kv = n > two, p = two && (n & 1) ? page1 : page0;
-                    const unsigned slot = rc % T_RAW;
-                    if (rc >= T_RAW) ok = __all_sync(0xffffffffu, a_bar_wait(raw_empty + 8 * slot, ((rc / T_RAW) - 1) & 1));
+                    if (lane == 0) a_bar_arrive(raw_empty + 8 * slot);    // in registers
+                    if (++slot == T_RAW) { slot = 0; phase ^= 1; }
+                    uint32_t next[4] = {0u, 0u, 0u, 0u}, next_scale = 0u;
+                    int next_real = 0;
+                    if (n + 1 < 2 * npage) {
+                        if (!__all_sync(0xffffffffu, raw_ready != 0u)) ok = __all_sync(0xffffffffu, a_bar_wait(raw_full + 8 * slot, phase));
+                        take(next, next_scale, next_real);
+                    }
+                    raw_ready = t_test(raw_full + (slot + 1 == T_RAW ? 0u : 8 * (slot + 1)), slot + 1 == T_RAW ? phase ^ 1u : phase);
+                    const unsigned s = c % T_STAGES;
+                    if (h == 0 && c >= T_STAGES && ok && !__all_sync(0xffffffffu, stage_ready != 0u))
+                        ok = __all_sync(0xffffffffu, a_bar_wait((kv ? v_empty : k_empty) + 8 * s, ((c / T_STAGES) - 1) & 1));
                     if (!ok) break;
-                    if (lane == 0) {
-                        // none of a page that does not exist; of V those up to the last entry (their weights are 0, but scales may be NaN)
-                        s_real[slot] = p < 0 ? 0 : kv ? it.q.len - (it.p0 + 2 * i + (two ? n & 1 : 0)) * PAGE : PAGE;
-                        if (p < 0) {
-                            a_bar_arrive(raw_full + 8 * slot);
-                        } else {
-                            const size_t row = ((size_t)p * pv.H + it.h) * PAGE;
-                            const uint32_t dst = base + S::OFF_RAW + slot * Feed<D>::RAW;
-                            a_bar_expect_tx(raw_full + 8 * slot, PAGE * (d / 2 + d / 16));
-                            t_bulk(dst, (kv ? cache.codes[1] : cache.codes[0]) + row * (d / 2), PAGE * (d / 2), raw_full + 8 * slot);
-                            t_bulk(dst + PAGE * (d / 2), (kv ? cache.scales[1] : cache.scales[0]) + row * (d / 16), PAGE * (d / 16), raw_full + 8 * slot);
+                    const bool last_page = h == 1 || left == 1;           // of the tile
+                    if (last_page) {
+                        const unsigned nc = c + kv;                       // the next part: V of this tile, or K of the next
+                        stage_ready = t_test((kv ? k_empty : v_empty) + 8 * (nc % T_STAGES), ((nc / T_STAGES) - 1) & 1);
+                    }
+                    if (F::STEPS == T_FEED || fw / F::STEPS == h) {
+                        // K: a plane holds the rows of both pages; V: planes of a page, then of the next
+                        const uint32_t out = out0 + s * S::TILE + (kv ? S::OFF_V + (h * S::PLANES + part / 2) * T_PLANE : part / 2 * S::KPLANE + h * T_PLANE);
+                        const uint32_t sc = p4_scales(on && row0 + lrow < real ? scale : 0u), lo = p4_both_low(sc), hi = p4_both_high(sc);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {                     // (chunk x lies 16 x further, but for the swizzle)
+                            uint32_t r4[4];
+                            p4_codes(word[x], r4);
+                            const uint32_t by = x < 2 ? lo : hi;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out ^ (x * 16)), "r"(p4_mul(r4[0], by)), "r"(p4_mul(r4[1], by)),
+                                         "r"(p4_mul(r4[2], by)), "r"(p4_mul(r4[3], by)) : "memory");
                         }
                     }
-                    __syncwarp();
-                }
-            }
-            if (!ok && lane == 0) *s_fail = 1;
-            ct += (unsigned)ntile;
-            if (!stretch_done()) {                                     // copies in flight land before the block leaves (bounded)
-                for (unsigned k = rc > T_RAW ? rc - T_RAW : 0; k < rc; ++k) a_bar_wait(raw_full + 8 * (k % T_RAW), (k / T_RAW) & 1);
-                break;
-            }
-        }
-    } else if (warp > T_SOFT + T_FEED + 1) {
-        while (walk->more && stretch_done()) {}
-    } else {
-        // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue order), for one group
-        // after the other
-        while (walk->more) {
-            const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
-            const bool both = min(T_UNIT, it.q.n * g - it.u * T_UNIT) > T_ROWS;
-            if (ntile > 0) {
-                a_fence_before();
-                asm volatile("bar.sync 1, %0;" ::"n"((T_SOFT + 1) * 32) : "memory");      // Q is there
-                a_fence_after();
-                bool ok = true;
-                const uint32_t leader = t_elect();
-                const uint32_t ub = t_uniform(base), ut = t_uniform(tmem), uct = t_uniform(ct), uct1 = t_uniform(ct1);
-                const int un = (int)t_uniform((uint32_t)ntile), upages = (int)t_uniform((uint32_t)npage), uboth = (int)t_uniform(both ? 1u : 0u);
-                auto issue_s = [&](int i, int gq) {
-                    const uint32_t c = uct + i, s = c % T_STAGES;
-                    ok = __all_sync(0xffffffffu, a_bar_wait(k_full + 8 * s, (c / T_STAGES) & 1));
-                    if (!ok) return;
-                    a_fence_after();
-                    const uint32_t k_lo = t_desc_lo(ub, 16) + s * (S::TILE >> 4), q_lo = t_desc_lo(ub + S::OFF_Q, 16) + gq * (S::PLANES * T_QPLANE >> 4);
-                    const uint32_t idesc = 2 * i + 1 < upages ? S::IDESC_S2 : S::IDESC_S1;
-#pragma unroll
-                    for (int p = 0; p < S::PLANES; ++p)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)                   // 16 channels per instruction, 32 bytes along the row
-                            t_umma(leader, ut + 128 * gq, q_lo + (p * T_QPLANE + j * 32) / 16, k_lo + (p * S::KPLANE + j * 32) / 16, idesc, (p | j) != 0);
-                    t_commit(leader, bars + 64 + 8 * gq);             // S ready (and everything issued before: O up to the last tile)
-                    if (gq == 1 || !uboth) t_commit(leader, k_empty + 8 * s);
-                };
-                auto wait_v = [&](int i) {
-                    const uint32_t c = uct + i;
-                    ok = __all_sync(0xffffffffu, a_bar_wait(v_full + 8 * (c % T_STAGES), (c / T_STAGES) & 1));
-                };
-                auto issue_pv = [&](int i, int gq) {
-                    const uint32_t c = uct + i, s = c % T_STAGES;
-                    const uint32_t v_lo = t_desc_lo(ub + S::OFF_V, T_PLANE) + s * (S::TILE >> 4);     // the next 64 channels: one plane further
-                    const uint32_t d_o = ut + 256 + 128 * gq, a_p = ut + 128 * gq;
-                    ok = __all_sync(0xffffffffu, a_bar_wait(p_ready0 + 8 * gq, ((gq ? uct1 : uct) + i) & 1));
-                    if (!ok) return;
-                    a_fence_after();
-#pragma unroll
-                    for (int j = 0; j < PAGE / 16; ++j)               // 16 entries per instruction: P +8 columns, V +2 row groups
-                        t_umma_ts(leader, d_o, a_p + j * 8, v_lo + j * 128, S::IDESC_PV, i != 0 || j != 0);
-                    if (2 * i + 1 < upages) {
-#pragma unroll
-                        for (int j = 0; j < PAGE / 16; ++j)
-                            t_umma_ts(leader, d_o, a_p + 64 + j * 8, v_lo + S::PLANES * T_PLANE / 16 + j * 128, S::IDESC_PV, 1u);
+                    if (last_page) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) a_bar_arrive((kv ? v_full : k_full) + 8 * s);
+                        h = 0;
+                        if (kv) { ++c; left -= 2; }
+                        kv ^= 1;
+                    } else {
+                        h = 1;
                     }
-                    if (gq == 1 || !uboth) t_commit(leader, v_empty + 8 * s);
-                    if (i + 1 == un) t_commit(leader, done0 + 8 * gq);
-                };
-                issue_s(0, 0);
-                if (ok && uboth) issue_s(0, 1);
-                for (int i = 0; i < un && ok; ++i) {
-                    wait_v(i);
-                    if (ok) issue_pv(i, 0);
-                    if (ok && i + 1 < un) issue_s(i + 1, 0);
-                    if (ok && uboth) issue_pv(i, 1);
-                    if (ok && uboth && i + 1 < un) issue_s(i + 1, 1);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) word[x] = next[x];
+                    scale = next_scale;
+                    real = next_real;
                 }
                 if (!ok && lane == 0) *s_fail = 1;
+                ct += (unsigned)ntile;
+                if (!stretch_done()) break;
             }
-            ct += (unsigned)ntile;
-            if (both) ct1 += (unsigned)ntile;
-            if (!stretch_done()) break;
+        } else if (warp == T_SOFT + T_FEED) {
+            // ---- copies: lane l holds page l of the current run of 32
+            unsigned rc = 0;
+            bool ok = true;
+            while (walk->more) {
+                const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+                int phys = -1;
+#pragma unroll 1
+                for (int i = 0; i < ntile && ok; ++i) {
+                    if ((i & 15) == 0) phys = 2 * i + lane < npage ? paged_physical(pb, pv, it.r, it.p0 + 2 * i + lane) : -1;
+                    const int two = 2 * i + 1 < npage, page0 = __shfl_sync(0xffffffffu, phys, (2 * i) & 31), page1 = __shfl_sync(0xffffffffu, phys, (2 * i + 1) & 31);
+                    if (lane == 0) {                                      // a page that does not exist: every row masks it
+                        const unsigned c = ct + i;
+                        s_e0[c % T_E0 * 2] = page0 < 0 ? T_NO_PAGE : (it.p0 + 2 * i) * PAGE;
+                        s_e0[c % T_E0 * 2 + 1] = !two ? -1 : page1 < 0 ? T_NO_PAGE : (it.p0 + 2 * i + 1) * PAGE;
+                    }
+#pragma unroll 1
+                    for (int n = 0; n < 2 * (1 + two) && ok; ++n, ++rc) {
+                        const int kv = n > two, p = two && (n & 1) ? page1 : page0;
+                        const unsigned slot = rc % T_RAW;
+                        if (rc >= T_RAW) ok = __all_sync(0xffffffffu, a_bar_wait(raw_empty + 8 * slot, ((rc / T_RAW) - 1) & 1));
+                        if (!ok) break;
+                        if (lane == 0) {
+                            // none of a page that does not exist; of V those up to the last entry (their weights are 0, but scales may be NaN)
+                            s_real[slot] = p < 0 ? 0 : kv ? it.q.len - (it.p0 + 2 * i + (two ? n & 1 : 0)) * PAGE : PAGE;
+                            if (p < 0) {
+                                a_bar_arrive(raw_full + 8 * slot);
+                            } else {
+                                const size_t row = ((size_t)p * pv.H + it.h) * PAGE;
+                                const uint32_t dst = base + S::OFF_RAW + slot * Feed<D>::RAW;
+                                a_bar_expect_tx(raw_full + 8 * slot, PAGE * (d / 2 + d / 16));
+                                t_bulk(dst, (kv ? cache.codes[1] : cache.codes[0]) + row * (d / 2), PAGE * (d / 2), raw_full + 8 * slot);
+                                t_bulk(dst + PAGE * (d / 2), (kv ? cache.scales[1] : cache.scales[0]) + row * (d / 16), PAGE * (d / 16), raw_full + 8 * slot);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (!ok && lane == 0) *s_fail = 1;
+                ct += (unsigned)ntile;
+                if (!stretch_done()) {                                     // copies in flight land before the block leaves (bounded)
+                    for (unsigned k = rc > T_RAW ? rc - T_RAW : 0; k < rc; ++k) a_bar_wait(raw_full + 8 * (k % T_RAW), (k / T_RAW) & 1);
+                    break;
+                }
+            }
+        } else if (warp > T_SOFT + T_FEED + 1) {
+            while (walk->more && stretch_done()) {}
+        } else {
+            // ---- MMA issuer: P V of a tile, then S of the next, which overwrites that tile's P (the pipe runs in issue order), for one group
+            // after the other
+            while (walk->more) {
+                const int npage = it.p1 - it.p0, ntile = (npage + 1) / 2;
+                const bool both = min(T_UNIT, it.q.n * g - it.u * T_UNIT) > T_ROWS;
+                if (ntile > 0) {
+                    a_fence_before();
+                    asm volatile("bar.sync 1, %0;" ::"n"((T_SOFT + 1) * 32) : "memory");      // Q is there
+                    a_fence_after();
+                    bool ok = true;
+                    const uint32_t leader = t_elect();
+                    const uint32_t ub = t_uniform(base), ut = t_uniform(tmem), uct = t_uniform(ct), uct1 = t_uniform(ct1);
+                    const int un = (int)t_uniform((uint32_t)ntile), upages = (int)t_uniform((uint32_t)npage), uboth = (int)t_uniform(both ? 1u : 0u);
+                    auto issue_s = [&](int i, int gq) {
+                        const uint32_t c = uct + i, s = c % T_STAGES;
+                        ok = __all_sync(0xffffffffu, a_bar_wait(k_full + 8 * s, (c / T_STAGES) & 1));
+                        if (!ok) return;
+                        a_fence_after();
+                        const uint32_t k_lo = t_desc_lo(ub, 16) + s * (S::TILE >> 4), q_lo = t_desc_lo(ub + S::OFF_Q, 16) + gq * (S::PLANES * T_QPLANE >> 4);
+                        const uint32_t idesc = 2 * i + 1 < upages ? S::IDESC_S2 : S::IDESC_S1;
+#pragma unroll
+                        for (int p = 0; p < S::PLANES; ++p)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)                   // 16 channels per instruction, 32 bytes along the row
+                                t_umma(leader, ut + 128 * gq, q_lo + (p * T_QPLANE + j * 32) / 16, k_lo + (p * S::KPLANE + j * 32) / 16, idesc, (p | j) != 0);
+                        t_commit(leader, bars + 64 + 8 * gq);             // S ready (and everything issued before: O up to the last tile)
+                        if (gq == 1 || !uboth) t_commit(leader, k_empty + 8 * s);
+                    };
+                    auto wait_v = [&](int i) {
+                        const uint32_t c = uct + i;
+                        ok = __all_sync(0xffffffffu, a_bar_wait(v_full + 8 * (c % T_STAGES), (c / T_STAGES) & 1));
+                    };
+                    auto issue_pv = [&](int i, int gq) {
+                        const uint32_t c = uct + i, s = c % T_STAGES;
+                        const uint32_t v_lo = t_desc_lo(ub + S::OFF_V, T_PLANE) + s * (S::TILE >> 4);     // the next 64 channels: one plane further
+                        const uint32_t d_o = ut + 256 + 128 * gq, a_p = ut + 128 * gq;
+                        ok = __all_sync(0xffffffffu, a_bar_wait(p_ready0 + 8 * gq, ((gq ? uct1 : uct) + i) & 1));
+                        if (!ok) return;
+                        a_fence_after();
+#pragma unroll
+                        for (int j = 0; j < PAGE / 16; ++j)               // 16 entries per instruction: P +8 columns, V +2 row groups
+                            t_umma_ts(leader, d_o, a_p + j * 8, v_lo + j * 128, S::IDESC_PV, i != 0 || j != 0);
+                        if (2 * i + 1 < upages) {
+#pragma unroll
+                            for (int j = 0; j < PAGE / 16; ++j)
+                                t_umma_ts(leader, d_o, a_p + 64 + j * 8, v_lo + S::PLANES * T_PLANE / 16 + j * 128, S::IDESC_PV, 1u);
+                        }
+                        if (gq == 1 || !uboth) t_commit(leader, v_empty + 8 * s);
+                        if (i + 1 == un) t_commit(leader, done0 + 8 * gq);
+                    };
+                    issue_s(0, 0);
+                    if (ok && uboth) issue_s(0, 1);
+                    for (int i = 0; i < un && ok; ++i) {
+                        wait_v(i);
+                        if (ok) issue_pv(i, 0);
+                        if (ok && i + 1 < un) issue_s(i + 1, 0);
+                        if (ok && uboth) issue_pv(i, 1);
+                        if (ok && uboth && i + 1 < un) issue_s(i + 1, 1);
+                    }
+                    if (!ok && lane == 0) *s_fail = 1;
+                }
+                ct += (unsigned)ntile;
+                if (both) ct1 += (unsigned)ntile;
+                if (!stretch_done()) break;
+            }
         }
-    }
     }
     __syncthreads();
     if (warp == T_SOFT + T_FEED + 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(T_TMEM_COLS) : "memory");

@@ -298,6 +298,17 @@ def test_move_makes_bounds_of_completed_pages(dtype, d):
             assert torch.equal(torch.nan_to_num(b[p, :, 1].float(), nan=9e9), torch.nan_to_num(hi, nan=9e9))
 
 
+def test_move_makes_bounds_of_arrays_with_different_heads():
+    gen, n_pages = torch.Generator().manual_seed(1), 6
+    arrays = [torch.randn(n_pages, h, PAGE, 64, generator=gen).to(DEV, torch.bfloat16) for h in (1, 9, 4, 16)]
+    bounds = [torch.full((n_pages, a.shape[1], 2, 64), 7.0, dtype=a.dtype, device=DEV) for a in arrays]
+    src, dst = list(range(100)), [3 * PAGE + e for e in range(20, 120)]
+    binding.paged_move(arrays, ints(src), ints(dst), ints([100]), key_bounds=bounds)
+    for a, b in zip(arrays, bounds):
+        assert torch.equal(b[3, :, 0], a[3].amin(1)) and torch.equal(b[3, :, 1], a[3].amax(1))
+        assert (b[[0, 1, 2, 4, 5]] == 7).all()
+
+
 def test_move_skips_what_does_not_exist():
     a = torch.arange(2 * PAGE, dtype=torch.float32, device=DEV).view(2, 1, PAGE, 1).expand(2, 1, PAGE, 4).contiguous()
     for pair in ((-1, 5), (5, -1), (128, 3), (3, 128), (-7, 2), (1 << 30, 4)):
