@@ -288,23 +288,23 @@ __device__ __forceinline__ void join_add(float4& s, float e, const float4& v) {
 }
 __device__ __forceinline__ float join_factor(float l) { return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l); }      // rows that see nothing: 0; NaN stays
 
-template <typename T>
+// FEWER: blocks than workers, J_NOTES of them for each at most.
+template <typename T, bool FEWER>
 __global__ void __launch_bounds__(J_THREADS, 2)
 paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_rows, int chunk, int workers) {
     extern __shared__ __align__(16) float4 s_sum[];               // [J_WARPS][d / 4]
     __shared__ float2 s_ml[J_WARPS];
-    __shared__ int4 s_unit[J_NOTES];
+    __shared__ int4 s_unit[FEWER ? J_NOTES : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = (int)by_g.d;
     grid_dependents_may_launch();
     grid_dependency_wait();
-    // the units of workers blockIdx.x, + gridDim.x, ...: all notes at once where there is more than one
-    if ((int)gridDim.x < workers) {
+    if constexpr (FEWER) {                                        // the notes of workers blockIdx.x, + gridDim.x, ..., all at once
         const int at = (int)(blockIdx.x + threadIdx.x * gridDim.x);
         if (threadIdx.x < J_NOTES) s_unit[threadIdx.x] = at < workers ? wk.shared[at] : make_int4(0, 0, 0, 0);
         __syncthreads();
     }
-    for (int w = blockIdx.x, note = 0; w < workers; w += (int)gridDim.x, ++note) {
-        const int4 unit = (int)gridDim.x < workers ? s_unit[note] : wk.shared[w];
+    for (int w = blockIdx.x, note = 0; FEWER ? w < workers : note == 0; w += (int)gridDim.x, ++note) {
+        const int4 unit = FEWER ? s_unit[note] : wk.shared[w];
         const int r0 = (int)blockIdx.y * chunk, nr = min(chunk, (unit.z & 4095) - r0), n = unit.z >> 12;
         if (nr <= 0) continue;
         int shift = 0;                                                // 2^shift warps per row
@@ -367,9 +367,9 @@ paged_join_kernel(T* out, PagedWork wk, FastDiv by_g, int Hq, int d, int unit_ro
                 float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int x = 0; x < 1 << shift; ++x) join_add(sum, exp2f(s_ml[warp + x].x - ref), s_sum[(warp + x) * (d / 4) + c0 / 4]);
                 join_store(o + c0, sum, join_factor(L));
+            }
         }
-        }
-        __syncthreads();                                              // the sums are read
+        if constexpr (FEWER) __syncthreads();                         // the sums are read
     }
 }
 
@@ -399,7 +399,8 @@ cudaError_t launch_paged_join(const PagedView& pv, const PagedBatch& pb, int is_
     const dim3 grid((unsigned)std::min(blocks, workers), (unsigned)((unit_rows + chunk - 1) / chunk)), block(J_THREADS);
     const size_t smem = (size_t)J_WARPS * pv.d * sizeof(float);
     auto go = [&](auto kernel, auto* o) { return paged_launch(kernel, grid, block, smem, 1, true, st, o, w, pb.by_g, pb.Hq, pv.d, unit_rows, chunk, workers); };
-    return is_bf16 ? go(paged_join_kernel<__nv_bfloat16>, (__nv_bfloat16*)out) : go(paged_join_kernel<float>, (float*)out);
+    if (blocks < workers) return is_bf16 ? go(paged_join_kernel<__nv_bfloat16, true>, (__nv_bfloat16*)out) : go(paged_join_kernel<float, true>, (float*)out);
+    return is_bf16 ? go(paged_join_kernel<__nv_bfloat16, false>, (__nv_bfloat16*)out) : go(paged_join_kernel<float, false>, (float*)out);
 }
 
 cudaError_t launch_paged_attention_f32(const PagedView& pv, const PagedBatch& pb, const void* q, void* out, float scale, const PagedWork& w,
