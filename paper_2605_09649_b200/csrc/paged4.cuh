@@ -7,6 +7,8 @@
 // in bf16), and the tensor cores see the cache's values without a rounding; one instruction turns a byte of codes into two fp16.
 #pragma once
 
+#include <float.h>
+
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -27,6 +29,12 @@ __device__ __forceinline__ int p4_shift(const Paged4View& c, int kv, int h) {
     return c.shift[kv] ? max(-P4_MAX_SHIFT, min(P4_MAX_SHIFT, c.shift[kv][h])) : 0;
 }
 __device__ __forceinline__ float p4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // 2^e, -126 <= e <= 127
+
+// From a row's products to logits in log2 units, scale_log2 2^e.  A scale, a shift and a row's own power of two may together leave fp32's
+// range; a factor of 0 or infinity would make masked (-inf) or zero products NaN.  At the lower end logits are below 2^-95 either way.
+__device__ __forceinline__ float p4_to_log2(float scale_log2, int e) {
+    return fminf(fmaxf(scale_log2 * p4_pow2(max(-126, min(127, e))), FLT_MIN), FLT_MAX);
+}
 
 // Four bytes of codes as eight fp16: r[i] = {low half of byte i, high half}.
 __device__ __forceinline__ void p4_codes(uint32_t b, uint32_t (&r)[4]) {

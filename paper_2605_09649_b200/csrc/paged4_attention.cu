@@ -300,7 +300,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                         }
                     }
                 }
-                const float back = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));      // of row gq; this thread's columns are 2 tq, + 1
+                const float back = p4_to_log2(scale_log2, ksh - up);      // of row gq; this thread's columns are 2 tq, + 1
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     to_log2[nt][c] = __shfl_sync(0xffffffffu, back, (2 * tq + c) * 4);

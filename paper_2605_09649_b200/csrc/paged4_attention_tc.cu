@@ -242,7 +242,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
 #pragma unroll
                         for (int e = 0; e < 4; ++e) w4[e] = p4_f16x2(__uint_as_float(vw[e] << 16) * f, __uint_as_float(vw[e] & 0xffff0000u) * f);
                         *reinterpret_cast<uint4*>(gen + S::OFF_Q + (grp * S::PLANES + (c >> 3)) * T_QPLANE + rq * 128 + (((c & 7) ^ (rq & 7)) << 4)) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
-                        if (c == 0) s_up[grp * T_ROWS + rq] = scale_log2 * p4_pow2(max(-126, min(127, ksh - up)));
+                        if (c == 0) s_up[grp * T_ROWS + rq] = p4_to_log2(scale_log2, ksh - up);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // Q, before the async proxy uses it
