@@ -22,7 +22,8 @@
 // The reference of a row's weights lags its maximum by up to 2^8, and weights are 2^7 times their value: at most 2^15, and what
 // fp16 cannot hold is below 2^-32 of the row's largest weight.
 // Entries behind the request's last one: any code is finite, so only their scales are put to zero (for V; K's products are masked).
-// Every wait is bounded: on expiry a warp latches TRIMKV_E_TIMEOUT and returns, those that bring tiles once their copies have landed.
+// Every wait is bounded and, where a whole warp computes, voted on: on expiry the warp leaves as a whole, latches TRIMKV_E_TIMEOUT and returns;
+// those that bring tiles once their copies have landed.
 #include "async_copy.cuh"
 #include "mma_sync.cuh"
 #include "paged4.cuh"
@@ -81,6 +82,11 @@ __device__ __forceinline__ bool w4_test(uint64_t* bar, uint32_t parity) {      /
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
     return ok != 0;
+}
+// For the whole warp, whose lanes agree on the answer.  (The first try mostly does, and needs no loop with lanes that leave it apart.)
+__device__ __forceinline__ bool w4_wait(uint64_t* bar, uint32_t parity) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity));
 }
 // Entry that row r (0 .. 15) of a product's 16 stands for: neighbours and every second row fall on both halves of the 32 banks.
 __device__ __forceinline__ int w4_entry(int r) { return r ^ ((r >> 1) & 1); }
@@ -316,7 +322,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
             all_lo = pb.window > 0 ? max(all_end - pb.window, 0) : 0;
         }
 
-        ok = mbar_wait_bounded(full + stage, parity);
+        ok = w4_wait(full + stage, parity);
         if (!ok) break;
         const unsigned k_stage = stage;
         if (!S::WHOLE && ++stage == S::STAGES) { stage = 0; parity ^= 1u; }
@@ -380,7 +386,7 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
                 if (lane == 0) mbar_arrive(empty + k_stage);
             }
             if (!v_here) {
-                if (!S::WHOLE) ok = mbar_wait_bounded(full + stage, parity);
+                if (!S::WHOLE) ok = w4_wait(full + stage, parity);
                 if (!ok) break;
                 v_here = true;
                 const int held = len - e0;                            // entries of the page, if it is not full

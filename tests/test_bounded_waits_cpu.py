@@ -1,0 +1,38 @@
+"""Waits with a limit, by reading the sources (a wait that runs out in earnest has no place in a test): where a whole warp goes on together --
+shuffles, votes and products of the warp follow -- its lanes must agree on whether the wait ran out, or those that go on wait for those
+that left."""
+import os
+import re
+
+import pytest
+
+from test_dependent_launch_cpu import CSRC
+
+WAIT = re.compile(r"\b(?:mbar_wait_bounded|mbar_try_wait|a_bar_wait)\(")
+
+
+def without_comments(text):
+    return re.sub(r"/\*.*?\*/", "", re.sub(r"//[^\n]*", "", text), flags=re.S)
+
+
+def unvoted(text):
+    """Waits whose answer is used without the warp's vote.  (A wait that is a statement of its own waits for copies in flight.)"""
+    found = []
+    for m in WAIT.finditer(text):
+        before = text[:m.start()].rstrip()
+        if not before.endswith("__all_sync(0xffffffffu,") and before[-1] not in ";{})":
+            found.append(text[m.start() - 30:m.end() + 30])
+    return found
+
+
+def test_the_reader_tells_the_cases_apart():
+    text = without_comments("""{ ok = __all_sync(0xffffffffu, a_bar_wait(b, p)); /* ok = a_bar_wait(b, p); */ if (c) ok = mbar_wait_bounded(b, p); // a_bar_wait(
+                               if (!a_bar_wait(b, 0)) return; for (k = 0; k < n; ++k) mbar_wait_bounded(b + k, k & 1u); }""")
+    assert len(unvoted(text)) == 2
+
+
+@pytest.mark.parametrize("name", ["paged4_attention.cu", "paged4_attention_tc.cu", "paged_tc.cuh"])
+def test_waits_of_the_4_bit_kernels_are_voted_on(name):
+    text = without_comments(open(os.path.join(CSRC, name)).read())
+    assert WAIT.search(text)
+    assert unvoted(text) == []
