@@ -229,10 +229,9 @@ paged4_attn_warp_kernel(Paged4View cache, PagedBatch pb, const T* q, T* out, flo
             else if (++idle > W4_IDLE_LIMIT) break;
             else __nanosleep(W4_NAP);
         }
-        if (!done) {                                                  // a warp gave up: the copies in flight land before this one leaves (bounded)
-            latch_error(pb.status, TRIMKV_E_TIMEOUT);
-            for (unsigned k = part > S::STAGES ? part - S::STAGES : 0; k < part; ++k) mbar_wait_bounded(full + c * S::STAGES + k % S::STAGES, (k / S::STAGES) & 1u);
-        }
+        if (!done) latch_error(pb.status, TRIMKV_E_TIMEOUT);          // a warp gave up
+        // The copies in flight land before this warp leaves (bounded), also where all were issued: the warp that wants them may have given up.
+        for (unsigned k = part > S::STAGES ? part - S::STAGES : 0; k < part; ++k) mbar_wait_bounded(full + c * S::STAGES + k % S::STAGES, (k / S::STAGES) & 1u);
         return;
     }
 

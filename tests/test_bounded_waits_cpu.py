@@ -36,3 +36,17 @@ def test_waits_of_the_4_bit_kernels_are_voted_on(name):
     text = without_comments(open(os.path.join(CSRC, name)).read())
     assert WAIT.search(text)
     assert unvoted(text) == []
+
+
+def test_copies_of_the_4_bit_decode_kernel_land_before_their_warp_leaves():
+    """The warps that bring tiles wait for the last copies of every ring, whether or not there was more to bring: a warp that gave up leaves the
+    copies it asked for in flight, and shared memory goes to the next block."""
+    text = without_comments(open(os.path.join(CSRC, "paged4_attention.cu")).read())
+    block = text[text.index("if (warp >= S::WARPS) {"):text.index("const unsigned char* ring")]
+    depth, waits = 0, []
+    for i, ch in enumerate(block):
+        depth += {"{": 1, "}": -1}.get(ch, 0)
+        if block.startswith("mbar_wait_bounded(", i):
+            waits.append((depth, block[block.rfind(";", 0, block.rfind("for (", 0, i)) + 1:i]))
+    assert len(waits) == 1 and waits[0][0] == 1               # of the block itself, under no condition
+    assert "if" not in waits[0][1] and "for (unsigned k" in waits[0][1]
