@@ -145,15 +145,20 @@ inline bool paged_always_whole(const PagedBatch& pb, int H, int tile_rows, int w
     return pb.R <= PAGED_GROUPS && units * H <= workers && longest <= join_steps;
 }
 
-// Shared memory of the table: PAGED_GROUPS groups of consecutive requests.
-struct PagedTableMem {
+// Shared memory of the table: PAGED_GROUPS groups of consecutive requests, and what each of the block's warps sums up over them.  (A kernel
+// has room for its own warps, no more: with 200 bytes too many the fp32 kernel takes 23.8 us instead of 23.3 for a prompt of 512.)
+struct PagedTableLine {
     long long grp[PAGED_GROUPS + 1];          // steps before a group
     int4 req[PAGED_GROUPS];                   // {row0, n, len, units} of each request where a group is one request
-    long long steps[28], units[28];           // of the requests of each warp (the 4-bit tensor-core kernel has 28)
-    int longest[28], whole;
 };
+template <int WARPS>
+struct PagedTableMemOf : PagedTableLine {
+    long long steps[WARPS], units[WARPS];     // of the requests of each warp
+    int longest[WARPS], whole;
+};
+using PagedTableMem = PagedTableMemOf<18>;    // (the tensor-core kernel has 18)
 struct PagedTable {
-    PagedTableMem* mem;
+    PagedTableLine* mem;
     int gsz, ngrp, heads;
     int tile_rows, min_rows, max_rows;
     long long total;
@@ -178,9 +183,9 @@ __device__ __forceinline__ bool paged_choose_whole(long long steps, long long un
 }
 
 // Every thread of the block calls it.
-template <int SEL>
+template <int SEL, int WARPS>
 __device__ __forceinline__ void paged_build_table(PagedTable& t, const PagedBatch& pb, int heads, int tile_rows, int min_rows,
-                                                  int max_rows, int max_workers, int min_share, int join_steps, PagedTableMem* mem) {
+                                                  int max_rows, int max_workers, int min_share, int join_steps, PagedTableMemOf<WARPS>* mem) {
     t.mem = mem;
     t.heads = heads;
     t.tile_rows = tile_rows; t.min_rows = min_rows; t.max_rows = max_rows;

@@ -30,7 +30,7 @@ constexpr int T_SOFT = 16, T_FEED = 8;                                // softmax
 constexpr int T_THREADS = (T_SOFT + T_FEED + 4) * 32;
 constexpr int T_REGS = 72, T_SOFT_REGS = 96, T_REST_REGS = 40;        // a thread's registers at the launch, and as the warps divide them
 static_assert(T_SOFT * T_SOFT_REGS + (T_THREADS / 32 - T_SOFT) * T_REST_REGS <= T_THREADS / 32 * T_REGS, "no more than the block was launched with");
-static_assert(T_THREADS / 32 <= 28, "the table of requests has room for that many warps");
+using TableMem = PagedTableMemOf<T_THREADS / 32>;
 static_assert(T_SOFT % 4 == 0 && T_THREADS / 32 % 4 == 0, "registers are divided by groups of four warps");
 constexpr int T_TMEM_COLS = 512;      // group g: S of page h at columns 128 g + 64 h (P over its first 32); O at 256 + 128 g
 constexpr int T_POLY_EVERY = 3;
@@ -82,7 +82,7 @@ struct Tc4Shape {
     static constexpr int OFF_E0 = OFF_BAR + 256;
     static constexpr int OFF_MX = OFF_E0 + T_E0 * 8;                  // [tile parity; 2: sums][group][page of the tile][row]: maxima so far
     static constexpr int OFF_TAB = OFF_MX + 3 * 2 * 2 * T_ROWS * 4;
-    static constexpr int OFF_UP = (OFF_TAB + (int)sizeof(PagedTableMem) + 15) & ~15;      // from a row's S to log2 units
+    static constexpr int OFF_UP = (OFF_TAB + (int)sizeof(TableMem) + 15) & ~15;      // from a row's S to log2 units
     static constexpr int OFF_WALK = OFF_UP + T_UNIT * 4;
     static constexpr int OFF_RAW = (OFF_WALK + (int)sizeof(Walk) + 15) & ~15;
     static constexpr int SMEM = OFF_RAW + T_RAW * Feed<D>::RAW + 1024;      // 1024: alignment slack
@@ -144,7 +144,7 @@ paged4_attn_tc_kernel(Paged4View cache, PagedBatch pb, const __nv_bfloat16* q, _
     volatile int* s_redo = reinterpret_cast<volatile int*>(gen + S::OFF_BAR + 252);
     volatile int* s_e0 = reinterpret_cast<volatile int*>(gen + S::OFF_E0);
     float* s_mx = reinterpret_cast<float*>(gen + S::OFF_MX);
-    PagedTableMem* table_mem = reinterpret_cast<PagedTableMem*>(gen + S::OFF_TAB);
+    TableMem* table_mem = reinterpret_cast<TableMem*>(gen + S::OFF_TAB);
     float* s_up = reinterpret_cast<float*>(gen + S::OFF_UP);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = pb.g, d = pv.d;
 

@@ -1,8 +1,10 @@
 """The caller-owned paged cache in 4 bits on the GPU where its number formats end."""
+import random
+
 import pytest
 import torch
 
-from test_gpu_paged4 import ints, run
+from test_gpu_paged4 import check, ints, run
 from util_paged import queries
 from util_paged4 import Cache4, attention, values
 
@@ -42,3 +44,15 @@ def test_a_scale_too_large_for_the_shift(dtype, new):
     c.k = torch.zeros_like(c.k)
     q, cu = queries([new, new], H * g, d, dtype, seed=31)
     judge(c, q * 2.0 ** 67, cu, lens, 100.0)
+
+
+# ---------------------------------------------------------------- many requests
+
+@pytest.mark.parametrize("requests", [33, 480, 481, 1100])
+def test_chunks_of_more_requests_than_the_table_has_groups(requests):
+    """The chunk kernel has more warps than the table of requests has sums: chunks, single tokens and idle requests from one to three a group."""
+    rng = random.Random(requests)
+    lens = [rng.choice([1, 40, 64, 70, 129]) for _ in range(requests)]
+    new = [min(n, rng.choice([0, 1, 1, 33, 64])) for n in lens]
+    lens[-1], new[-1] = 200, 100
+    check(lens, new, 1, 2, 64, torch.bfloat16, seed=36)
