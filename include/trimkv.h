@@ -485,8 +485,11 @@ TRIMKV_API trimkv_status trimkv_paged4_read(const trimkv_paged4_cache* cache, in
 TRIMKV_API size_t trimkv_paged4_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim);
 
 /* trimkv_paged_attention over a cache in 4 bits: the same arguments and rules, q and out in dtype.  The values of the cache enter the
- * products exactly.  q is below 2^70.  bf16: weights are rounded to fp16 for their product with v (off by 2^-11 at most; weights below
- * 2^-21 of a row's largest by 2^-32 of that).  fp32: q and the weights in two fp16 parts each, 2^-22 relative.
+ * products exactly.  q is below 2^70; of a row's values, what is below 2^-35 of the largest is lost.  For their product with v
+ * weights are rounded.  bf16: by 2^-11 of the weight at most, or by 2^-29 of the row's largest weight where that is more, and a third of them may come
+ * from a polynomial off by 7.5e-5.  (Only 2^-32 of the largest, and no polynomial, where max_new -- or n_tokens, if it is 0 -- times the
+ * query heads of a KV head is at most 32, and for head sizes above 128.)  fp32: q and the weights in two fp16 parts each, 2^-22 of each, or 2^-32
+ * of the row's largest weight where that is more.
  * The tables, lengths and slots are trimkv_paged_plan's or trimkv_paged_share's.  There is no selection of pages (no key_bounds) here. */
 TRIMKV_API trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t dtype, int32_t n_req, int64_t n_tokens, int32_t max_new,
                                       int32_t q_heads, const void* q, int64_t q_stride, const int32_t* cu_new, const int32_t* lens,

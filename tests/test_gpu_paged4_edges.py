@@ -1,10 +1,11 @@
 """The caller-owned paged cache in 4 bits on the GPU where its number formats end."""
+import math
 import random
 
 import pytest
 import torch
 
-from test_gpu_paged4 import check, ints, run
+from test_gpu_paged4 import DEV, check, ints, run
 from util_paged import queries
 from util_paged4 import Cache4, attention, values
 
@@ -44,6 +45,36 @@ def test_a_scale_too_large_for_the_shift(dtype, new):
     c.k = torch.zeros_like(c.k)
     q, cu = queries([new, new], H * g, d, dtype, seed=31)
     judge(c, q * 2.0 ** 67, cu, lens, 100.0)
+
+
+# ---------------------------------------------------------------- small weights
+
+def far_below(c, log2_weight):
+    """Keys and values of a cache of one head: the first entry outweighs every other by 2^-log2_weight and has the value 0, the others' is 1."""
+    kc, ks, _, vc, vs, _ = c.arrays
+    kc.zero_(), vc.fill_(0x22), ks.fill_(56), vs.fill_(56)    # code 2: 1; byte 56: 1
+    first = int(c.table[0, 0])
+    kc[first, 0, 0, 0], vc[first, 0, 0] = 7, 0                # channel 0: 6
+    c.k, c.v = values(*c.arrays[:3]), values(*c.arrays[3:])
+    return log2_weight * math.log(2.0) / 6
+
+
+@pytest.mark.parametrize("dtype,new,bits,tail", [(torch.bfloat16, 1, 30.41, 32), (torch.float32, 1, 30.41, 32), (torch.bfloat16, 40, 27.41, 29), (torch.bfloat16, 40, 20.0, 29),
+                                                 (torch.bfloat16, 40, 24.3, 29), (torch.bfloat16, 40, 28.6, 29), (torch.bfloat16, 1, 24.3, 32)])
+def test_weights_that_fp16_rounds_coarsely(dtype, new, bits, tail):
+    """Many entries whose weights are 2^-20 to 2^-31 of the largest, halfway between two fp16 numbers among them.  Each is off by 2^-tail of the
+    largest at most: weights are 2^7 times their value, in the chunk kernel 2^4, and fp16's last step is 2^-24, half of it an error."""
+    H, g, d, n = 1, 4, 64, 256 if new > 1 else 1000           # (so few that no second worker shares the request, with a reference of its own)
+    c = Cache4([n], H, d, seed=32, shift=0)
+    scale = far_below(c, bits)
+    q = torch.zeros(new, H * g, d, dtype=dtype, device=DEV)
+    q[:, :, 0] = 1.0
+    cu = [0, new]
+    out, st = run(c, q, cu, new, scale=scale)
+    assert st == 0
+    want, bound = attention(c.k, c.v, q, cu, [n], c.table, scale)
+    bound = bound + n * (2.0 ** -tail - 2.0 ** -32)           # (every value is 1; `attention` counts 2^-32 for each entry)
+    assert (want > 0).all() and ((out.double().cpu() - want).abs() <= bound).all(), ((out.double().cpu() - want).abs() / bound).max().item()
 
 
 # ---------------------------------------------------------------- many requests
