@@ -391,6 +391,9 @@ typedef struct trimkv_paged_cache {
  * free_pages: int32 [n_pages], a stack of free pages of which the first *free_count are live.  Pages given back are pushed in
  * (request, page) order, then the missing ones are popped in (request, page) order; memory above the top is left as it is.
  * Where the table holds no page (E_ARG), -1 is pushed; who pops it gets -1 in its table and slots (E_ARG again).
+ * It knows no counts of holders: every page of the table has one holder here.  Once rows share pages (trimkv_paged_share), or a program keeps
+ * page_refs for them, only trimkv_paged_share and trimkv_paged_compact may change that table: this call would push a shared page on the stack
+ * once for each holder, let a row write into a partly filled page that others hold, and leave page_refs stale.
  * Table entries behind a request's last page are left as they are.
  * Written: block_table, free_pages, free_count_out [1], lens_out [n_req] (= new_lens), cu_new [n_req + 1], and for each of
  * the max_tokens places slot_map (page x 64 + row) and positions (may be NULL), -1 behind the last token.  free_count_out may
@@ -501,6 +504,8 @@ TRIMKV_API trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cach
  * paper, whose budgeted cache drops entries by itself.)
  *   page_refs    int32 [n_pages]: how many rows of the table hold each page, and whatever the program counts beside them; 0 for free
  *                ones.  A prefix that no request is using right now is kept by a row of its own.
+ *                Counts of a table that trimkv_paged_plan has made are 1 for each page that a row holds; from then on that call is no
+ *                longer for this table.
  * Outputs are apart from inputs: table_out is another array than block_table; refs_out may be page_refs, free_out free_pages and
  * free_count_out free_count; otherwise no output overlaps an input.  Table entries behind a row's last page are neither read nor written.
  * What moves: move_src, move_dst int32 [max_moves], *move_count pairs of slots (page x 64 + row) in ascending order of row and entry, -1
@@ -527,7 +532,9 @@ TRIMKV_API trimkv_status trimkv_paged_share(int32_t n_req, const int32_t* source
  * trimkv_select_topk writes them; bits from lens[r] on are ignored), in their order.  Pages up to the first dropped entry's stay;
  * what is kept from there on is listed to be moved to fresh pages, and the old pages are let go of; nothing moves if only a row's end
  * is dropped.  Fresh pages come from the stack as it was (popped in (row, place) order), pages whose count becomes 0 are pushed after that.
- * page_refs, refs_out: both NULL where no page has two holders. */
+ * page_refs, refs_out: both NULL where no page has two holders.
+ * Entries are renumbered: a row that keeps n entries goes on at position n.  So positions of later calls, and a window, count the entries that are
+ * left, not the tokens they were; a program that rotates keys or queries by the token's number keeps that number itself. */
 TRIMKV_API trimkv_status trimkv_paged_compact(int32_t n_req, const int32_t* lens, const uint64_t* keep_bits, const int32_t* block_table,
                                    int32_t* table_out, int32_t table_width, const int32_t* page_refs, int32_t* refs_out,
                                    const int32_t* free_pages, int32_t* free_out, int32_t n_pages, const int32_t* free_count,

@@ -510,7 +510,8 @@ def paged_plan(old_lens, keep_lens, new_lens, block_table, free_pages, free_coun
                positions=None, status=None):
     """Block tables and slot maps from request lengths (trimkv_paged_plan).  int32 tensors: old_lens, keep_lens (or None),
     new_lens, lens_out [R], block_table [R, W], free_pages [n_pages], free_count and free_count_out [1], cu_new [R + 1],
-    slot_map and positions (or None) [max_tokens], status [1].  Works in place; returns nothing."""
+    slot_map and positions (or None) [max_tokens], status [1].  Works in place; returns nothing.  Every page has one holder here: a
+    table whose rows share pages, or for which page_refs are kept, is changed by paged_share and paged_compact alone."""
     n = old_lens.get_device()
     if n < 0:
         raise ValueError("expected a CUDA tensor")
@@ -676,7 +677,8 @@ def paged_share(source, old_lens, keep_lens, new_lens, block_table, table_out, p
                 free_count_out, lens_out, cu_new, slot_map, positions, move_src, move_dst, move_count, status=None):
     """Forks, growth and release of rows that share pages (trimkv_paged_share).  int32 tensors: source, old_lens, keep_lens, new_lens,
     lens_out [R], block_table and table_out [R, W], page_refs, refs_out, free_pages, free_out [n_pages], free_count, free_count_out,
-    move_count, status [1], cu_new [R + 1], slot_map and positions (or None) [max_tokens], move_src and move_dst [max_moves]."""
+    move_count, status [1], cu_new [R + 1], slot_map and positions (or None) [max_tokens], move_src and move_dst [max_moves].  A table of
+    paged_plan's goes over with counts of 1; paged_plan is not called on it any more."""
     n = old_lens.get_device()
     if n < 0:
         raise ValueError("expected a CUDA tensor")
@@ -694,7 +696,8 @@ def paged_share(source, old_lens, keep_lens, new_lens, block_table, table_out, p
 def paged_compact(lens, keep_bits, block_table, table_out, page_refs, refs_out, free_pages, free_out, free_count, free_count_out, lens_out,
                   move_src, move_dst, move_count, status=None):
     """Rows without the entries whose bits in keep_bits (int64 [R, W]) are clear (trimkv_paged_compact).  int32 tensors as in
-    paged_share; page_refs and refs_out may both be None."""
+    paged_share; page_refs and refs_out may both be None where no page has two holders.  Entries are renumbered: positions of later calls, and
+    windows, count those that are left."""
     n = lens.get_device()
     if n < 0:
         raise ValueError("expected a CUDA tensor")
