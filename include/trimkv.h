@@ -474,8 +474,9 @@ typedef struct trimkv_paged4_cache {
 
 /* Rounds k and v (dtype TRIMKV_DTYPE_BF16 or TRIMKV_DTYPE_F32; rows and strides as in trimkv_paged_append) into slot slot_map[t] of the
  * cache; -1 skips a token; no slot is given twice.  With x' = x 2^-shift: scale = e4m3(max |x'| / 6), the quotient in fp32, to nearest even, at most 448;
- * code = e2m1(x' / scale), to nearest, ties to the code whose mantissa is 0, at most 6 in magnitude; codes 0 where the
- * scale is 0.  A block that holds a NaN becomes NaN; infinities become the largest value. */
+ * code = e2m1(x' / scale), to nearest, ties to the code whose mantissa is 0, at most 6 in magnitude; magnitude 0 where the
+ * scale is 0.  A code has the sign of its x, also where its magnitude is 0.  A block that holds a NaN gets a NaN scale, its codes say nothing;
+ * infinities become the largest value. */
 TRIMKV_API trimkv_status trimkv_paged4_append(const trimkv_paged4_cache* cache, int32_t dtype, int64_t n_tokens, const void* k, int64_t k_stride,
                                    const void* v, int64_t v_stride, const int32_t* slot_map, int32_t* status, void* stream);
 

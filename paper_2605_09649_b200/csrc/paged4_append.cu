@@ -1,8 +1,8 @@
 // Rounding of keys and values into the 4-bit paged cache, and reading them back.
 //
 // Append.  A block is 16 channels x of one entry and KV head, x' = x 2^-shift.  Its scale is s = e4m3(max |x'| / 6) (to nearest
-// even, at most 448), its codes are e2m1(x' / s): nearest, ties to the even code, at most 6; all codes 0 where s = 0, s = NaN where
-// the block holds one.  A thread takes two blocks: it reads 32 channels and writes 16 bytes of codes and two of scales.
+// even, at most 448), its codes are e2m1(x' / s): nearest, ties to the even code, at most 6; magnitude 0 where s = 0, the sign always that of x; s = NaN
+// where the block holds one.  A thread takes two blocks: it reads 32 channels and writes 16 bytes of codes and two of scales.
 //   The quotient.  bf16: x' has 8 significant bits, the halfway points m s (m of three bits, s of four) have 7, so a quotient is
 // a halfway point or at least 2^-9 of it away; x' times the rounded reciprocal of s is off by 2^-22 and, rounded to 16
 // bits, is the halfway point itself where the quotient is one.  fp32: x' is compared with the seven halfway points m s,

@@ -5,9 +5,10 @@ import random
 import pytest
 import torch
 
-from test_gpu_paged4 import DEV, check, ints, run
-from util_paged import queries
-from util_paged4 import Cache4, attention, values
+from paper_2605_09649_b200 import binding
+from test_gpu_paged4 import DEV, check, empty_cache, hard_values, ints, run
+from util_paged import PAGE, queries
+from util_paged4 import Cache4, attention, quantise, values
 
 pytestmark = pytest.mark.gpu
 KINDS = [(torch.bfloat16, 1), (torch.float32, 1), (torch.bfloat16, 40), (torch.float32, 40)]      # (bf16, 40): the chunk kernel
@@ -75,6 +76,31 @@ def test_weights_that_fp16_rounds_coarsely(dtype, new, bits, tail):
     want, bound = attention(c.k, c.v, q, cu, [n], c.table, scale)
     bound = bound + n * (2.0 ** -tail - 2.0 ** -32)           # (every value is 1; `attention` counts 2^-32 for each entry)
     assert (want > 0).all() and ((out.double().cpu() - want).abs() <= bound).all(), ((out.double().cpu() - want).abs() / bound).max().item()
+
+
+# ---------------------------------------------------------------- codes to the bit
+
+@pytest.mark.parametrize("H,d,dtype", [(8, 128, torch.bfloat16), (2, 64, torch.float32), (3, 32, torch.bfloat16), (1, 256, torch.float32)])
+@pytest.mark.parametrize("shift", [0, -3, 40])
+def test_append_gives_the_defined_bytes(H, d, dtype, shift):
+    """Bytes, not values: a code has the sign of its channel also where it is 0, whether the channel is small, a negative zero, or its block's
+    scale is 0.  (Blocks with a NaN have a NaN scale; their codes say nothing.)"""
+    T, n_pages = 100, 2
+    arrays, cache = empty_cache(n_pages, H, d, [shift] * H)
+    x = hard_values(T, H, d, dtype, seed=5)
+    x[3, :, ::5] *= -0.0
+    x[4] = -2.0 ** -100
+    x[5] = -0.0
+    binding.paged4_append(cache, x.to(DEV), x.to(DEV), ints(range(T)))
+    codes, scale = quantise(x, torch.tensor([shift] * H))
+    want = (codes & 7) + 8 * torch.signbit(x).long()
+    real = (scale != 127).repeat_interleave(16, -1)
+    for kv in range(2):
+        got, got_s = (a.cpu().transpose(1, 2).reshape(n_pages * PAGE, H, -1)[:T].long() for a in arrays[2 * kv:2 * kv + 2])
+        got = torch.stack((got & 15, got >> 4), -1).flatten(-2)
+        assert torch.equal(got_s, scale)
+        assert torch.equal(got[real], want[real])
+    assert ((scale == 0).repeat_interleave(16, -1) & (want == 8)).any() and ((scale > 0).repeat_interleave(16, -1) & (want == 8)).any()
 
 
 # ---------------------------------------------------------------- many requests
