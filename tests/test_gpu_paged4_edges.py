@@ -103,6 +103,15 @@ def test_append_gives_the_defined_bytes(H, d, dtype, shift):
     assert ((scale == 0).repeat_interleave(16, -1) & (want == 8)).any() and ((scale > 0).repeat_interleave(16, -1) & (want == 8)).any()
 
 
+# ---------------------------------------------------------------- head sizes of fp32 queries
+
+@pytest.mark.parametrize("H,g,d", [(2, 4, 32), (1, 3, 96), (2, 2, 128), (1, 2, 160), (1, 4, 256)])
+def test_fp32_head_sizes(H, g, d):
+    check([1, 31, 64, 65, 200, 1500], [1] * 6, H, g, d, torch.float32, seed=33)
+    check([5, 40, 0, 64, 700, 130], [5, 3, 0, 0, 6, 1], H, g, d, torch.float32, seed=34)
+    check([130, 300, 90], [130, 77, 1], H, g, d, torch.float32, window=40, seed=35)
+
+
 # ---------------------------------------------------------------- many requests
 
 @pytest.mark.parametrize("requests", [33, 480, 481, 1100])
