@@ -52,7 +52,7 @@ trimkv_status trimkv_paged4_append(const trimkv_paged4_cache* cache, int32_t dty
     Paged4View c;
     const trimkv_status s = check_cache4(cache, dtype, &c);
     if (s != TRIMKV_OK) return s;
-    if (n_tokens < 0 || n_tokens * c.pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
+    if (n_tokens < 0 || n_tokens > (1LL << 30) / c.pv.H) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
     if (n_tokens == 0) return TRIMKV_OK;
     const int elt = dtype == TRIMKV_DTYPE_BF16 ? 2 : 4;
     if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
@@ -67,7 +67,7 @@ trimkv_status trimkv_paged4_read(const trimkv_paged4_cache* cache, int32_t dtype
     Paged4View c;
     const trimkv_status s = check_cache4(cache, dtype, &c);
     if (s != TRIMKV_OK) return s;
-    if (n_slots < 0 || n_slots * c.pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_slots x kv_heads must be in [0, 2^30]");
+    if (n_slots < 0 || n_slots > (1LL << 30) / c.pv.H) return refuse(TRIMKV_E_ARG, "n_slots x kv_heads must be in [0, 2^30]");
     if (n_slots == 0) return TRIMKV_OK;
     if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
     return done(launch_paged4_read(c, dtype == TRIMKV_DTYPE_BF16, (int)n_slots, slot_map, k, v, status, (cudaStream_t)stream), "read");

@@ -56,7 +56,7 @@ trimkv_status tkv::paged_check_batch(const PagedView& pv, int is_bf16, size_t ne
     if (n_req < 1 || n_req > PAGED_MAX_REQ) return refuse(TRIMKV_E_ARG, "n_req must be in [1, %d]", PAGED_MAX_REQ);
     if (table_width < 1 || table_width > TRIMKV_PAGED_MAX_WIDTH) return refuse(TRIMKV_E_ARG, "table_width must be in [1, %d]", TRIMKV_PAGED_MAX_WIDTH);
     if (q_heads < pv.H || q_heads % pv.H || q_heads / pv.H > 128) return refuse(TRIMKV_E_ARG, "q_heads must be kv_heads times 1 to 128");
-    if (n_tokens < 0 || n_tokens * q_heads > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x q_heads must be in [0, 2^30]");
+    if (n_tokens < 0 || n_tokens > (1LL << 30) / q_heads) return refuse(TRIMKV_E_ARG, "n_tokens x q_heads must be in [0, 2^30]");
     if (n_tokens > 0) {
         if (!q || !out || !ok16(q) || !ok16(out)) return refuse(TRIMKV_E_ARG, "q and out must be non-NULL and 16-byte aligned");
         if (q_stride < (int64_t)q_heads * pv.d || q_stride > (1LL << 31) || (q_stride * (is_bf16 ? 2 : 4)) % 16)
@@ -112,7 +112,7 @@ trimkv_status trimkv_paged_append(const trimkv_paged_cache* cache, int64_t n_tok
     PagedView pv;
     const trimkv_status s = check_cache(cache, &pv);
     if (s != TRIMKV_OK) return s;
-    if (n_tokens < 0 || n_tokens * pv.H > (1LL << 30)) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
+    if (n_tokens < 0 || n_tokens > (1LL << 30) / pv.H) return refuse(TRIMKV_E_ARG, "n_tokens x kv_heads must be in [0, 2^30]");
     if (n_tokens == 0) return TRIMKV_OK;
     const int is_bf16 = cache->kv_dtype == TRIMKV_DTYPE_BF16, elt = is_bf16 ? 2 : 4;
     if (!k || !v || !slot_map || !ok16(k) || !ok16(v) || !ok4(slot_map) || !ok4(status)) return refuse(TRIMKV_E_ARG, "k, v and slot_map must be non-NULL; k and v 16-byte aligned");
