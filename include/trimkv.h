@@ -533,7 +533,8 @@ TRIMKV_API trimkv_status trimkv_paged_share(int32_t n_req, const int32_t* source
  * trimkv_select_topk writes them; bits from lens[r] on are ignored), in their order.  Pages up to the first dropped entry's stay;
  * what is kept from there on is listed to be moved to fresh pages, and the old pages are let go of; nothing moves if only a row's end
  * is dropped.  Fresh pages come from the stack as it was (popped in (row, place) order), pages whose count becomes 0 are pushed after that.
- * page_refs, refs_out: both NULL where no page has two holders.
+ * page_refs, refs_out: both NULL where no page has two holders.  (Where one has, it comes back twice; E_ARG, after the fact, if the stack has no
+ * room for all that comes back.)
  * Entries are renumbered: a row that keeps n entries goes on at position n.  So positions of later calls, and a window, count the entries that are
  * left, not the tokens they were; a program that rotates keys or queries by the token's number keeps that number itself. */
 TRIMKV_API trimkv_status trimkv_paged_compact(int32_t n_req, const int32_t* lens, const uint64_t* keep_bits, const int32_t* block_table,

@@ -502,7 +502,11 @@ paged_compact_kernel(ShareArgs a, const u64* keep_bits) {
         }
     });
     for (int r = gt; r < R; r += GT) a.lens_out[r] = s_len[r];
-    if (gt == 0) *a.free_count_out = min(fc - taken + s_back[cut.tasks], a.n_pages);
+    if (gt == 0) {                            // more than there are pages: some have two holders, and nobody counted
+        const int live = fc - taken + s_back[cut.tasks];
+        *a.free_count_out = min(live, a.n_pages);
+        wrong |= live > a.n_pages;
+    }
     // ---- the entries that move: a warp takes up to 32 words of a row, a lane describes one; then a lane looks for the word and bit of an
     // entry, or, of many, all lanes list those of a word after another
     const int span = (int)min(32ll, max(2ll, ((long long)R * W + SH_WARPS - 1) / SH_WARPS)), per_row = (W + span - 1) / span;

@@ -94,3 +94,11 @@ def test_a_table_of_the_plan_goes_over_with_counts_of_one():
         assert status == 0 and [row[:pages(n)] for row, n in zip(got["table"], new)] == want[0] and got["refs"] == want[1]
         assert got["free"][:got["count"]] == want[3] and got["positions"] == want[6 + 1] and got["moves"] == len(want[8])
         rows, refs, stack, lens = got["table"], got["refs"], got["free"][:got["count"]], got["lens"]
+
+
+def test_compact_says_when_more_pages_come_back_than_there_are():
+    """Two rows hold a page without counts: it comes back twice, and the stack has no room for the second."""
+    got, st = run_compact([64, 64], [[], []], [[3], [3]], None, [0, 1, 2], 4, 1, 0)
+    assert st == binding.E_ARG and got["count"] == 4 and got["free"] == [0, 1, 2, 3] and got["lens"] == [0, 0]
+    got, st = run_compact([64, 64], [[], []], [[3], [2]], None, [0, 1], 4, 1, 0)
+    assert st == 0 and got["count"] == 4 and got["free"] == [0, 1, 3, 2]
