@@ -26,7 +26,8 @@ struct Paged4View {
 };
 
 __device__ __forceinline__ int p4_shift(const Paged4View& c, int kv, int h) {
-    return c.shift[kv] ? max(-P4_MAX_SHIFT, min(P4_MAX_SHIFT, c.shift[kv][h])) : 0;
+    const int32_t* shift = kv ? c.shift[1] : c.shift[0];      // (an index known only at run time would copy the view to local memory)
+    return shift ? max(-P4_MAX_SHIFT, min(P4_MAX_SHIFT, shift[h])) : 0;
 }
 __device__ __forceinline__ float p4_pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // 2^e, -126 <= e <= 127
 
