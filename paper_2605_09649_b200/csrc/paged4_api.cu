@@ -97,7 +97,15 @@ trimkv_status trimkv_paged4_attention(const trimkv_paged4_cache* cache, int32_t 
     const cudaStream_t st = (cudaStream_t)stream;
     const PagedWork w = carve4(workspace, P4_SHARED_BYTES, P4_WORKER_ROWS, c.pv.d);
     // Requests of up to 32 rows (tokens x query heads of a KV head) go to the warp kernel, larger ones to the tcgen05 kernel, where there is
-    // one.  max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
+    // one.  The warp kernel's time grows with every 16 rows, the other's stays to 128; where they cross depends on the lengths, which the host does
+    // not see.  Warp kernel against tcgen05 at 32, 48 and 64 rows, us:
+    //   32 requests over 2.3 K entries, 8 KV heads of 128    68, 90, 128    110, 111, 113
+    //   8 over 16 K, 8 of 128                               103, 142, 181    153, 154, 155
+    //   1 over 32 K, 8 of 128                                54, 61, 69       60, 61, 61
+    //   4 over 16 K, 8 of 64                                 44, 54, 66       77, 78, 78
+    //   16 over 1 K, 2 of 128 (a unit's pages to one warp)   42, 42, 42       22, 23, 23
+    // So 33 to 48 rows lose up to 24 us (a quarter, with heads of 64 a third) over many long requests, and 9 to 32 rows 20 us over few short ones.
+    // max_new may be wrong: every kernel takes any request, and where both run the device sorts them.
     const long long most = (long long)(max_new > 0 ? max_new : n_tokens) * pb.g;
     const int tile = most <= 8 || (c.pv.d > PAGED_TC_HEAD && most <= PAGED_WARP_ROWS) ? 8 : 16;
     cudaError_t e = cudaSuccess;

@@ -7,11 +7,11 @@
 // a halfway point or at least 2^-9 of it away; x' times the rounded reciprocal of s is off by 2^-22 and, rounded to 16
 // bits, is the halfway point itself where the quotient is one.  fp32: x' is compared with the seven halfway points m s,
 // which are exact.
-// Bound by the copy, 2 x 2 bytes per channel in, 2 x 0.5625 out: 12 K tokens of 8 heads of 128 in 16.1 us, 64 MB, 0.61 of the measured copy rate; 32 tokens in
-// 2.4 us.  (Half a block per thread, so that every access is contiguous: 29 us, the quotients are computed twice.)
+// 2 x 2 bytes per channel in, 2 x 0.5625 out: 12 K tokens of 8 heads of 128 in 15.7 us, 64 MB, 0.62 of the measured copy rate; fp32 30.8 us, 0.57; 32 tokens
+// in 2.4 us.  (Half a block per thread, so that every access is contiguous: 29 us, the quotients are computed twice.)
 //
-// Read.  The way back: every value is exact in bf16 (6 significant bits) and fp32.  12 K tokens in 15.1 us, four items' loads in flight per thread and whole
-// sectors stored (one item and 16-byte stores: 20.8).
+// Read.  The way back: every value is exact in bf16 (6 significant bits) and fp32.  12 K tokens in 11.0 us, 0.89 of the copy rate: four items' loads in
+// flight per thread and whole sectors stored.  fp32 37.4 us, 0.47: it stores half a sector at a time.
 #include <algorithm>
 
 #include "paged4.cuh"
