@@ -14,8 +14,8 @@
 // 16 entries of heads of 128 cost a warp 270 instructions, 122 of them on the ALU (64 conversions) and 95 on the FMA pipe (64 products
 // with scales).
 //
-// What bounds it: 302 MB of a decode step (8 requests of 32 K, 8 x 4 heads of 128) take 73 us, 19 of which no length changes (launch, table of
-// requests, first pages, join) and the rest 5.2 TB/s, 0.8 of the copy rate; without the conversions, or without the products with
+// What bounds it: 302 MB of a decode step (8 requests of 32 K, 8 x 4 heads of 128) take 73 us, 16 of which no length changes (launch, table of
+// requests, first pages, join) and the rest 5.3 TB/s, 0.8 of the copy rate; without the conversions, or without the products with
 // scales, it takes 9 us less.  Steps: 8 warps that fetch for themselves 121 us, 16 of them 100, head size known at compile time 82, 11 warps fed by
 // another 77.6, 14 fed by two 77.1, descriptions ahead of the copies and a join of 296 blocks 74.5.
 //
@@ -35,7 +35,10 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr unsigned W4_IDLE_LIMIT = 1u << 22, W4_NAP = 20;             // rounds without progress, and ns between them
-constexpr int W4_JOIN_STEPS = 16;                                     // what a join costs, in pages
+// Pages up to which units stay whole (paged_choose_whole), and up to which a table's width alone tells the host that no join is needed, whose launch is 3.5 us.
+// A lone warp takes 1.75 us a page.  16 against 4, us: 9 pages 20.9, 19.5 (32 requests of 8 heads of 128), 19.7, 24.2 (64, heads of 64), 28.3, 29.7
+// (32 x 5 tokens); 16 pages 33.2, 21.5; 30.6, 26.2; 44.9, 39.4; and 33.0, 16.6 for 8 requests.  So it is kind to many requests and dear to few.
+constexpr int W4_JOIN_STEPS = 16;
 constexpr float W4_RESCALE_STEP = 8.0f, W4_OFFSET = 7.0f;             // log2: how far the reference may lag; what the weights are scaled by
 
 // A tile that a warp is to read, and the stretch of a unit that it belongs to.
