@@ -2,8 +2,8 @@
 //
 // move_src[i] -> move_dst[i] (page x 64 + row), for each of up to 128 arrays and each of its heads in one launch.  Pairs come in ascending
 // runs, so a block takes 64 pairs of four heads, whose rows mostly lie side by side on both ends, and its threads take 16
-// bytes each (less where a row is not a multiple of 16).  Bound by the copy: 32 rows on average of 32 requests in 32 layers of 8 heads of 128 (265 MB) take 50 us,
-// 0.81 of the measured copy rate.  (A head a block, its array looked for and a division for every 16 bytes: 70 us.)
+// bytes each (less where a row is not a multiple of 16).  Bound by the copy: 32 rows on average of 32 requests in 32 layers of 8 heads of 128 (282 MB) take 49.5 us,
+// 0.87 of the measured copy rate.  (A head a block, its array looked for and a division for every 16 bytes: 70 us.)
 //
 // Bounds: pages whose last row (63) was a destination get the channelwise smallest and largest of their 64 keys, in a
 // second launch that reads them from L2.

@@ -50,3 +50,11 @@ def test_copies_of_the_4_bit_decode_kernel_land_before_their_warp_leaves():
             waits.append((depth, block[block.rfind(";", 0, block.rfind("for (", 0, i)) + 1:i]))
     assert len(waits) == 1 and waits[0][0] == 1               # of the block itself, under no condition
     assert "if" not in waits[0][1] and "for (unsigned k" in waits[0][1]
+
+
+def test_no_paged_kernel_promises_that_its_memory_stays():
+    """All files of the paged caches, whatever their launch bounds look like: a kernel that is placed before the one ahead of it has finished must
+    not promise the compiler that memory does not change."""
+    files = [f for f in sorted(os.listdir(CSRC)) if f.startswith("paged") and f.endswith((".cu", ".cuh"))]
+    assert {"paged4_attention.cu", "paged4_attention_tc.cu", "paged4_append.cu", "paged_share.cu", "paged_move.cu"} <= set(files)
+    assert [f for f in files if "__restrict__" in without_comments(open(os.path.join(CSRC, f)).read())] == []
